@@ -151,7 +151,7 @@ def _cache(case, gen, n_blocks):
 def prepare(case, seed):
     gen = torch.Generator(device=DEV)
     gen.manual_seed(seed)
-    state = {"op": case["op"], "case": case}
+    state = {"op": case["op"], "case": case, "status": torch.zeros(1, dtype=torch.int32, device=DEV)}
     if case["op"] in ("plan", "append"):
         b = case["block"]
         cached, added = _lengths(case)
@@ -326,16 +326,16 @@ def run(state):
     if own:
         from paper_2311_10359_amd import binding
         if s["op"] == "plan":
-            plan = binding.fikit_cache_plan(s["cached"], s["added"], s["n_tokens"], s["block"], s["table"], s["free"])
+            plan = binding.fikit_cache_plan(s["cached"], s["added"], s["n_tokens"], s["block"], s["table"], s["free"], s["status"])
             return {"table": s["table"], "lengths": plan.lengths, "offsets": plan.token_offsets, "slots": plan.slots, "pieces": plan.pieces, "counts": plan.counts}
         if s["op"] == "append":
-            binding.fikit_cache_append(s["k_cache"], s["v_cache"], s["k_exp"], s["v_exp"], s["k"], s["v"], s["pieces"])
+            binding.fikit_cache_append(s["k_cache"], s["v_cache"], s["k_exp"], s["v_exp"], s["k"], s["v"], s["pieces"], s["status"])
             return {"k": s["k_cache"], "v": s["v_cache"], "k_exp": s["k_exp"], "v_exp": s["v_exp"]}
         if s["op"] == "decode":
             got = binding.fikit_cache_attention(s["q"], s["k_cache"], s["v_cache"], s["k_exp"], s["v_exp"], s["table"], s["lens"], s["scale"],
-                                                max_length=s["longest"])
+                                                s["status"], max_length=s["longest"])
             return {"out": got.out, "lse": got.lse}
-        got = binding.fikit_prompt_attention(s["q"], s["k"], s["v"], s["offsets"], s["scale"])
+        got = binding.fikit_prompt_attention(s["q"], s["k"], s["v"], s["offsets"], s["scale"], s["status"])
         return {"out": got.out, "lse": got.lse}
     if s["op"] == "plan":
         return _plan_plain(s)
