@@ -36,12 +36,12 @@
  *     fikit_gapfill_static).  Inputs are left
  *     untouched.
  *   - All work is enqueued on `hip_stream` (a hipStream_t passed as void*; NULL = the default
- *     stream).  Every call but fikit_gapfill_static waits until its work there is done
- *     before it returns, so outputs and the returned status are final on return, for every stream,
+ *     stream).  Every call but fikit_gapfill_static and the attention calls of a language model
+ *     service (fikit_cache_*, fikit_prompt_attention) waits until its work there is done before it returns, so outputs and the returned status are final on return, for every stream,
  *     copy and thread.
  *   - Return value: FIKIT_OK or a negative fikit_status.  Nothing aborts or throws.  After an
  *     error the contents of the output buffers are unspecified.
- *   - Everything is integer arithmetic (nanoseconds, counts); results are exact.
+ *   - Everything but the attention calls is integer arithmetic (nanoseconds, counts); results are exact.
  *   - Limits: n_records, n_ids < 2^32 - 2^24.  Timestamps must be such that end - start and
  *     next start - end fit in int64, and a task's predicted timeline (sum of p50 values over
  *     its launches) fits in int64.
@@ -105,8 +105,9 @@ typedef enum fikit_status {
                                      (fikit_set_wait_limit)                                      */
   FIKIT_UNSUPPORTED = -7,         /* fikit_prio_fill: a scenario whose list entries and launches
                                      together number 2^32 or more                                 */
-  FIKIT_TOO_LARGE = -8            /* fikit_gapfill_static: more launches or tasks than its built-in
+  FIKIT_TOO_LARGE = -8,           /* fikit_gapfill_static: more launches or tasks than its built-in
                                      scratch buffer holds                                          */
+  FIKIT_CACHE_FULL = -9           /* fikit_cache_plan: more blocks needed than are free             */
 } fikit_status;
 
 /* Bytes of device workspace fikit_profile needs for these sizes (0 on size overflow). */
@@ -413,6 +414,153 @@ int fikit_profile_merge(const fikit_row* d_rows_a, const uint64_t* d_task_row_of
                         const fikit_row* d_rows_b, const uint64_t* d_task_row_offsets_b, uint32_t n_tasks,
                         fikit_row* d_rows_out, uint64_t row_capacity, uint64_t* d_task_row_offsets_out,
                         uint64_t* h_n_rows, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---- tasks of a language model service --------------------------------------------------------------------------
+ *
+ * The attention part of such a service, as kernels for the card whose idle times are evaluated above: a prompt (long launches
+ * that nobody waits for one by one, a low-priority task) and a decode step (short launches with idle time behind each, a
+ * high-priority task) over one cache.  Their launches, measured, are what fikit_profile and fikit_gapfill take.
+ *
+ * Four calls, in the order of a step:
+ *   fikit_cache_plan        from the requests' lengths: new blocks, where each new token goes, and the pieces that the blocks
+ *                           cut the new tokens into
+ *   fikit_prompt_attention  causal attention of packed prompts, on keys and values that are not in the cache yet
+ *   fikit_cache_append      puts the new tokens' keys and values into the cache
+ *   fikit_cache_attention   attention of one new token per request over the cache
+ *
+ * They allocate nothing, wait for nothing and create nothing: each enqueues its kernels on hip_stream and returns, so they can
+ * be captured into a HIP graph.  The return value covers what the host can see (INVALID_ARG, UNSUPPORTED, WORKSPACE_TOO_SMALL,
+ * HIP_ERROR).  What depends on data is reported through d_status, an int32 device word that the caller has set to FIKIT_OK: a
+ * call that finds an error (a negative length, offsets that are not monotone or end elsewhere, a block outside the cache, ...)
+ * writes its status there and reads and writes nothing outside the buffers it was given; a call that finds another value than
+ * FIKIT_OK there does nothing.  So a plan that has failed stops the calls behind it, and one look at the word, when the caller
+ * waits anyway, covers all calls since it was set.  After an error the contents of the output buffers are unspecified.
+ *
+ * The cache.  Keys and values are held as E4M3 codes (OCP, 8 bits, largest value 448) with one power-of-two scale for each block
+ * of tokens and head: a value is code * 2^(x - 127), x the exponent byte of its block and head, 1 .. 254.  A power of two makes
+ * scaling exact, so a value has one rounding, and rounding held codes again where a block's scale grows stays exact but for
+ * the codes' last bits.  Block b, head h: block_tokens rows of head_dim codes at ((b * kv_heads + h) * block_tokens) * head_dim.
+ */
+typedef enum fikit_value_type {
+  FIKIT_BF16 = 0,
+  FIKIT_F16 = 1
+} fikit_value_type;
+
+/* Vectors of head_dim 16-bit values, one per token and head; token t, head h at d_data + t * token_stride + h * head_stride
+ * (strides in values, multiples of 8; d_data 16-byte aligned), so that they may lie in one product's output. */
+typedef struct fikit_vectors {
+  const void* d_data;
+  uint64_t token_stride;
+  uint64_t head_stride;
+} fikit_vectors;
+
+typedef struct fikit_cache {
+  uint8_t* d_k;            /* [n_blocks][kv_heads][block_tokens][head_dim] codes, 16-byte aligned */
+  uint8_t* d_v;            /* the same of the values                                              */
+  uint8_t* d_k_exp;        /* [n_blocks][kv_heads] exponent bytes                                 */
+  uint8_t* d_v_exp;
+  uint32_t n_blocks;
+  uint32_t kv_heads;
+  uint32_t block_tokens;   /* 16, 32, 64, 128 or 256 */
+  uint32_t head_dim;       /* 64 or 128              */
+} fikit_cache;
+
+/* New tokens that lie one behind the other in one block.  An entry that is not used holds -1 in all four. */
+typedef struct fikit_piece {
+  int32_t block;
+  int32_t first_token;   /* among the new tokens of all requests */
+  int32_t at;            /* where the first one goes in the block; 0: the block holds nothing yet */
+  int32_t count;
+} fikit_piece;
+
+/* Most pieces that n_tokens new tokens of n_requests requests are cut into: the length of the list of pieces. */
+uint64_t fikit_cache_pieces(uint32_t n_tokens, uint32_t n_requests, uint32_t block_tokens);
+
+/* Bytes of device workspace fikit_cache_plan needs for these sizes. */
+size_t fikit_cache_plan_workspace_bytes(uint32_t n_requests);
+
+/*
+ * The plan of a step.  Request r has d_cached[r] tokens in the cache and gets d_added[r] more (either may be 0); its new tokens
+ * follow those of request r - 1 in the packed inputs.
+ *
+ *   n_tokens         sum of d_added (a mismatch is INVALID_ARG), < 2^31.
+ *   d_block_table    [n_requests][table_width] in and out: the blocks of a request in order.  The first ceil(cached /
+ *                    block_tokens) entries of a row are read where new tokens go into the last of them; the entries behind
+ *                    them, up to ceil((cached + added) / block_tokens), receive new blocks.  Others stay as they are.
+ *   d_free           [n_free] blocks that nobody holds; they are taken from the front, in the order of the requests and, for
+ *                    one request, of its tokens.
+ *   d_lengths        [n_requests] receives cached + added.
+ *   d_token_offsets  [n_requests+1] receives where each request's new tokens begin.
+ *   d_slots          [n_tokens] receives where each new token goes, block * block_tokens + place in the block.  May be NULL.
+ *   d_pieces         [fikit_cache_pieces(...)] receives the pieces, in order; the rest is filled with -1.
+ *   d_counts         [2] receives the number of blocks taken and of pieces.
+ *   d_workspace      256-byte aligned, at least fikit_cache_plan_workspace_bytes(n_requests) bytes.
+ *
+ * Through d_status: INVALID_ARG (also: a request longer than its row of the table or than 2^31 - 1), CACHE_FULL if n_free blocks
+ * do not suffice; the table is unchanged then.
+ */
+int fikit_cache_plan(const int32_t* d_cached, const int32_t* d_added, uint32_t n_requests, uint32_t n_tokens,
+                     uint32_t block_tokens, int32_t* d_block_table, uint32_t table_width, const int32_t* d_free,
+                     uint32_t n_free, int32_t* d_lengths, int32_t* d_token_offsets, int64_t* d_slots,
+                     fikit_piece* d_pieces, int32_t* d_counts, int32_t* d_status, void* d_workspace,
+                     size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Puts the keys and values of n_tokens new tokens into the cache, a piece at a time (no block may be in two pieces).
+ *
+ * Per piece and head, keys and values apart: the exponent is the smallest x >= 1 with |value| <= 448 * 2^(x - 127) for the
+ * piece's finite values, or, if at > 0, the block's present one if that is larger.  A value's code is the nearest one (ties
+ * to even), NaN for what is not finite.  Where the exponent of a block with earlier tokens grows, their codes are rounded again
+ * to the new scale.  Codes behind the piece are left as they are.
+ *
+ * Through d_status: INVALID_ARG for a piece outside the block, the cache or the tokens.
+ */
+int fikit_cache_append(const fikit_cache* h_cache, const fikit_vectors* h_k, const fikit_vectors* h_v, uint32_t n_tokens,
+                       int32_t value_type, const fikit_piece* d_pieces, uint64_t n_pieces, int32_t* d_status,
+                       void* hip_stream);
+
+/* Bytes of device workspace fikit_cache_attention needs for these sizes (0: sizes it does not take). */
+size_t fikit_cache_attention_workspace_bytes(uint32_t n_requests, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim,
+                                             uint32_t max_length);
+
+/*
+ * Attention of one query per request over the request's tokens in the cache.  Query head h reads the keys and values of head
+ * h / (q_heads / kv_heads).  With s_j = scale * (q . k_j) over the request's tokens j:
+ *
+ *   d_out   [n_requests][q_heads][head_dim], of the queries' type: sum_j exp(s_j) v_j / sum_j exp(s_j)
+ *   d_lse   [n_requests][q_heads] float: log(sum_j exp(s_j)), natural; what joins results over parts of a context.  May be NULL.
+ *
+ * A request of length 0 gets zeros and -infinity.
+ *
+ *   h_q            one vector per request and head.
+ *   q_heads        a multiple of kv_heads.
+ *   d_block_table  [n_requests][table_width], d_lengths [n_requests]: as fikit_cache_plan leaves them; entries behind a
+ *                  request's length are not looked at, codes behind it change nothing.
+ *   max_length     no request is longer (else INVALID_ARG through d_status); how the work is cut up goes by it.
+ *   d_workspace    256-byte aligned, at least fikit_cache_attention_workspace_bytes(...) bytes.
+ *
+ * Products and sums are held in 32 bits, weights are rounded to the queries' type before they meet the values.  With
+ * FIKIT_F16 cached values are read as f16: beyond 65504 as infinite.
+ */
+int fikit_cache_attention(const fikit_cache* h_cache, const fikit_vectors* h_q, uint32_t q_heads, int32_t value_type, float scale,
+                          const int32_t* d_block_table, uint32_t table_width, const int32_t* d_lengths, uint32_t n_requests,
+                          uint32_t max_length, void* d_out, float* d_lse, int32_t* d_status, void* d_workspace,
+                          size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Causal attention of packed prompts: prompt p owns tokens d_offsets[p] .. d_offsets[p+1]-1 (int32, non-decreasing, first 0, last
+ * n_tokens, < 2^31), and each of its tokens sees those up to itself.  What follows a token, infinities and NaN included, changes
+ * nothing in its row.
+ *
+ *   h_q, h_k, h_v  vectors of q_heads, kv_heads and kv_heads heads; q_heads a multiple of kv_heads.
+ *   head_dim       64 or 128.
+ *   d_out          [n_tokens][q_heads][head_dim], of the inputs' type; d_lse [n_tokens][q_heads] float or NULL; as in
+ *                  fikit_cache_attention.
+ */
+int fikit_prompt_attention(const fikit_vectors* h_q, const fikit_vectors* h_k, const fikit_vectors* h_v, uint32_t q_heads,
+                           uint32_t kv_heads, uint32_t head_dim, int32_t value_type, float scale, const int32_t* d_offsets,
+                           uint32_t n_prompts, uint32_t n_tokens, void* d_out, float* d_lse, int32_t* d_status,
+                           void* hip_stream);
 
 const char* fikit_status_string(int status);
 int fikit_version(void);

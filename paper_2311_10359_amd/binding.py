@@ -6,6 +6,7 @@ library is missing or cannot be loaded, importing the functions fails loudly.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import NamedTuple, Optional
@@ -24,6 +25,7 @@ FIKIT_UNKNOWN_ID = -5
 FIKIT_HIP_ERROR = -6
 FIKIT_UNSUPPORTED = -7
 FIKIT_TOO_LARGE = -8
+FIKIT_CACHE_FULL = -9
 FIKIT_STATIC_MAX_IDS = 1 << 20
 FIKIT_STATIC_MAX_TASKS = 16384
 FIKIT_PREDICT_P50, FIKIT_PREDICT_MEAN = 0, 1
@@ -32,7 +34,8 @@ EXPORTS = ("fikit_profile_workspace_bytes", "fikit_profile", "fikit_gapfill_work
            "fikit_gapfill", "fikit_profile_gapfill_workspace_bytes", "fikit_profile_gapfill", "fikit_gapfill_static", "fikit_measure_workspace_bytes", "fikit_measure", "fikit_replay_workspace_bytes",
            "fikit_gapfill_replay", "fikit_prio_fill_workspace_bytes", "fikit_prio_fill", "fikit_pairing_workspace_bytes",
            "fikit_pairing_best", "fikit_profile_merge_workspace_bytes", "fikit_profile_merge", "fikit_status_string", "fikit_version", "fikit_set_wait_limit",
-           "fikit_trace_enable", "fikit_trace_read")
+           "fikit_trace_enable", "fikit_trace_read", "fikit_cache_pieces", "fikit_cache_plan_workspace_bytes", "fikit_cache_plan",
+           "fikit_cache_append", "fikit_cache_attention_workspace_bytes", "fikit_cache_attention", "fikit_prompt_attention")
 
 # Layout of a profile row as seen from numpy (128 bytes; see fikit_row in fikit.h).
 STATS_DTYPE = np.dtype([("count", "<u8"), ("sum", "<u8"), ("min", "<i8"), ("max", "<i8"),
@@ -58,6 +61,16 @@ class _GapfillParams(ctypes.Structure):
 class _ReplayParams(ctypes.Structure):
     _fields_ = [("margin_ns", ctypes.c_int64), ("min_gap_ns", ctypes.c_int64), ("feedback", ctypes.c_int32),
                 ("predictor", ctypes.c_int32)]
+
+
+class _Vectors(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_uint64), ("head_stride", ctypes.c_uint64)]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p),
+                ("n_blocks", ctypes.c_uint32), ("kv_heads", ctypes.c_uint32), ("block_tokens", ctypes.c_uint32),
+                ("head_dim", ctypes.c_uint32)]
 
 
 _lib = None
@@ -115,6 +128,22 @@ def load() -> ctypes.CDLL:
         lib.fikit_gapfill_replay.restype = ctypes.c_int
         lib.fikit_gapfill_replay.argtypes = [vp, vp, u32, vp, vp, vp, vp, vp, u64, ctypes.POINTER(_ReplayParams), vp,
                                              vp, vp, vp, vp, vp, sz, vp]
+        i32, f32 = ctypes.c_int32, ctypes.c_float
+        p_vec, p_cache = ctypes.POINTER(_Vectors), ctypes.POINTER(_Cache)
+        lib.fikit_cache_pieces.restype = u64
+        lib.fikit_cache_pieces.argtypes = [u32, u32, u32]
+        lib.fikit_cache_plan_workspace_bytes.restype = sz
+        lib.fikit_cache_plan_workspace_bytes.argtypes = [u32]
+        lib.fikit_cache_plan.restype = ctypes.c_int
+        lib.fikit_cache_plan.argtypes = [vp, vp, u32, u32, u32, vp, u32, vp, u32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        lib.fikit_cache_append.restype = ctypes.c_int
+        lib.fikit_cache_append.argtypes = [p_cache, p_vec, p_vec, u32, i32, vp, u64, vp, vp]
+        lib.fikit_cache_attention_workspace_bytes.restype = sz
+        lib.fikit_cache_attention_workspace_bytes.argtypes = [u32, u32, u32, u32, u32]
+        lib.fikit_cache_attention.restype = ctypes.c_int
+        lib.fikit_cache_attention.argtypes = [p_cache, p_vec, u32, i32, f32, vp, u32, vp, u32, u32, vp, vp, vp, vp, sz, vp]
+        lib.fikit_prompt_attention.restype = ctypes.c_int
+        lib.fikit_prompt_attention.argtypes = [p_vec, p_vec, p_vec, u32, u32, u32, i32, f32, vp, u32, u32, vp, vp, vp, vp]
         lib.fikit_status_string.restype = ctypes.c_char_p
         lib.fikit_status_string.argtypes = [ctypes.c_int]
         lib.fikit_version.restype = ctypes.c_int
@@ -540,6 +569,190 @@ def fikit_profile_merge(rows_a: torch.Tensor, task_row_offsets_a: torch.Tensor, 
     if st != FIKIT_OK:
         raise FikitError(st, "fikit_profile_merge", n_rows=n_rows.value)
     return MergedProfile(rows_out[: n_rows.value], task_row_offsets_out, n_rows.value)
+
+
+# ---- tasks of a language model service -----------------------------------------------------------
+# These calls enqueue their kernels and return; errors that depend on data are left in `status`, an int32 [1] device tensor
+# that starts as zero and that fikit_check_status looks at.  Tensors that a call allocates belong to the stream it runs on.
+_VALUE_TYPES = {torch.bfloat16: 0, torch.float16: 1}
+
+
+def fikit_check_status(status: torch.Tensor, what: str = "a call on this status word") -> None:
+    """Waits for the current stream and raises FikitError if a call has left an error in the word."""
+    st = int(status.item())
+    if st != FIKIT_OK:
+        raise FikitError(st, what)
+
+
+def _on(stream: Optional[torch.cuda.Stream], device):
+    """The stream of a call as (handle, context to allocate and launch in)."""
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+        if device.index == torch.cuda.current_device():
+            return stream.cuda_stream, contextlib.nullcontext()
+    return stream.cuda_stream, torch.cuda.stream(stream)
+
+
+def _vectors(t: torch.Tensor, what: str) -> _Vectors:
+    if t.dim() != 3 or t.stride(2) != 1:
+        raise ValueError(f"{what}: [tokens, heads, head_dim] with the last dimension dense")
+    return _Vectors(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _need(condition: bool, what: str) -> None:
+    if not condition:
+        raise ValueError(what)
+
+
+def _dense(t: torch.Tensor, dtype: torch.dtype, device, what: str) -> int:
+    _need(t.dtype == dtype and t.device == device and t.is_contiguous(), f"{what}: a dense {dtype} tensor on {device}")
+    return t.data_ptr()
+
+
+def _cache_of(k_cache, v_cache, k_exp, v_exp, device) -> _Cache:
+    """k_cache, v_cache: [blocks, kv heads, block tokens, head dim] codes (float8_e4m3fn or their bytes)."""
+    _need(k_cache.dim() == 4 and v_cache.shape == k_cache.shape, "k_cache, v_cache: [blocks, kv heads, block tokens, head dim]")
+    for t in (k_cache, v_cache):
+        _need(t.dtype in (torch.float8_e4m3fn, torch.uint8) and t.device == device and t.is_contiguous(),
+              f"k_cache, v_cache: dense float8_e4m3fn tensors on {device}")
+    n, h, b, d = k_cache.shape
+    _need(k_exp.shape == (n, h) and v_exp.shape == (n, h), "k_exp, v_exp: [blocks, kv heads]")
+    return _Cache(k_cache.data_ptr(), v_cache.data_ptr(), _dense(k_exp, torch.uint8, device, "k_exp"),
+                  _dense(v_exp, torch.uint8, device, "v_exp"), n, h, b, d)
+
+
+class CachePlan(NamedTuple):
+    lengths: torch.Tensor           # int32 [R]
+    token_offsets: torch.Tensor     # int32 [R + 1]
+    slots: Optional[torch.Tensor]   # int64 [n_tokens]
+    pieces: torch.Tensor            # int32 [most pieces, 4]: block, first token, place in the block, count; -1 where unused
+    counts: torch.Tensor            # int32 [2]: blocks taken, pieces
+
+
+def fikit_cache_pieces(n_tokens: int, n_requests: int, block_tokens: int) -> int:
+    return int(load().fikit_cache_pieces(n_tokens, n_requests, block_tokens))
+
+
+def fikit_cache_plan(cached: torch.Tensor, added: torch.Tensor, n_tokens: int, block_tokens: int, block_table: torch.Tensor,
+                     free_blocks: torch.Tensor, status: torch.Tensor, *, want_slots: bool = True, out: Optional[CachePlan] = None,
+                     workspace_buf: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> CachePlan:
+    """cached, added: int32 [R]; n_tokens = sum of added; block_table: int32 [R, width], receives the new blocks;
+    free_blocks: int32 [F].  Output tensors are allocated unless given."""
+    lib, dev, n = load(), cached.device, cached.numel()
+    _need(added.numel() == n and block_table.dim() == 2 and block_table.shape[0] == n, "cached, added: [R]; block_table: [R, width]")
+    handle, context = _on(stream, dev)
+    with context:
+        if out is None:
+            head = torch.empty(2 * n + 3, dtype=torch.int32, device=dev)      # lengths, offsets and counts
+            slots = torch.empty(n_tokens, dtype=torch.int64, device=dev) if want_slots else None
+            pieces = torch.empty((lib.fikit_cache_pieces(n_tokens, n, block_tokens), 4), dtype=torch.int32, device=dev)
+            out = CachePlan(head[:n], head[n:2 * n + 1], slots, pieces, head[2 * n + 1:])
+        else:
+            _need(out.lengths.numel() == n and out.token_offsets.numel() == n + 1 and out.counts.numel() == 2 and
+                  out.pieces.numel() == 4 * lib.fikit_cache_pieces(n_tokens, n, block_tokens) and
+                  (out.slots is None or out.slots.numel() == n_tokens), "out: tensors of these sizes")
+        if workspace_buf is None:
+            workspace_buf = workspace(lib.fikit_cache_plan_workspace_bytes(n), dev)
+        i32 = torch.int32
+        st = lib.fikit_cache_plan(_dense(cached, i32, dev, "cached"), _dense(added, i32, dev, "added"), n, n_tokens, block_tokens,
+                                  _dense(block_table, i32, dev, "block_table"), block_table.shape[1],
+                                  _dense(free_blocks, i32, dev, "free_blocks"), free_blocks.numel(),
+                                  _dense(out.lengths, i32, dev, "lengths"), _dense(out.token_offsets, i32, dev, "token_offsets"),
+                                  None if out.slots is None else _dense(out.slots, torch.int64, dev, "slots"),
+                                  _dense(out.pieces, i32, dev, "pieces"), _dense(out.counts, i32, dev, "counts"),
+                                  _dense(status, i32, dev, "status"), workspace_buf.data_ptr(), workspace_buf.numel(), handle)
+    if st != FIKIT_OK:
+        raise FikitError(st, "fikit_cache_plan")
+    return out
+
+
+def fikit_cache_append(k_cache: torch.Tensor, v_cache: torch.Tensor, k_exp: torch.Tensor, v_exp: torch.Tensor, k: torch.Tensor,
+                       v: torch.Tensor, pieces: torch.Tensor, status: torch.Tensor, *,
+                       stream: Optional[torch.cuda.Stream] = None) -> None:
+    """k, v: bfloat16 or float16 [n_tokens, kv heads, head_dim], of any token and head strides that are multiples of 8;
+    pieces: as fikit_cache_plan leaves them.  The cache is written in place."""
+    lib, dev = load(), k.device
+    cache = _cache_of(k_cache, v_cache, k_exp, v_exp, dev)
+    _need(k.dtype in _VALUE_TYPES and v.dtype == k.dtype and v.device == dev, "k, v: bfloat16 or float16, both the same")
+    _need(k.shape == v.shape and k.shape[1:] == (cache.kv_heads, cache.head_dim), "k, v: [n_tokens, kv heads, head_dim] of the cache")
+    _need(pieces.dim() == 2 and pieces.shape[1] == 4, "pieces: [n, 4]")
+    handle, context = _on(stream, dev)
+    with context:
+        st = lib.fikit_cache_append(cache, _vectors(k, "k"), _vectors(v, "v"), k.shape[0], _VALUE_TYPES[k.dtype],
+                                    _dense(pieces, torch.int32, dev, "pieces"), pieces.shape[0],
+                                    _dense(status, torch.int32, dev, "status"), handle)
+    if st != FIKIT_OK:
+        raise FikitError(st, "fikit_cache_append")
+
+
+class Attention(NamedTuple):
+    out: torch.Tensor               # [rows, q heads, head_dim], the queries' type
+    lse: Optional[torch.Tensor]     # float32 [rows, q heads]: log of the sum of the exponentials of the scores
+
+
+def _attention_out(q, want_lse, out):
+    rows, heads, _ = q.shape
+    if out is None:
+        out = Attention(torch.empty(q.shape, dtype=q.dtype, device=q.device),
+                        torch.empty((rows, heads), dtype=torch.float32, device=q.device) if want_lse else None)
+    _need(out.out.shape == q.shape, "out: the shape of q")
+    _need(out.lse is None or out.lse.shape == (rows, heads), "lse: [rows, q heads]")
+    return out, _dense(out.out, q.dtype, q.device, "out"), None if out.lse is None else _dense(out.lse, torch.float32, q.device, "lse")
+
+
+def fikit_cache_attention_workspace_bytes(n_requests: int, q_heads: int, kv_heads: int, head_dim: int, max_length: int) -> int:
+    return int(load().fikit_cache_attention_workspace_bytes(n_requests, q_heads, kv_heads, head_dim, max_length))
+
+
+def fikit_cache_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, k_exp: torch.Tensor, v_exp: torch.Tensor,
+                          block_table: torch.Tensor, lengths: torch.Tensor, scale: float, status: torch.Tensor, *,
+                          max_length: Optional[int] = None, want_lse: bool = True, out: Optional[Attention] = None,
+                          workspace_buf: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> Attention:
+    """q: [R, q heads, head_dim], one query per request; block_table: int32 [R, width]; lengths: int32 [R], none above
+    max_length (the table's width if not given)."""
+    lib, dev = load(), q.device
+    cache = _cache_of(k_cache, v_cache, k_exp, v_exp, dev)
+    _need(q.dtype in _VALUE_TYPES, "q: bfloat16 or float16")
+    vectors = _vectors(q, "q")
+    n, heads, d = q.shape
+    _need(d == cache.head_dim and block_table.dim() == 2 and block_table.shape[0] == n and lengths.numel() == n,
+          "q: [R, q heads, head_dim]; block_table: [R, width]; lengths: [R]")
+    if max_length is None:
+        max_length = block_table.shape[1] * cache.block_tokens
+    handle, context = _on(stream, dev)
+    with context:
+        out, p_out, p_lse = _attention_out(q, want_lse, out)
+        if workspace_buf is None:
+            workspace_buf = workspace(lib.fikit_cache_attention_workspace_bytes(n, heads, cache.kv_heads, d, max_length), dev)
+        st = lib.fikit_cache_attention(cache, vectors, heads, _VALUE_TYPES[q.dtype], scale,
+                                       _dense(block_table, torch.int32, dev, "block_table"), block_table.shape[1],
+                                       _dense(lengths, torch.int32, dev, "lengths"), n, max_length, p_out, p_lse,
+                                       _dense(status, torch.int32, dev, "status"), workspace_buf.data_ptr(), workspace_buf.numel(), handle)
+    if st != FIKIT_OK:
+        raise FikitError(st, "fikit_cache_attention")
+    return out
+
+
+def fikit_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor, scale: float,
+                           status: torch.Tensor, *, want_lse: bool = True, out: Optional[Attention] = None,
+                           stream: Optional[torch.cuda.Stream] = None) -> Attention:
+    """q: [n_tokens, q heads, head_dim], k, v: [n_tokens, kv heads, head_dim], of any token and head strides that are multiples
+    of 8 (parts of one product's output, say); offsets: int32 [prompts + 1]."""
+    lib, dev = load(), q.device
+    _need(q.dtype in _VALUE_TYPES and k.dtype == q.dtype and v.dtype == q.dtype and k.device == dev and v.device == dev,
+          "q, k, v: bfloat16 or float16, all the same")
+    vectors = _vectors(q, "q"), _vectors(k, "k"), _vectors(v, "v")
+    n, heads, d = q.shape
+    _need(k.shape == v.shape and k.shape[0] == n and k.shape[2] == d, "k, v: [n_tokens, kv heads, head_dim]")
+    handle, context = _on(stream, dev)
+    with context:
+        out, p_out, p_lse = _attention_out(q, want_lse, out)
+        st = lib.fikit_prompt_attention(*vectors, heads, k.shape[1], d, _VALUE_TYPES[q.dtype], scale,
+                                        _dense(offsets, torch.int32, dev, "offsets"), offsets.numel() - 1, n, p_out, p_lse,
+                                        _dense(status, torch.int32, dev, "status"), handle)
+    if st != FIKIT_OK:
+        raise FikitError(st, "fikit_prompt_attention")
+    return out
 
 
 # ---- helpers to move host arrays in and out (marshalling only) ---------------------------------

@@ -10,10 +10,12 @@ CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libfikit.so")
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function",
 ]
+
+UNITS = ["fikit.hip", "serve.hip"]                       # translation units
 
 
 def sources():
@@ -32,13 +34,25 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     if not force and not stale():
         return LIB
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    objects, compilers = [], []
+    for unit in UNITS:                                   # side by side
+        obj = os.path.join(CSRC, f"{unit}.tmp{os.getpid()}.o")
+        cmd = [hipcc, *HIPCC_FLAGS, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-c", "-o", obj, os.path.join(CSRC, unit)]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        objects.append(obj)
+        compilers.append((cmd, subprocess.Popen(cmd)))
     tmp = LIB + f".tmp{os.getpid()}"
-    cmd = [hipcc, *HIPCC_FLAGS, "-I", os.path.join(ROOT, "include"), "-I", CSRC,
-           "-o", tmp, os.path.join(CSRC, "fikit.hip")]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.check_call(cmd)
-    os.replace(tmp, LIB)
+    try:
+        failed = [cmd for cmd, p in compilers if p.wait() != 0]
+        if failed:
+            raise subprocess.CalledProcessError(1, failed[0])
+        subprocess.check_call([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objects])
+        os.replace(tmp, LIB)
+    finally:
+        for obj in objects:
+            if os.path.exists(obj):
+                os.remove(obj)
     return LIB
 
 

@@ -10,6 +10,7 @@
 #include <thread>
 
 #include "common.hip.h"
+#include "launches.h"
 #include "gapfill_kernels.hip.h"
 #include "profile_kernels.hip.h"
 #include "sort_kernels.hip.h"
@@ -384,6 +385,10 @@ int launch_prio_walk(hipStream_t st, const uint64_t* off, const uint32_t* hp_tas
 
 }  // namespace
 
+namespace fikit {
+void count_launch() { ++t_launches; }
+}  // namespace fikit
+
 extern "C" {
 
 int fikit_version(void) { return 1; }
@@ -415,6 +420,7 @@ const char* fikit_status_string(int status) {
     case FIKIT_HIP_ERROR: return "HIP runtime error";
     case FIKIT_UNSUPPORTED: return "beyond a stated limit of this call (list entries and launches of a scenario number 2^32 or more)";
     case FIKIT_TOO_LARGE: return "input larger than the built-in scratch buffer of fikit_gapfill_static";
+    case FIKIT_CACHE_FULL: return "more cache blocks needed than are free";
     default: return "unknown status";
   }
 }

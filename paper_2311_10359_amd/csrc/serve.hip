@@ -1,0 +1,263 @@
+// C ABI of the attention calls: argument checks, how the work is cut up, kernel sequencing.
+#include "fikit.h"
+
+#include <hip/hip_runtime.h>
+
+#include "cache_kernels.hip.h"
+#include "decode_kernels.hip.h"
+#include "launches.h"
+#include "prompt_kernels.hip.h"
+
+namespace {
+
+using namespace fikit;
+
+inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+constexpr uint64_t MOST_GROUPS = 0x7fffffffull;   // workgroups of a launch
+
+template <typename... P, typename... A>
+int enqueue(void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t st, A... args) {
+  count_launch();
+  hipLaunchKernelGGL(kernel, grid, block, 0, st, args...);
+  return hipGetLastError() == hipSuccess ? FIKIT_OK : FIKIT_HIP_ERROR;
+}
+
+bool vectors_ok(const fikit_vectors* v) {
+  return v && v->d_data && aligned(v->d_data, 16) && v->token_stride % 8 == 0 && v->head_stride % 8 == 0;
+}
+
+// FIKIT_OK, or what is wrong with a cache.
+int cache_status(const fikit_cache* c) {
+  if (!c || !c->d_k || !c->d_v || !c->d_k_exp || !c->d_v_exp || !aligned(c->d_k, 16) || !aligned(c->d_v, 16) || c->n_blocks == 0 ||
+      c->n_blocks > 0x7fffffffu || c->kv_heads == 0)
+    return FIKIT_INVALID_ARG;
+  const uint32_t b = c->block_tokens;
+  if (b < 16 || b > 256 || (b & (b - 1)) || (c->head_dim != 64 && c->head_dim != 128) || c->kv_heads > 65535) return FIKIT_UNSUPPORTED;
+  return FIKIT_OK;
+}
+
+// Calls f<T, D>() for a value type and head size that have been checked.
+template <typename F>
+int with_types(int32_t value_type, uint32_t head_dim, F f) {
+  if (value_type == FIKIT_BF16) return head_dim == 128 ? f.template operator()<Bf16, 128>() : f.template operator()<Bf16, 64>();
+  return head_dim == 128 ? f.template operator()<F16, 128>() : f.template operator()<F16, 64>();
+}
+
+bool type_ok(int32_t value_type) { return value_type == FIKIT_BF16 || value_type == FIKIT_F16; }
+
+template <typename T, int D>
+int append_enqueue(const AppendArgs& a, uint32_t n_pieces, hipStream_t st) {
+  const dim3 grid(n_pieces, a.cache.kv_heads, 2), block(APPEND_THREADS);
+  switch (a.cache.block_tokens * D / 8 / APPEND_THREADS) {
+    case 0: case 1: return enqueue(k_cache_append<T, D, 1>, grid, block, st, a);
+    case 2: return enqueue(k_cache_append<T, D, 2>, grid, block, st, a);
+    case 4: return enqueue(k_cache_append<T, D, 4>, grid, block, st, a);
+    case 8: return enqueue(k_cache_append<T, D, 8>, grid, block, st, a);
+    default: return enqueue(k_cache_append<T, D, 16>, grid, block, st, a);
+  }
+}
+struct AppendCall {
+  const AppendArgs& a;
+  uint32_t n_pieces;
+  hipStream_t st;
+  template <typename T, int D>
+  int operator()() { return append_enqueue<T, D>(a, n_pieces, st); }
+};
+
+// How the contexts of a decode step are cut into parts: as many as give every part some 128 tokens at least and the chip
+// some 2048 workgroups.  A wave's quarter of a part must not hold more than 64 blocks.
+struct DecodeCut {
+  uint32_t head_tiles, part_tokens, parts;
+  uint64_t groups;
+};
+constexpr uint32_t DECODE_MOST_PART = 4096, DECODE_LEAST_PART = 128;
+constexpr uint64_t DECODE_GROUPS = 2048;
+
+DecodeCut decode_cut(uint32_t n_requests, uint32_t q_heads, uint32_t kv_heads, uint32_t max_length) {
+  DecodeCut c;
+  c.head_tiles = (q_heads / kv_heads + DECODE_ROWS - 1) / DECODE_ROWS;
+  const uint64_t units = static_cast<uint64_t>(n_requests) * kv_heads * c.head_tiles;
+  uint64_t part = (units * max_length + DECODE_GROUPS - 1) / DECODE_GROUPS;
+  part = (part + DECODE_LEAST_PART - 1) / DECODE_LEAST_PART * DECODE_LEAST_PART;
+  c.part_tokens = static_cast<uint32_t>(part < DECODE_LEAST_PART ? DECODE_LEAST_PART : part > DECODE_MOST_PART ? DECODE_MOST_PART : part);
+  c.parts = max_length == 0 ? 1 : (max_length + c.part_tokens - 1) / c.part_tokens;
+  c.groups = units * c.parts;
+  return c;
+}
+
+uint64_t part_sums_bytes(uint64_t rows) { return (rows * sizeof(float2) + 255) / 256 * 256; }
+
+struct DecodeCall {
+  const DecodeArgs& a;
+  uint32_t groups;
+  hipStream_t st;
+  template <typename T, int D>
+  int operator()() {
+    if (int rc = enqueue(k_decode<T, D>, dim3(groups), dim3(DECODE_WAVES * WAVE), st, a)) return rc;
+    if (a.parts == 1) return FIKIT_OK;
+    const uint64_t heads = static_cast<uint64_t>(a.n_requests) * a.q_heads;
+    return enqueue(k_decode_join<T, D>, dim3(static_cast<uint32_t>((heads + 3) / 4)), dim3(256), st, a);
+  }
+};
+
+constexpr int PROMPT_WAVES = 8;
+struct PromptCall {
+  const PromptArgs& a;
+  uint32_t groups;
+  hipStream_t st;
+  template <typename T, int D>
+  int operator()() { return enqueue(k_prompt<T, D, PROMPT_WAVES>, dim3(groups), dim3(PROMPT_WAVES * WAVE), st, a); }
+};
+
+}  // namespace
+
+extern "C" {
+
+uint64_t fikit_cache_pieces(uint32_t n_tokens, uint32_t n_requests, uint32_t block_tokens) {
+  if (block_tokens == 0) return 0;
+  const uint64_t cut = n_tokens / block_tokens + 2ull * n_requests;
+  return cut < n_tokens ? cut : n_tokens;
+}
+
+size_t fikit_cache_plan_workspace_bytes(uint32_t n_requests) { return (static_cast<size_t>(n_requests) * sizeof(int2) + 255) / 256 * 256 + 256; }
+
+int fikit_cache_plan(const int32_t* d_cached, const int32_t* d_added, uint32_t n_requests, uint32_t n_tokens,
+                     uint32_t block_tokens, int32_t* d_block_table, uint32_t table_width, const int32_t* d_free,
+                     uint32_t n_free, int32_t* d_lengths, int32_t* d_token_offsets, int64_t* d_slots,
+                     fikit_piece* d_pieces, int32_t* d_counts, int32_t* d_status, void* d_workspace,
+                     size_t workspace_bytes, void* hip_stream) {
+  if (!d_token_offsets || !d_counts || !d_status || !d_workspace || !aligned(d_token_offsets, 4) || !aligned(d_counts, 4) ||
+      !aligned(d_status, 4) || !aligned(d_workspace, 256))
+    return FIKIT_INVALID_ARG;
+  if (n_requests > 0 && (!d_cached || !d_added || !d_lengths || !aligned(d_cached, 4) || !aligned(d_added, 4) || !aligned(d_lengths, 4)))
+    return FIKIT_INVALID_ARG;
+  if (n_tokens > 0x7fffffffu || n_requests > 0x7fffffffu || n_free > 0x7fffffffu || table_width > 0x7fffffffu) return FIKIT_INVALID_ARG;
+  if (n_tokens > 0 && (n_requests == 0 || table_width == 0 || !d_block_table || !d_pieces)) return FIKIT_INVALID_ARG;
+  if (n_free > 0 && !d_free) return FIKIT_INVALID_ARG;
+  if (!aligned(d_block_table, 4) || !aligned(d_free, 4) || !aligned(d_slots, 8) || !aligned(d_pieces, 16)) return FIKIT_INVALID_ARG;
+  if (block_tokens < 16 || block_tokens > 256 || (block_tokens & (block_tokens - 1))) return FIKIT_UNSUPPORTED;
+  if (workspace_bytes < fikit_cache_plan_workspace_bytes(n_requests)) return FIKIT_WORKSPACE_TOO_SMALL;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  PlanArgs a{};
+  a.cached = d_cached;
+  a.added = d_added;
+  a.table = d_block_table;
+  a.free_blocks = d_free;
+  a.lengths = d_lengths;
+  a.token_offsets = d_token_offsets;
+  a.slots = d_slots;
+  a.pieces = reinterpret_cast<int4*>(d_pieces);
+  a.counts = d_counts;
+  a.status = d_status;
+  a.bases = static_cast<int2*>(d_workspace);
+  a.n_requests = n_requests;
+  a.n_tokens = n_tokens;
+  a.table_width = table_width;
+  a.n_free = n_free;
+  a.room = static_cast<uint32_t>(fikit_cache_pieces(n_tokens, n_requests, block_tokens));
+  a.shift = static_cast<uint32_t>(__builtin_ctz(block_tokens));
+  if (int rc = enqueue(k_plan_sums, dim3(1), dim3(PLAN_THREADS), st, a)) return rc;
+  if (n_tokens == 0) return FIKIT_OK;
+  return enqueue(k_plan_tokens, dim3((n_tokens + 255) / 256), dim3(256), st, a);
+}
+
+int fikit_cache_append(const fikit_cache* h_cache, const fikit_vectors* h_k, const fikit_vectors* h_v, uint32_t n_tokens,
+                       int32_t value_type, const fikit_piece* d_pieces, uint64_t n_pieces, int32_t* d_status,
+                       void* hip_stream) {
+  if (int rc = cache_status(h_cache)) return rc;
+  if (!type_ok(value_type) || !d_status || !aligned(d_status, 4) || !aligned(d_pieces, 16)) return FIKIT_INVALID_ARG;
+  if (n_tokens > 0x7fffffffu || n_pieces > MOST_GROUPS) return FIKIT_INVALID_ARG;
+  if (n_pieces == 0) return FIKIT_OK;
+  if (!d_pieces || !vectors_ok(h_k) || !vectors_ok(h_v)) return FIKIT_INVALID_ARG;
+  AppendArgs a{};
+  a.cache = *h_cache;
+  a.k = *h_k;
+  a.v = *h_v;
+  a.pieces = reinterpret_cast<const int4*>(d_pieces);
+  a.status = d_status;
+  a.n_tokens = n_tokens;
+  return with_types(value_type, h_cache->head_dim, AppendCall{a, static_cast<uint32_t>(n_pieces), static_cast<hipStream_t>(hip_stream)});
+}
+
+size_t fikit_cache_attention_workspace_bytes(uint32_t n_requests, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim,
+                                             uint32_t max_length) {
+  if (kv_heads == 0 || q_heads == 0 || q_heads % kv_heads || q_heads > 65535 || max_length > 0x7fffffffu || n_requests > 0x7fffffffu) return 0;
+  const DecodeCut c = decode_cut(n_requests, q_heads, kv_heads, max_length);
+  if (c.groups > MOST_GROUPS) return 0;
+  if (c.parts == 1) return 256;
+  const uint64_t rows = static_cast<uint64_t>(n_requests) * c.parts * q_heads;
+  return static_cast<size_t>(part_sums_bytes(rows) + rows * head_dim * sizeof(float));
+}
+
+int fikit_cache_attention(const fikit_cache* h_cache, const fikit_vectors* h_q, uint32_t q_heads, int32_t value_type, float scale,
+                          const int32_t* d_block_table, uint32_t table_width, const int32_t* d_lengths, uint32_t n_requests,
+                          uint32_t max_length, void* d_out, float* d_lse, int32_t* d_status, void* d_workspace,
+                          size_t workspace_bytes, void* hip_stream) {
+  if (int rc = cache_status(h_cache)) return rc;
+  if (!type_ok(value_type) || !d_status || !aligned(d_status, 4) || q_heads == 0 || q_heads % h_cache->kv_heads) return FIKIT_INVALID_ARG;
+  if (max_length > 0x7fffffffu || n_requests > 0x7fffffffu || table_width > 0x7fffffffu) return FIKIT_INVALID_ARG;
+  if (max_length > static_cast<uint64_t>(table_width) * h_cache->block_tokens) return FIKIT_INVALID_ARG;
+  if (q_heads > 65535) return FIKIT_UNSUPPORTED;
+  if (n_requests == 0) return FIKIT_OK;
+  if (!vectors_ok(h_q) || !d_lengths || !d_out || !aligned(d_block_table, 4) || !aligned(d_lengths, 4) || !aligned(d_out, 16) ||
+      !aligned(d_lse, 4) || (max_length > 0 && !d_block_table))
+    return FIKIT_INVALID_ARG;
+  const DecodeCut c = decode_cut(n_requests, q_heads, h_cache->kv_heads, max_length);
+  if (c.groups > MOST_GROUPS) return FIKIT_UNSUPPORTED;
+  if (c.parts > 1 && (!d_workspace || !aligned(d_workspace, 256))) return FIKIT_INVALID_ARG;
+  if (c.parts > 1 && workspace_bytes < fikit_cache_attention_workspace_bytes(n_requests, q_heads, h_cache->kv_heads, h_cache->head_dim, max_length))
+    return FIKIT_WORKSPACE_TOO_SMALL;
+  DecodeArgs a{};
+  a.cache = *h_cache;
+  a.q = *h_q;
+  a.table = d_block_table;
+  a.lengths = d_lengths;
+  a.out = d_out;
+  a.lse = d_lse;
+  a.status = d_status;
+  a.part_sums = static_cast<float2*>(d_workspace);
+  if (c.parts > 1)
+    a.part_out = reinterpret_cast<float*>(static_cast<unsigned char*>(d_workspace) + part_sums_bytes(static_cast<uint64_t>(n_requests) * c.parts * q_heads));
+  a.q_heads = q_heads;
+  a.table_width = table_width;
+  a.max_length = max_length;
+  a.parts = c.parts;
+  a.part_tokens = c.part_tokens;
+  a.head_tiles = c.head_tiles;
+  a.n_requests = n_requests;
+  a.scale = scale;
+  return with_types(value_type, h_cache->head_dim, DecodeCall{a, static_cast<uint32_t>(c.groups), static_cast<hipStream_t>(hip_stream)});
+}
+
+int fikit_prompt_attention(const fikit_vectors* h_q, const fikit_vectors* h_k, const fikit_vectors* h_v, uint32_t q_heads,
+                           uint32_t kv_heads, uint32_t head_dim, int32_t value_type, float scale, const int32_t* d_offsets,
+                           uint32_t n_prompts, uint32_t n_tokens, void* d_out, float* d_lse, int32_t* d_status,
+                           void* hip_stream) {
+  if (!type_ok(value_type) || !d_status || !aligned(d_status, 4) || kv_heads == 0 || q_heads == 0 || q_heads % kv_heads) return FIKIT_INVALID_ARG;
+  if (n_tokens > 0x7fffffffu || n_prompts > 0x7fffffffu || (n_tokens > 0 && n_prompts == 0)) return FIKIT_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128) return FIKIT_UNSUPPORTED;
+  if (n_tokens == 0) return FIKIT_OK;
+  if (!vectors_ok(h_q) || !vectors_ok(h_k) || !vectors_ok(h_v) || !d_offsets || !d_out || !aligned(d_offsets, 4) || !aligned(d_out, 16) ||
+      !aligned(d_lse, 4))
+    return FIKIT_INVALID_ARG;
+  const uint64_t slots = n_tokens / (PROMPT_WAVES * PROMPT_WAVE_ROWS) + static_cast<uint64_t>(n_prompts);
+  if (slots * q_heads > MOST_GROUPS) return FIKIT_UNSUPPORTED;
+  PromptArgs a{};
+  a.q = *h_q;
+  a.k = *h_k;
+  a.v = *h_v;
+  a.offsets = d_offsets;
+  a.out = d_out;
+  a.lse = d_lse;
+  a.status = d_status;
+  a.q_heads = q_heads;
+  a.kv_heads = kv_heads;
+  a.n_prompts = n_prompts;
+  a.n_tokens = n_tokens;
+  a.slots = static_cast<uint32_t>(slots);
+  a.scale = scale;
+  return with_types(value_type, head_dim, PromptCall{a, static_cast<uint32_t>(slots * q_heads), static_cast<hipStream_t>(hip_stream)});
+}
+
+}  // extern "C"
