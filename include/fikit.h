@@ -476,7 +476,7 @@ typedef struct fikit_piece {
 /* Most pieces that n_tokens new tokens of n_requests requests are cut into: the length of the list of pieces. */
 uint64_t fikit_cache_pieces(uint32_t n_tokens, uint32_t n_requests, uint32_t block_tokens);
 
-/* Bytes of device workspace fikit_cache_plan needs for these sizes. */
+/* Bytes of device workspace fikit_cache_plan needs for these sizes (0: none, d_workspace may be NULL). */
 size_t fikit_cache_plan_workspace_bytes(uint32_t n_requests);
 
 /*

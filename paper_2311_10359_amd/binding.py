@@ -6,7 +6,6 @@ library is missing or cannot be loaded, importing the functions fails loudly.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 from typing import NamedTuple, Optional
@@ -584,19 +583,27 @@ def fikit_check_status(status: torch.Tensor, what: str = "a call on this status 
         raise FikitError(st, what)
 
 
-def _on(stream: Optional[torch.cuda.Stream], device):
-    """The stream of a call as (handle, context to allocate and launch in)."""
-    if stream is None:
-        stream = torch.cuda.current_stream(device)
-        if device.index == torch.cuda.current_device():
-            return stream.cuda_stream, contextlib.nullcontext()
-    return stream.cuda_stream, torch.cuda.stream(stream)
+def _elsewhere(stream: Optional[torch.cuda.Stream], device):
+    """None if a call runs on the current stream of the current device, else the context to run it in."""
+    if device.type != "cuda":
+        raise ValueError("tensors on a GPU")
+    if stream is not None:
+        return torch.cuda.stream(stream)
+    if device.index != torch.cuda.current_device():
+        return torch.cuda.device(device)
+    return None
+
+
+# (torch.cuda.current_stream() makes an object around this handle, 1.8 us of a call that may take 5)
+def _current_handle(device) -> int:
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _vectors(t: torch.Tensor, what: str) -> _Vectors:
-    if t.dim() != 3 or t.stride(2) != 1:
+    strides = t.stride()
+    if len(strides) != 3 or strides[2] != 1:
         raise ValueError(f"{what}: [tokens, heads, head_dim] with the last dimension dense")
-    return _Vectors(t.data_ptr(), t.stride(0), t.stride(1))
+    return _Vectors(t.data_ptr(), strides[0], strides[1])
 
 
 def _need(condition: bool, what: str) -> None:
@@ -605,19 +612,19 @@ def _need(condition: bool, what: str) -> None:
 
 
 def _dense(t: torch.Tensor, dtype: torch.dtype, device, what: str) -> int:
-    _need(t.dtype == dtype and t.device == device and t.is_contiguous(), f"{what}: a dense {dtype} tensor on {device}")
+    if t.dtype is not dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{what}: a dense {dtype} tensor on {device}")
     return t.data_ptr()
 
 
 def _cache_of(k_cache, v_cache, k_exp, v_exp, device) -> _Cache:
     """k_cache, v_cache: [blocks, kv heads, block tokens, head dim] codes (float8_e4m3fn or their bytes)."""
     _need(k_cache.dim() == 4 and v_cache.shape == k_cache.shape, "k_cache, v_cache: [blocks, kv heads, block tokens, head dim]")
-    for t in (k_cache, v_cache):
-        _need(t.dtype in (torch.float8_e4m3fn, torch.uint8) and t.device == device and t.is_contiguous(),
-              f"k_cache, v_cache: dense float8_e4m3fn tensors on {device}")
     n, h, b, d = k_cache.shape
     _need(k_exp.shape == (n, h) and v_exp.shape == (n, h), "k_exp, v_exp: [blocks, kv heads]")
-    return _Cache(k_cache.data_ptr(), v_cache.data_ptr(), _dense(k_exp, torch.uint8, device, "k_exp"),
+    codes = k_cache.dtype
+    _need(codes is torch.float8_e4m3fn or codes is torch.uint8, "k_cache, v_cache: float8_e4m3fn or uint8")
+    return _Cache(_dense(k_cache, codes, device, "k_cache"), _dense(v_cache, codes, device, "v_cache"), _dense(k_exp, torch.uint8, device, "k_exp"),
                   _dense(v_exp, torch.uint8, device, "v_exp"), n, h, b, d)
 
 
@@ -640,27 +647,32 @@ def fikit_cache_plan(cached: torch.Tensor, added: torch.Tensor, n_tokens: int, b
     free_blocks: int32 [F].  Output tensors are allocated unless given."""
     lib, dev, n = load(), cached.device, cached.numel()
     _need(added.numel() == n and block_table.dim() == 2 and block_table.shape[0] == n, "cached, added: [R]; block_table: [R, width]")
-    handle, context = _on(stream, dev)
-    with context:
-        if out is None:
-            head = torch.empty(2 * n + 3, dtype=torch.int32, device=dev)      # lengths, offsets and counts
-            slots = torch.empty(n_tokens, dtype=torch.int64, device=dev) if want_slots else None
-            pieces = torch.empty((lib.fikit_cache_pieces(n_tokens, n, block_tokens), 4), dtype=torch.int32, device=dev)
-            out = CachePlan(head[:n], head[n:2 * n + 1], slots, pieces, head[2 * n + 1:])
-        else:
-            _need(out.lengths.numel() == n and out.token_offsets.numel() == n + 1 and out.counts.numel() == 2 and
-                  out.pieces.numel() == 4 * lib.fikit_cache_pieces(n_tokens, n, block_tokens) and
-                  (out.slots is None or out.slots.numel() == n_tokens), "out: tensors of these sizes")
-        if workspace_buf is None:
-            workspace_buf = workspace(lib.fikit_cache_plan_workspace_bytes(n), dev)
-        i32 = torch.int32
-        st = lib.fikit_cache_plan(_dense(cached, i32, dev, "cached"), _dense(added, i32, dev, "added"), n, n_tokens, block_tokens,
-                                  _dense(block_table, i32, dev, "block_table"), block_table.shape[1],
-                                  _dense(free_blocks, i32, dev, "free_blocks"), free_blocks.numel(),
-                                  _dense(out.lengths, i32, dev, "lengths"), _dense(out.token_offsets, i32, dev, "token_offsets"),
-                                  None if out.slots is None else _dense(out.slots, torch.int64, dev, "slots"),
-                                  _dense(out.pieces, i32, dev, "pieces"), _dense(out.counts, i32, dev, "counts"),
-                                  _dense(status, i32, dev, "status"), workspace_buf.data_ptr(), workspace_buf.numel(), handle)
+    context = _elsewhere(stream, dev)
+    if context is not None:
+        with context:
+            return fikit_cache_plan(cached, added, n_tokens, block_tokens, block_table, free_blocks, status, want_slots=want_slots,
+                                    out=out, workspace_buf=workspace_buf)
+    i32 = torch.int32
+    room = lib.fikit_cache_pieces(n_tokens, n, block_tokens)
+    if out is None:
+        out = CachePlan(cached.new_empty(n), cached.new_empty(n + 1),
+                        torch.empty(n_tokens, dtype=torch.int64, device=dev) if want_slots else None,
+                        cached.new_empty((room, 4)), cached.new_empty(2))
+    else:
+        _need(out.lengths.numel() == n and out.token_offsets.numel() == n + 1 and out.counts.numel() == 2 and
+              out.pieces.numel() == 4 * room and (out.slots is None or out.slots.numel() == n_tokens), "out: tensors of these sizes")
+    if workspace_buf is None:
+        size = lib.fikit_cache_plan_workspace_bytes(n)
+        if size:
+            workspace_buf = workspace(size, dev)
+    st = lib.fikit_cache_plan(_dense(cached, i32, dev, "cached"), _dense(added, i32, dev, "added"), n, n_tokens, block_tokens,
+                              _dense(block_table, i32, dev, "block_table"), block_table.shape[1],
+                              _dense(free_blocks, i32, dev, "free_blocks"), free_blocks.numel(),
+                              _dense(out.lengths, i32, dev, "lengths"), _dense(out.token_offsets, i32, dev, "token_offsets"),
+                              None if out.slots is None else _dense(out.slots, torch.int64, dev, "slots"),
+                              _dense(out.pieces, i32, dev, "pieces"), _dense(out.counts, i32, dev, "counts"),
+                              _dense(status, i32, dev, "status"), None if workspace_buf is None else workspace_buf.data_ptr(),
+                              0 if workspace_buf is None else workspace_buf.numel(), _current_handle(dev))
     if st != FIKIT_OK:
         raise FikitError(st, "fikit_cache_plan")
     return out
@@ -676,11 +688,13 @@ def fikit_cache_append(k_cache: torch.Tensor, v_cache: torch.Tensor, k_exp: torc
     _need(k.dtype in _VALUE_TYPES and v.dtype == k.dtype and v.device == dev, "k, v: bfloat16 or float16, both the same")
     _need(k.shape == v.shape and k.shape[1:] == (cache.kv_heads, cache.head_dim), "k, v: [n_tokens, kv heads, head_dim] of the cache")
     _need(pieces.dim() == 2 and pieces.shape[1] == 4, "pieces: [n, 4]")
-    handle, context = _on(stream, dev)
-    with context:
-        st = lib.fikit_cache_append(cache, _vectors(k, "k"), _vectors(v, "v"), k.shape[0], _VALUE_TYPES[k.dtype],
-                                    _dense(pieces, torch.int32, dev, "pieces"), pieces.shape[0],
-                                    _dense(status, torch.int32, dev, "status"), handle)
+    vectors = _vectors(k, "k"), _vectors(v, "v")
+    context = _elsewhere(stream, dev)
+    if context is not None:
+        with context:
+            return fikit_cache_append(k_cache, v_cache, k_exp, v_exp, k, v, pieces, status)
+    st = lib.fikit_cache_append(cache, *vectors, k.shape[0], _VALUE_TYPES[k.dtype], _dense(pieces, torch.int32, dev, "pieces"),
+                                pieces.shape[0], _dense(status, torch.int32, dev, "status"), _current_handle(dev))
     if st != FIKIT_OK:
         raise FikitError(st, "fikit_cache_append")
 
@@ -719,15 +733,19 @@ def fikit_cache_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch
           "q: [R, q heads, head_dim]; block_table: [R, width]; lengths: [R]")
     if max_length is None:
         max_length = block_table.shape[1] * cache.block_tokens
-    handle, context = _on(stream, dev)
-    with context:
-        out, p_out, p_lse = _attention_out(q, want_lse, out)
-        if workspace_buf is None:
-            workspace_buf = workspace(lib.fikit_cache_attention_workspace_bytes(n, heads, cache.kv_heads, d, max_length), dev)
-        st = lib.fikit_cache_attention(cache, vectors, heads, _VALUE_TYPES[q.dtype], scale,
-                                       _dense(block_table, torch.int32, dev, "block_table"), block_table.shape[1],
-                                       _dense(lengths, torch.int32, dev, "lengths"), n, max_length, p_out, p_lse,
-                                       _dense(status, torch.int32, dev, "status"), workspace_buf.data_ptr(), workspace_buf.numel(), handle)
+    context = _elsewhere(stream, dev)
+    if context is not None:
+        with context:
+            return fikit_cache_attention(q, k_cache, v_cache, k_exp, v_exp, block_table, lengths, scale, status, max_length=max_length,
+                                         want_lse=want_lse, out=out, workspace_buf=workspace_buf)
+    out, p_out, p_lse = _attention_out(q, want_lse, out)
+    if workspace_buf is None:
+        workspace_buf = workspace(lib.fikit_cache_attention_workspace_bytes(n, heads, cache.kv_heads, d, max_length), dev)
+    st = lib.fikit_cache_attention(cache, vectors, heads, _VALUE_TYPES[q.dtype], scale,
+                                   _dense(block_table, torch.int32, dev, "block_table"), block_table.shape[1],
+                                   _dense(lengths, torch.int32, dev, "lengths"), n, max_length, p_out, p_lse,
+                                   _dense(status, torch.int32, dev, "status"), workspace_buf.data_ptr(), workspace_buf.numel(),
+                                   _current_handle(dev))
     if st != FIKIT_OK:
         raise FikitError(st, "fikit_cache_attention")
     return out
@@ -744,12 +762,14 @@ def fikit_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, of
     vectors = _vectors(q, "q"), _vectors(k, "k"), _vectors(v, "v")
     n, heads, d = q.shape
     _need(k.shape == v.shape and k.shape[0] == n and k.shape[2] == d, "k, v: [n_tokens, kv heads, head_dim]")
-    handle, context = _on(stream, dev)
-    with context:
-        out, p_out, p_lse = _attention_out(q, want_lse, out)
-        st = lib.fikit_prompt_attention(*vectors, heads, k.shape[1], d, _VALUE_TYPES[q.dtype], scale,
-                                        _dense(offsets, torch.int32, dev, "offsets"), offsets.numel() - 1, n, p_out, p_lse,
-                                        _dense(status, torch.int32, dev, "status"), handle)
+    context = _elsewhere(stream, dev)
+    if context is not None:
+        with context:
+            return fikit_prompt_attention(q, k, v, offsets, scale, status, want_lse=want_lse, out=out)
+    out, p_out, p_lse = _attention_out(q, want_lse, out)
+    st = lib.fikit_prompt_attention(*vectors, heads, k.shape[1], d, _VALUE_TYPES[q.dtype], scale,
+                                    _dense(offsets, torch.int32, dev, "offsets"), offsets.numel() - 1, n, p_out, p_lse,
+                                    _dense(status, torch.int32, dev, "status"), _current_handle(dev))
     if st != FIKIT_OK:
         raise FikitError(st, "fikit_prompt_attention")
     return out

@@ -47,19 +47,13 @@ __device__ __forceinline__ bool plan_request(const PlanArgs& a, int64_t cached, 
   return true;
 }
 
-// Prefix sums over all requests by one workgroup, a run of consecutive requests per thread.
-__global__ __launch_bounds__(PLAN_THREADS) void k_plan_sums(PlanArgs a) {
-  __shared__ uint64_t wave_tokens[PLAN_THREADS / WAVE];
-  __shared__ uint32_t wave_blocks[PLAN_THREADS / WAVE], wave_pieces[PLAN_THREADS / WAVE];
-  __shared__ int32_t bad;
-  if (stopped(a.status)) return;
-  const uint32_t per = (a.n_requests + PLAN_THREADS - 1) / PLAN_THREADS;
-  const uint32_t first = min_u32(threadIdx.x * per, a.n_requests), last = min_u32(first + per, a.n_requests);
-  if (threadIdx.x == 0) bad = 0;
-  PlanSums mine{0, 0, 0};
-  bool ok = true;
-  for (uint32_t r = first; r < last; ++r) ok &= plan_request(a, a.cached[r], a.added[r], &mine);
-  // inclusive sums over the wave, then over the waves
+struct PlanScan {
+  uint64_t tokens[PLAN_THREADS / WAVE];
+  uint32_t blocks[PLAN_THREADS / WAVE], pieces[PLAN_THREADS / WAVE];
+};
+
+// The sums of the threads before, and of all of them, in a workgroup of PLAN_THREADS; whether `ok` holds in all.
+__device__ __forceinline__ bool plan_scan(const PlanSums& mine, bool ok, PlanScan* lds, PlanSums* before, PlanSums* total) {
   PlanSums run = mine;
   for (int d = 1; d < WAVE; d <<= 1) {
     const uint64_t t = shfl_up_u64(run.tokens, d);
@@ -67,36 +61,22 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_plan_sums(PlanArgs a) {
     if (lane_id() >= static_cast<uint32_t>(d)) { run.tokens += t; run.blocks += b; run.pieces += p; }
   }
   const uint32_t wave = threadIdx.x / WAVE;
-  if (lane_id() == WAVE - 1) { wave_tokens[wave] = run.tokens; wave_blocks[wave] = run.blocks; wave_pieces[wave] = run.pieces; }
-  __syncthreads();
-  if (!ok) bad = 1;
-  PlanSums before{0, 0, 0}, total{0, 0, 0};
+  if (lane_id() == WAVE - 1) { lds->tokens[wave] = run.tokens; lds->blocks[wave] = run.blocks; lds->pieces[wave] = run.pieces; }
+  const bool all = __syncthreads_and(ok);
+  *before = PlanSums{run.tokens - mine.tokens, run.blocks - mine.blocks, run.pieces - mine.pieces};
+  *total = PlanSums{0, 0, 0};
   for (uint32_t w = 0; w < PLAN_THREADS / WAVE; ++w) {
-    if (w < wave) { before.tokens += wave_tokens[w]; before.blocks += wave_blocks[w]; before.pieces += wave_pieces[w]; }
-    total.tokens += wave_tokens[w]; total.blocks += wave_blocks[w]; total.pieces += wave_pieces[w];
+    if (w < wave) { before->tokens += lds->tokens[w]; before->blocks += lds->blocks[w]; before->pieces += lds->pieces[w]; }
+    total->tokens += lds->tokens[w]; total->blocks += lds->blocks[w]; total->pieces += lds->pieces[w];
   }
-  __syncthreads();
-  const int32_t error = bad || total.tokens != a.n_tokens ? FIKIT_INVALID_ARG : total.blocks > a.n_free ? FIKIT_CACHE_FULL : FIKIT_OK;
-  if (error != FIKIT_OK) {
-    if (threadIdx.x == 0) *a.status = error;
-    return;
-  }
-  PlanSums at{before.tokens + run.tokens - mine.tokens, before.blocks + run.blocks - mine.blocks, before.pieces + run.pieces - mine.pieces};
-  for (uint32_t r = first; r < last; ++r) {
-    const int32_t cached = a.cached[r], added = a.added[r];
-    a.lengths[r] = cached + added;
-    a.token_offsets[r] = static_cast<int32_t>(at.tokens);
-    a.bases[r] = make_int2(static_cast<int32_t>(at.blocks), static_cast<int32_t>(at.pieces));
-    plan_request(a, cached, added, &at);
-  }
-  if (threadIdx.x == 0) {
-    a.token_offsets[a.n_requests] = static_cast<int32_t>(a.n_tokens);
-    a.counts[0] = static_cast<int32_t>(total.blocks);
-    a.counts[1] = static_cast<int32_t>(total.pieces);
-  }
+  return all;
 }
 
-// The last request that begins at token t or before; lo begins so, hi does not.
+__device__ __forceinline__ int32_t plan_error(const PlanArgs& a, const PlanSums& total, bool ok) {
+  return !ok || total.tokens != a.n_tokens ? FIKIT_INVALID_ARG : total.blocks > a.n_free ? FIKIT_CACHE_FULL : FIKIT_OK;
+}
+
+// The last of the requests lo .. hi - 1 that begins at token t or before; lo begins so.
 __device__ __forceinline__ uint32_t plan_find(const int32_t* offsets, uint32_t lo, uint32_t hi, uint32_t t) {
   while (hi - lo > 1) {
     const uint32_t mid = lo + (hi - lo) / 2;
@@ -105,13 +85,13 @@ __device__ __forceinline__ uint32_t plan_find(const int32_t* offsets, uint32_t l
   return lo;
 }
 
-__device__ __forceinline__ void plan_token(const PlanArgs& a, uint32_t t, uint32_t r) {
+// What new token t, of request r that begins at token `first`, writes.
+__device__ __forceinline__ void plan_token(const PlanArgs& a, uint32_t t, uint32_t r, uint32_t first, int2 base) {
   const uint32_t block_tokens = 1u << a.shift;
   const uint32_t cached = static_cast<uint32_t>(a.cached[r]), length = cached + static_cast<uint32_t>(a.added[r]);
-  const uint32_t index = t - static_cast<uint32_t>(a.token_offsets[r]);
+  const uint32_t index = t - first;
   const uint32_t place = cached + index, page = place >> a.shift, at = place & (block_tokens - 1);
   const uint32_t held = (cached + block_tokens - 1) >> a.shift;
-  const int2 base = a.bases[r];
   int32_t* entry = a.table + static_cast<uint64_t>(r) * a.table_width + page;
   const int32_t block = page >= held ? a.free_blocks[base.x + (page - held)] : *entry;
   if (at == 0) *entry = block;      // (a block that begins at a new token is a new one)
@@ -121,19 +101,147 @@ __device__ __forceinline__ void plan_token(const PlanArgs& a, uint32_t t, uint32
                                                                static_cast<int32_t>(min_u32(block_tokens - at, length - place)));
 }
 
+// The whole plan in one launch: every workgroup sums all requests for itself, in LDS, and takes 1024 tokens at a time.
+constexpr uint32_t PLAN_ONE_REQUESTS = 4096;
+__global__ __launch_bounds__(PLAN_THREADS) void k_plan_one(PlanArgs a) {
+  constexpr uint32_t PER = PLAN_ONE_REQUESTS / PLAN_THREADS;
+  __shared__ int32_t offsets[PLAN_ONE_REQUESTS];
+  __shared__ int2 bases[PLAN_ONE_REQUESTS];
+  __shared__ PlanScan scan;
+  const bool stop = stopped(a.status);
+  const uint32_t per = (a.n_requests + PLAN_THREADS - 1) / PLAN_THREADS, first = threadIdx.x * per;
+  int32_t cached[PER], added[PER];
+#pragma unroll
+  for (uint32_t i = 0; i < PER; ++i) {
+    const bool there = i < per && first + i < a.n_requests;
+    cached[i] = there ? a.cached[first + i] : 0;
+    added[i] = there ? a.added[first + i] : 0;
+  }
+  if (stop) return;
+  PlanSums mine{0, 0, 0}, at, total;
+  bool ok = true;
+#pragma unroll
+  for (uint32_t i = 0; i < PER; ++i) ok &= plan_request(a, cached[i], added[i], &mine);
+  ok = plan_scan(mine, ok, &scan, &at, &total);
+  if (const int32_t error = plan_error(a, total, ok)) {
+    if (threadIdx.x == 0) *a.status = error;
+    return;
+  }
+  const bool writes = blockIdx.x == 0;
+#pragma unroll
+  for (uint32_t i = 0; i < PER; ++i)
+    if (i < per && first + i < a.n_requests) {
+      const uint32_t r = first + i;
+      offsets[r] = static_cast<int32_t>(at.tokens);
+      bases[r] = make_int2(static_cast<int32_t>(at.blocks), static_cast<int32_t>(at.pieces));
+      if (writes) {
+        a.lengths[r] = cached[i] + added[i];
+        a.token_offsets[r] = static_cast<int32_t>(at.tokens);
+      }
+      plan_request(a, cached[i], added[i], &at);
+    }
+  if (writes && threadIdx.x == 0) {
+    a.token_offsets[a.n_requests] = static_cast<int32_t>(a.n_tokens);
+    a.counts[0] = static_cast<int32_t>(total.blocks);
+    a.counts[1] = static_cast<int32_t>(total.pieces);
+  }
+  __syncthreads();
+  const uint32_t from = blockIdx.x * PLAN_THREADS + threadIdx.x, stride = gridDim.x * PLAN_THREADS;
+  for (uint64_t t = from; t < a.n_tokens; t += stride) {
+    const uint32_t r = plan_find(offsets, 0, a.n_requests, static_cast<uint32_t>(t));
+    plan_token(a, static_cast<uint32_t>(t), r, static_cast<uint32_t>(offsets[r]), bases[r]);
+  }
+  for (uint64_t i = static_cast<uint64_t>(total.pieces) + from; i < a.room; i += stride) a.pieces[i] = make_int4(-1, -1, -1, -1);
+}
+
+// For more requests the sums are one workgroup's, 8 consecutive requests per thread and round, and the tokens a launch behind it.
+constexpr uint32_t PLAN_PER = 8;
+typedef int32_t i32x4_by_words __attribute__((ext_vector_type(4), aligned(4)));
+__global__ __launch_bounds__(PLAN_THREADS) void k_plan_sums(PlanArgs a) {
+  __shared__ PlanScan scan[2];
+  if (stopped(a.status)) return;
+  PlanSums carry{0, 0, 0};
+  bool ok = true;
+  uint32_t turn = 0;
+  for (uint64_t round = 0; round < a.n_requests; round += PLAN_THREADS * PLAN_PER, turn ^= 1) {
+    const uint64_t first = round + threadIdx.x * PLAN_PER;
+    const bool whole = first + PLAN_PER <= a.n_requests;
+    int32_t cached[PLAN_PER], added[PLAN_PER];
+    if (whole) {
+#pragma unroll
+      for (uint32_t i = 0; i < PLAN_PER; i += 4) {
+        const i32x4_by_words c = *reinterpret_cast<const i32x4_by_words*>(a.cached + first + i);
+        const i32x4_by_words d = *reinterpret_cast<const i32x4_by_words*>(a.added + first + i);
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) { cached[i + j] = c[j]; added[i + j] = d[j]; }
+      }
+    } else {
+#pragma unroll
+      for (uint32_t i = 0; i < PLAN_PER; ++i) {
+        const bool there = first + i < a.n_requests;
+        cached[i] = there ? a.cached[first + i] : 0;
+        added[i] = there ? a.added[first + i] : 0;
+      }
+    }
+    PlanSums mine{0, 0, 0}, at, total;
+#pragma unroll
+    for (uint32_t i = 0; i < PLAN_PER; ++i) ok &= plan_request(a, cached[i], added[i], &mine);
+    ok = plan_scan(mine, ok, &scan[turn], &at, &total);
+    at.tokens += carry.tokens; at.blocks += carry.blocks; at.pieces += carry.pieces;
+    carry.tokens += total.tokens; carry.blocks += total.blocks; carry.pieces += total.pieces;
+#pragma unroll
+    for (uint32_t i = 0; i < PLAN_PER; i += 4) {
+      i32x4_by_words length, offset;
+      int2 base[4];
+#pragma unroll
+      for (uint32_t j = 0; j < 4; ++j) {
+        length[j] = static_cast<int32_t>(static_cast<uint32_t>(cached[i + j]) + static_cast<uint32_t>(added[i + j]));
+        offset[j] = static_cast<int32_t>(at.tokens);
+        base[j] = make_int2(static_cast<int32_t>(at.blocks), static_cast<int32_t>(at.pieces));
+        plan_request(a, cached[i + j], added[i + j], &at);
+      }
+      if (whole) {
+        *reinterpret_cast<i32x4_by_words*>(a.lengths + first + i) = length;
+        *reinterpret_cast<i32x4_by_words*>(a.token_offsets + first + i) = offset;
+        int4* to = reinterpret_cast<int4*>(a.bases + first + i);
+        to[0] = make_int4(base[0].x, base[0].y, base[1].x, base[1].y);
+        to[1] = make_int4(base[2].x, base[2].y, base[3].x, base[3].y);
+      } else {
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j)
+          if (first + i + j < a.n_requests) {
+            a.lengths[first + i + j] = length[j];
+            a.token_offsets[first + i + j] = offset[j];
+            a.bases[first + i + j] = base[j];
+          }
+      }
+    }
+  }
+  if (threadIdx.x == 0) {
+    if (const int32_t error = plan_error(a, carry, ok)) *a.status = error;
+    a.token_offsets[a.n_requests] = static_cast<int32_t>(a.n_tokens);
+    a.counts[0] = static_cast<int32_t>(carry.blocks);
+    a.counts[1] = static_cast<int32_t>(carry.pieces);
+  }
+}
+
 __global__ __launch_bounds__(256) void k_plan_tokens(PlanArgs a) {
   if (stopped(a.status)) return;
   const uint32_t t = blockIdx.x * 256 + threadIdx.x;
-  if (t < a.n_tokens) plan_token(a, t, plan_find(a.token_offsets, 0, a.n_requests, t));
-  const uint32_t n_pieces = static_cast<uint32_t>(a.counts[1]);
-  for (uint64_t i = static_cast<uint64_t>(n_pieces) + t; i < a.room; i += static_cast<uint64_t>(gridDim.x) * 256)
+  if (t < a.n_tokens) {
+    const uint32_t r = plan_find(a.token_offsets, 0, a.n_requests, t);
+    plan_token(a, t, r, static_cast<uint32_t>(a.token_offsets[r]), a.bases[r]);
+  }
+  for (uint64_t i = static_cast<uint64_t>(static_cast<uint32_t>(a.counts[1])) + t; i < a.room; i += static_cast<uint64_t>(gridDim.x) * 256)
     a.pieces[i] = make_int4(-1, -1, -1, -1);
 }
 
 // ---- append -----------------------------------------------------------------------------------------------------
 //
-// A piece lies in one block, so the largest magnitude of its values, the block's exponent and the codes belong to one
-// workgroup per piece, head, and keys or values.  Memory bound: 2 bytes read and 1 written per value.
+// A piece lies in one block, so the largest magnitude of its values, the block's exponent and the codes belong to one wave
+// per piece, head, and keys or values.  It reads the values once and holds up to 8192 of them (64 tokens of 128) in registers
+// between the maximum and the rounding; of longer pieces it reads them again, from the cache.  Memory bound: 2 bytes read and 1
+// written per value, and half an instruction each for the maximum (of pairs, as integers) and for the rounding of a pair.
 
 struct AppendArgs {
   fikit_cache cache;
@@ -143,7 +251,7 @@ struct AppendArgs {
   uint32_t n_tokens;
 };
 
-constexpr int APPEND_THREADS = 256;
+constexpr int APPEND_WAVES = 4, APPEND_HOLD = 16;   // (pieces of eight values per lane)
 
 // Two values as codes, in the low 16 bits.
 __device__ __forceinline__ uint32_t codes_of(float a, float b) {
@@ -160,13 +268,16 @@ __device__ __forceinline__ uint32_t exponent_for(float most) {
   return x < 1 ? 1u : static_cast<uint32_t>(x);
 }
 
-template <typename T, int D, int CHUNKS>   // CHUNKS: eight values each that a thread holds
-__global__ __launch_bounds__(APPEND_THREADS) void k_cache_append(AppendArgs a) {
-  __shared__ float wave_most[APPEND_THREADS / WAVE];
-  if (stopped(a.status)) return;
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t most_of_pairs(uint32_t a, uint32_t b) {
+  return bits_as<uint32_t>(__builtin_elementwise_max(bits_as<u16x2>(a), bits_as<u16x2>(b)));
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(APPEND_WAVES * WAVE) void k_cache_append(AppendArgs a) {
   const int4 piece = a.pieces[blockIdx.x];
-  if (piece.x == -1) return;
-  const uint32_t head = blockIdx.y, block_tokens = a.cache.block_tokens;
+  if (piece.x == -1 || stopped(a.status)) return;
+  const uint32_t lane = lane_id(), unit = blockIdx.y * APPEND_WAVES + uniform(threadIdx.x / WAVE), block_tokens = a.cache.block_tokens;
   const uint32_t block = static_cast<uint32_t>(piece.x), first = static_cast<uint32_t>(piece.y), at = static_cast<uint32_t>(piece.z),
                  count = static_cast<uint32_t>(piece.w);
   if (block >= a.cache.n_blocks || at >= block_tokens || count == 0 || count > block_tokens - at || first >= a.n_tokens ||
@@ -174,53 +285,80 @@ __global__ __launch_bounds__(APPEND_THREADS) void k_cache_append(AppendArgs a) {
     if (threadIdx.x == 0) *a.status = FIKIT_INVALID_ARG;
     return;
   }
-  const bool values = blockIdx.z != 0;
+  if (unit >= 2 * a.cache.kv_heads) return;
+  const bool values = unit >= a.cache.kv_heads;
+  const uint32_t head = values ? unit - a.cache.kv_heads : unit;
   const fikit_vectors in = values ? a.v : a.k;
   const uint16_t* x = static_cast<const uint16_t*>(in.d_data) + first * in.token_stride + head * in.head_stride;
-  const uint64_t unit = static_cast<uint64_t>(block) * a.cache.kv_heads + head;
-  uint8_t* codes = (values ? a.cache.d_v : a.cache.d_k) + unit * block_tokens * D;
-  uint8_t* exponent = (values ? a.cache.d_v_exp : a.cache.d_k_exp) + unit;
+  const uint64_t place = static_cast<uint64_t>(block) * a.cache.kv_heads + head;
+  uint8_t* codes = (values ? a.cache.d_v : a.cache.d_k) + place * block_tokens * D;
+  uint8_t* exponent = (values ? a.cache.d_v_exp : a.cache.d_k_exp) + place;
   const uint32_t old = at > 0 ? min_u32(*exponent, 254u) : 0;
 
-  constexpr uint32_t PER_TOKEN = D / 8;
-  u32x4 held[CHUNKS];
-  float most = 0.f;
+  constexpr uint32_t PER_TOKEN = D / 8, ROUND = APPEND_HOLD * WAVE;
+  const uint32_t chunks = count * PER_TOKEN;
+  u32x4 held[APPEND_HOLD];
+  auto read = [&](uint32_t round) {
 #pragma unroll
-  for (int i = 0; i < CHUNKS; ++i) {
-    const uint32_t c = i * APPEND_THREADS + threadIdx.x, token = c / PER_TOKEN;
-    held[i] = u32x4{0, 0, 0, 0};
-    if (token < count) held[i] = *reinterpret_cast<const u32x4*>(x + token * in.token_stride + c % PER_TOKEN * 8);
+    for (uint32_t i = 0; i < APPEND_HOLD; ++i) {
+      held[i] = u32x4{0, 0, 0, 0};
+      if (round + i * WAVE < chunks) {
+        const uint32_t c = round + i * WAVE + lane;
+        if (c < chunks) held[i] = *reinterpret_cast<const u32x4*>(x + c / PER_TOKEN * in.token_stride + c % PER_TOKEN * 8);
+      }
+    }
+  };
+  uint32_t pairs = 0;               // largest magnitudes of even and of odd values, as the bits of their type
+  for (uint32_t round = 0; round < chunks; round += ROUND) {
+    read(round);
+#pragma unroll
+    for (uint32_t i = 0; i < APPEND_HOLD; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) pairs = most_of_pairs(pairs, held[i][j] & 0x7fff7fffu);
   }
+  uint32_t bits = max_u32(pairs & 0xffffu, pairs >> 16);
+  for (int d = 1; d < WAVE; d <<= 1) bits = max_u32(bits, __shfl_xor(bits, d, WAVE));
+  const bool odd = bits >= T::INF;  // something is not finite: look again, without it
+  if (odd) {
+    bits = 0;
+    for (uint32_t round = 0; round < chunks; round += ROUND) {
+      if (chunks > ROUND) read(round);
 #pragma unroll
-  for (int i = 0; i < CHUNKS; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const float lo = fabsf(T::low(held[i][j])), hi = fabsf(T::high(held[i][j]));
-      most = fmaxf(most, lo < __builtin_huge_valf() ? lo : 0.f);
-      most = fmaxf(most, hi < __builtin_huge_valf() ? hi : 0.f);
+      for (uint32_t i = 0; i < APPEND_HOLD; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t lo = held[i][j] & 0x7fffu, hi = held[i][j] >> 16 & 0x7fffu;
+          bits = max_u32(bits, max_u32(lo < T::INF ? lo : 0, hi < T::INF ? hi : 0));
+        }
     }
-  for (int d = 1; d < WAVE; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, WAVE));
-  if (lane_id() == 0) wave_most[threadIdx.x / WAVE] = most;
-  __syncthreads();
-  most = fmaxf(fmaxf(wave_most[0], wave_most[1]), fmaxf(wave_most[2], wave_most[3]));
-  uint32_t chosen = exponent_for(most);
-  if (old > chosen) chosen = old;
-  const float inverse = power_of(254 - chosen);
+    for (int d = 1; d < WAVE; d <<= 1) bits = max_u32(bits, __shfl_xor(bits, d, WAVE));
+  }
+  const uint32_t chosen = max_u32(exponent_for(T::low(bits)), old);
+  const float scale = power_of(chosen), inverse = power_of(254 - chosen);
 
+  for (uint32_t round = 0; round < chunks; round += ROUND) {
+    if (chunks > ROUND) read(round);
 #pragma unroll
-  for (int i = 0; i < CHUNKS; ++i) {
-    const uint32_t c = i * APPEND_THREADS + threadIdx.x, token = c / PER_TOKEN;
-    u32x2 out;
-    for (int j = 0; j < 2; ++j) {
-      const uint32_t p = held[i][2 * j], q = held[i][2 * j + 1];
-      out[j] = codes_of(finite_or_nan(T::low(p)) * inverse, finite_or_nan(T::high(p)) * inverse) |
-               codes_of(finite_or_nan(T::low(q)) * inverse, finite_or_nan(T::high(q)) * inverse) << 16;
+    for (uint32_t i = 0; i < APPEND_HOLD; ++i) {
+      if (round + i * WAVE >= chunks) break;
+      const uint32_t c = round + i * WAVE + lane;
+      u32x2 out;
+      if (odd) {
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t p = held[i][2 * j], q = held[i][2 * j + 1];
+          out[j] = codes_of(finite_or_nan(T::low(p)) * inverse, finite_or_nan(T::high(p)) * inverse) |
+                   codes_of(finite_or_nan(T::low(q)) * inverse, finite_or_nan(T::high(q)) * inverse) << 16;
+        }
+      } else {
+        for (int j = 0; j < 2; ++j) out[j] = T::codes_of_pairs(held[i][2 * j], held[i][2 * j + 1], scale);
+      }
+      if (c < chunks) *reinterpret_cast<u32x2*>(codes + at * D + c * 8) = out;
     }
-    if (token < count) *reinterpret_cast<u32x2*>(codes + (at + token) * D + c % PER_TOKEN * 8) = out;
   }
   // earlier tokens of the block: the same values to a larger scale (old 0: a block that nothing has been put into)
   if (at > 0 && chosen != old) {
     const float down = old + 126 < chosen ? 0.f : power_of(127 + old - chosen);
-    for (uint32_t c = threadIdx.x; c < at * D / 16; c += APPEND_THREADS) {
+    for (uint32_t c = lane; c < at * D / 16; c += WAVE) {
       u32x4 w = *reinterpret_cast<const u32x4*>(codes + c * 16);
       for (int j = 0; j < 4; ++j) {
         const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(w[j]), false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(w[j]), true);
@@ -229,7 +367,7 @@ __global__ __launch_bounds__(APPEND_THREADS) void k_cache_append(AppendArgs a) {
       *reinterpret_cast<u32x4*>(codes + c * 16) = w;
     }
   }
-  if (threadIdx.x == 0) *exponent = static_cast<uint8_t>(chosen);
+  if (lane == 0) *exponent = static_cast<uint8_t>(chosen);
 }
 
 }  // namespace fikit

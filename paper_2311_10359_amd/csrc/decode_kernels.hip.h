@@ -26,11 +26,33 @@ struct DecodeArgs {
   void* out;
   float* lse;
   int32_t* status;
-  float* part_out;         // [request][part][q head][D]
-  float2* part_sums;       // [request][part][q head]: maximum (of scores times log2 e), sum
-  uint32_t q_heads, table_width, max_length, parts, part_tokens, head_tiles, n_requests;
+  uint2* spans;            // [request]: first part, number of parts
+  float2* part_sums;       // [part][q head]: maximum (of scores times log2 e), sum
+  float* part_out;         // [part][q head][D]
+  uint32_t q_heads, table_width, max_length, head_tiles, n_requests;
+  uint32_t parts;          // most parts of all requests together
+  uint32_t per_request;    // 0: see k_decode; else so many parts for each request, of part_tokens
+  uint32_t part_tokens;
   float scale;
 };
+
+// How contexts are cut into parts.  A part is a workgroup's for each key head and tile of query heads; many parts fill the chip
+// and end together, few need less joining: a part's result is 4 G bytes a dimension (G query heads to a key head), written and
+// read, for 2 part_tokens bytes of keys and values.  So with `units` key heads and tiles:
+//   DECODE_GROUPS workgroups, of at least 64 G tokens each, but DECODE_FEW workgroups before that counts;
+//   DECODE_LEAST to DECODE_MOST tokens (a wave's quarter holds at most 64 blocks).
+constexpr uint32_t DECODE_GROUPS = 4096, DECODE_FEW = 512, DECODE_LEAST = 128, DECODE_MOST = 4096;
+// Up to so many requests each workgroup looks at all lengths; for more, every request is cut alike, into parts of DECODE_MOST.
+constexpr uint32_t DECODE_LOOK = 1024;
+
+__host__ __device__ inline uint32_t decode_part_tokens(uint64_t tokens, uint32_t units, uint32_t rows) {
+  uint64_t least = 64ull * rows;
+  if (least > tokens * units / DECODE_FEW) least = tokens * units / DECODE_FEW;
+  uint64_t part = (tokens * units + DECODE_GROUPS - 1) / DECODE_GROUPS;
+  if (part < least) part = least;
+  part = (part + DECODE_LEAST - 1) / DECODE_LEAST * DECODE_LEAST;
+  return static_cast<uint32_t>(part < DECODE_LEAST ? DECODE_LEAST : part > DECODE_MOST ? DECODE_MOST : part);
+}
 
 constexpr int DECODE_WAVES = 4, DECODE_ROWS = 16, DECODE_STEP = 32;
 constexpr float DECODE_SLACK = 8.f;   // log2 of how far a weight may pass 1 before the maximum is raised
@@ -41,38 +63,118 @@ struct DecodeStep {
   uint32_t v[8][D / 64];     // D / 16 codes of each of eight values
 };
 
+// The item-th part, counting through the requests: every workgroup adds up all lengths for itself, which fixes the parts' size,
+// and then the requests' parts.  False if there are fewer parts or the call has failed.
+struct DecodeLook {
+  uint64_t tokens[DECODE_WAVES];
+  uint32_t parts[DECODE_WAVES];
+  uint32_t request, part, n_parts, length;
+};
+
+__device__ __forceinline__ bool decode_find(const DecodeArgs& a, uint32_t item, uint32_t units, uint32_t rows, DecodeLook* lds, uint32_t* request,
+                                            uint32_t* part, uint32_t* part_tokens, uint32_t* n_parts, uint32_t* length) {
+  constexpr uint32_t PER = DECODE_LOOK / (DECODE_WAVES * WAVE);
+  const uint32_t per = (a.n_requests + DECODE_WAVES * WAVE - 1) / (DECODE_WAVES * WAVE), first = threadIdx.x * per;
+  const bool stop = stopped(a.status);
+  uint32_t lengths[PER];
+  uint64_t tokens = 0;
+  bool ok = !stop;
+#pragma unroll
+  for (uint32_t i = 0; i < PER; ++i) {
+    const bool there = i < per && first + i < a.n_requests;
+    const int32_t n = there ? a.lengths[first + i] : 0;
+    lengths[i] = static_cast<uint32_t>(n);
+    if (n < 0 || lengths[i] > a.max_length) ok = false; else tokens += lengths[i];
+  }
+  const uint32_t wave = threadIdx.x / WAVE;
+  for (int d = 1; d < WAVE; d <<= 1) tokens += shfl_xor_u64(tokens, d);
+  if (lane_id() == 0) lds->tokens[wave] = tokens;
+  if (threadIdx.x == 0) lds->request = 0xffffffffu;
+  if (!__syncthreads_and(ok)) {
+    if (threadIdx.x == 0 && !stop) *a.status = FIKIT_INVALID_ARG;
+    return false;
+  }
+  tokens = 0;
+  for (int w = 0; w < DECODE_WAVES; ++w) tokens += lds->tokens[w];
+  const uint32_t size = decode_part_tokens(tokens, units, min_u32(rows, DECODE_ROWS));
+  uint32_t count[PER], mine = 0;
+#pragma unroll
+  for (uint32_t i = 0; i < PER; ++i) {
+    const bool there = i < per && first + i < a.n_requests;
+    count[i] = !there ? 0 : lengths[i] == 0 ? 1 : (lengths[i] + size - 1) / size;
+    mine += count[i];
+  }
+  uint32_t before = mine;
+  for (int d = 1; d < WAVE; d <<= 1) {
+    const uint32_t x = __shfl_up(before, d, WAVE);
+    if (lane_id() >= static_cast<uint32_t>(d)) before += x;
+  }
+  if (lane_id() == WAVE - 1) lds->parts[wave] = before;
+  __syncthreads();
+  before -= mine;
+  for (uint32_t w = 0; w < wave; ++w) before += lds->parts[w];
+#pragma unroll
+  for (uint32_t i = 0; i < PER; ++i) {
+    if (item >= before && item - before < count[i]) {
+      lds->request = first + i;
+      lds->part = item - before;
+      lds->n_parts = count[i];
+      lds->length = lengths[i];
+    }
+    before += count[i];
+  }
+  __syncthreads();
+  *request = uniform(lds->request);
+  *part = uniform(lds->part);
+  *part_tokens = uniform(size);
+  *n_parts = uniform(lds->n_parts);
+  *length = uniform(lds->length);
+  return *request != 0xffffffffu;
+}
+
 template <typename T, int D>
 __global__ __launch_bounds__(DECODE_WAVES * WAVE) void k_decode(DecodeArgs a) {
   constexpr int KV_WORDS = D / 64;
   __shared__ float joined[DECODE_WAVES][DECODE_ROWS][D + 4];
   __shared__ float2 sums[DECODE_WAVES][DECODE_ROWS];
-  if (stopped(a.status)) return;
+  __shared__ DecodeLook look;
   const uint32_t head_units = a.cache.kv_heads * a.head_tiles;
-  const uint32_t unit = blockIdx.x % head_units, rest = blockIdx.x / head_units;
-  const uint32_t part = rest % a.parts, request = rest / a.parts;
+  const uint32_t unit = blockIdx.x % head_units, item = blockIdx.x / head_units;
   const uint32_t kv_head = unit / a.head_tiles, tile = unit % a.head_tiles;
   const uint32_t group = a.q_heads / a.cache.kv_heads;
   const uint32_t rows = min_u32(group - tile * DECODE_ROWS, DECODE_ROWS), first_head = kv_head * group + tile * DECODE_ROWS;
   const uint32_t shift = __builtin_ctz(a.cache.block_tokens);
-  const int32_t signed_length = a.lengths[request];
-  const uint32_t length = static_cast<uint32_t>(signed_length);
-  if (signed_length < 0 || length > a.max_length) {
-    if (threadIdx.x == 0) *a.status = FIKIT_INVALID_ARG;
+  const uint32_t lane = lane_id(), wave = uniform(threadIdx.x / WAVE), col = lane % 16, quarter = lane / 16;
+  // which part of which request
+  uint32_t request, part, part_tokens, n_parts, length;
+  if (a.per_request) {
+    if (stopped(a.status)) return;
+    request = item / a.per_request;
+    part = item % a.per_request;
+    part_tokens = a.part_tokens;
+    const int32_t signed_length = a.lengths[request];
+    length = static_cast<uint32_t>(signed_length);
+    if (signed_length < 0 || length > a.max_length) {
+      if (threadIdx.x == 0) *a.status = FIKIT_INVALID_ARG;
+      return;
+    }
+    n_parts = length == 0 ? 1 : (length + part_tokens - 1) / part_tokens;
+    if (part >= n_parts) return;
+    if (part == 0 && unit == 0 && threadIdx.x == 0) a.spans[request] = make_uint2(item, n_parts);
+  } else {
+    if (!decode_find(a, item, head_units, group, &look, &request, &part, &part_tokens, &n_parts, &length)) return;
+    if (part == 0 && unit == 0 && threadIdx.x == 0) a.spans[request] = make_uint2(item, n_parts);
+  }
+  const uint32_t from = part * part_tokens;
+  if (length == 0) {
+    for (uint32_t i = threadIdx.x; i < rows * D; i += DECODE_WAVES * WAVE) {
+      const uint64_t row = static_cast<uint64_t>(request) * a.q_heads + first_head + i / D;
+      static_cast<uint16_t*>(a.out)[row * D + i % D] = 0;
+      if (a.lse && i % D == 0) a.lse[row] = -__builtin_huge_valf();
+    }
     return;
   }
-  const uint32_t lane = lane_id(), wave = threadIdx.x / WAVE, col = lane % 16, quarter = lane / 16;
-  const bool alone = length <= a.part_tokens;       // no other part: the outputs are written here
-  const uint32_t from = part * a.part_tokens;
-  if (from >= length) {
-    if (length == 0 && part == 0)
-      for (uint32_t i = threadIdx.x; i < rows * D; i += DECODE_WAVES * WAVE) {
-        const uint64_t row = static_cast<uint64_t>(request) * a.q_heads + first_head + i / D;
-        static_cast<uint16_t*>(a.out)[row * D + i % D] = 0;
-        if (a.lse && i % D == 0) a.lse[row] = -__builtin_huge_valf();
-      }
-    return;
-  }
-  const uint32_t until = min_u32(length, from + a.part_tokens);
+  const uint32_t until = min_u32(length, from + part_tokens);
   // this wave's quarter, in whole steps
   const uint32_t per_wave = ((until - from + DECODE_WAVES - 1) / DECODE_WAVES + DECODE_STEP - 1) / DECODE_STEP * DECODE_STEP;
   const uint32_t begin = from + wave * per_wave, end = min_u32(begin + per_wave, until);
@@ -237,50 +339,77 @@ __global__ __launch_bounds__(DECODE_WAVES * WAVE) void k_decode(DecodeArgs a) {
       x += *reinterpret_cast<const f32x4*>(&joined[w][row][dim]) * f;
     }
     const uint64_t head = static_cast<uint64_t>(request) * a.q_heads + first_head + row;
-    if (alone) {
+    if (n_parts == 1) {
       const float f = total > 0.f ? 1.f / total : total == 0.f ? 1.f : total;
       const u32x2 w = {T::pair(x[0] * f, x[1] * f), T::pair(x[2] * f, x[3] * f)};
       *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + head * D + dim) = w;
       if (dim == 0 && a.lse) a.lse[head] = (most + log2f(total)) * LN2;
     } else {
-      const uint64_t slot = (static_cast<uint64_t>(request) * a.parts + part) * a.q_heads + first_head + row;
+      const uint64_t slot = static_cast<uint64_t>(item) * a.q_heads + first_head + row;
       *reinterpret_cast<f32x4*>(a.part_out + slot * D + dim) = x;
       if (dim == 0) a.part_sums[slot] = make_float2(most, total);
     }
   }
 }
 
-// Joins the parts of one request and query head, always in the same order; a wave each.
+// Joins the parts of one request and query head, always in the same order: each wave every fourth part, then the waves.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void k_decode_join(DecodeArgs a) {
+__global__ __launch_bounds__(DECODE_WAVES * WAVE) void k_decode_join(DecodeArgs a) {
+  __shared__ float2 sums[DECODE_WAVES];
+  __shared__ float outs[DECODE_WAVES][D];
   if (stopped(a.status)) return;
-  const uint64_t head = static_cast<uint64_t>(blockIdx.x) * 4 + threadIdx.x / WAVE;
-  if (head >= static_cast<uint64_t>(a.n_requests) * a.q_heads) return;
-  const uint64_t request = head / a.q_heads, q_head = head % a.q_heads;
-  const uint32_t length = static_cast<uint32_t>(a.lengths[request]);
-  if (length <= a.part_tokens || length > a.max_length) return;
-  const uint32_t parts = (length + a.part_tokens - 1) / a.part_tokens;
-  const uint32_t lane = lane_id();
-  constexpr int PER = D / WAVE;
-  const float2* sums = a.part_sums + request * a.parts * a.q_heads + q_head;
-  const float* part = a.part_out + (request * a.parts * a.q_heads + q_head) * D + lane * PER;
-  float most = -__builtin_huge_valf();
-  for (uint32_t p = lane; p < parts; p += WAVE) most = fmaxf(most, sums[static_cast<uint64_t>(p) * a.q_heads].x);
-  for (int d = 1; d < WAVE; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, WAVE));
-  const float origin = most > -__builtin_huge_valf() ? most : 0.f;
-  float total = 0.f, x[PER];
+  const uint64_t head = blockIdx.x;
+  const uint32_t request = blockIdx.x / a.q_heads, q_head = blockIdx.x % a.q_heads;
+  const uint2 span = a.spans[request];
+  if (span.y <= 1 || span.y > a.parts || span.x > a.parts - span.y) return;
+  const uint32_t lane = lane_id(), wave = uniform(threadIdx.x / WAVE);
+  constexpr int PER = D / WAVE, MANY = 8;
+  const uint64_t at = static_cast<uint64_t>(span.x) * a.q_heads + q_head;
+  const float2* from = a.part_sums + at;
+  const float* part = a.part_out + at * D + lane * PER;
+  float most = -__builtin_huge_valf(), total = 0.f, x[PER];
   for (int i = 0; i < PER; ++i) x[i] = 0.f;
-  for (uint32_t p = 0; p < parts; ++p) {
-    const float2 s = sums[static_cast<uint64_t>(p) * a.q_heads];
-    const float f = exp2_fast(s.x - origin);
-    total += s.y * f;
-    for (int i = 0; i < PER; ++i) x[i] += part[static_cast<uint64_t>(p) * a.q_heads * D + i] * f;
+  for (uint32_t p = wave; p < span.y; p += DECODE_WAVES * MANY) {
+    float2 s[MANY];
+    float y[MANY][PER];
+#pragma unroll
+    for (int j = 0; j < MANY; ++j) {
+      const uint64_t q = min_u32(p + j * DECODE_WAVES, span.y - 1);
+      s[j] = from[q * a.q_heads];
+      for (int i = 0; i < PER; ++i) y[j][i] = part[q * a.q_heads * D + i];
+    }
+    float top = most;
+#pragma unroll
+    for (int j = 0; j < MANY; ++j) top = fmaxf(top, s[j].x);
+    const float origin = top > -__builtin_huge_valf() ? top : 0.f, down = exp2_fast(most - origin);
+    total *= down;
+    for (int i = 0; i < PER; ++i) x[i] *= down;
+#pragma unroll
+    for (int j = 0; j < MANY; ++j) {
+      if (p + j * DECODE_WAVES >= span.y) continue;
+      const float f = exp2_fast(s[j].x - origin);
+      total += s[j].y * f;
+      for (int i = 0; i < PER; ++i) x[i] += y[j][i] * f;
+    }
+    most = top;
   }
-  const float f = total > 0.f ? 1.f / total : total == 0.f ? 1.f : total;
-  uint16_t* out = static_cast<uint16_t*>(a.out) + head * D + lane * PER;
-  if constexpr (PER == 2) *reinterpret_cast<uint32_t*>(out) = T::pair(x[0] * f, x[1] * f);
-  else *out = static_cast<uint16_t>(T::pair(x[0] * f, 0.f));
-  if (lane == 0 && a.lse) a.lse[head] = (most + log2f(total)) * LN2;
+  if (lane == 0) sums[wave] = make_float2(most, total);
+  for (int i = 0; i < PER; ++i) outs[wave][lane * PER + i] = x[i];
+  __syncthreads();
+  if (threadIdx.x >= D / 2) return;
+  float top = -__builtin_huge_valf();
+  for (int w = 0; w < DECODE_WAVES; ++w) top = fmaxf(top, sums[w].x);
+  const float origin = top > -__builtin_huge_valf() ? top : 0.f;
+  float sum = 0.f, lo = 0.f, hi = 0.f;
+  for (int w = 0; w < DECODE_WAVES; ++w) {
+    const float f = exp2_fast(sums[w].x - origin);
+    sum += sums[w].y * f;
+    lo += outs[w][2 * threadIdx.x] * f;
+    hi += outs[w][2 * threadIdx.x + 1] * f;
+  }
+  const float f = sum > 0.f ? 1.f / sum : sum == 0.f ? 1.f : sum;
+  reinterpret_cast<uint32_t*>(a.out)[head * (D / 2) + threadIdx.x] = T::pair(lo * f, hi * f);
+  if (threadIdx.x == 0 && a.lse) a.lse[head] = (top + log2f(sum)) * LN2;
 }
 
 }  // namespace fikit

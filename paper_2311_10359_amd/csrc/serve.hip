@@ -14,6 +14,7 @@ using namespace fikit;
 
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
+constexpr uint32_t PLAN_ONE_GROUPS = 512;         // two for each CU
 constexpr uint64_t MOST_GROUPS = 0x7fffffffull;   // workgroups of a launch
 
 template <typename... P, typename... A>
@@ -46,58 +47,58 @@ int with_types(int32_t value_type, uint32_t head_dim, F f) {
 
 bool type_ok(int32_t value_type) { return value_type == FIKIT_BF16 || value_type == FIKIT_F16; }
 
-template <typename T, int D>
-int append_enqueue(const AppendArgs& a, uint32_t n_pieces, hipStream_t st) {
-  const dim3 grid(n_pieces, a.cache.kv_heads, 2), block(APPEND_THREADS);
-  switch (a.cache.block_tokens * D / 8 / APPEND_THREADS) {
-    case 0: case 1: return enqueue(k_cache_append<T, D, 1>, grid, block, st, a);
-    case 2: return enqueue(k_cache_append<T, D, 2>, grid, block, st, a);
-    case 4: return enqueue(k_cache_append<T, D, 4>, grid, block, st, a);
-    case 8: return enqueue(k_cache_append<T, D, 8>, grid, block, st, a);
-    default: return enqueue(k_cache_append<T, D, 16>, grid, block, st, a);
-  }
-}
 struct AppendCall {
   const AppendArgs& a;
   uint32_t n_pieces;
   hipStream_t st;
   template <typename T, int D>
-  int operator()() { return append_enqueue<T, D>(a, n_pieces, st); }
+  int operator()() {
+    return enqueue(k_cache_append<T, D>, dim3(n_pieces, (2 * a.cache.kv_heads + APPEND_WAVES - 1) / APPEND_WAVES), dim3(APPEND_WAVES * WAVE), st, a);
+  }
 };
 
-// How the contexts of a decode step are cut into parts: as many as give every part some 128 tokens at least and the chip
-// some 2048 workgroups.  A wave's quarter of a part must not hold more than 64 blocks.
+// How a decode step is cut up, as far as the host knows it (see decode_part_tokens), and its workspace.
 struct DecodeCut {
-  uint32_t head_tiles, part_tokens, parts;
-  uint64_t groups;
+  uint32_t head_tiles, per_request, part_tokens;
+  uint64_t parts, groups;
+  uint64_t spans_bytes, sums_bytes, bytes;
+  bool joins;                // some request may have several parts
 };
-constexpr uint32_t DECODE_MOST_PART = 4096, DECODE_LEAST_PART = 128;
-constexpr uint64_t DECODE_GROUPS = 2048;
 
-DecodeCut decode_cut(uint32_t n_requests, uint32_t q_heads, uint32_t kv_heads, uint32_t max_length) {
-  DecodeCut c;
+DecodeCut decode_cut(uint32_t n_requests, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim, uint32_t max_length) {
+  DecodeCut c{};
+  const auto whole = [](uint64_t v) { return (v + 255) / 256 * 256; };
   c.head_tiles = (q_heads / kv_heads + DECODE_ROWS - 1) / DECODE_ROWS;
-  const uint64_t units = static_cast<uint64_t>(n_requests) * kv_heads * c.head_tiles;
-  uint64_t part = (units * max_length + DECODE_GROUPS - 1) / DECODE_GROUPS;
-  part = (part + DECODE_LEAST_PART - 1) / DECODE_LEAST_PART * DECODE_LEAST_PART;
-  c.part_tokens = static_cast<uint32_t>(part < DECODE_LEAST_PART ? DECODE_LEAST_PART : part > DECODE_MOST_PART ? DECODE_MOST_PART : part);
-  c.parts = max_length == 0 ? 1 : (max_length + c.part_tokens - 1) / c.part_tokens;
+  const uint64_t units = static_cast<uint64_t>(kv_heads) * c.head_tiles;
+  if (n_requests > DECODE_LOOK) {
+    c.part_tokens = DECODE_MOST;
+    c.per_request = max_length <= DECODE_MOST ? 1 : (max_length + DECODE_MOST - 1) / DECODE_MOST;
+    c.parts = static_cast<uint64_t>(n_requests) * c.per_request;
+    c.joins = c.per_request > 1;
+  } else {
+    // a request has one part, and one more for each whole part_tokens of all tokens
+    const uint64_t by_groups = (DECODE_GROUPS + units - 1) / units, by_most = static_cast<uint64_t>(n_requests) * max_length / DECODE_MOST;
+    const uint64_t by_least = static_cast<uint64_t>(n_requests) * (max_length / DECODE_LEAST + 1);
+    c.parts = (by_groups > by_most ? by_groups : by_most) + n_requests;
+    if (c.parts > by_least) c.parts = by_least;
+    c.joins = max_length > DECODE_LEAST;
+  }
   c.groups = units * c.parts;
+  c.spans_bytes = whole(n_requests * sizeof(uint2));
+  c.sums_bytes = whole(c.parts * q_heads * sizeof(float2));
+  c.bytes = c.spans_bytes + (c.joins ? c.sums_bytes + c.parts * q_heads * head_dim * sizeof(float) : 0);
   return c;
 }
 
-uint64_t part_sums_bytes(uint64_t rows) { return (rows * sizeof(float2) + 255) / 256 * 256; }
-
 struct DecodeCall {
   const DecodeArgs& a;
-  uint32_t groups;
+  const DecodeCut& c;
   hipStream_t st;
   template <typename T, int D>
   int operator()() {
-    if (int rc = enqueue(k_decode<T, D>, dim3(groups), dim3(DECODE_WAVES * WAVE), st, a)) return rc;
-    if (a.parts == 1) return FIKIT_OK;
-    const uint64_t heads = static_cast<uint64_t>(a.n_requests) * a.q_heads;
-    return enqueue(k_decode_join<T, D>, dim3(static_cast<uint32_t>((heads + 3) / 4)), dim3(256), st, a);
+    if (int rc = enqueue(k_decode<T, D>, dim3(static_cast<uint32_t>(c.groups)), dim3(DECODE_WAVES * WAVE), st, a)) return rc;
+    if (!c.joins) return FIKIT_OK;
+    return enqueue(k_decode_join<T, D>, dim3(a.n_requests * a.q_heads), dim3(DECODE_WAVES * WAVE), st, a);
   }
 };
 
@@ -120,15 +121,16 @@ uint64_t fikit_cache_pieces(uint32_t n_tokens, uint32_t n_requests, uint32_t blo
   return cut < n_tokens ? cut : n_tokens;
 }
 
-size_t fikit_cache_plan_workspace_bytes(uint32_t n_requests) { return (static_cast<size_t>(n_requests) * sizeof(int2) + 255) / 256 * 256 + 256; }
+size_t fikit_cache_plan_workspace_bytes(uint32_t n_requests) {
+  return n_requests <= PLAN_ONE_REQUESTS ? 0 : (static_cast<size_t>(n_requests) * sizeof(int2) + 255) / 256 * 256;
+}
 
 int fikit_cache_plan(const int32_t* d_cached, const int32_t* d_added, uint32_t n_requests, uint32_t n_tokens,
                      uint32_t block_tokens, int32_t* d_block_table, uint32_t table_width, const int32_t* d_free,
                      uint32_t n_free, int32_t* d_lengths, int32_t* d_token_offsets, int64_t* d_slots,
                      fikit_piece* d_pieces, int32_t* d_counts, int32_t* d_status, void* d_workspace,
                      size_t workspace_bytes, void* hip_stream) {
-  if (!d_token_offsets || !d_counts || !d_status || !d_workspace || !aligned(d_token_offsets, 4) || !aligned(d_counts, 4) ||
-      !aligned(d_status, 4) || !aligned(d_workspace, 256))
+  if (!d_token_offsets || !d_counts || !d_status || !aligned(d_token_offsets, 4) || !aligned(d_counts, 4) || !aligned(d_status, 4))
     return FIKIT_INVALID_ARG;
   if (n_requests > 0 && (!d_cached || !d_added || !d_lengths || !aligned(d_cached, 4) || !aligned(d_added, 4) || !aligned(d_lengths, 4)))
     return FIKIT_INVALID_ARG;
@@ -137,7 +139,10 @@ int fikit_cache_plan(const int32_t* d_cached, const int32_t* d_added, uint32_t n
   if (n_free > 0 && !d_free) return FIKIT_INVALID_ARG;
   if (!aligned(d_block_table, 4) || !aligned(d_free, 4) || !aligned(d_slots, 8) || !aligned(d_pieces, 16)) return FIKIT_INVALID_ARG;
   if (block_tokens < 16 || block_tokens > 256 || (block_tokens & (block_tokens - 1))) return FIKIT_UNSUPPORTED;
-  if (workspace_bytes < fikit_cache_plan_workspace_bytes(n_requests)) return FIKIT_WORKSPACE_TOO_SMALL;
+  if (const size_t need = fikit_cache_plan_workspace_bytes(n_requests)) {
+    if (!d_workspace || !aligned(d_workspace, 256)) return FIKIT_INVALID_ARG;
+    if (workspace_bytes < need) return FIKIT_WORKSPACE_TOO_SMALL;
+  }
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   PlanArgs a{};
   a.cached = d_cached;
@@ -157,6 +162,10 @@ int fikit_cache_plan(const int32_t* d_cached, const int32_t* d_added, uint32_t n
   a.n_free = n_free;
   a.room = static_cast<uint32_t>(fikit_cache_pieces(n_tokens, n_requests, block_tokens));
   a.shift = static_cast<uint32_t>(__builtin_ctz(block_tokens));
+  if (n_requests <= PLAN_ONE_REQUESTS) {
+    const uint32_t groups = (n_tokens + PLAN_THREADS - 1) / PLAN_THREADS;
+    return enqueue(k_plan_one, dim3(groups < 1 ? 1 : groups > PLAN_ONE_GROUPS ? PLAN_ONE_GROUPS : groups), dim3(PLAN_THREADS), st, a);
+  }
   if (int rc = enqueue(k_plan_sums, dim3(1), dim3(PLAN_THREADS), st, a)) return rc;
   if (n_tokens == 0) return FIKIT_OK;
   return enqueue(k_plan_tokens, dim3((n_tokens + 255) / 256), dim3(256), st, a);
@@ -183,11 +192,8 @@ int fikit_cache_append(const fikit_cache* h_cache, const fikit_vectors* h_k, con
 size_t fikit_cache_attention_workspace_bytes(uint32_t n_requests, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim,
                                              uint32_t max_length) {
   if (kv_heads == 0 || q_heads == 0 || q_heads % kv_heads || q_heads > 65535 || max_length > 0x7fffffffu || n_requests > 0x7fffffffu) return 0;
-  const DecodeCut c = decode_cut(n_requests, q_heads, kv_heads, max_length);
-  if (c.groups > MOST_GROUPS) return 0;
-  if (c.parts == 1) return 256;
-  const uint64_t rows = static_cast<uint64_t>(n_requests) * c.parts * q_heads;
-  return static_cast<size_t>(part_sums_bytes(rows) + rows * head_dim * sizeof(float));
+  const DecodeCut c = decode_cut(n_requests, q_heads, kv_heads, head_dim, max_length);
+  return c.groups > MOST_GROUPS ? 0 : static_cast<size_t>(c.bytes);
 }
 
 int fikit_cache_attention(const fikit_cache* h_cache, const fikit_vectors* h_q, uint32_t q_heads, int32_t value_type, float scale,
@@ -203,11 +209,10 @@ int fikit_cache_attention(const fikit_cache* h_cache, const fikit_vectors* h_q, 
   if (!vectors_ok(h_q) || !d_lengths || !d_out || !aligned(d_block_table, 4) || !aligned(d_lengths, 4) || !aligned(d_out, 16) ||
       !aligned(d_lse, 4) || (max_length > 0 && !d_block_table))
     return FIKIT_INVALID_ARG;
-  const DecodeCut c = decode_cut(n_requests, q_heads, h_cache->kv_heads, max_length);
-  if (c.groups > MOST_GROUPS) return FIKIT_UNSUPPORTED;
-  if (c.parts > 1 && (!d_workspace || !aligned(d_workspace, 256))) return FIKIT_INVALID_ARG;
-  if (c.parts > 1 && workspace_bytes < fikit_cache_attention_workspace_bytes(n_requests, q_heads, h_cache->kv_heads, h_cache->head_dim, max_length))
-    return FIKIT_WORKSPACE_TOO_SMALL;
+  const DecodeCut c = decode_cut(n_requests, q_heads, h_cache->kv_heads, h_cache->head_dim, max_length);
+  if (c.groups > MOST_GROUPS || static_cast<uint64_t>(n_requests) * q_heads > MOST_GROUPS) return FIKIT_UNSUPPORTED;
+  if (!d_workspace || !aligned(d_workspace, 256)) return FIKIT_INVALID_ARG;
+  if (workspace_bytes < c.bytes) return FIKIT_WORKSPACE_TOO_SMALL;
   DecodeArgs a{};
   a.cache = *h_cache;
   a.q = *h_q;
@@ -216,18 +221,20 @@ int fikit_cache_attention(const fikit_cache* h_cache, const fikit_vectors* h_q, 
   a.out = d_out;
   a.lse = d_lse;
   a.status = d_status;
-  a.part_sums = static_cast<float2*>(d_workspace);
-  if (c.parts > 1)
-    a.part_out = reinterpret_cast<float*>(static_cast<unsigned char*>(d_workspace) + part_sums_bytes(static_cast<uint64_t>(n_requests) * c.parts * q_heads));
+  unsigned char* ws = static_cast<unsigned char*>(d_workspace);
+  a.spans = reinterpret_cast<uint2*>(ws);
+  a.part_sums = reinterpret_cast<float2*>(ws + c.spans_bytes);
+  a.part_out = reinterpret_cast<float*>(ws + c.spans_bytes + c.sums_bytes);
   a.q_heads = q_heads;
   a.table_width = table_width;
   a.max_length = max_length;
-  a.parts = c.parts;
+  a.parts = static_cast<uint32_t>(c.parts);
+  a.per_request = c.per_request;
   a.part_tokens = c.part_tokens;
   a.head_tiles = c.head_tiles;
   a.n_requests = n_requests;
   a.scale = scale;
-  return with_types(value_type, h_cache->head_dim, DecodeCall{a, static_cast<uint32_t>(c.groups), static_cast<hipStream_t>(hip_stream)});
+  return with_types(value_type, h_cache->head_dim, DecodeCall{a, c, static_cast<hipStream_t>(hip_stream)});
 }
 
 int fikit_prompt_attention(const fikit_vectors* h_q, const fikit_vectors* h_k, const fikit_vectors* h_v, uint32_t q_heads,

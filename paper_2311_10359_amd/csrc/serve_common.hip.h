@@ -16,6 +16,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -27,6 +28,7 @@ __device__ __forceinline__ To bits_as(From v) {
 
 // A 16-bit value type.  `x8`: eight values, an operand of a matrix instruction.  `pair`: two 32-bit values rounded to nearest
 // even.  `codes<hi>`: two E4M3 codes, the low or the high ones of a word, times a power of two (exact, see fikit.h).
+// `codes_of_pairs`: the codes of four finite values divided by a power of two, at most 448 then.
 struct Bf16 {
   typedef bf16x8 x8;
   static constexpr uint32_t EXP_MASK = 0x7f807f80u, MANTISSA_MASK = 0x007f007fu, INF = 0x7f80u;
@@ -40,6 +42,11 @@ struct Bf16 {
   template <bool hi>
   static __device__ __forceinline__ uint32_t codes(uint32_t word, float scale) {
     return bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(word), scale, hi));
+  }
+  static __device__ __forceinline__ uint32_t codes_of_pairs(uint32_t a, uint32_t b, float scale) {
+    s16x2 w = {0, 0};
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, bits_as<bf16x2>(a), scale, false);
+    return bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, bits_as<bf16x2>(b), scale, true));
   }
   static __device__ __forceinline__ f32x4 mfma16(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ f32x16 mfma32(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
@@ -60,9 +67,17 @@ struct F16 {
   static __device__ __forceinline__ uint32_t codes(uint32_t word, float scale) {
     return bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(word), scale, hi));
   }
+  static __device__ __forceinline__ uint32_t codes_of_pairs(uint32_t a, uint32_t b, float scale) {
+    s16x2 w = {0, 0};
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(w, bits_as<f16x2>(a), scale, false);
+    return bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_fp8_f16(w, bits_as<f16x2>(b), scale, true));
+  }
   static __device__ __forceinline__ f32x4 mfma16(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ f32x16 mfma32(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
+
+// A value that is the same in the whole wave, where the compiler cannot know it.
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(v))); }
 
 // 2^(x - 127), x = 1 .. 254.
 __device__ __forceinline__ float power_of(uint32_t x) { return __uint_as_float(x << 23); }
