@@ -552,7 +552,8 @@ int fikit_cache_attention(const fikit_cache* h_cache, const fikit_vectors* h_q, 
  * n_tokens, < 2^31), and each of its tokens sees those up to itself.  What follows a token, infinities and NaN included, changes
  * nothing in its row.
  *
- *   h_q, h_k, h_v  vectors of q_heads, kv_heads and kv_heads heads; q_heads a multiple of kv_heads.
+ *   h_q, h_k, h_v  vectors of q_heads, kv_heads and kv_heads heads; q_heads a multiple of kv_heads; keys and values of
+ *                  token strides up to 2^24.
  *   head_dim       64 or 128.
  *   d_out          [n_tokens][q_heads][head_dim], of the inputs' type; d_lse [n_tokens][q_heads] float or NULL; as in
  *                  fikit_cache_attention.

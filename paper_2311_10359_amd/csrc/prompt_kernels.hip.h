@@ -29,14 +29,16 @@ struct PromptArgs {
 constexpr int PROMPT_KEYS = 64, PROMPT_WAVE_ROWS = 32;
 constexpr float PROMPT_SLACK = 8.f;
 
-typedef __attribute__((address_space(3))) uint16_t lds_u16;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char lds_char;
 
-__device__ __forceinline__ void load_to_lds(const uint16_t* from, uint16_t* to) {
+// 16 bytes per lane, to `to` and behind it in the order of the lanes.
+__device__ __forceinline__ void load_to_lds(const char* from, lds_char* to) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
-
-__device__ __forceinline__ u32x2 read_transposed(const uint16_t* at) {
+__device__ __forceinline__ u32x4 read_row(const lds_char* at) { return *(const __attribute__((address_space(3))) u32x4*)at; }
+// Of 16 lanes each that point at four rows of 16 values, lane l receives value l of the four rows.
+__device__ __forceinline__ u32x2 read_transposed(lds_char* at) {
   return bits_as<u32x2>(__builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at));
 }
 
@@ -52,197 +54,428 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
   return ((w & LO) == LO ? 0xffffu : 0u) | ((w & HI) == HI ? 0xffff0000u : 0u);
 }
 
-template <typename T, int D, int WAVES>
-__global__ __launch_bounds__(WAVES * WAVE) void k_prompt(PromptArgs a) {
-  constexpr int ROWS = WAVES * PROMPT_WAVE_ROWS, PIECES = D / 8, TILE = PROMPT_KEYS * D;
-  constexpr int LOADS = PROMPT_KEYS * PIECES / (WAVES * WAVE);
-  __shared__ __align__(16) uint16_t keys[2][TILE];
-  __shared__ __align__(16) uint16_t vals[2][TILE];
-  if (stopped(a.status)) return;
-  const uint32_t lane = lane_id(), wave = threadIdx.x / WAVE, col = lane % 32, half = lane / 32;
-  const uint32_t head = blockIdx.x % a.q_heads, slot = a.slots - 1 - blockIdx.x / a.q_heads;
-  if (blockIdx.x == 0) {
-    bool bad = a.offsets[0] != 0 || static_cast<uint32_t>(a.offsets[a.n_prompts]) != a.n_tokens;
-    for (uint32_t p = threadIdx.x; p < a.n_prompts; p += WAVES * WAVE) bad |= a.offsets[p] > a.offsets[p + 1];
-    if (bad) *a.status = FIKIT_INVALID_ARG;
-  }
-  // prompt p owns the slots from offsets[p] / ROWS + p on: enough for its rows, and found without a list
-  uint32_t prompt = 0;
-  for (uint32_t hi = a.n_prompts; hi - prompt > 1;) {
-    const uint32_t mid = prompt + (hi - prompt) / 2;
-    if (static_cast<uint32_t>(a.offsets[mid]) / ROWS + mid <= slot) prompt = mid; else hi = mid;
-  }
-  const uint32_t start = static_cast<uint32_t>(a.offsets[prompt]), stop = static_cast<uint32_t>(a.offsets[prompt + 1]);
-  if (start > stop || stop > a.n_tokens) {
-    if (threadIdx.x == 0) *a.status = FIKIT_INVALID_ARG;
-    return;
-  }
-  const uint32_t length = stop - start, first = (slot - (start / ROWS + prompt)) * ROWS;
-  if (first >= length) return;
-  const uint32_t row0 = first + wave * PROMPT_WAVE_ROWS, row = row0 + col;      // in the prompt
-  const uint32_t kv_head = head / (a.q_heads / a.kv_heads);
-  const uint32_t tiles = (min_u32(first + ROWS, length) + PROMPT_KEYS - 1) / PROMPT_KEYS;
-
-  const uint16_t* k = static_cast<const uint16_t*>(a.k.d_data) + start * a.k.token_stride + kv_head * a.k.head_stride;
-  const uint16_t* v = static_cast<const uint16_t*>(a.v.d_data) + start * a.v.token_stride + kv_head * a.v.head_stride;
-  auto fill = [&](uint32_t tile, int to) {
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const uint32_t base = (i * WAVES + wave) * WAVE, c = base + lane, r = c / PIECES, piece = c % PIECES;
-      const uint64_t token = min_u32(tile * PROMPT_KEYS + r, length - 1);       // (behind the end: the last token, masked)
-      load_to_lds(k + token * a.k.token_stride + (piece ^ key_swizzle<D>(r)) * 8, keys[to] + base * 8);
-      load_to_lds(v + token * a.v.token_stride + (piece ^ value_swizzle<D>(r)) * 8, vals[to] + base * 8);
-    }
-  };
-  fill(0, 0);
-
+template <typename T, int D>
+struct PromptWave {              // what a wave holds of its 32 rows; a lane of row lane % 32
+  static constexpr uint32_t ROW = D * 2, TILE = PROMPT_KEYS * ROW;
   typename T::x8 q[D / 16];
-  {
+  f32x16 s[2];                   // scores of the next tile, before scaling
+  f32x16 acc[D / 32];
+  float m, l;                    // reference of the weights (of scores times log2 e), sum over this lane's tokens
+  float most;                    // largest of this lane's scores, scaled
+  float scale;
+  uint32_t row;
+  uint32_t key_at, val_at;       // where this lane reads in a tile: the first place, from which the others differ in single bits
+
+  __device__ __forceinline__ void set_up(const PromptArgs& a, uint32_t start, uint32_t length, uint32_t row0, uint32_t head) {
+    const uint32_t lane = lane_id(), col = lane % 32, half = lane / 32;
+    // The largest score is found, and what is not seen masked, before scaling: that takes a scale above zero.
+    const bool flip = a.scale < 0.f, none = a.scale == 0.f;
+    scale = none ? LOG2E : fabsf(a.scale) * LOG2E;
+    row = row0 + col;
     const uint16_t* src = static_cast<const uint16_t*>(a.q.d_data) + (start + static_cast<uint64_t>(min_u32(row, length - 1))) * a.q.token_stride +
                           head * a.q.head_stride + half * 8;
 #pragma unroll
-    for (int j = 0; j < D / 16; ++j) q[j] = bits_as<typename T::x8>(*reinterpret_cast<const u32x4*>(src + j * 16));
-  }
-  f32x16 acc[D / 32];
-#pragma unroll
-  for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
-  float m = -__builtin_huge_valf(), l = 0.f;
-  const float scale = a.scale * LOG2E;
-  const uint32_t l16 = lane % 16, pair16 = (lane / 16) % 2;
-
-  for (uint32_t tile = 0; tile < tiles; ++tile) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (tile + 1 < tiles) fill(tile + 1, (tile + 1) & 1);
-    const uint32_t token0 = tile * PROMPT_KEYS;
-    if (token0 > row0 + PROMPT_WAVE_ROWS - 1) continue;        // (nothing of it is seen by this wave's rows)
-    const uint16_t* kt = keys[tile & 1];
-    const uint16_t* vt = vals[tile & 1];
-    const bool masked = token0 + PROMPT_KEYS - 1 > row0;
-    f32x16 s[2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[t][r] = 0.f;
-      const uint32_t r = t * 32 + col;
-#pragma unroll
-      for (int j = 0; j < D / 16; ++j) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(kt + r * D + ((2 * j + half) ^ key_swizzle<D>(r)) * 8);
-        s[t] = T::mfma32(bits_as<typename T::x8>(w), q[j], s[t]);
-      }
+    for (int j = 0; j < D / 16; ++j) {
+      u32x4 x = *reinterpret_cast<const u32x4*>(src + j * 16);
+      if (flip) x ^= 0x80008000u;
+      if (none) x = u32x4{0, 0, 0, 0};
+      q[j] = bits_as<typename T::x8>(x);
     }
-    float most = -__builtin_huge_valf();
+    // (a row's piece 2 j + half is stored at (2 j + half) ^ swizzle, value piece 4 d + .. likewise)
+    const uint32_t l16 = lane % 16, r = half * 4 + l16 / 4;
+    key_at = col * ROW + (half ^ key_swizzle<D>(col)) * 16;
+    val_at = r * ROW + ((2 * (lane / 16 % 2) + l16 % 4 / 2) ^ value_swizzle<D>(r)) * 16 + l16 % 2 * 8;
+  }
+  __device__ __forceinline__ void start() {
+    m = -__builtin_huge_valf();
+    l = 0.f;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
+  }
+  __device__ __forceinline__ void scores(const lds_char* keys) {
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (j == 0)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[t][r] = 0.f;
+        s[t] = T::mfma32(bits_as<typename T::x8>(read_row(keys + (key_at ^ j * 32) + t * 32 * ROW)), q[j], s[t]);
+      }
+  }
+  __device__ __forceinline__ void mask(uint32_t token0) {
+    const uint32_t half = lane_id() / 32;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[t][r] *= scale;
-        if (masked && token0 + t * 32 + r / 4 * 8 + half * 4 + r % 4 > row) s[t][r] = -__builtin_huge_valf();
-        most = fmaxf(most, s[t][r]);
-      }
+      for (int r = 0; r < 16; ++r)
+        if (token0 + t * 32 + r / 4 * 8 + half * 4 + r % 4 > row) s[t][r] = -__builtin_huge_valf();
+  }
+  __device__ __forceinline__ void find_most() {
+    float x = s[0][0];
+#pragma unroll
+    for (int i = 1; i < 31; i += 2) x = fmaxf(fmaxf(x, s[i / 16][i % 16]), s[(i + 1) / 16][(i + 1) % 16]);
+    most = fmaxf(x, s[1][15]) * scale;
+  }
+  __device__ __forceinline__ void raise() {
     if (ballot(most > m + (PROMPT_SLACK + T::WEIGHT_BIAS))) {
-      most = fmaxf(most, __shfl_xor(most, 32, WAVE));
-      const float raised = fmaxf(m, most - T::WEIGHT_BIAS);
+      const float both = fmaxf(most, __shfl_xor(most, 32, WAVE));
+      const float raised = fmaxf(m, both - T::WEIGHT_BIAS);
       const float down = raised > -__builtin_huge_valf() ? exp2_fast(m - raised) : 1.f;
       m = raised;
       l *= down;
 #pragma unroll
       for (int d = 0; d < D / 32; ++d) acc[d] *= down;
     }
+  }
+  __device__ __forceinline__ void weigh(typename T::x8 (&weights)[4]) {
     const float origin = m > -__builtin_huge_valf() ? m : 0.f;
-    typename T::x8 weights[4];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        u32x4 w;
+        u32x4 p;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float p = exp2_fast(s[t][8 * u + 2 * i] - origin), r = exp2_fast(s[t][8 * u + 2 * i + 1] - origin);
-          l += p + r;
-          w[i] = T::pair(p, r);
+          const float x = exp2_fast(__builtin_fmaf(s[t][8 * u + 2 * i], scale, -origin)), y = exp2_fast(__builtin_fmaf(s[t][8 * u + 2 * i + 1], scale, -origin));
+          l += x;
+          l += y;
+          p[i] = T::pair(x, y);
         }
-        weights[2 * t + u] = bits_as<typename T::x8>(w);
+        weights[2 * t + u] = bits_as<typename T::x8>(p);
       }
-    auto value = [&](int step, int d) {
-      u32x4 w;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const uint32_t r = step * 16 + e * 8 + half * 4 + l16 / 4, piece = 4 * d + 2 * pair16 + l16 % 4 / 2;
-        const u32x2 x = read_transposed(vt + r * D + (piece ^ value_swizzle<D>(r)) * 8 + l16 % 2 * 4);
-        w[2 * e] = x[0];
-        w[2 * e + 1] = x[1];
-      }
-      return w;
-    };
-    uint32_t dirty = 0;
+  }
+  __device__ __forceinline__ u32x4 value(lds_char* vals, int step, int d) const {
+    const u32x2 x = read_transposed(vals + (val_at ^ d * 64) + step * 16 * ROW), y = read_transposed(vals + (val_at ^ d * 64) + (step * 16 + 8) * ROW);
+    return u32x4{x[0], x[1], y[0], y[1]};
+  }
+  __device__ __forceinline__ void sum(lds_char* vals, const typename T::x8 (&weights)[4]) {
 #pragma unroll
     for (int step = 0; step < 4; ++step)
 #pragma unroll
+      for (int d = 0; d < D / 32; ++d) acc[d] = T::mfma32(bits_as<typename T::x8>(value(vals, step, d)), weights[step], acc[d]);
+  }
+  // The same where a weight of zero may meet what is not finite: such values are left out of the product, and the rows that do
+  // see them are found with products of ones.
+  __device__ __forceinline__ void sum_with_care(lds_char* vals, const typename T::x8 (&weights)[4], uint32_t token0) {
+    const uint32_t half = lane_id() / 32;
+    for (int step = 0; step < 4; ++step) {
+      u32x4 seen;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t bits = 0;
+        for (int b = 0; b < 2; ++b) {
+          const uint32_t j = 2 * i + b, token = token0 + step * 16 + j / 4 * 8 + half * 4 + j % 4;
+          if (token <= row) bits |= T::ONE << (16 * b);
+        }
+        seen[i] = bits;
+      }
+      const typename T::x8 weight = step == 0 ? weights[0] : step == 1 ? weights[1] : step == 2 ? weights[2] : weights[3];
+#pragma unroll
       for (int d = 0; d < D / 32; ++d) {
-        u32x4 w = value(step, d);
-        if (masked) {      // a weight of zero must not meet what is not finite
+        const u32x4 v = value(vals, step, d);
+        u32x4 clean;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) clean[i] = v[i] & ~not_finite<T>(v[i]);
+        acc[d] = T::mfma32(bits_as<typename T::x8>(clean), weight, acc[d]);
+        for (uint32_t kind = 0; kind < 3; ++kind) {      // infinity, -infinity, NaN
+          u32x4 ones;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint32_t x = not_finite<T>(w[i]);
-            dirty |= x;
-            w[i] &= ~x;
-          }
-        }
-        acc[d] = T::mfma32(bits_as<typename T::x8>(w), weights[step], acc[d]);
-      }
-    if (masked && ballot(dirty != 0)) {      // rows that do see it: found with products of ones
-      for (int step = 0; step < 4; ++step) {
-        u32x4 seen;
-        for (int i = 0; i < 4; ++i) {
-          uint32_t bits = 0;
-          for (int b = 0; b < 2; ++b) {
-            const uint32_t j = 2 * i + b, token = token0 + step * 16 + j / 4 * 8 + half * 4 + j % 4;
-            if (token <= row) bits |= T::pair(1.f, 0.f) << (16 * b);
-          }
-          seen[i] = bits;
-        }
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d) {
-          const u32x4 w = value(step, d);
-          for (uint32_t kind = 0; kind < 3; ++kind) {      // infinity, -infinity, NaN
-            u32x4 ones;
-            for (int i = 0; i < 4; ++i) {
-              uint32_t bits = 0;
-              for (int b = 0; b < 2; ++b) {
-                const uint32_t x = w[i] >> (16 * b) & 0xffffu;
-                const uint32_t is = x == T::INF ? 0 : x == (T::INF | 0x8000u) ? 1 : (x & T::INF) == T::INF ? 2 : 3;
-                if (is == kind) bits |= T::pair(1.f, 0.f) << (16 * b);
-              }
-              ones[i] = bits;
+            uint32_t bits = 0;
+            for (int b = 0; b < 2; ++b) {
+              const uint32_t x = v[i] >> (16 * b) & 0xffffu;
+              const uint32_t is = x == T::INF ? 0 : x == (T::INF | 0x8000u) ? 1 : (x & T::INF) == T::INF ? 2 : 3;
+              if (is == kind) bits |= T::ONE << (16 * b);
             }
-            f32x16 c;
-            for (int r = 0; r < 16; ++r) c[r] = 0.f;
-            c = T::mfma32(bits_as<typename T::x8>(ones), bits_as<typename T::x8>(seen), c);
-            const float add = kind == 0 ? __builtin_huge_valf() : kind == 1 ? -__builtin_huge_valf() : __builtin_nanf("");
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-              if (c[r] > 0.f) acc[d][r] += add;
+            ones[i] = bits;
           }
+          f32x16 c;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) c[r] = 0.f;
+          c = T::mfma32(bits_as<typename T::x8>(ones), bits_as<typename T::x8>(seen), c);
+          const float add = kind == 0 ? __builtin_huge_valf() : kind == 1 ? -__builtin_huge_valf() : __builtin_nanf("");
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (c[r] > 0.f) acc[d][r] += add;
         }
       }
     }
   }
-  l += __shfl_xor(l, 32, WAVE);
-  if (row >= length) return;
-  const float f = l > 0.f ? 1.f / l : l == 0.f ? 1.f : l;
-  const uint64_t at = (start + static_cast<uint64_t>(row)) * a.q_heads + head;
-  uint16_t* out = static_cast<uint16_t*>(a.out) + at * D + half * 4;
+  // Weighs and sums one tile and makes the scores of the next, matrix instructions and others in turn: the matrix unit is busy for
+  // 32 clocks with one, of which the wave needs 16, and the weights of a tile take as long as its products.
+  __device__ __forceinline__ void weigh_and_go_on(const lds_char* next_keys, lds_char* vals) {
+    __builtin_amdgcn_sched_barrier(0);
+    typename T::x8 weights[4];
+    weigh(weights);
+    scores(next_keys);
+    sum(vals, weights);
+    find_most();
+    asm volatile("" : "+v"(l), "+v"(most));      // (made here and not where they are next needed)
+    constexpr int MFMA = 0x8, READ = 0x100, OTHER = 0x2, HALF = D / 16;
+    __builtin_amdgcn_sched_group_barrier(READ, 4, 0);
 #pragma unroll
-  for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const u32x2 w = {T::pair(acc[d][4 * r] * f, acc[d][4 * r + 1] * f), T::pair(acc[d][4 * r + 2] * f, acc[d][4 * r + 3] * f)};
-      *reinterpret_cast<u32x2*>(out + d * 32 + r * 8) = w;
+    for (int i = 0; i < 2 * HALF - 4; ++i) {
+      __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(OTHER, 64 / (2 * HALF), 0);
+      __builtin_amdgcn_sched_group_barrier(READ, 1, 0);
     }
-  if (a.lse && half == 0) a.lse[at] = (m + log2f(l)) * LN2;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(OTHER, 64 / (2 * HALF), 0);
+      __builtin_amdgcn_sched_group_barrier(READ, 2, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < HALF; ++i) {
+      __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(READ, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(OTHER, 48 / HALF, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < HALF; ++i) {
+      __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(READ, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(OTHER, 16 / HALF, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  __device__ __forceinline__ void write(const PromptArgs& a, uint32_t start, uint32_t length, uint32_t head) const {
+    const float sum = l + __shfl_xor(l, 32, WAVE);
+    if (row >= length) return;
+    const float f = sum > 0.f ? 1.f / sum : sum == 0.f ? 1.f : sum;
+    const uint32_t half = lane_id() / 32;
+    const uint64_t at = (start + static_cast<uint64_t>(row)) * a.q_heads + head;
+    uint16_t* out = static_cast<uint16_t*>(a.out) + at * D + half * 4;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const u32x2 x = {T::pair(acc[d][4 * r] * f, acc[d][4 * r + 1] * f), T::pair(acc[d][4 * r + 2] * f, acc[d][4 * r + 3] * f)};
+        *reinterpret_cast<u32x2*>(out + d * 32 + r * 8) = x;
+      }
+    if (a.lse && half == 0) a.lse[at] = (m + log2f(sum)) * LN2;
+  }
+  __device__ __forceinline__ bool finite() const {
+    float z = 0.f;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) z = __builtin_fmaf(acc[d][r], 0.f, z);
+    return z == 0.f;
+  }
+};
+
+// The sum over the wave, in every lane.
+__device__ __forceinline__ uint32_t wave_sum(uint32_t v) {
+  v += static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x111, 0xf, 0xf, true));   // shifts within rows of 16
+  v += static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x112, 0xf, 0xf, true));
+  v += static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x114, 0xf, 0xf, true));
+  v += static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x118, 0xf, 0xf, true));
+  return read_lane_u32(v, 15) + read_lane_u32(v, 31) + read_lane_u32(v, 47) + read_lane_u32(v, 63);
+}
+
+// Which rows a workgroup takes.  Later rows see more, so up to PROMPT_ORDERED prompts the work is handed out by the rows'
+// place in their prompt, the last ones first: item i is in level L (rows L * rows .. of a prompt) if C(L + 1) <= i < C(L), C(L) =
+// sum over prompts of max(0, slots - L).  For more prompts, which fill the chip many times over, slot by slot from the back; prompt
+// p owns the slots from offsets[p] / rows + p on, enough for its rows and found without a list.
+constexpr uint32_t PROMPT_ORDERED = 64;
+__device__ __forceinline__ bool prompt_find(const PromptArgs& a, uint32_t rows, uint32_t item, uint32_t* start, uint32_t* length, uint32_t* first) {
+  if (a.n_prompts <= PROMPT_ORDERED) {
+    const uint32_t lane = lane_id(), p = min_u32(lane, a.n_prompts - 1);
+    const uint32_t from = static_cast<uint32_t>(a.offsets[p]), to = static_cast<uint32_t>(a.offsets[p + 1]);
+    const bool good = from <= to && to <= a.n_tokens;
+    if (ballot(!good)) return false;
+    const uint32_t slots = lane < a.n_prompts ? (to - from + rows - 1) / rows : 0;
+    uint32_t low = 0, high = a.slots;           // C(low) > item >= C(high); the second holds as no prompt has so many
+    if (wave_sum(slots) <= item) { *length = *first = *start = 0; return true; }
+    while (high - low > 1) {
+      const uint32_t mid = low + (high - low) / 2;
+      if (wave_sum(slots > mid ? slots - mid : 0) > item) low = mid; else high = mid;
+    }
+    uint64_t these = ballot(slots > low);
+    for (uint32_t skip = item - wave_sum(slots > low + 1 ? slots - low - 1 : 0); skip > 0; --skip) these &= these - 1;
+    const uint32_t owner = uniform(static_cast<uint32_t>(__builtin_ctzll(these)));
+    *start = read_lane_u32(from, owner);
+    *length = read_lane_u32(to - from, owner);
+    *first = low * rows;
+    return true;
+  }
+  const uint32_t slot = a.slots - 1 - item;
+  uint32_t prompt = 0;
+  for (uint32_t hi = a.n_prompts; hi - prompt > 1;) {
+    const uint32_t mid = prompt + (hi - prompt) / 2;
+    if (static_cast<uint32_t>(a.offsets[mid]) / rows + mid <= slot) prompt = mid; else hi = mid;
+  }
+  const uint32_t from = static_cast<uint32_t>(a.offsets[prompt]), to = static_cast<uint32_t>(a.offsets[prompt + 1]);
+  if (from > to || to > a.n_tokens) return false;
+  *start = uniform(from);
+  *length = uniform(to - from);
+  *first = uniform((slot - (from / rows + prompt)) * rows);
+  return true;
+}
+
+// This thread's 16-byte pieces of a tile of keys or of values, which go from global memory straight to LDS.
+template <int D, int WAVES>
+struct PromptFill {
+  static constexpr uint32_t PIECES = D / 8, ROW = D * 2;
+  static constexpr int LOADS = PROMPT_KEYS * PIECES / (WAVES * WAVE);
+  const char* from;
+  uint64_t stride;               // of a token, in bytes
+  uint32_t off[LOADS];
+  uint32_t wave;
+
+  __device__ __forceinline__ void set_up(const fikit_vectors& x, uint32_t start, uint32_t head, uint32_t wave_, bool values) {
+    wave = wave_;
+    from = reinterpret_cast<const char*>(static_cast<const uint16_t*>(x.d_data) + start * x.token_stride + head * x.head_stride);
+    stride = x.token_stride * 2;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const uint32_t c = (i * WAVES + wave) * WAVE + lane_id(), r = c / PIECES, piece = c % PIECES;
+      off[i] = r * static_cast<uint32_t>(stride) + (piece ^ (values ? value_swizzle<D>(r) : key_swizzle<D>(r))) * 16;
+    }
+  }
+  __device__ __forceinline__ void load(uint32_t tile, uint32_t length, lds_char* to) const {
+    const char* at = from + tile * (PROMPT_KEYS * stride);
+    to += wave * WAVE * 16;
+    if ((tile + 1) * PROMPT_KEYS <= length) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) load_to_lds(at + off[i], to + i * WAVES * WAVE * 16);
+    } else {                     // rows behind the prompt's end: its last token's, which are masked
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const uint32_t r = ((i * WAVES + wave) * WAVE + lane_id()) / PIECES, last = length - 1 - tile * PROMPT_KEYS, back = r > last ? r - last : 0;
+        load_to_lds(at + (off[i] - back * static_cast<uint32_t>(stride)), to + i * WAVES * WAVE * 16);
+      }
+    }
+  }
+};
+
+// What this wave has asked for is in LDS, and so is what the others have.
+__device__ __forceinline__ void prompt_arrive() {
+  __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0)
+  __syncthreads();
+}
+
+// A workgroup's rows where values that are not finite follow tokens: one tile after the other, nothing ahead of time.
+template <typename T, int D, int WAVES>
+__device__ __attribute__((noinline)) void prompt_with_care(PromptArgs a, uint32_t start, uint32_t length, uint32_t first, uint32_t head, uint32_t kv_head,
+                                                           lds_char* keys, lds_char* vals) {
+  constexpr uint32_t ROWS = WAVES * PROMPT_WAVE_ROWS;
+  const uint32_t wave = uniform(threadIdx.x / WAVE), row0 = first + wave * PROMPT_WAVE_ROWS;
+  const uint32_t tiles = (min_u32(first + ROWS, length) + PROMPT_KEYS - 1) / PROMPT_KEYS;
+  PromptFill<D, WAVES> k, v;
+  k.set_up(a.k, start, kv_head, wave, false);
+  v.set_up(a.v, start, kv_head, wave, true);
+  PromptWave<T, D> w;
+  w.set_up(a, start, length, row0, head);
+  w.start();
+  for (uint32_t tile = 0; tile < tiles; ++tile) {
+    __syncthreads();
+    k.load(tile, length, keys);
+    v.load(tile, length, vals);
+    prompt_arrive();
+    const uint32_t token0 = tile * PROMPT_KEYS;
+    if (token0 > row0 + PROMPT_WAVE_ROWS - 1) continue;
+    typename T::x8 weights[4];
+    w.scores(keys);
+    w.mask(token0);
+    w.find_most();
+    w.raise();
+    w.weigh(weights);
+    w.sum_with_care(vals, weights, token0);
+  }
+  w.write(a, start, length, head);
+}
+
+template <typename T, int D, int WAVES>
+__global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs a) {
+  constexpr uint32_t ROWS = WAVES * PROMPT_WAVE_ROWS, TILE = PROMPT_KEYS * D * 2;
+  // Keys and values of two tiles.  (Arrays of their own: the compiler sees that a tile that is read is not one that is being filled,
+  // and does not wait for the latter.)
+  __shared__ __align__(1024) char lds_k0[TILE], lds_k1[TILE], lds_v0[TILE], lds_v1[TILE];
+  lds_char *const k0 = (lds_char*)lds_k0, *const k1 = (lds_char*)lds_k1, *const v0 = (lds_char*)lds_v0, *const v1 = (lds_char*)lds_v1;
+  const bool stop = stopped(a.status);      // (looked at below, where the offsets have arrived too)
+  const uint32_t wave = uniform(threadIdx.x / WAVE);
+  // neighbours in the grid go to different dies: those of one key head are kept on few of them
+  const uint32_t place = blockIdx.x % a.q_heads;
+  const uint32_t kv_head = place % a.kv_heads, head = kv_head * (a.q_heads / a.kv_heads) + place / a.kv_heads;
+  if (blockIdx.x == 0 && !stop) {
+    bool bad = a.offsets[0] != 0 || static_cast<uint32_t>(a.offsets[a.n_prompts]) != a.n_tokens;
+    for (uint32_t p = threadIdx.x; p < a.n_prompts; p += WAVES * WAVE) bad |= a.offsets[p] > a.offsets[p + 1];
+    if (bad) *a.status = FIKIT_INVALID_ARG;
+  }
+  uint32_t start, length, first;
+  if (!prompt_find(a, ROWS, blockIdx.x / a.q_heads, &start, &length, &first)) {
+    if (threadIdx.x == 0 && !stop) *a.status = FIKIT_INVALID_ARG;
+    return;
+  }
+  if (stop || first >= length) return;
+  const uint32_t row0 = first + wave * PROMPT_WAVE_ROWS;
+  const uint32_t tiles = (min_u32(first + ROWS, length) + PROMPT_KEYS - 1) / PROMPT_KEYS;
+
+  PromptFill<D, WAVES> k, v;
+  k.set_up(a.k, start, kv_head, wave, false);
+  v.set_up(a.v, start, kv_head, wave, true);
+  k.load(0, length, k0);
+  if (tiles > 1) k.load(1, length, k1);
+  v.load(0, length, v0);
+
+  PromptWave<T, D> w;
+  w.set_up(a, start, length, row0, head);
+  // Tile i's scores are made while tile i - 1 is weighed and summed.  Before each tile: its values and the next one's keys have
+  // arrived, and what their successors replace is no longer read.
+  static_assert(ROWS == 2 * PROMPT_KEYS, "tiles that some rows see in part: the last two");
+  const uint32_t full = first / PROMPT_KEYS;      // tiles that all rows of the workgroup see whole, an even number
+  w.start();
+  prompt_arrive();
+  w.scores(k0);
+  w.find_most();
+  for (uint32_t tile = 0; tile < full; tile += 2) {
+    prompt_arrive();
+    k.load(tile + 2, length, k0);
+    v.load(tile + 1, length, v1);
+    w.raise();
+    w.weigh_and_go_on(k1, v0);
+    prompt_arrive();
+    if (tile + 3 < tiles) k.load(tile + 3, length, k1);
+    v.load(tile + 2, length, v0);
+    w.raise();
+    w.weigh_and_go_on(k0, v1);
+  }
+  prompt_arrive();
+  if (full + 1 < tiles) v.load(full + 1, length, v1);
+  {
+    typename T::x8 weights[4];
+    w.mask(full * PROMPT_KEYS);
+    w.find_most();
+    w.raise();
+    w.weigh(weights);
+    w.sum(v0, weights);
+  }
+  if (full + 1 < tiles) {
+    if (row0 >= (full + 1) * PROMPT_KEYS) {
+      w.scores(k1);
+      w.mask((full + 1) * PROMPT_KEYS);
+      w.find_most();
+      w.raise();
+    }
+    prompt_arrive();
+    if (row0 >= (full + 1) * PROMPT_KEYS) {
+      typename T::x8 weights[4];
+      w.weigh(weights);
+      w.sum(v1, weights);
+    }
+  }
+  // Weights of zero have met whatever values follow a row's token.  If that has left anything that is not finite, which only values
+  // that are not finite can, all of it is done again with care.
+  if (__syncthreads_or(!w.finite())) {
+    prompt_with_care<T, D, WAVES>(a, start, length, first, head, kv_head, k0, v0);
+    return;
+  }
+  w.write(a, start, length, head);
 }
 
 }  // namespace fikit

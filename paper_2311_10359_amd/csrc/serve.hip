@@ -24,6 +24,8 @@ int enqueue(void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t st, A... ar
   return hipGetLastError() == hipSuccess ? FIKIT_OK : FIKIT_HIP_ERROR;
 }
 
+constexpr uint64_t MOST_STRIDE = 1ull << 24;      // of a token, in values: places within a tile are 32-bit numbers of bytes
+
 bool vectors_ok(const fikit_vectors* v) {
   return v && v->d_data && aligned(v->d_data, 16) && v->token_stride % 8 == 0 && v->head_stride % 8 == 0;
 }
@@ -102,7 +104,7 @@ struct DecodeCall {
   }
 };
 
-constexpr int PROMPT_WAVES = 8;
+constexpr int PROMPT_WAVES = 4;
 struct PromptCall {
   const PromptArgs& a;
   uint32_t groups;
@@ -248,6 +250,7 @@ int fikit_prompt_attention(const fikit_vectors* h_q, const fikit_vectors* h_k, c
   if (!vectors_ok(h_q) || !vectors_ok(h_k) || !vectors_ok(h_v) || !d_offsets || !d_out || !aligned(d_offsets, 4) || !aligned(d_out, 16) ||
       !aligned(d_lse, 4))
     return FIKIT_INVALID_ARG;
+  if (h_k->token_stride > MOST_STRIDE || h_v->token_stride > MOST_STRIDE) return FIKIT_UNSUPPORTED;
   const uint64_t slots = n_tokens / (PROMPT_WAVES * PROMPT_WAVE_ROWS) + static_cast<uint64_t>(n_prompts);
   if (slots * q_heads > MOST_GROUPS) return FIKIT_UNSUPPORTED;
   PromptArgs a{};

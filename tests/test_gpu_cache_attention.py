@@ -172,3 +172,21 @@ def test_replays_of_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(out.out, want.out) and torch.equal(out.lse, want.lse)
         binding.fikit_check_status(status)
+
+
+def test_more_requests_than_a_workgroup_looks_at():
+    """1024 requests are the most whose lengths every workgroup adds up."""
+    for n in (1023, 1024, 1025):
+        lengths = [(13 * i) % 40 for i in range(n)]
+        lengths[n // 2] = 4500
+        c = Case(n, lengths, 2, 1, 64, 16, torch.bfloat16)
+        c.check(c.run())
+
+
+def test_a_status_that_is_set_stops_it():
+    c = Case(30, [100, 3000], 4, 2, 64, 16, torch.bfloat16)
+    d = [t.to(DEV) for t in (c.q, *c.codes, *c.exps, c.table, torch.tensor(c.lengths, dtype=torch.int32))]
+    out = binding.Attention(torch.full_like(d[0], 7), None)
+    status = torch.tensor([binding.FIKIT_CACHE_FULL], dtype=torch.int32, device=DEV)
+    binding.fikit_cache_attention(*d, c.scale, status, out=out)
+    assert (out.out == 7).all() and int(status) == binding.FIKIT_CACHE_FULL

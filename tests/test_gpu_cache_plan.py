@@ -126,3 +126,8 @@ def test_replays_of_a_graph():
         assert out.slots.tolist() == want["slots"] and out.pieces.tolist() == want["pieces"] and out.counts.tolist() == want["counts"]
         assert np.array_equal(d_table.cpu().numpy(), table)
         binding.fikit_check_status(word)
+
+
+@pytest.mark.parametrize("n", [4095, 4096, 4097, 8200])
+def test_on_both_sides_of_one_launch(n):
+    check(*case(n, n, 50, lambda r: r.integers(0, 4) if r.random() < 0.9 else r.integers(0, 60), 16), 16)

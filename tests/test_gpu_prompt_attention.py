@@ -154,3 +154,21 @@ def test_replays_of_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(out.out, want.out) and torch.equal(out.lse, want.lse)
         binding.fikit_check_status(status)
+
+
+@pytest.mark.parametrize("n", [63, 64, 65, 66])
+def test_numbers_of_prompts_on_both_sides_of_the_ordered_ones(n):
+    lengths = [(37 * i) % 290 for i in range(n)]
+    q, k, v = inputs(12, lengths, 2, 1, 64, torch.bfloat16)
+    check(q, k, v, lengths, 0.125, run(q, k, v, lengths, 0.125), rows=9)
+    lengths = [0] * (n - 1) + [130]
+    q, k, v = inputs(13, lengths, 2, 1, 128, torch.float16)
+    check(q, k, v, lengths, 0.125, run(q, k, v, lengths, 0.125), rows=30)
+
+
+def test_a_status_that_is_set_stops_it():
+    q, k, v = (t.to(DEV) for t in inputs(14, [100], 2, 1, 64, torch.bfloat16))
+    out = binding.Attention(torch.full((100, 2, 64), 7.0, dtype=torch.bfloat16, device=DEV), None)
+    status = torch.tensor([binding.FIKIT_CACHE_FULL], dtype=torch.int32, device=DEV)
+    binding.fikit_prompt_attention(q, k, v, torch.tensor([0, 100], dtype=torch.int32, device=DEV), 0.1, status, out=out)
+    assert (out.out == 7).all() and int(status) == binding.FIKIT_CACHE_FULL
