@@ -5,18 +5,26 @@
 
 namespace fikit {
 
-// One pass over the keys and values with the running maximum and sum of the softmax.  A workgroup takes a part of one request's
-// context for one key head and up to 16 of its query heads; its waves take a quarter of the part each, in steps of 32 tokens:
+// One pass over the keys and values with the running maximum and sum of the softmax.  A workgroup takes a stretch of one request's
+// context for one key head and up to 16 of its query heads; its waves take a quarter of it each, in steps of 32 tokens:
 //
-//   scores   S^T[token][query] = K Q^T, two 16x16 tiles: lane l holds the key codes of token l % 16, a quarter (l / 16) of the
-//            dimensions, and the query's same quarter.  It receives the scores of query l % 16 at tokens 4 (l / 16) + 0..3.
+//   scores   S^T[token][query] = K Q^T, two 16x16 tiles: lane l holds key codes of token l % 16, a quarter of the dimensions (by
+//            l / 16), and the same of query l % 16.  It receives the scores of that query at tokens 4 (l / 16) + 0..3.
 //   weights  p = 2^(s - m), in the lane that has the score; m is raised, and what has been summed rescaled, only when a score
 //            passes it by 2^8 (32 bits have room), so most steps exchange nothing between lanes.
 //   outputs  O^T[dim][query] += V^T P^T: the order of the tokens within the product is free, so lane l takes as its eight
-//            those whose weights it has, and reads their value codes at D / 16 consecutive dimensions.
+//            those whose weights it has, and reads their value codes at D / 16 consecutive dimensions.  Rounding a weight to
+//            bfloat16 would cost as much as rounding the output; what it leaves is a second operand, which costs nothing here.
 //
 // Codes become 16-bit values, scale included, in one instruction for two; nothing goes through LDS but the joining of
-// the waves' results.  Parts of one request are joined by k_decode_join.
+// the waves' results.
+//
+// The work is cut evenly: with 128 tokens of a request, for one unit (key head and tile of query heads), as a chunk, and chunks in
+// the order of requests, units, tokens, workgroup b of W takes chunks b T / W .. (b + 1) T / W - 1 of all T, whatever requests they
+// belong to.  W is what the chip holds at once, so nothing is left over at the end, and what a workgroup begins with (adding up all
+// lengths, first loads) is paid once.  Beginning and ending a stretch takes as long as DECODE_FIXED chunks, so a request's chunks
+// are followed by so many empty ones.  Only the first and the last of a workgroup's stretches can be parts of longer ones; these are
+// joined by k_decode_join.
 
 struct DecodeArgs {
   fikit_cache cache;
@@ -26,328 +34,381 @@ struct DecodeArgs {
   void* out;
   float* lse;
   int32_t* status;
-  uint2* spans;            // [request]: first part, number of parts
-  float2* part_sums;       // [part][q head]: maximum (of scores times log2 e), sum
-  float* part_out;         // [part][q head][D]
-  uint32_t q_heads, table_width, max_length, head_tiles, n_requests;
-  uint32_t parts;          // most parts of all requests together
-  uint32_t per_request;    // 0: see k_decode; else so many parts for each request, of part_tokens
-  uint32_t part_tokens;
+  uint32_t* firsts;        // [request]: chunks, of one unit, of the requests before; [n_requests]: of all
+  float2* part_sums;       // [2 W][rows]: maximum (of scores times log2 e), sum
+  float* part_out;         // [2 W][rows][D]
+  uint32_t q_heads, table_width, max_length, head_tiles, n_requests, groups;
   float scale;
 };
 
-// How contexts are cut into parts.  A part is a workgroup's for each key head and tile of query heads; many parts fill the chip
-// and end together, few need less joining: a part's result is 4 G bytes a dimension (G query heads to a key head), written and
-// read, for 2 part_tokens bytes of keys and values.  So with `units` key heads and tiles:
-//   DECODE_GROUPS workgroups, of at least 64 G tokens each, but DECODE_FEW workgroups before that counts;
-//   DECODE_LEAST to DECODE_MOST tokens (a wave's quarter holds at most 64 blocks).
-constexpr uint32_t DECODE_GROUPS = 4096, DECODE_FEW = 512, DECODE_LEAST = 128, DECODE_MOST = 4096;
-// Up to so many requests each workgroup looks at all lengths; for more, every request is cut alike, into parts of DECODE_MOST.
-constexpr uint32_t DECODE_LOOK = 1024;
-
-__host__ __device__ inline uint32_t decode_part_tokens(uint64_t tokens, uint32_t units, uint32_t rows) {
-  uint64_t least = 64ull * rows;
-  if (least > tokens * units / DECODE_FEW) least = tokens * units / DECODE_FEW;
-  uint64_t part = (tokens * units + DECODE_GROUPS - 1) / DECODE_GROUPS;
-  if (part < least) part = least;
-  part = (part + DECODE_LEAST - 1) / DECODE_LEAST * DECODE_LEAST;
-  return static_cast<uint32_t>(part < DECODE_LEAST ? DECODE_LEAST : part > DECODE_MOST ? DECODE_MOST : part);
-}
-
 constexpr int DECODE_WAVES = 4, DECODE_ROWS = 16, DECODE_STEP = 32;
+constexpr uint32_t DECODE_CHUNK = DECODE_WAVES * DECODE_STEP;
 constexpr float DECODE_SLACK = 8.f;   // log2 of how far a weight may pass 1 before the maximum is raised
 
-template <int D>
-struct DecodeStep {
-  u32x4 k[2][D / 64];        // D / 4 codes of a key, two tiles of tokens
-  uint32_t v[8][D / 64];     // D / 16 codes of each of eight values
-};
+// (a request without tokens has one chunk too, in which its outputs are written)
+__host__ __device__ inline uint32_t decode_chunks(uint32_t length) { return length == 0 ? 1 : (length + DECODE_CHUNK - 1) / DECODE_CHUNK; }
 
-// The item-th part, counting through the requests: every workgroup adds up all lengths for itself, which fixes the parts' size,
-// and then the requests' parts.  False if there are fewer parts or the call has failed.
+constexpr uint32_t DECODE_FIXED = 1;
+__host__ __device__ inline uint32_t decode_weight(uint32_t length) { return decode_chunks(length) + DECODE_FIXED; }
+
+// Chunks of all requests, and the request that chunk `at` of a unit belongs to.
 struct DecodeLook {
-  uint64_t tokens[DECODE_WAVES];
-  uint32_t parts[DECODE_WAVES];
-  uint32_t request, part, n_parts, length;
+  uint32_t sums[DECODE_WAVES];
+  uint32_t request, first;
 };
 
-__device__ __forceinline__ bool decode_find(const DecodeArgs& a, uint32_t item, uint32_t units, uint32_t rows, DecodeLook* lds, uint32_t* request,
-                                            uint32_t* part, uint32_t* part_tokens, uint32_t* n_parts, uint32_t* length) {
-  constexpr uint32_t PER = DECODE_LOOK / (DECODE_WAVES * WAVE);
+// Adds up the chunks of all requests in every workgroup, a run of consecutive requests per thread; false if the call has failed.
+__device__ __forceinline__ bool decode_look(const DecodeArgs& a, DecodeLook* lds, uint32_t* before, uint32_t* mine, uint32_t* total) {
   const uint32_t per = (a.n_requests + DECODE_WAVES * WAVE - 1) / (DECODE_WAVES * WAVE), first = threadIdx.x * per;
   const bool stop = stopped(a.status);
-  uint32_t lengths[PER];
-  uint64_t tokens = 0;
   bool ok = !stop;
-#pragma unroll
-  for (uint32_t i = 0; i < PER; ++i) {
-    const bool there = i < per && first + i < a.n_requests;
-    const int32_t n = there ? a.lengths[first + i] : 0;
-    lengths[i] = static_cast<uint32_t>(n);
-    if (n < 0 || lengths[i] > a.max_length) ok = false; else tokens += lengths[i];
+  uint32_t sum = 0;
+#pragma unroll 4
+  for (uint32_t r = first; r < min_u32(first + per, a.n_requests); ++r) {
+    const int32_t n = a.lengths[r];
+    ok &= n >= 0 && static_cast<uint32_t>(n) <= a.max_length;
+    sum += decode_weight(static_cast<uint32_t>(n));
+  }
+  uint32_t run = sum;
+  for (int d = 1; d < WAVE; d <<= 1) {
+    const uint32_t x = __shfl_up(run, d, WAVE);
+    if (lane_id() >= static_cast<uint32_t>(d)) run += x;
   }
   const uint32_t wave = threadIdx.x / WAVE;
-  for (int d = 1; d < WAVE; d <<= 1) tokens += shfl_xor_u64(tokens, d);
-  if (lane_id() == 0) lds->tokens[wave] = tokens;
-  if (threadIdx.x == 0) lds->request = 0xffffffffu;
+  if (lane_id() == WAVE - 1) lds->sums[wave] = run;
   if (!__syncthreads_and(ok)) {
     if (threadIdx.x == 0 && !stop) *a.status = FIKIT_INVALID_ARG;
     return false;
   }
-  tokens = 0;
-  for (int w = 0; w < DECODE_WAVES; ++w) tokens += lds->tokens[w];
-  const uint32_t size = decode_part_tokens(tokens, units, min_u32(rows, DECODE_ROWS));
-  uint32_t count[PER], mine = 0;
-#pragma unroll
-  for (uint32_t i = 0; i < PER; ++i) {
-    const bool there = i < per && first + i < a.n_requests;
-    count[i] = !there ? 0 : lengths[i] == 0 ? 1 : (lengths[i] + size - 1) / size;
-    mine += count[i];
+  uint32_t all = 0, earlier = 0;
+  for (uint32_t w = 0; w < DECODE_WAVES; ++w) {
+    if (w < wave) earlier += lds->sums[w];
+    all += lds->sums[w];
   }
-  uint32_t before = mine;
-  for (int d = 1; d < WAVE; d <<= 1) {
-    const uint32_t x = __shfl_up(before, d, WAVE);
-    if (lane_id() >= static_cast<uint32_t>(d)) before += x;
-  }
-  if (lane_id() == WAVE - 1) lds->parts[wave] = before;
-  __syncthreads();
-  before -= mine;
-  for (uint32_t w = 0; w < wave; ++w) before += lds->parts[w];
-#pragma unroll
-  for (uint32_t i = 0; i < PER; ++i) {
-    if (item >= before && item - before < count[i]) {
-      lds->request = first + i;
-      lds->part = item - before;
-      lds->n_parts = count[i];
-      lds->length = lengths[i];
-    }
-    before += count[i];
-  }
-  __syncthreads();
-  *request = uniform(lds->request);
-  *part = uniform(lds->part);
-  *part_tokens = uniform(size);
-  *n_parts = uniform(lds->n_parts);
-  *length = uniform(lds->length);
-  return *request != 0xffffffffu;
+  *before = earlier + run - sum;
+  *mine = sum;
+  *total = uniform(all);
+  return true;
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(DECODE_WAVES * WAVE) void k_decode(DecodeArgs a) {
+// Which of `groups` workgroups takes chunk i of t.
+__device__ __forceinline__ uint32_t decode_owner(uint64_t i, uint64_t t, uint32_t groups) { return static_cast<uint32_t>(((i + 1) * groups - 1) / t); }
+
+// ONCE: no other workgroup reads these keys and values, so they are read past the caches (a tenth of the time of large
+// calls).  That is the case for up to 16 query heads to a key head; for 32 the second reader finds them in a cache.
+template <typename T, int D, bool ONCE>
+__global__ __launch_bounds__(DECODE_WAVES * WAVE, D == 128 ? 2 : 4) void k_decode(DecodeArgs a) {
   constexpr int KV_WORDS = D / 64;
+  const auto read = [](const auto* p) { return ONCE ? __builtin_nontemporal_load(p) : *p; };
   __shared__ float joined[DECODE_WAVES][DECODE_ROWS][D + 4];
   __shared__ float2 sums[DECODE_WAVES][DECODE_ROWS];
   __shared__ DecodeLook look;
-  const uint32_t head_units = a.cache.kv_heads * a.head_tiles;
-  const uint32_t unit = blockIdx.x % head_units, item = blockIdx.x / head_units;
-  const uint32_t kv_head = unit / a.head_tiles, tile = unit % a.head_tiles;
-  const uint32_t group = a.q_heads / a.cache.kv_heads;
-  const uint32_t rows = min_u32(group - tile * DECODE_ROWS, DECODE_ROWS), first_head = kv_head * group + tile * DECODE_ROWS;
+  const uint32_t units = a.cache.kv_heads * a.head_tiles, group = a.q_heads / a.cache.kv_heads, most_rows = min_u32(group, DECODE_ROWS);
   const uint32_t shift = __builtin_ctz(a.cache.block_tokens);
   const uint32_t lane = lane_id(), wave = uniform(threadIdx.x / WAVE), col = lane % 16, quarter = lane / 16;
-  // which part of which request
-  uint32_t request, part, part_tokens, n_parts, length;
-  if (a.per_request) {
-    if (stopped(a.status)) return;
-    request = item / a.per_request;
-    part = item % a.per_request;
-    part_tokens = a.part_tokens;
-    const int32_t signed_length = a.lengths[request];
-    length = static_cast<uint32_t>(signed_length);
-    if (signed_length < 0 || length > a.max_length) {
-      if (threadIdx.x == 0) *a.status = FIKIT_INVALID_ARG;
-      return;
-    }
-    n_parts = length == 0 ? 1 : (length + part_tokens - 1) / part_tokens;
-    if (part >= n_parts) return;
-    if (part == 0 && unit == 0 && threadIdx.x == 0) a.spans[request] = make_uint2(item, n_parts);
-  } else {
-    if (!decode_find(a, item, head_units, group, &look, &request, &part, &part_tokens, &n_parts, &length)) return;
-    if (part == 0 && unit == 0 && threadIdx.x == 0) a.spans[request] = make_uint2(item, n_parts);
+  const uint64_t unit_bytes = static_cast<uint64_t>(a.cache.block_tokens) * D;
+  const float scale = a.scale * LOG2E;
+
+  uint32_t before, mine, per_unit;
+  if (!decode_look(a, &look, &before, &mine, &per_unit)) return;
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.firsts[a.n_requests] = per_unit;
+  const uint64_t total = static_cast<uint64_t>(per_unit) * units;
+  const uint32_t groups = total < a.groups ? static_cast<uint32_t>(total) : a.groups;
+  if (blockIdx.x >= groups) return;
+  const uint64_t lo = blockIdx.x * total / groups, hi = (blockIdx.x + 1) * total / groups;
+  uint64_t left = hi - lo;
+  const uint32_t target = static_cast<uint32_t>(lo / units);
+  const uint32_t per_thread = (a.n_requests + DECODE_WAVES * WAVE - 1) / (DECODE_WAVES * WAVE);
+  if (target >= before && target - before < mine) {
+    look.request = threadIdx.x * per_thread;
+    look.first = before;
   }
-  const uint32_t from = part * part_tokens;
-  if (length == 0) {
-    for (uint32_t i = threadIdx.x; i < rows * D; i += DECODE_WAVES * WAVE) {
-      const uint64_t row = static_cast<uint64_t>(request) * a.q_heads + first_head + i / D;
-      static_cast<uint16_t*>(a.out)[row * D + i % D] = 0;
-      if (a.lse && i % D == 0) a.lse[row] = -__builtin_huge_valf();
+  __syncthreads();
+  uint32_t request = uniform(look.request), first = uniform(look.first), length, weight;
+  for (;;) {               // of the requests that a thread has added up, 64 at a time, the one that holds chunk `target`
+    const uint32_t r = request + lane;
+    const uint32_t n = r < a.n_requests ? static_cast<uint32_t>(a.lengths[r]) : 0, c = decode_weight(n);
+    uint32_t run = c;
+    for (int d = 1; d < WAVE; d <<= 1) {
+      const uint32_t x = __shfl_up(run, d, WAVE);
+      if (lane >= static_cast<uint32_t>(d)) run += x;
     }
-    return;
+    const uint64_t beyond = ballot(first + run > target);
+    if (beyond) {
+      const uint32_t owner = uniform(static_cast<uint32_t>(__builtin_ctzll(beyond)));
+      length = read_lane_u32(n, owner);
+      weight = read_lane_u32(c, owner);
+      first += read_lane_u32(run, owner) - weight;
+      request += owner;
+      break;
+    }
+    first += read_lane_u32(run, WAVE - 1);
+    request += WAVE;
   }
-  const uint32_t until = min_u32(length, from + part_tokens);
-  // this wave's quarter, in whole steps
-  const uint32_t per_wave = ((until - from + DECODE_WAVES - 1) / DECODE_WAVES + DECODE_STEP - 1) / DECODE_STEP * DECODE_STEP;
-  const uint32_t begin = from + wave * per_wave, end = min_u32(begin + per_wave, until);
+  const uint64_t inside = lo - static_cast<uint64_t>(first) * units;
+  uint32_t unit = static_cast<uint32_t>(inside / weight), chunk = static_cast<uint32_t>(inside % weight);
 
-  f32x4 acc[D / 16];
+  // Lane i of a wave holds block and exponents of the i-th page of a window of 64 of its tokens.
+  uint32_t my_block = 0;
+  auto quarter_of = [&](uint32_t from, uint32_t until, uint32_t* begin, uint32_t* end) {      // this wave's, in whole steps
+    const uint32_t per_wave = ((until - from + DECODE_WAVES - 1) / DECODE_WAVES + DECODE_STEP - 1) / DECODE_STEP * DECODE_STEP;
+    *begin = from + wave * per_wave;
+    *end = min_u32(*begin + per_wave, until);
+  };
+  auto ask_blocks = [&](uint32_t request, uint32_t begin, uint32_t end) {
+    if (begin < end) my_block = static_cast<uint32_t>(a.table[static_cast<uint64_t>(request) * a.table_width + min_u32((begin >> shift) + lane, (end - 1) >> shift)]);
+  };
+  bool there = false;      // my_block holds what the stretch needs
+  for (bool first_stretch = true;; first_stretch = false) {
+    const uint32_t take = left < weight - chunk ? static_cast<uint32_t>(left) : weight - chunk;
+    const uint32_t chunks = weight - DECODE_FIXED, last_chunk = min_u32(chunk + take, chunks);
+    const uint32_t kv_head = unit / a.head_tiles, tile = unit % a.head_tiles;
+    const uint32_t rows = min_u32(group - tile * DECODE_ROWS, DECODE_ROWS), first_head = kv_head * group + tile * DECODE_ROWS;
+    const uint32_t from = chunk * DECODE_CHUNK, until = min_u32(length, last_chunk * DECODE_CHUNK);
+    const uint32_t next_length = static_cast<uint32_t>(a.lengths[min_u32(request + 1, a.n_requests - 1)]);
+    left -= take;
+    uint32_t begin, end;
+    quarter_of(from, until, &begin, &end);
+    if (chunk < last_chunk) {
+      if (!there) ask_blocks(request, begin, end);
+      if (unit == 0 && chunk == 0 && threadIdx.x == 0) a.firsts[request] = first;
+      f32x4 acc[D / 16];
 #pragma unroll
-  for (int t = 0; t < D / 16; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = -__builtin_huge_valf(), l = 0.f;        // of query col; l over this lane's tokens
+      for (int t = 0; t < D / 16; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      float m = -__builtin_huge_valf(), l = 0.f;        // of query col; l over this lane's tokens
 
-  if (begin < end) {
-    // the queries: this lane's quarter of the dimensions of query col
-    typename T::x8 q[D / 32];
-    {
-      const uint16_t* src = static_cast<const uint16_t*>(a.q.d_data) + request * a.q.token_stride +
-                            static_cast<uint64_t>(first_head + min_u32(col, rows - 1)) * a.q.head_stride + quarter * (D / 4);
-#pragma unroll
-      for (int j = 0; j < D / 32; ++j) {
-        u32x4 w = *reinterpret_cast<const u32x4*>(src + j * 8);
-        if (col >= rows) w = u32x4{0, 0, 0, 0};
-        q[j] = bits_as<typename T::x8>(w);
-      }
-    }
-    // lane i holds block and exponents of the i-th page of the wave's tokens (at most 64, see the host)
-    const uint32_t first_page = begin >> shift, last_page = (end - 1) >> shift;
-    const uint32_t my_page = min_u32(first_page + lane, last_page);
-    const int32_t my_block = a.table[static_cast<uint64_t>(request) * a.table_width + my_page];
-    const bool bad = static_cast<uint32_t>(my_block) >= a.cache.n_blocks;
-    if (ballot(bad)) {
-      if (lane == 0) *a.status = FIKIT_INVALID_ARG;
-    } else {
-      const uint64_t my_unit = static_cast<uint64_t>(my_block) * a.cache.kv_heads + kv_head;
-      const uint32_t my_exps = a.cache.d_k_exp[my_unit] | static_cast<uint32_t>(a.cache.d_v_exp[my_unit]) << 8;
-      const uint64_t unit_bytes = static_cast<uint64_t>(a.cache.block_tokens) * D;
-      const float scale = a.scale * LOG2E;
-
-      // tiles of 16 tokens lie in one page; a tile behind the last token is read from the last page
-      auto tile_at = [&](uint32_t token, uint32_t* exps) {
-        const uint32_t page = min_u32(token >> shift, last_page) - first_page;
-        const uint32_t block = read_lane_u32(static_cast<uint32_t>(my_block), page);
-        *exps = read_lane_u32(my_exps, page);
-        return (static_cast<uint64_t>(block) * a.cache.kv_heads + kv_head) * unit_bytes + static_cast<uint64_t>(token & (a.cache.block_tokens - 1)) * D;
-      };
-      auto load = [&](uint32_t token, DecodeStep<D>* s, uint32_t* exps) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint64_t at = tile_at(token + 16 * h, exps + h);
-          const uint8_t* k = a.cache.d_k + at + (col * D + quarter * (D / 4));
-          const uint8_t* v = a.cache.d_v + at + (quarter * 4 * D + col * (D / 16));
-#pragma unroll
-          for (int j = 0; j < KV_WORDS; ++j) s->k[h][j] = *reinterpret_cast<const u32x4*>(k + j * 16);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if constexpr (KV_WORDS == 2) {
-              const u32x2 w = *reinterpret_cast<const u32x2*>(v + i * D);
-              s->v[4 * h + i][0] = w[0];
-              s->v[4 * h + i][1] = w[1];
-            } else {
-              s->v[4 * h + i][0] = *reinterpret_cast<const uint32_t*>(v + i * D);
-            }
-          }
-        }
-      };
-      DecodeStep<D> now, next;
-      uint32_t exps[2], next_exps[2];
-      load(begin, &now, exps);
-      for (uint32_t token = begin; token < end; token += DECODE_STEP) {
-        if (token + DECODE_STEP < end) load(token + DECODE_STEP, &next, next_exps);
-        float s[8];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          f32x4 c = {0.f, 0.f, 0.f, 0.f};
-          const float up = power_of(exps[h] & 255u);
+      if (begin < end) {
+        // Of the next window the blocks are read when a window begins, and the exponents a step later.
+        const uint32_t last_page = (end - 1) >> shift;
+        const int32_t* table = a.table + static_cast<uint64_t>(request) * a.table_width;
+        uint32_t window = begin >> shift, next_block = 0, next_exps = 0;
+        bool asked = false;
+        auto checked = [&](uint32_t block) {      // (a block outside the cache: the call has failed, block 0 is read instead)
+          const bool bad = block >= a.cache.n_blocks;
+          if (ballot(bad)) *a.status = FIKIT_INVALID_ARG;
+          return bad ? 0u : block;
+        };
+        auto exponents = [&](uint32_t block) {
+          const uint64_t at = static_cast<uint64_t>(block) * a.cache.kv_heads + kv_head;
+          return a.cache.d_k_exp[at] | static_cast<uint32_t>(a.cache.d_v_exp[at]) << 8;
+        };
+        auto ask_next = [&] {
+          asked = window + WAVE <= last_page;
+          if (asked) next_block = static_cast<uint32_t>(table[min_u32(window + WAVE + lane, last_page)]);
+        };
+        // the queries: of query col the dimensions of which this lane reads the keys, 16 of every 64
+        typename T::x8 q[D / 32];
+        {
+          const uint16_t* src = static_cast<const uint16_t*>(a.q.d_data) + request * a.q.token_stride +
+                                static_cast<uint64_t>(first_head + min_u32(col, rows - 1)) * a.q.head_stride + quarter * 16;
 #pragma unroll
           for (int j = 0; j < D / 32; ++j) {
-            u32x4 w;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const uint32_t codes = now.k[h][j / 2][(j & 1) * 2 + i];
-              w[2 * i] = T::template codes<false>(codes, up);
-              w[2 * i + 1] = T::template codes<true>(codes, up);
-            }
-            c = T::mfma16(bits_as<typename T::x8>(w), q[j], c);
+            u32x4 w = *reinterpret_cast<const u32x4*>(src + j / 2 * 64 + j % 2 * 8);
+            if (col >= rows) w = u32x4{0, 0, 0, 0};
+            q[j] = bits_as<typename T::x8>(w);
+          }
+        }
+        my_block = checked(my_block);
+        uint32_t my_exps = exponents(my_block);
+
+        // tiles of 16 tokens lie in one page; a tile behind the last token is read from the last page
+        auto tile_at = [&](uint32_t token, uint32_t* exps) {
+          const uint32_t page = min_u32(token >> shift, last_page) - window;
+          const uint32_t block = read_lane_u32(my_block, page);
+          *exps = read_lane_u32(my_exps, page);
+          return (static_cast<uint64_t>(block) * a.cache.kv_heads + kv_head) * unit_bytes + static_cast<uint64_t>(token & (a.cache.block_tokens - 1)) * D;
+        };
+        // Two steps are on their way: a step's keys and values are read into the registers of the step two before as soon as these have
+        // been used.
+        struct Step {
+          u32x4 k[2][D / 64];        // 16 of every 64 codes of a key, of two tiles of tokens
+          uint32_t v[8][KV_WORDS];   // D / 16 codes of each of eight values
+          uint32_t exps[2];
+          uint64_t at[2];
+        };
+        auto load_keys = [&](uint32_t token, Step& x) {
+          if ((token >> shift) - window >= WAVE) {
+            window += WAVE;
+            my_block = next_block;
+            my_exps = next_exps;
+            ask_next();
+          } else if (asked) {
+            asked = false;
+            next_block = checked(next_block);
+            next_exps = exponents(next_block);
           }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[4 * h + i] = c[i] * scale;
-        }
-        if (token + DECODE_STEP > end) {     // what lies behind the last token counts for nothing, whatever it is
+          for (int h = 0; h < 2; ++h) {
+            x.at[h] = tile_at(token + 16 * h, x.exps + h);
+            const uint8_t* from = a.cache.d_k + x.at[h] + (col * D + quarter * 16);
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (token + (i / 4) * 16 + quarter * 4 + i % 4 >= end) {
-              s[i] = -__builtin_huge_valf();
+            for (int j = 0; j < KV_WORDS; ++j) x.k[h][j] = read(reinterpret_cast<const u32x4*>(from + j * 64));
+          }
+        };
+        auto load_values = [&](Step& x) {
 #pragma unroll
-              for (int j = 0; j < KV_WORDS; ++j) now.v[i][j] = 0;
+          for (int h = 0; h < 2; ++h) {
+            const uint8_t* from = a.cache.d_v + x.at[h] + (quarter * 4 * D + col * (D / 16));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              if constexpr (KV_WORDS == 2) {
+                const u32x2 w = read(reinterpret_cast<const u32x2*>(from + i * D));
+                x.v[4 * h + i][0] = w[0];
+                x.v[4 * h + i][1] = w[1];
+              } else {
+                x.v[4 * h + i][0] = read(reinterpret_cast<const uint32_t*>(from + i * D));
+              }
             }
-        }
-        float most = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-        if (ballot(most > m + (DECODE_SLACK + T::WEIGHT_BIAS))) {
-          most = fmaxf(most, __shfl_xor(most, 16, WAVE));
-          most = fmaxf(most, __shfl_xor(most, 32, WAVE));
-          const float raised = fmaxf(m, most - T::WEIGHT_BIAS);
-          const float down = raised > -__builtin_huge_valf() ? exp2_fast(m - raised) : 1.f;
-          m = raised;
-          l *= down;
+          }
+        };
+        auto step = [&](uint32_t token, Step& x) {
+          const uint32_t ahead = token + 2 * DECODE_STEP;
+          const float up[2] = {power_of(x.exps[0] >> 8), power_of(x.exps[1] >> 8)};
+          float s[8];
 #pragma unroll
-          for (int t = 0; t < D / 16; ++t) acc[t] *= down;
-        }
-        const float origin = m > -__builtin_huge_valf() ? m : 0.f;
-        u32x4 w;
+          for (int h = 0; h < 2; ++h) {
+            f32x4 c = {0.f, 0.f, 0.f, 0.f};
+            const float k_up = power_of(x.exps[h] & 255u);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float p = exp2_fast(s[2 * i] - origin), r = exp2_fast(s[2 * i + 1] - origin);
-          l += p + r;
-          w[i] = T::pair(p, r);
-        }
-        const typename T::x8 weights = bits_as<typename T::x8>(w);
-        const float up[2] = {power_of(exps[0] >> 8), power_of(exps[1] >> 8)};
+            for (int j = 0; j < D / 32; ++j) {
+              u32x4 w;
 #pragma unroll
-        for (int j = 0; j < KV_WORDS; ++j) {
-          u32x4 v[4];       // operands of four tiles of dimensions
+              for (int i = 0; i < 2; ++i) {
+                const uint32_t codes = x.k[h][j / 2][(j & 1) * 2 + i];
+                w[2 * i] = T::template codes<false>(codes, k_up);
+                w[2 * i + 1] = T::template codes<true>(codes, k_up);
+              }
+              c = T::mfma16(bits_as<typename T::x8>(w), q[j], c);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[4 * h + i] = c[i] * scale;
+          }
+          if (ahead < end) load_keys(ahead, x);
+          if (token + DECODE_STEP > end) {     // what lies behind the last token counts for nothing, whatever it is
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (token + (i / 4) * 16 + quarter * 4 + i % 4 >= end) {
+                s[i] = -__builtin_huge_valf();
+#pragma unroll
+                for (int j = 0; j < KV_WORDS; ++j) x.v[i][j] = 0;
+              }
+          }
+          float most = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+          if (ballot(most > m + (DECODE_SLACK + T::WEIGHT_BIAS))) {
+            most = fmaxf(most, __shfl_xor(most, 16, WAVE));
+            most = fmaxf(most, __shfl_xor(most, 32, WAVE));
+            const float raised = fmaxf(m, most - T::WEIGHT_BIAS);
+            const float down = raised > -__builtin_huge_valf() ? exp2_fast(m - raised) : 1.f;
+            m = raised;
+            l *= down;
+#pragma unroll
+            for (int t = 0; t < D / 16; ++t) acc[t] *= down;
+          }
+          const float origin = m > -__builtin_huge_valf() ? m : 0.f;
+          u32x4 w, rest;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            // bytes of two tokens side by side: dimensions 0 and 1, 2 and 3
-            const uint32_t lo = __builtin_amdgcn_perm(now.v[2 * i + 1][j], now.v[2 * i][j], 0x05010400u);
-            const uint32_t hi = __builtin_amdgcn_perm(now.v[2 * i + 1][j], now.v[2 * i][j], 0x07030602u);
-            v[0][i] = T::template codes<false>(lo, up[i / 2]);
-            v[1][i] = T::template codes<true>(lo, up[i / 2]);
-            v[2][i] = T::template codes<false>(hi, up[i / 2]);
-            v[3][i] = T::template codes<true>(hi, up[i / 2]);
+            const float p = exp2_fast(s[2 * i] - origin), r = exp2_fast(s[2 * i + 1] - origin);
+            l += p + r;
+            w[i] = T::pair(p, r);
+            if (T::WEIGHTS == 2) rest[i] = T::pair(p - T::low(w[i]), r - T::high(w[i]));
           }
+          const typename T::x8 weights = bits_as<typename T::x8>(w);
 #pragma unroll
-          for (int t = 0; t < 4; ++t) acc[4 * j + t] = T::mfma16(bits_as<typename T::x8>(v[t]), weights, acc[4 * j + t]);
+          for (int j = 0; j < KV_WORDS; ++j) {
+            u32x4 y[4];       // operands of four tiles of dimensions
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              // bytes of two tokens side by side: dimensions 0 and 1, 2 and 3
+              const uint32_t lo = __builtin_amdgcn_perm(x.v[2 * i + 1][j], x.v[2 * i][j], 0x05010400u);
+              const uint32_t hi = __builtin_amdgcn_perm(x.v[2 * i + 1][j], x.v[2 * i][j], 0x07030602u);
+              y[0][i] = T::template codes<false>(lo, up[i / 2]);
+              y[1][i] = T::template codes<true>(lo, up[i / 2]);
+              y[2][i] = T::template codes<false>(hi, up[i / 2]);
+              y[3][i] = T::template codes<true>(hi, up[i / 2]);
+            }
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+              acc[4 * j + t] = T::mfma16(bits_as<typename T::x8>(y[t]), weights, acc[4 * j + t]);
+              if (T::WEIGHTS == 2) acc[4 * j + t] = T::mfma16(bits_as<typename T::x8>(y[t]), bits_as<typename T::x8>(rest), acc[4 * j + t]);
+            }
+          }
+          if (ahead < end) load_values(x);
+        };
+        Step even, odd;
+        load_keys(begin, even);
+        load_values(even);
+        ask_next();
+        if (begin + DECODE_STEP < end) {
+          load_keys(begin + DECODE_STEP, odd);
+          load_values(odd);
         }
-        now = next;
-        exps[0] = next_exps[0];
-        exps[1] = next_exps[1];
+        for (uint32_t token = begin; token < end; token += 2 * DECODE_STEP) {
+          step(token, even);
+          if (token + DECODE_STEP < end) step(token + DECODE_STEP, odd);
+        }
+        l += __shfl_xor(l, 16, WAVE);
+        l += __shfl_xor(l, 32, WAVE);
       }
-      l += __shfl_xor(l, 16, WAVE);
-      l += __shfl_xor(l, 32, WAVE);
-    }
-  }
-  // join the waves: lane l holds of query col the dimensions (D / 16) * (4 * quarter + i) + t
-  if (quarter == 0) sums[wave][col] = make_float2(m, l);
+      // the next stretch's blocks are on their way while this one is joined; for another key head they are mostly the same
+      there = left > 0;
+      if (there) {
+        const bool same = unit + 1 < units;
+        const uint32_t next_until = same ? length : next_length, next_chunks = decode_chunks(next_until);
+        uint32_t next_begin, next_end;
+        quarter_of(0, left < next_chunks ? min_u32(next_until, static_cast<uint32_t>(left) * DECODE_CHUNK) : next_until, &next_begin, &next_end);
+        if (!same || next_begin != begin || next_end != end || ((end - 1) >> shift) - (begin >> shift) >= WAVE)
+          ask_blocks(same ? request : request + 1, next_begin, next_end);
+      }
+      // join the waves: lane l holds of query col the dimensions (D / 16) * (4 * quarter + i) + t
+      __syncthreads();          // (the stretch before has been read)
+      if (quarter == 0) sums[wave][col] = make_float2(m, l);
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int t = 0; t < D / 16; t += 4) {
-      const f32x4 x = {acc[t][i], acc[t + 1][i], acc[t + 2][i], acc[t + 3][i]};
-      *reinterpret_cast<f32x4*>(&joined[wave][col][D / 16 * (4 * quarter + i) + t]) = x;
-    }
-  __syncthreads();
-  for (uint32_t at = threadIdx.x * 4; at < rows * D; at += DECODE_WAVES * WAVE * 4) {
-    const uint32_t row = at / D, dim = at % D;
-    float most = -__builtin_huge_valf(), total = 0.f;
+        for (int t = 0; t < D / 16; t += 4) {
+          const f32x4 x = {acc[t][i], acc[t + 1][i], acc[t + 2][i], acc[t + 3][i]};
+          *reinterpret_cast<f32x4*>(&joined[wave][col][D / 16 * (4 * quarter + i) + t]) = x;
+        }
+      __syncthreads();
+      const bool whole = chunk == 0 && last_chunk == chunks;
+      const uint32_t slot = 2 * blockIdx.x + (first_stretch ? 0 : 1);
+      for (uint32_t at = threadIdx.x * 4; at < rows * D; at += DECODE_WAVES * WAVE * 4) {
+        const uint32_t row = at / D, dim = at % D;
+        float most = -__builtin_huge_valf(), sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < DECODE_WAVES; ++w) most = fmaxf(most, sums[w][row].x);
-    const float origin = most > -__builtin_huge_valf() ? most : 0.f;
-    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        for (int w = 0; w < DECODE_WAVES; ++w) most = fmaxf(most, sums[w][row].x);
+        const float origin = most > -__builtin_huge_valf() ? most : 0.f;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < DECODE_WAVES; ++w) {
-      const float f = exp2_fast(sums[w][row].x - origin);
-      total += sums[w][row].y * f;
-      x += *reinterpret_cast<const f32x4*>(&joined[w][row][dim]) * f;
-    }
-    const uint64_t head = static_cast<uint64_t>(request) * a.q_heads + first_head + row;
-    if (n_parts == 1) {
-      const float f = total > 0.f ? 1.f / total : total == 0.f ? 1.f : total;
-      const u32x2 w = {T::pair(x[0] * f, x[1] * f), T::pair(x[2] * f, x[3] * f)};
-      *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + head * D + dim) = w;
-      if (dim == 0 && a.lse) a.lse[head] = (most + log2f(total)) * LN2;
+        for (int w = 0; w < DECODE_WAVES; ++w) {
+          const float f = exp2_fast(sums[w][row].x - origin);
+          sum += sums[w][row].y * f;
+          x += *reinterpret_cast<const f32x4*>(&joined[w][row][dim]) * f;
+        }
+        if (whole) {
+          const uint64_t head = static_cast<uint64_t>(request) * a.q_heads + first_head + row;
+          const float f = sum > 0.f ? 1.f / sum : sum == 0.f ? 1.f : sum;
+          const u32x2 w = {T::pair(x[0] * f, x[1] * f), T::pair(x[2] * f, x[3] * f)};
+          *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + head * D + dim) = w;
+          if (dim == 0 && a.lse) a.lse[head] = (most + log2f(sum)) * LN2;
+        } else {
+          const uint64_t to = static_cast<uint64_t>(slot) * most_rows + row;
+          *reinterpret_cast<f32x4*>(a.part_out + to * D + dim) = x;
+          if (dim == 0) a.part_sums[to] = make_float2(most, sum);
+        }
+      }
     } else {
-      const uint64_t slot = static_cast<uint64_t>(item) * a.q_heads + first_head + row;
-      *reinterpret_cast<f32x4*>(a.part_out + slot * D + dim) = x;
-      if (dim == 0) a.part_sums[slot] = make_float2(most, total);
+      there = false;
+    }
+    if (left == 0) return;
+    chunk = 0;
+    if (++unit == units) {
+      unit = 0;
+      first += weight;
+      ++request;
+      length = uniform(next_length);
+      weight = decode_weight(length);
     }
   }
 }
@@ -357,43 +418,49 @@ template <typename T, int D>
 __global__ __launch_bounds__(DECODE_WAVES * WAVE) void k_decode_join(DecodeArgs a) {
   __shared__ float2 sums[DECODE_WAVES];
   __shared__ float outs[DECODE_WAVES][D];
-  if (stopped(a.status)) return;
-  const uint64_t head = blockIdx.x;
   const uint32_t request = blockIdx.x / a.q_heads, q_head = blockIdx.x % a.q_heads;
-  const uint2 span = a.spans[request];
-  if (span.y <= 1 || span.y > a.parts || span.x > a.parts - span.y) return;
+  const uint32_t first = a.firsts[request], per_unit = a.firsts[a.n_requests], length = static_cast<uint32_t>(a.lengths[request]);
+  if (stopped(a.status)) return;
+  const uint32_t units = a.cache.kv_heads * a.head_tiles, group = a.q_heads / a.cache.kv_heads, most_rows = min_u32(group, DECODE_ROWS);
+  const uint32_t unit = q_head / group * a.head_tiles + q_head % group / DECODE_ROWS, row = q_head % group % DECODE_ROWS;
+  const uint64_t total = static_cast<uint64_t>(per_unit) * units;
+  const uint32_t groups = total < a.groups ? static_cast<uint32_t>(total) : a.groups;
+  const uint32_t chunks = decode_chunks(length);
+  const uint64_t begin = static_cast<uint64_t>(first) * units + static_cast<uint64_t>(unit) * decode_weight(length);
+  const uint32_t from = decode_owner(begin, total, groups), to = decode_owner(begin + chunks - 1, total, groups);
+  if (from >= to || to >= groups) return;
+  // the first part is its workgroup's last stretch, and its first one too if the workgroup begins here
+  const uint32_t from_slot = 2 * from + (from * total / groups >= begin ? 0 : 1), parts = to - from + 1;
   const uint32_t lane = lane_id(), wave = uniform(threadIdx.x / WAVE);
-  constexpr int PER = D / WAVE, MANY = 8;
-  const uint64_t at = static_cast<uint64_t>(span.x) * a.q_heads + q_head;
-  const float2* from = a.part_sums + at;
-  const float* part = a.part_out + at * D + lane * PER;
-  float most = -__builtin_huge_valf(), total = 0.f, x[PER];
+  constexpr int PER = D / WAVE, MANY = 4;
+  float most = -__builtin_huge_valf(), total_sum = 0.f, x[PER];
   for (int i = 0; i < PER; ++i) x[i] = 0.f;
-  for (uint32_t p = wave; p < span.y; p += DECODE_WAVES * MANY) {
+  for (uint32_t p = wave; p < parts; p += DECODE_WAVES * MANY) {
     float2 s[MANY];
     float y[MANY][PER];
 #pragma unroll
     for (int j = 0; j < MANY; ++j) {
-      const uint64_t q = min_u32(p + j * DECODE_WAVES, span.y - 1);
-      s[j] = from[q * a.q_heads];
-      for (int i = 0; i < PER; ++i) y[j][i] = part[q * a.q_heads * D + i];
+      const uint32_t part = min_u32(p + j * DECODE_WAVES, parts - 1);
+      const uint64_t at = static_cast<uint64_t>(part == 0 ? from_slot : 2 * (from + part)) * most_rows + row;
+      s[j] = a.part_sums[at];
+      for (int i = 0; i < PER; ++i) y[j][i] = a.part_out[at * D + lane * PER + i];
     }
     float top = most;
 #pragma unroll
     for (int j = 0; j < MANY; ++j) top = fmaxf(top, s[j].x);
     const float origin = top > -__builtin_huge_valf() ? top : 0.f, down = exp2_fast(most - origin);
-    total *= down;
+    total_sum *= down;
     for (int i = 0; i < PER; ++i) x[i] *= down;
 #pragma unroll
     for (int j = 0; j < MANY; ++j) {
-      if (p + j * DECODE_WAVES >= span.y) continue;
+      if (p + j * DECODE_WAVES >= parts) continue;
       const float f = exp2_fast(s[j].x - origin);
-      total += s[j].y * f;
+      total_sum += s[j].y * f;
       for (int i = 0; i < PER; ++i) x[i] += y[j][i] * f;
     }
     most = top;
   }
-  if (lane == 0) sums[wave] = make_float2(most, total);
+  if (lane == 0) sums[wave] = make_float2(most, total_sum);
   for (int i = 0; i < PER; ++i) outs[wave][lane * PER + i] = x[i];
   __syncthreads();
   if (threadIdx.x >= D / 2) return;
@@ -408,6 +475,7 @@ __global__ __launch_bounds__(DECODE_WAVES * WAVE) void k_decode_join(DecodeArgs 
     hi += outs[w][2 * threadIdx.x + 1] * f;
   }
   const float f = sum > 0.f ? 1.f / sum : sum == 0.f ? 1.f : sum;
+  const uint64_t head = blockIdx.x;
   reinterpret_cast<uint32_t*>(a.out)[head * (D / 2) + threadIdx.x] = T::pair(lo * f, hi * f);
   if (threadIdx.x == 0 && a.lse) a.lse[head] = (top + log2f(sum)) * LN2;
 }

@@ -59,36 +59,26 @@ struct AppendCall {
   }
 };
 
-// How a decode step is cut up, as far as the host knows it (see decode_part_tokens), and its workspace.
+// How many workgroups a decode step takes, and its workspace.
 struct DecodeCut {
-  uint32_t head_tiles, per_request, part_tokens;
-  uint64_t parts, groups;
-  uint64_t spans_bytes, sums_bytes, bytes;
-  bool joins;                // some request may have several parts
+  uint32_t head_tiles, groups;
+  uint64_t firsts_bytes, sums_bytes, bytes;
+  bool fits;
 };
+constexpr uint64_t DECODE_CHIP_128 = 512, DECODE_CHIP_64 = 1024;     // what the chip holds at once of k_decode, by the head's size
 
 DecodeCut decode_cut(uint32_t n_requests, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim, uint32_t max_length) {
   DecodeCut c{};
   const auto whole = [](uint64_t v) { return (v + 255) / 256 * 256; };
-  c.head_tiles = (q_heads / kv_heads + DECODE_ROWS - 1) / DECODE_ROWS;
-  const uint64_t units = static_cast<uint64_t>(kv_heads) * c.head_tiles;
-  if (n_requests > DECODE_LOOK) {
-    c.part_tokens = DECODE_MOST;
-    c.per_request = max_length <= DECODE_MOST ? 1 : (max_length + DECODE_MOST - 1) / DECODE_MOST;
-    c.parts = static_cast<uint64_t>(n_requests) * c.per_request;
-    c.joins = c.per_request > 1;
-  } else {
-    // a request has one part, and one more for each whole part_tokens of all tokens
-    const uint64_t by_groups = (DECODE_GROUPS + units - 1) / units, by_most = static_cast<uint64_t>(n_requests) * max_length / DECODE_MOST;
-    const uint64_t by_least = static_cast<uint64_t>(n_requests) * (max_length / DECODE_LEAST + 1);
-    c.parts = (by_groups > by_most ? by_groups : by_most) + n_requests;
-    if (c.parts > by_least) c.parts = by_least;
-    c.joins = max_length > DECODE_LEAST;
-  }
-  c.groups = units * c.parts;
-  c.spans_bytes = whole(n_requests * sizeof(uint2));
-  c.sums_bytes = whole(c.parts * q_heads * sizeof(float2));
-  c.bytes = c.spans_bytes + (c.joins ? c.sums_bytes + c.parts * q_heads * head_dim * sizeof(float) : 0);
+  const uint64_t group = q_heads / kv_heads, rows = group < DECODE_ROWS ? group : DECODE_ROWS;
+  c.head_tiles = static_cast<uint32_t>((group + DECODE_ROWS - 1) / DECODE_ROWS);
+  const uint64_t chunks = static_cast<uint64_t>(n_requests) * decode_chunks(max_length), all = chunks * kv_heads * c.head_tiles;
+  c.fits = chunks < (1ull << 32) && static_cast<uint64_t>(n_requests) * q_heads <= MOST_GROUPS;
+  const uint64_t chip = head_dim == 128 ? DECODE_CHIP_128 : DECODE_CHIP_64;
+  c.groups = static_cast<uint32_t>(all < chip ? all : chip);
+  c.firsts_bytes = whole((static_cast<uint64_t>(n_requests) + 1) * sizeof(uint32_t));
+  c.sums_bytes = whole(2 * c.groups * rows * sizeof(float2));
+  c.bytes = c.firsts_bytes + c.sums_bytes + 2 * c.groups * rows * head_dim * sizeof(float);
   return c;
 }
 
@@ -98,8 +88,9 @@ struct DecodeCall {
   hipStream_t st;
   template <typename T, int D>
   int operator()() {
-    if (int rc = enqueue(k_decode<T, D>, dim3(static_cast<uint32_t>(c.groups)), dim3(DECODE_WAVES * WAVE), st, a)) return rc;
-    if (!c.joins) return FIKIT_OK;
+    const dim3 grid(c.groups), block(DECODE_WAVES * WAVE);
+    if (int rc = c.head_tiles == 1 ? enqueue(k_decode<T, D, true>, grid, block, st, a) : enqueue(k_decode<T, D, false>, grid, block, st, a)) return rc;
+    if (a.max_length <= DECODE_CHUNK) return FIKIT_OK;      // (no request has several chunks)
     return enqueue(k_decode_join<T, D>, dim3(a.n_requests * a.q_heads), dim3(DECODE_WAVES * WAVE), st, a);
   }
 };
@@ -195,7 +186,7 @@ size_t fikit_cache_attention_workspace_bytes(uint32_t n_requests, uint32_t q_hea
                                              uint32_t max_length) {
   if (kv_heads == 0 || q_heads == 0 || q_heads % kv_heads || q_heads > 65535 || max_length > 0x7fffffffu || n_requests > 0x7fffffffu) return 0;
   const DecodeCut c = decode_cut(n_requests, q_heads, kv_heads, head_dim, max_length);
-  return c.groups > MOST_GROUPS ? 0 : static_cast<size_t>(c.bytes);
+  return c.fits ? static_cast<size_t>(c.bytes) : 0;
 }
 
 int fikit_cache_attention(const fikit_cache* h_cache, const fikit_vectors* h_q, uint32_t q_heads, int32_t value_type, float scale,
@@ -212,7 +203,7 @@ int fikit_cache_attention(const fikit_cache* h_cache, const fikit_vectors* h_q, 
       !aligned(d_lse, 4) || (max_length > 0 && !d_block_table))
     return FIKIT_INVALID_ARG;
   const DecodeCut c = decode_cut(n_requests, q_heads, h_cache->kv_heads, h_cache->head_dim, max_length);
-  if (c.groups > MOST_GROUPS || static_cast<uint64_t>(n_requests) * q_heads > MOST_GROUPS) return FIKIT_UNSUPPORTED;
+  if (!c.fits) return FIKIT_UNSUPPORTED;
   if (!d_workspace || !aligned(d_workspace, 256)) return FIKIT_INVALID_ARG;
   if (workspace_bytes < c.bytes) return FIKIT_WORKSPACE_TOO_SMALL;
   DecodeArgs a{};
@@ -224,15 +215,13 @@ int fikit_cache_attention(const fikit_cache* h_cache, const fikit_vectors* h_q, 
   a.lse = d_lse;
   a.status = d_status;
   unsigned char* ws = static_cast<unsigned char*>(d_workspace);
-  a.spans = reinterpret_cast<uint2*>(ws);
-  a.part_sums = reinterpret_cast<float2*>(ws + c.spans_bytes);
-  a.part_out = reinterpret_cast<float*>(ws + c.spans_bytes + c.sums_bytes);
+  a.firsts = reinterpret_cast<uint32_t*>(ws);
+  a.part_sums = reinterpret_cast<float2*>(ws + c.firsts_bytes);
+  a.part_out = reinterpret_cast<float*>(ws + c.firsts_bytes + c.sums_bytes);
   a.q_heads = q_heads;
   a.table_width = table_width;
   a.max_length = max_length;
-  a.parts = static_cast<uint32_t>(c.parts);
-  a.per_request = c.per_request;
-  a.part_tokens = c.part_tokens;
+  a.groups = c.groups;
   a.head_tiles = c.head_tiles;
   a.n_requests = n_requests;
   a.scale = scale;
