@@ -13,8 +13,8 @@ namespace fikit {
 //   weights  p = 2^(s - m), in the lane that has the score; m is raised, and what has been summed rescaled, only when a score
 //            passes it by 2^8 (32 bits have room), so most steps exchange nothing between lanes.
 //   outputs  O^T[dim][query] += V^T P^T: the order of the tokens within the product is free, so lane l takes as its eight
-//            those whose weights it has, and reads their value codes at D / 16 consecutive dimensions.  Rounding a weight to
-//            bfloat16 would cost as much as rounding the output; what it leaves is a second operand, which costs nothing here.
+//            those whose weights it has, and reads their value codes at D / 16 consecutive dimensions.  Rounding a weight to 16
+//            bits would cost as much as rounding the output; what it leaves is a second operand, which costs nothing here.
 //
 // Codes become 16-bit values, scale included, in one instruction for two; nothing goes through LDS but the joining of
 // the waves' results.
@@ -34,7 +34,8 @@ struct DecodeArgs {
   void* out;
   float* lse;
   int32_t* status;
-  uint32_t* firsts;        // [request]: chunks, of one unit, of the requests before; [n_requests]: of all
+  uint4* cuts;             // [W]: request, unit, chunk and chunks (with the empty ones) where a workgroup begins
+  uint32_t* per_unit;      // chunks of one unit of all requests
   float2* part_sums;       // [2 W][rows]: maximum (of scores times log2 e), sum
   float* part_out;         // [2 W][rows][D]
   uint32_t q_heads, table_width, max_length, head_tiles, n_requests, groups;
@@ -111,7 +112,7 @@ __global__ __launch_bounds__(DECODE_WAVES * WAVE, D == 128 ? 2 : 4) void k_decod
 
   uint32_t before, mine, per_unit;
   if (!decode_look(a, &look, &before, &mine, &per_unit)) return;
-  if (blockIdx.x == 0 && threadIdx.x == 0) a.firsts[a.n_requests] = per_unit;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.per_unit = per_unit;
   const uint64_t total = static_cast<uint64_t>(per_unit) * units;
   const uint32_t groups = total < a.groups ? static_cast<uint32_t>(total) : a.groups;
   if (blockIdx.x >= groups) return;
@@ -148,336 +149,351 @@ __global__ __launch_bounds__(DECODE_WAVES * WAVE, D == 128 ? 2 : 4) void k_decod
   const uint64_t inside = lo - static_cast<uint64_t>(first) * units;
   uint32_t unit = static_cast<uint32_t>(inside / weight), chunk = static_cast<uint32_t>(inside % weight);
 
-  // Lane i of a wave holds block and exponents of the i-th page of a window of 64 of its tokens.
-  uint32_t my_block = 0;
-  auto quarter_of = [&](uint32_t from, uint32_t until, uint32_t* begin, uint32_t* end) {      // this wave's, in whole steps
-    const uint32_t per_wave = ((until - from + DECODE_WAVES - 1) / DECODE_WAVES + DECODE_STEP - 1) / DECODE_STEP * DECODE_STEP;
-    *begin = from + wave * per_wave;
-    *end = min_u32(*begin + per_wave, until);
-  };
-  auto ask_blocks = [&](uint32_t request, uint32_t begin, uint32_t end) {
-    if (begin < end) my_block = static_cast<uint32_t>(a.table[static_cast<uint64_t>(request) * a.table_width + min_u32((begin >> shift) + lane, (end - 1) >> shift)]);
-  };
-  bool there = false;      // my_block holds what the stretch needs
-  for (bool first_stretch = true;; first_stretch = false) {
-    const uint32_t take = left < weight - chunk ? static_cast<uint32_t>(left) : weight - chunk;
-    const uint32_t chunks = weight - DECODE_FIXED, last_chunk = min_u32(chunk + take, chunks);
-    const uint32_t kv_head = unit / a.head_tiles, tile = unit % a.head_tiles;
-    const uint32_t rows = min_u32(group - tile * DECODE_ROWS, DECODE_ROWS), first_head = kv_head * group + tile * DECODE_ROWS;
-    const uint32_t from = chunk * DECODE_CHUNK, until = min_u32(length, last_chunk * DECODE_CHUNK);
-    const uint32_t next_length = static_cast<uint32_t>(a.lengths[min_u32(request + 1, a.n_requests - 1)]);
+  if (threadIdx.x == 0) a.cuts[blockIdx.x] = make_uint4(request, unit, chunk, weight);
+
+  // The stretch that is next to be read: chunks chunk .. last_chunk - 1 of a request and unit, this wave's quarter of its tokens.
+  uint32_t next_length = 0, last_chunk, kv_head, first_head, rows, begin, end;
+  bool first_stretch = true;
+  auto derive = [&] {
+    const uint32_t take = left < weight - chunk ? static_cast<uint32_t>(left) : weight - chunk, tile = unit % a.head_tiles;
     left -= take;
-    uint32_t begin, end;
-    quarter_of(from, until, &begin, &end);
-    if (chunk < last_chunk) {
-      if (!there) ask_blocks(request, begin, end);
-      if (unit == 0 && chunk == 0 && threadIdx.x == 0) a.firsts[request] = first;
-      f32x4 acc[D / 16];
-#pragma unroll
-      for (int t = 0; t < D / 16; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-      float m = -__builtin_huge_valf(), l = 0.f;        // of query col; l over this lane's tokens
-
-      if (begin < end) {
-        // Of the next window the blocks are read when a window begins, and the exponents a step later.
-        const uint32_t last_page = (end - 1) >> shift;
-        const int32_t* table = a.table + static_cast<uint64_t>(request) * a.table_width;
-        uint32_t window = begin >> shift, next_block = 0, next_exps = 0;
-        bool asked = false;
-        auto checked = [&](uint32_t block) {      // (a block outside the cache: the call has failed, block 0 is read instead)
-          const bool bad = block >= a.cache.n_blocks;
-          if (ballot(bad)) *a.status = FIKIT_INVALID_ARG;
-          return bad ? 0u : block;
-        };
-        auto exponents = [&](uint32_t block) {
-          const uint64_t at = static_cast<uint64_t>(block) * a.cache.kv_heads + kv_head;
-          return a.cache.d_k_exp[at] | static_cast<uint32_t>(a.cache.d_v_exp[at]) << 8;
-        };
-        auto ask_next = [&] {
-          asked = window + WAVE <= last_page;
-          if (asked) next_block = static_cast<uint32_t>(table[min_u32(window + WAVE + lane, last_page)]);
-        };
-        // the queries: of query col the dimensions of which this lane reads the keys, 16 of every 64
-        typename T::x8 q[D / 32];
-        {
-          const uint16_t* src = static_cast<const uint16_t*>(a.q.d_data) + request * a.q.token_stride +
-                                static_cast<uint64_t>(first_head + min_u32(col, rows - 1)) * a.q.head_stride + quarter * 16;
-#pragma unroll
-          for (int j = 0; j < D / 32; ++j) {
-            u32x4 w = *reinterpret_cast<const u32x4*>(src + j / 2 * 64 + j % 2 * 8);
-            if (col >= rows) w = u32x4{0, 0, 0, 0};
-            q[j] = bits_as<typename T::x8>(w);
-          }
-        }
-        my_block = checked(my_block);
-        uint32_t my_exps = exponents(my_block);
-
-        // tiles of 16 tokens lie in one page; a tile behind the last token is read from the last page
-        auto tile_at = [&](uint32_t token, uint32_t* exps) {
-          const uint32_t page = min_u32(token >> shift, last_page) - window;
-          const uint32_t block = read_lane_u32(my_block, page);
-          *exps = read_lane_u32(my_exps, page);
-          return (static_cast<uint64_t>(block) * a.cache.kv_heads + kv_head) * unit_bytes + static_cast<uint64_t>(token & (a.cache.block_tokens - 1)) * D;
-        };
-        // Two steps are on their way: a step's keys and values are read into the registers of the step two before as soon as these have
-        // been used.
-        struct Step {
-          u32x4 k[2][D / 64];        // 16 of every 64 codes of a key, of two tiles of tokens
-          uint32_t v[8][KV_WORDS];   // D / 16 codes of each of eight values
-          uint32_t exps[2];
-          uint64_t at[2];
-        };
-        auto load_keys = [&](uint32_t token, Step& x) {
-          if ((token >> shift) - window >= WAVE) {
-            window += WAVE;
-            my_block = next_block;
-            my_exps = next_exps;
-            ask_next();
-          } else if (asked) {
-            asked = false;
-            next_block = checked(next_block);
-            next_exps = exponents(next_block);
-          }
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            x.at[h] = tile_at(token + 16 * h, x.exps + h);
-            const uint8_t* from = a.cache.d_k + x.at[h] + (col * D + quarter * 16);
-#pragma unroll
-            for (int j = 0; j < KV_WORDS; ++j) x.k[h][j] = read(reinterpret_cast<const u32x4*>(from + j * 64));
-          }
-        };
-        auto load_values = [&](Step& x) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint8_t* from = a.cache.d_v + x.at[h] + (quarter * 4 * D + col * (D / 16));
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              if constexpr (KV_WORDS == 2) {
-                const u32x2 w = read(reinterpret_cast<const u32x2*>(from + i * D));
-                x.v[4 * h + i][0] = w[0];
-                x.v[4 * h + i][1] = w[1];
-              } else {
-                x.v[4 * h + i][0] = read(reinterpret_cast<const uint32_t*>(from + i * D));
-              }
-            }
-          }
-        };
-        auto step = [&](uint32_t token, Step& x) {
-          const uint32_t ahead = token + 2 * DECODE_STEP;
-          const float up[2] = {power_of(x.exps[0] >> 8), power_of(x.exps[1] >> 8)};
-          float s[8];
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            f32x4 c = {0.f, 0.f, 0.f, 0.f};
-            const float k_up = power_of(x.exps[h] & 255u);
-#pragma unroll
-            for (int j = 0; j < D / 32; ++j) {
-              u32x4 w;
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                const uint32_t codes = x.k[h][j / 2][(j & 1) * 2 + i];
-                w[2 * i] = T::template codes<false>(codes, k_up);
-                w[2 * i + 1] = T::template codes<true>(codes, k_up);
-              }
-              c = T::mfma16(bits_as<typename T::x8>(w), q[j], c);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[4 * h + i] = c[i] * scale;
-          }
-          if (ahead < end) load_keys(ahead, x);
-          if (token + DECODE_STEP > end) {     // what lies behind the last token counts for nothing, whatever it is
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if (token + (i / 4) * 16 + quarter * 4 + i % 4 >= end) {
-                s[i] = -__builtin_huge_valf();
-#pragma unroll
-                for (int j = 0; j < KV_WORDS; ++j) x.v[i][j] = 0;
-              }
-          }
-          float most = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-          if (ballot(most > m + (DECODE_SLACK + T::WEIGHT_BIAS))) {
-            most = fmaxf(most, __shfl_xor(most, 16, WAVE));
-            most = fmaxf(most, __shfl_xor(most, 32, WAVE));
-            const float raised = fmaxf(m, most - T::WEIGHT_BIAS);
-            const float down = raised > -__builtin_huge_valf() ? exp2_fast(m - raised) : 1.f;
-            m = raised;
-            l *= down;
-#pragma unroll
-            for (int t = 0; t < D / 16; ++t) acc[t] *= down;
-          }
-          const float origin = m > -__builtin_huge_valf() ? m : 0.f;
-          u32x4 w, rest;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float p = exp2_fast(s[2 * i] - origin), r = exp2_fast(s[2 * i + 1] - origin);
-            l += p + r;
-            w[i] = T::pair(p, r);
-            if (T::WEIGHTS == 2) rest[i] = T::pair(p - T::low(w[i]), r - T::high(w[i]));
-          }
-          const typename T::x8 weights = bits_as<typename T::x8>(w);
-#pragma unroll
-          for (int j = 0; j < KV_WORDS; ++j) {
-            u32x4 y[4];       // operands of four tiles of dimensions
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              // bytes of two tokens side by side: dimensions 0 and 1, 2 and 3
-              const uint32_t lo = __builtin_amdgcn_perm(x.v[2 * i + 1][j], x.v[2 * i][j], 0x05010400u);
-              const uint32_t hi = __builtin_amdgcn_perm(x.v[2 * i + 1][j], x.v[2 * i][j], 0x07030602u);
-              y[0][i] = T::template codes<false>(lo, up[i / 2]);
-              y[1][i] = T::template codes<true>(lo, up[i / 2]);
-              y[2][i] = T::template codes<false>(hi, up[i / 2]);
-              y[3][i] = T::template codes<true>(hi, up[i / 2]);
-            }
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-              acc[4 * j + t] = T::mfma16(bits_as<typename T::x8>(y[t]), weights, acc[4 * j + t]);
-              if (T::WEIGHTS == 2) acc[4 * j + t] = T::mfma16(bits_as<typename T::x8>(y[t]), bits_as<typename T::x8>(rest), acc[4 * j + t]);
-            }
-          }
-          if (ahead < end) load_values(x);
-        };
-        Step even, odd;
-        load_keys(begin, even);
-        load_values(even);
-        ask_next();
-        if (begin + DECODE_STEP < end) {
-          load_keys(begin + DECODE_STEP, odd);
-          load_values(odd);
-        }
-        for (uint32_t token = begin; token < end; token += 2 * DECODE_STEP) {
-          step(token, even);
-          if (token + DECODE_STEP < end) step(token + DECODE_STEP, odd);
-        }
-        l += __shfl_xor(l, 16, WAVE);
-        l += __shfl_xor(l, 32, WAVE);
-      }
-      // the next stretch's blocks are on their way while this one is joined; for another key head they are mostly the same
-      there = left > 0;
-      if (there) {
-        const bool same = unit + 1 < units;
-        const uint32_t next_until = same ? length : next_length, next_chunks = decode_chunks(next_until);
-        uint32_t next_begin, next_end;
-        quarter_of(0, left < next_chunks ? min_u32(next_until, static_cast<uint32_t>(left) * DECODE_CHUNK) : next_until, &next_begin, &next_end);
-        if (!same || next_begin != begin || next_end != end || ((end - 1) >> shift) - (begin >> shift) >= WAVE)
-          ask_blocks(same ? request : request + 1, next_begin, next_end);
-      }
-      // join the waves: lane l holds of query col the dimensions (D / 16) * (4 * quarter + i) + t
-      __syncthreads();          // (the stretch before has been read)
-      if (quarter == 0) sums[wave][col] = make_float2(m, l);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int t = 0; t < D / 16; t += 4) {
-          const f32x4 x = {acc[t][i], acc[t + 1][i], acc[t + 2][i], acc[t + 3][i]};
-          *reinterpret_cast<f32x4*>(&joined[wave][col][D / 16 * (4 * quarter + i) + t]) = x;
-        }
-      __syncthreads();
-      const bool whole = chunk == 0 && last_chunk == chunks;
-      const uint32_t slot = 2 * blockIdx.x + (first_stretch ? 0 : 1);
-      for (uint32_t at = threadIdx.x * 4; at < rows * D; at += DECODE_WAVES * WAVE * 4) {
-        const uint32_t row = at / D, dim = at % D;
-        float most = -__builtin_huge_valf(), sum = 0.f;
-#pragma unroll
-        for (int w = 0; w < DECODE_WAVES; ++w) most = fmaxf(most, sums[w][row].x);
-        const float origin = most > -__builtin_huge_valf() ? most : 0.f;
-        f32x4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < DECODE_WAVES; ++w) {
-          const float f = exp2_fast(sums[w][row].x - origin);
-          sum += sums[w][row].y * f;
-          x += *reinterpret_cast<const f32x4*>(&joined[w][row][dim]) * f;
-        }
-        if (whole) {
-          const uint64_t head = static_cast<uint64_t>(request) * a.q_heads + first_head + row;
-          const float f = sum > 0.f ? 1.f / sum : sum == 0.f ? 1.f : sum;
-          const u32x2 w = {T::pair(x[0] * f, x[1] * f), T::pair(x[2] * f, x[3] * f)};
-          *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + head * D + dim) = w;
-          if (dim == 0 && a.lse) a.lse[head] = (most + log2f(sum)) * LN2;
-        } else {
-          const uint64_t to = static_cast<uint64_t>(slot) * most_rows + row;
-          *reinterpret_cast<f32x4*>(a.part_out + to * D + dim) = x;
-          if (dim == 0) a.part_sums[to] = make_float2(most, sum);
-        }
-      }
-    } else {
-      there = false;
-    }
-    if (left == 0) return;
+    last_chunk = min_u32(chunk + take, weight - DECODE_FIXED);
+    kv_head = unit / a.head_tiles;
+    first_head = kv_head * group + tile * DECODE_ROWS;
+    rows = min_u32(group - tile * DECODE_ROWS, DECODE_ROWS);
+    const uint32_t from = chunk * DECODE_CHUNK, until = min_u32(length, last_chunk * DECODE_CHUNK);
+    const uint32_t per_wave = (((until - from) + DECODE_WAVES - 1) / DECODE_WAVES + DECODE_STEP - 1) / DECODE_STEP * DECODE_STEP;
+    begin = from + wave * per_wave;
+    end = min_u32(begin + per_wave, until);
+  };
+  auto ask_length = [&] { next_length = static_cast<uint32_t>(a.lengths[min_u32(request + 1, a.n_requests - 1)]); };
+  auto advance = [&] {
+    if (left == 0) return false;
+    first_stretch = false;
     chunk = 0;
     if (++unit == units) {
       unit = 0;
-      first += weight;
       ++request;
       length = uniform(next_length);
       weight = decode_weight(length);
+      ask_length();
     }
+    derive();
+    return true;
+  };
+
+  // Lane i holds block and exponents of the i-th page of a window of 64; of the next window the blocks are read when a window
+  // begins, and the exponents a step later.
+  uint32_t window = 0, last_page = 0, my_block = 0, my_exps = 0, next_block = 0, next_exps = 0;
+  bool asked = false;
+  const int32_t* table = a.table;
+  auto checked = [&](uint32_t block) {      // (a block outside the cache: the call has failed, block 0 is read instead)
+    const bool bad = block >= a.cache.n_blocks;
+    if (ballot(bad)) *a.status = FIKIT_INVALID_ARG;
+    return bad ? 0u : block;
+  };
+  auto exponents = [&](uint32_t block) {
+    const uint64_t at = static_cast<uint64_t>(block) * a.cache.kv_heads + kv_head;
+    return a.cache.d_k_exp[at] | static_cast<uint32_t>(a.cache.d_v_exp[at]) << 8;
+  };
+  auto ask_blocks = [&] {
+    if (begin >= end) return;
+    window = begin >> shift;
+    last_page = (end - 1) >> shift;
+    table = a.table + static_cast<uint64_t>(request) * a.table_width;
+    my_block = static_cast<uint32_t>(table[min_u32(window + lane, last_page)]);
+  };
+  auto ask_next_blocks = [&] {
+    asked = window + WAVE <= last_page;
+    if (asked) next_block = static_cast<uint32_t>(table[min_u32(window + WAVE + lane, last_page)]);
+  };
+  // Two steps are on their way: a step's keys and values are read into the registers of the step two before as soon as these have
+  // been used.
+  struct Step {
+    u32x4 k[2][D / 64];        // 16 of every 64 codes of a key, of two tiles of tokens
+    uint32_t v[8][KV_WORDS];   // D / 16 codes of each of eight values
+    uint32_t exps[2];
+    uint64_t at[2];
+  };
+  // (tiles of 16 tokens lie in one page; a tile behind the last token is read from the last page)
+  auto page_of = [&](uint32_t token) { return min_u32(token >> shift, last_page) - window; };
+  auto load_keys = [&](uint32_t token, Step& x) {
+    if ((token >> shift) - window >= WAVE) {
+      window += WAVE;
+      my_block = next_block;
+      my_exps = next_exps;
+      ask_next_blocks();
+    } else if (asked) {
+      asked = false;
+      next_block = checked(next_block);
+      next_exps = exponents(next_block);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t block = read_lane_u32(my_block, page_of(token + 16 * h));
+      x.at[h] = (static_cast<uint64_t>(block) * a.cache.kv_heads + kv_head) * unit_bytes + static_cast<uint64_t>((token + 16 * h) & (a.cache.block_tokens - 1)) * D;
+      const uint8_t* from = a.cache.d_k + x.at[h] + (col * D + quarter * 16);
+#pragma unroll
+      for (int j = 0; j < KV_WORDS; ++j) x.k[h][j] = read(reinterpret_cast<const u32x4*>(from + j * 64));
+    }
+  };
+  auto load_values = [&](uint32_t token, Step& x) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint8_t* from = a.cache.d_v + x.at[h] + (quarter * 4 * D + col * (D / 16));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (KV_WORDS == 2) {
+          const u32x2 w = read(reinterpret_cast<const u32x2*>(from + i * D));
+          x.v[4 * h + i][0] = w[0];
+          x.v[4 * h + i][1] = w[1];
+        } else {
+          x.v[4 * h + i][0] = read(reinterpret_cast<const uint32_t*>(from + i * D));
+        }
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) x.exps[h] = read_lane_u32(my_exps, page_of(token + 16 * h));
+  };
+  Step even, odd;
+  typename T::x8 q[D / 32];      // of query col the dimensions of which this lane reads the keys, 16 of every 64
+  auto begin_reading = [&] {     // (ask_blocks before)
+    if (begin >= end) return;
+    const uint16_t* src = static_cast<const uint16_t*>(a.q.d_data) + request * a.q.token_stride +
+                          static_cast<uint64_t>(first_head + min_u32(col, rows - 1)) * a.q.head_stride + quarter * 16;
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {
+      u32x4 w = *reinterpret_cast<const u32x4*>(src + j / 2 * 64 + j % 2 * 8);
+      if (col >= rows) w = u32x4{0, 0, 0, 0};
+      q[j] = bits_as<typename T::x8>(w);
+    }
+    my_block = checked(my_block);
+    my_exps = exponents(my_block);
+    asked = false;
+    load_keys(begin, even);
+    const bool two = begin + DECODE_STEP < end;
+    if (two) load_keys(begin + DECODE_STEP, odd);
+    load_values(begin, even);
+    if (two) load_values(begin + DECODE_STEP, odd);
+    ask_next_blocks();
+  };
+
+  ask_length();
+  derive();
+  if (chunk >= last_chunk && !advance()) return;
+  ask_blocks();
+  begin_reading();
+  for (;;) {
+    f32x4 acc[D / 16];
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -__builtin_huge_valf(), l = 0.f;        // of query col; l over this lane's tokens
+    auto step = [&](uint32_t token, Step& x) {
+      const uint32_t ahead = token + 2 * DECODE_STEP;
+      const float up[2] = {power_of(x.exps[0] >> 8), power_of(x.exps[1] >> 8)};
+      float s[8];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        f32x4 c = {0.f, 0.f, 0.f, 0.f};
+        const float k_up = power_of(x.exps[h] & 255u);
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) {
+          u32x4 w;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t codes = x.k[h][j / 2][(j & 1) * 2 + i];
+            w[2 * i] = T::template codes<false>(codes, k_up);
+            w[2 * i + 1] = T::template codes<true>(codes, k_up);
+          }
+          c = T::mfma16(bits_as<typename T::x8>(w), q[j], c);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[4 * h + i] = c[i] * scale;
+      }
+      if (ahead < end) load_keys(ahead, x);
+      if (token + DECODE_STEP > end) {     // what lies behind the last token counts for nothing, whatever it is
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (token + (i / 4) * 16 + quarter * 4 + i % 4 >= end) {
+            s[i] = -__builtin_huge_valf();
+#pragma unroll
+            for (int j = 0; j < KV_WORDS; ++j) x.v[i][j] = 0;
+          }
+      }
+      float most = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+      if (ballot(most > m + (DECODE_SLACK + T::WEIGHT_BIAS))) {
+        most = fmaxf(most, __shfl_xor(most, 16, WAVE));
+        most = fmaxf(most, __shfl_xor(most, 32, WAVE));
+        const float raised = fmaxf(m, most - T::WEIGHT_BIAS);
+        const float down = raised > -__builtin_huge_valf() ? exp2_fast(m - raised) : 1.f;
+        m = raised;
+        l *= down;
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t) acc[t] *= down;
+      }
+      const float origin = m > -__builtin_huge_valf() ? m : 0.f;
+      u32x4 w, rest;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p = exp2_fast(s[2 * i] - origin), r = exp2_fast(s[2 * i + 1] - origin);
+        l += p + r;
+        w[i] = T::pair(p, r);
+        rest[i] = T::pair(p - T::low(w[i]), r - T::high(w[i]));
+      }
+      const typename T::x8 weights = bits_as<typename T::x8>(w);
+#pragma unroll
+      for (int j = 0; j < KV_WORDS; ++j) {
+        u32x4 y[4];       // operands of four tiles of dimensions
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          // bytes of two tokens side by side: dimensions 0 and 1, 2 and 3
+          const uint32_t lo = __builtin_amdgcn_perm(x.v[2 * i + 1][j], x.v[2 * i][j], 0x05010400u);
+          const uint32_t hi = __builtin_amdgcn_perm(x.v[2 * i + 1][j], x.v[2 * i][j], 0x07030602u);
+          y[0][i] = T::template codes<false>(lo, up[i / 2]);
+          y[1][i] = T::template codes<true>(lo, up[i / 2]);
+          y[2][i] = T::template codes<false>(hi, up[i / 2]);
+          y[3][i] = T::template codes<true>(hi, up[i / 2]);
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          acc[4 * j + t] = T::mfma16(bits_as<typename T::x8>(y[t]), weights, acc[4 * j + t]);
+          acc[4 * j + t] = T::mfma16(bits_as<typename T::x8>(y[t]), bits_as<typename T::x8>(rest), acc[4 * j + t]);
+        }
+      }
+      if (ahead < end) load_values(ahead, x);
+    };
+    for (uint32_t token = begin; token < end; token += 2 * DECODE_STEP) {
+      step(token, even);
+      if (token + DECODE_STEP < end) step(token + DECODE_STEP, odd);
+    }
+    l += __shfl_xor(l, 16, WAVE);
+    l += __shfl_xor(l, 32, WAVE);
+    // where the results go; then the next stretch's blocks are asked for, while the waves write what they have, and its keys and
+    // values, while that is joined (for another key head of a request the blocks are mostly the same)
+    const uint64_t out_head = static_cast<uint64_t>(request) * a.q_heads + first_head;
+    const uint32_t out_rows = rows, slot = 2 * blockIdx.x + (first_stretch ? 0 : 1);
+    const bool whole = chunk == 0 && last_chunk == weight - DECODE_FIXED;
+    const uint32_t old_request = request, old_begin = begin, old_end = end;
+    const bool more = advance();
+    if (more && (request != old_request || begin != old_begin || end != old_end || ((end - 1) >> shift) - (begin >> shift) >= WAVE)) ask_blocks();
+
+    __syncthreads();          // (the stretch before has been read)
+    // lane l holds of query col the dimensions (D / 16) * (4 * quarter + i) + t
+    if (quarter == 0) sums[wave][col] = make_float2(m, l);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int t = 0; t < D / 16; t += 4) {
+        const f32x4 x = {acc[t][i], acc[t + 1][i], acc[t + 2][i], acc[t + 3][i]};
+        *reinterpret_cast<f32x4*>(&joined[wave][col][D / 16 * (4 * quarter + i) + t]) = x;
+      }
+    __syncthreads();
+    if (more) begin_reading();
+    for (uint32_t at = threadIdx.x * 4; at < out_rows * D; at += DECODE_WAVES * WAVE * 4) {
+      const uint32_t row = at / D, dim = at % D;
+      float most = -__builtin_huge_valf(), sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < DECODE_WAVES; ++w) most = fmaxf(most, sums[w][row].x);
+      const float origin = most > -__builtin_huge_valf() ? most : 0.f;
+      f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < DECODE_WAVES; ++w) {
+        const float f = exp2_fast(sums[w][row].x - origin);
+        sum += sums[w][row].y * f;
+        x += *reinterpret_cast<const f32x4*>(&joined[w][row][dim]) * f;
+      }
+      if (whole) {
+        const float f = sum > 0.f ? 1.f / sum : sum == 0.f ? 1.f : sum;
+        const u32x2 w = {T::pair(x[0] * f, x[1] * f), T::pair(x[2] * f, x[3] * f)};
+        *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + (out_head + row) * D + dim) = w;
+        if (dim == 0 && a.lse) a.lse[out_head + row] = (most + log2f(sum)) * LN2;
+      } else {
+        const uint64_t to = static_cast<uint64_t>(slot) * most_rows + row;
+        *reinterpret_cast<f32x4*>(a.part_out + to * D + dim) = x;
+        if (dim == 0) a.part_sums[to] = make_float2(most, sum);
+      }
+    }
+    if (!more) return;
   }
 }
 
-// Joins the parts of one request and query head, always in the same order: each wave every fourth part, then the waves.
+// Joins the parts of a request and unit that was cut.  A workgroup for each place where one of k_decode's workgroups began: the n
+// parts of a unit have n - 1 such places, whose workgroups share its query heads.  The parts of a head are added up in the same order
+// always: by one wave, or, if a workgroup has a single head, by each wave every fourth part and then the waves.
 template <typename T, int D>
 __global__ __launch_bounds__(DECODE_WAVES * WAVE) void k_decode_join(DecodeArgs a) {
   __shared__ float2 sums[DECODE_WAVES];
   __shared__ float outs[DECODE_WAVES][D];
-  const uint32_t request = blockIdx.x / a.q_heads, q_head = blockIdx.x % a.q_heads;
-  const uint32_t first = a.firsts[request], per_unit = a.firsts[a.n_requests], length = static_cast<uint32_t>(a.lengths[request]);
   if (stopped(a.status)) return;
   const uint32_t units = a.cache.kv_heads * a.head_tiles, group = a.q_heads / a.cache.kv_heads, most_rows = min_u32(group, DECODE_ROWS);
-  const uint32_t unit = q_head / group * a.head_tiles + q_head % group / DECODE_ROWS, row = q_head % group % DECODE_ROWS;
-  const uint64_t total = static_cast<uint64_t>(per_unit) * units;
+  const uint64_t total = static_cast<uint64_t>(*a.per_unit) * units;
   const uint32_t groups = total < a.groups ? static_cast<uint32_t>(total) : a.groups;
-  const uint32_t chunks = decode_chunks(length);
-  const uint64_t begin = static_cast<uint64_t>(first) * units + static_cast<uint64_t>(unit) * decode_weight(length);
-  const uint32_t from = decode_owner(begin, total, groups), to = decode_owner(begin + chunks - 1, total, groups);
-  if (from >= to || to >= groups) return;
+  if (blockIdx.x >= groups) return;
+  const uint4 cut = a.cuts[blockIdx.x];
+  const uint32_t request = cut.x, unit = cut.y, chunks = cut.w - DECODE_FIXED;
+  if (cut.z == 0 || cut.z >= chunks) return;                  // (begins with the unit, or behind its last chunk)
+  const uint64_t begin = blockIdx.x * total / groups - cut.z;
+  const uint32_t from = decode_owner(begin, total, groups), parts = decode_owner(begin + chunks - 1, total, groups) - from + 1;
+  const uint32_t mine = blockIdx.x - from - 1, sharers = parts - 1;
+  const uint32_t tile = unit % a.head_tiles, rows = min_u32(group - tile * DECODE_ROWS, DECODE_ROWS);
+  if (mine >= sharers || mine >= rows) return;
+  const uint64_t head0 = static_cast<uint64_t>(request) * a.q_heads + unit / a.head_tiles * group + tile * DECODE_ROWS;
   // the first part is its workgroup's last stretch, and its first one too if the workgroup begins here
-  const uint32_t from_slot = 2 * from + (from * total / groups >= begin ? 0 : 1), parts = to - from + 1;
+  const uint32_t from_slot = 2 * from + (from * total / groups >= begin ? 0 : 1);
   const uint32_t lane = lane_id(), wave = uniform(threadIdx.x / WAVE);
-  constexpr int PER = D / WAVE, MANY = 4;
-  float most = -__builtin_huge_valf(), total_sum = 0.f, x[PER];
-  for (int i = 0; i < PER; ++i) x[i] = 0.f;
-  for (uint32_t p = wave; p < parts; p += DECODE_WAVES * MANY) {
-    float2 s[MANY];
-    float y[MANY][PER];
+  const bool shared = rows <= mine + sharers;                 // one head, all waves
+  const uint32_t stride = shared ? DECODE_WAVES : 1;
+  constexpr int PER = D / WAVE, MANY = 8;
+  for (uint32_t row = mine + (shared ? 0 : wave * sharers); row < rows; row += sharers * DECODE_WAVES) {
+    float most = -__builtin_huge_valf(), sum = 0.f, x[PER];
+    for (int i = 0; i < PER; ++i) x[i] = 0.f;
+    for (uint32_t p = shared ? wave : 0; p < parts; p += stride * MANY) {
+      float2 s[MANY];
+      float y[MANY][PER];
 #pragma unroll
-    for (int j = 0; j < MANY; ++j) {
-      const uint32_t part = min_u32(p + j * DECODE_WAVES, parts - 1);
-      const uint64_t at = static_cast<uint64_t>(part == 0 ? from_slot : 2 * (from + part)) * most_rows + row;
-      s[j] = a.part_sums[at];
-      for (int i = 0; i < PER; ++i) y[j][i] = a.part_out[at * D + lane * PER + i];
+      for (int j = 0; j < MANY; ++j) {
+        const uint32_t part = min_u32(p + j * stride, parts - 1);
+        const uint64_t at = static_cast<uint64_t>(part == 0 ? from_slot : 2 * (from + part)) * most_rows + row;
+        s[j] = a.part_sums[at];
+        for (int i = 0; i < PER; ++i) y[j][i] = a.part_out[at * D + lane * PER + i];
+      }
+      float top = most;
+#pragma unroll
+      for (int j = 0; j < MANY; ++j) top = fmaxf(top, s[j].x);
+      const float origin = top > -__builtin_huge_valf() ? top : 0.f, down = exp2_fast(most - origin);
+      sum *= down;
+      for (int i = 0; i < PER; ++i) x[i] *= down;
+#pragma unroll
+      for (int j = 0; j < MANY; ++j) {
+        if (p + j * stride >= parts) continue;
+        const float f = exp2_fast(s[j].x - origin);
+        sum += s[j].y * f;
+        for (int i = 0; i < PER; ++i) x[i] += y[j][i] * f;
+      }
+      most = top;
     }
-    float top = most;
-#pragma unroll
-    for (int j = 0; j < MANY; ++j) top = fmaxf(top, s[j].x);
-    const float origin = top > -__builtin_huge_valf() ? top : 0.f, down = exp2_fast(most - origin);
-    total_sum *= down;
-    for (int i = 0; i < PER; ++i) x[i] *= down;
-#pragma unroll
-    for (int j = 0; j < MANY; ++j) {
-      if (p + j * DECODE_WAVES >= parts) continue;
-      const float f = exp2_fast(s[j].x - origin);
-      total_sum += s[j].y * f;
-      for (int i = 0; i < PER; ++i) x[i] += y[j][i] * f;
+    if (shared) {
+      if (lane == 0) sums[wave] = make_float2(most, sum);
+      for (int i = 0; i < PER; ++i) outs[wave][lane * PER + i] = x[i];
+      __syncthreads();
+      if (wave != 0) return;
+      most = -__builtin_huge_valf();
+      for (int w = 0; w < DECODE_WAVES; ++w) most = fmaxf(most, sums[w].x);
+      const float origin = most > -__builtin_huge_valf() ? most : 0.f;
+      sum = 0.f;
+      for (int i = 0; i < PER; ++i) x[i] = 0.f;
+      for (int w = 0; w < DECODE_WAVES; ++w) {
+        const float f = exp2_fast(sums[w].x - origin);
+        sum += sums[w].y * f;
+        for (int i = 0; i < PER; ++i) x[i] += outs[w][lane * PER + i] * f;
+      }
     }
-    most = top;
+    const float f = sum > 0.f ? 1.f / sum : sum == 0.f ? 1.f : sum;
+    uint16_t* out = static_cast<uint16_t*>(a.out) + (head0 + row) * D + lane * PER;
+    if constexpr (PER == 2) *reinterpret_cast<uint32_t*>(out) = T::pair(x[0] * f, x[1] * f);
+    else *out = static_cast<uint16_t>(T::pair(x[0] * f, 0.f));
+    if (lane == 0 && a.lse) a.lse[head0 + row] = (most + log2f(sum)) * LN2;
   }
-  if (lane == 0) sums[wave] = make_float2(most, total_sum);
-  for (int i = 0; i < PER; ++i) outs[wave][lane * PER + i] = x[i];
-  __syncthreads();
-  if (threadIdx.x >= D / 2) return;
-  float top = -__builtin_huge_valf();
-  for (int w = 0; w < DECODE_WAVES; ++w) top = fmaxf(top, sums[w].x);
-  const float origin = top > -__builtin_huge_valf() ? top : 0.f;
-  float sum = 0.f, lo = 0.f, hi = 0.f;
-  for (int w = 0; w < DECODE_WAVES; ++w) {
-    const float f = exp2_fast(sums[w].x - origin);
-    sum += sums[w].y * f;
-    lo += outs[w][2 * threadIdx.x] * f;
-    hi += outs[w][2 * threadIdx.x + 1] * f;
-  }
-  const float f = sum > 0.f ? 1.f / sum : sum == 0.f ? 1.f : sum;
-  const uint64_t head = blockIdx.x;
-  reinterpret_cast<uint32_t*>(a.out)[head * (D / 2) + threadIdx.x] = T::pair(lo * f, hi * f);
-  if (threadIdx.x == 0 && a.lse) a.lse[head] = (top + log2f(sum)) * LN2;
 }
 
 }  // namespace fikit

@@ -62,7 +62,7 @@ struct AppendCall {
 // How many workgroups a decode step takes, and its workspace.
 struct DecodeCut {
   uint32_t head_tiles, groups;
-  uint64_t firsts_bytes, sums_bytes, bytes;
+  uint64_t cuts_bytes, sums_bytes, bytes;
   bool fits;
 };
 constexpr uint64_t DECODE_CHIP_128 = 512, DECODE_CHIP_64 = 1024;     // what the chip holds at once of k_decode, by the head's size
@@ -73,12 +73,12 @@ DecodeCut decode_cut(uint32_t n_requests, uint32_t q_heads, uint32_t kv_heads, u
   const uint64_t group = q_heads / kv_heads, rows = group < DECODE_ROWS ? group : DECODE_ROWS;
   c.head_tiles = static_cast<uint32_t>((group + DECODE_ROWS - 1) / DECODE_ROWS);
   const uint64_t chunks = static_cast<uint64_t>(n_requests) * decode_chunks(max_length), all = chunks * kv_heads * c.head_tiles;
-  c.fits = chunks < (1ull << 32) && static_cast<uint64_t>(n_requests) * q_heads <= MOST_GROUPS;
+  c.fits = chunks + n_requests * DECODE_FIXED < (1ull << 32);
   const uint64_t chip = head_dim == 128 ? DECODE_CHIP_128 : DECODE_CHIP_64;
   c.groups = static_cast<uint32_t>(all < chip ? all : chip);
-  c.firsts_bytes = whole((static_cast<uint64_t>(n_requests) + 1) * sizeof(uint32_t));
+  c.cuts_bytes = whole(c.groups * sizeof(uint4) + sizeof(uint32_t));
   c.sums_bytes = whole(2 * c.groups * rows * sizeof(float2));
-  c.bytes = c.firsts_bytes + c.sums_bytes + 2 * c.groups * rows * head_dim * sizeof(float);
+  c.bytes = c.cuts_bytes + c.sums_bytes + 2 * c.groups * rows * head_dim * sizeof(float);
   return c;
 }
 
@@ -91,7 +91,7 @@ struct DecodeCall {
     const dim3 grid(c.groups), block(DECODE_WAVES * WAVE);
     if (int rc = c.head_tiles == 1 ? enqueue(k_decode<T, D, true>, grid, block, st, a) : enqueue(k_decode<T, D, false>, grid, block, st, a)) return rc;
     if (a.max_length <= DECODE_CHUNK) return FIKIT_OK;      // (no request has several chunks)
-    return enqueue(k_decode_join<T, D>, dim3(a.n_requests * a.q_heads), dim3(DECODE_WAVES * WAVE), st, a);
+    return enqueue(k_decode_join<T, D>, grid, block, st, a);
   }
 };
 
@@ -215,9 +215,10 @@ int fikit_cache_attention(const fikit_cache* h_cache, const fikit_vectors* h_q, 
   a.lse = d_lse;
   a.status = d_status;
   unsigned char* ws = static_cast<unsigned char*>(d_workspace);
-  a.firsts = reinterpret_cast<uint32_t*>(ws);
-  a.part_sums = reinterpret_cast<float2*>(ws + c.firsts_bytes);
-  a.part_out = reinterpret_cast<float*>(ws + c.firsts_bytes + c.sums_bytes);
+  a.cuts = reinterpret_cast<uint4*>(ws);
+  a.per_unit = reinterpret_cast<uint32_t*>(ws + c.groups * sizeof(uint4));
+  a.part_sums = reinterpret_cast<float2*>(ws + c.cuts_bytes);
+  a.part_out = reinterpret_cast<float*>(ws + c.cuts_bytes + c.sums_bytes);
   a.q_heads = q_heads;
   a.table_width = table_width;
   a.max_length = max_length;

@@ -34,7 +34,6 @@ struct Bf16 {
   typedef bf16x8 x8;
   static constexpr uint32_t EXP_MASK = 0x7f807f80u, INF = 0x7f80u, ONE = 0x3f80u;
   static constexpr float WEIGHT_BIAS = 0.f;
-  static constexpr int WEIGHTS = 2;      // operands that a weight takes where products are not what bounds a kernel
   static __device__ __forceinline__ uint32_t pair(float a, float b) {
     const bf16x2 v = {static_cast<__bf16>(a), static_cast<__bf16>(b)};
     return bits_as<uint32_t>(v);
@@ -62,7 +61,6 @@ struct F16 {
   static constexpr uint32_t EXP_MASK = 0x7c007c00u, INF = 0x7c00u, ONE = 0x3c00u;
   // Weights are held relative to the largest score seen, times 2^7: what is far below it keeps its bits longer.
   static constexpr float WEIGHT_BIAS = 7.f;
-  static constexpr int WEIGHTS = 1;
   static __device__ __forceinline__ uint32_t pair(float a, float b) {
     const f16x2 v = {static_cast<_Float16>(a), static_cast<_Float16>(b)};
     return bits_as<uint32_t>(v);
