@@ -24,52 +24,52 @@ struct PlanArgs {
   int4* pieces;
   int32_t* counts;
   int32_t* status;
-  int2* bases;              // per request: new blocks and pieces of those before it
+  uint2* bases;             // per request: new blocks and pieces of those before it
   uint32_t n_requests, n_tokens, table_width, n_free, room;
   uint32_t shift;           // of the block length
 };
 
-struct PlanSums {
-  uint64_t tokens;
-  uint32_t blocks, pieces;  // (at most as many as tokens that fit 31 bits, or the call has failed)
-};
-
 constexpr int PLAN_THREADS = 1024;
 
-// What request r adds to the sums; false if its lengths cannot be.
-__device__ __forceinline__ bool plan_request(const PlanArgs& a, int64_t cached, int64_t added, PlanSums* s) {
-  const int64_t length = cached + added;
-  if (cached < 0 || added < 0 || length > INT32_MAX || length > static_cast<int64_t>(a.table_width) << a.shift) return false;
-  const int64_t block = int64_t{1} << a.shift;
-  s->tokens += static_cast<uint64_t>(added);
-  s->blocks += static_cast<uint32_t>(((length + block - 1) >> a.shift) - ((cached + block - 1) >> a.shift));
-  if (added > 0) s->pieces += static_cast<uint32_t>(((length - 1) >> a.shift) - (cached >> a.shift) + 1);
-  return true;
+struct PlanSums {
+  uint32_t tokens, blocks, pieces;
+};
+
+// What a request of c cached and a added tokens adds to the sums; false if these cannot be, or a sum does not fit.  (Blocks and
+// pieces are at most as many as tokens.)
+__device__ __forceinline__ bool plan_request(const PlanArgs& a, int32_t c, int32_t d, PlanSums* s) {
+  const uint32_t cached = static_cast<uint32_t>(c), added = static_cast<uint32_t>(d), length = cached + added, last = (1u << a.shift) - 1;
+  const bool ok = c >= 0 && d >= 0 && length <= INT32_MAX && ((static_cast<uint64_t>(length) + last) >> a.shift) <= a.table_width;
+  s->blocks += ((length + last) >> a.shift) - ((cached + last) >> a.shift);
+  s->pieces += d > 0 ? ((length - 1) >> a.shift) - (cached >> a.shift) + 1 : 0;
+  s->tokens += added;
+  return ok && s->tokens >= added;
 }
 
 struct PlanScan {
-  uint64_t tokens[PLAN_THREADS / WAVE];
   uint32_t blocks[PLAN_THREADS / WAVE], pieces[PLAN_THREADS / WAVE];
+  uint64_t tokens[PLAN_THREADS / WAVE];
 };
 
-// The sums of the threads before, and of all of them, in a workgroup of PLAN_THREADS; whether `ok` holds in all.
+// The sums of the threads before, and of all of them, in a workgroup of PLAN_THREADS; whether `ok` holds in all and all sums fit.
 __device__ __forceinline__ bool plan_scan(const PlanSums& mine, bool ok, PlanScan* lds, PlanSums* before, PlanSums* total) {
-  PlanSums run = mine;
-  for (int d = 1; d < WAVE; d <<= 1) {
-    const uint64_t t = shfl_up_u64(run.tokens, d);
-    const uint32_t b = __shfl_up(run.blocks, d, WAVE), p = __shfl_up(run.pieces, d, WAVE);
-    if (lane_id() >= static_cast<uint32_t>(d)) { run.tokens += t; run.blocks += b; run.pieces += p; }
-  }
-  const uint32_t wave = threadIdx.x / WAVE;
-  if (lane_id() == WAVE - 1) { lds->tokens[wave] = run.tokens; lds->blocks[wave] = run.blocks; lds->pieces[wave] = run.pieces; }
+  constexpr uint32_t WAVES = PLAN_THREADS / WAVE;
+  const uint64_t run_tokens = wave_incl_scan_u64(mine.tokens);
+  const uint32_t run_blocks = wave_incl_scan_u32(mine.blocks), run_pieces = wave_incl_scan_u32(mine.pieces);
+  const uint32_t wave = uniform(threadIdx.x / WAVE), lane = lane_id();
+  if (lane == WAVE - 1) { lds->tokens[wave] = run_tokens; lds->blocks[wave] = run_blocks; lds->pieces[wave] = run_pieces; }
   const bool all = __syncthreads_and(ok);
-  *before = PlanSums{run.tokens - mine.tokens, run.blocks - mine.blocks, run.pieces - mine.pieces};
-  *total = PlanSums{0, 0, 0};
-  for (uint32_t w = 0; w < PLAN_THREADS / WAVE; ++w) {
-    if (w < wave) { before->tokens += lds->tokens[w]; before->blocks += lds->blocks[w]; before->pieces += lds->pieces[w]; }
-    total->tokens += lds->tokens[w]; total->blocks += lds->blocks[w]; total->pieces += lds->pieces[w];
-  }
-  return all;
+  // each wave scans the waves' sums
+  const bool there = lane < WAVES;
+  const uint64_t tokens = there ? lds->tokens[lane % WAVES] : 0;
+  const uint32_t blocks = there ? lds->blocks[lane % WAVES] : 0, pieces = there ? lds->pieces[lane % WAVES] : 0;
+  const uint64_t upto = wave_incl_scan_u64(tokens);
+  const uint32_t upto_blocks = wave_incl_scan_u32(blocks), upto_pieces = wave_incl_scan_u32(pieces);
+  *total = PlanSums{read_lane_u32(static_cast<uint32_t>(upto), WAVES - 1), read_lane_u32(upto_blocks, WAVES - 1), read_lane_u32(upto_pieces, WAVES - 1)};
+  *before = PlanSums{read_lane_u32(static_cast<uint32_t>(upto - tokens), wave) + static_cast<uint32_t>(run_tokens) - mine.tokens,
+                     read_lane_u32(upto_blocks - blocks, wave) + run_blocks - mine.blocks,
+                     read_lane_u32(upto_pieces - pieces, wave) + run_pieces - mine.pieces};
+  return all && read_lane_u64(upto, WAVES - 1) <= INT32_MAX;
 }
 
 __device__ __forceinline__ int32_t plan_error(const PlanArgs& a, const PlanSums& total, bool ok) {
@@ -85,38 +85,54 @@ __device__ __forceinline__ uint32_t plan_find(const int32_t* offsets, uint32_t l
   return lo;
 }
 
-// What new token t, of request r that begins at token `first`, writes.
-__device__ __forceinline__ void plan_token(const PlanArgs& a, uint32_t t, uint32_t r, uint32_t first, int2 base) {
+// What new token t, of request r that begins at token `first`, writes; `blocks`, `pieces`: those of the requests before.
+__device__ __forceinline__ void plan_token(const PlanArgs& a, uint32_t t, uint32_t r, uint32_t first, uint32_t blocks, uint32_t pieces) {
   const uint32_t block_tokens = 1u << a.shift;
   const uint32_t cached = static_cast<uint32_t>(a.cached[r]), length = cached + static_cast<uint32_t>(a.added[r]);
   const uint32_t index = t - first;
   const uint32_t place = cached + index, page = place >> a.shift, at = place & (block_tokens - 1);
   const uint32_t held = (cached + block_tokens - 1) >> a.shift;
   int32_t* entry = a.table + static_cast<uint64_t>(r) * a.table_width + page;
-  const int32_t block = page >= held ? a.free_blocks[base.x + (page - held)] : *entry;
+  const int32_t block = page >= held ? a.free_blocks[blocks + (page - held)] : *entry;
   if (at == 0) *entry = block;      // (a block that begins at a new token is a new one)
   if (a.slots) a.slots[t] = static_cast<int64_t>(block) * block_tokens + at;
   if (at == 0 || index == 0)
-    a.pieces[base.y + (page - (cached >> a.shift))] = make_int4(block, static_cast<int32_t>(t), static_cast<int32_t>(at),
+    a.pieces[pieces + (page - (cached >> a.shift))] = make_int4(block, static_cast<int32_t>(t), static_cast<int32_t>(at),
                                                                static_cast<int32_t>(min_u32(block_tokens - at, length - place)));
 }
 
-// The whole plan in one launch: every workgroup sums all requests for itself, in LDS, and takes 1024 tokens at a time.
-constexpr uint32_t PLAN_ONE_REQUESTS = 4096;
+// Eight or sixteen consecutive requests are read as vectors of words; the arrays need no more alignment than that.
+typedef int32_t i32x4_by_words __attribute__((ext_vector_type(4), aligned(4)));
+template <uint32_t PER>
+__device__ __forceinline__ void plan_read(const int32_t* from, uint64_t first, uint32_t n, int32_t (&to)[PER]) {
+  if (PER % 4 == 0 && first + PER <= n) {
+#pragma unroll
+    for (uint32_t i = 0; i < PER; i += 4) {
+      const i32x4_by_words x = *reinterpret_cast<const i32x4_by_words*>(from + first + i);
+#pragma unroll
+      for (uint32_t j = 0; j < 4; ++j) to[i + j] = x[j];
+    }
+  } else {
+#pragma unroll
+    for (uint32_t i = 0; i < PER; ++i) to[i] = first + i < n ? from[first + i] : 0;
+  }
+}
+
+// The whole plan in one launch: every workgroup sums all requests for itself, a run of PER consecutive ones per thread, and takes
+// 1024 tokens at a time.  Where each request begins is kept in LDS; its blocks and pieces too for runs of up to four, else they
+// are added up again from where its run begins.
+constexpr uint32_t PLAN_ONE_REQUESTS = 16 * PLAN_THREADS;
+template <uint32_t PER>
 __global__ __launch_bounds__(PLAN_THREADS) void k_plan_one(PlanArgs a) {
-  constexpr uint32_t PER = PLAN_ONE_REQUESTS / PLAN_THREADS;
-  __shared__ int32_t offsets[PLAN_ONE_REQUESTS];
-  __shared__ int2 bases[PLAN_ONE_REQUESTS];
+  constexpr bool ALL = PER <= 4;
+  __shared__ int32_t offsets[PER * PLAN_THREADS];
+  __shared__ uint2 bases[(ALL ? PER : 1) * PLAN_THREADS];
   __shared__ PlanScan scan;
   const bool stop = stopped(a.status);
-  const uint32_t per = (a.n_requests + PLAN_THREADS - 1) / PLAN_THREADS, first = threadIdx.x * per;
+  const uint32_t first = threadIdx.x * PER;
   int32_t cached[PER], added[PER];
-#pragma unroll
-  for (uint32_t i = 0; i < PER; ++i) {
-    const bool there = i < per && first + i < a.n_requests;
-    cached[i] = there ? a.cached[first + i] : 0;
-    added[i] = there ? a.added[first + i] : 0;
-  }
+  plan_read<PER>(a.cached, first, a.n_requests, cached);
+  plan_read<PER>(a.added, first, a.n_requests, added);
   if (stop) return;
   PlanSums mine{0, 0, 0}, at, total;
   bool ok = true;
@@ -128,18 +144,18 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_plan_one(PlanArgs a) {
     return;
   }
   const bool writes = blockIdx.x == 0;
+  if (!ALL) bases[threadIdx.x] = make_uint2(at.blocks, at.pieces);
 #pragma unroll
-  for (uint32_t i = 0; i < PER; ++i)
-    if (i < per && first + i < a.n_requests) {
-      const uint32_t r = first + i;
-      offsets[r] = static_cast<int32_t>(at.tokens);
-      bases[r] = make_int2(static_cast<int32_t>(at.blocks), static_cast<int32_t>(at.pieces));
-      if (writes) {
-        a.lengths[r] = cached[i] + added[i];
-        a.token_offsets[r] = static_cast<int32_t>(at.tokens);
-      }
-      plan_request(a, cached[i], added[i], &at);
+  for (uint32_t i = 0; i < PER; ++i) {
+    const uint32_t r = first + i;
+    offsets[r] = static_cast<int32_t>(at.tokens);
+    if (ALL) bases[r] = make_uint2(at.blocks, at.pieces);
+    if (writes && r < a.n_requests) {
+      a.lengths[r] = cached[i] + added[i];
+      a.token_offsets[r] = static_cast<int32_t>(at.tokens);
     }
+    plan_request(a, cached[i], added[i], &at);
+  }
   if (writes && threadIdx.x == 0) {
     a.token_offsets[a.n_requests] = static_cast<int32_t>(a.n_tokens);
     a.counts[0] = static_cast<int32_t>(total.blocks);
@@ -149,14 +165,17 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_plan_one(PlanArgs a) {
   const uint32_t from = blockIdx.x * PLAN_THREADS + threadIdx.x, stride = gridDim.x * PLAN_THREADS;
   for (uint64_t t = from; t < a.n_tokens; t += stride) {
     const uint32_t r = plan_find(offsets, 0, a.n_requests, static_cast<uint32_t>(t));
-    plan_token(a, static_cast<uint32_t>(t), r, static_cast<uint32_t>(offsets[r]), bases[r]);
+    const uint2 base = bases[ALL ? r : r / PER];
+    PlanSums s{0, base.x, base.y};
+    if (!ALL)
+      for (uint32_t j = r / PER * PER; j < r; ++j) plan_request(a, a.cached[j], a.added[j], &s);
+    plan_token(a, static_cast<uint32_t>(t), r, static_cast<uint32_t>(offsets[r]), s.blocks, s.pieces);
   }
   for (uint64_t i = static_cast<uint64_t>(total.pieces) + from; i < a.room; i += stride) a.pieces[i] = make_int4(-1, -1, -1, -1);
 }
 
 // For more requests the sums are one workgroup's, 8 consecutive requests per thread and round, and the tokens a launch behind it.
 constexpr uint32_t PLAN_PER = 8;
-typedef int32_t i32x4_by_words __attribute__((ext_vector_type(4), aligned(4)));
 __global__ __launch_bounds__(PLAN_THREADS) void k_plan_sums(PlanArgs a) {
   __shared__ PlanScan scan[2];
   if (stopped(a.status)) return;
@@ -167,45 +186,32 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_plan_sums(PlanArgs a) {
     const uint64_t first = round + threadIdx.x * PLAN_PER;
     const bool whole = first + PLAN_PER <= a.n_requests;
     int32_t cached[PLAN_PER], added[PLAN_PER];
-    if (whole) {
-#pragma unroll
-      for (uint32_t i = 0; i < PLAN_PER; i += 4) {
-        const i32x4_by_words c = *reinterpret_cast<const i32x4_by_words*>(a.cached + first + i);
-        const i32x4_by_words d = *reinterpret_cast<const i32x4_by_words*>(a.added + first + i);
-#pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) { cached[i + j] = c[j]; added[i + j] = d[j]; }
-      }
-    } else {
-#pragma unroll
-      for (uint32_t i = 0; i < PLAN_PER; ++i) {
-        const bool there = first + i < a.n_requests;
-        cached[i] = there ? a.cached[first + i] : 0;
-        added[i] = there ? a.added[first + i] : 0;
-      }
-    }
+    plan_read<PLAN_PER>(a.cached, first, a.n_requests, cached);
+    plan_read<PLAN_PER>(a.added, first, a.n_requests, added);
     PlanSums mine{0, 0, 0}, at, total;
 #pragma unroll
     for (uint32_t i = 0; i < PLAN_PER; ++i) ok &= plan_request(a, cached[i], added[i], &mine);
     ok = plan_scan(mine, ok, &scan[turn], &at, &total);
     at.tokens += carry.tokens; at.blocks += carry.blocks; at.pieces += carry.pieces;
     carry.tokens += total.tokens; carry.blocks += total.blocks; carry.pieces += total.pieces;
+    ok &= carry.tokens >= total.tokens;
 #pragma unroll
     for (uint32_t i = 0; i < PLAN_PER; i += 4) {
       i32x4_by_words length, offset;
-      int2 base[4];
+      uint2 base[4];
 #pragma unroll
       for (uint32_t j = 0; j < 4; ++j) {
         length[j] = static_cast<int32_t>(static_cast<uint32_t>(cached[i + j]) + static_cast<uint32_t>(added[i + j]));
         offset[j] = static_cast<int32_t>(at.tokens);
-        base[j] = make_int2(static_cast<int32_t>(at.blocks), static_cast<int32_t>(at.pieces));
+        base[j] = make_uint2(at.blocks, at.pieces);
         plan_request(a, cached[i + j], added[i + j], &at);
       }
       if (whole) {
         *reinterpret_cast<i32x4_by_words*>(a.lengths + first + i) = length;
         *reinterpret_cast<i32x4_by_words*>(a.token_offsets + first + i) = offset;
-        int4* to = reinterpret_cast<int4*>(a.bases + first + i);
-        to[0] = make_int4(base[0].x, base[0].y, base[1].x, base[1].y);
-        to[1] = make_int4(base[2].x, base[2].y, base[3].x, base[3].y);
+        uint4* to = reinterpret_cast<uint4*>(a.bases + first + i);
+        to[0] = make_uint4(base[0].x, base[0].y, base[1].x, base[1].y);
+        to[1] = make_uint4(base[2].x, base[2].y, base[3].x, base[3].y);
       } else {
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j)
@@ -230,7 +236,7 @@ __global__ __launch_bounds__(256) void k_plan_tokens(PlanArgs a) {
   const uint32_t t = blockIdx.x * 256 + threadIdx.x;
   if (t < a.n_tokens) {
     const uint32_t r = plan_find(a.token_offsets, 0, a.n_requests, t);
-    plan_token(a, t, r, static_cast<uint32_t>(a.token_offsets[r]), a.bases[r]);
+    plan_token(a, t, r, static_cast<uint32_t>(a.token_offsets[r]), a.bases[r].x, a.bases[r].y);
   }
   for (uint64_t i = static_cast<uint64_t>(static_cast<uint32_t>(a.counts[1])) + t; i < a.room; i += static_cast<uint64_t>(gridDim.x) * 256)
     a.pieces[i] = make_int4(-1, -1, -1, -1);
@@ -276,7 +282,8 @@ __device__ __forceinline__ uint32_t most_of_pairs(uint32_t a, uint32_t b) {
 template <typename T, int D>
 __global__ __launch_bounds__(APPEND_WAVES * WAVE) void k_cache_append(AppendArgs a) {
   const int4 piece = a.pieces[blockIdx.x];
-  if (piece.x == -1 || stopped(a.status)) return;
+  const bool stop = stopped(a.status);
+  if (piece.x == -1 || stop) return;
   const uint32_t lane = lane_id(), unit = blockIdx.y * APPEND_WAVES + uniform(threadIdx.x / WAVE), block_tokens = a.cache.block_tokens;
   const uint32_t block = static_cast<uint32_t>(piece.x), first = static_cast<uint32_t>(piece.y), at = static_cast<uint32_t>(piece.z),
                  count = static_cast<uint32_t>(piece.w);
@@ -317,7 +324,7 @@ __global__ __launch_bounds__(APPEND_WAVES * WAVE) void k_cache_append(AppendArgs
       for (int j = 0; j < 4; ++j) pairs = most_of_pairs(pairs, held[i][j] & 0x7fff7fffu);
   }
   uint32_t bits = max_u32(pairs & 0xffffu, pairs >> 16);
-  for (int d = 1; d < WAVE; d <<= 1) bits = max_u32(bits, __shfl_xor(bits, d, WAVE));
+  bits = max_over_wave(bits);
   const bool odd = bits >= T::INF;  // something is not finite: look again, without it
   if (odd) {
     bits = 0;
@@ -331,7 +338,7 @@ __global__ __launch_bounds__(APPEND_WAVES * WAVE) void k_cache_append(AppendArgs
           bits = max_u32(bits, max_u32(lo < T::INF ? lo : 0, hi < T::INF ? hi : 0));
         }
     }
-    for (int d = 1; d < WAVE; d <<= 1) bits = max_u32(bits, __shfl_xor(bits, d, WAVE));
+    bits = max_over_wave(bits);
   }
   const uint32_t chosen = max_u32(exponent_for(T::low(bits)), old);
   const float scale = power_of(chosen), inverse = power_of(254 - chosen);

@@ -70,11 +70,7 @@ __device__ __forceinline__ bool decode_look(const DecodeArgs& a, DecodeLook* lds
     ok &= n >= 0 && static_cast<uint32_t>(n) <= a.max_length;
     sum += decode_weight(static_cast<uint32_t>(n));
   }
-  uint32_t run = sum;
-  for (int d = 1; d < WAVE; d <<= 1) {
-    const uint32_t x = __shfl_up(run, d, WAVE);
-    if (lane_id() >= static_cast<uint32_t>(d)) run += x;
-  }
+  const uint32_t run = wave_incl_scan_u32(sum);
   const uint32_t wave = threadIdx.x / WAVE;
   if (lane_id() == WAVE - 1) lds->sums[wave] = run;
   if (!__syncthreads_and(ok)) {
@@ -129,11 +125,7 @@ __global__ __launch_bounds__(DECODE_WAVES * WAVE, D == 128 ? 2 : 4) void k_decod
   for (;;) {               // of the requests that a thread has added up, 64 at a time, the one that holds chunk `target`
     const uint32_t r = request + lane;
     const uint32_t n = r < a.n_requests ? static_cast<uint32_t>(a.lengths[r]) : 0, c = decode_weight(n);
-    uint32_t run = c;
-    for (int d = 1; d < WAVE; d <<= 1) {
-      const uint32_t x = __shfl_up(run, d, WAVE);
-      if (lane >= static_cast<uint32_t>(d)) run += x;
-    }
+    const uint32_t run = wave_incl_scan_u32(c);
     const uint64_t beyond = ballot(first + run > target);
     if (beyond) {
       const uint32_t owner = uniform(static_cast<uint32_t>(__builtin_ctzll(beyond)));

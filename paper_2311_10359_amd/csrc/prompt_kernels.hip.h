@@ -268,15 +268,6 @@ struct PromptWave {              // what a wave holds of its 32 rows; a lane of 
   }
 };
 
-// The sum over the wave, in every lane.
-__device__ __forceinline__ uint32_t wave_sum(uint32_t v) {
-  v += static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x111, 0xf, 0xf, true));   // shifts within rows of 16
-  v += static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x112, 0xf, 0xf, true));
-  v += static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x114, 0xf, 0xf, true));
-  v += static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x118, 0xf, 0xf, true));
-  return read_lane_u32(v, 15) + read_lane_u32(v, 31) + read_lane_u32(v, 47) + read_lane_u32(v, 63);
-}
-
 // Which rows a workgroup takes.  Later rows see more, so up to PROMPT_ORDERED prompts the work is handed out by the rows'
 // place in their prompt, the last ones first: item i is in level L (rows L * rows .. of a prompt) if C(L + 1) <= i < C(L), C(L) =
 // sum over prompts of max(0, slots - L).  For more prompts, which fill the chip many times over, slot by slot from the back; prompt
@@ -290,13 +281,13 @@ __device__ __forceinline__ bool prompt_find(const PromptArgs& a, uint32_t rows, 
     if (ballot(!good)) return false;
     const uint32_t slots = lane < a.n_prompts ? (to - from + rows - 1) / rows : 0;
     uint32_t low = 0, high = a.slots;           // C(low) > item >= C(high); the second holds as no prompt has so many
-    if (wave_sum(slots) <= item) { *length = *first = *start = 0; return true; }
+    if (sum_over_wave(slots) <= item) { *length = *first = *start = 0; return true; }
     while (high - low > 1) {
       const uint32_t mid = low + (high - low) / 2;
-      if (wave_sum(slots > mid ? slots - mid : 0) > item) low = mid; else high = mid;
+      if (sum_over_wave(slots > mid ? slots - mid : 0) > item) low = mid; else high = mid;
     }
     uint64_t these = ballot(slots > low);
-    for (uint32_t skip = item - wave_sum(slots > low + 1 ? slots - low - 1 : 0); skip > 0; --skip) these &= these - 1;
+    for (uint32_t skip = item - sum_over_wave(slots > low + 1 ? slots - low - 1 : 0); skip > 0; --skip) these &= these - 1;
     const uint32_t owner = uniform(static_cast<uint32_t>(__builtin_ctzll(these)));
     *start = read_lane_u32(from, owner);
     *length = read_lane_u32(to - from, owner);

@@ -115,7 +115,7 @@ uint64_t fikit_cache_pieces(uint32_t n_tokens, uint32_t n_requests, uint32_t blo
 }
 
 size_t fikit_cache_plan_workspace_bytes(uint32_t n_requests) {
-  return n_requests <= PLAN_ONE_REQUESTS ? 0 : (static_cast<size_t>(n_requests) * sizeof(int2) + 255) / 256 * 256;
+  return n_requests <= PLAN_ONE_REQUESTS ? 0 : (static_cast<size_t>(n_requests) * sizeof(uint2) + 255) / 256 * 256;
 }
 
 int fikit_cache_plan(const int32_t* d_cached, const int32_t* d_added, uint32_t n_requests, uint32_t n_tokens,
@@ -148,7 +148,7 @@ int fikit_cache_plan(const int32_t* d_cached, const int32_t* d_added, uint32_t n
   a.pieces = reinterpret_cast<int4*>(d_pieces);
   a.counts = d_counts;
   a.status = d_status;
-  a.bases = static_cast<int2*>(d_workspace);
+  a.bases = static_cast<uint2*>(d_workspace);
   a.n_requests = n_requests;
   a.n_tokens = n_tokens;
   a.table_width = table_width;
@@ -157,7 +157,10 @@ int fikit_cache_plan(const int32_t* d_cached, const int32_t* d_added, uint32_t n
   a.shift = static_cast<uint32_t>(__builtin_ctz(block_tokens));
   if (n_requests <= PLAN_ONE_REQUESTS) {
     const uint32_t groups = (n_tokens + PLAN_THREADS - 1) / PLAN_THREADS;
-    return enqueue(k_plan_one, dim3(groups < 1 ? 1 : groups > PLAN_ONE_GROUPS ? PLAN_ONE_GROUPS : groups), dim3(PLAN_THREADS), st, a);
+    const dim3 grid(groups < 1 ? 1 : groups > PLAN_ONE_GROUPS ? PLAN_ONE_GROUPS : groups), block(PLAN_THREADS);
+    if (n_requests <= PLAN_THREADS) return enqueue(k_plan_one<1>, grid, block, st, a);
+    if (n_requests <= 4 * PLAN_THREADS) return enqueue(k_plan_one<4>, grid, block, st, a);
+    return enqueue(k_plan_one<16>, grid, block, st, a);
   }
   if (int rc = enqueue(k_plan_sums, dim3(1), dim3(PLAN_THREADS), st, a)) return rc;
   if (n_tokens == 0) return FIKIT_OK;

@@ -93,6 +93,18 @@ constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// The sum and the maximum over the wave, by data-parallel-primitive moves (see wave_incl_scan_u32).
+__device__ __forceinline__ uint32_t sum_over_wave(uint32_t v) { return read_lane_u32(wave_incl_scan_u32(v), WAVE - 1); }
+__device__ __forceinline__ uint32_t max_over_wave(uint32_t v) {
+  v = max_u32(v, dpp_or_zero<0x111, 0xf>(v));
+  v = max_u32(v, dpp_or_zero<0x112, 0xf>(v));
+  v = max_u32(v, dpp_or_zero<0x114, 0xf>(v));
+  v = max_u32(v, dpp_or_zero<0x118, 0xf>(v));
+  v = max_u32(v, dpp_or_zero<0x142, 0xa>(v));
+  v = max_u32(v, dpp_or_zero<0x143, 0xc>(v));
+  return read_lane_u32(v, WAVE - 1);
+}
+
 // Errors are written, success is not: see fikit.h.
 __device__ __forceinline__ bool stopped(const int32_t* status) { return *static_cast<const volatile int32_t*>(status) != FIKIT_OK; }
 

@@ -80,6 +80,25 @@ def test_many_requests_without_tokens_between_others():
     check(cached, added, np.full((n, 32), -1, np.int32), np.arange(need, dtype=np.int32), 16)
 
 
+def test_sums_beyond_32_bits():
+    """Lengths each of which could be, whose sum is the number of tokens modulo 2^32."""
+    for n in (3, 2000, 9000, 20000):
+        added = [0] * n
+        added[0], added[n // 2], added[n - 1] = 2 ** 31 - 1, 2 ** 31 - 1, 7
+        word = i32([0])
+        table = torch.full((n, 4), 9, dtype=torch.int32, device=DEV)
+        # (rows of the table that are long enough: the width is what the call is told)
+        lib = binding.load()
+        out = binding.CachePlan(*(torch.zeros(k, dtype=torch.int32, device=DEV) for k in (n, n + 1)), None,
+                                torch.zeros((5, 4), dtype=torch.int32, device=DEV), torch.zeros(2, dtype=torch.int32, device=DEV))
+        ws = binding.workspace(lib.fikit_cache_plan_workspace_bytes(n), DEV)
+        cached, d_added, free = i32([0] * n), i32(added), i32([1] * 50)
+        assert lib.fikit_cache_plan(cached.data_ptr(), d_added.data_ptr(), n, 5, 16, table.data_ptr(), 2 ** 27, free.data_ptr(), 50,
+                                    out.lengths.data_ptr(), out.token_offsets.data_ptr(), None, out.pieces.data_ptr(), out.counts.data_ptr(),
+                                    word.data_ptr(), ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream) == 0
+        assert int(word) == binding.FIKIT_INVALID_ARG and (table == 9).all()
+
+
 @pytest.mark.parametrize("cached, added, total, width, free, status", [
     ([3, 4], [1, 1], 3, 4, 8, binding.FIKIT_INVALID_ARG),          # tokens do not add up
     ([3, -1], [1, 1], 2, 4, 8, binding.FIKIT_INVALID_ARG),
@@ -128,6 +147,6 @@ def test_replays_of_a_graph():
         binding.fikit_check_status(word)
 
 
-@pytest.mark.parametrize("n", [4095, 4096, 4097, 8200])
+@pytest.mark.parametrize("n", [1023, 1025, 4095, 4096, 4097, 8200, 16383, 16384, 16385, 33000])
 def test_on_both_sides_of_one_launch(n):
     check(*case(n, n, 50, lambda r: r.integers(0, 4) if r.random() < 0.9 else r.integers(0, 60), 16), 16)
