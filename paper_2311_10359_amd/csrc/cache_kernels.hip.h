@@ -125,7 +125,8 @@ constexpr uint32_t PLAN_ONE_REQUESTS = 16 * PLAN_THREADS;
 template <uint32_t PER>
 __global__ __launch_bounds__(PLAN_THREADS) void k_plan_one(PlanArgs a) {
   constexpr bool ALL = PER <= 4;
-  __shared__ int32_t offsets[PER * PLAN_THREADS];
+  constexpr uint32_t GAP = ALL ? 0 : 1;       // (a word behind every run, so that threads write to different banks)
+  __shared__ int32_t offsets[(PER + GAP) * PLAN_THREADS];
   __shared__ uint2 bases[(ALL ? PER : 1) * PLAN_THREADS];
   __shared__ PlanScan scan;
   const bool stop = stopped(a.status);
@@ -148,13 +149,14 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_plan_one(PlanArgs a) {
 #pragma unroll
   for (uint32_t i = 0; i < PER; ++i) {
     const uint32_t r = first + i;
-    offsets[r] = static_cast<int32_t>(at.tokens);
+    offsets[r + GAP * threadIdx.x] = static_cast<int32_t>(at.tokens);
     if (ALL) bases[r] = make_uint2(at.blocks, at.pieces);
     if (writes && r < a.n_requests) {
       a.lengths[r] = cached[i] + added[i];
       a.token_offsets[r] = static_cast<int32_t>(at.tokens);
     }
-    plan_request(a, cached[i], added[i], &at);
+    if (ALL) plan_request(a, cached[i], added[i], &at);
+    else at.tokens += static_cast<uint32_t>(added[i]);
   }
   if (writes && threadIdx.x == 0) {
     a.token_offsets[a.n_requests] = static_cast<int32_t>(a.n_tokens);
@@ -164,12 +166,31 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_plan_one(PlanArgs a) {
   __syncthreads();
   const uint32_t from = blockIdx.x * PLAN_THREADS + threadIdx.x, stride = gridDim.x * PLAN_THREADS;
   for (uint64_t t = from; t < a.n_tokens; t += stride) {
-    const uint32_t r = plan_find(offsets, 0, a.n_requests, static_cast<uint32_t>(t));
-    const uint2 base = bases[ALL ? r : r / PER];
-    PlanSums s{0, base.x, base.y};
-    if (!ALL)
-      for (uint32_t j = r / PER * PER; j < r; ++j) plan_request(a, a.cached[j], a.added[j], &s);
-    plan_token(a, static_cast<uint32_t>(t), r, static_cast<uint32_t>(offsets[r]), s.blocks, s.pieces);
+    const uint32_t token = static_cast<uint32_t>(t);
+    if constexpr (ALL) {
+      const uint32_t r = plan_find(offsets, 0, a.n_requests, token);
+      plan_token(a, token, r, static_cast<uint32_t>(offsets[r]), bases[r].x, bases[r].y);
+    } else {
+      // the run, then the request in it
+      uint32_t run = 0;
+      for (uint32_t hi = (a.n_requests + PER - 1) / PER; hi - run > 1;) {
+        const uint32_t mid = run + (hi - run) / 2;
+        if (static_cast<uint32_t>(offsets[mid * (PER + GAP)]) <= token) run = mid; else hi = mid;
+      }
+      plan_read<PER>(a.cached, run * PER, a.n_requests, cached);
+      plan_read<PER>(a.added, run * PER, a.n_requests, added);
+      PlanSums s{static_cast<uint32_t>(offsets[run * (PER + GAP)]), bases[run].x, bases[run].y};
+      uint32_t r = run * PER;
+#pragma unroll
+      for (uint32_t i = 0; i + 1 < PER; ++i) {        // past the requests that end at the token or before
+        const bool past = r == run * PER + i && r + 1 < a.n_requests && s.tokens + static_cast<uint32_t>(added[i]) <= token;
+        if (past) {
+          plan_request(a, cached[i], added[i], &s);
+          ++r;
+        }
+      }
+      plan_token(a, token, r, s.tokens, s.blocks, s.pieces);
+    }
   }
   for (uint64_t i = static_cast<uint64_t>(total.pieces) + from; i < a.room; i += stride) a.pieces[i] = make_int4(-1, -1, -1, -1);
 }

@@ -32,9 +32,9 @@ constexpr float PROMPT_SLACK = 8.f;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) char lds_char;
 
-// 16 bytes per lane, to `to` and behind it in the order of the lanes.
-__device__ __forceinline__ void load_to_lds(const char* from, lds_char* to) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+// 16 bytes per lane, to `to` and behind it in the order of the lanes; zeros for what lies behind the end of `from`.
+__device__ __forceinline__ void load_to_lds(bounded from, uint32_t at, lds_char* to) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, static_cast<int>(at), 0, 0, 0);
 }
 __device__ __forceinline__ u32x4 read_row(const lds_char* at) { return *(const __attribute__((address_space(3))) u32x4*)at; }
 // Of 16 lanes each that point at four rows of 16 values, lane l receives value l of the four rows.
@@ -94,7 +94,14 @@ struct PromptWave {              // what a wave holds of its 32 rows; a lane of 
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
   }
-  __device__ __forceinline__ void scores(const lds_char* keys) {
+  __device__ __forceinline__ u32x4 key(const lds_char* keys, int j, int t) const { return read_row(keys + (key_at ^ j * 32) + t * 32 * ROW); }
+  // The first operands of a tile's scores, read before what stands between them and the products.
+  u32x4 first_keys[4];
+  __device__ __forceinline__ void read_ahead(const lds_char* keys) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) first_keys[i] = key(keys, i / 2, i % 2);
+  }
+  __device__ __forceinline__ void scores(const lds_char* keys, bool ahead) {
 #pragma unroll
     for (int j = 0; j < D / 16; ++j)
 #pragma unroll
@@ -102,7 +109,7 @@ struct PromptWave {              // what a wave holds of its 32 rows; a lane of 
         if (j == 0)
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[t][r] = 0.f;
-        s[t] = T::mfma32(bits_as<typename T::x8>(read_row(keys + (key_at ^ j * 32) + t * 32 * ROW)), q[j], s[t]);
+        s[t] = T::mfma32(bits_as<typename T::x8>(ahead && j < 2 ? first_keys[2 * j + t] : key(keys, j, t)), q[j], s[t]);
       }
   }
   __device__ __forceinline__ void mask(uint32_t token0) {
@@ -210,12 +217,13 @@ struct PromptWave {              // what a wave holds of its 32 rows; a lane of 
     __builtin_amdgcn_sched_barrier(0);
     typename T::x8 weights[4];
     weigh(weights);
-    scores(next_keys);
+    scores(next_keys, true);
     sum(vals, weights);
     find_most();
     asm volatile("" : "+v"(l), "+v"(most));      // (made here and not where they are next needed)
     constexpr int MFMA = 0x8, READ = 0x100, OTHER = 0x2, HALF = D / 16;
-    __builtin_amdgcn_sched_group_barrier(READ, 4, 0);
+    __builtin_amdgcn_sched_group_barrier(READ, 2, 0);
+    __builtin_amdgcn_sched_group_barrier(OTHER, 8, 0);
 #pragma unroll
     for (int i = 0; i < 2 * HALF - 4; ++i) {
       __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);
@@ -328,19 +336,13 @@ struct PromptFill {
       off[i] = r * static_cast<uint32_t>(stride) + (piece ^ (values ? value_swizzle<D>(r) : key_swizzle<D>(r))) * 16;
     }
   }
+  // (rows behind the prompt's end become zeros)
   __device__ __forceinline__ void load(uint32_t tile, uint32_t length, lds_char* to) const {
-    const char* at = from + tile * (PROMPT_KEYS * stride);
-    to += wave * WAVE * 16;
-    if ((tile + 1) * PROMPT_KEYS <= length) {
+    const uint32_t rows = min_u32(length - tile * PROMPT_KEYS, PROMPT_KEYS);
+    const bounded at = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from + tile * (PROMPT_KEYS * stride)), 0,
+                                                         static_cast<int>((rows - 1) * static_cast<uint32_t>(stride) + ROW), 0x00027000);
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) load_to_lds(at + off[i], to + i * WAVES * WAVE * 16);
-    } else {                     // rows behind the prompt's end: its last token's, which are masked
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const uint32_t r = ((i * WAVES + wave) * WAVE + lane_id()) / PIECES, last = length - 1 - tile * PROMPT_KEYS, back = r > last ? r - last : 0;
-        load_to_lds(at + (off[i] - back * static_cast<uint32_t>(stride)), to + i * WAVES * WAVE * 16);
-      }
-    }
+    for (int i = 0; i < LOADS; ++i) load_to_lds(at, off[i], to + (i * WAVES + wave) * WAVE * 16);
   }
 };
 
@@ -371,7 +373,7 @@ __device__ __attribute__((noinline)) void prompt_with_care(PromptArgs a, uint32_
     const uint32_t token0 = tile * PROMPT_KEYS;
     if (token0 > row0 + PROMPT_WAVE_ROWS - 1) continue;
     typename T::x8 weights[4];
-    w.scores(keys);
+    w.scores(keys, false);
     w.mask(token0);
     w.find_most();
     w.raise();
@@ -422,15 +424,17 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs a) {
   const uint32_t full = first / PROMPT_KEYS;      // tiles that all rows of the workgroup see whole, an even number
   w.start();
   prompt_arrive();
-  w.scores(k0);
+  w.scores(k0, false);
   w.find_most();
   for (uint32_t tile = 0; tile < full; tile += 2) {
     prompt_arrive();
+    w.read_ahead(k1);
     k.load(tile + 2, length, k0);
     v.load(tile + 1, length, v1);
     w.raise();
     w.weigh_and_go_on(k1, v0);
     prompt_arrive();
+    w.read_ahead(k0);
     if (tile + 3 < tiles) k.load(tile + 3, length, k1);
     v.load(tile + 2, length, v0);
     w.raise();
@@ -448,7 +452,7 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs a) {
   }
   if (full + 1 < tiles) {
     if (row0 >= (full + 1) * PROMPT_KEYS) {
-      w.scores(k1);
+      w.scores(k1, false);
       w.mask((full + 1) * PROMPT_KEYS);
       w.find_most();
       w.raise();
