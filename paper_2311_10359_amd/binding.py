@@ -573,7 +573,12 @@ def fikit_profile_merge(rows_a: torch.Tensor, task_row_offsets_a: torch.Tensor, 
 # ---- tasks of a language model service -----------------------------------------------------------
 # These calls enqueue their kernels and return; errors that depend on data are left in `status`, an int32 [1] device tensor
 # that starts as zero and that fikit_check_status looks at.  Tensors that a call allocates belong to the stream it runs on.
-_VALUE_TYPES = {torch.bfloat16: 0, torch.float16: 1}
+
+
+def _outputs(kind, got, what: str):
+    if type(got) is int:
+        raise FikitError(got, what)
+    return tuple.__new__(kind, got)
 
 
 def fikit_check_status(status: torch.Tensor, what: str = "a call on this status word") -> None:
@@ -595,37 +600,25 @@ def _elsewhere(stream: Optional[torch.cuda.Stream], device):
 
 
 # (torch.cuda.current_stream() makes an object around this handle, 1.8 us of a call that may take 5)
-def _current_handle(device) -> int:
-    return torch._C._cuda_getCurrentRawStream(device.index)
+_stream_of = torch._C._cuda_getCurrentRawStream
 
 
-def _vectors(t: torch.Tensor, what: str) -> _Vectors:
-    strides = t.stride()
-    if len(strides) != 3 or strides[2] != 1:
-        raise ValueError(f"{what}: [tokens, heads, head_dim] with the last dimension dense")
-    return _Vectors(t.data_ptr(), strides[0], strides[1])
+def _marshal():
+    """The compiled marshalling of these calls (csrc/serve_marshal.cpp), with the library's addresses."""
+    global _native
+    if _native is None:
+        lib = load()
+        if not os.path.exists(_build.MARSHAL):
+            _build.build_marshal()
+        from . import _serve_marshal
+        _serve_marshal.bind(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in (
+            "fikit_cache_pieces", "fikit_cache_plan_workspace_bytes", "fikit_cache_plan", "fikit_cache_append",
+            "fikit_cache_attention_workspace_bytes", "fikit_cache_attention", "fikit_prompt_attention")))
+        _native = _serve_marshal
+    return _native
 
 
-def _need(condition: bool, what: str) -> None:
-    if not condition:
-        raise ValueError(what)
-
-
-def _dense(t: torch.Tensor, dtype: torch.dtype, device, what: str) -> int:
-    if t.dtype is not dtype or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{what}: a dense {dtype} tensor on {device}")
-    return t.data_ptr()
-
-
-def _cache_of(k_cache, v_cache, k_exp, v_exp, device) -> _Cache:
-    """k_cache, v_cache: [blocks, kv heads, block tokens, head dim] codes (float8_e4m3fn or their bytes)."""
-    _need(k_cache.dim() == 4 and v_cache.shape == k_cache.shape, "k_cache, v_cache: [blocks, kv heads, block tokens, head dim]")
-    n, h, b, d = k_cache.shape
-    _need(k_exp.shape == (n, h) and v_exp.shape == (n, h), "k_exp, v_exp: [blocks, kv heads]")
-    codes = k_cache.dtype
-    _need(codes is torch.float8_e4m3fn or codes is torch.uint8, "k_cache, v_cache: float8_e4m3fn or uint8")
-    return _Cache(_dense(k_cache, codes, device, "k_cache"), _dense(v_cache, codes, device, "v_cache"), _dense(k_exp, torch.uint8, device, "k_exp"),
-                  _dense(v_exp, torch.uint8, device, "v_exp"), n, h, b, d)
+_native = None
 
 
 class CachePlan(NamedTuple):
@@ -645,37 +638,14 @@ def fikit_cache_plan(cached: torch.Tensor, added: torch.Tensor, n_tokens: int, b
                      workspace_buf: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> CachePlan:
     """cached, added: int32 [R]; n_tokens = sum of added; block_table: int32 [R, width], receives the new blocks;
     free_blocks: int32 [F].  Output tensors are allocated unless given."""
-    lib, dev, n = load(), cached.device, cached.numel()
-    _need(added.numel() == n and block_table.dim() == 2 and block_table.shape[0] == n, "cached, added: [R]; block_table: [R, width]")
-    context = _elsewhere(stream, dev)
+    context = _elsewhere(stream, cached.device)
     if context is not None:
         with context:
             return fikit_cache_plan(cached, added, n_tokens, block_tokens, block_table, free_blocks, status, want_slots=want_slots,
                                     out=out, workspace_buf=workspace_buf)
-    i32 = torch.int32
-    room = lib.fikit_cache_pieces(n_tokens, n, block_tokens)
-    if out is None:
-        out = CachePlan(cached.new_empty(n), cached.new_empty(n + 1),
-                        torch.empty(n_tokens, dtype=torch.int64, device=dev) if want_slots else None,
-                        cached.new_empty((room, 4)), cached.new_empty(2))
-    else:
-        _need(out.lengths.numel() == n and out.token_offsets.numel() == n + 1 and out.counts.numel() == 2 and
-              out.pieces.numel() == 4 * room and (out.slots is None or out.slots.numel() == n_tokens), "out: tensors of these sizes")
-    if workspace_buf is None:
-        size = lib.fikit_cache_plan_workspace_bytes(n)
-        if size:
-            workspace_buf = workspace(size, dev)
-    st = lib.fikit_cache_plan(_dense(cached, i32, dev, "cached"), _dense(added, i32, dev, "added"), n, n_tokens, block_tokens,
-                              _dense(block_table, i32, dev, "block_table"), block_table.shape[1],
-                              _dense(free_blocks, i32, dev, "free_blocks"), free_blocks.numel(),
-                              _dense(out.lengths, i32, dev, "lengths"), _dense(out.token_offsets, i32, dev, "token_offsets"),
-                              None if out.slots is None else _dense(out.slots, torch.int64, dev, "slots"),
-                              _dense(out.pieces, i32, dev, "pieces"), _dense(out.counts, i32, dev, "counts"),
-                              _dense(status, i32, dev, "status"), None if workspace_buf is None else workspace_buf.data_ptr(),
-                              0 if workspace_buf is None else workspace_buf.numel(), _current_handle(dev))
-    if st != FIKIT_OK:
-        raise FikitError(st, "fikit_cache_plan")
-    return out
+    got = (_native or _marshal()).cache_plan(cached, added, n_tokens, block_tokens, block_table, free_blocks, status, want_slots, out,
+                                             workspace_buf, _stream_of(cached.device.index))
+    return _outputs(CachePlan, got, "fikit_cache_plan")
 
 
 def fikit_cache_append(k_cache: torch.Tensor, v_cache: torch.Tensor, k_exp: torch.Tensor, v_exp: torch.Tensor, k: torch.Tensor,
@@ -683,18 +653,11 @@ def fikit_cache_append(k_cache: torch.Tensor, v_cache: torch.Tensor, k_exp: torc
                        stream: Optional[torch.cuda.Stream] = None) -> None:
     """k, v: bfloat16 or float16 [n_tokens, kv heads, head_dim], of any token and head strides that are multiples of 8;
     pieces: as fikit_cache_plan leaves them.  The cache is written in place."""
-    lib, dev = load(), k.device
-    cache = _cache_of(k_cache, v_cache, k_exp, v_exp, dev)
-    _need(k.dtype in _VALUE_TYPES and v.dtype == k.dtype and v.device == dev, "k, v: bfloat16 or float16, both the same")
-    _need(k.shape == v.shape and k.shape[1:] == (cache.kv_heads, cache.head_dim), "k, v: [n_tokens, kv heads, head_dim] of the cache")
-    _need(pieces.dim() == 2 and pieces.shape[1] == 4, "pieces: [n, 4]")
-    vectors = _vectors(k, "k"), _vectors(v, "v")
-    context = _elsewhere(stream, dev)
+    context = _elsewhere(stream, k.device)
     if context is not None:
         with context:
             return fikit_cache_append(k_cache, v_cache, k_exp, v_exp, k, v, pieces, status)
-    st = lib.fikit_cache_append(cache, *vectors, k.shape[0], _VALUE_TYPES[k.dtype], _dense(pieces, torch.int32, dev, "pieces"),
-                                pieces.shape[0], _dense(status, torch.int32, dev, "status"), _current_handle(dev))
+    st = (_native or _marshal()).cache_append(k_cache, v_cache, k_exp, v_exp, k, v, pieces, status, _stream_of(k.device.index))
     if st != FIKIT_OK:
         raise FikitError(st, "fikit_cache_append")
 
@@ -702,16 +665,6 @@ def fikit_cache_append(k_cache: torch.Tensor, v_cache: torch.Tensor, k_exp: torc
 class Attention(NamedTuple):
     out: torch.Tensor               # [rows, q heads, head_dim], the queries' type
     lse: Optional[torch.Tensor]     # float32 [rows, q heads]: log of the sum of the exponentials of the scores
-
-
-def _attention_out(q, want_lse, out):
-    rows, heads, _ = q.shape
-    if out is None:
-        out = Attention(torch.empty(q.shape, dtype=q.dtype, device=q.device),
-                        torch.empty((rows, heads), dtype=torch.float32, device=q.device) if want_lse else None)
-    _need(out.out.shape == q.shape, "out: the shape of q")
-    _need(out.lse is None or out.lse.shape == (rows, heads), "lse: [rows, q heads]")
-    return out, _dense(out.out, q.dtype, q.device, "out"), None if out.lse is None else _dense(out.lse, torch.float32, q.device, "lse")
 
 
 def fikit_cache_attention_workspace_bytes(n_requests: int, q_heads: int, kv_heads: int, head_dim: int, max_length: int) -> int:
@@ -724,31 +677,14 @@ def fikit_cache_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch
                           workspace_buf: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> Attention:
     """q: [R, q heads, head_dim], one query per request; block_table: int32 [R, width]; lengths: int32 [R], none above
     max_length (the table's width if not given)."""
-    lib, dev = load(), q.device
-    cache = _cache_of(k_cache, v_cache, k_exp, v_exp, dev)
-    _need(q.dtype in _VALUE_TYPES, "q: bfloat16 or float16")
-    vectors = _vectors(q, "q")
-    n, heads, d = q.shape
-    _need(d == cache.head_dim and block_table.dim() == 2 and block_table.shape[0] == n and lengths.numel() == n,
-          "q: [R, q heads, head_dim]; block_table: [R, width]; lengths: [R]")
-    if max_length is None:
-        max_length = block_table.shape[1] * cache.block_tokens
-    context = _elsewhere(stream, dev)
+    context = _elsewhere(stream, q.device)
     if context is not None:
         with context:
             return fikit_cache_attention(q, k_cache, v_cache, k_exp, v_exp, block_table, lengths, scale, status, max_length=max_length,
                                          want_lse=want_lse, out=out, workspace_buf=workspace_buf)
-    out, p_out, p_lse = _attention_out(q, want_lse, out)
-    if workspace_buf is None:
-        workspace_buf = workspace(lib.fikit_cache_attention_workspace_bytes(n, heads, cache.kv_heads, d, max_length), dev)
-    st = lib.fikit_cache_attention(cache, vectors, heads, _VALUE_TYPES[q.dtype], scale,
-                                   _dense(block_table, torch.int32, dev, "block_table"), block_table.shape[1],
-                                   _dense(lengths, torch.int32, dev, "lengths"), n, max_length, p_out, p_lse,
-                                   _dense(status, torch.int32, dev, "status"), workspace_buf.data_ptr(), workspace_buf.numel(),
-                                   _current_handle(dev))
-    if st != FIKIT_OK:
-        raise FikitError(st, "fikit_cache_attention")
-    return out
+    got = (_native or _marshal()).cache_attention(k_cache, v_cache, k_exp, v_exp, q, block_table, lengths, scale, status, max_length,
+                                                  want_lse, out, workspace_buf, _stream_of(q.device.index))
+    return _outputs(Attention, got, "fikit_cache_attention")
 
 
 def fikit_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor, scale: float,
@@ -756,23 +692,12 @@ def fikit_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, of
                            stream: Optional[torch.cuda.Stream] = None) -> Attention:
     """q: [n_tokens, q heads, head_dim], k, v: [n_tokens, kv heads, head_dim], of any token and head strides that are multiples
     of 8 (parts of one product's output, say); offsets: int32 [prompts + 1]."""
-    lib, dev = load(), q.device
-    _need(q.dtype in _VALUE_TYPES and k.dtype == q.dtype and v.dtype == q.dtype and k.device == dev and v.device == dev,
-          "q, k, v: bfloat16 or float16, all the same")
-    vectors = _vectors(q, "q"), _vectors(k, "k"), _vectors(v, "v")
-    n, heads, d = q.shape
-    _need(k.shape == v.shape and k.shape[0] == n and k.shape[2] == d, "k, v: [n_tokens, kv heads, head_dim]")
-    context = _elsewhere(stream, dev)
+    context = _elsewhere(stream, q.device)
     if context is not None:
         with context:
             return fikit_prompt_attention(q, k, v, offsets, scale, status, want_lse=want_lse, out=out)
-    out, p_out, p_lse = _attention_out(q, want_lse, out)
-    st = lib.fikit_prompt_attention(*vectors, heads, k.shape[1], d, _VALUE_TYPES[q.dtype], scale,
-                                    _dense(offsets, torch.int32, dev, "offsets"), offsets.numel() - 1, n, p_out, p_lse,
-                                    _dense(status, torch.int32, dev, "status"), _current_handle(dev))
-    if st != FIKIT_OK:
-        raise FikitError(st, "fikit_prompt_attention")
-    return out
+    got = (_native or _marshal()).prompt_attention(q, k, v, offsets, scale, status, want_lse, out, _stream_of(q.device.index))
+    return _outputs(Attention, got, "fikit_prompt_attention")
 
 
 # ---- helpers to move host arrays in and out (marshalling only) ---------------------------------

@@ -8,6 +8,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libfikit.so")
+MARSHAL = os.path.join(_HERE, "_serve_marshal.so")       # compiled marshalling of the attention calls for Python
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -56,5 +57,26 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
+def build_marshal(force: bool = False, verbose: bool = False) -> str:
+    """Host code only, against torch's headers."""
+    source = os.path.join(CSRC, "serve_marshal.cpp")
+    if not force and os.path.exists(MARSHAL) and all(
+            os.path.getmtime(f) <= os.path.getmtime(MARSHAL) for f in (source, os.path.join(ROOT, "include", "fikit.h"))):
+        return MARSHAL
+    import sysconfig
+    import torch
+    at = os.path.dirname(torch.__file__)
+    tmp = MARSHAL + f".tmp{os.getpid()}"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+           "-I", os.path.join(ROOT, "include"), "-I", os.path.join(at, "include"),
+           "-I", os.path.join(at, "include", "torch", "csrc", "api", "include"), "-I", sysconfig.get_paths()["include"],
+           "-o", tmp, source, "-L", os.path.join(at, "lib"), "-lc10", "-ltorch_cpu", "-ltorch_python"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.check_call(cmd)
+    os.replace(tmp, MARSHAL)
+    return MARSHAL
+
+
 if __name__ == "__main__":
-    print(build_library(force=True, verbose=True))
+    print(build_library(force=True, verbose=True), build_marshal(force=True, verbose=True))
