@@ -483,6 +483,7 @@ size_t fikit_cache_plan_workspace_bytes(uint32_t n_requests);
  * The plan of a step.  Request r has d_cached[r] tokens in the cache and gets d_added[r] more (either may be 0); its new tokens
  * follow those of request r - 1 in the packed inputs.
  *
+ *   n_requests       up to 2^20.
  *   n_tokens         sum of d_added (a mismatch is INVALID_ARG), < 2^31.
  *   d_block_table    [n_requests][table_width] in and out: the blocks of a request in order.  The first ceil(cached /
  *                    block_tokens) entries of a row are read where new tokens go into the last of them; the entries behind

@@ -588,13 +588,16 @@ def fikit_check_status(status: torch.Tensor, what: str = "a call on this status 
         raise FikitError(st, what)
 
 
+_current_device = torch._C._cuda_getDevice
+
+
 def _elsewhere(stream: Optional[torch.cuda.Stream], device):
     """None if a call runs on the current stream of the current device, else the context to run it in."""
     if device.type != "cuda":
         raise ValueError("tensors on a GPU")
     if stream is not None:
         return torch.cuda.stream(stream)
-    if device.index != torch.cuda.current_device():
+    if device.index != _current_device():
         return torch.cuda.device(device)
     return None
 
@@ -622,6 +625,7 @@ _native = None
 
 
 class CachePlan(NamedTuple):
+    """Allocated by a call, these are parts of one piece of memory."""
     lengths: torch.Tensor           # int32 [R]
     token_offsets: torch.Tensor     # int32 [R + 1]
     slots: Optional[torch.Tensor]   # int64 [n_tokens]

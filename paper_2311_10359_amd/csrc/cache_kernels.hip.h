@@ -8,10 +8,17 @@ namespace fikit {
 // ---- plan -------------------------------------------------------------------------------------------------------
 //
 // With B = tokens per block, c cached and a added tokens of a request: it holds ceil(c / B) blocks, needs ceil((c + a) / B), and
-// its new tokens are cut into floor((c + a - 1) / B) - floor(c / B) + 1 pieces (none if a = 0).  Three prefix sums over the
-// requests (tokens, new blocks, pieces) say where everything of a request begins; then each new token finds its request by
-// a search in the token sums and writes its slot, and those that open a block or a piece write these, with no word from one to
-// another.
+// its new tokens are cut into ceil((c + a) / B) - floor(c / B) pieces (none if a = 0).  Three prefix sums over the requests (tokens,
+// new blocks, pieces) say where everything of a request begins; then each new token finds its request by a search in the
+// token sums and writes its slot, and those that open a block or a piece write these, with no word from one to another.
+//
+// A few bytes per request and token: bound by the latency of one load behind the other, so launches and dependent loads are few.
+
+struct PlanTile {           // sums over 1024 requests
+  uint64_t tokens;          // PLAN_BAD: a length that cannot be
+  uint32_t blocks, pieces;
+};
+constexpr uint64_t PLAN_BAD = 1ull << 62;
 
 struct PlanArgs {
   const int32_t* cached;
@@ -24,34 +31,40 @@ struct PlanArgs {
   int4* pieces;
   int32_t* counts;
   int32_t* status;
-  uint2* bases;             // per request: new blocks and pieces of those before it
+  PlanTile* tiles;
   uint32_t n_requests, n_tokens, table_width, n_free, room;
   uint32_t shift;           // of the block length
 };
 
 constexpr int PLAN_THREADS = 1024;
 
-struct PlanSums {
-  uint32_t tokens, blocks, pieces;
+// What a request of c cached and a added tokens adds to the sums; false if these cannot be.
+struct PlanRequest {
+  uint32_t cached, length, blocks, pieces;
+  bool ok;
+  __device__ __forceinline__ PlanRequest(const PlanArgs& a, int32_t c, int32_t d) {
+    const uint32_t last = (1u << a.shift) - 1;
+    cached = static_cast<uint32_t>(c);
+    length = cached + static_cast<uint32_t>(d);
+    const uint32_t needs = static_cast<uint32_t>((static_cast<uint64_t>(length) + last) >> a.shift);
+    blocks = needs - ((cached + last) >> a.shift);
+    pieces = d > 0 ? needs - (cached >> a.shift) : 0;
+    ok = c >= 0 && d >= 0 && length <= INT32_MAX && needs <= a.table_width;
+  }
+  __device__ __forceinline__ uint32_t added() const { return length - cached; }
 };
 
-// What a request of c cached and a added tokens adds to the sums; false if these cannot be, or a sum does not fit.  (Blocks and
-// pieces are at most as many as tokens.)
-__device__ __forceinline__ bool plan_request(const PlanArgs& a, int32_t c, int32_t d, PlanSums* s) {
-  const uint32_t cached = static_cast<uint32_t>(c), added = static_cast<uint32_t>(d), length = cached + added, last = (1u << a.shift) - 1;
-  const bool ok = c >= 0 && d >= 0 && length <= INT32_MAX && ((static_cast<uint64_t>(length) + last) >> a.shift) <= a.table_width;
-  s->blocks += ((length + last) >> a.shift) - ((cached + last) >> a.shift);
-  s->pieces += d > 0 ? ((length - 1) >> a.shift) - (cached >> a.shift) + 1 : 0;
-  s->tokens += added;
-  return ok && s->tokens >= added;
-}
+struct PlanSums {
+  uint64_t tokens;
+  uint32_t blocks, pieces;
+};
 
 struct PlanScan {
   uint32_t blocks[PLAN_THREADS / WAVE], pieces[PLAN_THREADS / WAVE];
   uint64_t tokens[PLAN_THREADS / WAVE];
 };
 
-// The sums of the threads before, and of all of them, in a workgroup of PLAN_THREADS; whether `ok` holds in all and all sums fit.
+// The sums of the threads before, and of all of them, in a workgroup of PLAN_THREADS; whether `ok` holds in all.
 __device__ __forceinline__ bool plan_scan(const PlanSums& mine, bool ok, PlanScan* lds, PlanSums* before, PlanSums* total) {
   constexpr uint32_t WAVES = PLAN_THREADS / WAVE;
   const uint64_t run_tokens = wave_incl_scan_u64(mine.tokens);
@@ -65,202 +78,156 @@ __device__ __forceinline__ bool plan_scan(const PlanSums& mine, bool ok, PlanSca
   const uint32_t blocks = there ? lds->blocks[lane % WAVES] : 0, pieces = there ? lds->pieces[lane % WAVES] : 0;
   const uint64_t upto = wave_incl_scan_u64(tokens);
   const uint32_t upto_blocks = wave_incl_scan_u32(blocks), upto_pieces = wave_incl_scan_u32(pieces);
-  *total = PlanSums{read_lane_u32(static_cast<uint32_t>(upto), WAVES - 1), read_lane_u32(upto_blocks, WAVES - 1), read_lane_u32(upto_pieces, WAVES - 1)};
-  *before = PlanSums{read_lane_u32(static_cast<uint32_t>(upto - tokens), wave) + static_cast<uint32_t>(run_tokens) - mine.tokens,
-                     read_lane_u32(upto_blocks - blocks, wave) + run_blocks - mine.blocks,
+  *total = PlanSums{read_lane_u64(upto, WAVES - 1), read_lane_u32(upto_blocks, WAVES - 1), read_lane_u32(upto_pieces, WAVES - 1)};
+  *before = PlanSums{read_lane_u64(upto - tokens, wave) + run_tokens - mine.tokens, read_lane_u32(upto_blocks - blocks, wave) + run_blocks - mine.blocks,
                      read_lane_u32(upto_pieces - pieces, wave) + run_pieces - mine.pieces};
-  return all && read_lane_u64(upto, WAVES - 1) <= INT32_MAX;
+  return all;
 }
 
+// (blocks and pieces are at most as many as tokens)
 __device__ __forceinline__ int32_t plan_error(const PlanArgs& a, const PlanSums& total, bool ok) {
   return !ok || total.tokens != a.n_tokens ? FIKIT_INVALID_ARG : total.blocks > a.n_free ? FIKIT_CACHE_FULL : FIKIT_OK;
 }
 
-// The last of the requests lo .. hi - 1 that begins at token t or before; lo begins so.
-__device__ __forceinline__ uint32_t plan_find(const int32_t* offsets, uint32_t lo, uint32_t hi, uint32_t t) {
+__device__ __forceinline__ void plan_counts(const PlanArgs& a, const PlanSums& total) {
+  a.token_offsets[a.n_requests] = static_cast<int32_t>(a.n_tokens);
+  a.counts[0] = static_cast<int32_t>(total.blocks);
+  a.counts[1] = static_cast<int32_t>(total.pieces);
+}
+
+// The last of the entries lo .. hi - 1 that is t or less; the first one is.
+__device__ __forceinline__ uint32_t plan_find(const uint32_t* from, uint32_t lo, uint32_t hi, uint32_t t) {
   while (hi - lo > 1) {
     const uint32_t mid = lo + (hi - lo) / 2;
-    if (static_cast<uint32_t>(offsets[mid]) <= t) lo = mid; else hi = mid;
+    if (from[mid] <= t) lo = mid; else hi = mid;
   }
   return lo;
 }
 
-// What new token t, of request r that begins at token `first`, writes; `blocks`, `pieces`: those of the requests before.
-__device__ __forceinline__ void plan_token(const PlanArgs& a, uint32_t t, uint32_t r, uint32_t first, uint32_t blocks, uint32_t pieces) {
-  const uint32_t block_tokens = 1u << a.shift;
-  const uint32_t cached = static_cast<uint32_t>(a.cached[r]), length = cached + static_cast<uint32_t>(a.added[r]);
-  const uint32_t index = t - first;
+// 1024 requests of a workgroup, one per thread, in LDS.
+struct PlanRequests {
+  uint32_t first[PLAN_THREADS];           // token at which a request begins
+  uint4 rest[PLAN_THREADS];               // cached, length, blocks and pieces of the requests before
+};
+
+// What new token t writes, whose request is one of n that begin with request r0.
+__device__ __forceinline__ void plan_token(const PlanArgs& a, const PlanRequests& lds, uint32_t r0, uint32_t n, uint32_t t) {
+  const uint32_t i = plan_find(lds.first, 0, n, t), block_tokens = 1u << a.shift;
+  const uint4 rest = lds.rest[i];
+  const uint32_t cached = rest.x, length = rest.y, index = t - lds.first[i];
   const uint32_t place = cached + index, page = place >> a.shift, at = place & (block_tokens - 1);
   const uint32_t held = (cached + block_tokens - 1) >> a.shift;
-  int32_t* entry = a.table + static_cast<uint64_t>(r) * a.table_width + page;
-  const int32_t block = page >= held ? a.free_blocks[blocks + (page - held)] : *entry;
+  int32_t* entry = a.table + static_cast<uint64_t>(r0 + i) * a.table_width + page;
+  const int32_t block = page >= held ? a.free_blocks[rest.z + (page - held)] : *entry;
   if (at == 0) *entry = block;      // (a block that begins at a new token is a new one)
   if (a.slots) a.slots[t] = static_cast<int64_t>(block) * block_tokens + at;
   if (at == 0 || index == 0)
-    a.pieces[pieces + (page - (cached >> a.shift))] = make_int4(block, static_cast<int32_t>(t), static_cast<int32_t>(at),
+    a.pieces[rest.w + (page - (cached >> a.shift))] = make_int4(block, static_cast<int32_t>(t), static_cast<int32_t>(at),
                                                                static_cast<int32_t>(min_u32(block_tokens - at, length - place)));
 }
 
-// Eight or sixteen consecutive requests are read as vectors of words; the arrays need no more alignment than that.
-typedef int32_t i32x4_by_words __attribute__((ext_vector_type(4), aligned(4)));
-template <uint32_t PER>
-__device__ __forceinline__ void plan_read(const int32_t* from, uint64_t first, uint32_t n, int32_t (&to)[PER]) {
-  if (PER % 4 == 0 && first + PER <= n) {
-#pragma unroll
-    for (uint32_t i = 0; i < PER; i += 4) {
-      const i32x4_by_words x = *reinterpret_cast<const i32x4_by_words*>(from + first + i);
-#pragma unroll
-      for (uint32_t j = 0; j < 4; ++j) to[i + j] = x[j];
-    }
-  } else {
-#pragma unroll
-    for (uint32_t i = 0; i < PER; ++i) to[i] = first + i < n ? from[first + i] : 0;
-  }
+__device__ __forceinline__ void plan_rest(const PlanArgs& a, uint32_t pieces, uint32_t from, uint32_t stride) {
+  for (uint64_t i = static_cast<uint64_t>(pieces) + from; i < a.room; i += stride) a.pieces[i] = make_int4(-1, -1, -1, -1);
 }
 
-// The whole plan in one launch: every workgroup sums all requests for itself, a run of PER consecutive ones per thread, and takes
-// 1024 tokens at a time.  Where each request begins is kept in LDS; its blocks and pieces too for runs of up to four, else they
-// are added up again from where its run begins.
-constexpr uint32_t PLAN_ONE_REQUESTS = 16 * PLAN_THREADS;
-template <uint32_t PER>
+// Up to 1024 requests: one launch, in which every workgroup sums all of them for itself and takes 1024 tokens at a time.
 __global__ __launch_bounds__(PLAN_THREADS) void k_plan_one(PlanArgs a) {
-  constexpr bool ALL = PER <= 4;
-  constexpr uint32_t GAP = ALL ? 0 : 1;       // (a word behind every run, so that threads write to different banks)
-  __shared__ int32_t offsets[(PER + GAP) * PLAN_THREADS];
-  __shared__ uint2 bases[(ALL ? PER : 1) * PLAN_THREADS];
+  __shared__ PlanRequests requests;
   __shared__ PlanScan scan;
-  const bool stop = stopped(a.status);
-  const uint32_t first = threadIdx.x * PER;
-  int32_t cached[PER], added[PER];
-  plan_read<PER>(a.cached, first, a.n_requests, cached);
-  plan_read<PER>(a.added, first, a.n_requests, added);
+  const bool stop = stopped(a.status), there = threadIdx.x < a.n_requests;
+  const PlanRequest mine(a, there ? a.cached[threadIdx.x] : 0, there ? a.added[threadIdx.x] : 0);
   if (stop) return;
-  PlanSums mine{0, 0, 0}, at, total;
-  bool ok = true;
-#pragma unroll
-  for (uint32_t i = 0; i < PER; ++i) ok &= plan_request(a, cached[i], added[i], &mine);
-  ok = plan_scan(mine, ok, &scan, &at, &total);
+  PlanSums at, total;
+  const bool ok = plan_scan(PlanSums{mine.added(), mine.blocks, mine.pieces}, mine.ok, &scan, &at, &total);
   if (const int32_t error = plan_error(a, total, ok)) {
     if (threadIdx.x == 0) *a.status = error;
     return;
   }
-  const bool writes = blockIdx.x == 0;
-  if (!ALL) bases[threadIdx.x] = make_uint2(at.blocks, at.pieces);
-#pragma unroll
-  for (uint32_t i = 0; i < PER; ++i) {
-    const uint32_t r = first + i;
-    offsets[r + GAP * threadIdx.x] = static_cast<int32_t>(at.tokens);
-    if (ALL) bases[r] = make_uint2(at.blocks, at.pieces);
-    if (writes && r < a.n_requests) {
-      a.lengths[r] = cached[i] + added[i];
-      a.token_offsets[r] = static_cast<int32_t>(at.tokens);
+  requests.first[threadIdx.x] = static_cast<uint32_t>(at.tokens);
+  requests.rest[threadIdx.x] = make_uint4(mine.cached, mine.length, at.blocks, at.pieces);
+  if (blockIdx.x == 0) {
+    if (there) {
+      a.lengths[threadIdx.x] = static_cast<int32_t>(mine.length);
+      a.token_offsets[threadIdx.x] = static_cast<int32_t>(at.tokens);
     }
-    if (ALL) plan_request(a, cached[i], added[i], &at);
-    else at.tokens += static_cast<uint32_t>(added[i]);
-  }
-  if (writes && threadIdx.x == 0) {
-    a.token_offsets[a.n_requests] = static_cast<int32_t>(a.n_tokens);
-    a.counts[0] = static_cast<int32_t>(total.blocks);
-    a.counts[1] = static_cast<int32_t>(total.pieces);
+    if (threadIdx.x == 0) plan_counts(a, total);
   }
   __syncthreads();
   const uint32_t from = blockIdx.x * PLAN_THREADS + threadIdx.x, stride = gridDim.x * PLAN_THREADS;
-  for (uint64_t t = from; t < a.n_tokens; t += stride) {
-    const uint32_t token = static_cast<uint32_t>(t);
-    if constexpr (ALL) {
-      const uint32_t r = plan_find(offsets, 0, a.n_requests, token);
-      plan_token(a, token, r, static_cast<uint32_t>(offsets[r]), bases[r].x, bases[r].y);
-    } else {
-      // the run, then the request in it
-      uint32_t run = 0;
-      for (uint32_t hi = (a.n_requests + PER - 1) / PER; hi - run > 1;) {
-        const uint32_t mid = run + (hi - run) / 2;
-        if (static_cast<uint32_t>(offsets[mid * (PER + GAP)]) <= token) run = mid; else hi = mid;
-      }
-      plan_read<PER>(a.cached, run * PER, a.n_requests, cached);
-      plan_read<PER>(a.added, run * PER, a.n_requests, added);
-      PlanSums s{static_cast<uint32_t>(offsets[run * (PER + GAP)]), bases[run].x, bases[run].y};
-      uint32_t r = run * PER;
-#pragma unroll
-      for (uint32_t i = 0; i + 1 < PER; ++i) {        // past the requests that end at the token or before
-        const bool past = r == run * PER + i && r + 1 < a.n_requests && s.tokens + static_cast<uint32_t>(added[i]) <= token;
-        if (past) {
-          plan_request(a, cached[i], added[i], &s);
-          ++r;
-        }
-      }
-      plan_token(a, token, r, s.tokens, s.blocks, s.pieces);
-    }
-  }
-  for (uint64_t i = static_cast<uint64_t>(total.pieces) + from; i < a.room; i += stride) a.pieces[i] = make_int4(-1, -1, -1, -1);
+  for (uint64_t t = from; t < a.n_tokens; t += stride) plan_token(a, requests, 0, a.n_requests, static_cast<uint32_t>(t));
+  plan_rest(a, total.pieces, from, stride);
 }
 
-// For more requests the sums are one workgroup's, 8 consecutive requests per thread and round, and the tokens a launch behind it.
-constexpr uint32_t PLAN_PER = 8;
-__global__ __launch_bounds__(PLAN_THREADS) void k_plan_sums(PlanArgs a) {
-  __shared__ PlanScan scan[2];
-  if (stopped(a.status)) return;
-  PlanSums carry{0, 0, 0};
-  bool ok = true;
-  uint32_t turn = 0;
-  for (uint64_t round = 0; round < a.n_requests; round += PLAN_THREADS * PLAN_PER, turn ^= 1) {
-    const uint64_t first = round + threadIdx.x * PLAN_PER;
-    const bool whole = first + PLAN_PER <= a.n_requests;
-    int32_t cached[PLAN_PER], added[PLAN_PER];
-    plan_read<PLAN_PER>(a.cached, first, a.n_requests, cached);
-    plan_read<PLAN_PER>(a.added, first, a.n_requests, added);
-    PlanSums mine{0, 0, 0}, at, total;
-#pragma unroll
-    for (uint32_t i = 0; i < PLAN_PER; ++i) ok &= plan_request(a, cached[i], added[i], &mine);
-    ok = plan_scan(mine, ok, &scan[turn], &at, &total);
-    at.tokens += carry.tokens; at.blocks += carry.blocks; at.pieces += carry.pieces;
-    carry.tokens += total.tokens; carry.blocks += total.blocks; carry.pieces += total.pieces;
-    ok &= carry.tokens >= total.tokens;
-#pragma unroll
-    for (uint32_t i = 0; i < PLAN_PER; i += 4) {
-      i32x4_by_words length, offset;
-      uint2 base[4];
-#pragma unroll
-      for (uint32_t j = 0; j < 4; ++j) {
-        length[j] = static_cast<int32_t>(static_cast<uint32_t>(cached[i + j]) + static_cast<uint32_t>(added[i + j]));
-        offset[j] = static_cast<int32_t>(at.tokens);
-        base[j] = make_uint2(at.blocks, at.pieces);
-        plan_request(a, cached[i + j], added[i + j], &at);
-      }
-      if (whole) {
-        *reinterpret_cast<i32x4_by_words*>(a.lengths + first + i) = length;
-        *reinterpret_cast<i32x4_by_words*>(a.token_offsets + first + i) = offset;
-        uint4* to = reinterpret_cast<uint4*>(a.bases + first + i);
-        to[0] = make_uint4(base[0].x, base[0].y, base[1].x, base[1].y);
-        to[1] = make_uint4(base[2].x, base[2].y, base[3].x, base[3].y);
-      } else {
-#pragma unroll
-        for (uint32_t j = 0; j < 4; ++j)
-          if (first + i + j < a.n_requests) {
-            a.lengths[first + i + j] = length[j];
-            a.token_offsets[first + i + j] = offset[j];
-            a.bases[first + i + j] = base[j];
-          }
-      }
-    }
-  }
-  if (threadIdx.x == 0) {
-    if (const int32_t error = plan_error(a, carry, ok)) *a.status = error;
-    a.token_offsets[a.n_requests] = static_cast<int32_t>(a.n_tokens);
-    a.counts[0] = static_cast<int32_t>(carry.blocks);
-    a.counts[1] = static_cast<int32_t>(carry.pieces);
-  }
+// More: first the sums of every 1024 requests ...
+__global__ __launch_bounds__(PLAN_THREADS) void k_plan_tiles(PlanArgs a) {
+  __shared__ PlanScan scan;
+  const uint32_t r = blockIdx.x * PLAN_THREADS + threadIdx.x;
+  const bool there = r < a.n_requests;
+  const PlanRequest mine(a, there ? a.cached[r] : 0, there ? a.added[r] : 0);
+  PlanSums at, total;
+  const bool ok = plan_scan(PlanSums{mine.added(), mine.blocks, mine.pieces}, mine.ok, &scan, &at, &total);
+  if (threadIdx.x == 0) a.tiles[blockIdx.x] = PlanTile{ok ? total.tokens : PLAN_BAD, total.blocks, total.pieces};
 }
 
-__global__ __launch_bounds__(256) void k_plan_tokens(PlanArgs a) {
-  if (stopped(a.status)) return;
-  const uint32_t t = blockIdx.x * 256 + threadIdx.x;
-  if (t < a.n_tokens) {
-    const uint32_t r = plan_find(a.token_offsets, 0, a.n_requests, t);
-    plan_token(a, t, r, static_cast<uint32_t>(a.token_offsets[r]), a.bases[r].x, a.bases[r].y);
+// ... then every workgroup sums the up to 1024 tiles, and of those that hold its tokens the requests.  (16,384 requests: 3 and 9 us; one
+// launch in which every workgroup summed all requests took 20.)
+constexpr uint32_t PLAN_MOST_REQUESTS = PLAN_THREADS * PLAN_THREADS;
+__global__ __launch_bounds__(PLAN_THREADS) void k_plan_tokens(PlanArgs a) {
+  __shared__ PlanRequests requests;
+  __shared__ uint32_t tile_tokens[PLAN_THREADS];
+  __shared__ uint2 tile_rest[PLAN_THREADS];
+  __shared__ PlanScan scans[2];
+  const uint32_t n_tiles = (a.n_requests + PLAN_THREADS - 1) / PLAN_THREADS;
+  const bool stop = stopped(a.status);
+  PlanTile tile{0, 0, 0};
+  if (threadIdx.x < n_tiles) tile = a.tiles[threadIdx.x];
+  if (stop) return;
+  PlanSums at, total;
+  const bool ok = plan_scan(PlanSums{tile.tokens, tile.blocks, tile.pieces}, tile.tokens < PLAN_BAD, &scans[0], &at, &total);
+  if (const int32_t error = plan_error(a, total, ok)) {
+    if (threadIdx.x == 0) *a.status = error;
+    return;
   }
-  for (uint64_t i = static_cast<uint64_t>(static_cast<uint32_t>(a.counts[1])) + t; i < a.room; i += static_cast<uint64_t>(gridDim.x) * 256)
-    a.pieces[i] = make_int4(-1, -1, -1, -1);
+  tile_tokens[threadIdx.x] = static_cast<uint32_t>(at.tokens);
+  tile_rest[threadIdx.x] = make_uint2(at.blocks, at.pieces);
+  __syncthreads();
+  uint32_t turn = 0, held = 0xffffffffu;
+  auto read_tile = [&](uint32_t i) {             // (i is the same in the workgroup)
+    if (i == held) return;
+    held = i;
+    turn ^= 1;
+    const uint32_t r = i * PLAN_THREADS + threadIdx.x;
+    const bool there = r < a.n_requests;
+    const PlanRequest mine(a, there ? a.cached[r] : 0, there ? a.added[r] : 0);
+    PlanSums before, all;
+    plan_scan(PlanSums{mine.added(), mine.blocks, mine.pieces}, true, &scans[turn], &before, &all);
+    requests.first[threadIdx.x] = tile_tokens[i] + static_cast<uint32_t>(before.tokens);
+    requests.rest[threadIdx.x] = make_uint4(mine.cached, mine.length, tile_rest[i].x + before.blocks, tile_rest[i].y + before.pieces);
+    __syncthreads();
+  };
+  plan_rest(a, total.pieces, blockIdx.x * PLAN_THREADS + threadIdx.x, gridDim.x * PLAN_THREADS);
+  if (blockIdx.x < n_tiles) {                    // the first workgroups write the requests' outputs, a tile each
+    read_tile(blockIdx.x);
+    const uint32_t r = blockIdx.x * PLAN_THREADS + threadIdx.x;
+    if (r < a.n_requests) {
+      a.lengths[r] = static_cast<int32_t>(requests.rest[threadIdx.x].y);
+      a.token_offsets[r] = static_cast<int32_t>(requests.first[threadIdx.x]);
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) plan_counts(a, total);
+    return;
+  }
+  const uint64_t stride = static_cast<uint64_t>(gridDim.x - n_tiles) * PLAN_THREADS;
+  for (uint64_t from = static_cast<uint64_t>(blockIdx.x - n_tiles) * PLAN_THREADS; from < a.n_tokens; from += stride) {
+    const uint32_t t = static_cast<uint32_t>(from) + threadIdx.x;
+    for (uint64_t next = from; next < from + PLAN_THREADS && next < a.n_tokens;) {
+      const uint32_t i = plan_find(tile_tokens, 0, n_tiles, static_cast<uint32_t>(next));
+      const uint32_t end = i + 1 < n_tiles ? tile_tokens[i + 1] : a.n_tokens;
+      read_tile(i);
+      if (t >= next && t < end) plan_token(a, requests, i * PLAN_THREADS, min_u32(a.n_requests - i * PLAN_THREADS, PLAN_THREADS), t);
+      next = end;
+      // (the tile's place is written again only behind the next plan_scan's barrier, which all pass after they have read this one)
+    }
+  }
 }
 
 // ---- append -----------------------------------------------------------------------------------------------------

@@ -14,7 +14,7 @@ using namespace fikit;
 
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
-constexpr uint32_t PLAN_ONE_GROUPS = 512;         // two for each CU
+constexpr uint32_t PLAN_GROUPS = 512;             // two for each CU
 constexpr uint64_t MOST_GROUPS = 0x7fffffffull;   // workgroups of a launch
 
 template <typename... P, typename... A>
@@ -115,7 +115,7 @@ uint64_t fikit_cache_pieces(uint32_t n_tokens, uint32_t n_requests, uint32_t blo
 }
 
 size_t fikit_cache_plan_workspace_bytes(uint32_t n_requests) {
-  return n_requests <= PLAN_ONE_REQUESTS ? 0 : (static_cast<size_t>(n_requests) * sizeof(uint2) + 255) / 256 * 256;
+  return n_requests <= PLAN_THREADS ? 0 : ((static_cast<size_t>(n_requests) + PLAN_THREADS - 1) / PLAN_THREADS * sizeof(PlanTile) + 255) / 256 * 256;
 }
 
 int fikit_cache_plan(const int32_t* d_cached, const int32_t* d_added, uint32_t n_requests, uint32_t n_tokens,
@@ -132,6 +132,7 @@ int fikit_cache_plan(const int32_t* d_cached, const int32_t* d_added, uint32_t n
   if (n_free > 0 && !d_free) return FIKIT_INVALID_ARG;
   if (!aligned(d_block_table, 4) || !aligned(d_free, 4) || !aligned(d_slots, 8) || !aligned(d_pieces, 16)) return FIKIT_INVALID_ARG;
   if (block_tokens < 16 || block_tokens > 256 || (block_tokens & (block_tokens - 1))) return FIKIT_UNSUPPORTED;
+  if (n_requests > PLAN_MOST_REQUESTS) return FIKIT_UNSUPPORTED;
   if (const size_t need = fikit_cache_plan_workspace_bytes(n_requests)) {
     if (!d_workspace || !aligned(d_workspace, 256)) return FIKIT_INVALID_ARG;
     if (workspace_bytes < need) return FIKIT_WORKSPACE_TOO_SMALL;
@@ -148,23 +149,19 @@ int fikit_cache_plan(const int32_t* d_cached, const int32_t* d_added, uint32_t n
   a.pieces = reinterpret_cast<int4*>(d_pieces);
   a.counts = d_counts;
   a.status = d_status;
-  a.bases = static_cast<uint2*>(d_workspace);
+  a.tiles = static_cast<PlanTile*>(d_workspace);
   a.n_requests = n_requests;
   a.n_tokens = n_tokens;
   a.table_width = table_width;
   a.n_free = n_free;
   a.room = static_cast<uint32_t>(fikit_cache_pieces(n_tokens, n_requests, block_tokens));
   a.shift = static_cast<uint32_t>(__builtin_ctz(block_tokens));
-  if (n_requests <= PLAN_ONE_REQUESTS) {
-    const uint32_t groups = (n_tokens + PLAN_THREADS - 1) / PLAN_THREADS;
-    const dim3 grid(groups < 1 ? 1 : groups > PLAN_ONE_GROUPS ? PLAN_ONE_GROUPS : groups), block(PLAN_THREADS);
-    if (n_requests <= PLAN_THREADS) return enqueue(k_plan_one<1>, grid, block, st, a);
-    if (n_requests <= 4 * PLAN_THREADS) return enqueue(k_plan_one<4>, grid, block, st, a);
-    return enqueue(k_plan_one<16>, grid, block, st, a);
-  }
-  if (int rc = enqueue(k_plan_sums, dim3(1), dim3(PLAN_THREADS), st, a)) return rc;
-  if (n_tokens == 0) return FIKIT_OK;
-  return enqueue(k_plan_tokens, dim3((n_tokens + 255) / 256), dim3(256), st, a);
+  const dim3 block(PLAN_THREADS);
+  const uint32_t of_tokens = (n_tokens + PLAN_THREADS - 1) / PLAN_THREADS, tiles = (n_requests + PLAN_THREADS - 1) / PLAN_THREADS;
+  const uint32_t groups = of_tokens < PLAN_GROUPS ? of_tokens : PLAN_GROUPS;
+  if (n_requests <= PLAN_THREADS) return enqueue(k_plan_one, dim3(groups < 1 ? 1 : groups), block, st, a);
+  if (int rc = enqueue(k_plan_tiles, dim3(tiles), block, st, a)) return rc;
+  return enqueue(k_plan_tokens, dim3(tiles + groups), block, st, a);
 }
 
 int fikit_cache_append(const fikit_cache* h_cache, const fikit_vectors* h_k, const fikit_vectors* h_v, uint32_t n_tokens,

@@ -76,6 +76,14 @@ at::Tensor workspace_of(PyObject* given, size_t bytes, const at::Device& device)
 
 void* stream_of(PyObject* o) { return reinterpret_cast<void*>(THPUtils_unpackLong(o)); }
 
+// A tensor in the memory of another one, from place `from` (in its own type) on.
+at::Tensor part_of(const at::Tensor& all, at::ScalarType type, int64_t from, at::IntArrayRef sizes) {
+  at::Tensor t = at::detail::make_tensor<at::TensorImpl>(at::TensorImpl::VIEW, at::Storage(all.storage()), all.key_set(), at::scalarTypeToTypeMeta(type));
+  t.unsafeGetTensorImpl()->set_sizes_contiguous(sizes);
+  t.unsafeGetTensorImpl()->set_storage_offset(from);
+  return t;
+}
+
 PyObject* wrapped(const at::Tensor& t) {
   if (!t.defined()) Py_RETURN_NONE;
   return THPVariable_Wrap(t);
@@ -97,11 +105,14 @@ PyObject* py_cache_plan(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   const auto i32 = at::TensorOptions().dtype(at::kInt).device(device);
   at::Tensor lengths, offsets, slots, pieces, counts;
   if (a[8] == Py_None) {
-    lengths = at::empty({n}, i32);
-    offsets = at::empty({static_cast<int64_t>(n) + 1}, i32);
-    if (a[7] == Py_True) slots = at::empty({n_tokens}, i32.dtype(at::kLong));
-    pieces = at::empty({room, 4}, i32);
-    counts = at::empty({2}, i32);
+    // one allocation: slots (two words each), pieces, lengths, places, counts
+    const int64_t of_pieces = a[7] == Py_True ? (2 * static_cast<int64_t>(n_tokens) + 3) / 4 * 4 : 0, of_lengths = of_pieces + 4 * room;
+    const at::Tensor all = at::empty({of_lengths + 2 * static_cast<int64_t>(n) + 3}, i32);
+    if (a[7] == Py_True) slots = part_of(all, at::kLong, 0, {n_tokens});
+    pieces = part_of(all, at::kInt, of_pieces, {room, 4});
+    lengths = part_of(all, at::kInt, of_lengths, {n});
+    offsets = part_of(all, at::kInt, of_lengths + n, {static_cast<int64_t>(n) + 1});
+    counts = part_of(all, at::kInt, of_lengths + 2 * static_cast<int64_t>(n) + 1, {2});
   } else {
     TORCH_CHECK_VALUE(PyTuple_Check(a[8]) && PyTuple_GET_SIZE(a[8]) == 5, "out: a CachePlan");
     lengths = tensor(PyTuple_GET_ITEM(a[8], 0), "lengths");

@@ -24,7 +24,7 @@ def plan(**change):
     (dict(lengths=NULL), INVALID), (dict(offsets=NULL), INVALID), (dict(slots=FAKE + 4), INVALID), (dict(pieces=NULL), INVALID),
     (dict(pieces=FAKE + 8), INVALID), (dict(counts=NULL), INVALID), (dict(status=NULL), INVALID),
     (dict(n_requests=20000, ws=NULL), INVALID), (dict(n_requests=20000, ws=FAKE + 16), INVALID),
-    (dict(n_requests=0), INVALID), (dict(n_tokens=1 << 31), INVALID), (dict(n_requests=20000, ws_bytes=256), SMALL),
+    (dict(n_requests=0), INVALID), (dict(n_tokens=1 << 31), INVALID), (dict(n_requests=20000, ws_bytes=16), SMALL), (dict(n_requests=(1 << 20) + 1), UNSUPPORTED),
     (dict(block=0), UNSUPPORTED), (dict(block=8), UNSUPPORTED), (dict(block=48), UNSUPPORTED), (dict(block=512), UNSUPPORTED),
 ])
 def test_plan(change, want):
@@ -105,7 +105,7 @@ def test_sizes():
         got = model.plan(cached, added, 16, np.array(table), range(99))
         assert got["counts"][1] <= binding.fikit_cache_pieces(sum(added), len(cached), 16)
     lib = binding.load()
-    assert lib.fikit_cache_plan_workspace_bytes(20000) >= 160000
+    assert lib.fikit_cache_plan_workspace_bytes(1024) == 0 and lib.fikit_cache_plan_workspace_bytes(1025) >= 32
     assert binding.fikit_cache_attention_workspace_bytes(4, 6, 4, 64, 100) == 0
     assert 0 < binding.fikit_cache_attention_workspace_bytes(1, 8, 8, 64, 100) <= binding.fikit_cache_attention_workspace_bytes(1, 8, 8, 128, 100000)
     assert binding.status_string(binding.FIKIT_CACHE_FULL) not in ("ok", "unknown status")
