@@ -347,7 +347,7 @@ __global__ __launch_bounds__(APPEND_WAVES * WAVE) void k_cache_append(AppendArgs
       } else {
         for (int j = 0; j < 2; ++j) out[j] = T::codes_of_pairs(held[i][2 * j], held[i][2 * j + 1], scale);
       }
-      if (c < chunks) *reinterpret_cast<u32x2*>(codes + at * D + c * 8) = out;
+      if (c < chunks) __builtin_nontemporal_store(out, reinterpret_cast<u32x2*>(codes + at * D + c * 8));      // (13.3 us of 11,000 tokens; 14.9 through the caches)
     }
   }
   // earlier tokens of the block: the same values to a larger scale (old 0: a block that nothing has been put into)

@@ -52,7 +52,6 @@ __host__ __device__ inline uint32_t decode_chunks(uint32_t length) { return leng
 constexpr uint32_t DECODE_FIXED = 1;
 __host__ __device__ inline uint32_t decode_weight(uint32_t length) { return decode_chunks(length) + DECODE_FIXED; }
 
-// Chunks of all requests, and the request that chunk `at` of a unit belongs to.
 struct DecodeLook {
   uint32_t sums[DECODE_WAVES];
   uint32_t request, first;
@@ -106,38 +105,60 @@ __global__ __launch_bounds__(DECODE_WAVES * WAVE, D == 128 ? 2 : 4) void k_decod
   const uint64_t unit_bytes = static_cast<uint64_t>(a.cache.block_tokens) * D;
   const float scale = a.scale * LOG2E;
 
-  uint32_t before, mine, per_unit;
-  if (!decode_look(a, &look, &before, &mine, &per_unit)) return;
-  if (blockIdx.x == 0 && threadIdx.x == 0) *a.per_unit = per_unit;
-  const uint64_t total = static_cast<uint64_t>(per_unit) * units;
-  const uint32_t groups = total < a.groups ? static_cast<uint32_t>(total) : a.groups;
-  if (blockIdx.x >= groups) return;
-  const uint64_t lo = blockIdx.x * total / groups, hi = (blockIdx.x + 1) * total / groups;
-  uint64_t left = hi - lo;
-  const uint32_t target = static_cast<uint32_t>(lo / units);
-  const uint32_t per_thread = (a.n_requests + DECODE_WAVES * WAVE - 1) / (DECODE_WAVES * WAVE);
-  if (target >= before && target - before < mine) {
-    look.request = threadIdx.x * per_thread;
-    look.first = before;
-  }
-  __syncthreads();
-  uint32_t request = uniform(look.request), first = uniform(look.first), length, weight;
-  for (;;) {               // of the requests that a thread has added up, 64 at a time, the one that holds chunk `target`
-    const uint32_t r = request + lane;
-    const uint32_t n = r < a.n_requests ? static_cast<uint32_t>(a.lengths[r]) : 0, c = decode_weight(n);
-    const uint32_t run = wave_incl_scan_u32(c);
-    const uint64_t beyond = ballot(first + run > target);
-    if (beyond) {
-      const uint32_t owner = uniform(static_cast<uint32_t>(__builtin_ctzll(beyond)));
-      length = read_lane_u32(n, owner);
-      weight = read_lane_u32(c, owner);
-      first += read_lane_u32(run, owner) - weight;
-      request += owner;
-      break;
+  // where this workgroup's chunks begin: request, its length, its weight, the weights of the requests before
+  uint32_t request, length, weight, first, per_unit, groups;
+  uint64_t total, lo, left;
+  auto cut = [&] {
+    total = static_cast<uint64_t>(per_unit) * units;
+    groups = total < a.groups ? static_cast<uint32_t>(total) : a.groups;
+    lo = blockIdx.x * total / groups;
+    left = (blockIdx.x + 1) * total / groups - lo;
+    return static_cast<uint32_t>(lo / units);
+  };
+  auto pick = [&](uint32_t n, uint32_t w, uint32_t upto, uint32_t target) {      // the lane's request whose weight reaches past the target
+    const uint64_t beyond = ballot(upto > target);
+    if (!beyond) return false;
+    const uint32_t owner = uniform(static_cast<uint32_t>(__builtin_ctzll(beyond)));
+    length = read_lane_u32(n, owner);
+    weight = read_lane_u32(w, owner);
+    first = read_lane_u32(upto, owner) - weight;
+    request += owner;
+    return true;
+  };
+  if (a.n_requests <= WAVE) {      // each wave by itself, nothing is exchanged
+    const bool stop = stopped(a.status), there = lane < a.n_requests;
+    const int32_t n = there ? a.lengths[lane] : 0;
+    if (ballot(n < 0 || static_cast<uint32_t>(n) > a.max_length) || stop) {
+      if (threadIdx.x == 0 && !stop) *a.status = FIKIT_INVALID_ARG;
+      return;
     }
-    first += read_lane_u32(run, WAVE - 1);
-    request += WAVE;
+    const uint32_t w = there ? decode_weight(static_cast<uint32_t>(n)) : 0, upto = wave_incl_scan_u32(w);
+    per_unit = read_lane_u32(upto, WAVE - 1);
+    const uint32_t target = cut();
+    if (blockIdx.x >= groups) return;
+    request = 0;
+    pick(static_cast<uint32_t>(n), w, upto, target);
+  } else {
+    uint32_t before, mine;
+    if (!decode_look(a, &look, &before, &mine, &per_unit)) return;
+    const uint32_t target = cut();
+    if (blockIdx.x >= groups) return;
+    if (target >= before && target - before < mine) {
+      look.request = threadIdx.x * ((a.n_requests + DECODE_WAVES * WAVE - 1) / (DECODE_WAVES * WAVE));
+      look.first = before;
+    }
+    __syncthreads();
+    request = uniform(look.request);
+    uint32_t upto = uniform(look.first);
+    for (;;) {               // of the requests that a thread has added up, 64 at a time
+      const uint32_t r = request + lane;
+      const uint32_t n = r < a.n_requests ? static_cast<uint32_t>(a.lengths[r]) : 0, w = decode_weight(n), run = wave_incl_scan_u32(w);
+      if (pick(n, w, upto + run, target)) break;
+      upto += read_lane_u32(run, WAVE - 1);
+      request += WAVE;
+    }
   }
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.per_unit = per_unit;
   const uint64_t inside = lo - static_cast<uint64_t>(first) * units;
   uint32_t unit = static_cast<uint32_t>(inside / weight), chunk = static_cast<uint32_t>(inside % weight);
 
