@@ -607,7 +607,7 @@ _stream_of = torch._C._cuda_getCurrentRawStream
 
 
 def _marshal():
-    """The compiled marshalling of these calls (csrc/serve_marshal.cpp), with the library's addresses."""
+    """The compiled marshalling of these calls (csrc/service/serve_marshal.cpp), with the library's addresses."""
     global _native
     if _native is None:
         lib = load()

@@ -16,11 +16,11 @@ HIPCC_FLAGS = [
     "-Wall", "-Wno-unused-function",
 ]
 
-UNITS = ["fikit.hip", "serve.hip"]                       # translation units
+UNITS = ["fikit.hip", os.path.join("service", "serve.hip")]        # translation units
 
 
 def sources():
-    return sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".hip", ".h")))
+    return sorted(os.path.join(d, f) for d, _, files in os.walk(CSRC) for f in files if f.endswith((".hip", ".h")))
 
 
 def stale() -> bool:
@@ -59,7 +59,7 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
 
 def build_marshal(force: bool = False, verbose: bool = False) -> str:
     """Host code only, against torch's headers."""
-    source = os.path.join(CSRC, "serve_marshal.cpp")
+    source = os.path.join(CSRC, "service", "serve_marshal.cpp")
     if not force and os.path.exists(MARSHAL) and all(
             os.path.getmtime(f) <= os.path.getmtime(MARSHAL) for f in (source, os.path.join(ROOT, "include", "fikit.h"))):
         return MARSHAL
