@@ -33,6 +33,7 @@ class Sizes(NamedTuple):
     dim: int = 128
     block: int = 64
     blocks: int = 4096         # of the cache, per layer
+    vocabulary: int = 8192
 
     @property
     def hidden(self) -> int:
@@ -79,6 +80,7 @@ class Service:
             return torch.randn((rows, cols), generator=gen, device=device, dtype=torch.float32).div_(math.sqrt(rows)).to(torch.bfloat16)
         self.w_qkv = [weight(sizes.hidden, heads * sizes.dim) for _ in range(sizes.layers)]
         self.w_out = [weight(sizes.hidden, sizes.hidden) for _ in range(sizes.layers)]
+        self.w_tokens = weight(sizes.hidden, sizes.vocabulary)
         shape = (sizes.blocks, sizes.kv_heads, sizes.block, sizes.dim)
         self.caches = [[torch.zeros(shape, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn) for _ in range(2)] +
                        [torch.ones(shape[:2], dtype=torch.uint8, device=device) for _ in range(2)] for _ in range(sizes.layers)]
@@ -117,7 +119,7 @@ class Service:
         return x
 
     def step(self, record, x: torch.Tensor) -> torch.Tensor:
-        """x: [requests, hidden], one new token per request."""
+        """x: [requests, hidden], one new token per request; returns the logits of the next."""
         n = x.shape[0]
         plan = self._plan(record, [1] * n)
         scale = 1 / math.sqrt(self.sizes.dim)
@@ -125,8 +127,9 @@ class Service:
             x = self._layer(record, x, layer, lambda q, k, v, at: record(
                 "cache attention", (n, 1, 1), binding.fikit_cache_attention, q, *self.caches[at], self.table, plan.lengths, scale,
                 self.status, max_length=self.longest + 1, want_lse=False).out, plan)
+        logits = record("to tokens", (n, 1, 1), torch.mm, x, self.w_tokens)
         self._settle(plan, 1)
-        return x
+        return logits
 
     def _settle(self, plan, most_added) -> None:
         """What the host does at the end of a step, when it waits for the outputs anyway."""

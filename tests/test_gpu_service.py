@@ -10,11 +10,7 @@ import serve_model as model
 from paper_2311_10359_amd import binding, service, traces
 
 pytestmark = pytest.mark.gpu
-SIZES = service.Sizes(layers=2, q_heads=8, kv_heads=2, dim=64, block=16, blocks=400)
-
-
-def plain(record_name, sizes, f, *args, **more):
-    return f(*args, **more)
+SIZES = service.Sizes(layers=2, q_heads=8, kv_heads=2, dim=64, block=16, blocks=400, vocabulary=512)
 
 
 def test_steps_see_what_prompts_and_steps_have_put_into_the_cache():
@@ -58,8 +54,8 @@ def test_steps_see_what_prompts_and_steps_have_put_into_the_cache():
 def test_records_go_through_the_profile_and_the_gap_fill():
     (decode, names), (prompts, _), got, s = service.measure(SIZES, requests=5, longest_prompt=60, steps=4, host_ms=0.2)
     assert torch.isfinite(got["step"]).all() and torch.isfinite(got["prompts"]).all() and int(s.status) == 0
-    assert decode.size == 4 * (1 + 2 * 4) and prompts.size == 1 + 2 * 4 and set(names) == {"plan", "append", "cache attention", "back",
-                                                                                          "to queries, keys, values"}
+    assert decode.size == 4 * (2 + 2 * 4) and prompts.size == 1 + 2 * 4 and set(names) == {"plan", "append", "cache attention", "back",
+                                                                                          "to queries, keys, values", "to tokens"}
     assert (decode["end_ns"] >= decode["start_ns"]).all() and (np.diff(decode["start_ns"]) >= 0).all()
     decode["run"] = 0
     rec = np.concatenate([decode, prompts])
