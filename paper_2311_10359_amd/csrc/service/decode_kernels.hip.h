@@ -14,17 +14,25 @@ namespace fikit {
 //            passes it by 2^8 (32 bits have room), so most steps exchange nothing between lanes.
 //   outputs  O^T[dim][query] += V^T P^T: the order of the tokens within the product is free, so lane l takes as its eight
 //            those whose weights it has, and reads their value codes at D / 16 consecutive dimensions.  Rounding a weight to 16
-//            bits would cost as much as rounding the output; what it leaves is a second operand, which costs nothing here.
+//            bits would cost as much as rounding the output; what it leaves is a second operand, which costs nothing here: the
+//            matrix unit is busy for an eighth of the time.
 //
 // Codes become 16-bit values, scale included, in one instruction for two; nothing goes through LDS but the joining of
 // the waves' results.
+//
+// Bound by memory: a token costs 2 D bytes a key head and no more than 4 D operations for each of its query heads.  Two steps of codes are
+// in flight per wave, in registers, which is what 8 waves (16 with heads of 64) on a compute unit leave room for.  128 requests of 4096 to
+// 16,384 tokens, 8 heads of 128 (2.2 GB): 340 us, 6.5 TB/s, of the 7.2 that a kernel reaches which only reads past the caches; 64 requests
+// of 1 to 13,517 tokens, 16 heads of 64, blocks of 16 (145 MB): 31 us, 4.6 TB/s; 2 of 76,687 and 127,690, 4 heads of 128 (209 MB, half of it
+// found in the last-level cache): 38; one of 4097 (8 MB): 6.8, latency.
 //
 // The work is cut evenly: with 128 tokens of a request, for one unit (key head and tile of query heads), as a chunk, and chunks in
 // the order of requests, units, tokens, workgroup b of W takes chunks b T / W .. (b + 1) T / W - 1 of all T, whatever requests they
 // belong to.  W is what the chip holds at once, so nothing is left over at the end, and what a workgroup begins with (adding up all
 // lengths, first loads) is paid once.  Beginning and ending a stretch takes as long as DECODE_FIXED chunks, so a request's chunks
-// are followed by so many empty ones.  Only the first and the last of a workgroup's stretches can be parts of longer ones; these are
-// joined by k_decode_join.
+// are followed by so many empty ones (the 64 ragged requests with the joining: one 36.8 us, none 43.1, two 38.3, four 40.6).  Only the first and
+// the last of a workgroup's stretches can be parts of longer ones; these are joined by k_decode_join.  (One workgroup for each part of equal
+// length, as many as the longest request takes of all, was 41 us for the ragged requests, most of it for workgroups that found nothing to do.)
 
 struct DecodeArgs {
   fikit_cache cache;
@@ -90,8 +98,9 @@ __device__ __forceinline__ bool decode_look(const DecodeArgs& a, DecodeLook* lds
 // Which of `groups` workgroups takes chunk i of t.
 __device__ __forceinline__ uint32_t decode_owner(uint64_t i, uint64_t t, uint32_t groups) { return static_cast<uint32_t>(((i + 1) * groups - 1) / t); }
 
-// ONCE: no other workgroup reads these keys and values, so they are read past the caches (a tenth of the time of large
-// calls).  That is the case for up to 16 query heads to a key head; for 32 the second reader finds them in a cache.
+// ONCE: no other workgroup reads these keys and values, so they are read past the caches: 5 to 10 % of the time of large
+// calls.  That is the case for up to 16 query heads to a key head; for 32 the second reader finds them in a cache (64 requests of 8192
+// tokens, 2 heads of 128: 94 us through the caches, 119 past them).
 template <typename T, int D, bool ONCE>
 __global__ __launch_bounds__(DECODE_WAVES * WAVE, D == 128 ? 2 : 4) void k_decode(DecodeArgs a) {
   constexpr int KV_WORDS = D / 64;
@@ -432,7 +441,9 @@ __global__ __launch_bounds__(DECODE_WAVES * WAVE, D == 128 ? 2 : 4) void k_decod
 
 // Joins the parts of a request and unit that was cut.  A workgroup for each place where one of k_decode's workgroups began: the n
 // parts of a unit have n - 1 such places, whose workgroups share its query heads.  The parts of a head are added up in the same order
-// always: by one wave, or, if a workgroup has a single head, by each wave every fourth part and then the waves.
+// always: by one wave, or, if a workgroup has a single head, by each wave every fourth part and then the waves.  Latency of two dependent
+// loads and a launch: 4.9 us for up to 512 cuts, 6.8 where two requests of 76,687 and 127,690 tokens left up to 80 parts to a unit.  (A workgroup for each
+// request and head took 30 us for 4000 requests, of which few were cut.)
 template <typename T, int D>
 __global__ __launch_bounds__(DECODE_WAVES * WAVE) void k_decode_join(DecodeArgs a) {
   __shared__ float2 sums[DECODE_WAVES];
