@@ -106,6 +106,9 @@ __device__ __forceinline__ uint32_t max_over_wave(uint32_t v) {
 }
 
 // Errors are written, success is not: see fikit.h.
-__device__ __forceinline__ bool stopped(const int32_t* status) { return *static_cast<const volatile int32_t*>(status) != FIKIT_OK; }
+// (Read once and through the caches: what this kernel's other workgroups write there may be seen or not.)
+__device__ __forceinline__ bool stopped(const int32_t* status) {
+  return __hip_atomic_load(status, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT) != FIKIT_OK;
+}
 
 }  // namespace fikit
