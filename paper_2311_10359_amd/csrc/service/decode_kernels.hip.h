@@ -95,8 +95,22 @@ __device__ __forceinline__ bool decode_look(const DecodeArgs& a, DecodeLook* lds
   return true;
 }
 
-// Which of `groups` workgroups takes chunk i of t.
-__device__ __forceinline__ uint32_t decode_owner(uint64_t i, uint64_t t, uint32_t groups) { return static_cast<uint32_t>(((i + 1) * groups - 1) / t); }
+// (Numbers of chunks fit 32 bits nearly always, and dividing 64 takes half a microsecond.)
+__device__ __forceinline__ uint64_t quotient(uint64_t a, uint64_t b) {
+  return (a | b) >> 32 ? a / b : static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+}
+// Of all chunks workgroup b takes first(b) = b * total / groups and those up to first(b + 1), so the larger shares are spread evenly.
+struct DecodeShares {
+  uint32_t groups, more;
+  uint64_t total, each;
+  __device__ __forceinline__ DecodeShares(uint64_t total_, uint32_t most_groups) : total(total_) {
+    groups = total < most_groups ? static_cast<uint32_t>(total) : most_groups;
+    each = quotient(total, groups);
+    more = static_cast<uint32_t>(total - each * groups);
+  }
+  __device__ __forceinline__ uint64_t first(uint32_t group) const { return group * each + group * more / groups; }      // (2^10 groups at most)
+  __device__ __forceinline__ uint32_t owner(uint64_t chunk) const { return static_cast<uint32_t>(quotient((chunk + 1) * groups - 1, total)); }
+};
 
 // ONCE: no other workgroup reads these keys and values, so they are read past the caches: 5 to 10 % of the time of large
 // calls.  That is the case for up to 16 query heads to a key head; for 32 the second reader finds them in a cache (64 requests of 8192
@@ -116,13 +130,13 @@ __global__ __launch_bounds__(DECODE_WAVES * WAVE, D == 128 ? 2 : 4) void k_decod
 
   // where this workgroup's chunks begin: request, its length, its weight, the weights of the requests before
   uint32_t request, length, weight, first, per_unit, groups;
-  uint64_t total, lo, left;
+  uint64_t lo, left;
   auto cut = [&] {
-    total = static_cast<uint64_t>(per_unit) * units;
-    groups = total < a.groups ? static_cast<uint32_t>(total) : a.groups;
-    lo = blockIdx.x * total / groups;
-    left = (blockIdx.x + 1) * total / groups - lo;
-    return static_cast<uint32_t>(lo / units);
+    const DecodeShares shares(static_cast<uint64_t>(per_unit) * units, a.groups);
+    groups = shares.groups;
+    lo = shares.first(blockIdx.x);
+    left = shares.first(blockIdx.x + 1) - lo;
+    return static_cast<uint32_t>(quotient(lo, units));
   };
   auto pick = [&](uint32_t n, uint32_t w, uint32_t upto, uint32_t target) {      // the lane's request whose weight reaches past the target
     const uint64_t beyond = ballot(upto > target);
@@ -169,7 +183,7 @@ __global__ __launch_bounds__(DECODE_WAVES * WAVE, D == 128 ? 2 : 4) void k_decod
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) *a.per_unit = per_unit;
   const uint64_t inside = lo - static_cast<uint64_t>(first) * units;
-  uint32_t unit = static_cast<uint32_t>(inside / weight), chunk = static_cast<uint32_t>(inside % weight);
+  uint32_t unit = static_cast<uint32_t>(quotient(inside, weight)), chunk = static_cast<uint32_t>(inside - static_cast<uint64_t>(unit) * weight);
 
   if (threadIdx.x == 0) a.cuts[blockIdx.x] = make_uint4(request, unit, chunk, weight);
 
@@ -448,22 +462,25 @@ template <typename T, int D>
 __global__ __launch_bounds__(DECODE_WAVES * WAVE) void k_decode_join(DecodeArgs a) {
   __shared__ float2 sums[DECODE_WAVES];
   __shared__ float outs[DECODE_WAVES][D];
-  if (stopped(a.status)) return;
+  const bool stop = stopped(a.status);        // (of the three loads none waits for another)
+  const uint32_t per_unit = uniform(*a.per_unit);
+  uint4 cut = a.cuts[blockIdx.x];
+  asm volatile("" : "+v"(cut.x), "+v"(cut.y), "+v"(cut.z), "+v"(cut.w));      // (or it is read behind the branch)
+  if (stop) return;
   const uint32_t units = a.cache.kv_heads * a.head_tiles, group = a.q_heads / a.cache.kv_heads, most_rows = min_u32(group, DECODE_ROWS);
-  const uint64_t total = static_cast<uint64_t>(*a.per_unit) * units;
-  const uint32_t groups = total < a.groups ? static_cast<uint32_t>(total) : a.groups;
-  if (blockIdx.x >= groups) return;
-  const uint4 cut = a.cuts[blockIdx.x];
+  const DecodeShares shares(static_cast<uint64_t>(per_unit) * units, a.groups);
+  if (blockIdx.x >= shares.groups) return;
+  cut = make_uint4(uniform(cut.x), uniform(cut.y), uniform(cut.z), uniform(cut.w));
   const uint32_t request = cut.x, unit = cut.y, chunks = cut.w - DECODE_FIXED;
   if (cut.z == 0 || cut.z >= chunks) return;                  // (begins with the unit, or behind its last chunk)
-  const uint64_t begin = blockIdx.x * total / groups - cut.z;
-  const uint32_t from = decode_owner(begin, total, groups), parts = decode_owner(begin + chunks - 1, total, groups) - from + 1;
+  const uint64_t begin = shares.first(blockIdx.x) - cut.z;
+  const uint32_t from = shares.owner(begin), parts = shares.owner(begin + chunks - 1) - from + 1;
   const uint32_t mine = blockIdx.x - from - 1, sharers = parts - 1;
   const uint32_t tile = unit % a.head_tiles, rows = min_u32(group - tile * DECODE_ROWS, DECODE_ROWS);
   if (mine >= sharers || mine >= rows) return;
   const uint64_t head0 = static_cast<uint64_t>(request) * a.q_heads + unit / a.head_tiles * group + tile * DECODE_ROWS;
   // the first part is its workgroup's last stretch, and its first one too if the workgroup begins here
-  const uint32_t from_slot = 2 * from + (from * total / groups >= begin ? 0 : 1);
+  const uint32_t from_slot = 2 * from + (shares.first(from) >= begin ? 0 : 1);
   const uint32_t lane = lane_id(), wave = uniform(threadIdx.x / WAVE);
   const bool shared = rows <= mine + sharers;                 // one head, all waves
   const uint32_t stride = shared ? DECODE_WAVES : 1;
