@@ -37,8 +37,9 @@
  *     untouched.
  *   - All work is enqueued on `hip_stream` (a hipStream_t passed as void*; NULL = the default
  *     stream).  Every call but fikit_gapfill_static and the attention calls of a language model
- *     service (fikit_cache_*, fikit_prompt_attention) waits until its work there is done before it returns, so outputs and the returned status are final on return, for every stream,
- *     copy and thread.
+ *     service (fikit_cache_*, fikit_prompt_attention) waits until its work there is done before it
+ *     returns, so outputs and the returned status are final on return, for every stream, copy and
+ *     thread.
  *   - Return value: FIKIT_OK or a negative fikit_status.  Nothing aborts or throws.  After an
  *     error the contents of the output buffers are unspecified.
  *   - Everything but the attention calls is integer arithmetic (nanoseconds, counts); results are exact.
@@ -540,8 +541,9 @@ size_t fikit_cache_attention_workspace_bytes(uint32_t n_requests, uint32_t q_hea
  *   max_length     no request is longer (else INVALID_ARG through d_status); how the work is cut up goes by it.
  *   d_workspace    256-byte aligned, at least fikit_cache_attention_workspace_bytes(...) bytes.
  *
- * Products and sums are held in 32 bits, weights are rounded to the queries' type before they meet the values.  With
- * FIKIT_F16 cached values are read as f16: beyond 65504 as infinite.
+ * Products and sums are held in 32 bits.  Sums are taken relative to a score that the largest one may pass by 8 binary places, and
+ * divided at the end, so they may become infinite where values are within 2^8 times their number of the largest float.  A
+ * weight meets the values as two numbers of the queries' type.  With FIKIT_F16 cached values are read as f16: beyond 65504 as infinite.
  */
 int fikit_cache_attention(const fikit_cache* h_cache, const fikit_vectors* h_q, uint32_t q_heads, int32_t value_type, float scale,
                           const int32_t* d_block_table, uint32_t table_width, const int32_t* d_lengths, uint32_t n_requests,
@@ -558,6 +560,8 @@ int fikit_cache_attention(const fikit_cache* h_cache, const fikit_vectors* h_q, 
  *   head_dim       64 or 128.
  *   d_out          [n_tokens][q_heads][head_dim], of the inputs' type; d_lse [n_tokens][q_heads] float or NULL; as in
  *                  fikit_cache_attention.
+ *
+ * Products and sums as in fikit_cache_attention, but a weight is rounded to the inputs' type before it meets the values.
  */
 int fikit_prompt_attention(const fikit_vectors* h_q, const fikit_vectors* h_k, const fikit_vectors* h_v, uint32_t q_heads,
                            uint32_t kv_heads, uint32_t head_dim, int32_t value_type, float scale, const int32_t* d_offsets,

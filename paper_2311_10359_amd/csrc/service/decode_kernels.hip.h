@@ -23,8 +23,8 @@ namespace fikit {
 // Bound by memory: a token costs 2 D bytes a key head and no more than 4 D operations for each of its query heads.  Two steps of codes are
 // in flight per wave, in registers, which is what 8 waves (16 with heads of 64) on a compute unit leave room for.  128 requests of 4096 to
 // 16,384 tokens, 8 heads of 128 (2.2 GB): 340 us, 6.5 TB/s, of the 7.2 that a kernel reaches which only reads past the caches; 64 requests
-// of 1 to 13,517 tokens, 16 heads of 64, blocks of 16 (145 MB): 31 us, 4.6 TB/s; 2 of 76,687 and 127,690, 4 heads of 128 (209 MB, half of it
-// found in the last-level cache): 38; one of 4097 (8 MB): 6.8, latency.
+// of 1 to 13,517 tokens, 16 heads of 64, blocks of 16 (145 MB): 31 us, 4.6 TB/s; 2 of 76,687 and 127,690, 4 heads of 128 (209 MB): 38, 5.4
+// TB/s; one of 4097 (8 MB): 6.8, latency.
 //
 // The work is cut evenly: with 128 tokens of a request, for one unit (key head and tile of query heads), as a chunk, and chunks in
 // the order of requests, units, tokens, workgroup b of W takes chunks b T / W .. (b + 1) T / W - 1 of all T, whatever requests they
