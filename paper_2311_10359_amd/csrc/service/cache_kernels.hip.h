@@ -278,8 +278,9 @@ __global__ __launch_bounds__(APPEND_WAVES * WAVE) void k_cache_append(AppendArgs
   const uint32_t lane = lane_id(), unit = blockIdx.y * APPEND_WAVES + uniform(threadIdx.x / WAVE), block_tokens = a.cache.block_tokens;
   const uint32_t block = static_cast<uint32_t>(piece.x), first = static_cast<uint32_t>(piece.y), at = static_cast<uint32_t>(piece.z),
                  count = static_cast<uint32_t>(piece.w);
-  if (block >= a.cache.n_blocks || at >= block_tokens || count == 0 || count > block_tokens - at || first >= a.n_tokens ||
-      count > a.n_tokens - first) {
+  const bool bad = (block >= a.cache.n_blocks) | (at >= block_tokens) | (count == 0) | (count > block_tokens - at) | (first >= a.n_tokens) |
+                   (count > a.n_tokens - first);        // (at once: what they look at is loaded together)
+  if (bad) {
     if (threadIdx.x == 0) *a.status = FIKIT_INVALID_ARG;
     return;
   }

@@ -69,7 +69,7 @@ struct DecodeLook {
 __device__ __forceinline__ bool decode_look(const DecodeArgs& a, DecodeLook* lds, uint32_t* before, uint32_t* mine, uint32_t* total) {
   const uint32_t per = (a.n_requests + DECODE_WAVES * WAVE - 1) / (DECODE_WAVES * WAVE), first = threadIdx.x * per;
   const bool stop = stopped(a.status);
-  bool ok = !stop;
+  bool ok = true;
   uint32_t sum = 0;
 #pragma unroll 4
   for (uint32_t r = first; r < min_u32(first + per, a.n_requests); ++r) {
@@ -80,7 +80,7 @@ __device__ __forceinline__ bool decode_look(const DecodeArgs& a, DecodeLook* lds
   const uint32_t run = wave_incl_scan_u32(sum);
   const uint32_t wave = threadIdx.x / WAVE;
   if (lane_id() == WAVE - 1) lds->sums[wave] = run;
-  if (!__syncthreads_and(ok)) {
+  if (!__syncthreads_and(ok & !stop)) {
     if (threadIdx.x == 0 && !stop) *a.status = FIKIT_INVALID_ARG;
     return false;
   }

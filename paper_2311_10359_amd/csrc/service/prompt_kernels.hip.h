@@ -305,10 +305,12 @@ struct PromptWave {              // what a wave holds of its 32 rows; a lane of 
 // sum over prompts of max(0, slots - L).  For more prompts, which fill the chip many times over, slot by slot from the back; prompt
 // p owns the slots from offsets[p] / rows + p on, enough for its rows and found without a list.
 constexpr uint32_t PROMPT_ORDERED = 64;
-__device__ __forceinline__ bool prompt_find(const PromptArgs& a, uint32_t rows, uint32_t item, uint32_t* start, uint32_t* length, uint32_t* first) {
+// False if the offsets cannot be; `stop`: an earlier call has failed (asked here, so that it is on its way together with the offsets).
+__device__ __forceinline__ bool prompt_find(const PromptArgs& a, uint32_t rows, uint32_t item, uint32_t* start, uint32_t* length, uint32_t* first, bool* stop) {
   if (a.n_prompts <= PROMPT_ORDERED) {
     const uint32_t lane = lane_id(), p = min_u32(lane, a.n_prompts - 1);
     const uint32_t from = static_cast<uint32_t>(a.offsets[p]), to = static_cast<uint32_t>(a.offsets[p + 1]);
+    *stop = stopped(a.status);
     const bool good = from <= to && to <= a.n_tokens;
     if (ballot(!good)) return false;
     const uint32_t slots = lane < a.n_prompts ? (to - from + rows - 1) / rows : 0;
@@ -331,6 +333,7 @@ __device__ __forceinline__ bool prompt_find(const PromptArgs& a, uint32_t rows, 
     *first = level * rows;
     return true;
   }
+  *stop = stopped(a.status);
   const uint32_t slot = a.slots - 1 - item;
   uint32_t prompt = 0;
   for (uint32_t hi = a.n_prompts; hi - prompt > 1;) {
@@ -413,20 +416,21 @@ __device__ __attribute__((noinline)) void prompt_with_care(PromptArgs a, uint32_
   w.write(a, start, length, head, keys + wave * (32 * D), vals + wave * (32 * D));
 }
 
+// Heads of 64 leave room for a third workgroup on a compute unit (4 prompts of 4096 tokens: 155 us; with two 168, with four, which spill, 171).
 template <typename T, int D, int WAVES>
-__global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs a) {
+__global__ __launch_bounds__(WAVES * WAVE, D == 64 ? 3 : 2) void k_prompt(PromptArgs a) {
   constexpr uint32_t ROWS = WAVES * PROMPT_WAVE_ROWS, TILE = PROMPT_KEYS * D * 2;
   // Keys and values of two tiles.  (Arrays of their own: the compiler sees that a tile that is read is not one that is being filled,
   // and does not wait for the latter.)
   __shared__ __align__(1024) char lds_k0[TILE], lds_k1[TILE], lds_v0[TILE], lds_v1[TILE];
   lds_char *const k0 = (lds_char*)lds_k0, *const k1 = (lds_char*)lds_k1, *const v0 = (lds_char*)lds_v0, *const v1 = (lds_char*)lds_v1;
-  const bool stop = stopped(a.status);      // (looked at below, where the offsets have arrived too)
   const uint32_t wave = uniform(threadIdx.x / WAVE);
   // neighbours in the grid go to different dies: those of one key head are kept on few of them
   const uint32_t place = blockIdx.x % a.q_heads;
   const uint32_t kv_head = place % a.kv_heads, head = kv_head * (a.q_heads / a.kv_heads) + place / a.kv_heads;
   uint32_t start, length, first;
-  if (!prompt_find(a, ROWS, blockIdx.x / a.q_heads, &start, &length, &first)) {
+  bool stop;
+  if (!prompt_find(a, ROWS, blockIdx.x / a.q_heads, &start, &length, &first, &stop)) {
     if (threadIdx.x == 0 && !stop) *a.status = FIKIT_INVALID_ARG;
     return;
   }
