@@ -172,3 +172,15 @@ def test_a_status_that_is_set_stops_it():
     status = torch.tensor([binding.FIKIT_CACHE_FULL], dtype=torch.int32, device=DEV)
     binding.fikit_prompt_attention(q, k, v, torch.tensor([0, 100], dtype=torch.int32, device=DEV), 0.1, status, out=out)
     assert (out.out == 7).all() and int(status) == binding.FIKIT_CACHE_FULL
+
+
+@pytest.mark.parametrize("lengths", [[129] * 64, [0] * 63 + [1000], [1000] + [1] * 63, list(range(0, 640, 10)), [2000, 3, 1000, 0, 0, 500, 128, 129],
+                                     [1] * 65, [300] * 70, [5] * 40 + [1500] + [7] * 40], ids=str)
+def test_every_row_is_written_whatever_the_lengths(lengths):
+    """Rows are handed out by a search over the prompts' lengths: each of them once, by the rows' place up to 64 prompts."""
+    q, k, v = inputs(3, lengths, 2, 1, 64, torch.bfloat16)
+    total = sum(lengths)
+    out = binding.Attention(torch.full((total, 2, 64), float("nan"), dtype=torch.bfloat16, device=DEV), torch.full((total, 2), float("nan"), device=DEV))
+    got = run(q, k, v, lengths, 0.125, out=out)
+    assert bool(torch.isfinite(got.out).all()) and bool(torch.isfinite(got.lse).all())
+    check(q, k, v, lengths, 0.125, got, rows=6)
