@@ -105,14 +105,16 @@ __device__ __forceinline__ uint32_t plan_find(const uint32_t* from, uint32_t lo,
   return lo;
 }
 
-// 1024 requests of a workgroup, one per thread, in LDS.
+// N requests in LDS.
+template <int N>
 struct PlanRequests {
-  uint32_t first[PLAN_THREADS];           // token at which a request begins
-  uint4 rest[PLAN_THREADS];               // cached, length, blocks and pieces of the requests before
+  uint32_t first[N];           // token at which a request begins
+  uint4 rest[N];               // cached, length, blocks and pieces of the requests before
 };
 
 // What new token t writes, whose request is one of n that begin with request r0.
-__device__ __forceinline__ void plan_token(const PlanArgs& a, const PlanRequests& lds, uint32_t r0, uint32_t n, uint32_t t) {
+template <int N>
+__device__ __forceinline__ void plan_token(const PlanArgs& a, const PlanRequests<N>& lds, uint32_t r0, uint32_t n, uint32_t t) {
   const uint32_t i = plan_find(lds.first, 0, n, t), block_tokens = 1u << a.shift;
   const uint4 rest = lds.rest[i];
   const uint32_t cached = rest.x, length = rest.y, index = t - lds.first[i];
@@ -131,29 +133,54 @@ __device__ __forceinline__ void plan_rest(const PlanArgs& a, uint32_t pieces, ui
   for (uint64_t i = static_cast<uint64_t>(pieces) + from; i < a.room; i += stride) a.pieces[i] = make_int4(-1, -1, -1, -1);
 }
 
-// Up to 1024 requests: one launch, in which every workgroup sums all of them for itself and takes 1024 tokens at a time.  256
-// requests with a new token each: 3.9 us, as an empty launch; 64 prompts of up to 4096 tokens, 36,000 in all: 4.8.
+// Up to 4096 requests: one launch, in which every workgroup sums all of them for itself, PER to a thread, and takes 1024 tokens at a
+// time.  256 requests with a new token each: 3.9 us, as an empty launch; 64 prompts of up to 4096 tokens, 36,000 in all: 4.8.  With four to a
+// thread, up to 4096, LDS holds one workgroup on a compute unit; a call for 1500 requests takes 5.9 to 6.4 us and for 4000 7.4 to 7.5, where
+// the two launches below take 9.3 to 12.5.
+constexpr int PLAN_PER = 4;
+template <int PER>
 __global__ __launch_bounds__(PLAN_THREADS) void k_plan_one(PlanArgs a) {
-  __shared__ PlanRequests requests;
+  __shared__ PlanRequests<PLAN_THREADS * PER> requests;
   __shared__ PlanScan scan;
-  const bool stop = stopped(a.status), there = threadIdx.x < a.n_requests;
-  const PlanRequest mine(a, there ? a.cached[threadIdx.x] : 0, there ? a.added[threadIdx.x] : 0);
+  const bool stop = stopped(a.status);
+  const uint32_t r0 = threadIdx.x * PER;
+  int32_t cached[PER], added[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const bool there = r0 + i < a.n_requests;
+    cached[i] = there ? a.cached[r0 + i] : 0;
+    added[i] = there ? a.added[r0 + i] : 0;
+  }
   if (stop) return;
-  PlanSums at, total;
-  const bool ok = plan_scan(PlanSums{mine.added(), mine.blocks, mine.pieces}, mine.ok, &scan, &at, &total);
+  PlanSums mine{0, 0, 0}, at, total;
+  bool all = true;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const PlanRequest r(a, cached[i], added[i]);
+    mine.tokens += r.added();
+    mine.blocks += r.blocks;
+    mine.pieces += r.pieces;
+    all &= r.ok;
+  }
+  const bool ok = plan_scan(mine, all, &scan, &at, &total);
   if (const int32_t error = plan_error(a, total, ok)) {
     if (threadIdx.x == 0) *a.status = error;
     return;
   }
-  requests.first[threadIdx.x] = static_cast<uint32_t>(at.tokens);
-  requests.rest[threadIdx.x] = make_uint4(mine.cached, mine.length, at.blocks, at.pieces);
-  if (blockIdx.x == 0) {
-    if (there) {
-      a.lengths[threadIdx.x] = static_cast<int32_t>(mine.length);
-      a.token_offsets[threadIdx.x] = static_cast<int32_t>(at.tokens);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const PlanRequest r(a, cached[i], added[i]);
+    requests.first[r0 + i] = static_cast<uint32_t>(at.tokens);
+    requests.rest[r0 + i] = make_uint4(r.cached, r.length, at.blocks, at.pieces);
+    if (blockIdx.x == 0 && r0 + i < a.n_requests) {
+      a.lengths[r0 + i] = static_cast<int32_t>(r.length);
+      a.token_offsets[r0 + i] = static_cast<int32_t>(at.tokens);
     }
-    if (threadIdx.x == 0) plan_counts(a, total);
+    at.tokens += r.added();
+    at.blocks += r.blocks;
+    at.pieces += r.pieces;
   }
+  if (blockIdx.x == 0 && threadIdx.x == 0) plan_counts(a, total);
   __syncthreads();
   const uint32_t from = blockIdx.x * PLAN_THREADS + threadIdx.x, stride = gridDim.x * PLAN_THREADS;
   for (uint64_t t = from; t < a.n_tokens; t += stride) plan_token(a, requests, 0, a.n_requests, static_cast<uint32_t>(t));
@@ -175,7 +202,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_plan_tiles(PlanArgs a) {
 // one launch in which every workgroup summed all requests took 20.)
 constexpr uint32_t PLAN_MOST_REQUESTS = PLAN_THREADS * PLAN_THREADS;
 __global__ __launch_bounds__(PLAN_THREADS) void k_plan_tokens(PlanArgs a) {
-  __shared__ PlanRequests requests;
+  __shared__ PlanRequests<PLAN_THREADS> requests;
   __shared__ uint32_t tile_tokens[PLAN_THREADS];
   __shared__ uint2 tile_rest[PLAN_THREADS];
   __shared__ PlanScan scans[2];

@@ -163,7 +163,9 @@ int fikit_cache_plan(const int32_t* d_cached, const int32_t* d_added, uint32_t n
   const dim3 block(PLAN_THREADS);
   const uint32_t of_tokens = (n_tokens + PLAN_THREADS - 1) / PLAN_THREADS, tiles = (n_requests + PLAN_THREADS - 1) / PLAN_THREADS;
   const uint32_t groups = of_tokens < PLAN_GROUPS ? of_tokens : PLAN_GROUPS;
-  if (n_requests <= PLAN_THREADS) return enqueue(k_plan_one, dim3(groups < 1 ? 1 : groups), block, st, a);
+  const dim3 one(groups < 1 ? 1 : groups);
+  if (n_requests <= PLAN_THREADS) return enqueue(k_plan_one<1>, one, block, st, a);
+  if (n_requests <= PLAN_THREADS * PLAN_PER) return enqueue(k_plan_one<PLAN_PER>, one, block, st, a);
   if (int rc = enqueue(k_plan_tiles, dim3(tiles), block, st, a)) return rc;
   return enqueue(k_plan_tokens, dim3(tiles + groups), block, st, a);
 }
