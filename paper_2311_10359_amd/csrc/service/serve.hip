@@ -118,6 +118,7 @@ uint64_t fikit_cache_pieces(uint32_t n_tokens, uint32_t n_requests, uint32_t blo
   return cut < n_tokens ? cut : n_tokens;
 }
 
+// (Asked for from 1025 requests on, read and written beyond 4096: which kernels take how many is no part of the interface.)
 size_t fikit_cache_plan_workspace_bytes(uint32_t n_requests) {
   return n_requests <= PLAN_THREADS ? 0 : ((static_cast<size_t>(n_requests) + PLAN_THREADS - 1) / PLAN_THREADS * sizeof(PlanTile) + 255) / 256 * 256;
 }
