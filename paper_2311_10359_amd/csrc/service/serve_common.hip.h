@@ -28,7 +28,6 @@ __device__ __forceinline__ To bits_as(From v) {
 
 // A 16-bit value type.  `x8`: eight values, an operand of a matrix instruction.  `pair`: two 32-bit values rounded to nearest
 // even.  `codes<hi>`: two E4M3 codes, the low or the high ones of a word, times a power of two (exact, see fikit.h).
-// `add_pair`: a sum and a pair's two values.
 // `codes_of_pairs`: the codes of four finite values divided by a power of two, at most 448 then.
 struct Bf16 {
   typedef bf16x8 x8;
@@ -48,9 +47,6 @@ struct Bf16 {
     s16x2 w = {0, 0};
     w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, bits_as<bf16x2>(a), scale, false);
     return bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, bits_as<bf16x2>(b), scale, true));
-  }
-  static __device__ __forceinline__ float add_pair(uint32_t v, float sum) {
-    return __builtin_amdgcn_fdot2_f32_bf16(bits_as<bf16x2>(v), bits_as<bf16x2>(ONE | ONE << 16), sum, false);
   }
   static __device__ __forceinline__ f32x4 mfma16(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ f32x16 mfma32(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
@@ -75,9 +71,6 @@ struct F16 {
     s16x2 w = {0, 0};
     w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(w, bits_as<f16x2>(a), scale, false);
     return bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_fp8_f16(w, bits_as<f16x2>(b), scale, true));
-  }
-  static __device__ __forceinline__ float add_pair(uint32_t v, float sum) {
-    return __builtin_amdgcn_fdot2(bits_as<f16x2>(v), bits_as<f16x2>(ONE | ONE << 16), sum, false);
   }
   static __device__ __forceinline__ f32x4 mfma16(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ f32x16 mfma32(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
