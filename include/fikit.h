@@ -543,7 +543,7 @@ size_t fikit_cache_attention_workspace_bytes(uint32_t n_requests, uint32_t q_hea
  *
  * Products and sums are held in 32 bits.  Sums are taken relative to a score that the largest one may pass by 8 binary places, and
  * divided at the end, so they may become infinite where values are within 2^8 times their number of the largest float.  A
- * weight meets the values as two numbers of the queries' type.  With FIKIT_F16 cached values are read as f16: beyond 65504 as infinite.
+ * weight meets the values as two bfloat16 numbers, whatever the queries' type; the cache's whole range counts with either type.
  */
 int fikit_cache_attention(const fikit_cache* h_cache, const fikit_vectors* h_q, uint32_t q_heads, int32_t value_type, float scale,
                           const int32_t* d_block_table, uint32_t table_width, const int32_t* d_lengths, uint32_t n_requests,

@@ -17,8 +17,10 @@ namespace fikit {
 //            bits would cost as much as rounding the output; what it leaves is a second operand, which costs nothing here: the
 //            matrix unit is busy for an eighth of the time.
 //
-// Codes become 16-bit values, scale included, in one instruction for two; nothing goes through LDS but the joining of
-// the waves' results.
+// Codes become 16-bit values in one instruction for two; nothing goes through LDS but the joining of the waves' results.  No 16-bit type
+// may cut the cache's range: codes without their scale are exact in either type, so keys become values of the queries' type and the
+// scale meets the score, in 32 bits; values become bfloat16, which holds them with their scale, whatever the queries' type (in
+// float16 the largest float16 values, 65,536 in the cache, would be infinite), and so do the weights, 16 bits of them in two operands.
 //
 // Bound by memory: a token costs 2 D bytes a key head and no more than 4 D operations for each of its query heads.  Two steps of codes are
 // in flight per wave, in registers, which is what 8 waves (16 with heads of 64) on a compute unit leave room for.  128 requests of 4096 to
@@ -338,13 +340,13 @@ __global__ __launch_bounds__(DECODE_WAVES * WAVE, D == 128 ? 2 : 4) void k_decod
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const uint32_t codes = x.k[h][j / 2][(j & 1) * 2 + i];
-            w[2 * i] = T::template codes<false>(codes, k_up);
-            w[2 * i + 1] = T::template codes<true>(codes, k_up);
+            w[2 * i] = T::template codes<false>(codes, 1.f);
+            w[2 * i + 1] = T::template codes<true>(codes, 1.f);
           }
           c = T::mfma16(bits_as<typename T::x8>(w), q[j], c);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[4 * h + i] = c[i] * scale;
+        for (int i = 0; i < 4; ++i) s[4 * h + i] = c[i] * k_up * scale;
       }
       if (ahead < end) load_keys(ahead, x);
       if (token + DECODE_STEP > end) {     // what lies behind the last token counts for nothing, whatever it is
@@ -357,10 +359,10 @@ __global__ __launch_bounds__(DECODE_WAVES * WAVE, D == 128 ? 2 : 4) void k_decod
           }
       }
       float most = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-      if (ballot(most > m + (DECODE_SLACK + T::WEIGHT_BIAS))) {
+      if (ballot(most > m + DECODE_SLACK)) {
         most = fmaxf(most, __shfl_xor(most, 16, WAVE));
         most = fmaxf(most, __shfl_xor(most, 32, WAVE));
-        const float raised = fmaxf(m, most - T::WEIGHT_BIAS);
+        const float raised = fmaxf(m, most);
         const float down = raised > -__builtin_huge_valf() ? exp2_fast(m - raised) : 1.f;
         m = raised;
         l *= down;
@@ -373,10 +375,10 @@ __global__ __launch_bounds__(DECODE_WAVES * WAVE, D == 128 ? 2 : 4) void k_decod
       for (int i = 0; i < 4; ++i) {
         const float p = exp2_fast(s[2 * i] - origin), r = exp2_fast(s[2 * i + 1] - origin);
         l += p + r;
-        w[i] = T::pair(p, r);
-        rest[i] = T::pair(p - T::low(w[i]), r - T::high(w[i]));
+        w[i] = Bf16::pair(p, r);
+        rest[i] = Bf16::pair(p - Bf16::low(w[i]), r - Bf16::high(w[i]));
       }
-      const typename T::x8 weights = bits_as<typename T::x8>(w);
+      const Bf16::x8 weights = bits_as<Bf16::x8>(w);
 #pragma unroll
       for (int j = 0; j < KV_WORDS; ++j) {
         u32x4 y[4];       // operands of four tiles of dimensions
@@ -385,15 +387,15 @@ __global__ __launch_bounds__(DECODE_WAVES * WAVE, D == 128 ? 2 : 4) void k_decod
           // bytes of two tokens side by side: dimensions 0 and 1, 2 and 3
           const uint32_t lo = __builtin_amdgcn_perm(x.v[2 * i + 1][j], x.v[2 * i][j], 0x05010400u);
           const uint32_t hi = __builtin_amdgcn_perm(x.v[2 * i + 1][j], x.v[2 * i][j], 0x07030602u);
-          y[0][i] = T::template codes<false>(lo, up[i / 2]);
-          y[1][i] = T::template codes<true>(lo, up[i / 2]);
-          y[2][i] = T::template codes<false>(hi, up[i / 2]);
-          y[3][i] = T::template codes<true>(hi, up[i / 2]);
+          y[0][i] = Bf16::codes<false>(lo, up[i / 2]);
+          y[1][i] = Bf16::codes<true>(lo, up[i / 2]);
+          y[2][i] = Bf16::codes<false>(hi, up[i / 2]);
+          y[3][i] = Bf16::codes<true>(hi, up[i / 2]);
         }
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-          acc[4 * j + t] = T::mfma16(bits_as<typename T::x8>(y[t]), weights, acc[4 * j + t]);
-          acc[4 * j + t] = T::mfma16(bits_as<typename T::x8>(y[t]), bits_as<typename T::x8>(rest), acc[4 * j + t]);
+          acc[4 * j + t] = Bf16::mfma16(bits_as<Bf16::x8>(y[t]), weights, acc[4 * j + t]);
+          acc[4 * j + t] = Bf16::mfma16(bits_as<Bf16::x8>(y[t]), bits_as<Bf16::x8>(rest), acc[4 * j + t]);
         }
       }
       if (ahead < end) load_values(ahead, x);

@@ -27,7 +27,7 @@ __device__ __forceinline__ To bits_as(From v) {
 }
 
 // A 16-bit value type.  `x8`: eight values, an operand of a matrix instruction.  `pair`: two 32-bit values rounded to nearest
-// even.  `codes<hi>`: two E4M3 codes, the low or the high ones of a word, times a power of two (exact, see fikit.h).
+// even.  `codes<hi>`: two E4M3 codes, the low or the high ones of a word, times a power of two (exact in the type's range).
 // `codes_of_pairs`: the codes of four finite values divided by a power of two, at most 448 then.
 struct Bf16 {
   typedef bf16x8 x8;
