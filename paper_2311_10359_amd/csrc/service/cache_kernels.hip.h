@@ -63,31 +63,37 @@ struct PlanSums {
 struct PlanScan {
   uint32_t blocks[PLAN_THREADS / WAVE], pieces[PLAN_THREADS / WAVE];
   uint64_t tokens[PLAN_THREADS / WAVE];
+  uint32_t flags[PLAN_THREADS / WAVE];
 };
 
-// The sums of the threads before, and of all of them, in a workgroup of PLAN_THREADS; whether `ok` holds in all.
-__device__ __forceinline__ bool plan_scan(const PlanSums& mine, bool ok, PlanScan* lds, PlanSums* before, PlanSums* total) {
+// The sums of the threads before, and of all of them, in a workgroup of PLAN_THREADS; which of the flags any thread has.
+// (What a wave knows and the others may not, a status that another workgroup has just written among it, is a flag: the workgroup
+// goes on or ends as a whole, and no wave's sums are missing.)
+constexpr uint32_t PLAN_CANNOT_BE = 1, PLAN_STOP = 2;
+__device__ __forceinline__ uint32_t plan_scan(const PlanSums& mine, uint32_t flags, PlanScan* lds, PlanSums* before, PlanSums* total) {
   constexpr uint32_t WAVES = PLAN_THREADS / WAVE;
   const uint64_t run_tokens = wave_incl_scan_u64(mine.tokens);
   const uint32_t run_blocks = wave_incl_scan_u32(mine.blocks), run_pieces = wave_incl_scan_u32(mine.pieces);
   const uint32_t wave = uniform(threadIdx.x / WAVE), lane = lane_id();
-  if (lane == WAVE - 1) { lds->tokens[wave] = run_tokens; lds->blocks[wave] = run_blocks; lds->pieces[wave] = run_pieces; }
-  const bool all = __syncthreads_and(ok);
+  const uint32_t any = (ballot(flags & PLAN_CANNOT_BE) ? PLAN_CANNOT_BE : 0) | (ballot(flags & PLAN_STOP) ? PLAN_STOP : 0);
+  if (lane == WAVE - 1) { lds->tokens[wave] = run_tokens; lds->blocks[wave] = run_blocks; lds->pieces[wave] = run_pieces; lds->flags[wave] = any; }
+  __syncthreads();
   // each wave scans the waves' sums
   const bool there = lane < WAVES;
   const uint64_t tokens = there ? lds->tokens[lane % WAVES] : 0;
   const uint32_t blocks = there ? lds->blocks[lane % WAVES] : 0, pieces = there ? lds->pieces[lane % WAVES] : 0;
+  const uint32_t theirs = there ? lds->flags[lane % WAVES] : 0;
   const uint64_t upto = wave_incl_scan_u64(tokens);
   const uint32_t upto_blocks = wave_incl_scan_u32(blocks), upto_pieces = wave_incl_scan_u32(pieces);
   *total = PlanSums{read_lane_u64(upto, WAVES - 1), read_lane_u32(upto_blocks, WAVES - 1), read_lane_u32(upto_pieces, WAVES - 1)};
   *before = PlanSums{read_lane_u64(upto - tokens, wave) + run_tokens - mine.tokens, read_lane_u32(upto_blocks - blocks, wave) + run_blocks - mine.blocks,
                      read_lane_u32(upto_pieces - pieces, wave) + run_pieces - mine.pieces};
-  return all;
+  return (ballot(theirs & PLAN_CANNOT_BE) ? PLAN_CANNOT_BE : 0) | (ballot(theirs & PLAN_STOP) ? PLAN_STOP : 0);
 }
 
 // (blocks and pieces are at most as many as tokens)
-__device__ __forceinline__ int32_t plan_error(const PlanArgs& a, const PlanSums& total, bool ok) {
-  return !ok || total.tokens != a.n_tokens ? FIKIT_INVALID_ARG : total.blocks > a.n_free ? FIKIT_CACHE_FULL : FIKIT_OK;
+__device__ __forceinline__ int32_t plan_error(const PlanArgs& a, const PlanSums& total, uint32_t flags) {
+  return (flags & PLAN_CANNOT_BE) || total.tokens != a.n_tokens ? FIKIT_INVALID_ARG : total.blocks > a.n_free ? FIKIT_CACHE_FULL : FIKIT_OK;
 }
 
 __device__ __forceinline__ void plan_counts(const PlanArgs& a, const PlanSums& total) {
@@ -151,7 +157,6 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_plan_one(PlanArgs a) {
     cached[i] = there ? a.cached[r0 + i] : 0;
     added[i] = there ? a.added[r0 + i] : 0;
   }
-  if (stop) return;
   PlanSums mine{0, 0, 0}, at, total;
   bool all = true;
 #pragma unroll
@@ -162,8 +167,9 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_plan_one(PlanArgs a) {
     mine.pieces += r.pieces;
     all &= r.ok;
   }
-  const bool ok = plan_scan(mine, all, &scan, &at, &total);
-  if (const int32_t error = plan_error(a, total, ok)) {
+  const uint32_t flags = plan_scan(mine, (all ? 0 : PLAN_CANNOT_BE) | (stop ? PLAN_STOP : 0), &scan, &at, &total);
+  if (flags & PLAN_STOP) return;
+  if (const int32_t error = plan_error(a, total, flags)) {
     if (threadIdx.x == 0) *a.status = error;
     return;
   }
@@ -194,8 +200,8 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_plan_tiles(PlanArgs a) {
   const bool there = r < a.n_requests;
   const PlanRequest mine(a, there ? a.cached[r] : 0, there ? a.added[r] : 0);
   PlanSums at, total;
-  const bool ok = plan_scan(PlanSums{mine.added(), mine.blocks, mine.pieces}, mine.ok, &scan, &at, &total);
-  if (threadIdx.x == 0) a.tiles[blockIdx.x] = PlanTile{ok ? total.tokens : PLAN_BAD, total.blocks, total.pieces};
+  const uint32_t flags = plan_scan(PlanSums{mine.added(), mine.blocks, mine.pieces}, mine.ok ? 0 : PLAN_CANNOT_BE, &scan, &at, &total);
+  if (threadIdx.x == 0) a.tiles[blockIdx.x] = PlanTile{flags ? PLAN_BAD : total.tokens, total.blocks, total.pieces};
 }
 
 // ... then every workgroup sums the up to 1024 tiles, and of those that hold its tokens the requests.  (16,384 requests, 3 MB: 3.3 and 11.7 us;
@@ -210,10 +216,11 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_plan_tokens(PlanArgs a) {
   const bool stop = stopped(a.status);
   PlanTile tile{0, 0, 0};
   if (threadIdx.x < n_tiles) tile = a.tiles[threadIdx.x];
-  if (stop) return;
   PlanSums at, total;
-  const bool ok = plan_scan(PlanSums{tile.tokens, tile.blocks, tile.pieces}, tile.tokens < PLAN_BAD, &scans[0], &at, &total);
-  if (const int32_t error = plan_error(a, total, ok)) {
+  const uint32_t mine = (tile.tokens < PLAN_BAD ? 0 : PLAN_CANNOT_BE) | (stop ? PLAN_STOP : 0);
+  const uint32_t flags = plan_scan(PlanSums{tile.tokens, tile.blocks, tile.pieces}, mine, &scans[0], &at, &total);
+  if (flags & PLAN_STOP) return;
+  if (const int32_t error = plan_error(a, total, flags)) {
     if (threadIdx.x == 0) *a.status = error;
     return;
   }
@@ -229,7 +236,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_plan_tokens(PlanArgs a) {
     const bool there = r < a.n_requests;
     const PlanRequest mine(a, there ? a.cached[r] : 0, there ? a.added[r] : 0);
     PlanSums before, all;
-    plan_scan(PlanSums{mine.added(), mine.blocks, mine.pieces}, true, &scans[turn], &before, &all);
+    plan_scan(PlanSums{mine.added(), mine.blocks, mine.pieces}, 0, &scans[turn], &before, &all);
     requests.first[threadIdx.x] = tile_tokens[i] + static_cast<uint32_t>(before.tokens);
     requests.rest[threadIdx.x] = make_uint4(mine.cached, mine.length, tile_rest[i].x + before.blocks, tile_rest[i].y + before.pieces);
     __syncthreads();
