@@ -308,7 +308,7 @@ template <typename T, int D>
 __global__ __launch_bounds__(APPEND_WAVES * WAVE) void k_cache_append(AppendArgs a) {
   const int4 piece = a.pieces[blockIdx.x];
   const bool stop = stopped(a.status);
-  if (piece.x == -1 || stop) return;
+  if ((piece.x & piece.y & piece.z & piece.w) == -1 || stop) return;      // (all four are -1: not used)
   const uint32_t lane = lane_id(), unit = blockIdx.y * APPEND_WAVES + uniform(threadIdx.x / WAVE), block_tokens = a.cache.block_tokens;
   const uint32_t block = static_cast<uint32_t>(piece.x), first = static_cast<uint32_t>(piece.y), at = static_cast<uint32_t>(piece.z),
                  count = static_cast<uint32_t>(piece.w);
