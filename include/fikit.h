@@ -515,6 +515,8 @@ int fikit_cache_plan(const int32_t* d_cached, const int32_t* d_added, uint32_t n
  * to even), NaN for what is not finite.  Where the exponent of a block with earlier tokens grows, their codes are rounded again
  * to the new scale.  Codes behind the piece are left as they are.
  *
+ * n_pieces up to 2^24 - 1 (UNSUPPORTED beyond).
+ *
  * Through d_status: INVALID_ARG for a piece outside the block, the cache or the tokens.
  */
 int fikit_cache_append(const fikit_cache* h_cache, const fikit_vectors* h_k, const fikit_vectors* h_v, uint32_t n_tokens,
@@ -558,6 +560,7 @@ int fikit_cache_attention(const fikit_cache* h_cache, const fikit_vectors* h_q, 
  *   h_q, h_k, h_v  vectors of q_heads, kv_heads and kv_heads heads; q_heads a multiple of kv_heads; keys and values of
  *                  token strides up to 2^24.
  *   head_dim       64 or 128.
+ *   n_prompts      (n_tokens / 128 + n_prompts) * q_heads up to 2^24 - 1 (UNSUPPORTED beyond).
  *   d_out          [n_tokens][q_heads][head_dim], of the inputs' type; d_lse [n_tokens][q_heads] float or NULL; as in
  *                  fikit_cache_attention.
  *

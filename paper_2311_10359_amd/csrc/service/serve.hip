@@ -15,7 +15,7 @@ using namespace fikit;
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 constexpr uint32_t PLAN_GROUPS = 512;             // two for each CU
-constexpr uint64_t MOST_GROUPS = 0x7fffffffull;   // workgroups of a launch
+constexpr uint64_t MOST_GROUPS = 0xffffffull;     // workgroups of 256 threads of a launch, whose threads number less than 2^32
 
 template <typename... P, typename... A>
 int enqueue(void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t st, A... args) {
@@ -49,6 +49,7 @@ int with_types(int32_t value_type, uint32_t head_dim, F f) {
 
 bool type_ok(int32_t value_type) { return value_type == FIKIT_BF16 || value_type == FIKIT_F16; }
 
+static_assert(APPEND_WAVES * WAVE == 256, "threads of MOST_GROUPS");
 struct AppendCall {
   const AppendArgs& a;
   uint32_t n_pieces;
@@ -100,6 +101,7 @@ struct DecodeCall {
 // values half as often, and lose that again by waiting together (24 prompts of up to 2048 tokens: 113 us against 95 at the time; 64 of 500: 197 against 156;
 // one of 8192: 491 against 493).
 constexpr int PROMPT_WAVES = 4;
+static_assert(PROMPT_WAVES * WAVE == 256, "threads of MOST_GROUPS");
 struct PromptCall {
   const PromptArgs& a;
   uint32_t groups;
@@ -176,9 +178,10 @@ int fikit_cache_append(const fikit_cache* h_cache, const fikit_vectors* h_k, con
                        void* hip_stream) {
   if (int rc = cache_status(h_cache)) return rc;
   if (!type_ok(value_type) || !d_status || !aligned(d_status, 4) || !aligned(d_pieces, 16)) return FIKIT_INVALID_ARG;
-  if (n_tokens > 0x7fffffffu || n_pieces > MOST_GROUPS) return FIKIT_INVALID_ARG;
+  if (n_tokens > 0x7fffffffu || n_pieces > 0x7fffffffu) return FIKIT_INVALID_ARG;
   if (n_pieces == 0) return FIKIT_OK;
   if (!d_pieces || !vectors_ok(h_k) || !vectors_ok(h_v)) return FIKIT_INVALID_ARG;
+  if (n_pieces > MOST_GROUPS) return FIKIT_UNSUPPORTED;
   AppendArgs a{};
   a.cache = *h_cache;
   a.k = *h_k;

@@ -1,0 +1,19 @@
+"""Limits of the attention calls and how they are told, without a GPU: what is refused here is refused before any HIP call."""
+import pytest
+
+from paper_2311_10359_amd import binding
+from test_serve_refusals import FAKE, append, vectors
+
+UNSUPPORTED = binding.FIKIT_UNSUPPORTED
+MOST = (1 << 24) - 1          # workgroups of 256 threads of a launch, which may have fewer than 2^32 threads
+
+
+def prompt(prompts, tokens, q_heads):
+    return binding.load().fikit_prompt_attention(vectors(), vectors(), vectors(), q_heads, 1, 64, 0, 0.1, FAKE, prompts, tokens, FAKE + 4096, None, FAKE, None)
+
+
+def test_more_workgroups_than_a_launch_takes():
+    assert prompt(262144, 262144, 64) == UNSUPPORTED                  # one-token prompts: 262,144 + 2048 times 64
+    assert prompt(MOST + 1, 1, 1) == UNSUPPORTED and prompt(1, MOST, 256) == UNSUPPORTED
+    assert append(n_tokens=1 << 30, n_pieces=MOST + 1) == UNSUPPORTED
+    assert append(n_tokens=1 << 30, n_pieces=(1 << 31) - 1) == UNSUPPORTED
