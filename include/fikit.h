@@ -105,7 +105,9 @@ typedef enum fikit_status {
   FIKIT_HIP_ERROR = -6,           /* the HIP runtime reported an error, or a bounded wait ran out
                                      (fikit_set_wait_limit)                                      */
   FIKIT_UNSUPPORTED = -7,         /* fikit_prio_fill: a scenario whose list entries and launches
-                                     together number 2^32 or more                                 */
+                                     together number 2^32 or more; fikit_cache_*,
+                                     fikit_prompt_attention: sizes beyond those they state (head
+                                     and block sizes, heads, requests, prompts, pieces)            */
   FIKIT_TOO_LARGE = -8,           /* fikit_gapfill_static: more launches or tasks than its built-in
                                      scratch buffer holds                                          */
   FIKIT_CACHE_FULL = -9           /* fikit_cache_plan: more blocks needed than are free             */

@@ -418,7 +418,7 @@ const char* fikit_status_string(int status) {
     case FIKIT_BAD_RECORD: return "record with end_ns < start_ns";
     case FIKIT_UNKNOWN_ID: return "launch ID missing from its task's profile";
     case FIKIT_HIP_ERROR: return "HIP runtime error";
-    case FIKIT_UNSUPPORTED: return "beyond a stated limit of this call (list entries and launches of a scenario number 2^32 or more)";
+    case FIKIT_UNSUPPORTED: return "beyond a stated limit of this call, or a size or form that it does not take";
     case FIKIT_TOO_LARGE: return "input larger than the built-in scratch buffer of fikit_gapfill_static";
     case FIKIT_CACHE_FULL: return "more cache blocks needed than are free";
     default: return "unknown status";

@@ -17,3 +17,9 @@ def test_more_workgroups_than_a_launch_takes():
     assert prompt(MOST + 1, 1, 1) == UNSUPPORTED and prompt(1, MOST, 256) == UNSUPPORTED
     assert append(n_tokens=1 << 30, n_pieces=MOST + 1) == UNSUPPORTED
     assert append(n_tokens=1 << 30, n_pieces=(1 << 31) - 1) == UNSUPPORTED
+
+
+def test_what_unsupported_is_called():
+    """The calls that return it take different things: its text fits all of them."""
+    text = binding.status_string(UNSUPPORTED)
+    assert "limit" in text and "size" in text and "scenario" not in text
