@@ -498,6 +498,8 @@ size_t fikit_cache_plan_workspace_bytes(uint32_t n_requests);
  *   d_slots          [n_tokens] receives where each new token goes, block * block_tokens + place in the block.  May be NULL.
  *   d_pieces         [fikit_cache_pieces(...)] receives the pieces, in order; the rest is filled with -1.
  *   d_counts         [2] receives the number of blocks taken and of pieces.
+ *                    Outputs may not overlap each other, d_cached, d_added or d_free (INVALID_ARG): every workgroup reads
+ *                    the requests while others write, so lengths are copied back behind the call and not updated in place.
  *   d_workspace      256-byte aligned, at least fikit_cache_plan_workspace_bytes(n_requests) bytes.
  *
  * Through d_status: INVALID_ARG (also: a request longer than its row of the table or than 2^31 - 1), CACHE_FULL if n_free blocks

@@ -641,7 +641,8 @@ def fikit_cache_plan(cached: torch.Tensor, added: torch.Tensor, n_tokens: int, b
                      free_blocks: torch.Tensor, status: torch.Tensor, *, want_slots: bool = True, out: Optional[CachePlan] = None,
                      workspace_buf: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> CachePlan:
     """cached, added: int32 [R]; n_tokens = sum of added; block_table: int32 [R, width], receives the new blocks;
-    free_blocks: int32 [F].  Output tensors are allocated unless given."""
+    free_blocks: int32 [F].  Output tensors are allocated unless given, and then overlap neither each other nor what is read (`cached`
+    is not updated in place)."""
     context = _elsewhere(stream, cached.device)
     if context is not None:
         with context:

@@ -24,6 +24,15 @@ int enqueue(void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t st, A... ar
   return hipGetLastError() == hipSuccess ? FIKIT_OK : FIKIT_HIP_ERROR;
 }
 
+struct Extent {
+  const void* begin;
+  uint64_t bytes;
+};
+bool overlap(const Extent& a, const Extent& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.begin), y = reinterpret_cast<uintptr_t>(b.begin);
+  return a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
+}
+
 constexpr uint64_t MOST_STRIDE = 1ull << 24;      // of a token, in values: places within a tile are 32-bit numbers of bytes
 
 bool vectors_ok(const fikit_vectors* v) {
@@ -144,6 +153,14 @@ int fikit_cache_plan(const int32_t* d_cached, const int32_t* d_added, uint32_t n
     if (!d_workspace || !aligned(d_workspace, 256)) return FIKIT_INVALID_ARG;
     if (workspace_bytes < need) return FIKIT_WORKSPACE_TOO_SMALL;
   }
+  const uint64_t room = fikit_cache_pieces(n_tokens, n_requests, block_tokens);
+  // (outputs, then what every workgroup reads while others write)
+  const Extent extents[] = {{d_lengths, 4ull * n_requests}, {d_token_offsets, 4ull * n_requests + 4}, {d_slots, d_slots ? 8ull * n_tokens : 0},
+                            {d_pieces, sizeof(fikit_piece) * room}, {d_counts, 8}, {d_cached, 4ull * n_requests}, {d_added, 4ull * n_requests},
+                            {d_free, 4ull * n_free}};
+  for (int out = 0; out < 5; ++out)
+    for (int other = out + 1; other < 8; ++other)
+      if (overlap(extents[out], extents[other])) return FIKIT_INVALID_ARG;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   PlanArgs a{};
   a.cached = d_cached;
@@ -161,7 +178,7 @@ int fikit_cache_plan(const int32_t* d_cached, const int32_t* d_added, uint32_t n
   a.n_tokens = n_tokens;
   a.table_width = table_width;
   a.n_free = n_free;
-  a.room = static_cast<uint32_t>(fikit_cache_pieces(n_tokens, n_requests, block_tokens));
+  a.room = static_cast<uint32_t>(room);
   a.shift = static_cast<uint32_t>(__builtin_ctz(block_tokens));
   const dim3 block(PLAN_THREADS);
   const uint32_t of_tokens = (n_tokens + PLAN_THREADS - 1) / PLAN_THREADS, tiles = (n_requests + PLAN_THREADS - 1) / PLAN_THREADS;

@@ -2,7 +2,7 @@
 import pytest
 
 from paper_2311_10359_amd import binding
-from test_serve_refusals import FAKE, append, vectors
+from test_serve_refusals import FAKE, append, plan, vectors
 
 UNSUPPORTED = binding.FIKIT_UNSUPPORTED
 MOST = (1 << 24) - 1          # workgroups of 256 threads of a launch, which may have fewer than 2^32 threads
@@ -23,3 +23,19 @@ def test_what_unsupported_is_called():
     """The calls that return it take different things: its text fits all of them."""
     text = binding.status_string(UNSUPPORTED)
     assert "limit" in text and "size" in text and "scenario" not in text
+
+
+def apart():
+    """Arguments of a plan of 4 requests and 9 tokens, each in memory of its own."""
+    names = ("cached", "added", "table", "free", "lengths", "offsets", "slots", "pieces", "counts", "status", "ws")
+    return {name: FAKE + 4096 * i for i, name in enumerate(names)}
+
+
+@pytest.mark.parametrize("output, at", [("lengths", "cached"), ("lengths", "added"), ("offsets", "cached"), ("offsets", "added"), ("counts", "cached"),
+                                        ("counts", "free"), ("slots", "added"), ("pieces", "free"), ("lengths", "offsets"), ("pieces", "slots")])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_outputs_of_a_plan_over_what_it_reads(output, at, shift):
+    """Every workgroup reads the requests while the first one writes: in place there would be a race."""
+    a = apart()
+    a[output] = a[at] + 16 * shift if output == "pieces" or shift == 0 else a[at] + 8
+    assert plan(**a) == binding.FIKIT_INVALID_ARG
