@@ -566,7 +566,7 @@ int fikit_cache_attention(const fikit_cache* h_cache, const fikit_vectors* h_q, 
  *   head_dim       64 or 128.
  *   n_prompts      (n_tokens / 128 + n_prompts) * q_heads up to 2^24 - 1 (UNSUPPORTED beyond).
  *   d_out          [n_tokens][q_heads][head_dim], of the inputs' type; d_lse [n_tokens][q_heads] float or NULL; as in
- *                  fikit_cache_attention.
+ *                  fikit_cache_attention.  Neither may overlap the inputs (INVALID_ARG where d_out begins with one).
  *
  * Products and sums as in fikit_cache_attention, but a weight is rounded to the inputs' type before it meets the values.
  */

@@ -268,6 +268,8 @@ int fikit_prompt_attention(const fikit_vectors* h_q, const fikit_vectors* h_k, c
       !aligned(d_lse, 4))
     return FIKIT_INVALID_ARG;
   if (h_k->token_stride > MOST_STRIDE || h_v->token_stride > MOST_STRIDE) return FIKIT_UNSUPPORTED;
+  // (rows are read again where values are not finite, after they have been written)
+  if (d_out == h_q->d_data || d_out == h_k->d_data || d_out == h_v->d_data) return FIKIT_INVALID_ARG;
   const uint64_t slots = n_tokens / (PROMPT_WAVES * PROMPT_WAVE_ROWS) + static_cast<uint64_t>(n_prompts);
   if (slots * q_heads > MOST_GROUPS) return FIKIT_UNSUPPORTED;
   PromptArgs a{};

@@ -39,3 +39,11 @@ def test_outputs_of_a_plan_over_what_it_reads(output, at, shift):
     a = apart()
     a[output] = a[at] + 16 * shift if output == "pieces" or shift == 0 else a[at] + 8
     assert plan(**a) == binding.FIKIT_INVALID_ARG
+
+
+def test_a_prompts_output_over_its_inputs():
+    """Rows with values that are not finite are done again, from the queries."""
+    q, k, v, offsets, status = (FAKE + 4096 * i for i in range(5))
+    for out in (q, k, v):
+        assert binding.load().fikit_prompt_attention(vectors(q), vectors(k), vectors(v), 4, 2, 64, 0, 0.1, offsets, 2, 9, out, None, status,
+                                                     None) == binding.FIKIT_INVALID_ARG
