@@ -212,6 +212,7 @@ int fikit_cache_append(const fikit_cache* h_cache, const fikit_vectors* h_k, con
 size_t fikit_cache_attention_workspace_bytes(uint32_t n_requests, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim,
                                              uint32_t max_length) {
   if (kv_heads == 0 || q_heads == 0 || q_heads % kv_heads || q_heads > 65535 || max_length > 0x7fffffffu || n_requests > 0x7fffffffu) return 0;
+  if (head_dim != 64 && head_dim != 128) return 0;
   const DecodeCut c = decode_cut(n_requests, q_heads, kv_heads, head_dim, max_length);
   return c.fits ? static_cast<size_t>(c.bytes) : 0;
 }

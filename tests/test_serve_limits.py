@@ -47,3 +47,8 @@ def test_a_prompts_output_over_its_inputs():
     for out in (q, k, v):
         assert binding.load().fikit_prompt_attention(vectors(q), vectors(k), vectors(v), 4, 2, 64, 0, 0.1, offsets, 2, 9, out, None, status,
                                                      None) == binding.FIKIT_INVALID_ARG
+
+
+@pytest.mark.parametrize("dim", [0, 32, 80, 96, 256])
+def test_no_workspace_for_head_sizes_that_are_not_taken(dim):
+    assert binding.fikit_cache_attention_workspace_bytes(1, 8, 8, dim, 100000) == 0
