@@ -41,6 +41,12 @@ uint32_t count(int64_t n, const char* what) {
 }
 uint32_t count(PyObject* o, const char* what) { return count(THPUtils_unpackLong(o), what); }
 
+bool truth(PyObject* o) {
+  const int is = PyObject_IsTrue(o);
+  if (is < 0) throw python_error();
+  return is;
+}
+
 int32_t value_type(const at::Tensor& t, const char* what) {
   TORCH_CHECK_VALUE(t.scalar_type() == at::kBFloat16 || t.scalar_type() == at::kHalf, what, ": bfloat16 or float16");
   return t.scalar_type() == at::kBFloat16 ? FIKIT_BF16 : FIKIT_F16;
@@ -101,14 +107,15 @@ PyObject* py_cache_plan(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   const uint32_t n = count(cached.numel(), "cached"), n_tokens = count(a[2], "n_tokens"), block_tokens = count(a[3], "block_tokens");
   TORCH_CHECK_VALUE(added.numel() == n && table.dim() == 2 && table.size(0) == n, "cached, added: [R]; block_table: [R, width]");
   TORCH_CHECK_VALUE(status.numel() == 1, "status: [1]");
+  const bool want_slots = truth(a[7]);
   const int64_t room = static_cast<int64_t>(cache_pieces(n_tokens, n, block_tokens));
   const auto i32 = at::TensorOptions().dtype(at::kInt).device(device);
   at::Tensor lengths, offsets, slots, pieces, counts;
   if (a[8] == Py_None) {
     // one allocation: slots (two words each), pieces, lengths, places, counts
-    const int64_t of_pieces = a[7] == Py_True ? (2 * static_cast<int64_t>(n_tokens) + 3) / 4 * 4 : 0, of_lengths = of_pieces + 4 * room;
+    const int64_t of_pieces = want_slots ? (2 * static_cast<int64_t>(n_tokens) + 3) / 4 * 4 : 0, of_lengths = of_pieces + 4 * room;
     const at::Tensor all = at::empty({of_lengths + 2 * static_cast<int64_t>(n) + 3}, i32);
-    if (a[7] == Py_True) slots = part_of(all, at::kLong, 0, {n_tokens});
+    if (want_slots) slots = part_of(all, at::kLong, 0, {n_tokens});
     pieces = part_of(all, at::kInt, of_pieces, {room, 4});
     lengths = part_of(all, at::kInt, of_lengths, {n});
     offsets = part_of(all, at::kInt, of_lengths + n, {static_cast<int64_t>(n) + 1});
@@ -197,7 +204,7 @@ PyObject* py_cache_attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   const uint32_t width = count(table.size(1), "block_table");
   const uint32_t longest = a[9] == Py_None ? count(static_cast<int64_t>(width) * cache.block_tokens, "max_length") : count(a[9], "max_length");
   at::Tensor out, lse;
-  attention_out(q, a[10] == Py_True, a[11], &out, &lse);
+  attention_out(q, truth(a[10]), a[11], &out, &lse);
   const at::Tensor ws = workspace_of(a[12], cache_attention_workspace_bytes(n, heads, cache.kv_heads, cache.head_dim, longest), device);
   const int rc = cache_attention(&cache, &qv, heads, type, static_cast<float>(THPUtils_unpackDouble(a[7])),
                                  dense<int32_t>(table, at::kInt, device, "block_table"), width, dense<int32_t>(lengths, at::kInt, device, "lengths"), n,
@@ -220,7 +227,7 @@ PyObject* py_prompt_attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) 
   TORCH_CHECK_VALUE(k.sizes() == v.sizes() && k.size(0) == q.size(0) && k.size(2) == q.size(2), "k, v: [n_tokens, kv heads, head_dim]");
   TORCH_CHECK_VALUE(offsets.numel() >= 1 && status.numel() == 1, "offsets: [prompts + 1]; status: [1]");
   at::Tensor out, lse;
-  attention_out(q, a[6] == Py_True, a[7], &out, &lse);
+  attention_out(q, truth(a[6]), a[7], &out, &lse);
   const int rc = prompt_attention(&qv, &kv, &vv, count(q.size(1), "q heads"), count(k.size(1), "kv heads"), count(q.size(2), "head_dim"), type,
                                   static_cast<float>(THPUtils_unpackDouble(a[4])), dense<int32_t>(offsets, at::kInt, device, "offsets"),
                                   count(offsets.numel() - 1, "offsets"), count(q.size(0), "tokens"), dense<void>(out, q.scalar_type(), device, "out"),
