@@ -71,11 +71,24 @@ fikit_cache cache_of(PyObject* const* a, const at::Device& device) {
                      count(k.size(0), "blocks"), count(k.size(1), "kv heads"), count(k.size(2), "block tokens"), count(k.size(3), "head_dim")};
 }
 
-at::Tensor workspace_of(PyObject* given, size_t bytes, const at::Device& device) {
-  if (given != Py_None) {
-    const at::Tensor& t = tensor(given, "workspace_buf");
-    dense<uint8_t>(t, at::kByte, device, "workspace_buf");
-    return t;
+// Other Python threads run while this lives: an allocation may wait for memory, and a launch for room in a queue.  What is taken from
+// Python objects is taken before.
+class Unlocked {
+  PyThreadState* state = PyEval_SaveThread();
+
+ public:
+  Unlocked() = default;
+  Unlocked(const Unlocked&) = delete;
+  ~Unlocked() { PyEval_RestoreThread(state); }
+};
+
+// A tensor, or one that is not defined.
+at::Tensor given_or_none(PyObject* o, const char* what) { return o == Py_None ? at::Tensor() : tensor(o, what); }
+
+at::Tensor workspace_of(const at::Tensor& given, size_t bytes, const at::Device& device) {
+  if (given.defined()) {
+    dense<uint8_t>(given, at::kByte, device, "workspace_buf");
+    return given;
   }
   return bytes ? at::empty({static_cast<int64_t>(bytes < 256 ? 256 : bytes)}, at::TensorOptions().dtype(at::kByte).device(device)) : at::Tensor();
 }
@@ -109,39 +122,46 @@ PyObject* py_cache_plan(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   TORCH_CHECK_VALUE(status.numel() == 1, "status: [1]");
   const bool want_slots = truth(a[7]);
   const int64_t room = static_cast<int64_t>(cache_pieces(n_tokens, n, block_tokens));
-  const auto i32 = at::TensorOptions().dtype(at::kInt).device(device);
   at::Tensor lengths, offsets, slots, pieces, counts;
-  if (a[8] == Py_None) {
-    // one allocation: slots (two words each), pieces, lengths, places, counts
-    const int64_t of_pieces = want_slots ? (2 * static_cast<int64_t>(n_tokens) + 3) / 4 * 4 : 0, of_lengths = of_pieces + 4 * room;
-    const at::Tensor all = at::empty({of_lengths + 2 * static_cast<int64_t>(n) + 3}, i32);
-    if (want_slots) slots = part_of(all, at::kLong, 0, {n_tokens});
-    pieces = part_of(all, at::kInt, of_pieces, {room, 4});
-    lengths = part_of(all, at::kInt, of_lengths, {n});
-    offsets = part_of(all, at::kInt, of_lengths + n, {static_cast<int64_t>(n) + 1});
-    counts = part_of(all, at::kInt, of_lengths + 2 * static_cast<int64_t>(n) + 1, {2});
-  } else {
+  const bool allocate = a[8] == Py_None;
+  if (!allocate) {
     TORCH_CHECK_VALUE(PyTuple_Check(a[8]) && PyTuple_GET_SIZE(a[8]) == 5, "out: a CachePlan");
     lengths = tensor(PyTuple_GET_ITEM(a[8], 0), "lengths");
     offsets = tensor(PyTuple_GET_ITEM(a[8], 1), "token_offsets");
-    if (PyTuple_GET_ITEM(a[8], 2) != Py_None) slots = tensor(PyTuple_GET_ITEM(a[8], 2), "slots");
+    slots = given_or_none(PyTuple_GET_ITEM(a[8], 2), "slots");
     pieces = tensor(PyTuple_GET_ITEM(a[8], 3), "pieces");
     counts = tensor(PyTuple_GET_ITEM(a[8], 4), "counts");
     TORCH_CHECK_VALUE(lengths.numel() == n && offsets.numel() == static_cast<int64_t>(n) + 1 && counts.numel() == 2 && pieces.numel() == 4 * room &&
                           (!slots.defined() || slots.numel() == n_tokens),
                       "out: tensors of the plan's sizes");
   }
-  const at::Tensor ws = workspace_of(a[9], cache_plan_workspace_bytes(n), device);
-  const int rc = cache_plan(dense<int32_t>(cached, at::kInt, device, "cached"), dense<int32_t>(added, at::kInt, device, "added"), n, n_tokens, block_tokens,
-                            dense<int32_t>(table, at::kInt, device, "block_table"), count(table.size(1), "block_table"),
-                            dense<int32_t>(free, at::kInt, device, "free_blocks"), count(free.numel(), "free_blocks"),
-                            dense<int32_t>(lengths, at::kInt, device, "lengths"), dense<int32_t>(offsets, at::kInt, device, "token_offsets"),
-                            slots.defined() ? dense<int64_t>(slots, at::kLong, device, "slots") : nullptr,
-                            dense<fikit_piece>(pieces, at::kInt, device, "pieces"), dense<int32_t>(counts, at::kInt, device, "counts"),
-                            dense<int32_t>(status, at::kInt, device, "status"), ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? ws.numel() : 0,
-                            stream_of(a[10]));
+  const at::Tensor workspace = given_or_none(a[9], "workspace_buf");
+  void* const stream = stream_of(a[10]);
+  int rc;
+  {
+    const Unlocked unlocked;
+    if (allocate) {
+      // one allocation: slots (two words each), pieces, lengths, places, counts
+      const int64_t of_pieces = want_slots ? (2 * static_cast<int64_t>(n_tokens) + 3) / 4 * 4 : 0, of_lengths = of_pieces + 4 * room;
+      const at::Tensor all = at::empty({of_lengths + 2 * static_cast<int64_t>(n) + 3}, at::TensorOptions().dtype(at::kInt).device(device));
+      if (want_slots) slots = part_of(all, at::kLong, 0, {n_tokens});
+      pieces = part_of(all, at::kInt, of_pieces, {room, 4});
+      lengths = part_of(all, at::kInt, of_lengths, {n});
+      offsets = part_of(all, at::kInt, of_lengths + n, {static_cast<int64_t>(n) + 1});
+      counts = part_of(all, at::kInt, of_lengths + 2 * static_cast<int64_t>(n) + 1, {2});
+    }
+    const at::Tensor ws = workspace_of(workspace, cache_plan_workspace_bytes(n), device);
+    rc = cache_plan(dense<int32_t>(cached, at::kInt, device, "cached"), dense<int32_t>(added, at::kInt, device, "added"), n, n_tokens, block_tokens,
+                    dense<int32_t>(table, at::kInt, device, "block_table"), count(table.size(1), "block_table"),
+                    dense<int32_t>(free, at::kInt, device, "free_blocks"), count(free.numel(), "free_blocks"),
+                    dense<int32_t>(lengths, at::kInt, device, "lengths"), dense<int32_t>(offsets, at::kInt, device, "token_offsets"),
+                    slots.defined() ? dense<int64_t>(slots, at::kLong, device, "slots") : nullptr,
+                    dense<fikit_piece>(pieces, at::kInt, device, "pieces"), dense<int32_t>(counts, at::kInt, device, "counts"),
+                    dense<int32_t>(status, at::kInt, device, "status"), ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? ws.numel() : 0,
+                    stream);
+  }
   if (rc != FIKIT_OK) return PyLong_FromLong(rc);
-  if (a[8] != Py_None) {
+  if (!allocate) {
     Py_INCREF(a[8]);
     return a[8];
   }
@@ -160,24 +180,32 @@ PyObject* py_cache_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   const fikit_vectors kv = vectors(k, k.scalar_type(), device, "k"), vv = vectors(v, k.scalar_type(), device, "v");
   TORCH_CHECK_VALUE(k.sizes() == v.sizes() && k.size(1) == cache.kv_heads && k.size(2) == cache.head_dim, "k, v: [n_tokens, kv heads, head_dim] of the cache");
   TORCH_CHECK_VALUE(pieces.dim() == 2 && pieces.size(1) == 4 && status.numel() == 1, "pieces: [n, 4]; status: [1]");
-  const int rc = cache_append(&cache, &kv, &vv, count(k.size(0), "tokens"), type, dense<fikit_piece>(pieces, at::kInt, device, "pieces"),
-                              static_cast<uint64_t>(pieces.size(0)), dense<int32_t>(status, at::kInt, device, "status"), stream_of(a[8]));
+  void* const stream = stream_of(a[8]);
+  int rc;
+  {
+    const Unlocked unlocked;
+    rc = cache_append(&cache, &kv, &vv, count(k.size(0), "tokens"), type, dense<fikit_piece>(pieces, at::kInt, device, "pieces"),
+                      static_cast<uint64_t>(pieces.size(0)), dense<int32_t>(status, at::kInt, device, "status"), stream);
+  }
   return PyLong_FromLong(rc);
   END_HANDLE_TH_ERRORS
 }
 
-// The outputs of an attention call: those given, or new ones.
-void attention_out(const at::Tensor& q, bool want_lse, PyObject* given, at::Tensor* out, at::Tensor* lse) {
-  if (given == Py_None) {
-    *out = at::empty(q.sizes(), at::TensorOptions().dtype(q.scalar_type()).device(q.device()));
-    if (want_lse) *lse = at::empty({q.size(0), q.size(1)}, at::TensorOptions().dtype(at::kFloat).device(q.device()));
-    return;
-  }
+// The outputs of an attention call that are given.
+void given_out(const at::Tensor& q, PyObject* given, at::Tensor* out, at::Tensor* lse) {
+  if (given == Py_None) return;
   TORCH_CHECK_VALUE(PyTuple_Check(given) && PyTuple_GET_SIZE(given) == 2, "out: an Attention");
   *out = tensor(PyTuple_GET_ITEM(given, 0), "out");
-  if (PyTuple_GET_ITEM(given, 1) != Py_None) *lse = tensor(PyTuple_GET_ITEM(given, 1), "lse");
+  *lse = given_or_none(PyTuple_GET_ITEM(given, 1), "lse");
   TORCH_CHECK_VALUE(out->sizes() == q.sizes(), "out: the shape of q");
   TORCH_CHECK_VALUE(!lse->defined() || (lse->dim() == 2 && lse->size(0) == q.size(0) && lse->size(1) == q.size(1)), "lse: [rows, q heads]");
+}
+
+// New ones, if none are.
+void new_out(const at::Tensor& q, bool want_lse, at::Tensor* out, at::Tensor* lse) {
+  if (out->defined()) return;
+  *out = at::empty(q.sizes(), at::TensorOptions().dtype(q.scalar_type()).device(q.device()));
+  if (want_lse) *lse = at::empty({q.size(0), q.size(1)}, at::TensorOptions().dtype(at::kFloat).device(q.device()));
 }
 
 PyObject* attention_result(int rc, PyObject* given, const at::Tensor& out, const at::Tensor& lse) {
@@ -204,14 +232,21 @@ PyObject* py_cache_attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   const uint32_t width = count(table.size(1), "block_table");
   const uint32_t longest = a[9] == Py_None ? count(static_cast<int64_t>(width) * cache.block_tokens, "max_length") : count(a[9], "max_length");
   at::Tensor out, lse;
-  attention_out(q, truth(a[10]), a[11], &out, &lse);
-  const at::Tensor ws = workspace_of(a[12], cache_attention_workspace_bytes(n, heads, cache.kv_heads, cache.head_dim, longest), device);
-  const int rc = cache_attention(&cache, &qv, heads, type, static_cast<float>(THPUtils_unpackDouble(a[7])),
-                                 dense<int32_t>(table, at::kInt, device, "block_table"), width, dense<int32_t>(lengths, at::kInt, device, "lengths"), n,
-                                 longest, dense<void>(out, q.scalar_type(), device, "out"),
-                                 lse.defined() ? dense<float>(lse, at::kFloat, device, "lse") : nullptr,
-                                 dense<int32_t>(status, at::kInt, device, "status"), ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? ws.numel() : 0,
-                                 stream_of(a[13]));
+  given_out(q, a[11], &out, &lse);
+  const bool want_lse = truth(a[10]);
+  const float scale = static_cast<float>(THPUtils_unpackDouble(a[7]));
+  const at::Tensor workspace = given_or_none(a[12], "workspace_buf");
+  void* const stream = stream_of(a[13]);
+  int rc;
+  {
+    const Unlocked unlocked;
+    new_out(q, want_lse, &out, &lse);
+    const at::Tensor ws = workspace_of(workspace, cache_attention_workspace_bytes(n, heads, cache.kv_heads, cache.head_dim, longest), device);
+    rc = cache_attention(&cache, &qv, heads, type, scale, dense<int32_t>(table, at::kInt, device, "block_table"), width,
+                         dense<int32_t>(lengths, at::kInt, device, "lengths"), n, longest, dense<void>(out, q.scalar_type(), device, "out"),
+                         lse.defined() ? dense<float>(lse, at::kFloat, device, "lse") : nullptr, dense<int32_t>(status, at::kInt, device, "status"),
+                         ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? ws.numel() : 0, stream);
+  }
   return attention_result(rc, a[11], out, lse);
   END_HANDLE_TH_ERRORS
 }
@@ -227,12 +262,19 @@ PyObject* py_prompt_attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) 
   TORCH_CHECK_VALUE(k.sizes() == v.sizes() && k.size(0) == q.size(0) && k.size(2) == q.size(2), "k, v: [n_tokens, kv heads, head_dim]");
   TORCH_CHECK_VALUE(offsets.numel() >= 1 && status.numel() == 1, "offsets: [prompts + 1]; status: [1]");
   at::Tensor out, lse;
-  attention_out(q, truth(a[6]), a[7], &out, &lse);
-  const int rc = prompt_attention(&qv, &kv, &vv, count(q.size(1), "q heads"), count(k.size(1), "kv heads"), count(q.size(2), "head_dim"), type,
-                                  static_cast<float>(THPUtils_unpackDouble(a[4])), dense<int32_t>(offsets, at::kInt, device, "offsets"),
-                                  count(offsets.numel() - 1, "offsets"), count(q.size(0), "tokens"), dense<void>(out, q.scalar_type(), device, "out"),
-                                  lse.defined() ? dense<float>(lse, at::kFloat, device, "lse") : nullptr,
-                                  dense<int32_t>(status, at::kInt, device, "status"), stream_of(a[8]));
+  given_out(q, a[7], &out, &lse);
+  const bool want_lse = truth(a[6]);
+  const float scale = static_cast<float>(THPUtils_unpackDouble(a[4]));
+  void* const stream = stream_of(a[8]);
+  int rc;
+  {
+    const Unlocked unlocked;
+    new_out(q, want_lse, &out, &lse);
+    rc = prompt_attention(&qv, &kv, &vv, count(q.size(1), "q heads"), count(k.size(1), "kv heads"), count(q.size(2), "head_dim"), type, scale,
+                          dense<int32_t>(offsets, at::kInt, device, "offsets"), count(offsets.numel() - 1, "offsets"), count(q.size(0), "tokens"),
+                          dense<void>(out, q.scalar_type(), device, "out"), lse.defined() ? dense<float>(lse, at::kFloat, device, "lse") : nullptr,
+                          dense<int32_t>(status, at::kInt, device, "status"), stream);
+  }
   return attention_result(rc, a[7], out, lse);
   END_HANDLE_TH_ERRORS
 }

@@ -69,3 +69,10 @@ def test_wanted_outputs_go_by_truth(marshal, want):
     assert (plan(native, want)[2] is not None) == bool(want)
     assert (decode(native, want_lse=want)[1] is not None) == bool(want)
     assert (prompt(native, want_lse=want)[1] is not None) == bool(want)
+
+
+def test_the_interpreter_is_free_while_a_call_enqueues(marshal):
+    """PyGILState_Check, called in the place of the C calls, tells whether the calling thread holds the interpreter's lock."""
+    native = marshal(ctypes.pythonapi.PyGILState_Check)
+    assert isinstance(plan(native), tuple) and isinstance(decode(native), tuple) and isinstance(prompt(native), tuple)
+    assert append(native) == 0
