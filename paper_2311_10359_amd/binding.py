@@ -573,6 +573,7 @@ def fikit_profile_merge(rows_a: torch.Tensor, task_row_offsets_a: torch.Tensor, 
 # ---- tasks of a language model service -----------------------------------------------------------
 # These calls enqueue their kernels and return; errors that depend on data are left in `status`, an int32 [1] device tensor
 # that starts as zero and that fikit_check_status looks at.  Tensors that a call allocates belong to the stream it runs on.
+# For inference only: inputs that require gradients are a ValueError unless gradients are off.
 
 
 def _outputs(kind, got, what: str):

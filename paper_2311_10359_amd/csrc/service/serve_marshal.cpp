@@ -6,6 +6,7 @@
 // for what a pointer cannot describe.
 #include <torch/csrc/python_headers.h>
 
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -52,11 +53,12 @@ int32_t value_type(const at::Tensor& t, const char* what) {
   return t.scalar_type() == at::kBFloat16 ? FIKIT_BF16 : FIKIT_F16;
 }
 
-// [tokens, heads, head_dim] with the last dimension dense.
+// [tokens, heads, head_dim] with the last dimension dense.  (For inference only: an output that silently had no gradient would be wrong.)
 fikit_vectors vectors(const at::Tensor& t, at::ScalarType type, const at::Device& device, const char* what) {
   TORCH_CHECK_VALUE(t.dim() == 3 && (t.stride(2) == 1 || t.size(2) <= 1) && t.stride(0) >= 0 && t.stride(1) >= 0 && t.scalar_type() == type &&
                         t.device() == device,
                     what, ": [tokens, heads, head_dim] ", type, " on ", device, ", the last dimension dense");
+  TORCH_CHECK_VALUE(!(t.requires_grad() && at::GradMode::is_enabled()), what, ": requires a gradient, and there is no backward pass; detach it or use no_grad()");
   return fikit_vectors{t.data_ptr(), static_cast<uint64_t>(t.stride(0)), static_cast<uint64_t>(t.stride(1))};
 }
 

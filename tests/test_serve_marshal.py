@@ -76,3 +76,16 @@ def test_the_interpreter_is_free_while_a_call_enqueues(marshal):
     native = marshal(ctypes.pythonapi.PyGILState_Check)
     assert isinstance(plan(native), tuple) and isinstance(decode(native), tuple) and isinstance(prompt(native), tuple)
     assert append(native) == 0
+
+
+def test_inputs_that_require_gradients_are_refused(marshal):
+    """Their outputs would be cut off from them without a word; there is no backward pass."""
+    native = marshal(nothing)
+    x = vectors().requires_grad_()
+    for call in (lambda: decode(native, q=x), lambda: prompt(native, q=x), lambda: prompt(native, k=x), lambda: prompt(native, v=x),
+                 lambda: append(native, k=x), lambda: append(native, v=x)):
+        with pytest.raises(ValueError, match="no_grad"):
+            call()
+        with torch.no_grad():
+            call()
+    decode(native, q=x.detach())
