@@ -59,7 +59,8 @@ fikit_vectors vectors(const at::Tensor& t, at::ScalarType type, const at::Device
                         t.device() == device,
                     what, ": [tokens, heads, head_dim] ", type, " on ", device, ", the last dimension dense");
   TORCH_CHECK_VALUE(!(t.requires_grad() && at::GradMode::is_enabled()), what, ": requires a gradient, and there is no backward pass; detach it or use no_grad()");
-  return fikit_vectors{t.data_ptr(), static_cast<uint64_t>(t.stride(0)), static_cast<uint64_t>(t.stride(1))};
+  // (the stride of a dimension of size one may be anything, and is not used)
+  return fikit_vectors{t.data_ptr(), t.size(0) > 1 ? static_cast<uint64_t>(t.stride(0)) : 0, t.size(1) > 1 ? static_cast<uint64_t>(t.stride(1)) : 0};
 }
 
 fikit_cache cache_of(PyObject* const* a, const at::Device& device) {

@@ -89,3 +89,19 @@ def test_inputs_that_require_gradients_are_refused(marshal):
         with torch.no_grad():
             call()
     decode(native, q=x.detach())
+
+
+def test_strides_of_single_tokens_and_heads_do_not_count(marshal):
+    """What a dimension of size one has for a stride is chance: a slice's, say, that is no multiple of 8 values."""
+    seen = []
+
+    @ctypes.CFUNCTYPE(ctypes.c_int, ctypes.POINTER(binding._Vectors), ctypes.POINTER(binding._Vectors), ctypes.POINTER(binding._Vectors))
+    def prompt_attention(q, k, v):
+        seen.extend((x.contents.token_stride, x.contents.head_stride) for x in (q, k, v))
+        return 0
+    native = marshal(prompt_attention)
+    one_token = torch.as_strided(torch.zeros(1024, dtype=torch.bfloat16), (1, 2, 64), (17, 64, 1))
+    prompt(native, q=one_token, k=one_token, v=one_token)
+    one_head = torch.as_strided(torch.zeros(1024, dtype=torch.bfloat16), (3, 1, 64), (72, 3, 1))
+    prompt(native, q=one_head, k=one_head, v=one_head)
+    assert seen == [(0, 64)] * 3 + [(72, 0)] * 3
