@@ -597,6 +597,8 @@ def _elsewhere(stream: Optional[torch.cuda.Stream], device):
     if device.type != "cuda":
         raise ValueError("tensors on a GPU")
     if stream is not None:
+        if stream.device != device:
+            raise ValueError("a stream of the tensors' device")
         return torch.cuda.stream(stream)
     if device.index != _current_device():
         return torch.cuda.device(device)
