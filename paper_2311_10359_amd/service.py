@@ -108,7 +108,10 @@ class Service:
         return x + record("back", (n, 1, 1), torch.mm, out.view(n, -1), self.w_out[layer])
 
     def prompts(self, record, x: torch.Tensor, lengths: List[int]) -> torch.Tensor:
-        """x: [sum of lengths, hidden], the prompts one behind the other; returns the last layer's output."""
+        """x: [sum of lengths, hidden], the prompts one behind the other; returns the last layer's output.  They come first: prompt
+        attention sees the new tokens only, so prompts behind tokens in the cache are refused."""
+        if self.longest > 0:
+            raise ValueError("prompts of requests that have no tokens in the cache")
         plan = self._plan(record, lengths)
         scale = 1 / math.sqrt(self.sizes.dim)
         for layer in range(self.sizes.layers):
