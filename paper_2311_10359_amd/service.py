@@ -93,11 +93,9 @@ class Service:
 
     def _plan(self, record, added: List[int]) -> binding.CachePlan:
         n, sizes = sum(added), self.sizes
-        plan = record("plan", (len(added), 1, 1), binding.fikit_cache_plan, self.lengths,
+        return record("plan", (len(added), 1, 1), binding.fikit_cache_plan, self.lengths,
                       torch.tensor(added, dtype=torch.int32).to(self.device, non_blocking=True), n, sizes.block, self.table,
                       self.free[self.taken:], self.status, want_slots=False)
-        self.lengths = plan.lengths
-        return plan
 
     def _layer(self, record, x, layer, attend, plan):
         sizes, n = self.sizes, x.shape[0]
@@ -136,7 +134,12 @@ class Service:
 
     def _settle(self, plan, most_added) -> None:
         """What the host does at the end of a step, when it waits for the outputs anyway."""
-        binding.fikit_check_status(self.status)
+        try:
+            binding.fikit_check_status(self.status)
+        except binding.FikitError:
+            self.status.zero_()           # nothing of the step counts, and it can be tried again
+            raise
+        self.lengths = plan.lengths
         self.taken += int(plan.counts[0])
         self.longest += most_added
 

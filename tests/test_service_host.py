@@ -54,3 +54,14 @@ def test_prompts_are_not_continued():
     one_token_first.step(Fake(), tokens(2))
     with pytest.raises(ValueError):
         one_token_first.prompts(Fake(), tokens(3), [1, 2])
+
+
+def test_a_step_that_fails_leaves_the_service_as_it_was():
+    s = service.Service(SIZES, 2, 64, device="cpu")
+    s.prompts(Fake(), tokens(9), [4, 5])
+    with pytest.raises(binding.FikitError) as e:
+        s.step(Fake(binding.FIKIT_CACHE_FULL), tokens(2))
+    assert e.value.status == binding.FIKIT_CACHE_FULL
+    assert s.lengths.tolist() == [4, 5] and s.taken == 3 and s.longest == 5 and int(s.status) == 0
+    s.step(Fake(), tokens(2))
+    assert s.lengths.tolist() == [5, 6]
