@@ -140,8 +140,8 @@ __device__ __forceinline__ void plan_rest(const PlanArgs& a, uint32_t pieces, ui
 }
 
 // Up to 4096 requests: one launch, in which every workgroup sums all of them for itself, PER to a thread, and takes 1024 tokens at a
-// time.  256 requests with a new token each: 3.9 us, as an empty launch; 64 prompts of up to 4096 tokens, 36,000 in all: 4.8.  With four to a
-// thread, up to 4096, LDS holds one workgroup on a compute unit; a call for 1500 requests takes 5.9 to 6.4 us and for 4000 7.4 to 7.5, where
+// time.  256 requests with a new token each: 3.8 us, as an empty launch; 64 prompts of up to 4096 tokens, 36,000 in all: 4.6.  With four to a
+// thread, up to 4096, LDS holds one workgroup on a compute unit; a call for 1500 requests takes 5.9 to 6.8 us and for 4000 7.3 to 7.6, where
 // the two launches below take 9.3 to 12.5.
 constexpr int PLAN_PER = 4;
 template <int PER>
@@ -204,7 +204,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_plan_tiles(PlanArgs a) {
   if (threadIdx.x == 0) a.tiles[blockIdx.x] = PlanTile{flags ? PLAN_BAD : total.tokens, total.blocks, total.pieces};
 }
 
-// ... then every workgroup sums the up to 1024 tiles, and of those that hold its tokens the requests.  (16,384 requests, 3 MB: 3.3 and 11.7 us;
+// ... then every workgroup sums the up to 1024 tiles, and of those that hold its tokens the requests.  (16,384 requests, 3 MB: 3.0 and 10.4 us;
 // one launch in which every workgroup summed all requests took 20.)
 constexpr uint32_t PLAN_MOST_REQUESTS = PLAN_THREADS * PLAN_THREADS;
 __global__ __launch_bounds__(PLAN_THREADS) void k_plan_tokens(PlanArgs a) {
@@ -272,7 +272,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_plan_tokens(PlanArgs a) {
 // per piece, head, and keys or values.  It reads the values once and holds up to 8192 of them (64 tokens of 128) in registers
 // between the maximum and the rounding; of longer pieces it reads them again, from the cache.  Memory bound: 2 bytes read and 1
 // written per value, and half an instruction each for the maximum (of pairs, as integers) and for the rounding of a pair.  11,600
-// tokens of 16 prompts, 8 heads of 128 (71 MB): 13.4 us, 5.3 TB/s; a token each for 256 requests: 5.0, latency.
+// tokens of 16 prompts, 8 heads of 128 (71 MB): 12.7 us, 5.6 TB/s; a token each for 256 requests: 4.9, latency.
 
 struct AppendArgs {
   fikit_cache cache;

@@ -24,7 +24,7 @@ namespace fikit {
 //
 // Bound by memory: a token costs 2 D bytes a key head and no more than 4 D operations for each of its query heads.  Two steps of codes are
 // in flight per wave, in registers, which is what 8 waves (16 with heads of 64) on a compute unit leave room for.  128 requests of 4096 to
-// 16,384 tokens, 8 heads of 128 (2.2 GB): 340 us, 6.5 TB/s, of the 7.2 that a kernel reaches which only reads past the caches; 64 requests
+// 16,384 tokens, 8 heads of 128 (2.2 GB): 340 to 350 us, 6.4 to 6.5 TB/s, of the 7.2 that a kernel reaches which only reads past the caches; 64 requests
 // of 1 to 13,517 tokens, 16 heads of 64, blocks of 16 (145 MB): 31 us, 4.6 TB/s; 2 of 76,687 and 127,690, 4 heads of 128 (209 MB): 38, 5.4
 // TB/s; one of 4097 (8 MB): 6.8, latency.
 //

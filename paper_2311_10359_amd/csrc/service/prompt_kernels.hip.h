@@ -19,10 +19,13 @@ namespace fikit {
 // Bound by the rate of matrix instructions together with the vector instructions of the softmax, five for each score: heads of 128 take
 // 32 products of 32 clocks for a wave's 64 tokens, and 130 vector instructions, 32 of them exponentials at twice the time.  So both are made at
 // once, the scores of a tile while the one before is weighed, in an order that is written down (weigh_and_go_on); one after the other took
-// 778 us where this takes 500.  One prompt of 8192 tokens, 32 query and 8 key heads of 128: 490 to 530 us from card to card, 1.04 to 1.12
+// 778 us where this takes 500.  One prompt of 8192 tokens, 32 query and 8 key heads of 128: 485 to 530 us from card to card, 1.04 to 1.13
 // PFLOP/s of the 1.6 that a large product reaches; the matrix unit is busy for 65 % of the time, at the clock of 1.7 GHz that the power
-// allows.  24 prompts of 1 to 1788 tokens: 84 us, 0.73 PFLOP/s, with tiles that are seen in part and, for each 128 rows, 5 us before and
-// behind the tiles, mostly latency.  5 of 3 to 49 tokens: 5.4 us, a launch and four loads that depend on each other.
+// allows.  (That is in a row, from the 60th call on; of calls that begin on an idle card the first three take 510, the next ones up to 670
+// while the clock settles, the 20th 540.)  Heads of 64 have half the products for as many vector instructions, about 660 clocks of these
+// for 512 of those, so the vector unit binds: 4 prompts of 4096 tokens, 16 heads: 155 to 162 us, 0.85 to 0.89 PFLOP/s.  24 prompts of 1 to
+// 1788 tokens: 83 to 90 us, 0.68 to 0.73 PFLOP/s, with tiles that are seen in part and, for each 128 rows, 5 us before and behind the
+// tiles, mostly latency.  5 of 3 to 49 tokens: 5.4 us, a launch and four loads that depend on each other.
 
 struct PromptArgs {
   fikit_vectors q, k, v;
@@ -146,8 +149,9 @@ struct PromptWave {              // what a wave holds of its 32 rows; a lane of 
     }
   }
   // Weights are rounded to 16 bits, as an operand of the matrix instruction has to be, and summed before that: error against 64 bits
-  // 0.0020 (bfloat16), 0.0015 of which is the rounding of the output.  What rounding leaves as a second operand would be a quarter more
-  // products of the kernel that products bind.
+  // 0.0019 to 0.0021 (bfloat16) and 0.00021 (float16); the rounding of the output is 0.0015 and 0.00018.  What rounding leaves as a second
+  // operand, as in a decode step, brings it down to the output's and is half more products of the kernel that products bind: 8192 tokens
+  // 514 -> 712 us, 4 prompts of 4096 with heads of 64 162 -> 223, 24 ragged ones 88 -> 109, 64 of 500 142 -> 165.
   __device__ __forceinline__ void weigh(typename T::x8 (&weights)[4]) {
     const float origin = m > -__builtin_huge_valf() ? m : 0.f;
 #pragma unroll
@@ -416,7 +420,7 @@ __device__ __attribute__((noinline)) void prompt_with_care(PromptArgs a, uint32_
   w.write(a, start, length, head, keys + wave * (32 * D), vals + wave * (32 * D));
 }
 
-// Heads of 64 leave room for a third workgroup on a compute unit (4 prompts of 4096 tokens: 155 us; with two 168, with four, which spill, 171).
+// Heads of 64 leave room for a third workgroup on a compute unit (4 prompts of 4096 tokens: 155 to 162 us; with two 168, with four, which spill, 171).
 template <typename T, int D, int WAVES>
 __global__ __launch_bounds__(WAVES * WAVE, D == 64 ? 3 : 2) void k_prompt(PromptArgs a) {
   constexpr uint32_t ROWS = WAVES * PROMPT_WAVE_ROWS, TILE = PROMPT_KEYS * D * 2;
