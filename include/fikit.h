@@ -36,13 +36,13 @@
  *     fikit_gapfill_static).  Inputs are left
  *     untouched.
  *   - All work is enqueued on `hip_stream` (a hipStream_t passed as void*; NULL = the default
- *     stream).  Every call but fikit_gapfill_static and the attention calls of a language model
- *     service (fikit_cache_*, fikit_prompt_attention) waits until its work there is done before it
+ *     stream).  Every call but fikit_gapfill_static and the calls of a language model service
+ *     (fikit_cache_*, fikit_prompt_attention, fikit_rotate_heads, fikit_token_scores) waits until its work there is done before it
  *     returns, so outputs and the returned status are final on return, for every stream, copy and
  *     thread.
  *   - Return value: FIKIT_OK or a negative fikit_status.  Nothing aborts or throws.  After an
  *     error the contents of the output buffers are unspecified.
- *   - Everything but the attention calls is integer arithmetic (nanoseconds, counts); results are exact.
+ *   - Everything but the calls of a language model service is integer arithmetic (nanoseconds, counts); results are exact.
  *   - Limits: n_records, n_ids < 2^32 - 2^24.  Timestamps must be such that end - start and
  *     next start - end fit in int64, and a task's predicted timeline (sum of p50 values over
  *     its launches) fits in int64.
@@ -446,7 +446,8 @@ int fikit_profile_merge(const fikit_row* d_rows_a, const uint64_t* d_task_row_of
  */
 typedef enum fikit_value_type {
   FIKIT_BF16 = 0,
-  FIKIT_F16 = 1
+  FIKIT_F16 = 1,
+  FIKIT_F32 = 2          /* fikit_token_scores only */
 } fikit_value_type;
 
 /* Vectors of head_dim 16-bit values, one per token and head; token t, head h at d_data + t * token_stride + h * head_stride
@@ -574,6 +575,45 @@ int fikit_prompt_attention(const fikit_vectors* h_q, const fikit_vectors* h_k, c
                            uint32_t kv_heads, uint32_t head_dim, int32_t value_type, float scale, const int32_t* d_offsets,
                            uint32_t n_prompts, uint32_t n_tokens, void* d_out, float* d_lse, int32_t* d_status,
                            void* hip_stream);
+
+/* ---- around the attention ----------------------------------------------------------------------------------------
+ *
+ * What such a service does with its heads, cache and logits beside the four calls above, in the same manner: nothing is allocated
+ * or waited for, and d_status is looked at and written as there.
+ *
+ *   fikit_rotate_heads      norm of query and key heads and their rotation by position, between the product and the append
+ */
+
+typedef enum fikit_pairs {
+  FIKIT_PAIRS_HALVES = 0,       /* value i of a head with i + rotary_dim / 2 */
+  FIKIT_PAIRS_NEIGHBOURS = 1    /* value 2 i with 2 i + 1                    */
+} fikit_pairs;
+
+/*
+ * Norm and rotation of the query and key heads of n_tokens tokens.  A head x becomes
+ *
+ *   y = x * weight / sqrt(mean(x^2) + epsilon)        if its weight is given, else y = x,
+ *
+ * and of y's first rotary_dim values the pairs (a, b) become (a cos t - b sin t, b cos t + a sin t), where t = d_positions[token] *
+ * d_frequencies[i] for pair i.  The others stay.  Held in 32 bits, angles in 64, and rounded once.
+ *
+ *   h_q, h_k          inputs as in fikit_prompt_attention; h_k may be NULL with kv_heads = 0, and h_q with q_heads = 0.
+ *   head_dim          64, 128 or 256.
+ *   d_q_weight, d_k_weight   [head_dim] of the heads' type, 16-byte aligned, or NULL: no norm.
+ *   epsilon           at least 2^-126, finite (looked at where there is a weight).
+ *   d_positions       [n_tokens]; a token of negative position is left out: its outputs stay as they are.
+ *   d_frequencies     [rotary_dim / 2] radians for a position (any table); NULL if rotary_dim is 0.
+ *   rotary_dim        a multiple of 16 up to head_dim.
+ *   pairs             a fikit_pairs.
+ *   h_q_out, h_k_out  outputs of the same sizes, strides of at least head_dim where there are several.  An output may be its own input (the
+ *                     same address and strides); else outputs overlap neither each other nor an input.
+ *
+ * The range of the type counts: a norm of values whose squares pass the largest float is right.
+ */
+int fikit_rotate_heads(const fikit_vectors* h_q, const fikit_vectors* h_k, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim,
+                       int32_t value_type, const void* d_q_weight, const void* d_k_weight, float epsilon, const int32_t* d_positions,
+                       const float* d_frequencies, uint32_t rotary_dim, int32_t pairs, uint32_t n_tokens, const fikit_vectors* h_q_out,
+                       const fikit_vectors* h_k_out, int32_t* d_status, void* hip_stream);
 
 const char* fikit_status_string(int status);
 int fikit_version(void);

@@ -34,7 +34,8 @@ EXPORTS = ("fikit_profile_workspace_bytes", "fikit_profile", "fikit_gapfill_work
            "fikit_gapfill_replay", "fikit_prio_fill_workspace_bytes", "fikit_prio_fill", "fikit_pairing_workspace_bytes",
            "fikit_pairing_best", "fikit_profile_merge_workspace_bytes", "fikit_profile_merge", "fikit_status_string", "fikit_version", "fikit_set_wait_limit",
            "fikit_trace_enable", "fikit_trace_read", "fikit_cache_pieces", "fikit_cache_plan_workspace_bytes", "fikit_cache_plan",
-           "fikit_cache_append", "fikit_cache_attention_workspace_bytes", "fikit_cache_attention", "fikit_prompt_attention")
+           "fikit_cache_append", "fikit_cache_attention_workspace_bytes", "fikit_cache_attention", "fikit_prompt_attention",
+           "fikit_rotate_heads")
 
 # Layout of a profile row as seen from numpy (128 bytes; see fikit_row in fikit.h).
 STATS_DTYPE = np.dtype([("count", "<u8"), ("sum", "<u8"), ("min", "<i8"), ("max", "<i8"),
@@ -143,6 +144,8 @@ def load() -> ctypes.CDLL:
         lib.fikit_cache_attention.argtypes = [p_cache, p_vec, u32, i32, f32, vp, u32, vp, u32, u32, vp, vp, vp, vp, sz, vp]
         lib.fikit_prompt_attention.restype = ctypes.c_int
         lib.fikit_prompt_attention.argtypes = [p_vec, p_vec, p_vec, u32, u32, u32, i32, f32, vp, u32, u32, vp, vp, vp, vp]
+        lib.fikit_rotate_heads.restype = ctypes.c_int
+        lib.fikit_rotate_heads.argtypes = [p_vec, p_vec, u32, u32, u32, i32, vp, vp, f32, vp, vp, u32, i32, u32, p_vec, p_vec, vp, vp]
         lib.fikit_status_string.restype = ctypes.c_char_p
         lib.fikit_status_string.argtypes = [ctypes.c_int]
         lib.fikit_version.restype = ctypes.c_int
@@ -620,6 +623,7 @@ def _marshal():
         _serve_marshal.bind(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in (
             "fikit_cache_pieces", "fikit_cache_plan_workspace_bytes", "fikit_cache_plan", "fikit_cache_append",
             "fikit_cache_attention_workspace_bytes", "fikit_cache_attention", "fikit_prompt_attention")))
+        _serve_marshal.bind_around(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in ("fikit_rotate_heads",)))
         _native = _serve_marshal
     return _native
 
@@ -706,6 +710,32 @@ def fikit_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, of
             return fikit_prompt_attention(q, k, v, offsets, scale, status, want_lse=want_lse, out=out)
     got = (_native or _marshal()).prompt_attention(q, k, v, offsets, scale, status, want_lse, out, _stream_of(q.device.index))
     return _outputs(Attention, got, "fikit_prompt_attention")
+
+
+class RotatedHeads(NamedTuple):
+    """Allocated by a call, these are parts of one piece of memory."""
+    q: Optional[torch.Tensor]       # [n_tokens, q heads, head_dim]
+    k: Optional[torch.Tensor]       # [n_tokens, kv heads, head_dim]
+
+
+def fikit_rotate_heads(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor, frequencies: Optional[torch.Tensor],
+                       status: torch.Tensor, *, q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                       epsilon: float = 1e-6, neighbours: bool = False, out: Optional[RotatedHeads] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> RotatedHeads:
+    """q, k: bfloat16 or float16 [n_tokens, heads, head_dim], of any token and head strides that are multiples of 8, or None; positions: int32
+    [n_tokens], a negative one leaves its token's outputs as they are; frequencies: float32 [pairs], radians for a position, None for no
+    rotation; weights: [head_dim] of the heads' type, None for no norm.  Output tensors are allocated unless given; they may be the inputs."""
+    if q is None and k is None:
+        raise ValueError("q or k")
+    device = (k if q is None else q).device
+    context = _elsewhere(stream, device)
+    if context is not None:
+        with context:
+            return fikit_rotate_heads(q, k, positions, frequencies, status, q_weight=q_weight, k_weight=k_weight, epsilon=epsilon,
+                                      neighbours=neighbours, out=out)
+    got = (_native or _marshal()).rotate_heads(q, k, positions, frequencies, status, q_weight, k_weight, epsilon, neighbours, out,
+                                               _stream_of(device.index))
+    return _outputs(RotatedHeads, got, "fikit_rotate_heads")
 
 
 # ---- helpers to move host arrays in and out (marshalling only) ---------------------------------

@@ -16,7 +16,7 @@ HIPCC_FLAGS = [
     "-Wall", "-Wno-unused-function",
 ]
 
-UNITS = ["fikit.hip", os.path.join("service", "serve.hip")]        # translation units
+UNITS = ["fikit.hip", os.path.join("service", "serve.hip"), os.path.join("service", "around.hip")]        # translation units
 
 
 def sources():

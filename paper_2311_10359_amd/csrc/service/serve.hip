@@ -5,49 +5,16 @@
 
 #include "cache_kernels.hip.h"
 #include "decode_kernels.hip.h"
-#include "launches.h"
 #include "prompt_kernels.hip.h"
+#include "serve_host.h"
 
 namespace {
 
 using namespace fikit;
 
-inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-
 constexpr uint32_t PLAN_GROUPS = 512;             // two for each CU
-constexpr uint64_t MOST_GROUPS = 0xffffffull;     // workgroups of 256 threads of a launch, whose threads number less than 2^32
-
-template <typename... P, typename... A>
-int enqueue(void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t st, A... args) {
-  count_launch();
-  hipLaunchKernelGGL(kernel, grid, block, 0, st, args...);
-  return hipGetLastError() == hipSuccess ? FIKIT_OK : FIKIT_HIP_ERROR;
-}
-
-struct Extent {
-  const void* begin;
-  uint64_t bytes;
-};
-bool overlap(const Extent& a, const Extent& b) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a.begin), y = reinterpret_cast<uintptr_t>(b.begin);
-  return a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
-}
 
 constexpr uint64_t MOST_STRIDE = 1ull << 24;      // of a token, in values: places within a tile are 32-bit numbers of bytes
-
-bool vectors_ok(const fikit_vectors* v) {
-  return v && v->d_data && aligned(v->d_data, 16) && v->token_stride % 8 == 0 && v->head_stride % 8 == 0;
-}
-
-// FIKIT_OK, or what is wrong with a cache.
-int cache_status(const fikit_cache* c) {
-  if (!c || !c->d_k || !c->d_v || !c->d_k_exp || !c->d_v_exp || !aligned(c->d_k, 16) || !aligned(c->d_v, 16) || c->n_blocks == 0 ||
-      c->n_blocks > 0x7fffffffu || c->kv_heads == 0)
-    return FIKIT_INVALID_ARG;
-  const uint32_t b = c->block_tokens;
-  if (b < 16 || b > 256 || (b & (b - 1)) || (c->head_dim != 64 && c->head_dim != 128) || c->kv_heads > 65535) return FIKIT_UNSUPPORTED;
-  return FIKIT_OK;
-}
 
 // Calls f<T, D>() for a value type and head size that have been checked.
 template <typename F>
@@ -55,8 +22,6 @@ int with_types(int32_t value_type, uint32_t head_dim, F f) {
   if (value_type == FIKIT_BF16) return head_dim == 128 ? f.template operator()<Bf16, 128>() : f.template operator()<Bf16, 64>();
   return head_dim == 128 ? f.template operator()<F16, 128>() : f.template operator()<F16, 64>();
 }
-
-bool type_ok(int32_t value_type) { return value_type == FIKIT_BF16 || value_type == FIKIT_F16; }
 
 static_assert(APPEND_WAVES * WAVE == 256, "threads of MOST_GROUPS");
 struct AppendCall {

@@ -1,4 +1,4 @@
-// Marshalling of the attention calls (fikit_cache_*, fikit_prompt_attention) for Python, compiled: checks of tensors, output
+// Marshalling of the calls of a language model service (fikit_cache_*, fikit_prompt_attention, fikit_rotate_heads) for Python, compiled: checks of tensors, output
 // tensors, and the C calls, whose addresses binding.py passes in.  A call on the GPU may take 4 us; the same checks and
 // allocations as Python statements take 9.
 //
@@ -23,6 +23,7 @@ decltype(&fikit_cache_append) cache_append;
 decltype(&fikit_cache_attention_workspace_bytes) cache_attention_workspace_bytes;
 decltype(&fikit_cache_attention) cache_attention;
 decltype(&fikit_prompt_attention) prompt_attention;
+decltype(&fikit_rotate_heads) rotate_heads;
 
 const at::Tensor& tensor(PyObject* o, const char* what) {
   TORCH_CHECK_VALUE(THPVariable_Check(o), what, ": a tensor");
@@ -53,12 +54,17 @@ int32_t value_type(const at::Tensor& t, const char* what) {
   return t.scalar_type() == at::kBFloat16 ? FIKIT_BF16 : FIKIT_F16;
 }
 
-// [tokens, heads, head_dim] with the last dimension dense.  (For inference only: an output that silently had no gradient would be wrong.)
+// (For inference only: an output that silently had no gradient would be wrong.)
+void without_gradient(const at::Tensor& t, const char* what) {
+  TORCH_CHECK_VALUE(!(t.requires_grad() && at::GradMode::is_enabled()), what, ": requires a gradient, and there is no backward pass; detach it or use no_grad()");
+}
+
+// [tokens, heads, head_dim] with the last dimension dense.
 fikit_vectors vectors(const at::Tensor& t, at::ScalarType type, const at::Device& device, const char* what) {
   TORCH_CHECK_VALUE(t.dim() == 3 && (t.stride(2) == 1 || t.size(2) <= 1) && t.stride(0) >= 0 && t.stride(1) >= 0 && t.scalar_type() == type &&
                         t.device() == device,
                     what, ": [tokens, heads, head_dim] ", type, " on ", device, ", the last dimension dense");
-  TORCH_CHECK_VALUE(!(t.requires_grad() && at::GradMode::is_enabled()), what, ": requires a gradient, and there is no backward pass; detach it or use no_grad()");
+  without_gradient(t, what);
   // (the stride of a dimension of size one may be anything, and is not used)
   return fikit_vectors{t.data_ptr(), t.size(0) > 1 ? static_cast<uint64_t>(t.stride(0)) : 0, t.size(1) > 1 ? static_cast<uint64_t>(t.stride(1)) : 0};
 }
@@ -282,24 +288,107 @@ PyObject* py_prompt_attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) 
   END_HANDLE_TH_ERRORS
 }
 
-// The addresses of the C calls, in the order of the variables above.
+// q or None, k or None, positions, frequencies or None, status, q_weight or None, k_weight or None, epsilon, neighbours, out, stream
+PyObject* py_rotate_heads(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  need_arguments(n_args, 11);
+  const at::Tensor q = given_or_none(a[0], "q"), k = given_or_none(a[1], "k");
+  TORCH_CHECK_VALUE(q.defined() || k.defined(), "q or k: a tensor");
+  const at::Tensor &any = q.defined() ? q : k, &positions = tensor(a[2], "positions"), frequencies = given_or_none(a[3], "frequencies"),
+                   &status = tensor(a[4], "status"), q_weight = given_or_none(a[5], "q_weight"), k_weight = given_or_none(a[6], "k_weight");
+  const at::Device device = any.device();
+  const at::ScalarType type = any.scalar_type();
+  const int32_t of_values = value_type(any, "q, k");
+  const float epsilon = static_cast<float>(THPUtils_unpackDouble(a[7]));
+  const bool neighbours = truth(a[8]);
+  void* const stream = stream_of(a[10]);
+  at::Tensor q_out, k_out;
+  if (a[9] != Py_None) {
+    TORCH_CHECK_VALUE(PyTuple_Check(a[9]) && PyTuple_GET_SIZE(a[9]) == 2, "out: a RotatedHeads");
+    q_out = given_or_none(PyTuple_GET_ITEM(a[9], 0), "out.q");
+    k_out = given_or_none(PyTuple_GET_ITEM(a[9], 1), "out.k");
+    TORCH_CHECK_VALUE(q_out.defined() == q.defined() && k_out.defined() == k.defined(), "out: a tensor for each one that is given");
+  }
+  fikit_vectors in[2] = {}, out[2] = {};
+  uint32_t heads[2] = {};
+  const at::Tensor* const sides[2][3] = {{&q, &q_out, &q_weight}, {&k, &k_out, &k_weight}};
+  const char* const names[2][3] = {{"q", "out.q", "q_weight"}, {"k", "out.k", "k_weight"}};
+  const void* weights[2] = {};
+  for (int i = 0; i < 2; ++i) {
+    const at::Tensor &x = *sides[i][0], &y = *sides[i][1], &w = *sides[i][2];
+    TORCH_CHECK_VALUE(x.defined() || !w.defined(), names[i][2], ": without heads");
+    if (!x.defined()) continue;
+    in[i] = vectors(x, type, device, names[i][0]);
+    TORCH_CHECK_VALUE(x.size(0) == any.size(0) && x.size(2) == any.size(2), "q, k: [n_tokens, heads, head_dim]");
+    heads[i] = count(x.size(1), names[i][0]);
+    if (y.defined()) {
+      TORCH_CHECK_VALUE(y.sizes() == x.sizes(), names[i][1], ": the shape of its input");
+      out[i] = vectors(y, type, device, names[i][1]);
+    }
+    if (w.defined()) {
+      TORCH_CHECK_VALUE(w.numel() == x.size(2), names[i][2], ": [head_dim]");
+      without_gradient(w, names[i][2]);
+      weights[i] = dense<void>(w, type, device, names[i][2]);
+    }
+  }
+  TORCH_CHECK_VALUE(positions.numel() == any.size(0) && status.numel() == 1, "positions: [n_tokens]; status: [1]");
+  if (frequencies.defined()) without_gradient(frequencies, "frequencies");
+  int rc;
+  {
+    const Unlocked unlocked;
+    if (a[9] == Py_None) {      // one allocation
+      const int64_t of_q = q.defined() ? q.numel() : 0;
+      const at::Tensor all = at::empty({of_q + (k.defined() ? k.numel() : 0)}, at::TensorOptions().dtype(type).device(device));
+      if (q.defined()) q_out = part_of(all, type, 0, q.sizes());
+      if (k.defined()) k_out = part_of(all, type, of_q, k.sizes());
+      if (q.defined()) out[0] = vectors(q_out, type, device, "out.q");
+      if (k.defined()) out[1] = vectors(k_out, type, device, "out.k");
+    }
+    rc = rotate_heads(&in[0], &in[1], heads[0], heads[1], count(any.size(2), "head_dim"), of_values, weights[0], weights[1], epsilon,
+                      dense<int32_t>(positions, at::kInt, device, "positions"),
+                      frequencies.defined() ? dense<float>(frequencies, at::kFloat, device, "frequencies") : nullptr,
+                      frequencies.defined() ? count(2 * frequencies.numel(), "frequencies") : 0, neighbours ? FIKIT_PAIRS_NEIGHBOURS : FIKIT_PAIRS_HALVES,
+                      count(any.size(0), "tokens"), &out[0], &out[1], dense<int32_t>(status, at::kInt, device, "status"), stream);
+  }
+  if (rc != FIKIT_OK) return PyLong_FromLong(rc);
+  if (a[9] != Py_None) {
+    Py_INCREF(a[9]);
+    return a[9];
+  }
+  return Py_BuildValue("(NN)", wrapped(q_out), wrapped(k_out));
+  END_HANDLE_TH_ERRORS
+}
+
+template <typename F>
+void set_address(F& f, PyObject* o) { f = reinterpret_cast<F>(PyLong_AsVoidPtr(o)); }
+
+// The addresses of the C calls around the attention, in the order of the variables above.
+PyObject* py_bind_around(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  need_arguments(n_args, 1);
+  set_address(rotate_heads, a[0]);
+  Py_RETURN_NONE;
+  END_HANDLE_TH_ERRORS
+}
+
+// The addresses of the attention calls, in the order of the variables above.
 PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   HANDLE_TH_ERRORS
   need_arguments(n_args, 7);
-  const auto set = [&](auto& f, int i) { f = reinterpret_cast<std::remove_reference_t<decltype(f)>>(PyLong_AsVoidPtr(a[i])); };
-  set(cache_pieces, 0);
-  set(cache_plan_workspace_bytes, 1);
-  set(cache_plan, 2);
-  set(cache_append, 3);
-  set(cache_attention_workspace_bytes, 4);
-  set(cache_attention, 5);
-  set(prompt_attention, 6);
+  set_address(cache_pieces, a[0]);
+  set_address(cache_plan_workspace_bytes, a[1]);
+  set_address(cache_plan, a[2]);
+  set_address(cache_append, a[3]);
+  set_address(cache_attention_workspace_bytes, a[4]);
+  set_address(cache_attention, a[5]);
+  set_address(prompt_attention, a[6]);
   Py_RETURN_NONE;
   END_HANDLE_TH_ERRORS
 }
 
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_##name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {METHOD(bind), METHOD(cache_plan), METHOD(cache_append), METHOD(cache_attention), METHOD(prompt_attention), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {METHOD(bind), METHOD(cache_plan), METHOD(cache_append), METHOD(cache_attention), METHOD(prompt_attention),
+                         METHOD(bind_around), METHOD(rotate_heads), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_serve_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
