@@ -582,6 +582,13 @@ int fikit_prompt_attention(const fikit_vectors* h_q, const fikit_vectors* h_k, c
  * or waited for, and d_status is looked at and written as there.
  *
  *   fikit_rotate_heads      norm of query and key heads and their rotation by position, between the product and the append
+ *   fikit_cache_fork        requests that are continued once, several times or not at all: their rows of the table, blocks given back
+ *   fikit_cache_compact     the blocks in use moved together
+ *   fikit_cache_copy        what these two want copied, in the caches of all layers
+ *
+ * Nobody keeps count of a block's holders: it is held as long as a row of the table names it within the request's length, and several
+ * rows may (their requests have the same tokens there).  New tokens go into blocks that one request holds alone: fikit_cache_fork leaves every
+ * last block that is not full to one request.
  */
 
 typedef enum fikit_pairs {
@@ -614,6 +621,74 @@ int fikit_rotate_heads(const fikit_vectors* h_q, const fikit_vectors* h_k, uint3
                        int32_t value_type, const void* d_q_weight, const void* d_k_weight, float epsilon, const int32_t* d_positions,
                        const float* d_frequencies, uint32_t rotary_dim, int32_t pairs, uint32_t n_tokens, const fikit_vectors* h_q_out,
                        const fikit_vectors* h_k_out, int32_t* d_status, void* hip_stream);
+
+/* A block to copy.  Lists of these hold -1 in both behind their last entry. */
+typedef struct fikit_block_copy {
+  int32_t from, to;
+} fikit_block_copy;
+
+/* Bytes of device workspace fikit_cache_fork needs for these sizes (0: sizes it does not take). */
+size_t fikit_cache_fork_workspace_bytes(uint32_t n_requests, uint32_t n_children, uint32_t n_blocks);
+
+/*
+ * The requests of the next step from those of the last: child i continues request d_parents[i], with all its tokens; several children may
+ * continue one request, and a request that none continues has ended.  -1 makes an empty request.
+ *
+ *   d_block_table    [n_requests][table_width], d_lengths [n_requests]: as fikit_cache_plan leaves them; what lies behind a request's
+ *                    blocks is not looked at.  n_requests, n_children up to 16,384.
+ *   n_blocks         of the cache, up to 2^20.
+ *   d_free           [n_free] blocks that nobody holds, n_free <= n_blocks.
+ *   d_new_table      [n_children][table_width] receives the children's rows, -1 behind their blocks.  Full blocks are shared.  If a request's
+ *                    last block is not full, it stays with its first child (the lowest), and each later one gets a block of its own.
+ *   d_new_lengths    [n_children].
+ *   d_copies         [n_children] receives what fikit_cache_copy has to copy before new tokens come, in the order of the children.
+ *   d_new_free       [n_blocks] receives the free blocks that are left, -1 behind them: blocks are taken from the front of d_free and behind it
+ *                    those given back, in ascending order, and these two without the taken ones are the new list.
+ *   d_counts         [3] receives the number of blocks taken, given back, and free.
+ *                    Outputs overlap neither each other nor an input (INVALID_ARG).
+ *   d_workspace      256-byte aligned, at least fikit_cache_fork_workspace_bytes(...) bytes.
+ *
+ * Through d_status: INVALID_ARG (a parent, a length or a block that cannot be), CACHE_FULL if too few blocks are free.
+ */
+int fikit_cache_fork(const int32_t* d_block_table, uint32_t table_width, const int32_t* d_lengths, uint32_t n_requests,
+                     const int32_t* d_parents, uint32_t n_children, uint32_t block_tokens, uint32_t n_blocks, const int32_t* d_free,
+                     uint32_t n_free, int32_t* d_new_table, int32_t* d_new_lengths, fikit_block_copy* d_copies, int32_t* d_new_free,
+                     int32_t* d_counts, int32_t* d_status, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Bytes of device workspace fikit_cache_compact needs for these sizes (0: sizes it does not take). */
+size_t fikit_cache_compact_workspace_bytes(uint32_t n_requests, uint32_t n_blocks);
+
+/*
+ * Compaction: of the blocks in use and the free ones together, the lowest ones are in use afterwards, so that the rest can be given
+ * away in one piece.  (Blocks that are neither stay where they are.)
+ *
+ *   d_block_table, d_lengths, n_blocks, d_free   as for fikit_cache_fork.  A block that is both free and in use, or free twice, is
+ *                    INVALID_ARG through d_status.
+ *   d_new_table      [n_requests][table_width] receives the rows, -1 behind a request's blocks.
+ *   d_copies         [min(n_free, n_blocks / 2)] receives the blocks to copy, ascending on both sides: with n_used distinct blocks in use and the
+ *                    border behind the n_used lowest of all, the k-th one in use behind the border goes to the k-th free one before it.
+ *                    Nobody may write the cache before fikit_cache_copy has copied them.
+ *   d_new_free       [n_free] receives the free blocks, ascending: all that lie behind the border.
+ *   d_counts         [2] receives the number of copies and n_used.
+ *                    Outputs overlap neither each other nor an input (INVALID_ARG).
+ *   d_workspace      256-byte aligned, at least fikit_cache_compact_workspace_bytes(...) bytes.
+ */
+int fikit_cache_compact(const int32_t* d_block_table, uint32_t table_width, const int32_t* d_lengths, uint32_t n_requests,
+                        uint32_t block_tokens, uint32_t n_blocks, const int32_t* d_free, uint32_t n_free, int32_t* d_new_table,
+                        fikit_block_copy* d_copies, int32_t* d_new_free, int32_t* d_counts, int32_t* d_status, void* d_workspace,
+                        size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Copies blocks, codes and exponents of keys and values, in each of n_caches caches of the same sizes (those of a model's layers).
+ *
+ *   h_caches         [n_caches]; they must not overlap.
+ *   d_copies         [n_copies]; an entry of -1 in both, or of a block to itself, copies nothing.  No block is written by two entries that copy, or
+ *                    read by one and written by another.
+ *
+ * Through d_status: INVALID_ARG for a block outside the cache.
+ */
+int fikit_cache_copy(const fikit_cache* h_caches, uint32_t n_caches, const fikit_block_copy* d_copies, uint32_t n_copies,
+                     int32_t* d_status, void* hip_stream);
 
 const char* fikit_status_string(int status);
 int fikit_version(void);

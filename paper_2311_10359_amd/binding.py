@@ -35,7 +35,8 @@ EXPORTS = ("fikit_profile_workspace_bytes", "fikit_profile", "fikit_gapfill_work
            "fikit_pairing_best", "fikit_profile_merge_workspace_bytes", "fikit_profile_merge", "fikit_status_string", "fikit_version", "fikit_set_wait_limit",
            "fikit_trace_enable", "fikit_trace_read", "fikit_cache_pieces", "fikit_cache_plan_workspace_bytes", "fikit_cache_plan",
            "fikit_cache_append", "fikit_cache_attention_workspace_bytes", "fikit_cache_attention", "fikit_prompt_attention",
-           "fikit_rotate_heads")
+           "fikit_rotate_heads", "fikit_cache_fork_workspace_bytes", "fikit_cache_fork", "fikit_cache_compact_workspace_bytes",
+           "fikit_cache_compact", "fikit_cache_copy")
 
 # Layout of a profile row as seen from numpy (128 bytes; see fikit_row in fikit.h).
 STATS_DTYPE = np.dtype([("count", "<u8"), ("sum", "<u8"), ("min", "<i8"), ("max", "<i8"),
@@ -146,6 +147,16 @@ def load() -> ctypes.CDLL:
         lib.fikit_prompt_attention.argtypes = [p_vec, p_vec, p_vec, u32, u32, u32, i32, f32, vp, u32, u32, vp, vp, vp, vp]
         lib.fikit_rotate_heads.restype = ctypes.c_int
         lib.fikit_rotate_heads.argtypes = [p_vec, p_vec, u32, u32, u32, i32, vp, vp, f32, vp, vp, u32, i32, u32, p_vec, p_vec, vp, vp]
+        lib.fikit_cache_fork_workspace_bytes.restype = sz
+        lib.fikit_cache_fork_workspace_bytes.argtypes = [u32, u32, u32]
+        lib.fikit_cache_fork.restype = ctypes.c_int
+        lib.fikit_cache_fork.argtypes = [vp, u32, vp, u32, vp, u32, u32, u32, vp, u32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        lib.fikit_cache_compact_workspace_bytes.restype = sz
+        lib.fikit_cache_compact_workspace_bytes.argtypes = [u32, u32]
+        lib.fikit_cache_compact.restype = ctypes.c_int
+        lib.fikit_cache_compact.argtypes = [vp, u32, vp, u32, u32, u32, vp, u32, vp, vp, vp, vp, vp, vp, sz, vp]
+        lib.fikit_cache_copy.restype = ctypes.c_int
+        lib.fikit_cache_copy.argtypes = [p_cache, u32, vp, u32, vp, vp]
         lib.fikit_status_string.restype = ctypes.c_char_p
         lib.fikit_status_string.argtypes = [ctypes.c_int]
         lib.fikit_version.restype = ctypes.c_int
@@ -623,7 +634,9 @@ def _marshal():
         _serve_marshal.bind(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in (
             "fikit_cache_pieces", "fikit_cache_plan_workspace_bytes", "fikit_cache_plan", "fikit_cache_append",
             "fikit_cache_attention_workspace_bytes", "fikit_cache_attention", "fikit_prompt_attention")))
-        _serve_marshal.bind_around(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in ("fikit_rotate_heads",)))
+        _serve_marshal.bind_around(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in (
+            "fikit_rotate_heads", "fikit_cache_fork_workspace_bytes", "fikit_cache_fork", "fikit_cache_compact_workspace_bytes",
+            "fikit_cache_compact", "fikit_cache_copy")))
         _native = _serve_marshal
     return _native
 
@@ -736,6 +749,71 @@ def fikit_rotate_heads(q: Optional[torch.Tensor], k: Optional[torch.Tensor], pos
     got = (_native or _marshal()).rotate_heads(q, k, positions, frequencies, status, q_weight, k_weight, epsilon, neighbours, out,
                                                _stream_of(device.index))
     return _outputs(RotatedHeads, got, "fikit_rotate_heads")
+
+
+class CacheFork(NamedTuple):
+    """Allocated by a call, these are parts of one piece of memory."""
+    block_table: torch.Tensor       # int32 [children, width]
+    lengths: torch.Tensor           # int32 [children]
+    copies: torch.Tensor            # int32 [children, 2]: from, to; -1 behind the last one
+    free_blocks: torch.Tensor       # int32 [n_blocks]; -1 behind the last one
+    counts: torch.Tensor            # int32 [3]: blocks taken, given back, free
+
+
+def fikit_cache_fork_workspace_bytes(n_requests: int, n_children: int, n_blocks: int) -> int:
+    return int(load().fikit_cache_fork_workspace_bytes(n_requests, n_children, n_blocks))
+
+
+def fikit_cache_fork(block_table: torch.Tensor, lengths: torch.Tensor, parents: torch.Tensor, block_tokens: int, n_blocks: int,
+                     free_blocks: torch.Tensor, status: torch.Tensor, *, out: Optional[CacheFork] = None,
+                     workspace_buf: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> CacheFork:
+    """block_table: int32 [R, width]; lengths: int32 [R]; parents: int32 [children], -1 for an empty request; free_blocks: int32 [F].
+    Output tensors are allocated unless given, and then overlap neither each other nor what is read."""
+    context = _elsewhere(stream, block_table.device)
+    if context is not None:
+        with context:
+            return fikit_cache_fork(block_table, lengths, parents, block_tokens, n_blocks, free_blocks, status, out=out, workspace_buf=workspace_buf)
+    got = (_native or _marshal()).cache_fork(block_table, lengths, parents, block_tokens, n_blocks, free_blocks, status, out, workspace_buf,
+                                             _stream_of(block_table.device.index))
+    return _outputs(CacheFork, got, "fikit_cache_fork")
+
+
+class CacheCompaction(NamedTuple):
+    """Allocated by a call, these are parts of one piece of memory."""
+    block_table: torch.Tensor       # int32 [R, width]
+    copies: torch.Tensor            # int32 [min(F, n_blocks / 2), 2]: from, to; -1 behind the last one
+    free_blocks: torch.Tensor       # int32 [F]
+    counts: torch.Tensor            # int32 [2]: copies, blocks in use
+
+
+def fikit_cache_compact_workspace_bytes(n_requests: int, n_blocks: int) -> int:
+    return int(load().fikit_cache_compact_workspace_bytes(n_requests, n_blocks))
+
+
+def fikit_cache_compact(block_table: torch.Tensor, lengths: torch.Tensor, block_tokens: int, n_blocks: int, free_blocks: torch.Tensor,
+                        status: torch.Tensor, *, out: Optional[CacheCompaction] = None, workspace_buf: Optional[torch.Tensor] = None,
+                        stream: Optional[torch.cuda.Stream] = None) -> CacheCompaction:
+    """block_table: int32 [R, width]; lengths: int32 [R]; free_blocks: int32 [F].  Output tensors are allocated unless given, and then
+    overlap neither each other nor what is read."""
+    context = _elsewhere(stream, block_table.device)
+    if context is not None:
+        with context:
+            return fikit_cache_compact(block_table, lengths, block_tokens, n_blocks, free_blocks, status, out=out, workspace_buf=workspace_buf)
+    got = (_native or _marshal()).cache_compact(block_table, lengths, block_tokens, n_blocks, free_blocks, status, out, workspace_buf,
+                                                _stream_of(block_table.device.index))
+    return _outputs(CacheCompaction, got, "fikit_cache_compact")
+
+
+def fikit_cache_copy(caches, copies: torch.Tensor, status: torch.Tensor, *, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """caches: a sequence of (k_cache, v_cache, k_exp, v_exp) of the same sizes, written in place; copies: int32 [n, 2], as fikit_cache_fork or
+    fikit_cache_compact leaves them."""
+    context = _elsewhere(stream, copies.device)
+    if context is not None:
+        with context:
+            return fikit_cache_copy(caches, copies, status)
+    st = (_native or _marshal()).cache_copy(caches, copies, status, _stream_of(copies.device.index))
+    if st != FIKIT_OK:
+        raise FikitError(st, "fikit_cache_copy")
 
 
 # ---- helpers to move host arrays in and out (marshalling only) ---------------------------------

@@ -3,6 +3,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include "blocks_kernels.hip.h"
 #include "rotate_kernels.hip.h"
 #include "serve_host.h"
 
@@ -36,9 +37,193 @@ bool rotates_in_place_or_elsewhere(const fikit_vectors* in, const fikit_vectors*
   return in->d_data != out->d_data || ((heads <= 1 || in->head_stride == out->head_stride) && (n_tokens <= 1 || in->token_stride == out->token_stride));
 }
 
+// Parts of the workspace of a fork or a compaction, one behind the other.
+struct Parts {
+  uint64_t bytes = 0;
+  uint64_t take(uint64_t count) {
+    const uint64_t at = bytes;
+    bytes += (4 * count + 255) / 256 * 256;
+    return at;
+  }
+};
+struct ForkParts : Parts {
+  uint64_t words, marks, marks_too, first, rank, wants;
+  ForkParts(uint32_t n_requests, uint32_t n_children, uint32_t n_blocks) : words((n_blocks + 31) / 32) {
+    take(1);
+    marks = take(words);
+    marks_too = take(words);
+    first = take(n_requests);
+    rank = take(n_children);
+    wants = take(n_children);
+  }
+};
+struct CompactParts : Parts {
+  uint64_t words, marks, marks_too, before;
+  explicit CompactParts(uint32_t n_blocks) : words((n_blocks + 31) / 32) {
+    take(2);
+    marks = take(words);
+    marks_too = take(words);
+    before = take(words);
+  }
+};
+
+bool blocks_fit(uint32_t n_requests, uint32_t n_children, uint32_t n_blocks) {
+  return n_requests <= BLOCKS_MOST_REQUESTS && n_children <= BLOCKS_MOST_REQUESTS && n_blocks <= BLOCKS_MOST_BLOCKS;
+}
+
+// FIKIT_OK, or what is wrong with the inputs that fork and compaction share.
+int blocks_status(const int32_t* d_block_table, uint32_t table_width, const int32_t* d_lengths, uint32_t n_requests, uint32_t n_children,
+                  uint32_t block_tokens, uint32_t n_blocks, const int32_t* d_free, uint32_t n_free, const int32_t* d_status) {
+  if (!d_status || !aligned(d_status, 4) || n_blocks == 0 || n_free > n_blocks || table_width > 0x7fffffffu) return FIKIT_INVALID_ARG;
+  if (n_requests > 0 && (!d_lengths || (table_width > 0 && !d_block_table))) return FIKIT_INVALID_ARG;
+  if (n_free > 0 && !d_free) return FIKIT_INVALID_ARG;
+  if (!aligned(d_block_table, 4) || !aligned(d_lengths, 4) || !aligned(d_free, 4)) return FIKIT_INVALID_ARG;
+  if (block_tokens < 16 || block_tokens > 256 || (block_tokens & (block_tokens - 1))) return FIKIT_UNSUPPORTED;
+  return blocks_fit(n_requests, n_children, n_blocks) ? FIKIT_OK : FIKIT_UNSUPPORTED;
+}
+
+// The first `outputs` of n extents overlap neither each other nor those behind them.
+bool outputs_apart(const Extent* extents, int outputs, int n) {
+  for (int out = 0; out < outputs; ++out)
+    for (int other = out + 1; other < n; ++other)
+      if (overlap(extents[out], extents[other])) return false;
+  return true;
+}
+
+BlocksArgs blocks_args(const int32_t* d_block_table, uint32_t table_width, const int32_t* d_lengths, uint32_t n_requests, uint32_t block_tokens,
+                       uint32_t n_blocks, const int32_t* d_free, uint32_t n_free, int32_t* d_status) {
+  BlocksArgs a{};
+  a.table = d_block_table;
+  a.lengths = d_lengths;
+  a.free_blocks = d_free;
+  a.status = d_status;
+  a.n_requests = n_requests;
+  a.width = table_width;
+  a.n_blocks = n_blocks;
+  a.n_free = n_free;
+  a.words = (n_blocks + 31) / 32;
+  a.shift = static_cast<uint32_t>(__builtin_ctz(block_tokens));
+  return a;
+}
+
+constexpr uint32_t CLEAR_GROUPS = 8;
+constexpr uint32_t COPY_GROUPS = 4096;
+
 }  // namespace
 
 extern "C" {
+
+size_t fikit_cache_fork_workspace_bytes(uint32_t n_requests, uint32_t n_children, uint32_t n_blocks) {
+  return blocks_fit(n_requests, n_children, n_blocks) ? static_cast<size_t>(ForkParts(n_requests, n_children, n_blocks).bytes) : 0;
+}
+
+int fikit_cache_fork(const int32_t* d_block_table, uint32_t table_width, const int32_t* d_lengths, uint32_t n_requests,
+                     const int32_t* d_parents, uint32_t n_children, uint32_t block_tokens, uint32_t n_blocks, const int32_t* d_free,
+                     uint32_t n_free, int32_t* d_new_table, int32_t* d_new_lengths, fikit_block_copy* d_copies, int32_t* d_new_free,
+                     int32_t* d_counts, int32_t* d_status, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+  if (int rc = blocks_status(d_block_table, table_width, d_lengths, n_requests, n_children, block_tokens, n_blocks, d_free, n_free, d_status)) return rc;
+  if (n_children > 0 && (!d_parents || !d_new_lengths || !d_copies || (table_width > 0 && !d_new_table))) return FIKIT_INVALID_ARG;
+  if (!d_new_free || !d_counts || !d_workspace || !aligned(d_parents, 4) || !aligned(d_new_table, 4) || !aligned(d_new_lengths, 4) ||
+      !aligned(d_copies, 8) || !aligned(d_new_free, 4) || !aligned(d_counts, 4) || !aligned(d_workspace, 256))
+    return FIKIT_INVALID_ARG;
+  const uint64_t row = 4ull * table_width;
+  const Extent extents[] = {{d_new_table, row * n_children}, {d_new_lengths, 4ull * n_children}, {d_copies, sizeof(fikit_block_copy) * n_children},
+                            {d_new_free, 4ull * n_blocks}, {d_counts, 12}, {d_block_table, row * n_requests}, {d_lengths, 4ull * n_requests},
+                            {d_parents, 4ull * n_children}, {d_free, 4ull * n_free}};
+  if (!outputs_apart(extents, 5, 9)) return FIKIT_INVALID_ARG;
+  const ForkParts parts(n_requests, n_children, n_blocks);
+  if (workspace_bytes < parts.bytes) return FIKIT_WORKSPACE_TOO_SMALL;
+  BlocksArgs a = blocks_args(d_block_table, table_width, d_lengths, n_requests, block_tokens, n_blocks, d_free, n_free, d_status);
+  const auto part = [&](uint64_t at) { return reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(d_workspace) + at); };
+  a.parents = d_parents;
+  a.new_table = d_new_table;
+  a.new_lengths = d_new_lengths;
+  a.copies = reinterpret_cast<int2*>(d_copies);
+  a.new_free = d_new_free;
+  a.counts = d_counts;
+  a.words_of_call = part(0);
+  a.marks = part(parts.marks);
+  a.marks_too = part(parts.marks_too);
+  a.first = part(parts.first);
+  a.rank = reinterpret_cast<int32_t*>(part(parts.rank));
+  a.wants = part(parts.wants);
+  a.n_children = n_children;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (int rc = enqueue(k_fork_begin, dim3(1 + CLEAR_GROUPS), dim3(BLOCKS_THREADS), st, a)) return rc;
+  if (const uint32_t rows = n_requests + n_children)
+    if (int rc = enqueue(k_fork_rows, dim3((rows + ROW_WAVES - 1) / ROW_WAVES), dim3(ROW_WAVES * WAVE), st, a)) return rc;
+  return enqueue(k_fork_end, dim3((a.words + SLICE - 1) / SLICE), dim3(BLOCKS_THREADS), st, a);
+}
+
+size_t fikit_cache_compact_workspace_bytes(uint32_t n_requests, uint32_t n_blocks) {
+  return blocks_fit(n_requests, 0, n_blocks) ? static_cast<size_t>(CompactParts(n_blocks).bytes) : 0;
+}
+
+int fikit_cache_compact(const int32_t* d_block_table, uint32_t table_width, const int32_t* d_lengths, uint32_t n_requests,
+                        uint32_t block_tokens, uint32_t n_blocks, const int32_t* d_free, uint32_t n_free, int32_t* d_new_table,
+                        fikit_block_copy* d_copies, int32_t* d_new_free, int32_t* d_counts, int32_t* d_status, void* d_workspace,
+                        size_t workspace_bytes, void* hip_stream) {
+  if (int rc = blocks_status(d_block_table, table_width, d_lengths, n_requests, 0, block_tokens, n_blocks, d_free, n_free, d_status)) return rc;
+  const uint32_t room = n_free < n_blocks / 2 ? n_free : n_blocks / 2;
+  if ((n_requests > 0 && table_width > 0 && !d_new_table) || (room > 0 && !d_copies) || (n_free > 0 && !d_new_free)) return FIKIT_INVALID_ARG;
+  if (!d_counts || !d_workspace || !aligned(d_new_table, 4) || !aligned(d_copies, 8) || !aligned(d_new_free, 4) || !aligned(d_counts, 4) ||
+      !aligned(d_workspace, 256))
+    return FIKIT_INVALID_ARG;
+  const uint64_t table = 4ull * table_width * n_requests;
+  const Extent extents[] = {{d_new_table, table}, {d_copies, sizeof(fikit_block_copy) * room}, {d_new_free, 4ull * n_free}, {d_counts, 8},
+                            {d_block_table, table}, {d_lengths, 4ull * n_requests}, {d_free, 4ull * n_free}};
+  if (!outputs_apart(extents, 4, 7)) return FIKIT_INVALID_ARG;
+  const CompactParts parts(n_blocks);
+  if (workspace_bytes < parts.bytes) return FIKIT_WORKSPACE_TOO_SMALL;
+  BlocksArgs a = blocks_args(d_block_table, table_width, d_lengths, n_requests, block_tokens, n_blocks, d_free, n_free, d_status);
+  const auto part = [&](uint64_t at) { return reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(d_workspace) + at); };
+  a.new_table = d_new_table;
+  a.copies = reinterpret_cast<int2*>(d_copies);
+  a.new_free = d_new_free;
+  a.counts = d_counts;
+  a.words_of_call = part(0);
+  a.marks = part(parts.marks);
+  a.marks_too = part(parts.marks_too);
+  a.before = part(parts.before);
+  a.room = room;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  const dim3 rows(ROW_WAVES * WAVE);
+  const uint32_t waves = n_requests + (n_free + WAVE - 1) / WAVE;
+  if (int rc = enqueue(k_compact_begin, dim3(CLEAR_GROUPS), dim3(BLOCKS_THREADS), st, a)) return rc;
+  if (waves > 0)
+    if (int rc = enqueue(k_compact_mark, dim3((waves + ROW_WAVES - 1) / ROW_WAVES), rows, st, a)) return rc;
+  if (int rc = enqueue(k_compact_lists, dim3((a.words + SLICE - 1) / SLICE), dim3(BLOCKS_THREADS), st, a)) return rc;
+  return n_requests > 0 ? enqueue(k_compact_rows, dim3((n_requests + ROW_WAVES - 1) / ROW_WAVES), rows, st, a) : FIKIT_OK;
+}
+
+int fikit_cache_copy(const fikit_cache* h_caches, uint32_t n_caches, const fikit_block_copy* d_copies, uint32_t n_copies,
+                     int32_t* d_status, void* hip_stream) {
+  if (!d_status || !aligned(d_status, 4) || !aligned(d_copies, 8) || n_copies > 0x7fffffffu || (n_caches > 0 && !h_caches)) return FIKIT_INVALID_ARG;
+  for (uint32_t i = 0; i < n_caches; ++i) {
+    if (int rc = cache_status(h_caches + i)) return rc;
+    const fikit_cache &c = h_caches[i], &one = h_caches[0];
+    if (c.n_blocks != one.n_blocks || c.kv_heads != one.kv_heads || c.block_tokens != one.block_tokens || c.head_dim != one.head_dim) return FIKIT_INVALID_ARG;
+  }
+  if (n_caches == 0 || n_copies == 0) return FIKIT_OK;
+  if (!d_copies) return FIKIT_INVALID_ARG;
+  CopyArgs a{};
+  a.copies = reinterpret_cast<const int2*>(d_copies);
+  a.status = d_status;
+  a.n_blocks = h_caches->n_blocks;
+  a.heads = h_caches->kv_heads;
+  a.block_bytes = a.heads * h_caches->block_tokens * h_caches->head_dim;      // (below 2^31)
+  a.chunks = (a.block_bytes + COPY_CHUNK - 1) / COPY_CHUNK;
+  a.n_copies = n_copies;
+  for (uint32_t from = 0; from < n_caches; from += COPY_CACHES) {
+    const uint32_t n = n_caches - from < COPY_CACHES ? n_caches - from : COPY_CACHES;
+    for (uint32_t i = 0; i < n; ++i) a.caches[i] = {h_caches[from + i].d_k, h_caches[from + i].d_v, h_caches[from + i].d_k_exp, h_caches[from + i].d_v_exp};
+    a.per_copy = 2 * n * a.chunks;                   // (at most 64 * 2^17)
+    const uint32_t most = COPY_GROUPS / a.per_copy;
+    a.step = most < 1 ? 1 : most < n_copies ? most : n_copies;
+    if (int rc = enqueue(k_cache_copy, dim3(a.per_copy * a.step), dim3(COPY_THREADS), static_cast<hipStream_t>(hip_stream), a)) return rc;
+  }
+  return FIKIT_OK;
+}
 
 int fikit_rotate_heads(const fikit_vectors* h_q, const fikit_vectors* h_k, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim,
                        int32_t value_type, const void* d_q_weight, const void* d_k_weight, float epsilon, const int32_t* d_positions,

@@ -1,0 +1,370 @@
+// Blocks of the paged cache: requests that fork and end, compaction, copies.
+#pragma once
+
+#include "serve_common.hip.h"
+
+namespace fikit {
+
+// Nobody counts who holds a block: what is held follows from the table and the lengths, so a call marks blocks in bitmaps of its own and the
+// order of its marks changes nothing.  With L = a request's length and B = tokens per block it holds the first ceil(L / B) entries of
+// its row.
+//
+// Four bytes are read for an entry and four written for an entry of the new table: bound by the latency of launches and of loads one
+// behind the other.
+
+struct BlocksArgs {
+  const int32_t* table;
+  const int32_t* lengths;
+  const int32_t* parents;
+  const int32_t* free_blocks;
+  int32_t* new_table;
+  int32_t* new_lengths;
+  int2* copies;
+  int32_t* new_free;
+  int32_t* counts;
+  int32_t* status;
+  uint32_t* marks;          // fork: blocks of requests that nobody continues; compaction: used blocks
+  uint32_t* marks_too;      // fork: blocks of the others; compaction: free ones
+  uint32_t* first;          // fork, [n_requests]: a request's first child, or NO_CHILD
+  int32_t* rank;            // fork, [n_children]: a child's place among those that need a block for a copy, or -1
+  uint32_t* wants;          // fork, [n_children]: the child of a place
+  uint32_t* before;         // compaction, [words]: used blocks before a word's
+  uint32_t* words_of_call;  // fork: blocks taken; compaction: the border, used blocks before it
+  uint32_t n_requests, n_children, width, n_blocks, n_free, room, words;
+  uint32_t shift;           // of the block length
+};
+
+constexpr int BLOCKS_THREADS = 1024, ROW_WAVES = 4;
+constexpr uint32_t BLOCKS_MOST_REQUESTS = 16384, BLOCKS_MOST_BLOCKS = 1u << 20;
+constexpr uint32_t SLICE = 256;                // words of the bitmaps whose blocks a workgroup lists
+constexpr uint32_t NO_CHILD = 0xffffffffu;
+
+__device__ __forceinline__ uint32_t pages_of(const BlocksArgs& a, uint32_t length) { return (length + (1u << a.shift) - 1) >> a.shift; }
+
+// Can a request be that long?  (no more entries than its row of the table has)
+__device__ __forceinline__ bool length_ok(const BlocksArgs& a, int32_t length) {
+  return length >= 0 && (static_cast<uint64_t>(length) + (1u << a.shift) - 1) >> a.shift <= a.width;
+}
+
+__device__ __forceinline__ void mark(uint32_t* marks, uint32_t block) {
+  __hip_atomic_fetch_or(marks + block / 32, 1u << block % 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+__device__ __forceinline__ void clear_marks(const BlocksArgs& a, uint32_t from, uint32_t stride) {
+  for (uint32_t i = from; i < a.words; i += stride) a.marks[i] = a.marks_too[i] = 0;
+}
+
+// ---- fork -------------------------------------------------------------------------------------------------------
+//
+// Child i continues request parents[i].  The first child keeps the parent's last block if that is not full, each later one needs a block:
+// its place among those is a prefix sum over the children.  Blocks to take come from the front of (free blocks, blocks given back in
+// ascending order); what is left of the two is the new list.
+
+// The children, in one workgroup; the others clear the bitmaps.
+__global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_begin(BlocksArgs a) {
+  __shared__ uint32_t first[BLOCKS_MOST_REQUESTS];
+  __shared__ uint32_t scan[BLOCKS_THREADS / WAVE];
+  if (blockIdx.x > 0) {
+    clear_marks(a, (blockIdx.x - 1) * BLOCKS_THREADS + threadIdx.x, (gridDim.x - 1) * BLOCKS_THREADS);
+    return;
+  }
+  if (stopped(a.status)) return;               // (nobody else writes it in this launch)
+  bool bad = false;
+  for (uint32_t r = threadIdx.x; r < a.n_requests; r += BLOCKS_THREADS) {
+    first[r] = NO_CHILD;
+    bad |= !length_ok(a, a.lengths[r]);
+  }
+  __syncthreads();
+  for (uint32_t c = threadIdx.x; c < a.n_children; c += BLOCKS_THREADS) {
+    const int32_t p = a.parents[c];
+    if (p >= 0 && static_cast<uint32_t>(p) < a.n_requests) atomicMin(&first[p], c);
+    bad |= p < -1 || (p >= 0 && static_cast<uint32_t>(p) >= a.n_requests);
+  }
+  if (__syncthreads_or(bad)) {
+    if (threadIdx.x == 0) *a.status = FIKIT_INVALID_ARG;
+    return;
+  }
+  for (uint32_t r = threadIdx.x; r < a.n_requests; r += BLOCKS_THREADS) a.first[r] = first[r];
+  uint32_t taken = 0;
+  for (uint32_t base = 0; base < a.n_children; base += BLOCKS_THREADS) {
+    const uint32_t c = base + threadIdx.x;
+    const int32_t p = c < a.n_children ? a.parents[c] : -1;
+    const int32_t length = p >= 0 ? a.lengths[p] : 0;
+    const bool need = p >= 0 && (static_cast<uint32_t>(length) & ((1u << a.shift) - 1)) && first[p] != c;
+    uint32_t total;
+    const uint32_t place = taken + block_excl_scan_1024(need, scan, total);
+    if (c < a.n_children) {
+      a.new_lengths[c] = length;
+      a.rank[c] = need ? static_cast<int32_t>(place) : -1;
+      if (need) a.wants[place] = c;
+    }
+    taken += total;
+  }
+  if (threadIdx.x == 0) a.words_of_call[0] = taken;
+}
+
+// A wave for each request, which marks its blocks, and for each child, which writes its row.
+__global__ __launch_bounds__(ROW_WAVES * WAVE) void k_fork_rows(BlocksArgs a) {
+  if (stopped(a.status)) return;
+  const uint32_t lane = lane_id(), row = blockIdx.x * ROW_WAVES + uniform(threadIdx.x / WAVE);
+  if (row < a.n_requests) {
+    const uint32_t pages = pages_of(a, static_cast<uint32_t>(a.lengths[row]));
+    uint32_t* marks = a.first[row] == NO_CHILD ? a.marks : a.marks_too;
+    const int32_t* entries = a.table + static_cast<uint64_t>(row) * a.width;
+    for (uint32_t page = lane; page < pages; page += WAVE) {
+      const uint32_t block = static_cast<uint32_t>(entries[page]);
+      if (block < a.n_blocks) mark(marks, block);
+      else *a.status = FIKIT_INVALID_ARG;
+    }
+    return;
+  }
+  const uint32_t c = row - a.n_requests;
+  if (c >= a.n_children) return;
+  const int32_t p = a.parents[c], rank = a.rank[c];
+  const uint32_t pages = p >= 0 ? pages_of(a, static_cast<uint32_t>(a.lengths[p])) : 0;
+  const int32_t* entries = a.table + static_cast<uint64_t>(p >= 0 ? p : 0) * a.width;
+  int32_t* out = a.new_table + static_cast<uint64_t>(c) * a.width;
+  for (uint32_t page = lane; page < a.width; page += WAVE) {
+    int32_t block = page < pages ? entries[page] : -1;
+    if (page + 1 == pages && rank >= 0) {
+      a.copies[rank].x = block;
+      if (static_cast<uint32_t>(rank) < a.n_free) {
+        block = a.free_blocks[rank];
+        if (static_cast<uint32_t>(block) >= a.n_blocks) *a.status = FIKIT_INVALID_ARG;
+        a.copies[rank].y = block;
+      }                                          // (else what is given back says which: k_fork_end)
+    }
+    out[page] = block;
+  }
+}
+
+// The sums of N counts over the words of the bitmaps, in every workgroup: those of the words before each word of the workgroup's slice, in LDS,
+// and of all words.  count(word, out) gives the counts of a word, of which there are up to 1024 to a thread.
+template <int N>
+struct WordSums {
+  uint32_t before[SLICE][N];
+  uint32_t scan[BLOCKS_THREADS / WAVE];
+};
+template <int N, typename F>
+__device__ __forceinline__ void word_sums(uint32_t words, uint32_t slice, WordSums<N>* lds, uint32_t (&mine)[N], uint32_t (&total)[N], F count) {
+  const uint32_t per = (words + BLOCKS_THREADS - 1) / BLOCKS_THREADS, from = threadIdx.x * per, to = min_u32(from + per, words);
+  uint32_t sums[N] = {};
+  for (uint32_t w = from; w < to; ++w) {
+    uint32_t of[N];
+    count(w, of);
+    for (int i = 0; i < N; ++i) sums[i] += of[i];
+  }
+  for (int i = 0; i < N; ++i) mine[i] = block_excl_scan_1024(sums[i], lds->scan, total[i]);
+  uint32_t at[N];
+  for (int i = 0; i < N; ++i) at[i] = mine[i];
+  if (from < slice + SLICE && to > slice)
+    for (uint32_t w = from; w < to; ++w) {
+      if (w >= slice && w < slice + SLICE)
+        for (int i = 0; i < N; ++i) lds->before[w - slice][i] = at[i];
+      uint32_t of[N];
+      count(w, of);
+      for (int i = 0; i < N; ++i) at[i] += of[i];
+    }
+  __syncthreads();
+}
+
+// The lists.
+__global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_end(BlocksArgs a) {
+  __shared__ WordSums<1> sums;
+  if (__syncthreads_or(stopped(a.status))) return;
+  const uint32_t slice = blockIdx.x * SLICE, taken = a.words_of_call[0];
+  uint32_t mine[1], given[1];
+  word_sums<1>(a.words, slice, &sums, mine, given, [&](uint32_t w, uint32_t (&of)[1]) { of[0] = __popc(a.marks[w] & ~a.marks_too[w]); });
+  const uint32_t total = a.n_free + given[0];          // (below 2^32: n_free is at most n_blocks)
+  if (taken > total || total - taken > a.n_blocks) {   // (too few; or a list that names blocks in use)
+    if (threadIdx.x == 0) *a.status = taken > total ? FIKIT_CACHE_FULL : FIKIT_INVALID_ARG;
+    return;
+  }
+  for (uint32_t i = threadIdx.x; i < SLICE * 32; i += BLOCKS_THREADS) {
+    const uint32_t w = slice + i / 32;
+    if (w >= a.words) break;
+    const uint32_t marks = a.marks[w] & ~a.marks_too[w], bit = 1u << i % 32;
+    if (!(marks & bit)) continue;
+    const uint32_t place = a.n_free + sums.before[i / 32][0] + __popc(marks & (bit - 1)), block = w * 32 + i % 32;
+    if (place >= taken) {
+      a.new_free[place - taken] = static_cast<int32_t>(block);
+    } else {
+      const uint32_t c = a.wants[place];
+      a.copies[place].y = static_cast<int32_t>(block);
+      a.new_table[static_cast<uint64_t>(c) * a.width + pages_of(a, static_cast<uint32_t>(a.new_lengths[c])) - 1] = static_cast<int32_t>(block);
+    }
+  }
+  const uint32_t from = blockIdx.x * BLOCKS_THREADS + threadIdx.x, stride = gridDim.x * BLOCKS_THREADS;
+  for (uint32_t i = taken + from; i < a.n_free; i += stride) a.new_free[i - taken] = a.free_blocks[i];
+  for (uint32_t i = total - taken + from; i < a.n_blocks; i += stride) a.new_free[i] = -1;
+  for (uint32_t i = taken + from; i < a.n_children; i += stride) a.copies[i] = make_int2(-1, -1);
+  if (from == 0) {
+    a.counts[0] = static_cast<int32_t>(taken);
+    a.counts[1] = static_cast<int32_t>(given[0]);
+    a.counts[2] = static_cast<int32_t>(total - taken);
+  }
+}
+
+// ---- compaction -------------------------------------------------------------------------------------------------
+//
+// Used and free blocks together, ascending: behind the first n_used of them lies the border.  The k-th used block behind the border goes
+// to the k-th free one before it, and what lies behind it is the new free list.
+
+__global__ __launch_bounds__(BLOCKS_THREADS) void k_compact_begin(BlocksArgs a) {
+  clear_marks(a, blockIdx.x * BLOCKS_THREADS + threadIdx.x, gridDim.x * BLOCKS_THREADS);
+}
+
+// A wave for each request marks its blocks; the waves behind them the free ones, 64 each.
+__global__ __launch_bounds__(ROW_WAVES * WAVE) void k_compact_mark(BlocksArgs a) {
+  if (stopped(a.status)) return;
+  const uint32_t lane = lane_id(), row = blockIdx.x * ROW_WAVES + uniform(threadIdx.x / WAVE);
+  if (row < a.n_requests) {
+    const int32_t length = a.lengths[row];
+    if (!length_ok(a, length)) {
+      *a.status = FIKIT_INVALID_ARG;
+      return;
+    }
+    const uint32_t pages = pages_of(a, static_cast<uint32_t>(length));
+    const int32_t* entries = a.table + static_cast<uint64_t>(row) * a.width;
+    for (uint32_t page = lane; page < pages; page += WAVE) {
+      const uint32_t block = static_cast<uint32_t>(entries[page]);
+      if (block < a.n_blocks) mark(a.marks, block);
+      else *a.status = FIKIT_INVALID_ARG;
+    }
+    return;
+  }
+  const uint32_t i = (row - a.n_requests) * WAVE + lane;
+  if (i >= a.n_free) return;
+  const uint32_t block = static_cast<uint32_t>(a.free_blocks[i]);
+  if (block < a.n_blocks) mark(a.marks_too, block);
+  else *a.status = FIKIT_INVALID_ARG;
+}
+
+struct Border {
+  uint32_t block, used;          // the border, and the used blocks before it
+  uint32_t bad;                  // a block is used and free
+};
+
+// Where the border lies, in every workgroup: the thread whose words hold the last of the first n_used blocks finds it.
+__device__ __forceinline__ void find_border(const BlocksArgs& a, const uint32_t (&mine)[2], const uint32_t (&total)[2], Border* lds) {
+  const uint32_t per = (a.words + BLOCKS_THREADS - 1) / BLOCKS_THREADS, from = threadIdx.x * per, to = min_u32(from + per, a.words);
+  uint32_t used = mine[0], all = mine[0] + mine[1];
+  if (threadIdx.x == 0 && total[0] == 0) { lds->block = 0; lds->used = 0; }
+  for (uint32_t w = from; w < to && all < total[0]; ++w) {
+    uint32_t of = a.marks[w] | a.marks_too[w];
+    const uint32_t here = __popc(of);
+    if (all + here >= total[0]) {
+      for (uint32_t skip = total[0] - all - 1; skip > 0; --skip) of &= of - 1;
+      const uint32_t bit = __ffs(static_cast<int>(of)) - 1, below = bit == 31 ? ~0u : (2u << bit) - 1;
+      lds->block = w * 32 + bit + 1;
+      lds->used = used + __popc(a.marks[w] & below);
+    }
+    all += here;
+    used += __popc(a.marks[w]);
+  }
+}
+
+__global__ __launch_bounds__(BLOCKS_THREADS) void k_compact_lists(BlocksArgs a) {
+  __shared__ WordSums<2> sums;
+  __shared__ Border border;
+  if (__syncthreads_or(stopped(a.status))) return;
+  const uint32_t slice = blockIdx.x * SLICE;
+  uint32_t mine[2], total[2], both = 0;
+  word_sums<2>(a.words, slice, &sums, mine, total, [&](uint32_t w, uint32_t (&of)[2]) {
+    of[0] = __popc(a.marks[w]);
+    of[1] = __popc(a.marks_too[w]);
+    both |= a.marks[w] & a.marks_too[w];
+  });
+  find_border(a, mine, total, &border);
+  if (__syncthreads_or(both != 0) || total[1] != a.n_free) {       // a block that is used and free, or free twice
+    if (threadIdx.x == 0) *a.status = FIKIT_INVALID_ARG;
+    return;
+  }
+  for (uint32_t i = threadIdx.x; i < SLICE * 32; i += BLOCKS_THREADS) {
+    const uint32_t w = slice + i / 32;
+    if (w >= a.words) break;
+    const uint32_t used = a.marks[w], spare = a.marks_too[w], bit = 1u << i % 32, block = w * 32 + i % 32;
+    const uint32_t used_before = sums.before[i / 32][0] + __popc(used & (bit - 1)), spare_before = sums.before[i / 32][1] + __popc(spare & (bit - 1));
+    if (i % 32 == 0) a.before[w] = used_before;
+    if (block >= border.block) {
+      if (used & bit) a.copies[used_before - border.used].x = static_cast<int32_t>(block);
+      if ((used | spare) & bit) a.new_free[used_before + spare_before - total[0]] = static_cast<int32_t>(block);
+    } else if (spare & bit) {
+      a.copies[spare_before].y = static_cast<int32_t>(block);
+    }
+  }
+  const uint32_t moved = total[0] - border.used, from = blockIdx.x * BLOCKS_THREADS + threadIdx.x, stride = gridDim.x * BLOCKS_THREADS;
+  for (uint32_t i = moved + from; i < a.room; i += stride) a.copies[i] = make_int2(-1, -1);
+  if (from == 0) {
+    a.counts[0] = static_cast<int32_t>(moved);
+    a.counts[1] = static_cast<int32_t>(total[0]);
+    a.words_of_call[0] = border.block;
+    a.words_of_call[1] = border.used;
+  }
+}
+
+// A wave for each request writes its row.
+__global__ __launch_bounds__(ROW_WAVES * WAVE) void k_compact_rows(BlocksArgs a) {
+  if (stopped(a.status)) return;
+  const uint32_t lane = lane_id(), row = blockIdx.x * ROW_WAVES + uniform(threadIdx.x / WAVE);
+  if (row >= a.n_requests) return;
+  const uint32_t border = a.words_of_call[0], used = a.words_of_call[1], pages = pages_of(a, static_cast<uint32_t>(a.lengths[row]));
+  const int32_t* entries = a.table + static_cast<uint64_t>(row) * a.width;
+  int32_t* out = a.new_table + static_cast<uint64_t>(row) * a.width;
+  for (uint32_t page = lane; page < a.width; page += WAVE) {
+    int32_t block = page < pages ? entries[page] : -1;
+    if (block >= 0 && static_cast<uint32_t>(block) >= border) {
+      const uint32_t w = static_cast<uint32_t>(block) / 32, bit = 1u << block % 32;
+      block = a.copies[a.before[w] + __popc(a.marks[w] & (bit - 1)) - used].y;
+    }
+    out[page] = block;
+  }
+}
+
+// ---- copies -----------------------------------------------------------------------------------------------------
+//
+// A block's codes of one cache lie in one piece, so a workgroup moves 16 KiB of it, four 16-byte loads a thread on their way; memory bound.
+// Workgroups are a piece of a block, of keys or values, in a cache, for every `step`-th entry of the list; a wave looks at 64 of its entries at
+// once, so that a long list of which little is used costs little.
+
+constexpr int COPY_CACHES = 32, COPY_THREADS = 256, COPY_LOADS = 4;
+constexpr uint32_t COPY_CHUNK = COPY_THREADS * COPY_LOADS * 16;
+struct CopyArgs {
+  struct { uint8_t *k, *v, *k_exp, *v_exp; } caches[COPY_CACHES];
+  const int2* copies;
+  int32_t* status;
+  uint32_t n_copies, n_blocks, heads, block_bytes, chunks, per_copy, step;      // per_copy: pieces of a copy, in all caches
+};
+
+__global__ __launch_bounds__(COPY_THREADS) void k_cache_copy(CopyArgs a) {
+  if (stopped(a.status)) return;
+  const uint32_t rest = blockIdx.x % a.per_copy, side = rest / a.chunks, chunk = rest % a.chunks, lane = lane_id();
+  const auto& cache = a.caches[side / 2];
+  uint8_t* codes = side % 2 ? cache.v : cache.k;
+  uint8_t* exps = side % 2 ? cache.v_exp : cache.k_exp;
+  const uint32_t begin = chunk * COPY_CHUNK + threadIdx.x * 16;
+  for (uint64_t first = blockIdx.x / a.per_copy; first < a.n_copies; first += static_cast<uint64_t>(WAVE) * a.step) {
+    const uint64_t mine = first + static_cast<uint64_t>(lane) * a.step;
+    const int2 copy = mine < a.n_copies ? a.copies[mine] : make_int2(-1, -1);
+    const bool used = (copy.x & copy.y) != -1;
+    const bool bad = used && (static_cast<uint32_t>(copy.x) >= a.n_blocks || static_cast<uint32_t>(copy.y) >= a.n_blocks);
+    if (bad) *a.status = FIKIT_INVALID_ARG;
+    for (uint64_t left = ballot(used && !bad && copy.x != copy.y); left; left &= left - 1) {
+      const uint32_t which = static_cast<uint32_t>(__builtin_ctzll(left));
+      const uint64_t from = read_lane_u32(static_cast<uint32_t>(copy.x), which), to = read_lane_u32(static_cast<uint32_t>(copy.y), which);
+      const uint8_t* x = codes + from * a.block_bytes;
+      uint8_t* y = codes + to * a.block_bytes;
+      u32x4 held[COPY_LOADS];
+#pragma unroll
+      for (int i = 0; i < COPY_LOADS; ++i)
+        if (begin + i * COPY_THREADS * 16 < a.block_bytes) held[i] = *reinterpret_cast<const u32x4*>(x + begin + i * COPY_THREADS * 16);
+#pragma unroll
+      for (int i = 0; i < COPY_LOADS; ++i)
+        if (begin + i * COPY_THREADS * 16 < a.block_bytes) *reinterpret_cast<u32x4*>(y + begin + i * COPY_THREADS * 16) = held[i];
+      if (chunk == 0)
+        for (uint32_t h = threadIdx.x; h < a.heads; h += COPY_THREADS) exps[to * a.heads + h] = exps[from * a.heads + h];
+    }
+  }
+}
+
+}  // namespace fikit

@@ -12,6 +12,8 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/python_numbers.h>
 
+#include <vector>
+
 #include "fikit.h"
 
 namespace {
@@ -24,6 +26,11 @@ decltype(&fikit_cache_attention_workspace_bytes) cache_attention_workspace_bytes
 decltype(&fikit_cache_attention) cache_attention;
 decltype(&fikit_prompt_attention) prompt_attention;
 decltype(&fikit_rotate_heads) rotate_heads;
+decltype(&fikit_cache_fork_workspace_bytes) cache_fork_workspace_bytes;
+decltype(&fikit_cache_fork) cache_fork;
+decltype(&fikit_cache_compact_workspace_bytes) cache_compact_workspace_bytes;
+decltype(&fikit_cache_compact) cache_compact;
+decltype(&fikit_cache_copy) cache_copy;
 
 const at::Tensor& tensor(PyObject* o, const char* what) {
   TORCH_CHECK_VALUE(THPVariable_Check(o), what, ": a tensor");
@@ -359,14 +366,167 @@ PyObject* py_rotate_heads(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
+// The tensors of a tuple that is given for a call's outputs.
+template <int N>
+void given_tuple(PyObject* given, at::Tensor* const (&parts)[N], const char* what) {
+  TORCH_CHECK_VALUE(PyTuple_Check(given) && PyTuple_GET_SIZE(given) == N, "out: a ", what);
+  for (int i = 0; i < N; ++i) *parts[i] = tensor(PyTuple_GET_ITEM(given, i), "out");
+}
+
+// Dense tensors of 32-bit integers in one allocation; pairs come first, which are 8-byte aligned.
+struct Ints {
+  at::Tensor all;
+  int64_t at = 0;
+  Ints(int64_t n, const at::Device& device) : all(at::empty({n}, at::TensorOptions().dtype(at::kInt).device(device))) {}
+  at::Tensor take(at::IntArrayRef sizes) {
+    const at::Tensor t = part_of(all, at::kInt, at, sizes);
+    at += t.numel();
+    return t;
+  }
+};
+
+// block_table, lengths, parents, block_tokens, n_blocks, free_blocks, status, out, workspace_buf, stream
+PyObject* py_cache_fork(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  need_arguments(n_args, 10);
+  const at::Tensor &table = tensor(a[0], "block_table"), &lengths = tensor(a[1], "lengths"), &parents = tensor(a[2], "parents"),
+                   &free = tensor(a[5], "free_blocks"), &status = tensor(a[6], "status");
+  const at::Device device = table.device();
+  const uint32_t block_tokens = count(a[3], "block_tokens"), n_blocks = count(a[4], "n_blocks");
+  TORCH_CHECK_VALUE(table.dim() == 2 && lengths.numel() == table.size(0) && status.numel() == 1, "block_table: [R, width]; lengths: [R]; status: [1]");
+  const uint32_t n = count(table.size(0), "block_table"), width = count(table.size(1), "block_table"), children = count(parents.numel(), "parents");
+  at::Tensor new_table, new_lengths, copies, new_free, counts;
+  const bool allocate = a[7] == Py_None;
+  if (!allocate) {
+    given_tuple(a[7], {&new_table, &new_lengths, &copies, &new_free, &counts}, "CacheFork");
+    TORCH_CHECK_VALUE(new_table.dim() == 2 && new_table.size(0) == children && new_table.size(1) == width && new_lengths.numel() == children &&
+                          copies.numel() == 2 * static_cast<int64_t>(children) && new_free.numel() == n_blocks && counts.numel() == 3,
+                      "out: tensors of the fork's sizes");
+  }
+  const at::Tensor workspace = given_or_none(a[8], "workspace_buf");
+  void* const stream = stream_of(a[9]);
+  int rc;
+  {
+    const Unlocked unlocked;
+    if (allocate) {
+      const int64_t c = children;
+      Ints ints(2 * c + c * width + c + n_blocks + 3, device);
+      copies = ints.take({c, 2});
+      new_table = ints.take({c, width});
+      new_lengths = ints.take({c});
+      new_free = ints.take({n_blocks});
+      counts = ints.take({3});
+    }
+    const at::Tensor ws = workspace_of(workspace, cache_fork_workspace_bytes(n, children, n_blocks), device);
+    rc = cache_fork(dense<int32_t>(table, at::kInt, device, "block_table"), width, dense<int32_t>(lengths, at::kInt, device, "lengths"), n,
+                    dense<int32_t>(parents, at::kInt, device, "parents"), children, block_tokens, n_blocks,
+                    dense<int32_t>(free, at::kInt, device, "free_blocks"), count(free.numel(), "free_blocks"),
+                    dense<int32_t>(new_table, at::kInt, device, "out"), dense<int32_t>(new_lengths, at::kInt, device, "out"),
+                    dense<fikit_block_copy>(copies, at::kInt, device, "out"), dense<int32_t>(new_free, at::kInt, device, "out"),
+                    dense<int32_t>(counts, at::kInt, device, "out"), dense<int32_t>(status, at::kInt, device, "status"),
+                    ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? ws.numel() : 0, stream);
+  }
+  if (rc != FIKIT_OK) return PyLong_FromLong(rc);
+  if (!allocate) {
+    Py_INCREF(a[7]);
+    return a[7];
+  }
+  return Py_BuildValue("(NNNNN)", wrapped(new_table), wrapped(new_lengths), wrapped(copies), wrapped(new_free), wrapped(counts));
+  END_HANDLE_TH_ERRORS
+}
+
+// block_table, lengths, block_tokens, n_blocks, free_blocks, status, out, workspace_buf, stream
+PyObject* py_cache_compact(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  need_arguments(n_args, 9);
+  const at::Tensor &table = tensor(a[0], "block_table"), &lengths = tensor(a[1], "lengths"), &free = tensor(a[4], "free_blocks"), &status = tensor(a[5], "status");
+  const at::Device device = table.device();
+  const uint32_t block_tokens = count(a[2], "block_tokens"), n_blocks = count(a[3], "n_blocks"), n_free = count(free.numel(), "free_blocks");
+  TORCH_CHECK_VALUE(table.dim() == 2 && lengths.numel() == table.size(0) && status.numel() == 1, "block_table: [R, width]; lengths: [R]; status: [1]");
+  const uint32_t n = count(table.size(0), "block_table"), width = count(table.size(1), "block_table");
+  const int64_t room = n_free < n_blocks / 2 ? n_free : n_blocks / 2;
+  at::Tensor new_table, copies, new_free, counts;
+  const bool allocate = a[6] == Py_None;
+  if (!allocate) {
+    given_tuple(a[6], {&new_table, &copies, &new_free, &counts}, "CacheCompaction");
+    TORCH_CHECK_VALUE(new_table.sizes() == table.sizes() && copies.numel() == 2 * room && new_free.numel() == n_free && counts.numel() == 2,
+                      "out: tensors of the compaction's sizes");
+  }
+  const at::Tensor workspace = given_or_none(a[7], "workspace_buf");
+  void* const stream = stream_of(a[8]);
+  int rc;
+  {
+    const Unlocked unlocked;
+    if (allocate) {
+      Ints ints(2 * room + table.numel() + n_free + 2, device);
+      copies = ints.take({room, 2});
+      new_table = ints.take(table.sizes());
+      new_free = ints.take({n_free});
+      counts = ints.take({2});
+    }
+    const at::Tensor ws = workspace_of(workspace, cache_compact_workspace_bytes(n, n_blocks), device);
+    rc = cache_compact(dense<int32_t>(table, at::kInt, device, "block_table"), width, dense<int32_t>(lengths, at::kInt, device, "lengths"), n, block_tokens,
+                       n_blocks, dense<int32_t>(free, at::kInt, device, "free_blocks"), n_free, dense<int32_t>(new_table, at::kInt, device, "out"),
+                       dense<fikit_block_copy>(copies, at::kInt, device, "out"), dense<int32_t>(new_free, at::kInt, device, "out"),
+                       dense<int32_t>(counts, at::kInt, device, "out"), dense<int32_t>(status, at::kInt, device, "status"),
+                       ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? ws.numel() : 0, stream);
+  }
+  if (rc != FIKIT_OK) return PyLong_FromLong(rc);
+  if (!allocate) {
+    Py_INCREF(a[6]);
+    return a[6];
+  }
+  return Py_BuildValue("(NNNN)", wrapped(new_table), wrapped(copies), wrapped(new_free), wrapped(counts));
+  END_HANDLE_TH_ERRORS
+}
+
+// A reference of one's own.
+struct Owned {
+  PyObject* o;
+  explicit Owned(PyObject* given) : o(given) { if (!o) throw python_error(); }
+  Owned(const Owned&) = delete;
+  ~Owned() { Py_DECREF(o); }
+};
+
+// caches (a sequence of sequences k_cache, v_cache, k_exp, v_exp), copies, status, stream
+PyObject* py_cache_copy(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  need_arguments(n_args, 4);
+  const at::Tensor &copies = tensor(a[1], "copies"), &status = tensor(a[2], "status");
+  const at::Device device = copies.device();
+  TORCH_CHECK_VALUE(copies.dim() == 2 && copies.size(1) == 2 && status.numel() == 1, "copies: [n, 2]; status: [1]");
+  const Owned all(PySequence_Tuple(a[0]));
+  std::vector<fikit_cache> caches;
+  for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(all.o); ++i) {
+    const Owned one(PySequence_Tuple(PyTuple_GET_ITEM(all.o, i)));
+    TORCH_CHECK_VALUE(PyTuple_GET_SIZE(one.o) == 4, "caches: of k_cache, v_cache, k_exp, v_exp each");
+    PyObject* const parts[] = {PyTuple_GET_ITEM(one.o, 0), PyTuple_GET_ITEM(one.o, 1), PyTuple_GET_ITEM(one.o, 2), PyTuple_GET_ITEM(one.o, 3)};
+    caches.push_back(cache_of(parts, device));
+  }
+  void* const stream = stream_of(a[3]);
+  int rc;
+  {
+    const Unlocked unlocked;
+    rc = cache_copy(caches.data(), count(static_cast<int64_t>(caches.size()), "caches"), dense<fikit_block_copy>(copies, at::kInt, device, "copies"),
+                    count(copies.size(0), "copies"), dense<int32_t>(status, at::kInt, device, "status"), stream);
+  }
+  return PyLong_FromLong(rc);
+  END_HANDLE_TH_ERRORS
+}
+
 template <typename F>
 void set_address(F& f, PyObject* o) { f = reinterpret_cast<F>(PyLong_AsVoidPtr(o)); }
 
 // The addresses of the C calls around the attention, in the order of the variables above.
 PyObject* py_bind_around(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   HANDLE_TH_ERRORS
-  need_arguments(n_args, 1);
+  need_arguments(n_args, 6);
   set_address(rotate_heads, a[0]);
+  set_address(cache_fork_workspace_bytes, a[1]);
+  set_address(cache_fork, a[2]);
+  set_address(cache_compact_workspace_bytes, a[3]);
+  set_address(cache_compact, a[4]);
+  set_address(cache_copy, a[5]);
   Py_RETURN_NONE;
   END_HANDLE_TH_ERRORS
 }
@@ -388,7 +548,7 @@ PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
 
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(bind), METHOD(cache_plan), METHOD(cache_append), METHOD(cache_attention), METHOD(prompt_attention),
-                         METHOD(bind_around), METHOD(rotate_heads), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(bind_around), METHOD(rotate_heads), METHOD(cache_fork), METHOD(cache_compact), METHOD(cache_copy), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_serve_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -36,3 +36,40 @@ def near(got, want, bound):
     fine = torch.isfinite(want)
     kinds = torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got[~fine & ~torch.isnan(want)], want[~fine & ~torch.isnan(want)])
     return kinds and bool(((got - want).abs()[fine] <= bound[fine]).all())
+
+
+def fork(table, lengths, parents, block, n_blocks, free):
+    """Everything fikit_cache_fork writes, from the definitions, a child at a time; lists of Python numbers in and out.  None: too few blocks."""
+    def pages(n):
+        return -(-n // block)
+    continued = {p for p in parents if p >= 0}
+    kept = {b for p in continued for b in table[p][:pages(lengths[p])]}
+    given = sorted({b for r, row in enumerate(table) for b in row[:pages(lengths[r])]} - kept)
+    pool, taken, seen, copies, rows, new_lengths = list(free) + given, 0, set(), [], [], []
+    for p in parents:
+        n = lengths[p] if p >= 0 else 0
+        row = list(table[p][:pages(n)]) if p >= 0 else []
+        if n % block and p in seen:
+            if taken == len(pool):
+                return None
+            copies.append([row[-1], pool[taken]])
+            row[-1] = pool[taken]
+            taken += 1
+        seen.add(p)
+        rows.append(row + [-1] * (len(table[0]) - len(row) if table else 0))
+        new_lengths.append(n)
+    left = pool[taken:]
+    return {"block_table": rows, "lengths": new_lengths, "copies": copies + [[-1, -1]] * (len(parents) - len(copies)),
+            "free_blocks": left + [-1] * (n_blocks - len(left)), "counts": [taken, len(given), len(left)]}
+
+
+def compact(table, lengths, block, n_blocks, free):
+    """Everything fikit_cache_compact writes, from the definitions."""
+    held = [row[:-(-n // block)] for row, n in zip(table, lengths)]
+    used = sorted({b for row in held for b in row})
+    both = sorted(used + list(free))
+    front, rest = set(both[:len(used)]), both[len(used):]
+    moves = dict(zip([b for b in used if b not in front], sorted(front - set(used))))
+    room = min(len(free), n_blocks // 2)
+    return {"block_table": [[moves.get(b, b) for b in row] + [-1] * (len(table[0]) - len(row)) for row in held],
+            "copies": [list(m) for m in moves.items()] + [[-1, -1]] * (room - len(moves)), "free_blocks": rest, "counts": [len(moves), len(used)]}

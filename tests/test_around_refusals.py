@@ -59,3 +59,88 @@ def test_rotate_heads_binding():
                 dict(out=(x,)), dict(out=(x, None)), dict(out=(x[:2], x)), dict(q=x.transpose(1, 2))):
         with pytest.raises(ValueError):
             call(**bad)
+
+
+def fork(**change):
+    a = dict(table=0x1000000, width=3, lengths=0x2000000, n=4, parents=0x3000000, children=5, block=16, n_blocks=100, free=0x4000000, n_free=9, new_table=0x5000000,
+             new_lengths=0x6000000, copies=0x7000000, new_free=0x8000000, counts=0x9000000, status=0xa000000, ws=0xb000000, ws_bytes=1 << 20)
+    assert set(change) <= set(a)
+    a.update(change)
+    return binding.load().fikit_cache_fork(*a.values(), None)
+
+
+def compact(**change):
+    a = dict(table=0x1000000, width=3, lengths=0x2000000, n=4, block=16, n_blocks=100, free=0x4000000, n_free=9, new_table=0x5000000, copies=0x7000000,
+             new_free=0x8000000, counts=0x9000000, status=0xa000000, ws=0xb000000, ws_bytes=1 << 20)
+    assert set(change) <= set(a)
+    a.update(change)
+    return binding.load().fikit_cache_compact(*a.values(), None)
+
+
+SHARED = [
+    (dict(table=NULL), INVALID), (dict(table=0x1000002), INVALID), (dict(lengths=NULL), INVALID), (dict(lengths=ODD), INVALID), (dict(free=NULL), INVALID),
+    (dict(free=ODD), INVALID), (dict(n_free=101), INVALID), (dict(n_blocks=0), INVALID), (dict(new_table=NULL), INVALID), (dict(new_table=ODD), INVALID),
+    (dict(copies=NULL), INVALID), (dict(copies=0x7000004), INVALID), (dict(new_free=NULL), INVALID), (dict(new_free=ODD), INVALID), (dict(counts=NULL), INVALID),
+    (dict(counts=ODD), INVALID), (dict(status=NULL), INVALID), (dict(status=ODD), INVALID), (dict(ws=NULL), INVALID), (dict(ws=0xb000010), INVALID),
+    (dict(width=1 << 31), INVALID), (dict(new_table=0x1000000), INVALID), (dict(new_free=0x4000000), INVALID), (dict(new_free=0x4000000 + 32), INVALID),
+    (dict(counts=0x2000000), INVALID), (dict(copies=0x5000000), INVALID), (dict(ws_bytes=256), SMALL), (dict(block=8), UNSUPPORTED), (dict(block=0), UNSUPPORTED),
+    (dict(block=48), UNSUPPORTED), (dict(block=512), UNSUPPORTED), (dict(n=16385), UNSUPPORTED), (dict(n_blocks=(1 << 20) + 1), UNSUPPORTED)]
+
+
+@pytest.mark.parametrize("change, want", SHARED + [(dict(parents=NULL), INVALID), (dict(parents=ODD), INVALID), (dict(new_lengths=NULL), INVALID),
+                                                  (dict(new_lengths=ODD), INVALID), (dict(new_lengths=0x3000000), INVALID), (dict(children=16385), UNSUPPORTED)])
+def test_fork(change, want):
+    assert fork(**change) == want
+
+
+@pytest.mark.parametrize("change, want", SHARED)
+def test_compact(change, want):
+    assert compact(**change) == want
+
+
+def test_block_workspaces():
+    for f, sizes in ((binding.fikit_cache_fork_workspace_bytes, (7, 9)), (binding.fikit_cache_compact_workspace_bytes, (7,))):
+        assert 0 < f(*sizes, 1) <= f(*sizes, 1 << 20) and f(*sizes, (1 << 20) + 1) == 0 and f(*(16385 for _ in sizes), 5) == 0
+
+
+def cache(**change):
+    a = dict(k=FAKE, v=FAKE, k_exp=FAKE, v_exp=FAKE, n_blocks=10, kv_heads=2, block_tokens=16, head_dim=64)
+    assert set(change) <= set(a)
+    a.update(change)
+    return binding._Cache(*a.values())
+
+
+def test_copy():
+    def call(caches=(cache(),), copies=FAKE, n=3, status=FAKE):
+        return binding.load().fikit_cache_copy((binding._Cache * len(caches))(*caches), len(caches), copies, n, status, None)
+    for change, want in [(dict(k=NULL), INVALID), (dict(v=ODD), INVALID), (dict(k_exp=NULL), INVALID), (dict(n_blocks=0), INVALID), (dict(kv_heads=0), INVALID),
+                         (dict(block_tokens=24), UNSUPPORTED), (dict(head_dim=96), UNSUPPORTED)]:
+        assert call((cache(**change),)) == want and call((cache(), cache(**change))) == want
+    for change in (dict(n_blocks=11), dict(kv_heads=3), dict(block_tokens=32), dict(head_dim=128)):
+        assert call((cache(), cache(**change))) == INVALID
+    assert call(copies=NULL) == INVALID and call(copies=FAKE + 4) == INVALID and call(status=NULL) == INVALID and call(n=1 << 31) == INVALID
+    assert call(n=0, copies=NULL) == OK and call(()) == OK
+    assert binding.load().fikit_cache_copy(None, 1, FAKE, 3, FAKE, None) == INVALID
+
+
+def test_block_bindings():
+    i = torch.zeros(3, dtype=torch.int32)
+    table, status, native = torch.zeros((3, 2), dtype=torch.int32), torch.zeros(1, dtype=torch.int32), binding._marshal()
+    codes, exps = torch.zeros((4, 2, 16, 64), dtype=torch.uint8), torch.ones((4, 2), dtype=torch.uint8)
+    with pytest.raises(ValueError):
+        binding.fikit_cache_fork(table, i, i, 16, 9, i, status)              # tensors on a GPU
+    for bad in ((table[0], i, i, i), (table, i[:2], i, i), (table, i, i.long(), i), (table, i, i, i.float()), (table.t(), i[:2], i, i)):
+        with pytest.raises(ValueError):
+            native.cache_fork(bad[0], bad[1], bad[2], 16, 9, bad[3], status, None, None, 0)
+    for out in ((i,), (table, i, table, i, i), binding.CacheFork(table, i, table, torch.zeros(9, dtype=torch.int32), i[:2])):
+        with pytest.raises(ValueError):
+            native.cache_fork(table, i, i, 16, 9, i, status, out, None, 0)
+    with pytest.raises(ValueError):
+        native.cache_compact(table, i, 16, 9, i, status, binding.CacheCompaction(table, table, i, i), None, 0)
+    for caches in ([(codes, codes, exps)], [(codes, codes, exps, exps.long())], [(codes, codes[:2], exps, exps)], [codes]):
+        with pytest.raises(ValueError):
+            native.cache_copy(caches, table, status, 0)
+    with pytest.raises((ValueError, TypeError)):
+        native.cache_copy(5, table, status, 0)
+    with pytest.raises(ValueError):
+        native.cache_copy([(codes, codes, exps, exps)], i, status, 0)
