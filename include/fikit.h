@@ -585,6 +585,7 @@ int fikit_prompt_attention(const fikit_vectors* h_q, const fikit_vectors* h_k, c
  *   fikit_cache_fork        requests that are continued once, several times or not at all: their rows of the table, blocks given back
  *   fikit_cache_compact     the blocks in use moved together
  *   fikit_cache_copy        what these two want copied, in the caches of all layers
+ *   fikit_token_scores      what rows of logits say: log probabilities of given tokens, entropy, alternatives
  *
  * Nobody keeps count of a block's holders: it is held as long as a row of the table names it within the request's length, and several
  * rows may (their requests have the same tokens there).  New tokens go into blocks that one request holds alone: fikit_cache_fork leaves every
@@ -689,6 +690,38 @@ int fikit_cache_compact(const int32_t* d_block_table, uint32_t table_width, cons
  */
 int fikit_cache_copy(const fikit_cache* h_caches, uint32_t n_caches, const fikit_block_copy* d_copies, uint32_t n_copies,
                      int32_t* d_status, void* hip_stream);
+
+/* Bytes of device workspace fikit_token_scores needs for these sizes (0: none, d_workspace may be NULL). */
+size_t fikit_token_scores_workspace_bytes(uint32_t n_rows, uint32_t vocabulary, int32_t value_type, uint32_t n_top);
+
+/*
+ * What rows of logits say about tokens.  With z = scale * x of a row's logits x, in 32 bits and natural logarithms:
+ *
+ *   d_lse          [n_rows] log(sum_j exp(z_j))
+ *   d_logprob      [n_rows] z[token] - lse of the row's given token
+ *   d_entropy      [n_rows] -sum_j p_j log(p_j), p_j = exp(z_j - lse)
+ *   d_top_tokens   [n_rows][n_top] the tokens of the largest logits, the largest first; of equal logits the lowest token first
+ *   d_top_logprob  [n_rows][n_top] their z - lse
+ *
+ * Outputs may be NULL and are not written then; the last two are both given or both not (n_top 0).
+ *
+ *   d_logits       n_rows rows of `vocabulary` values, dense within a row, row r at r * row_stride values (any stride, 0 too), aligned as
+ *                  one value is; value_type FIKIT_BF16, FIKIT_F16 or FIKIT_F32.
+ *   d_tokens       [n_rows]; a negative one is none, and its log probability 0.  One of `vocabulary` or more is INVALID_ARG through
+ *                  d_status.  NULL: none is given.
+ *   n_top          up to 32 (UNSUPPORTED beyond).
+ *   scale          from 2^-100 to 2^100: one over the temperature.
+ *   n_rows, vocabulary   < 2^31; n_rows up to 2^24 - 1 (UNSUPPORTED beyond).
+ *   d_workspace    256-byte aligned, at least fikit_token_scores_workspace_bytes(...) bytes.
+ *
+ * A logit of minus infinity is a token that cannot come: log probability minus infinity, and no alternative; where fewer alternatives are
+ * left than n_top, the rest are token -1 with minus infinity.  A row without any other logit has lse and log probability minus infinity
+ * and entropy 0.  A row that holds NaN or plus infinity has no probabilities: NaN in all its values (but for a token that is not given) and
+ * tokens of -1.  Finite logits count whatever their size, the type's lowest value among them, as long as z is finite in 32 bits.
+ */
+int fikit_token_scores(const void* d_logits, int32_t value_type, uint64_t row_stride, uint32_t n_rows, uint32_t vocabulary, float scale,
+                       const int32_t* d_tokens, uint32_t n_top, float* d_logprob, float* d_entropy, float* d_lse, int32_t* d_top_tokens,
+                       float* d_top_logprob, int32_t* d_status, void* d_workspace, size_t workspace_bytes, void* hip_stream);
 
 const char* fikit_status_string(int status);
 int fikit_version(void);

@@ -36,7 +36,7 @@ EXPORTS = ("fikit_profile_workspace_bytes", "fikit_profile", "fikit_gapfill_work
            "fikit_trace_enable", "fikit_trace_read", "fikit_cache_pieces", "fikit_cache_plan_workspace_bytes", "fikit_cache_plan",
            "fikit_cache_append", "fikit_cache_attention_workspace_bytes", "fikit_cache_attention", "fikit_prompt_attention",
            "fikit_rotate_heads", "fikit_cache_fork_workspace_bytes", "fikit_cache_fork", "fikit_cache_compact_workspace_bytes",
-           "fikit_cache_compact", "fikit_cache_copy")
+           "fikit_cache_compact", "fikit_cache_copy", "fikit_token_scores_workspace_bytes", "fikit_token_scores")
 
 # Layout of a profile row as seen from numpy (128 bytes; see fikit_row in fikit.h).
 STATS_DTYPE = np.dtype([("count", "<u8"), ("sum", "<u8"), ("min", "<i8"), ("max", "<i8"),
@@ -157,6 +157,10 @@ def load() -> ctypes.CDLL:
         lib.fikit_cache_compact.argtypes = [vp, u32, vp, u32, u32, u32, vp, u32, vp, vp, vp, vp, vp, vp, sz, vp]
         lib.fikit_cache_copy.restype = ctypes.c_int
         lib.fikit_cache_copy.argtypes = [p_cache, u32, vp, u32, vp, vp]
+        lib.fikit_token_scores_workspace_bytes.restype = sz
+        lib.fikit_token_scores_workspace_bytes.argtypes = [u32, u32, i32, u32]
+        lib.fikit_token_scores.restype = ctypes.c_int
+        lib.fikit_token_scores.argtypes = [vp, i32, u64, u32, u32, f32, vp, u32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         lib.fikit_status_string.restype = ctypes.c_char_p
         lib.fikit_status_string.argtypes = [ctypes.c_int]
         lib.fikit_version.restype = ctypes.c_int
@@ -636,7 +640,7 @@ def _marshal():
             "fikit_cache_attention_workspace_bytes", "fikit_cache_attention", "fikit_prompt_attention")))
         _serve_marshal.bind_around(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in (
             "fikit_rotate_heads", "fikit_cache_fork_workspace_bytes", "fikit_cache_fork", "fikit_cache_compact_workspace_bytes",
-            "fikit_cache_compact", "fikit_cache_copy")))
+            "fikit_cache_compact", "fikit_cache_copy", "fikit_token_scores_workspace_bytes", "fikit_token_scores")))
         _native = _serve_marshal
     return _native
 
@@ -814,6 +818,33 @@ def fikit_cache_copy(caches, copies: torch.Tensor, status: torch.Tensor, *, stre
     st = (_native or _marshal()).cache_copy(caches, copies, status, _stream_of(copies.device.index))
     if st != FIKIT_OK:
         raise FikitError(st, "fikit_cache_copy")
+
+
+class TokenScores(NamedTuple):
+    """Allocated by a call, these are parts of one piece of memory.  Natural logarithms, float32."""
+    logprob: Optional[torch.Tensor]         # [rows], of the given tokens; None if none are
+    entropy: Optional[torch.Tensor]         # [rows]
+    lse: Optional[torch.Tensor]             # [rows]: log of the sum of the exponentials
+    top_tokens: Optional[torch.Tensor]      # int32 [rows, n_top], the most probable first, of equal ones the lowest; -1 where none is left
+    top_logprob: Optional[torch.Tensor]     # [rows, n_top]
+
+
+def fikit_token_scores_workspace_bytes(n_rows: int, vocabulary: int, value_type: int, n_top: int) -> int:
+    return int(load().fikit_token_scores_workspace_bytes(n_rows, vocabulary, value_type, n_top))
+
+
+def fikit_token_scores(logits: torch.Tensor, tokens: Optional[torch.Tensor], status: torch.Tensor, *, scale: float = 1.0, n_top: int = 0,
+                       out: Optional[TokenScores] = None, workspace_buf: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> TokenScores:
+    """logits: bfloat16, float16 or float32 [rows, vocabulary], rows of any stride; tokens: int32 [rows], a negative one is none, or None; scale
+    is one over the temperature; n_top: up to 32.  Output tensors are allocated unless given; of given ones those that are None are not
+    computed."""
+    context = _elsewhere(stream, logits.device)
+    if context is not None:
+        with context:
+            return fikit_token_scores(logits, tokens, status, scale=scale, n_top=n_top, out=out, workspace_buf=workspace_buf)
+    got = (_native or _marshal()).token_scores(logits, tokens, status, scale, n_top, out, workspace_buf, _stream_of(logits.device.index))
+    return _outputs(TokenScores, got, "fikit_token_scores")
 
 
 # ---- helpers to move host arrays in and out (marshalling only) ---------------------------------

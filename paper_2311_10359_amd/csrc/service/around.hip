@@ -5,6 +5,7 @@
 
 #include "blocks_kernels.hip.h"
 #include "rotate_kernels.hip.h"
+#include "scores_kernels.hip.h"
 #include "serve_host.h"
 
 namespace {
@@ -105,6 +106,41 @@ BlocksArgs blocks_args(const int32_t* d_block_table, uint32_t table_width, const
   a.shift = static_cast<uint32_t>(__builtin_ctz(block_tokens));
   return a;
 }
+
+// How rows of logits are cut up, and the workspace.
+struct ScoresCut {
+  uint32_t parts, per_wave;
+  uint64_t sums_bytes, bytes;
+};
+constexpr uint32_t SCORES_CHIP = 512;             // workgroups: two for each CU
+
+ScoresCut scores_cut(uint32_t n_rows, uint32_t vocabulary, int32_t value_type, uint32_t n_top) {
+  ScoresCut c{};
+  const uint32_t groups = vocabulary / (value_type == FIKIT_F32 ? LogitsF32::VEC : LogitsBf16::VEC), turn = SCORES_BATCH * WAVE;
+  const uint32_t most = (groups + SCORES_WAVES * turn - 1) / (SCORES_WAVES * turn), want = n_rows ? (SCORES_CHIP + n_rows - 1) / n_rows : 1;
+  c.parts = want < most ? want : most;
+  if (c.parts < 1) c.parts = 1;
+  const uint32_t waves = c.parts * SCORES_WAVES, each = (groups + waves - 1) / waves;
+  c.per_wave = (each + WAVE - 1) / WAVE * WAVE;
+  if (c.parts == 1) return c;
+  const uint64_t lists = static_cast<uint64_t>(n_rows) * c.parts;
+  c.sums_bytes = (lists * sizeof(float4) + 255) / 256 * 256;
+  c.bytes = c.sums_bytes + (lists * n_top * sizeof(float2) + 255) / 256 * 256;
+  return c;
+}
+
+struct ScoresCall {
+  const ScoresArgs& a;
+  hipStream_t st;
+  template <typename L>
+  int run() {
+    const dim3 block(SCORES_WAVES * WAVE);
+    if (int rc = enqueue(k_scores<L>, dim3(a.rows * a.parts), block, st, a)) return rc;
+    return a.parts == 1 ? FIKIT_OK : enqueue(k_scores_join<L>, dim3((a.rows + SCORES_WAVES - 1) / SCORES_WAVES), block, st, a);
+  }
+};
+
+bool logits_ok(int32_t value_type) { return type_ok(value_type) || value_type == FIKIT_F32; }
 
 constexpr uint32_t CLEAR_GROUPS = 8;
 constexpr uint32_t COPY_GROUPS = 4096;
@@ -265,6 +301,50 @@ int fikit_rotate_heads(const fikit_vectors* h_q, const fikit_vectors* h_k, uint3
   a.epsilon = epsilon;
   RotateCall call{a, pairs == FIKIT_PAIRS_NEIGHBOURS, static_cast<hipStream_t>(hip_stream)};
   return value_type == FIKIT_BF16 ? call.with_dim<Bf16>(head_dim) : call.with_dim<F16>(head_dim);
+}
+
+size_t fikit_token_scores_workspace_bytes(uint32_t n_rows, uint32_t vocabulary, int32_t value_type, uint32_t n_top) {
+  if (!logits_ok(value_type) || n_rows > MOST_GROUPS || vocabulary > 0x7fffffffu || n_top > SCORES_MOST) return 0;
+  return static_cast<size_t>(scores_cut(n_rows, vocabulary, value_type, n_top).bytes);
+}
+
+int fikit_token_scores(const void* d_logits, int32_t value_type, uint64_t row_stride, uint32_t n_rows, uint32_t vocabulary, float scale,
+                       const int32_t* d_tokens, uint32_t n_top, float* d_logprob, float* d_entropy, float* d_lse, int32_t* d_top_tokens,
+                       float* d_top_logprob, int32_t* d_status, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!logits_ok(value_type) || !d_status || !aligned(d_status, 4) || n_rows > 0x7fffffffu || vocabulary > 0x7fffffffu) return FIKIT_INVALID_ARG;
+  if (!(scale >= 0x1p-100f && scale <= 0x1p100f)) return FIKIT_INVALID_ARG;
+  if (n_top > SCORES_MOST || n_rows > MOST_GROUPS) return FIKIT_UNSUPPORTED;
+  if (n_rows == 0) return FIKIT_OK;
+  if ((vocabulary > 0 && !d_logits) || !aligned(d_logits, value_type == FIKIT_F32 ? 4 : 2) || !aligned(d_tokens, 4) || !aligned(d_logprob, 4) ||
+      !aligned(d_entropy, 4) || !aligned(d_lse, 4) || !aligned(d_top_tokens, 4) || !aligned(d_top_logprob, 4))
+    return FIKIT_INVALID_ARG;
+  if (n_top > 0 && (!d_top_tokens || !d_top_logprob)) return FIKIT_INVALID_ARG;
+  const ScoresCut c = scores_cut(n_rows, vocabulary, value_type, n_top);
+  if (c.bytes > 0) {
+    if (!d_workspace || !aligned(d_workspace, 256)) return FIKIT_INVALID_ARG;
+    if (workspace_bytes < c.bytes) return FIKIT_WORKSPACE_TOO_SMALL;
+  }
+  ScoresArgs a{};
+  a.logits = d_logits;
+  a.row_stride = row_stride;
+  a.tokens = d_tokens;
+  a.logprob = d_logprob;
+  a.entropy = d_entropy;
+  a.lse = d_lse;
+  a.top_tokens = d_top_tokens;
+  a.top_logprob = d_top_logprob;
+  a.status = d_status;
+  a.sums = static_cast<float4*>(d_workspace);
+  a.lists = reinterpret_cast<float2*>(static_cast<unsigned char*>(d_workspace) + c.sums_bytes);
+  a.rows = n_rows;
+  a.vocabulary = vocabulary;
+  a.n_top = n_top;
+  a.parts = c.parts;
+  a.per_wave = c.per_wave;
+  a.scale = scale;
+  a.c = scale * LOG2E;
+  ScoresCall call{a, static_cast<hipStream_t>(hip_stream)};
+  return value_type == FIKIT_BF16 ? call.run<LogitsBf16>() : value_type == FIKIT_F16 ? call.run<LogitsF16>() : call.run<LogitsF32>();
 }
 
 }  // extern "C"

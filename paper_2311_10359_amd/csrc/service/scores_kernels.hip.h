@@ -1,0 +1,431 @@
+// What rows of logits say about tokens: log probabilities, entropy, alternatives.
+#pragma once
+
+#include "serve_common.hip.h"
+
+namespace fikit {
+
+// A row x of V logits and a scale s.  In units of log 2, with c = s log2(e), R a number near the largest c x and d = c x - R:
+//
+//   S = sum 2^d,  T = sum 2^d d      log(sum exp(s x)) = ln 2 (R + log2 S)      entropy = ln 2 (log2 S - T / S)
+//   log probability of a token = ln 2 (d - log2 S)
+//
+// in one pass: every lane keeps R, S and T of what it has seen.  R is a whole number, so sums move to another R by a power of two,
+// exactly, and d has one rounding.  (R = c max x would have a rounding of its own, 2^-24 of up to 150, in every d.)  From 2^22 on, where a float
+// holds no halves, whole or not makes no difference and the rounding of c x would: there d is a difference of rounded products, 0 for equal
+// logits whatever their size.  So that the type's lowest value, a mask in many programs, stays finite, R is held as R / 4.
+//
+// The k alternatives lie in k groups of neighbouring logits (16 bytes, as one load brings them): those with the largest maxima, among equal ones
+// the first, since of any other group k groups before it in this order hold a value that comes before all of its own.  So the pass looks
+// at one maximum for a group, and at the end the k groups are read again and k of their values taken.  A wave takes groups in ascending order,
+// so a later group that is only as large as the k-th so far is none of them, and few pass: about k (1 + log(groups / k)).
+//
+// V * bytes are read: bound by memory, if a logit takes few instructions: one to unpack, one for maximum and minimum, three for d, S and T, and the
+// exponential, which takes the time of four.
+
+struct ScoresArgs {
+  const void* logits;
+  uint64_t row_stride;
+  const int32_t* tokens;
+  float* logprob;
+  float* entropy;
+  float* lse;
+  int32_t* top_tokens;
+  float* top_logprob;
+  int32_t* status;
+  float4* sums;             // workspace: [rows][parts] R, S, T and the number of groups in the list
+  float2* lists;            // [rows][parts][n_top] maxima and groups
+  uint32_t rows, vocabulary, n_top, parts, per_wave;      // per_wave: groups
+  float scale, c;           // c = scale log2(e)
+};
+
+constexpr int SCORES_WAVES = 4, SCORES_BATCH = 8, SCORES_MOST = 32, SCORES_ROOM = 128;
+constexpr float NO_SUM = -3.4028234663852886e38f;       // R / 4 where nothing has been seen
+constexpr float WHOLE = 0x1p20f;                        // R / 4 below which R is whole
+
+struct LogitsBf16 {
+  typedef uint16_t raw;
+  static constexpr int VEC = 8, KEY_BITS = 16;            // KEY_BITS: what differs between values
+  static __device__ __forceinline__ float value(raw v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); }
+  static __device__ __forceinline__ void unpack(const u32x4& w, float* x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { x[2 * i] = Bf16::low(w[i]); x[2 * i + 1] = Bf16::high(w[i]); }
+  }
+  static constexpr uint32_t NOTHING = 0xff80ff80u;        // minus infinity
+};
+struct LogitsF16 {
+  typedef uint16_t raw;
+  static constexpr int VEC = 8, KEY_BITS = 19;
+  static __device__ __forceinline__ float value(raw v) { return static_cast<float>(bits_as<_Float16>(v)); }
+  static __device__ __forceinline__ void unpack(const u32x4& w, float* x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { x[2 * i] = F16::low(w[i]); x[2 * i + 1] = F16::high(w[i]); }
+  }
+  static constexpr uint32_t NOTHING = 0xfc00fc00u;
+};
+struct LogitsF32 {
+  typedef float raw;
+  static constexpr int VEC = 4, KEY_BITS = 32;
+  static __device__ __forceinline__ float value(raw v) { return v; }
+  static __device__ __forceinline__ void unpack(const u32x4& w, float* x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(w[i]);
+  }
+  static constexpr uint32_t NOTHING = 0xff800000u;
+};
+
+// Whole numbers in the order of the values; zeros of both signs are equal.
+__device__ __forceinline__ uint32_t key_of(float v) {
+  const uint32_t bits = __float_as_uint(v + 0.f);
+  return bits >> 31 ? ~bits : bits | 0x80000000u;
+}
+__device__ __forceinline__ float value_of_key(uint32_t key) { return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key); }
+
+// The largest key that k or more of the wave's keys reach (N to a lane; 0: none), of which the upper BITS differ.
+template <int BITS, int N>
+__device__ __forceinline__ uint32_t reached_by(const uint32_t (&keys)[N], uint32_t k) {
+  uint32_t found = 0;
+#pragma unroll 1
+  for (int b = 31; b >= 32 - BITS; --b) {
+    const uint32_t next = found | 1u << b;
+    uint32_t n = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) n += popc64(ballot(keys[i] >= next));
+    if (n >= k) found = next;
+  }
+  return found;
+}
+
+// Which of the keys are the first k: those beyond the k-th largest, and of those equal to it the first ones.  Their places in turn.
+template <int BITS, int N>
+__device__ __forceinline__ uint32_t first_of(const uint32_t (&keys)[N], uint32_t k, bool (&keep)[N], uint32_t (&place)[N]) {
+  const uint32_t border = reached_by<BITS, N>(keys, k);
+  constexpr uint32_t LOW = BITS == 32 ? 0 : (1u << (32 - BITS) % 32) - 1;
+  uint32_t larger = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) larger += popc64(ballot(keys[i] > (border | LOW)));
+  uint32_t equal = k - larger, n = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint64_t same = ballot(keys[i] >= border && keys[i] <= (border | LOW));
+    keep[i] = keys[i] > (border | LOW) || ((same >> lane_id() & 1) && popc_below(same) < equal);
+    const uint32_t of = popc64(same);
+    equal -= of < equal ? of : equal;
+    const uint64_t kept = ballot(keep[i]);
+    place[i] = n + popc_below(kept);
+    n += popc64(kept);
+  }
+  return border;
+}
+
+struct ScoresLds {          // of a wave: its groups, ascending
+  float most[SCORES_ROOM];
+  uint32_t group[SCORES_ROOM];
+};
+
+__device__ __forceinline__ void lds_in_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// R / 4, S and T of some logits.
+struct Sums {
+  float r = NO_SUM, s = 0, t = 0;
+
+  // The same relative to another R that is no smaller; far below it nothing is left.
+  __device__ __forceinline__ void move_to(float next) {
+    const float move = 4.f * (r - next), f = exp2_fast(move);
+    t = f == 0.f ? 0.f : (t + move * s) * f;
+    s *= f;
+    r = next;
+  }
+  __device__ __forceinline__ void add(Sums other) {
+    const float next = fmaxf(r, other.r);
+    move_to(next);
+    other.move_to(next);
+    s += other.s;
+    t += other.t;
+  }
+  // d of a logit
+  __device__ __forceinline__ float exponent(float x, float c) const {
+    if (fabsf(r) < WHOLE) return __builtin_fmaf(x, c, -4.f * r);
+    return difference(x, c);
+  }
+  __device__ __forceinline__ float difference(float x, float c) const {
+#pragma clang fp contract(off)
+    const float y = x * (0.25f * c);
+    return 4.f * (y - r);
+  }
+};
+
+// What a wave has seen of a row.
+template <typename L>
+struct Seen {
+  Sums sums;                               // of each lane
+  uint32_t n = 0, k;                       // groups in the list; how many are wanted
+  float border;                            // only groups beyond it are
+
+  __device__ __forceinline__ explicit Seen(uint32_t n_top) : k(n_top), border(n_top ? -INFINITY : INFINITY) {}
+
+  template <int N>
+  __device__ __forceinline__ void add(const float (&x)[N], float most, float least, float c) {
+    const float quarter = most * (0.25f * c);
+    sums.move_to(fmaxf(sums.r, fabsf(quarter) < WHOLE ? 0.25f * __builtin_rintf(4.f * quarter) : quarter));
+    const float whole = 4.f * sums.r;
+    float s = 0, t = 0;
+    if (ballot(!(fabsf(sums.r) < WHOLE) || __builtin_fmaf(least, c, -whole) == -INFINITY)) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float d = sums.difference(x[i], c), e = exp2_fast(d);
+        s += e;
+        t = __builtin_fmaf(e, d == -INFINITY ? 0.f : d, t);       // (nothing times minus infinity)
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float d = __builtin_fmaf(x[i], c, -whole), e = exp2_fast(d);
+        s += e;
+        t = __builtin_fmaf(e, d, t);
+      }
+    }
+    sums.s += s;
+    sums.t += t;
+  }
+
+  // A group for each lane that has one, ascending over the lanes and behind all before.
+  __device__ __forceinline__ void offer(bool has, float most, uint32_t group, ScoresLds* lds) {
+    const uint64_t hits = ballot(has && most > border);
+    if (!hits) return;
+    if (hits >> lane_id() & 1) {
+      const uint32_t at = n + popc_below(hits);
+      lds->most[at] = most;
+      lds->group[at] = group;
+    }
+    n += popc64(hits);
+    lds_in_order();
+    if (n > WAVE) shorten(lds);
+  }
+
+  // The first k stay.  (n is up to SCORES_ROOM)
+  __device__ __forceinline__ void shorten(ScoresLds* lds) {
+    if (n <= k) return;
+    constexpr int N = SCORES_ROOM / WAVE;
+    const uint32_t lane = lane_id();
+    uint32_t keys[N], groups[N], place[N];
+    bool keep[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const bool there = lane + i * WAVE < n;
+      keys[i] = there ? key_of(lds->most[lane + i * WAVE]) : 0;
+      groups[i] = lds->group[lane + i * WAVE];
+    }
+    lds_in_order();
+    const uint32_t last = first_of<L::KEY_BITS, N>(keys, k, keep, place);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (keep[i]) {
+        lds->most[place[i]] = value_of_key(keys[i]);
+        lds->group[place[i]] = groups[i];
+      }
+    lds_in_order();
+    n = k;
+    constexpr uint32_t LOW = L::KEY_BITS == 32 ? 0 : (1u << (32 - L::KEY_BITS) % 32) - 1;
+    border = value_of_key(last >> 31 ? last : last | LOW);
+  }
+
+  // The lanes' sums become one, in all lanes.
+  __device__ __forceinline__ void sum_over_lanes() {
+    float most = sums.r;
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) most = fmaxf(most, __shfl_xor(most, m, WAVE));
+    sums.move_to(most);
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) { sums.s += __shfl_xor(sums.s, m, WAVE); sums.t += __shfl_xor(sums.t, m, WAVE); }
+  }
+};
+
+// A row: `head` logits in front of the first 16-byte border, whole groups, and the rest.  Group 0 is the head, 1 .. whole the groups, then the rest.
+template <typename L>
+struct Row {
+  const typename L::raw* x;
+  uint32_t head, whole, vocabulary;
+  __device__ __forceinline__ Row(const ScoresArgs& a, uint32_t row) {
+    x = static_cast<const typename L::raw*>(a.logits) + row * a.row_stride;
+    vocabulary = a.vocabulary;
+    const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(x) % 16) / sizeof(typename L::raw);
+    head = min_u32(off ? L::VEC - off : 0, vocabulary);
+    whole = (vocabulary - head) / L::VEC;
+  }
+  __device__ __forceinline__ uint32_t rest() const { return vocabulary - head - whole * L::VEC; }
+  // the i-th logit of a group, and whether there is one
+  __device__ __forceinline__ bool place(uint32_t group, uint32_t i, uint32_t* at) const {
+    *at = group == 0 ? i : head + (group - 1) * L::VEC + i;
+    return group == 0 ? i < head : *at < vocabulary;
+  }
+};
+
+// Everything that a row's outputs need is known to one wave.
+template <typename L>
+__device__ __forceinline__ void finish_row(const ScoresArgs& a, const Row<L>& row, uint32_t r, const Seen<L>& seen, ScoresLds* lds) {
+  const uint32_t lane = lane_id(), k = a.n_top;
+  const Sums& sums = seen.sums;
+  const bool nothing = sums.s == 0.f, odd = sums.s != sums.s;
+  const float log_s = __builtin_amdgcn_logf(sums.s), lse = __builtin_fmaf(4.f * LN2, sums.r, LN2 * log_s);
+  auto logprob = [&](float x) {
+    if (nothing || x == -INFINITY) return -INFINITY;
+    const float d = sums.exponent(x, a.c);
+    return d > -4.f * WHOLE ? fminf(LN2 * (d - log_s), 0.f) : x * a.scale - lse;
+  };
+  if (lane == 0) {
+    const int32_t token = a.tokens ? a.tokens[r] : -1;
+    float of_token = 0.f;
+    if (token >= 0) {
+      if (static_cast<uint32_t>(token) < a.vocabulary) of_token = odd ? NAN : logprob(L::value(row.x[token]));
+      else *a.status = FIKIT_INVALID_ARG;
+    }
+    if (a.logprob) a.logprob[r] = of_token;
+    if (a.lse) a.lse[r] = nothing ? -INFINITY : odd ? NAN : lse;
+    if (a.entropy) a.entropy[r] = nothing ? 0.f : odd ? NAN : fmaxf(LN2 * (log_s - sums.t / sums.s), 0.f);
+  }
+  if (k == 0) return;
+  // the values of the groups
+  constexpr int N = SCORES_MOST * L::VEC / WAVE;
+  uint32_t keys[N], at[N], place[N];
+  bool keep[N];
+  uint32_t valid = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint32_t e = lane + i * WAVE;
+    keys[i] = 0;
+    at[i] = 0;
+    if (e / L::VEC < seen.n && row.place(lds->group[e / L::VEC], e % L::VEC, &at[i])) {
+      const float x = L::value(row.x[at[i]]);
+      if (x > -INFINITY) keys[i] = key_of(x);
+    }
+    keep[i] = keys[i] != 0;
+    const uint64_t there = ballot(keep[i]);
+    place[i] = valid + popc_below(there);
+    valid += popc64(there);
+  }
+  if (valid > k) first_of<L::KEY_BITS, N>(keys, k, keep, place);
+  const uint32_t n = min_u32(valid, k);
+  lds_in_order();
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (keep[i]) {
+      lds->most[place[i]] = value_of_key(keys[i]);
+      lds->group[place[i]] = at[i];
+    }
+  lds_in_order();
+  if (lane >= k) return;
+  const uint64_t out = static_cast<uint64_t>(r) * k;
+  if (lane >= n || odd) {
+    a.top_tokens[out + lane] = -1;
+    a.top_logprob[out + lane] = odd ? NAN : -INFINITY;
+    return;
+  }
+  const float mine = lds->most[lane];
+  uint32_t rank = 0;
+  for (uint32_t i = 0; i < n; ++i) {
+    const float other = lds->most[i];
+    rank += other > mine || (other == mine && i < lane);
+  }
+  a.top_tokens[out + rank] = static_cast<int32_t>(lds->group[lane]);
+  a.top_logprob[out + rank] = logprob(mine);
+}
+
+template <typename L>
+__global__ __launch_bounds__(SCORES_WAVES * WAVE) void k_scores(ScoresArgs a) {
+  __shared__ ScoresLds lists[SCORES_WAVES];
+  __shared__ float4 sums[SCORES_WAVES];
+  if (__syncthreads_or(stopped(a.status))) return;
+  const uint32_t lane = lane_id(), wave = uniform(threadIdx.x / WAVE), r = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
+  const Row<L> row(a, r);
+  ScoresLds* lds = &lists[wave];
+  Seen<L> seen(a.n_top);
+  const uint32_t chunk = part * SCORES_WAVES + wave;
+  const uint64_t begin = static_cast<uint64_t>(chunk) * a.per_wave;
+  auto edge = [&](uint32_t group, uint32_t first, uint32_t count) {        // less than a group, a logit to a lane
+    const float x[1] = {lane < count ? L::value(row.x[first + lane]) : -INFINITY};
+    seen.add(x, x[0], x[0], a.c);
+    seen.offer(lane == 0, value_of_key(max_over_wave(key_of(x[0]))), group, lds);
+  };
+  if (chunk == 0 && row.head > 0) edge(0, 0, row.head);
+  const uint32_t end = begin + a.per_wave < row.whole ? static_cast<uint32_t>(begin) + a.per_wave : row.whole;
+  const u32x4* groups = reinterpret_cast<const u32x4*>(row.x + row.head);
+  for (uint64_t at = begin; at < end; at += SCORES_BATCH * WAVE) {
+    u32x4 w[SCORES_BATCH];
+    const uint32_t mine = static_cast<uint32_t>(at) + lane;
+#pragma unroll
+    for (int i = 0; i < SCORES_BATCH; ++i) {
+      w[i] = u32x4{L::NOTHING, L::NOTHING, L::NOTHING, L::NOTHING};
+      if (mine + i * WAVE < end) w[i] = groups[mine + i * WAVE];
+    }
+    float x[SCORES_BATCH * L::VEC], most[SCORES_BATCH], all = -INFINITY, least = INFINITY;
+#pragma unroll
+    for (int i = 0; i < SCORES_BATCH; ++i) {
+      L::unpack(w[i], x + i * L::VEC);
+      most[i] = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < L::VEC; j += 2) {
+        most[i] = fmaxf(fmaxf(most[i], x[i * L::VEC + j]), x[i * L::VEC + j + 1]);
+        least = fminf(fminf(least, x[i * L::VEC + j]), x[i * L::VEC + j + 1]);
+      }
+      all = fmaxf(all, most[i]);
+    }
+    seen.add(x, all, least, a.c);
+#pragma unroll
+    for (int i = 0; i < SCORES_BATCH; ++i) seen.offer(mine + i * WAVE < end, most[i], 1 + mine + i * WAVE, lds);
+  }
+  if (chunk == a.parts * SCORES_WAVES - 1 && row.rest() > 0) edge(row.whole + 1, row.vocabulary - row.rest(), row.rest());
+  seen.shorten(lds);
+  seen.sum_over_lanes();
+  if (lane == 0) sums[wave] = make_float4(seen.sums.r, seen.sums.s, seen.sums.t, __uint_as_float(seen.n));
+  __syncthreads();
+  if (wave > 0) return;
+  // the first wave joins the others' sums and lists, in turn
+  seen.sums = Sums{};
+  if (lane < SCORES_WAVES) seen.sums = Sums{sums[lane].x, sums[lane].y, sums[lane].z};
+  seen.sum_over_lanes();
+  for (uint32_t w = 1; w < SCORES_WAVES; ++w) {
+    const bool there = lane < __float_as_uint(sums[w].w);
+    const float most = there ? lists[w].most[lane] : 0.f;
+    const uint32_t group = there ? lists[w].group[lane] : 0;
+    seen.offer(there, most, group, lds);
+  }
+  seen.shorten(lds);
+  if (a.parts == 1) {
+    finish_row<L>(a, row, r, seen, lds);
+    return;
+  }
+  if (lane == 0) a.sums[blockIdx.x] = make_float4(seen.sums.r, seen.sums.s, seen.sums.t, __uint_as_float(seen.n));
+  if (lane < seen.n) a.lists[static_cast<uint64_t>(blockIdx.x) * a.n_top + lane] = make_float2(lds->most[lane], __uint_as_float(lds->group[lane]));
+}
+
+// Joins a row's parts: a wave each.
+template <typename L>
+__global__ __launch_bounds__(SCORES_WAVES * WAVE) void k_scores_join(ScoresArgs a) {
+  __shared__ ScoresLds lists[SCORES_WAVES];
+  if (stopped(a.status)) return;
+  const uint32_t lane = lane_id(), wave = uniform(threadIdx.x / WAVE), r = blockIdx.x * SCORES_WAVES + wave;
+  if (r >= a.rows) return;
+  const Row<L> row(a, r);
+  ScoresLds* lds = &lists[wave];
+  Seen<L> seen(a.n_top);
+  const uint64_t first = static_cast<uint64_t>(r) * a.parts;
+  for (uint32_t p = lane; p < a.parts; p += WAVE) {
+    const float4 of = a.sums[first + p];
+    seen.sums.add(Sums{of.x, of.y, of.z});
+  }
+  seen.sum_over_lanes();
+  for (uint32_t at = 0; at < a.parts * a.n_top; at += WAVE) {
+    const uint32_t e = at + lane, p = a.n_top ? e / a.n_top : 0;
+    const bool there = p < a.parts && e - p * a.n_top < __float_as_uint(a.sums[first + (p < a.parts ? p : 0)].w);
+    const float2 of = there ? a.lists[first * a.n_top + e] : make_float2(0.f, 0.f);
+    seen.offer(there, of.x, __float_as_uint(of.y), lds);
+  }
+  seen.shorten(lds);
+  finish_row<L>(a, row, r, seen, lds);
+}
+
+}  // namespace fikit

@@ -1,4 +1,5 @@
-// Marshalling of the calls of a language model service (fikit_cache_*, fikit_prompt_attention, fikit_rotate_heads) for Python, compiled: checks of tensors, output
+// Marshalling of the calls of a language model service (fikit_cache_*, fikit_prompt_attention, fikit_rotate_heads,
+// fikit_token_scores) for Python, compiled: checks of tensors, output
 // tensors, and the C calls, whose addresses binding.py passes in.  A call on the GPU may take 4 us; the same checks and
 // allocations as Python statements take 9.
 //
@@ -31,6 +32,8 @@ decltype(&fikit_cache_fork) cache_fork;
 decltype(&fikit_cache_compact_workspace_bytes) cache_compact_workspace_bytes;
 decltype(&fikit_cache_compact) cache_compact;
 decltype(&fikit_cache_copy) cache_copy;
+decltype(&fikit_token_scores_workspace_bytes) token_scores_workspace_bytes;
+decltype(&fikit_token_scores) token_scores;
 
 const at::Tensor& tensor(PyObject* o, const char* what) {
   TORCH_CHECK_VALUE(THPVariable_Check(o), what, ": a tensor");
@@ -514,19 +517,78 @@ PyObject* py_cache_copy(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
+// logits, tokens or None, status, scale, n_top, out, workspace_buf, stream
+PyObject* py_token_scores(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  need_arguments(n_args, 8);
+  const at::Tensor &logits = tensor(a[0], "logits"), tokens = given_or_none(a[1], "tokens"), &status = tensor(a[2], "status");
+  const at::Device device = logits.device();
+  TORCH_CHECK_VALUE(logits.dim() == 2 && (logits.stride(1) == 1 || logits.size(1) <= 1) && logits.stride(0) >= 0, "logits: [rows, vocabulary], the last dimension dense");
+  without_gradient(logits, "logits");
+  const at::ScalarType type = logits.scalar_type();
+  TORCH_CHECK_VALUE(type == at::kFloat || type == at::kBFloat16 || type == at::kHalf, "logits: bfloat16, float16 or float32");
+  const int32_t of_values = type == at::kFloat ? FIKIT_F32 : value_type(logits, "logits");
+  const float scale = static_cast<float>(THPUtils_unpackDouble(a[3]));
+  const uint32_t n_top = count(a[4], "n_top"), rows = count(logits.size(0), "rows"), vocabulary = count(logits.size(1), "vocabulary");
+  TORCH_CHECK_VALUE((!tokens.defined() || tokens.numel() == rows) && status.numel() == 1, "tokens: [rows]; status: [1]");
+  at::Tensor logprob, entropy, lse, top_tokens, top_logprob;
+  const bool allocate = a[5] == Py_None;
+  if (!allocate) {
+    TORCH_CHECK_VALUE(PyTuple_Check(a[5]) && PyTuple_GET_SIZE(a[5]) == 5, "out: a TokenScores");
+    logprob = given_or_none(PyTuple_GET_ITEM(a[5], 0), "logprob");
+    entropy = given_or_none(PyTuple_GET_ITEM(a[5], 1), "entropy");
+    lse = given_or_none(PyTuple_GET_ITEM(a[5], 2), "lse");
+    top_tokens = given_or_none(PyTuple_GET_ITEM(a[5], 3), "top_tokens");
+    top_logprob = given_or_none(PyTuple_GET_ITEM(a[5], 4), "top_logprob");
+    for (const at::Tensor* t : {&logprob, &entropy, &lse}) TORCH_CHECK_VALUE(!t->defined() || t->numel() == rows, "out: [rows]");
+    const int64_t tops = static_cast<int64_t>(rows) * n_top;
+    for (const at::Tensor* t : {&top_tokens, &top_logprob}) TORCH_CHECK_VALUE(t->defined() ? t->numel() == tops : n_top == 0, "out: [rows, n_top]");
+  }
+  const at::Tensor workspace = given_or_none(a[6], "workspace_buf");
+  void* const stream = stream_of(a[7]);
+  int rc;
+  {
+    const Unlocked unlocked;
+    if (allocate && n_top <= 32) {      // one allocation
+      const int64_t n = rows, k = n_top;
+      const at::Tensor all = at::empty({n * (3 + 2 * k)}, at::TensorOptions().dtype(at::kFloat).device(device));
+      if (tokens.defined()) logprob = part_of(all, at::kFloat, 0, {n});
+      entropy = part_of(all, at::kFloat, n, {n});
+      lse = part_of(all, at::kFloat, 2 * n, {n});
+      top_logprob = part_of(all, at::kFloat, 3 * n, {n, k});
+      top_tokens = part_of(all, at::kInt, 3 * n + n * k, {n, k});
+    }
+    const auto floats = [&](const at::Tensor& t) { return t.defined() ? dense<float>(t, at::kFloat, device, "out") : nullptr; };
+    const at::Tensor ws = workspace_of(workspace, token_scores_workspace_bytes(rows, vocabulary, of_values, n_top), device);
+    rc = token_scores(logits.data_ptr(), of_values, rows > 1 ? static_cast<uint64_t>(logits.stride(0)) : 0, rows, vocabulary, scale,
+                      tokens.defined() ? dense<int32_t>(tokens, at::kInt, device, "tokens") : nullptr, n_top, floats(logprob), floats(entropy), floats(lse),
+                      top_tokens.defined() ? dense<int32_t>(top_tokens, at::kInt, device, "out") : nullptr, floats(top_logprob),
+                      dense<int32_t>(status, at::kInt, device, "status"), ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? ws.numel() : 0, stream);
+  }
+  if (rc != FIKIT_OK) return PyLong_FromLong(rc);
+  if (!allocate) {
+    Py_INCREF(a[5]);
+    return a[5];
+  }
+  return Py_BuildValue("(NNNNN)", wrapped(logprob), wrapped(entropy), wrapped(lse), wrapped(top_tokens), wrapped(top_logprob));
+  END_HANDLE_TH_ERRORS
+}
+
 template <typename F>
 void set_address(F& f, PyObject* o) { f = reinterpret_cast<F>(PyLong_AsVoidPtr(o)); }
 
 // The addresses of the C calls around the attention, in the order of the variables above.
 PyObject* py_bind_around(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   HANDLE_TH_ERRORS
-  need_arguments(n_args, 6);
+  need_arguments(n_args, 8);
   set_address(rotate_heads, a[0]);
   set_address(cache_fork_workspace_bytes, a[1]);
   set_address(cache_fork, a[2]);
   set_address(cache_compact_workspace_bytes, a[3]);
   set_address(cache_compact, a[4]);
   set_address(cache_copy, a[5]);
+  set_address(token_scores_workspace_bytes, a[6]);
+  set_address(token_scores, a[7]);
   Py_RETURN_NONE;
   END_HANDLE_TH_ERRORS
 }
@@ -548,7 +610,8 @@ PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
 
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(bind), METHOD(cache_plan), METHOD(cache_append), METHOD(cache_attention), METHOD(prompt_attention),
-                         METHOD(bind_around), METHOD(rotate_heads), METHOD(cache_fork), METHOD(cache_compact), METHOD(cache_copy), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(bind_around), METHOD(rotate_heads), METHOD(cache_fork), METHOD(cache_compact), METHOD(cache_copy),
+                         METHOD(token_scores), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_serve_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

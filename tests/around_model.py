@@ -73,3 +73,66 @@ def compact(table, lengths, block, n_blocks, free):
     room = min(len(free), n_blocks // 2)
     return {"block_table": [[moves.get(b, b) for b in row] + [-1] * (len(table[0]) - len(row)) for row in held],
             "copies": [list(m) for m in moves.items()] + [[-1, -1]] * (room - len(moves)), "free_blocks": rest, "counts": [len(moves), len(used)]}
+
+
+class Scores:
+    """What fikit_token_scores says about logits [rows, V], in 64 bits, and how far it may be off.
+
+    A term exp(z_j) has the relative error e_j = 2^-22 (1 + |z_j| + |z_j - max z|): the constant scale * log2(e) is rounded twice (2^-23 |z_j|), the
+    difference to the reference once, the exponential is within 2^-23.  Sums: a lane adds up V / 64 terms at most, then 20 steps join lanes, waves and
+    parts, n = (V / 64 + 20) 2^-24 in all.  So the sum's logarithm is off by sum p e + n and its own rounding 2^-22 (1 + |lse|), a log
+    probability by e of its token besides, and the entropy sum p (-log p) by 2 sum p e (1 + |log p|) + 2 n (1 + sum p |z - max z|) + 2^-21 (1 + H)."""
+
+    def __init__(self, logits, tokens, scale, top):
+        x = logits.double().cpu()
+        rows, v = x.shape
+        inf = float("inf")
+        z = x * float(torch.tensor(scale, dtype=torch.float32))
+        odd = (torch.isnan(x) | (x == inf)).any(1)
+        nothing = (x == -inf).all(1)
+        fine = ~odd & ~nothing
+        zz = torch.where(fine[:, None], z, torch.zeros(()).double())
+        most = zz.amax(1, keepdim=True) if v else zz.new_zeros((rows, 1))
+        beyond = torch.logsumexp(zz - most, 1)                      # (relative to the largest, whatever its size)
+        lse = most[:, 0] + beyond
+        log_p = zz - most - beyond[:, None]
+        p = log_p.exp()
+        size, away = torch.where(p > 0, zz.abs(), 0.0), torch.where(p > 0, (zz - most).abs(), 0.0)
+        e = 2.0 ** -22 * (1 + size + away)
+        n = (v / 64 + 20) * 2.0 ** -24
+        minus_log = torch.where(p > 0, -log_p, 0.0)
+        h = (p * minus_log).sum(1)
+        self.bound = {"lse": (p * e).sum(1) + n + 2.0 ** -22 * (1 + lse.abs())}
+        self.bound["entropy"] = 2 * (p * e * (1 + minus_log)).sum(1) + 2 * n * (1 + (p * away).sum(1)) + 2.0 ** -21 * (1 + h)
+
+        def whole(values, of_nothing):
+            return torch.where(odd, torch.nan, torch.where(nothing, of_nothing, values))
+        self.want = {"lse": whole(lse, -inf), "entropy": whole(h, 0.0)}
+        of_token = self.bound["lse"][:, None] + 2.0 ** -22 * (1 + z.abs() + (z - most).abs())
+        values = torch.where(torch.isfinite(z) & fine[:, None], log_p, torch.full((), -inf).double())
+        values = torch.where(odd[:, None], torch.nan, values)
+        if tokens is not None:
+            t = tokens.long().cpu()
+            at = t.clamp(min=0)[:, None]
+            given = t >= 0
+            self.want["logprob"] = torch.where(given, values.gather(1, at)[:, 0], 0.0) if v else torch.zeros(rows).double()
+            self.bound["logprob"] = torch.where(given, of_token.gather(1, at)[:, 0], 0.0) if v else torch.zeros(rows).double()
+        order = torch.sort(torch.where(torch.isnan(x), -inf, x + 0.0), dim=1, descending=True, stable=True).indices[:, :top]
+        there = torch.zeros((rows, top), dtype=torch.bool)
+        there[:, :order.shape[1]] = torch.isfinite(z.gather(1, order)) & fine[:, None]
+        order = torch.nn.functional.pad(order, (0, top - order.shape[1]))
+        self.want["top_tokens"] = torch.where(there, order, -1)
+        if v:
+            self.want["top_logprob"] = torch.where(odd[:, None], torch.nan, torch.where(there, values.gather(1, order), -inf))
+            self.bound["top_logprob"] = of_token.gather(1, order)
+        else:
+            self.want["top_logprob"], self.bound["top_logprob"] = torch.full((rows, top), -inf).double(), torch.zeros((rows, top)).double()
+
+    def differs(self, got):
+        """Names of the outputs that are not as wanted."""
+        bad = []
+        for name, want in self.want.items():
+            g = getattr(got, name).cpu()
+            if not (torch.equal(g.long(), want) if name == "top_tokens" else near(g, want, self.bound[name])):
+                bad.append(name)
+        return bad

@@ -144,3 +144,44 @@ def test_block_bindings():
         native.cache_copy(5, table, status, 0)
     with pytest.raises(ValueError):
         native.cache_copy([(codes, codes, exps, exps)], i, status, 0)
+
+
+def scores(**change):
+    a = dict(logits=FAKE, value_type=0, stride=70000, rows=4, vocabulary=70000, scale=1.0, tokens=FAKE, n_top=3, logprob=FAKE, entropy=FAKE, lse=FAKE, top_tokens=FAKE,
+             top_logprob=FAKE, status=FAKE, ws=FAKE, ws_bytes=1 << 30)
+    assert set(change) <= set(a)
+    a.update(change)
+    return binding.load().fikit_token_scores(*a.values(), None)
+
+
+@pytest.mark.parametrize("change, want", [
+    (dict(logits=NULL), INVALID), (dict(logits=ODD), INVALID), (dict(logits=FAKE + 2, value_type=2), INVALID), (dict(value_type=3), INVALID), (dict(value_type=-1), INVALID),
+    (dict(rows=1 << 31), INVALID), (dict(vocabulary=1 << 31), INVALID), (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID), (dict(scale=float("nan")), INVALID),
+    (dict(scale=float("inf")), INVALID), (dict(scale=1e-31), INVALID), (dict(scale=2e30), INVALID), (dict(tokens=ODD), INVALID), (dict(logprob=ODD), INVALID),
+    (dict(entropy=ODD), INVALID), (dict(lse=ODD), INVALID), (dict(top_tokens=NULL), INVALID), (dict(top_tokens=ODD), INVALID), (dict(top_logprob=NULL), INVALID),
+    (dict(top_logprob=ODD), INVALID), (dict(status=NULL), INVALID), (dict(status=ODD), INVALID), (dict(ws=NULL), INVALID), (dict(ws=FAKE + 16), INVALID),
+    (dict(ws_bytes=16), SMALL), (dict(n_top=33), UNSUPPORTED), (dict(rows=1 << 24), UNSUPPORTED), (dict(rows=0, logits=NULL, ws=NULL), OK)])
+def test_token_scores(change, want):
+    assert scores(**change) == want
+
+
+def test_token_scores_workspace():
+    f = binding.fikit_token_scores_workspace_bytes
+    assert f(1, 131072, 0, 20) > 0 and f(1, 131072, 2, 32) > f(1, 131072, 2, 0) > 0
+    assert f(1, 131072, 0, 33) == f(1 << 24, 10, 0, 3) == f(1, 10, 3, 3) == f(1, 10, 0, 3) == f(100000, 131072, 0, 20) == 0
+
+
+def test_token_scores_binding():
+    x, t, status, native = torch.zeros(3, 10), torch.zeros(3, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), binding._marshal()
+
+    def call(logits=x, tokens=t, n_top=2, out=None):
+        return native.token_scores(logits, tokens, status, 1.0, n_top, out, None, 0)
+    with pytest.raises(ValueError):
+        binding.fikit_token_scores(x, t, status)                             # tensors on a GPU
+    f = torch.zeros(3)
+    for bad in (dict(logits=x.double()), dict(logits=x[0]), dict(logits=x.t()), dict(tokens=t[:2]), dict(tokens=t.long()), dict(logits=x.clone().requires_grad_()),
+                dict(n_top=-1), dict(out=(f, f, f)), dict(out=(f, f, f, None, None)), dict(out=(f[:2], f, f, x[:, :2].int(), x[:, :2])),
+                dict(out=(f, f, f, x[:, :2].contiguous(), x[:, :2].contiguous()))):
+        with pytest.raises(ValueError):
+            call(**bad)
+    assert call(n_top=33) == UNSUPPORTED and call(logits=x[:0], tokens=t[:0])[0].shape == (0,)

@@ -1,0 +1,209 @@
+"""Log probabilities, entropy and alternatives of rows of logits against 64 bits."""
+import math
+
+import pytest
+import torch
+
+import around_model as model
+from paper_2311_10359_amd import binding
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = [torch.bfloat16, torch.float16, torch.float32]
+
+
+def status_word():
+    return torch.zeros(1, dtype=torch.int32, device=DEV)
+
+
+def normal(seed, *shape):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed), dtype=torch.float32)
+
+
+def tokens_for(seed, rows, v):
+    t = torch.randint(0, max(v, 1), (rows,), generator=torch.Generator().manual_seed(seed), dtype=torch.int32)
+    t[::5] = -1 - t[::5]
+    return t.to(DEV)
+
+
+def check(logits, tokens, top, scale=1.0):
+    status = status_word()
+    got = binding.fikit_token_scores(logits, tokens, status, scale=scale, n_top=top)
+    binding.fikit_check_status(status)
+    assert (got.logprob is None) == (tokens is None) and got.top_tokens.shape == (logits.shape[0], top)
+    assert model.Scores(logits, tokens, scale, top).differs(got) == []
+    return got
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("v", [1, 2, 3, 7, 8, 9, 15, 16, 17, 31, 64, 65, 511, 513, 4096, 4099, 16384, 16391, 50001, 131072])
+def test_vocabularies(v, dtype):
+    rows = 9
+    whole = torch.empty(rows * (v + 3) + 8, dtype=dtype, device=DEV)
+    for top, offset, gap in ((0, 0, 0), (1, 1, 0), (5, 3, 1), (20, 0, 3), (32, 5, 2)):
+        x = whole[offset:offset + rows * (v + gap)].view(rows, v + gap)[:, :v]
+        x.copy_(normal(v + top, rows, v) * 3)
+        check(x, tokens_for(top, rows, v), top, (1.0, 0.7, 3.0, 1.25, 0.01)[top % 5])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_equal_values(dtype):
+    for v in (5, 33, 100, 700, 5000, 33333):
+        for seed, few in enumerate(([0.0], [0.0, -0.0], [1.0, 2.0], [-1.0, -2.0, -0.0, 0.0], [-float("inf"), 3.0])):
+            pick = torch.randint(0, len(few), (6, v), generator=torch.Generator().manual_seed(seed + v))
+            x = torch.tensor(few)[pick].to(dtype).to(DEV)
+            for top in (1, 7, 32):
+                check(x, tokens_for(seed, 6, v), top)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_orders(dtype):
+    """Ascending, descending, periodic and lone large values at every kind of place."""
+    for v in (600, 20000, 40007):
+        up = torch.linspace(-20, 20, v)
+        x = torch.stack([up, up.flip(0), torch.arange(v) % 512 / 16.0, torch.arange(v) % 8 / 1.0, torch.arange(v) % 4096 * 1.0 / 256, torch.where(torch.arange(v) < 40, 9.0, -9.0),
+                         torch.where(torch.arange(v) >= v - 40, 9.0, -9.0)])
+        y = normal(v, 40, v)
+        for i, at in enumerate([0, 1, 2, 7, 8, 9, 63, 64, 511, 512, 513, v // 4, v // 2, v - 1, v - 2, v - 7, v - 8, v - 9]):
+            y[i, at] = 30.0
+        for z in (x, y):
+            z = z.to(dtype).to(DEV)
+            for top in (3, 32):
+                check(z, tokens_for(1, z.shape[0], v), top)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("left", [0, 1, 2, 5, 31, 40])
+def test_masks(left, dtype):
+    for v in (1, 9, 100, 5000, 70001):
+        x = normal(left, 11, v)
+        for r in range(11):
+            order = torch.randperm(v, generator=torch.Generator().manual_seed(r))
+            x[r, order[left:]] = -math.inf
+        x = x.to(dtype).to(DEV)
+        for top in (0, 5, 32):
+            check(x, tokens_for(3, 11, v), top, 0.5)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_lowest_values_as_masks(dtype):
+    """The type's lowest value in masked places, in place of minus infinity."""
+    lowest = torch.finfo(dtype).min
+    for v in (40, 9000):
+        x = normal(5, 6, v).to(dtype)
+        x[0], x[1, 3:], x[2, ::2], x[3, :-1] = lowest, lowest, lowest, lowest
+        for scale in (2.0 ** -10, 0.7, 1.0):
+            check(x.to(DEV), tokens_for(4, 6, v), 12, scale)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_what_is_not_finite_stays_in_its_row(dtype):
+    for v in (8, 1000, 30011):
+        x = normal(6, 9, v).to(dtype)
+        x[1, 0], x[2, v - 1], x[4, v // 2], x[5, 1] = math.inf, math.nan, math.nan, math.inf
+        x[6], x[7] = math.nan, math.inf
+        x[2, :v // 2] = -math.inf
+        tokens = torch.zeros(9, dtype=torch.int32, device=DEV)
+        tokens[5] = -1
+        got = check(x.to(DEV), tokens, 4)
+        assert float(got.logprob[5]) == 0.0 and bool((got.top_tokens[1] == -1).all())
+
+
+def test_ranges():
+    for dtype, size in ((torch.float32, 1e4), (torch.float32, 1e-6), (torch.bfloat16, 3e4), (torch.bfloat16, 1e-30), (torch.float16, 6e4)):
+        x = (normal(7, 5, 3000).clamp(-1, 1) * size).to(dtype).to(DEV)
+        check(x, tokens_for(6, 5, 3000), 9)
+        check(x, tokens_for(6, 5, 3000), 9, 1e-3)
+    x = (normal(8, 5, 3000).clamp(-1, 1) * 3.3e38).to(torch.bfloat16).to(DEV)
+    check(x, tokens_for(6, 5, 3000), 9, 2.0 ** -100)
+    check(x, tokens_for(6, 5, 3000), 9, 2.0 ** -4)
+    x = (normal(8, 5, 3000) + 1000).to(torch.float32).to(DEV)
+    check(x, tokens_for(6, 5, 3000), 9, 2.0 ** 10)
+    check(x - 2000, tokens_for(6, 5, 3000), 9)
+
+
+def test_one_token_holds_all():
+    x = torch.zeros(3, 5001, device=DEV)
+    x[0, 17], x[1, 5000], x[2, 0] = 200.0, 1e5, 30.0
+    got = check(x, torch.tensor([17, 5000, 0], dtype=torch.int32, device=DEV), 2)
+    # The reference is the nearest whole number, so |d| <= 1/2 of the one that counts, S = 2^d (1 + 2^-23) and log2 S = d + 1.45 * 2^-23 + 2^-24 (its own
+    # rounding): entropy and log probability, ln 2 times what that differs from T / S = d (1 + 2^-24) and from d, are within 2^-22 of zero.
+    assert 0 <= float(got.entropy[0]) <= 2.0 ** -22 and -2.0 ** -22 <= float(got.logprob[0]) <= 0 and bool((got.logprob <= 0).all())
+
+
+@pytest.mark.parametrize("rows, v, dtype", [(70000, 13, torch.float32), (3000, 1000, torch.bfloat16), (600, 8192, torch.float16), (130, 50000, torch.bfloat16), (3, 1 << 20, torch.float16),
+                                            (1, 2_000_003, torch.float32), (2, 300_001, torch.bfloat16), (511, 20001, torch.bfloat16), (513, 20001, torch.bfloat16)])
+def test_rows(rows, v, dtype):
+    x = torch.randn((rows, v), generator=torch.Generator(device=DEV).manual_seed(rows), device=DEV, dtype=torch.float32).mul_(2).to(dtype)
+    check(x, tokens_for(8, rows, v), 20 if v > 100 else 3)
+
+
+def test_strides():
+    x = normal(9, 1, 5000).to(DEV)
+    got = check(x.expand(7, -1), tokens_for(9, 7, 5000), 5)
+    assert bool((got.lse == got.lse[0]).all())
+    check(normal(9, 40, 701).to(torch.bfloat16).to(DEV)[::3, 1:700], tokens_for(9, 14, 699), 5)
+    check(normal(9, 1, 6).to(DEV).t()[:, :1], tokens_for(9, 6, 1), 2)
+    check(torch.zeros((5, 0), device=DEV), torch.full((5,), -1, dtype=torch.int32, device=DEV), 3)
+
+
+def test_rows_beyond_32_bits():
+    rows, v = 33000, 131072
+    x = torch.zeros((rows, v), dtype=torch.bfloat16, device=DEV)
+    x[-3:] = (normal(10, 3, v) * 2).to(torch.bfloat16).to(DEV)
+    tokens = tokens_for(10, rows, v)
+    got = binding.fikit_token_scores(x, tokens, status_word(), n_top=4)
+    want = model.Scores(x[-4:], tokens[-4:], 1.0, 4)
+    assert want.differs(binding.TokenScores(*(t[-4:] for t in got))) == []
+    assert bool((got.top_tokens[:-3] == torch.arange(4, device=DEV)).all()) and bool(((got.entropy[:-3] - math.log(v)).abs() < 1e-4).all())
+
+
+def test_outputs_that_are_not_wanted():
+    x, tokens = normal(11, 5, 900).to(DEV), tokens_for(11, 5, 900)
+    want = check(x, tokens, 4)
+    for keep in range(3):
+        out = [None] * 5
+        out[keep] = torch.full((5,), 7.0, device=DEV)
+        got = binding.fikit_token_scores(x, tokens, status_word(), out=binding.TokenScores(*out))
+        assert torch.equal(got[keep], want[keep])
+    out = binding.TokenScores(None, None, None, torch.zeros((5, 4), dtype=torch.int32, device=DEV), torch.zeros((5, 4), device=DEV))
+    binding.fikit_token_scores(x, None, status_word(), n_top=4, out=out)
+    assert torch.equal(out.top_tokens, want.top_tokens) and torch.equal(out.top_logprob, want.top_logprob)
+    check(x, None, 4)
+    empty = binding.fikit_token_scores(x[:0], tokens[:0], status_word(), n_top=4)
+    assert empty.top_tokens.shape == (0, 4) and empty.lse.shape == (0,)
+
+
+def test_a_token_outside_the_vocabulary_and_a_status_that_stops():
+    for v in (50, 60000):
+        x = normal(12, 4, v).to(DEV)
+        for bad in (v, 2 ** 31 - 1):
+            status = status_word()
+            binding.fikit_token_scores(x, torch.tensor([0, bad, 1, 2], dtype=torch.int32, device=DEV), status, n_top=2)
+            assert int(status) == binding.FIKIT_INVALID_ARG
+        out = binding.TokenScores(*(torch.full((4,), 5.0, device=DEV) for _ in range(3)), None, None)
+        binding.fikit_token_scores(x, torch.zeros(4, dtype=torch.int32, device=DEV), status, out=out)
+        assert all(bool((t == 5).all()) for t in out[:3])
+
+
+def test_the_same_to_the_bit_replayed_and_on_another_stream():
+    for rows, v in ((2, 140_001), (700, 3001)):
+        x, tokens, status = normal(13, rows, v).to(torch.bfloat16).to(DEV), tokens_for(13, rows, v), status_word()
+        ws = torch.empty(max(256, binding.fikit_token_scores_workspace_bytes(rows, v, 0, 6)), dtype=torch.uint8, device=DEV)
+        want = check(x, tokens, 6)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        got = binding.fikit_token_scores(x, tokens, status, n_top=6, stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+        out = binding.TokenScores(*(torch.empty_like(t) for t in want))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            binding.fikit_token_scores(x, tokens, status, n_top=6, out=out, workspace_buf=ws)
+        for i in range(4):
+            x.copy_(normal(20 + i, rows, v))
+            ws.fill_(255 * (i % 2))
+            graph.replay()
+            want = binding.fikit_token_scores(x, tokens, status, n_top=6)
+            assert all(torch.equal(a, b) for a, b in zip(want, out))
+        assert int(status) == 0
