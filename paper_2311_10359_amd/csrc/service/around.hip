@@ -109,19 +109,23 @@ BlocksArgs blocks_args(const int32_t* d_block_table, uint32_t table_width, const
 
 // How rows of logits are cut up, and the workspace.
 struct ScoresCut {
-  uint32_t parts, per_wave;
+  uint32_t parts, per_part, waves;
   uint64_t sums_bytes, bytes;
 };
-constexpr uint32_t SCORES_CHIP = 512;             // workgroups: two for each CU
+constexpr uint32_t SCORES_FEW = 1024;             // rows below which 16 waves take a row, or a part of it; 4 beyond
+constexpr uint32_t SCORES_CHIP = 256;             // workgroups of 16 waves
 
 ScoresCut scores_cut(uint32_t n_rows, uint32_t vocabulary, int32_t value_type, uint32_t n_top) {
   ScoresCut c{};
-  const uint32_t groups = vocabulary / (value_type == FIKIT_F32 ? LogitsF32::VEC : LogitsBf16::VEC), turn = SCORES_BATCH * WAVE;
-  const uint32_t most = (groups + SCORES_WAVES * turn - 1) / (SCORES_WAVES * turn), want = n_rows ? (SCORES_CHIP + n_rows - 1) / n_rows : 1;
+  const uint32_t groups = vocabulary / (value_type == FIKIT_F32 ? LogitsF32::VEC : LogitsBf16::VEC);
+  c.waves = n_rows < SCORES_FEW ? 16 : 4;
+  const uint32_t turn = SCORES_BATCH * WAVE * c.waves, most = (groups + turn - 1) / turn;
+  const uint32_t want = n_rows == 0 || n_rows >= SCORES_CHIP ? 1 : SCORES_CHIP / n_rows;
   c.parts = want < most ? want : most;
   if (c.parts < 1) c.parts = 1;
-  const uint32_t waves = c.parts * SCORES_WAVES, each = (groups + waves - 1) / waves;
-  c.per_wave = (each + WAVE - 1) / WAVE * WAVE;
+  const uint32_t each = (groups + c.parts - 1) / c.parts;
+  c.per_part = (each + WAVE - 1) / WAVE * WAVE;
+  if (groups > 0) c.parts = (groups + c.per_part - 1) / c.per_part;
   if (c.parts == 1) return c;
   const uint64_t lists = static_cast<uint64_t>(n_rows) * c.parts;
   c.sums_bytes = (lists * sizeof(float4) + 255) / 256 * 256;
@@ -131,12 +135,13 @@ ScoresCut scores_cut(uint32_t n_rows, uint32_t vocabulary, int32_t value_type, u
 
 struct ScoresCall {
   const ScoresArgs& a;
+  uint32_t waves;
   hipStream_t st;
   template <typename L>
   int run() {
-    const dim3 block(SCORES_WAVES * WAVE);
-    if (int rc = enqueue(k_scores<L>, dim3(a.rows * a.parts), block, st, a)) return rc;
-    return a.parts == 1 ? FIKIT_OK : enqueue(k_scores_join<L>, dim3((a.rows + SCORES_WAVES - 1) / SCORES_WAVES), block, st, a);
+    const dim3 grid(a.rows * a.parts), block(waves * WAVE), join(JOIN_WAVES * WAVE);
+    if (int rc = waves == 16 ? enqueue(k_scores<L, 16>, grid, block, st, a) : enqueue(k_scores<L, 4>, grid, block, st, a)) return rc;
+    return a.parts == 1 ? FIKIT_OK : enqueue(k_scores_join<L>, dim3((a.rows + JOIN_WAVES - 1) / JOIN_WAVES), join, st, a);
   }
 };
 
@@ -340,10 +345,10 @@ int fikit_token_scores(const void* d_logits, int32_t value_type, uint64_t row_st
   a.vocabulary = vocabulary;
   a.n_top = n_top;
   a.parts = c.parts;
-  a.per_wave = c.per_wave;
+  a.per_part = c.per_part;
   a.scale = scale;
   a.c = scale * LOG2E;
-  ScoresCall call{a, static_cast<hipStream_t>(hip_stream)};
+  ScoresCall call{a, c.waves, static_cast<hipStream_t>(hip_stream)};
   return value_type == FIKIT_BF16 ? call.run<LogitsBf16>() : value_type == FIKIT_F16 ? call.run<LogitsF16>() : call.run<LogitsF32>();
 }
 

@@ -33,13 +33,13 @@ struct ScoresArgs {
   int32_t* top_tokens;
   float* top_logprob;
   int32_t* status;
-  float4* sums;             // workspace: [rows][parts] R, S, T and the number of groups in the list
-  float2* lists;            // [rows][parts][n_top] maxima and groups
-  uint32_t rows, vocabulary, n_top, parts, per_wave;      // per_wave: groups
+  float4* sums;             // workspace: [rows][parts] R / 4, S and T
+  float2* lists;            // [rows][parts][n_top] maxima and groups, minus infinity where there is none
+  uint32_t rows, vocabulary, n_top, parts, per_part;      // per_part: groups
   float scale, c;           // c = scale log2(e)
 };
 
-constexpr int SCORES_WAVES = 4, SCORES_BATCH = 8, SCORES_MOST = 32, SCORES_ROOM = 128;
+constexpr int SCORES_BATCH = 4, SCORES_MOST = 32, SCORES_ROOM = 128, JOIN_WAVES = 4;
 constexpr float NO_SUM = -3.4028234663852886e38f;       // R / 4 where nothing has been seen
 constexpr float WHOLE = 0x1p20f;                        // R / 4 below which R is whole
 
@@ -79,38 +79,56 @@ __device__ __forceinline__ uint32_t key_of(float v) {
   const uint32_t bits = __float_as_uint(v + 0.f);
   return bits >> 31 ? ~bits : bits | 0x80000000u;
 }
+constexpr uint32_t LOWEST_KEY = 0x00800000u;             // of the lowest finite value
 __device__ __forceinline__ float value_of_key(uint32_t key) { return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key); }
 
-// The largest key that k or more of the wave's keys reach (N to a lane; 0: none), of which the upper BITS differ.
+// A key that k of the wave's keys reach (N to a lane; 0: none) and no more, or the largest one that k or more reach, if some are equal.  More than k
+// keys are given, of which the upper BITS differ; the k-th largest is `least` or more.  (Bit by bit from the first one in which `least` and the
+// largest key differ.)
 template <int BITS, int N>
-__device__ __forceinline__ uint32_t reached_by(const uint32_t (&keys)[N], uint32_t k) {
-  uint32_t found = 0;
+__device__ __forceinline__ uint32_t reached_by(const uint32_t (&keys)[N], uint32_t k, uint32_t least) {
+  uint32_t most = keys[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) most = max_u32(most, keys[i]);
+  most = max_over_wave(most);
+  const int from = 31 - __builtin_clz((most ^ least) | 1);
+  uint32_t found = most >> from >> 1 << from << 1;
 #pragma unroll 1
-  for (int b = 31; b >= 32 - BITS; --b) {
+  for (int b = from; b >= 32 - BITS; --b) {
     const uint32_t next = found | 1u << b;
     uint32_t n = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) n += popc64(ballot(keys[i] >= next));
     if (n >= k) found = next;
+    if (n == k) break;
   }
   return found;
 }
 
-// Which of the keys are the first k: those beyond the k-th largest, and of those equal to it the first ones.  Their places in turn.
+// Which of the keys are the first k: the larger ones, and of those equal to the k-th largest the ones of the lowest `order`, which is different for
+// each.  Their places in turn.  Returns a key that all of them reach.
 template <int BITS, int N>
-__device__ __forceinline__ uint32_t first_of(const uint32_t (&keys)[N], uint32_t k, bool (&keep)[N], uint32_t (&place)[N]) {
-  const uint32_t border = reached_by<BITS, N>(keys, k);
-  constexpr uint32_t LOW = BITS == 32 ? 0 : (1u << (32 - BITS) % 32) - 1;
-  uint32_t larger = 0;
+__device__ __forceinline__ uint32_t first_of(const uint32_t (&keys)[N], const uint32_t (&order)[N], uint32_t k, uint32_t least, bool (&keep)[N],
+                                             uint32_t (&place)[N]) {
+  const uint32_t border = reached_by<BITS, N>(keys, k, least);
+  uint32_t reached = 0;
 #pragma unroll
-  for (int i = 0; i < N; ++i) larger += popc64(ballot(keys[i] > (border | LOW)));
-  uint32_t equal = k - larger, n = 0;
+  for (int i = 0; i < N; ++i) reached += popc64(ballot(keys[i] >= border));
+  uint32_t largest_equal = border, last = 0;   // of the keys border .. largest_equal, those whose ~order reaches `last` stay
+  if (reached > k) {
+    if (BITS < 32) largest_equal |= (1u << (32 - BITS) % 32) - 1;
+    uint32_t equal[N], larger = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      equal[i] = keys[i] >= border && keys[i] <= largest_equal ? ~order[i] : 0;
+      larger += popc64(ballot(keys[i] > largest_equal));
+    }
+    last = reached_by<32, N>(equal, k - larger, 0);
+  }
+  uint32_t n = 0;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const uint64_t same = ballot(keys[i] >= border && keys[i] <= (border | LOW));
-    keep[i] = keys[i] > (border | LOW) || ((same >> lane_id() & 1) && popc_below(same) < equal);
-    const uint32_t of = popc64(same);
-    equal -= of < equal ? of : equal;
+    keep[i] = keys[i] > largest_equal || (keys[i] >= border && ~order[i] >= last);
     const uint64_t kept = ballot(keep[i]);
     place[i] = n + popc_below(kept);
     n += popc64(kept);
@@ -118,7 +136,7 @@ __device__ __forceinline__ uint32_t first_of(const uint32_t (&keys)[N], uint32_t
   return border;
 }
 
-struct ScoresLds {          // of a wave: its groups, ascending
+struct ScoresLds {          // of a wave: its groups
   float most[SCORES_ROOM];
   uint32_t group[SCORES_ROOM];
 };
@@ -158,14 +176,25 @@ struct Sums {
   }
 };
 
+__device__ __forceinline__ float sum_over_wave(float v) {
+  const auto from = [](float x, auto dpp) { return __uint_as_float(dpp(__float_as_uint(x))); };
+  v += from(v, dpp_or_zero<0x111, 0xf>);
+  v += from(v, dpp_or_zero<0x112, 0xf>);
+  v += from(v, dpp_or_zero<0x114, 0xf>);
+  v += from(v, dpp_or_zero<0x118, 0xf>);
+  v += from(v, dpp_or_zero<0x142, 0xa>);
+  v += from(v, dpp_or_zero<0x143, 0xc>);
+  return __uint_as_float(read_lane_u32(__float_as_uint(v), WAVE - 1));
+}
+
 // What a wave has seen of a row.
 template <typename L>
 struct Seen {
   Sums sums;                               // of each lane
   uint32_t n = 0, k;                       // groups in the list; how many are wanted
-  float border;                            // only groups beyond it are
+  float border;                            // only groups that reach it are; none reaches NaN
 
-  __device__ __forceinline__ explicit Seen(uint32_t n_top) : k(n_top), border(n_top ? -INFINITY : INFINITY) {}
+  __device__ __forceinline__ explicit Seen(uint32_t n_top) : k(n_top), border(n_top ? -INFINITY : NAN) {}
 
   template <int N>
   __device__ __forceinline__ void add(const float (&x)[N], float most, float least, float c) {
@@ -192,9 +221,10 @@ struct Seen {
     sums.t += t;
   }
 
-  // A group for each lane that has one, ascending over the lanes and behind all before.
-  __device__ __forceinline__ void offer(bool has, float most, uint32_t group, ScoresLds* lds) {
-    const uint64_t hits = ballot(has && most > border);
+  // Groups, one to a lane, of which those that reach the border (or pass it: PASS, where they lie behind all others) join the list.
+  template <bool PASS>
+  __device__ __forceinline__ void offer(float most, uint32_t group, ScoresLds* lds) {
+    const uint64_t hits = ballot(PASS ? most > border : most >= border && most > -INFINITY);
     if (!hits) return;
     if (hits >> lane_id() & 1) {
       const uint32_t at = n + popc_below(hits);
@@ -220,7 +250,7 @@ struct Seen {
       groups[i] = lds->group[lane + i * WAVE];
     }
     lds_in_order();
-    const uint32_t last = first_of<L::KEY_BITS, N>(keys, k, keep, place);
+    const uint32_t reached = first_of<L::KEY_BITS, N>(keys, groups, k, key_of(border), keep, place);
 #pragma unroll
     for (int i = 0; i < N; ++i)
       if (keep[i]) {
@@ -229,18 +259,27 @@ struct Seen {
       }
     lds_in_order();
     n = k;
-    constexpr uint32_t LOW = L::KEY_BITS == 32 ? 0 : (1u << (32 - L::KEY_BITS) % 32) - 1;
-    border = value_of_key(last >> 31 ? last : last | LOW);
+    border = value_of_key(max_u32(reached, LOWEST_KEY));
+  }
+
+  // The first batch: the k-th largest of the lanes' maxima is a border for it, and no list of 64 groups in front of it has to be shortened.
+  __device__ __forceinline__ void begin(float most) {
+    const uint32_t keys[1] = {most > -INFINITY ? key_of(most) : 0};
+    if (popc64(ballot(keys[0] != 0)) <= k) return;
+    const uint32_t reached = reached_by<L::KEY_BITS, 1>(keys, k, 0);
+    if (reached > LOWEST_KEY) border = value_of_key(reached - (reached == 0x80000000u ? 2 : 1));         // (there is no key of -0)
+  }
+
+  // Lists of others: k groups of each reach its border.
+  __device__ __forceinline__ void begin_at(float theirs) {
+    if (k > 0) border = value_of_key(max_over_wave(key_of(theirs)));
   }
 
   // The lanes' sums become one, in all lanes.
   __device__ __forceinline__ void sum_over_lanes() {
-    float most = sums.r;
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) most = fmaxf(most, __shfl_xor(most, m, WAVE));
-    sums.move_to(most);
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) { sums.s += __shfl_xor(sums.s, m, WAVE); sums.t += __shfl_xor(sums.t, m, WAVE); }
+    sums.move_to(value_of_key(max_over_wave(key_of(sums.r))));
+    sums.s = sum_over_wave(sums.s);
+    sums.t = sum_over_wave(sums.t);
   }
 };
 
@@ -264,102 +303,120 @@ struct Row {
   }
 };
 
+// A row's given token, and its logit: asked for early.
+template <typename L>
+struct Given {
+  int32_t token = -1;
+  float x = 0;
+  __device__ __forceinline__ Given(const ScoresArgs& a, const Row<L>& row, uint32_t r) {
+    if (a.tokens) token = a.tokens[r];
+    if (token >= 0 && static_cast<uint32_t>(token) < a.vocabulary) x = L::value(row.x[token]);
+  }
+};
+
 // Everything that a row's outputs need is known to one wave.
 template <typename L>
-__device__ __forceinline__ void finish_row(const ScoresArgs& a, const Row<L>& row, uint32_t r, const Seen<L>& seen, ScoresLds* lds) {
+__device__ __forceinline__ void finish_row(const ScoresArgs& a, const Row<L>& row, uint32_t r, const Given<L>& given, const Seen<L>& seen, ScoresLds* lds) {
   const uint32_t lane = lane_id(), k = a.n_top;
+  // the values of the groups; where there are k groups, those below the least of their maxima are none of the k
+  constexpr int N = SCORES_MOST * L::VEC / WAVE;
+  uint32_t at[N];
+  float x[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint32_t e = lane + i * WAVE;
+    x[i] = NAN;
+    at[i] = 0;
+    if (e / L::VEC < seen.n && row.place(lds->group[e / L::VEC], e % L::VEC, &at[i])) x[i] = L::value(row.x[at[i]]);
+  }
   const Sums& sums = seen.sums;
   const bool nothing = sums.s == 0.f, odd = sums.s != sums.s;
   const float log_s = __builtin_amdgcn_logf(sums.s), lse = __builtin_fmaf(4.f * LN2, sums.r, LN2 * log_s);
-  auto logprob = [&](float x) {
-    if (nothing || x == -INFINITY) return -INFINITY;
-    const float d = sums.exponent(x, a.c);
-    return d > -4.f * WHOLE ? fminf(LN2 * (d - log_s), 0.f) : x * a.scale - lse;
+  auto logprob = [&](float v) {
+    if (nothing || v == -INFINITY) return -INFINITY;
+    const float d = sums.exponent(v, a.c);
+    return d > -4.f * WHOLE ? fminf(LN2 * (d - log_s), 0.f) : v * a.scale - lse;
   };
   if (lane == 0) {
-    const int32_t token = a.tokens ? a.tokens[r] : -1;
-    float of_token = 0.f;
-    if (token >= 0) {
-      if (static_cast<uint32_t>(token) < a.vocabulary) of_token = odd ? NAN : logprob(L::value(row.x[token]));
-      else *a.status = FIKIT_INVALID_ARG;
-    }
-    if (a.logprob) a.logprob[r] = of_token;
+    if (given.token >= 0 && static_cast<uint32_t>(given.token) >= a.vocabulary) *a.status = FIKIT_INVALID_ARG;
+    if (a.logprob) a.logprob[r] = given.token < 0 ? 0.f : odd ? NAN : logprob(given.x);
     if (a.lse) a.lse[r] = nothing ? -INFINITY : odd ? NAN : lse;
     if (a.entropy) a.entropy[r] = nothing ? 0.f : odd ? NAN : fmaxf(LN2 * (log_s - sums.t / sums.s), 0.f);
   }
   if (k == 0) return;
-  // the values of the groups
-  constexpr int N = SCORES_MOST * L::VEC / WAVE;
-  uint32_t keys[N], at[N], place[N];
+  float least = lane < seen.n ? lds->most[lane] : INFINITY;
+#pragma unroll
+  for (int m = SCORES_MOST / 2; m >= 1; m >>= 1) least = fminf(least, __shfl_xor(least, m, WAVE));
+  least = seen.n < k ? -INFINITY : __uint_as_float(read_lane_u32(__float_as_uint(least), 0));
   bool keep[N];
-  uint32_t valid = 0;
+  uint32_t place[N], n = 0;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const uint32_t e = lane + i * WAVE;
-    keys[i] = 0;
-    at[i] = 0;
-    if (e / L::VEC < seen.n && row.place(lds->group[e / L::VEC], e % L::VEC, &at[i])) {
-      const float x = L::value(row.x[at[i]]);
-      if (x > -INFINITY) keys[i] = key_of(x);
-    }
-    keep[i] = keys[i] != 0;
+    keep[i] = x[i] >= least && x[i] > -INFINITY;
     const uint64_t there = ballot(keep[i]);
-    place[i] = valid + popc_below(there);
-    valid += popc64(there);
+    place[i] = n + popc_below(there);
+    n += popc64(there);
   }
-  if (valid > k) first_of<L::KEY_BITS, N>(keys, k, keep, place);
-  const uint32_t n = min_u32(valid, k);
+  if (n > WAVE) {                              // (many equal ones)
+    uint32_t keys[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) keys[i] = keep[i] ? key_of(x[i]) : 0;
+    first_of<L::KEY_BITS, N>(keys, at, k, 0, keep, place);
+    n = k;
+  }
   lds_in_order();
 #pragma unroll
   for (int i = 0; i < N; ++i)
     if (keep[i]) {
-      lds->most[place[i]] = value_of_key(keys[i]);
+      lds->most[place[i]] = x[i];
       lds->group[place[i]] = at[i];
     }
   lds_in_order();
-  if (lane >= k) return;
   const uint64_t out = static_cast<uint64_t>(r) * k;
-  if (lane >= n || odd) {
+  if (lane < k && (lane >= n || odd)) {
     a.top_tokens[out + lane] = -1;
     a.top_logprob[out + lane] = odd ? NAN : -INFINITY;
-    return;
   }
+  if (lane >= n || odd) return;
   const float mine = lds->most[lane];
+  const uint32_t token = lds->group[lane];
   uint32_t rank = 0;
   for (uint32_t i = 0; i < n; ++i) {
     const float other = lds->most[i];
-    rank += other > mine || (other == mine && i < lane);
+    rank += other > mine || (other == mine && lds->group[i] < token);
   }
-  a.top_tokens[out + rank] = static_cast<int32_t>(lds->group[lane]);
+  if (rank >= k) return;
+  a.top_tokens[out + rank] = static_cast<int32_t>(token);
   a.top_logprob[out + rank] = logprob(mine);
 }
 
-template <typename L>
-__global__ __launch_bounds__(SCORES_WAVES * WAVE) void k_scores(ScoresArgs a) {
-  __shared__ ScoresLds lists[SCORES_WAVES];
-  __shared__ float4 sums[SCORES_WAVES];
+// A workgroup of W waves takes a part of a row, a batch of each wave's behind the other's.
+template <typename L, int W>
+__global__ __launch_bounds__(W * WAVE) void k_scores(ScoresArgs a) {
+  __shared__ ScoresLds lists[W];
+  __shared__ float2 firsts[W * SCORES_MOST];
+  __shared__ float4 sums[W];
   if (__syncthreads_or(stopped(a.status))) return;
   const uint32_t lane = lane_id(), wave = uniform(threadIdx.x / WAVE), r = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
   const Row<L> row(a, r);
+  const Given<L> given(a, row, r);
   ScoresLds* lds = &lists[wave];
   Seen<L> seen(a.n_top);
-  const uint32_t chunk = part * SCORES_WAVES + wave;
-  const uint64_t begin = static_cast<uint64_t>(chunk) * a.per_wave;
   auto edge = [&](uint32_t group, uint32_t first, uint32_t count) {        // less than a group, a logit to a lane
     const float x[1] = {lane < count ? L::value(row.x[first + lane]) : -INFINITY};
     seen.add(x, x[0], x[0], a.c);
-    seen.offer(lane == 0, value_of_key(max_over_wave(key_of(x[0]))), group, lds);
+    const float most = value_of_key(max_over_wave(key_of(x[0])));
+    seen.template offer<false>(lane == 0 ? most : -INFINITY, group, lds);
   };
-  if (chunk == 0 && row.head > 0) edge(0, 0, row.head);
-  const uint32_t end = begin + a.per_wave < row.whole ? static_cast<uint32_t>(begin) + a.per_wave : row.whole;
+  const uint32_t begin = part * a.per_part, end = row.whole - begin < a.per_part ? row.whole : begin + a.per_part;       // (parts begin within the row)
   const u32x4* groups = reinterpret_cast<const u32x4*>(row.x + row.head);
-  for (uint64_t at = begin; at < end; at += SCORES_BATCH * WAVE) {
+  for (uint64_t at = begin + wave * SCORES_BATCH * WAVE; at < end; at += W * SCORES_BATCH * WAVE) {
     u32x4 w[SCORES_BATCH];
     const uint32_t mine = static_cast<uint32_t>(at) + lane;
 #pragma unroll
     for (int i = 0; i < SCORES_BATCH; ++i) {
       w[i] = u32x4{L::NOTHING, L::NOTHING, L::NOTHING, L::NOTHING};
-      if (mine + i * WAVE < end) w[i] = groups[mine + i * WAVE];
+      if (mine + i * WAVE < end) w[i] = __builtin_nontemporal_load(groups + mine + i * WAVE);
     }
     float x[SCORES_BATCH * L::VEC], most[SCORES_BATCH], all = -INFINITY, least = INFINITY;
 #pragma unroll
@@ -374,58 +431,74 @@ __global__ __launch_bounds__(SCORES_WAVES * WAVE) void k_scores(ScoresArgs a) {
       all = fmaxf(all, most[i]);
     }
     seen.add(x, all, least, a.c);
+    if (seen.border == -INFINITY) seen.begin(all);
+    if (ballot(all > seen.border))
 #pragma unroll
-    for (int i = 0; i < SCORES_BATCH; ++i) seen.offer(mine + i * WAVE < end, most[i], 1 + mine + i * WAVE, lds);
+      for (int i = 0; i < SCORES_BATCH; ++i) seen.template offer<true>(most[i], 1 + mine + i * WAVE, lds);
   }
-  if (chunk == a.parts * SCORES_WAVES - 1 && row.rest() > 0) edge(row.whole + 1, row.vocabulary - row.rest(), row.rest());
+  if (part == 0 && wave == W - 1 && row.head > 0) edge(0, 0, row.head);
+  if (part == a.parts - 1 && wave == W - 2 && row.rest() > 0) edge(row.whole + 1, row.vocabulary - row.rest(), row.rest());
   seen.shorten(lds);
   seen.sum_over_lanes();
-  if (lane == 0) sums[wave] = make_float4(seen.sums.r, seen.sums.s, seen.sums.t, __uint_as_float(seen.n));
+  if (lane == 0) sums[wave] = make_float4(seen.sums.r, seen.sums.s, seen.sums.t, seen.border);
+  if (lane < a.n_top) firsts[wave * a.n_top + lane] = lane < seen.n ? make_float2(lds->most[lane], __uint_as_float(lds->group[lane])) : make_float2(-INFINITY, 0.f);
   __syncthreads();
   if (wave > 0) return;
-  // the first wave joins the others' sums and lists, in turn
-  seen.sums = Sums{};
-  if (lane < SCORES_WAVES) seen.sums = Sums{sums[lane].x, sums[lane].y, sums[lane].z};
-  seen.sum_over_lanes();
-  for (uint32_t w = 1; w < SCORES_WAVES; ++w) {
-    const bool there = lane < __float_as_uint(sums[w].w);
-    const float most = there ? lists[w].most[lane] : 0.f;
-    const uint32_t group = there ? lists[w].group[lane] : 0;
-    seen.offer(there, most, group, lds);
+  // the first wave joins the sums and the lists
+  Seen<L> joined(a.n_top);
+  const float4 of_wave = lane < W ? sums[lane] : make_float4(NO_SUM, 0.f, 0.f, -INFINITY);
+  joined.sums = Sums{of_wave.x, of_wave.y, of_wave.z};
+  joined.sum_over_lanes();
+  joined.begin_at(of_wave.w);
+  for (uint32_t at = 0; at < W * a.n_top; at += WAVE) {
+    const float2 of = at + lane < W * a.n_top ? firsts[at + lane] : make_float2(-INFINITY, 0.f);
+    joined.template offer<false>(of.x, __float_as_uint(of.y), lds);
   }
-  seen.shorten(lds);
+  joined.shorten(lds);
   if (a.parts == 1) {
-    finish_row<L>(a, row, r, seen, lds);
+    finish_row<L>(a, row, r, given, joined, lds);
     return;
   }
-  if (lane == 0) a.sums[blockIdx.x] = make_float4(seen.sums.r, seen.sums.s, seen.sums.t, __uint_as_float(seen.n));
-  if (lane < seen.n) a.lists[static_cast<uint64_t>(blockIdx.x) * a.n_top + lane] = make_float2(lds->most[lane], __uint_as_float(lds->group[lane]));
+  if (lane == 0) a.sums[blockIdx.x] = make_float4(joined.sums.r, joined.sums.s, joined.sums.t, joined.border);
+  if (lane < a.n_top)
+    a.lists[static_cast<uint64_t>(blockIdx.x) * a.n_top + lane] =
+        lane < joined.n ? make_float2(lds->most[lane], __uint_as_float(lds->group[lane])) : make_float2(-INFINITY, 0.f);
 }
 
 // Joins a row's parts: a wave each.
 template <typename L>
-__global__ __launch_bounds__(SCORES_WAVES * WAVE) void k_scores_join(ScoresArgs a) {
-  __shared__ ScoresLds lists[SCORES_WAVES];
+__global__ __launch_bounds__(JOIN_WAVES * WAVE) void k_scores_join(ScoresArgs a) {
+  __shared__ ScoresLds lists[JOIN_WAVES];
   if (stopped(a.status)) return;
-  const uint32_t lane = lane_id(), wave = uniform(threadIdx.x / WAVE), r = blockIdx.x * SCORES_WAVES + wave;
+  const uint32_t lane = lane_id(), wave = uniform(threadIdx.x / WAVE), r = blockIdx.x * JOIN_WAVES + wave;
   if (r >= a.rows) return;
   const Row<L> row(a, r);
+  const Given<L> given(a, row, r);
   ScoresLds* lds = &lists[wave];
   Seen<L> seen(a.n_top);
   const uint64_t first = static_cast<uint64_t>(r) * a.parts;
+  const uint32_t n = a.parts * a.n_top;
+  const float2* entries = a.lists + first * a.n_top;
+  constexpr int AHEAD = 4;                     // loads that wait for nothing
+  float2 of[AHEAD];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) of[i] = i * WAVE + lane < n ? entries[i * WAVE + lane] : make_float2(-INFINITY, 0.f);
+  float border = -INFINITY;
   for (uint32_t p = lane; p < a.parts; p += WAVE) {
-    const float4 of = a.sums[first + p];
-    seen.sums.add(Sums{of.x, of.y, of.z});
+    const float4 theirs = a.sums[first + p];
+    seen.sums.add(Sums{theirs.x, theirs.y, theirs.z});
+    border = fmaxf(border, theirs.w);
   }
   seen.sum_over_lanes();
-  for (uint32_t at = 0; at < a.parts * a.n_top; at += WAVE) {
-    const uint32_t e = at + lane, p = a.n_top ? e / a.n_top : 0;
-    const bool there = p < a.parts && e - p * a.n_top < __float_as_uint(a.sums[first + (p < a.parts ? p : 0)].w);
-    const float2 of = there ? a.lists[first * a.n_top + e] : make_float2(0.f, 0.f);
-    seen.offer(there, of.x, __float_as_uint(of.y), lds);
+  seen.begin_at(border);
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) seen.template offer<false>(of[i].x, __float_as_uint(of[i].y), lds);
+  for (uint32_t at = AHEAD * WAVE; at < n; at += WAVE) {
+    const float2 one = at + lane < n ? entries[at + lane] : make_float2(-INFINITY, 0.f);
+    seen.template offer<false>(one.x, __float_as_uint(one.y), lds);
   }
   seen.shorten(lds);
-  finish_row<L>(a, row, r, seen, lds);
+  finish_row<L>(a, row, r, given, seen, lds);
 }
 
 }  // namespace fikit
