@@ -39,7 +39,7 @@ struct ScoresArgs {
   float scale, c;           // c = scale log2(e)
 };
 
-constexpr int SCORES_BATCH = 4, SCORES_MOST = 32, SCORES_ROOM = 128, JOIN_WAVES = 4;
+constexpr int SCORES_BATCH = 4, SCORES_MOST = 32, SCORES_ROOM = 128, JOIN_WAVES = 4, JOIN_ROOM = 512;
 constexpr float NO_SUM = -3.4028234663852886e38f;       // R / 4 where nothing has been seen
 constexpr float WHOLE = 0x1p20f;                        // R / 4 below which R is whole
 
@@ -113,22 +113,25 @@ __device__ __forceinline__ uint32_t first_of(const uint32_t (&keys)[N], const ui
   const uint32_t border = reached_by<BITS, N>(keys, k, least);
   uint32_t reached = 0;
 #pragma unroll
-  for (int i = 0; i < N; ++i) reached += popc64(ballot(keys[i] >= border));
-  uint32_t largest_equal = border, last = 0;   // of the keys border .. largest_equal, those whose ~order reaches `last` stay
-  if (reached > k) {
-    if (BITS < 32) largest_equal |= (1u << (32 - BITS) % 32) - 1;
-    uint32_t equal[N], larger = 0;
+  for (int i = 0; i < N; ++i) {
+    keep[i] = keys[i] >= border;
+    reached += popc64(ballot(keep[i]));
+  }
+  if (reached > k) {                           // some are equal: one after the other, of the highest order first, goes
+    const uint32_t largest_equal = border | (BITS < 32 ? (1u << (32 - BITS) % 32) - 1 : 0);
+#pragma unroll 1
+    for (; reached > k; --reached) {
+      uint32_t last = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      equal[i] = keys[i] >= border && keys[i] <= largest_equal ? ~order[i] : 0;
-      larger += popc64(ballot(keys[i] > largest_equal));
+      for (int i = 0; i < N; ++i) last = max_u32(last, keep[i] && keys[i] <= largest_equal ? order[i] + 1 : 0);
+      last = max_over_wave(last);
+#pragma unroll
+      for (int i = 0; i < N; ++i) keep[i] = keep[i] && (keys[i] > largest_equal || order[i] + 1 != last);
     }
-    last = reached_by<32, N>(equal, k - larger, 0);
   }
   uint32_t n = 0;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    keep[i] = keys[i] > largest_equal || (keys[i] >= border && ~order[i] >= last);
     const uint64_t kept = ballot(keep[i]);
     place[i] = n + popc_below(kept);
     n += popc64(kept);
@@ -221,24 +224,33 @@ struct Seen {
     sums.t += t;
   }
 
-  // Groups, one to a lane, of which those that reach the border (or pass it: PASS, where they lie behind all others) join the list.
-  template <bool PASS>
-  __device__ __forceinline__ void offer(float most, uint32_t group, ScoresLds* lds) {
-    const uint64_t hits = ballot(PASS ? most > border : most >= border && most > -INFINITY);
+  // Groups, one to a lane, of which some join the list.  (It has room for 64 more.)
+  __device__ __forceinline__ void append(bool hit, float most, uint32_t group, ScoresLds* lds) {
+    const uint64_t hits = ballot(hit);
     if (!hits) return;
-    if (hits >> lane_id() & 1) {
+    if (hit) {
       const uint32_t at = n + popc_below(hits);
       lds->most[at] = most;
       lds->group[at] = group;
     }
     n += popc64(hits);
     lds_in_order();
-    if (n > WAVE) shorten(lds);
   }
 
-  // The first k stay.  (n is up to SCORES_ROOM)
+  // Takes from a list in LDS the first k that reach the border.  (In one loop, as elsewhere here: code that a wave runs once costs it more to fetch
+  // than to run.)
+  __device__ __forceinline__ void take(const float2* from, uint32_t count, ScoresLds* lds) {
+#pragma unroll 1
+    for (uint32_t at = 0;; at += WAVE) {
+      if (n > (at < count ? WAVE : k)) shorten(lds);
+      if (at >= count) break;
+      const float2 of = at + lane_id() < count ? from[at + lane_id()] : make_float2(-INFINITY, 0.f);
+      append(of.x >= border && of.x > -INFINITY, of.x, __float_as_uint(of.y), lds);
+    }
+  }
+
+  // The first k stay, of more.  (n is up to SCORES_ROOM)
   __device__ __forceinline__ void shorten(ScoresLds* lds) {
-    if (n <= k) return;
     constexpr int N = SCORES_ROOM / WAVE;
     const uint32_t lane = lane_id();
     uint32_t keys[N], groups[N], place[N];
@@ -303,32 +315,22 @@ struct Row {
   }
 };
 
-// A row's given token, and its logit: asked for early.
-template <typename L>
+// A row's given token; its logit is asked for early.
 struct Given {
-  int32_t token = -1;
-  float x = 0;
-  __device__ __forceinline__ Given(const ScoresArgs& a, const Row<L>& row, uint32_t r) {
-    if (a.tokens) token = a.tokens[r];
-    if (token >= 0 && static_cast<uint32_t>(token) < a.vocabulary) x = L::value(row.x[token]);
-  }
+  int32_t token;
+  float x;
 };
-
-// Everything that a row's outputs need is known to one wave.
 template <typename L>
-__device__ __forceinline__ void finish_row(const ScoresArgs& a, const Row<L>& row, uint32_t r, const Given<L>& given, const Seen<L>& seen, ScoresLds* lds) {
+__device__ __forceinline__ float given_logit(const ScoresArgs& a, const Row<L>& row, int32_t token) {
+  return token >= 0 && static_cast<uint32_t>(token) < a.vocabulary ? L::value(row.x[token]) : 0.f;
+}
+
+// The first k groups of the `count` in `from`, and, if this is all of the row, its outputs, by one wave that knows its sums.  `from` has room for the
+// groups' logits.
+template <typename L>
+__device__ __forceinline__ void finish_row(const ScoresArgs& a, const Row<L>& row, uint32_t r, const Given& given, Seen<L>& seen, float2* from, uint32_t count,
+                                           bool all, ScoresLds* lds) {
   const uint32_t lane = lane_id(), k = a.n_top;
-  // the values of the groups; where there are k groups, those below the least of their maxima are none of the k
-  constexpr int N = SCORES_MOST * L::VEC / WAVE;
-  uint32_t at[N];
-  float x[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const uint32_t e = lane + i * WAVE;
-    x[i] = NAN;
-    at[i] = 0;
-    if (e / L::VEC < seen.n && row.place(lds->group[e / L::VEC], e % L::VEC, &at[i])) x[i] = L::value(row.x[at[i]]);
-  }
   const Sums& sums = seen.sums;
   const bool nothing = sums.s == 0.f, odd = sums.s != sums.s;
   const float log_s = __builtin_amdgcn_logf(sums.s), lse = __builtin_fmaf(4.f * LN2, sums.r, LN2 * log_s);
@@ -337,41 +339,40 @@ __device__ __forceinline__ void finish_row(const ScoresArgs& a, const Row<L>& ro
     const float d = sums.exponent(v, a.c);
     return d > -4.f * WHOLE ? fminf(LN2 * (d - log_s), 0.f) : v * a.scale - lse;
   };
-  if (lane == 0) {
+  if (lane == 0 && all) {
     if (given.token >= 0 && static_cast<uint32_t>(given.token) >= a.vocabulary) *a.status = FIKIT_INVALID_ARG;
     if (a.logprob) a.logprob[r] = given.token < 0 ? 0.f : odd ? NAN : logprob(given.x);
     if (a.lse) a.lse[r] = nothing ? -INFINITY : odd ? NAN : lse;
     if (a.entropy) a.entropy[r] = nothing ? 0.f : odd ? NAN : fmaxf(LN2 * (log_s - sums.t / sums.s), 0.f);
   }
   if (k == 0) return;
-  float least = lane < seen.n ? lds->most[lane] : INFINITY;
+#pragma unroll 1
+  for (bool logits = false;; logits = true) {
+    seen.take(from, count, lds);
+    if (logits || !all) break;
+    // the groups' logits, of which those that reach the groups' border can be of the k
+    constexpr int N = SCORES_MOST * L::VEC / WAVE;
+    float x[N];
+    uint32_t at[N];
 #pragma unroll
-  for (int m = SCORES_MOST / 2; m >= 1; m >>= 1) least = fminf(least, __shfl_xor(least, m, WAVE));
-  least = seen.n < k ? -INFINITY : __uint_as_float(read_lane_u32(__float_as_uint(least), 0));
-  bool keep[N];
-  uint32_t place[N], n = 0;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    keep[i] = x[i] >= least && x[i] > -INFINITY;
-    const uint64_t there = ballot(keep[i]);
-    place[i] = n + popc_below(there);
-    n += popc64(there);
-  }
-  if (n > WAVE) {                              // (many equal ones)
-    uint32_t keys[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) keys[i] = keep[i] ? key_of(x[i]) : 0;
-    first_of<L::KEY_BITS, N>(keys, at, k, 0, keep, place);
-    n = k;
-  }
-  lds_in_order();
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-    if (keep[i]) {
-      lds->most[place[i]] = x[i];
-      lds->group[place[i]] = at[i];
+    for (int i = 0; i < N; ++i) {
+      const uint32_t e = lane + i * WAVE;
+      x[i] = -INFINITY;
+      at[i] = 0;
+      if (e / L::VEC < seen.n && row.place(lds->group[e / L::VEC], e % L::VEC, &at[i])) x[i] = L::value(row.x[at[i]]);
     }
-  lds_in_order();
+    count = seen.n * L::VEC;
+#pragma unroll
+    for (int i = 0; i < N; ++i) from[lane + i * WAVE] = make_float2(x[i], __uint_as_float(at[i]));
+    seen.n = 0;
+    lds_in_order();
+  }
+  const uint32_t n = seen.n;
+  if (!all) {
+    if (lane < k)
+      a.lists[static_cast<uint64_t>(blockIdx.x) * k + lane] = lane < n ? make_float2(lds->most[lane], __uint_as_float(lds->group[lane])) : make_float2(-INFINITY, 0.f);
+    return;
+  }
   const uint64_t out = static_cast<uint64_t>(r) * k;
   if (lane < k && (lane >= n || odd)) {
     a.top_tokens[out + lane] = -1;
@@ -385,7 +386,6 @@ __device__ __forceinline__ void finish_row(const ScoresArgs& a, const Row<L>& ro
     const float other = lds->most[i];
     rank += other > mine || (other == mine && lds->group[i] < token);
   }
-  if (rank >= k) return;
   a.top_tokens[out + rank] = static_cast<int32_t>(token);
   a.top_logprob[out + rank] = logprob(mine);
 }
@@ -394,25 +394,21 @@ __device__ __forceinline__ void finish_row(const ScoresArgs& a, const Row<L>& ro
 template <typename L, int W>
 __global__ __launch_bounds__(W * WAVE) void k_scores(ScoresArgs a) {
   __shared__ ScoresLds lists[W];
-  __shared__ float2 firsts[W * SCORES_MOST];
+  __shared__ float2 firsts[JOIN_ROOM];
   __shared__ float4 sums[W];
+  static_assert(W * SCORES_MOST <= JOIN_ROOM && SCORES_MOST * L::VEC <= JOIN_ROOM, "room for the waves' lists, and for their groups' logits");
   if (__syncthreads_or(stopped(a.status))) return;
   const uint32_t lane = lane_id(), wave = uniform(threadIdx.x / WAVE), r = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
   const Row<L> row(a, r);
-  const Given<L> given(a, row, r);
   ScoresLds* lds = &lists[wave];
   Seen<L> seen(a.n_top);
-  auto edge = [&](uint32_t group, uint32_t first, uint32_t count) {        // less than a group, a logit to a lane
-    const float x[1] = {lane < count ? L::value(row.x[first + lane]) : -INFINITY};
-    seen.add(x, x[0], x[0], a.c);
-    const float most = value_of_key(max_over_wave(key_of(x[0])));
-    seen.template offer<false>(lane == 0 ? most : -INFINITY, group, lds);
-  };
+  Given given{a.tokens ? a.tokens[r] : -1, 0.f};
   const uint32_t begin = part * a.per_part, end = row.whole - begin < a.per_part ? row.whole : begin + a.per_part;       // (parts begin within the row)
   const u32x4* groups = reinterpret_cast<const u32x4*>(row.x + row.head);
-  for (uint64_t at = begin + wave * SCORES_BATCH * WAVE; at < end; at += W * SCORES_BATCH * WAVE) {
+#pragma unroll 1
+  for (uint64_t from = begin + wave * SCORES_BATCH * WAVE; from < end; from += W * SCORES_BATCH * WAVE) {
     u32x4 w[SCORES_BATCH];
-    const uint32_t mine = static_cast<uint32_t>(at) + lane;
+    const uint32_t mine = static_cast<uint32_t>(from) + lane;
 #pragma unroll
     for (int i = 0; i < SCORES_BATCH; ++i) {
       w[i] = u32x4{L::NOTHING, L::NOTHING, L::NOTHING, L::NOTHING};
@@ -432,13 +428,31 @@ __global__ __launch_bounds__(W * WAVE) void k_scores(ScoresArgs a) {
     }
     seen.add(x, all, least, a.c);
     if (seen.border == -INFINITY) seen.begin(all);
-    if (ballot(all > seen.border))
+    if (!ballot(all > seen.border)) continue;
+#pragma unroll 1
+    for (uint32_t i = 0; i < SCORES_BATCH; ++i) {
+      float of = most[0];
 #pragma unroll
-      for (int i = 0; i < SCORES_BATCH; ++i) seen.template offer<true>(most[i], 1 + mine + i * WAVE, lds);
+      for (uint32_t j = 1; j < SCORES_BATCH; ++j) of = i == j ? most[j] : of;
+      seen.append(of > seen.border, of, 1 + mine + i * WAVE, lds);         // (a later group that is only as large as the k-th is none of the k)
+      if (seen.n > WAVE) seen.shorten(lds);
+    }
   }
-  if (part == 0 && wave == W - 1 && row.head > 0) edge(0, 0, row.head);
-  if (part == a.parts - 1 && wave == W - 2 && row.rest() > 0) edge(row.whole + 1, row.vocabulary - row.rest(), row.rest());
-  seen.shorten(lds);
+  if (wave == 0) given.x = given_logit(a, row, given.token);
+  if (wave == W - 1 && (part == 0 || part == a.parts - 1)) {
+    // what is less than a group, a logit to a lane: the head in the first eight lanes, the rest in the next
+    const uint32_t i = lane % 8;
+    const bool head = lane < 8 && part == 0 && i < row.head, rest = lane >= 8 && lane < 16 && part == a.parts - 1 && i < row.rest();
+    const float x[1] = {head || rest ? L::value(row.x[head ? i : row.vocabulary - row.rest() + i]) : -INFINITY};
+    seen.add(x, x[0], x[0], a.c);
+    uint32_t most = key_of(x[0]);
+    most = max_u32(most, dpp_move<0xB1>(most));
+    most = max_u32(most, dpp_move<0x4E>(most));
+    most = max_u32(most, dpp_move<0x141>(most));
+    const float of = value_of_key(most);
+    seen.append(i == 0 && of >= seen.border && of > -INFINITY, of, lane < 8 ? 0 : row.whole + 1, lds);
+  }
+  if (seen.n > a.n_top) seen.shorten(lds);
   seen.sum_over_lanes();
   if (lane == 0) sums[wave] = make_float4(seen.sums.r, seen.sums.s, seen.sums.t, seen.border);
   if (lane < a.n_top) firsts[wave * a.n_top + lane] = lane < seen.n ? make_float2(lds->most[lane], __uint_as_float(lds->group[lane])) : make_float2(-INFINITY, 0.f);
@@ -450,55 +464,51 @@ __global__ __launch_bounds__(W * WAVE) void k_scores(ScoresArgs a) {
   joined.sums = Sums{of_wave.x, of_wave.y, of_wave.z};
   joined.sum_over_lanes();
   joined.begin_at(of_wave.w);
-  for (uint32_t at = 0; at < W * a.n_top; at += WAVE) {
-    const float2 of = at + lane < W * a.n_top ? firsts[at + lane] : make_float2(-INFINITY, 0.f);
-    joined.template offer<false>(of.x, __float_as_uint(of.y), lds);
-  }
-  joined.shorten(lds);
-  if (a.parts == 1) {
-    finish_row<L>(a, row, r, given, joined, lds);
-    return;
-  }
-  if (lane == 0) a.sums[blockIdx.x] = make_float4(joined.sums.r, joined.sums.s, joined.sums.t, joined.border);
-  if (lane < a.n_top)
-    a.lists[static_cast<uint64_t>(blockIdx.x) * a.n_top + lane] =
-        lane < joined.n ? make_float2(lds->most[lane], __uint_as_float(lds->group[lane])) : make_float2(-INFINITY, 0.f);
+  if (a.parts > 1 && lane == 0) a.sums[blockIdx.x] = make_float4(joined.sums.r, joined.sums.s, joined.sums.t, joined.border);
+  finish_row<L>(a, row, r, given, joined, firsts, W * a.n_top, a.parts == 1, lds);
 }
 
 // Joins a row's parts: a wave each.
 template <typename L>
 __global__ __launch_bounds__(JOIN_WAVES * WAVE) void k_scores_join(ScoresArgs a) {
   __shared__ ScoresLds lists[JOIN_WAVES];
-  if (stopped(a.status)) return;
+  __shared__ float2 firsts[JOIN_WAVES][JOIN_ROOM];
   const uint32_t lane = lane_id(), wave = uniform(threadIdx.x / WAVE), r = blockIdx.x * JOIN_WAVES + wave;
   if (r >= a.rows) return;
-  const Row<L> row(a, r);
-  const Given<L> given(a, row, r);
-  ScoresLds* lds = &lists[wave];
-  Seen<L> seen(a.n_top);
+  const bool stop = stopped(a.status);
   const uint64_t first = static_cast<uint64_t>(r) * a.parts;
   const uint32_t n = a.parts * a.n_top;
   const float2* entries = a.lists + first * a.n_top;
-  constexpr int AHEAD = 4;                     // loads that wait for nothing
+  constexpr uint32_t AHEAD = 4;                // loads that wait for nothing
   float2 of[AHEAD];
 #pragma unroll
-  for (int i = 0; i < AHEAD; ++i) of[i] = i * WAVE + lane < n ? entries[i * WAVE + lane] : make_float2(-INFINITY, 0.f);
+  for (uint32_t i = 0; i < AHEAD; ++i) of[i] = i * WAVE + lane < n ? entries[i * WAVE + lane] : make_float2(-INFINITY, 0.f);
+  Given given{a.tokens ? a.tokens[r] : -1, 0.f};
+  Seen<L> seen(a.n_top);
   float border = -INFINITY;
   for (uint32_t p = lane; p < a.parts; p += WAVE) {
     const float4 theirs = a.sums[first + p];
     seen.sums.add(Sums{theirs.x, theirs.y, theirs.z});
     border = fmaxf(border, theirs.w);
   }
+  if (stop) return;
+  const Row<L> row(a, r);
+  given.x = given_logit(a, row, given.token);
   seen.sum_over_lanes();
   seen.begin_at(border);
+  ScoresLds* lds = &lists[wave];
 #pragma unroll
-  for (int i = 0; i < AHEAD; ++i) seen.template offer<false>(of[i].x, __float_as_uint(of[i].y), lds);
-  for (uint32_t at = AHEAD * WAVE; at < n; at += WAVE) {
-    const float2 one = at + lane < n ? entries[at + lane] : make_float2(-INFINITY, 0.f);
-    seen.template offer<false>(one.x, __float_as_uint(one.y), lds);
+  for (uint32_t i = 0; i < AHEAD; ++i) firsts[wave][i * WAVE + lane] = of[i];
+  uint32_t at = 0, count = min_u32(n, AHEAD * WAVE);
+  lds_in_order();
+  while (at + count < n) {                     // (more lists than there is room for: those so far become one)
+    seen.take(firsts[wave], count, lds);
+    at += count;
+    count = min_u32(n - at, JOIN_ROOM);
+    for (uint32_t e = lane; e < count; e += WAVE) firsts[wave][e] = entries[at + e];
+    lds_in_order();
   }
-  seen.shorten(lds);
-  finish_row<L>(a, row, r, given, seen, lds);
+  finish_row<L>(a, row, r, given, seen, firsts[wave], count, true, lds);
 }
 
 }  // namespace fikit
