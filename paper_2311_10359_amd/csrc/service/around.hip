@@ -147,6 +147,13 @@ struct ScoresCall {
 
 bool logits_ok(int32_t value_type) { return type_ok(value_type) || value_type == FIKIT_F32; }
 
+// Workgroups of the kernels that do all in one launch, or 0 for sizes that they do not take.
+uint32_t one_launch(uint32_t n_requests, uint32_t n_children, uint32_t rows, uint32_t table_width, uint32_t n_blocks) {
+  if (n_requests > ONE_REQUESTS || n_children > ONE_REQUESTS || n_blocks > ONE_BLOCKS || static_cast<uint64_t>(n_requests) * table_width > ONE_CELLS) return 0;
+  const uint32_t groups = (rows + BLOCKS_THREADS / WAVE - 1) / (BLOCKS_THREADS / WAVE);
+  return groups < 1 ? 1 : groups < ONE_MOST_GROUPS ? groups : ONE_MOST_GROUPS;
+}
+
 constexpr uint32_t CLEAR_GROUPS = 8;
 constexpr uint32_t COPY_GROUPS = 4096;
 
@@ -190,6 +197,8 @@ int fikit_cache_fork(const int32_t* d_block_table, uint32_t table_width, const i
   a.wants = part(parts.wants);
   a.n_children = n_children;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (const uint32_t groups = one_launch(n_requests, n_children, n_children, table_width, n_blocks))
+    return enqueue(k_fork_one, dim3(groups), dim3(BLOCKS_THREADS), st, a);
   if (int rc = enqueue(k_fork_begin, dim3(1 + CLEAR_GROUPS), dim3(BLOCKS_THREADS), st, a)) return rc;
   if (const uint32_t rows = n_requests + n_children)
     if (int rc = enqueue(k_fork_rows, dim3((rows + ROW_WAVES - 1) / ROW_WAVES), dim3(ROW_WAVES * WAVE), st, a)) return rc;
@@ -228,6 +237,8 @@ int fikit_cache_compact(const int32_t* d_block_table, uint32_t table_width, cons
   a.before = part(parts.before);
   a.room = room;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (const uint32_t groups = one_launch(n_requests, 0, n_requests, table_width, n_blocks))
+    return enqueue(k_compact_one, dim3(groups), dim3(BLOCKS_THREADS), st, a);
   const dim3 rows(ROW_WAVES * WAVE);
   const uint32_t waves = n_requests + (n_free + WAVE - 1) / WAVE;
   if (int rc = enqueue(k_compact_begin, dim3(CLEAR_GROUPS), dim3(BLOCKS_THREADS), st, a)) return rc;

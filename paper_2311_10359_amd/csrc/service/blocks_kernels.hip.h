@@ -54,6 +54,21 @@ __device__ __forceinline__ void clear_marks(const BlocksArgs& a, uint32_t from, 
   for (uint32_t i = from; i < a.words; i += stride) a.marks[i] = a.marks_too[i] = 0;
 }
 
+// f(page, entry) for the first `pages` entries of a row, by a wave, several loads on their way.
+template <typename F>
+__device__ __forceinline__ void each_page(const int32_t* entries, uint32_t pages, F f) {
+  constexpr int AHEAD = 4;
+  for (uint32_t from = lane_id(); from < pages; from += AHEAD * WAVE) {
+    int32_t held[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (from + i * WAVE < pages) held[i] = entries[from + i * WAVE];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (from + i * WAVE < pages) f(from + i * WAVE, held[i]);
+  }
+}
+
 // ---- fork -------------------------------------------------------------------------------------------------------
 //
 // Child i continues request parents[i].  The first child keeps the parent's last block if that is not full, each later one needs a block:
@@ -111,11 +126,11 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_fork_rows(BlocksArgs a) {
     const uint32_t pages = pages_of(a, static_cast<uint32_t>(a.lengths[row]));
     uint32_t* marks = a.first[row] == NO_CHILD ? a.marks : a.marks_too;
     const int32_t* entries = a.table + static_cast<uint64_t>(row) * a.width;
-    for (uint32_t page = lane; page < pages; page += WAVE) {
-      const uint32_t block = static_cast<uint32_t>(entries[page]);
+    each_page(entries, pages, [&](uint32_t, int32_t entry) {
+      const uint32_t block = static_cast<uint32_t>(entry);
       if (block < a.n_blocks) mark(marks, block);
       else *a.status = FIKIT_INVALID_ARG;
-    }
+    });
     return;
   }
   const uint32_t c = row - a.n_requests;
@@ -124,8 +139,7 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_fork_rows(BlocksArgs a) {
   const uint32_t pages = p >= 0 ? pages_of(a, static_cast<uint32_t>(a.lengths[p])) : 0;
   const int32_t* entries = a.table + static_cast<uint64_t>(p >= 0 ? p : 0) * a.width;
   int32_t* out = a.new_table + static_cast<uint64_t>(c) * a.width;
-  for (uint32_t page = lane; page < a.width; page += WAVE) {
-    int32_t block = page < pages ? entries[page] : -1;
+  each_page(entries, pages, [&](uint32_t page, int32_t block) {
     if (page + 1 == pages && rank >= 0) {
       a.copies[rank].x = block;
       if (static_cast<uint32_t>(rank) < a.n_free) {
@@ -135,7 +149,8 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_fork_rows(BlocksArgs a) {
       }                                          // (else what is given back says which: k_fork_end)
     }
     out[page] = block;
-  }
+  });
+  for (uint32_t page = pages + lane; page < a.width; page += WAVE) out[page] = -1;
 }
 
 // The sums of N counts over the words of the bitmaps, in every workgroup: those of the words before each word of the workgroup's slice, in LDS,
@@ -205,6 +220,129 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_end(BlocksArgs a) {
   }
 }
 
+// ---- one launch -------------------------------------------------------------------------------------------------
+//
+// Up to ONE_REQUESTS requests and children, ONE_BLOCKS blocks and ONE_CELLS entries of the table, with bitmaps in LDS: every workgroup marks all blocks for
+// itself and writes its share of the outputs, so that none waits for another.
+
+constexpr uint32_t ONE_REQUESTS = BLOCKS_THREADS, ONE_BLOCKS = 32 * BLOCKS_THREADS, ONE_CELLS = 65536, ONE_MOST_GROUPS = 64;
+
+struct OneLds {
+  uint32_t marks[BLOCKS_THREADS], marks_too[BLOCKS_THREADS], pages[ONE_REQUESTS], scan[BLOCKS_THREADS / WAVE];
+};
+
+// f(row, entry) for the entries of all requests, by a workgroup, several loads on their way.
+template <typename F>
+__device__ __forceinline__ void each_entry(const BlocksArgs& a, const uint32_t* pages, F f) {
+  constexpr int AHEAD = 8;
+  const uint32_t rows = BLOCKS_THREADS / a.width, rest = BLOCKS_THREADS % a.width;
+  uint32_t row = threadIdx.x / a.width, page = threadIdx.x % a.width;
+  while (row < a.n_requests) {
+    int32_t held[AHEAD];
+    uint32_t of[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const bool there = row < a.n_requests && page < pages[row < a.n_requests ? row : 0];
+      of[i] = there ? row : ~0u;
+      if (there) held[i] = a.table[row * a.width + page];
+      row += rows;
+      page += rest;
+      if (page >= a.width) { page -= a.width; ++row; }
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (of[i] != ~0u) f(of[i], static_cast<uint32_t>(held[i]));
+  }
+}
+
+// The k-th marked block: word(w) are the marks, before[w] those before them, ascending.
+template <typename F>
+__device__ __forceinline__ uint32_t marked_block(const uint32_t* before, uint32_t k, F word) {
+  uint32_t lo = 0, hi = BLOCKS_THREADS;
+  while (hi - lo > 1) {
+    const uint32_t mid = lo + (hi - lo) / 2;
+    if (before[mid] <= k) lo = mid; else hi = mid;
+  }
+  uint32_t left = word(lo);
+  for (uint32_t skip = k - before[lo]; skip > 0; --skip) left &= left - 1;
+  return lo * 32 + __ffs(static_cast<int>(left)) - 1;
+}
+
+__global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_one(BlocksArgs a) {
+  __shared__ OneLds lds;
+  __shared__ uint32_t before[BLOCKS_THREADS], first[ONE_REQUESTS], ranks[ONE_REQUESTS];
+  const uint32_t t = threadIdx.x, within = (1u << a.shift) - 1;
+  const bool stop = stopped(a.status);
+  const int32_t length = t < a.n_requests ? a.lengths[t] : 0, parent = t < a.n_children ? a.parents[t] : -1;
+  lds.marks[t] = lds.marks_too[t] = 0;
+  first[t] = NO_CHILD;
+  const bool whole = length_ok(a, length) && parent >= -1 && (parent < 0 || static_cast<uint32_t>(parent) < a.n_requests);
+  lds.pages[t] = whole ? pages_of(a, static_cast<uint32_t>(length)) : 0;
+  if (__syncthreads_or(stop)) return;
+  if (parent >= 0 && whole) atomicMin(&first[parent], t);
+  if (__syncthreads_or(!whole)) {
+    if (blockIdx.x == 0 && t == 0) *a.status = FIKIT_INVALID_ARG;
+    return;
+  }
+  const int32_t child_length = parent >= 0 ? a.lengths[parent] : 0;
+  bool bad = false;
+  if (a.width > 0)
+    each_entry(a, lds.pages, [&](uint32_t row, uint32_t block) {
+      if (block < a.n_blocks) atomicOr(&(first[row] == NO_CHILD ? lds.marks : lds.marks_too)[block / 32], 1u << block % 32);
+      else bad = true;
+    });
+  const bool need = parent >= 0 && (static_cast<uint32_t>(child_length) & within) && first[parent] != t;
+  uint32_t taken, given;
+  const uint32_t rank = block_excl_scan_1024(need, lds.scan, taken);
+  ranks[t] = need ? rank : ~0u;
+  if (__syncthreads_or(bad)) {
+    if (blockIdx.x == 0 && t == 0) *a.status = FIKIT_INVALID_ARG;
+    return;
+  }
+  const uint32_t word = lds.marks[t] & ~lds.marks_too[t];
+  before[t] = block_excl_scan_1024(__popc(word), lds.scan, given);
+  const uint32_t total = a.n_free + given;
+  if (taken > total || total - taken > a.n_blocks) {
+    if (blockIdx.x == 0 && t == 0) *a.status = taken > total ? FIKIT_CACHE_FULL : FIKIT_INVALID_ARG;
+    return;
+  }
+  __syncthreads();
+  const auto given_word = [&](uint32_t w) { return lds.marks[w] & ~lds.marks_too[w]; };
+  // rows, a wave each
+  const uint32_t lane = lane_id(), waves = BLOCKS_THREADS / WAVE;
+  for (uint32_t c = blockIdx.x * waves + uniform(t / WAVE); c < a.n_children; c += gridDim.x * waves) {
+    const int32_t p = a.parents[c];
+    const uint32_t pages = p >= 0 ? lds.pages[p] : 0, mine = ranks[c];
+    const int32_t* entries = a.table + static_cast<uint64_t>(p >= 0 ? p : 0) * a.width;
+    int32_t* out = a.new_table + static_cast<uint64_t>(c) * a.width;
+    each_page(entries, pages, [&](uint32_t page, int32_t block) {
+      if (page + 1 == pages && mine != ~0u) {
+        const uint32_t fresh = mine < a.n_free ? static_cast<uint32_t>(a.free_blocks[mine]) : marked_block(before, mine - a.n_free, given_word);
+        if (fresh >= a.n_blocks) *a.status = FIKIT_INVALID_ARG;
+        a.copies[mine] = make_int2(block, static_cast<int32_t>(fresh));
+        block = static_cast<int32_t>(fresh);
+      }
+      out[page] = block;
+    });
+    for (uint32_t page = pages + lane; page < a.width; page += WAVE) out[page] = -1;
+  }
+  const uint32_t from = blockIdx.x * BLOCKS_THREADS + t, stride = gridDim.x * BLOCKS_THREADS;
+  for (uint32_t block = from; block < a.n_blocks; block += stride) {
+    const uint32_t marks = given_word(block / 32), bit = 1u << block % 32, place = a.n_free + before[block / 32] + __popc(marks & (bit - 1));
+    if ((marks & bit) && place >= taken) a.new_free[place - taken] = static_cast<int32_t>(block);
+  }
+  for (uint32_t i = taken + from; i < a.n_free; i += stride) a.new_free[i - taken] = a.free_blocks[i];
+  for (uint32_t i = total - taken + from; i < a.n_blocks; i += stride) a.new_free[i] = -1;
+  for (uint32_t i = taken + from; i < a.n_children; i += stride) a.copies[i] = make_int2(-1, -1);
+  if (blockIdx.x > 0) return;
+  if (t < a.n_children) a.new_lengths[t] = child_length;
+  if (t == 0) {
+    a.counts[0] = static_cast<int32_t>(taken);
+    a.counts[1] = static_cast<int32_t>(given);
+    a.counts[2] = static_cast<int32_t>(total - taken);
+  }
+}
+
 // ---- compaction -------------------------------------------------------------------------------------------------
 //
 // Used and free blocks together, ascending: behind the first n_used of them lies the border.  The k-th used block behind the border goes
@@ -226,11 +364,11 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_compact_mark(BlocksArgs a)
     }
     const uint32_t pages = pages_of(a, static_cast<uint32_t>(length));
     const int32_t* entries = a.table + static_cast<uint64_t>(row) * a.width;
-    for (uint32_t page = lane; page < pages; page += WAVE) {
-      const uint32_t block = static_cast<uint32_t>(entries[page]);
+    each_page(entries, pages, [&](uint32_t, int32_t entry) {
+      const uint32_t block = static_cast<uint32_t>(entry);
       if (block < a.n_blocks) mark(a.marks, block);
       else *a.status = FIKIT_INVALID_ARG;
-    }
+    });
     return;
   }
   const uint32_t i = (row - a.n_requests) * WAVE + lane;
@@ -242,7 +380,6 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_compact_mark(BlocksArgs a)
 
 struct Border {
   uint32_t block, used;          // the border, and the used blocks before it
-  uint32_t bad;                  // a block is used and free
 };
 
 // Where the border lies, in every workgroup: the thread whose words hold the last of the first n_used blocks finds it.
@@ -311,13 +448,80 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_compact_rows(BlocksArgs a)
   const uint32_t border = a.words_of_call[0], used = a.words_of_call[1], pages = pages_of(a, static_cast<uint32_t>(a.lengths[row]));
   const int32_t* entries = a.table + static_cast<uint64_t>(row) * a.width;
   int32_t* out = a.new_table + static_cast<uint64_t>(row) * a.width;
-  for (uint32_t page = lane; page < a.width; page += WAVE) {
-    int32_t block = page < pages ? entries[page] : -1;
-    if (block >= 0 && static_cast<uint32_t>(block) >= border) {
-      const uint32_t w = static_cast<uint32_t>(block) / 32, bit = 1u << block % 32;
-      block = a.copies[a.before[w] + __popc(a.marks[w] & (bit - 1)) - used].y;
-    }
-    out[page] = block;
+  each_page(entries, pages, [&](uint32_t page, int32_t entry) {
+    const uint32_t block = static_cast<uint32_t>(entry), w = block / 32, bit = 1u << block % 32;
+    out[page] = block >= border ? a.copies[a.before[w] + __popc(a.marks[w] & (bit - 1)) - used].y : entry;
+  });
+  for (uint32_t page = pages + lane; page < a.width; page += WAVE) out[page] = -1;
+}
+
+// In one launch, as a fork.
+__global__ __launch_bounds__(BLOCKS_THREADS) void k_compact_one(BlocksArgs a) {
+  __shared__ OneLds lds;
+  __shared__ uint32_t used_before[BLOCKS_THREADS], spare_before[BLOCKS_THREADS];
+  __shared__ Border border;
+  const uint32_t t = threadIdx.x;
+  const bool stop = stopped(a.status);
+  const int32_t length = t < a.n_requests ? a.lengths[t] : 0;
+  lds.marks[t] = lds.marks_too[t] = 0;
+  bool bad = !length_ok(a, length);
+  lds.pages[t] = bad ? 0 : pages_of(a, static_cast<uint32_t>(length));
+  if (__syncthreads_or(stop)) return;
+  const auto put = [&](uint32_t* marks, uint32_t block) {
+    if (block < a.n_blocks) atomicOr(&marks[block / 32], 1u << block % 32);
+    else bad = true;
+  };
+  if (a.width > 0) each_entry(a, lds.pages, [&](uint32_t, uint32_t block) { put(lds.marks, block); });
+  constexpr int AHEAD = 4;
+  for (uint32_t i = t; i < a.n_free; i += AHEAD * BLOCKS_THREADS) {
+    int32_t held[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j)
+      if (i + j * BLOCKS_THREADS < a.n_free) held[j] = a.free_blocks[i + j * BLOCKS_THREADS];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j)
+      if (i + j * BLOCKS_THREADS < a.n_free) put(lds.marks_too, static_cast<uint32_t>(held[j]));
+  }
+  __syncthreads();
+  const uint32_t used = lds.marks[t], spare = lds.marks_too[t];
+  bad |= (used & spare) != 0;
+  uint32_t mine[2], total[2];
+  mine[0] = used_before[t] = block_excl_scan_1024(__popc(used), lds.scan, total[0]);
+  mine[1] = spare_before[t] = block_excl_scan_1024(__popc(spare), lds.scan, total[1]);
+  if (__syncthreads_or(bad) || total[1] != a.n_free) {             // also: a block that is used and free, or free twice
+    if (blockIdx.x == 0 && t == 0) *a.status = FIKIT_INVALID_ARG;
+    return;
+  }
+  a.marks = lds.marks;
+  a.marks_too = lds.marks_too;
+  a.words = BLOCKS_THREADS;
+  find_border(a, mine, total, &border);
+  __syncthreads();
+  const auto spare_word = [&](uint32_t w) { return lds.marks_too[w]; };
+  // where a used block behind the border goes
+  const auto goes = [&](uint32_t block) {
+    const uint32_t w = block / 32, k = used_before[w] + __popc(lds.marks[w] & ((1u << block % 32) - 1)) - border.used;
+    return static_cast<int32_t>(marked_block(spare_before, k, spare_word));
+  };
+  const uint32_t lane = lane_id(), waves = BLOCKS_THREADS / WAVE;
+  for (uint32_t r = blockIdx.x * waves + uniform(t / WAVE); r < a.n_requests; r += gridDim.x * waves) {
+    const uint32_t pages = lds.pages[r];
+    int32_t* out = a.new_table + static_cast<uint64_t>(r) * a.width;
+    each_page(a.table + static_cast<uint64_t>(r) * a.width, pages, [&](uint32_t page, int32_t entry) {
+      out[page] = static_cast<uint32_t>(entry) >= border.block ? goes(static_cast<uint32_t>(entry)) : entry;
+    });
+    for (uint32_t page = pages + lane; page < a.width; page += WAVE) out[page] = -1;
+  }
+  const uint32_t moved = total[0] - border.used, from = blockIdx.x * BLOCKS_THREADS + t, stride = gridDim.x * BLOCKS_THREADS;
+  for (uint32_t block = border.block + from; block < a.n_blocks; block += stride) {
+    const uint32_t w = block / 32, bit = 1u << block % 32, in_use = lds.marks[w], both = in_use | lds.marks_too[w];
+    if (in_use & bit) a.copies[used_before[w] + __popc(in_use & (bit - 1)) - border.used] = make_int2(static_cast<int32_t>(block), goes(block));
+    if (both & bit) a.new_free[used_before[w] + spare_before[w] + __popc(both & (bit - 1)) - total[0]] = static_cast<int32_t>(block);
+  }
+  for (uint32_t i = moved + from; i < a.room; i += stride) a.copies[i] = make_int2(-1, -1);
+  if (from == 0) {
+    a.counts[0] = static_cast<int32_t>(moved);
+    a.counts[1] = static_cast<int32_t>(total[0]);
   }
 }
 

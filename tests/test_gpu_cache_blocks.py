@@ -61,7 +61,7 @@ def check_compact(table, lengths, block, n_blocks, free, width):
 
 
 SIZES = [(1, 1, 16, 1), (1, 40, 16, 1), (3, 100, 32, 1), (8, 500, 16, 4), (65, 300, 64, 1), (100, 2000, 256, 5), (1025, 90, 16, 2), (40, 9000, 16, 8),
-         (3000, 200, 32, 3)]
+         (3000, 200, 32, 3), (1024, 60, 16, 4), (200, 9000, 16, 8)]
 
 
 @pytest.mark.parametrize("requests, longest, block, groups", SIZES)
