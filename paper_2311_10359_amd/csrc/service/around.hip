@@ -38,7 +38,7 @@ bool rotates_in_place_or_elsewhere(const fikit_vectors* in, const fikit_vectors*
   return in->d_data != out->d_data || ((heads <= 1 || in->head_stride == out->head_stride) && (n_tokens <= 1 || in->token_stride == out->token_stride));
 }
 
-// Parts of the workspace of a fork or a compaction, one behind the other.
+// Parts of the workspace of a fork or a compaction, one behind the other, in words.
 struct Parts {
   uint64_t bytes = 0;
   uint64_t take(uint64_t count) {
@@ -48,9 +48,11 @@ struct Parts {
   }
 };
 struct ForkParts : Parts {
-  uint64_t words, marks, marks_too, first, rank, wants;
+  uint64_t words, flags, flags_too, marks, marks_too, first, rank, wants;
   ForkParts(uint32_t n_requests, uint32_t n_children, uint32_t n_blocks) : words((n_blocks + 31) / 32) {
     take(1);
+    flags = take(8 * words);
+    flags_too = take(8 * words);
     marks = take(words);
     marks_too = take(words);
     first = take(n_requests);
@@ -59,9 +61,11 @@ struct ForkParts : Parts {
   }
 };
 struct CompactParts : Parts {
-  uint64_t words, marks, marks_too, before;
+  uint64_t words, flags, flags_too, marks, marks_too, before;
   explicit CompactParts(uint32_t n_blocks) : words((n_blocks + 31) / 32) {
     take(2);
+    flags = take(8 * words);
+    flags_too = take(8 * words);
     marks = take(words);
     marks_too = take(words);
     before = take(words);
@@ -154,7 +158,8 @@ uint32_t one_launch(uint32_t n_requests, uint32_t n_children, uint32_t rows, uin
   return groups < 1 ? 1 : groups < ONE_MOST_GROUPS ? groups : ONE_MOST_GROUPS;
 }
 
-constexpr uint32_t CLEAR_GROUPS = 8;
+dim3 clear_groups(uint32_t words) { return dim3((2 * words + BLOCKS_THREADS - 1) / BLOCKS_THREADS); }        // 16 flags of both kinds to a thread
+int pack(const BlocksArgs& a, hipStream_t st) { return enqueue(k_blocks_pack, clear_groups(a.words), dim3(BLOCKS_THREADS), st, a); }
 constexpr uint32_t COPY_GROUPS = 4096;
 
 }  // namespace
@@ -190,6 +195,8 @@ int fikit_cache_fork(const int32_t* d_block_table, uint32_t table_width, const i
   a.new_free = d_new_free;
   a.counts = d_counts;
   a.words_of_call = part(0);
+  a.flags = reinterpret_cast<uint8_t*>(part(parts.flags));
+  a.flags_too = reinterpret_cast<uint8_t*>(part(parts.flags_too));
   a.marks = part(parts.marks);
   a.marks_too = part(parts.marks_too);
   a.first = part(parts.first);
@@ -199,9 +206,10 @@ int fikit_cache_fork(const int32_t* d_block_table, uint32_t table_width, const i
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (const uint32_t groups = one_launch(n_requests, n_children, n_children, table_width, n_blocks))
     return enqueue(k_fork_one, dim3(groups), dim3(BLOCKS_THREADS), st, a);
-  if (int rc = enqueue(k_fork_begin, dim3(1 + CLEAR_GROUPS), dim3(BLOCKS_THREADS), st, a)) return rc;
+  if (int rc = enqueue(k_fork_begin, dim3(1 + clear_groups(a.words).x), dim3(BLOCKS_THREADS), st, a)) return rc;
   if (const uint32_t rows = n_requests + n_children)
     if (int rc = enqueue(k_fork_rows, dim3((rows + ROW_WAVES - 1) / ROW_WAVES), dim3(ROW_WAVES * WAVE), st, a)) return rc;
+  if (int rc = pack(a, st)) return rc;
   return enqueue(k_fork_end, dim3((a.words + SLICE - 1) / SLICE), dim3(BLOCKS_THREADS), st, a);
 }
 
@@ -232,6 +240,8 @@ int fikit_cache_compact(const int32_t* d_block_table, uint32_t table_width, cons
   a.new_free = d_new_free;
   a.counts = d_counts;
   a.words_of_call = part(0);
+  a.flags = reinterpret_cast<uint8_t*>(part(parts.flags));
+  a.flags_too = reinterpret_cast<uint8_t*>(part(parts.flags_too));
   a.marks = part(parts.marks);
   a.marks_too = part(parts.marks_too);
   a.before = part(parts.before);
@@ -241,9 +251,10 @@ int fikit_cache_compact(const int32_t* d_block_table, uint32_t table_width, cons
     return enqueue(k_compact_one, dim3(groups), dim3(BLOCKS_THREADS), st, a);
   const dim3 rows(ROW_WAVES * WAVE);
   const uint32_t waves = n_requests + (n_free + WAVE - 1) / WAVE;
-  if (int rc = enqueue(k_compact_begin, dim3(CLEAR_GROUPS), dim3(BLOCKS_THREADS), st, a)) return rc;
+  if (int rc = enqueue(k_compact_begin, clear_groups(a.words), dim3(BLOCKS_THREADS), st, a)) return rc;
   if (waves > 0)
     if (int rc = enqueue(k_compact_mark, dim3((waves + ROW_WAVES - 1) / ROW_WAVES), rows, st, a)) return rc;
+  if (int rc = pack(a, st)) return rc;
   if (int rc = enqueue(k_compact_lists, dim3((a.words + SLICE - 1) / SLICE), dim3(BLOCKS_THREADS), st, a)) return rc;
   return n_requests > 0 ? enqueue(k_compact_rows, dim3((n_requests + ROW_WAVES - 1) / ROW_WAVES), rows, st, a) : FIKIT_OK;
 }

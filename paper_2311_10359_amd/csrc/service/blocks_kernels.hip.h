@@ -23,8 +23,10 @@ struct BlocksArgs {
   int32_t* new_free;
   int32_t* counts;
   int32_t* status;
-  uint32_t* marks;          // fork: blocks of requests that nobody continues; compaction: used blocks
+  uint32_t* marks;          // bitmaps; fork: blocks of requests that nobody continues; compaction: used blocks
   uint32_t* marks_too;      // fork: blocks of the others; compaction: free ones
+  uint8_t* flags;           // the same with a byte for each block, in whole words of the bitmaps
+  uint8_t* flags_too;
   uint32_t* first;          // fork, [n_requests]: a request's first child, or NO_CHILD
   int32_t* rank;            // fork, [n_children]: a child's place among those that need a block for a copy, or -1
   uint32_t* wants;          // fork, [n_children]: the child of a place
@@ -46,13 +48,61 @@ __device__ __forceinline__ bool length_ok(const BlocksArgs& a, int32_t length) {
   return length >= 0 && (static_cast<uint64_t>(length) + (1u << a.shift) - 1) >> a.shift <= a.width;
 }
 
-__device__ __forceinline__ void mark(uint32_t* marks, uint32_t block) {
-  __hip_atomic_fetch_or(marks + block / 32, 1u << block % 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+// Whole sets of flags as words of 16 bytes.
+__device__ __forceinline__ void clear_flags(const BlocksArgs& a, uint32_t from, uint32_t stride) {
+  for (uint32_t i = from; i < 2 * a.words; i += stride)
+    reinterpret_cast<u32x4*>(a.flags)[i] = reinterpret_cast<u32x4*>(a.flags_too)[i] = u32x4{0, 0, 0, 0};
 }
 
-__device__ __forceinline__ void clear_marks(const BlocksArgs& a, uint32_t from, uint32_t stride) {
-  for (uint32_t i = from; i < a.words; i += stride) a.marks[i] = a.marks_too[i] = 0;
+// The bitmaps from the flags.  (Many workgroups mark at once.  Or-ing bits into words in memory took 10 us for 176,000 marks; stores of a byte, of which none
+// waits for another, and this take 3 and 2.)
+__device__ __forceinline__ uint32_t packed(const uint8_t* flags, uint32_t word) {
+  uint32_t bits = 0;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const u32x4 w = reinterpret_cast<const u32x4*>(flags)[2 * word + half];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)       // four bytes of 0 or 1
+      bits |= (w[i] * 0x01020408u >> 24 & 15u) << (16 * half + 4 * i);
+  }
+  return bits;
 }
+__global__ __launch_bounds__(BLOCKS_THREADS) void k_blocks_pack(BlocksArgs a) {
+  const uint32_t i = blockIdx.x * BLOCKS_THREADS + threadIdx.x;
+  if (i < a.words) a.marks[i] = packed(a.flags, i);
+  else if (i < 2 * a.words) a.marks_too[i - a.words] = packed(a.flags_too, i - a.words);
+}
+
+// The words of the bitmaps that a thread of a workgroup looks at, neighbours, in its registers.
+constexpr int WORDS_MOST = BLOCKS_MOST_BLOCKS / 32 / BLOCKS_THREADS;
+struct Words {
+  uint32_t from, count, marks[WORDS_MOST], marks_too[WORDS_MOST];
+
+  __device__ __forceinline__ explicit Words(const BlocksArgs& a) {
+    const uint32_t per = (a.words + BLOCKS_THREADS - 1) / BLOCKS_THREADS;
+    from = min_u32(threadIdx.x * per, a.words);
+    count = min_u32(per, a.words - from);
+#pragma unroll
+    for (uint32_t i = 0; i < WORDS_MOST; i += 8)
+      if (i < per)                         // (the same in the workgroup: eight loads of each on their way)
+#pragma unroll
+        for (uint32_t j = i; j < i + 8; ++j) {
+          marks[j] = j < count ? a.marks[from + j] : 0;
+          marks_too[j] = j < count ? a.marks_too[from + j] : 0;
+        }
+  }
+  // f(word, its marks, its other marks)
+  template <typename F>
+  __device__ __forceinline__ void each(const BlocksArgs& a, F f) const {
+    const uint32_t per = (a.words + BLOCKS_THREADS - 1) / BLOCKS_THREADS;
+#pragma unroll
+    for (uint32_t i = 0; i < WORDS_MOST; i += 8)
+      if (i < per)
+#pragma unroll
+        for (uint32_t j = i; j < i + 8; ++j)
+          if (j < count) f(from + j, marks[j], marks_too[j]);
+  }
+};
 
 // f(page, entry) for the first `pages` entries of a row, by a wave, several loads on their way.
 template <typename F>
@@ -77,43 +127,61 @@ __device__ __forceinline__ void each_page(const int32_t* entries, uint32_t pages
 
 // The children, in one workgroup; the others clear the bitmaps.
 __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_begin(BlocksArgs a) {
-  __shared__ uint32_t first[BLOCKS_MOST_REQUESTS];
-  __shared__ uint32_t scan[BLOCKS_THREADS / WAVE];
+  __shared__ uint32_t first[BLOCKS_MOST_REQUESTS], sums[BLOCKS_MOST_REQUESTS / WAVE], scan[BLOCKS_THREADS / WAVE];
   if (blockIdx.x > 0) {
-    clear_marks(a, (blockIdx.x - 1) * BLOCKS_THREADS + threadIdx.x, (gridDim.x - 1) * BLOCKS_THREADS);
+    clear_flags(a, (blockIdx.x - 1) * BLOCKS_THREADS + threadIdx.x, (gridDim.x - 1) * BLOCKS_THREADS);
     return;
   }
   if (stopped(a.status)) return;               // (nobody else writes it in this launch)
-  bool bad = false;
-  for (uint32_t r = threadIdx.x; r < a.n_requests; r += BLOCKS_THREADS) {
-    first[r] = NO_CHILD;
-    bad |= !length_ok(a, a.lengths[r]);
+  constexpr uint32_t PER = BLOCKS_MOST_REQUESTS / BLOCKS_THREADS, WAVES = BLOCKS_THREADS / WAVE;      // PER: requests and children of a thread, whose
+  bool bad = false;                                                                                  // loads are on their way at once
+  int32_t lengths[PER], parents[PER];
+#pragma unroll
+  for (uint32_t i = 0; i < PER; ++i) {
+    const uint32_t at = i * BLOCKS_THREADS + threadIdx.x;
+    lengths[i] = at < a.n_requests ? a.lengths[at] : 0;
+    parents[i] = at < a.n_children ? a.parents[at] : -1;
   }
-  __syncthreads();
-  for (uint32_t c = threadIdx.x; c < a.n_children; c += BLOCKS_THREADS) {
-    const int32_t p = a.parents[c];
-    if (p >= 0 && static_cast<uint32_t>(p) < a.n_requests) atomicMin(&first[p], c);
-    bad |= p < -1 || (p >= 0 && static_cast<uint32_t>(p) >= a.n_requests);
+#pragma unroll
+  for (uint32_t i = 0; i < PER; ++i) {
+    const uint32_t at = i * BLOCKS_THREADS + threadIdx.x;
+    if (at < a.n_requests) first[at] = NO_CHILD;
+    bad |= !length_ok(a, lengths[i]) || parents[i] < -1 || (parents[i] >= 0 && static_cast<uint32_t>(parents[i]) >= a.n_requests);
   }
   if (__syncthreads_or(bad)) {
     if (threadIdx.x == 0) *a.status = FIKIT_INVALID_ARG;
     return;
   }
+#pragma unroll
+  for (uint32_t i = 0; i < PER; ++i) {
+    if (parents[i] >= 0) atomicMin(&first[parents[i]], i * BLOCKS_THREADS + threadIdx.x);
+    lengths[i] = parents[i] >= 0 ? a.lengths[parents[i]] : 0;
+  }
+  __syncthreads();
   for (uint32_t r = threadIdx.x; r < a.n_requests; r += BLOCKS_THREADS) a.first[r] = first[r];
-  uint32_t taken = 0;
-  for (uint32_t base = 0; base < a.n_children; base += BLOCKS_THREADS) {
-    const uint32_t c = base + threadIdx.x;
-    const int32_t p = c < a.n_children ? a.parents[c] : -1;
-    const int32_t length = p >= 0 ? a.lengths[p] : 0;
-    const bool need = p >= 0 && (static_cast<uint32_t>(length) & ((1u << a.shift) - 1)) && first[p] != c;
-    uint32_t total;
-    const uint32_t place = taken + block_excl_scan_1024(need, scan, total);
+  // how many of each 64 children need a block, then the sums of the 64s before: a child's place
+  const uint32_t wave = uniform(threadIdx.x / WAVE);
+  uint64_t needs[PER];
+#pragma unroll
+  for (uint32_t i = 0; i < PER; ++i) {
+    const bool need = parents[i] >= 0 && (static_cast<uint32_t>(lengths[i]) & ((1u << a.shift) - 1)) && first[parents[i]] != i * BLOCKS_THREADS + threadIdx.x;
+    needs[i] = ballot(need);
+    if (lane_id() == 0) sums[i * WAVES + wave] = popc64(needs[i]);
+  }
+  __syncthreads();
+  uint32_t taken;
+  const uint32_t before = block_excl_scan_1024(threadIdx.x < PER * WAVES ? sums[threadIdx.x] : 0, scan, taken);
+  if (threadIdx.x < PER * WAVES) sums[threadIdx.x] = before;
+  __syncthreads();
+#pragma unroll
+  for (uint32_t i = 0; i < PER; ++i) {
+    const uint32_t c = i * BLOCKS_THREADS + threadIdx.x, place = sums[i * WAVES + wave] + popc_below(needs[i]);
     if (c < a.n_children) {
-      a.new_lengths[c] = length;
+      const bool need = needs[i] >> lane_id() & 1;
+      a.new_lengths[c] = lengths[i];
       a.rank[c] = need ? static_cast<int32_t>(place) : -1;
       if (need) a.wants[place] = c;
     }
-    taken += total;
   }
   if (threadIdx.x == 0) a.words_of_call[0] = taken;
 }
@@ -124,11 +192,11 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_fork_rows(BlocksArgs a) {
   const uint32_t lane = lane_id(), row = blockIdx.x * ROW_WAVES + uniform(threadIdx.x / WAVE);
   if (row < a.n_requests) {
     const uint32_t pages = pages_of(a, static_cast<uint32_t>(a.lengths[row]));
-    uint32_t* marks = a.first[row] == NO_CHILD ? a.marks : a.marks_too;
+    uint8_t* flags = a.first[row] == NO_CHILD ? a.flags : a.flags_too;
     const int32_t* entries = a.table + static_cast<uint64_t>(row) * a.width;
     each_page(entries, pages, [&](uint32_t, int32_t entry) {
       const uint32_t block = static_cast<uint32_t>(entry);
-      if (block < a.n_blocks) mark(marks, block);
+      if (block < a.n_blocks) flags[block] = 1;
       else *a.status = FIKIT_INVALID_ARG;
     });
     return;
@@ -153,33 +221,34 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_fork_rows(BlocksArgs a) {
   for (uint32_t page = pages + lane; page < a.width; page += WAVE) out[page] = -1;
 }
 
-// The sums of N counts over the words of the bitmaps, in every workgroup: those of the words before each word of the workgroup's slice, in LDS,
-// and of all words.  count(word, out) gives the counts of a word, of which there are up to 1024 to a thread.
+// The sums of N counts over the words of the bitmaps, in every workgroup: those of the words before a thread's and before each word of the workgroup's
+// slice, in LDS with the words themselves, and of all words.  count(marks, other marks, out) gives the counts of a word.
 template <int N>
 struct WordSums {
-  uint32_t before[SLICE][N];
+  uint32_t before[SLICE][N], marks[SLICE], marks_too[SLICE];
   uint32_t scan[BLOCKS_THREADS / WAVE];
 };
 template <int N, typename F>
-__device__ __forceinline__ void word_sums(uint32_t words, uint32_t slice, WordSums<N>* lds, uint32_t (&mine)[N], uint32_t (&total)[N], F count) {
-  const uint32_t per = (words + BLOCKS_THREADS - 1) / BLOCKS_THREADS, from = threadIdx.x * per, to = min_u32(from + per, words);
-  uint32_t sums[N] = {};
-  for (uint32_t w = from; w < to; ++w) {
+__device__ __forceinline__ void word_sums(const BlocksArgs& a, const Words& words, uint32_t slice, WordSums<N>* lds, uint32_t (&mine)[N], uint32_t (&total)[N],
+                                          F count) {
+  uint32_t sums[N] = {}, at[N];
+  words.each(a, [&](uint32_t, uint32_t m, uint32_t n) {
     uint32_t of[N];
-    count(w, of);
+    count(m, n, of);
     for (int i = 0; i < N; ++i) sums[i] += of[i];
-  }
-  for (int i = 0; i < N; ++i) mine[i] = block_excl_scan_1024(sums[i], lds->scan, total[i]);
-  uint32_t at[N];
-  for (int i = 0; i < N; ++i) at[i] = mine[i];
-  if (from < slice + SLICE && to > slice)
-    for (uint32_t w = from; w < to; ++w) {
-      if (w >= slice && w < slice + SLICE)
+  });
+  for (int i = 0; i < N; ++i) at[i] = mine[i] = block_excl_scan_1024(sums[i], lds->scan, total[i]);
+  if (words.from < slice + SLICE && words.from + words.count > slice)
+    words.each(a, [&](uint32_t w, uint32_t m, uint32_t n) {
+      if (w >= slice && w < slice + SLICE) {
         for (int i = 0; i < N; ++i) lds->before[w - slice][i] = at[i];
+        lds->marks[w - slice] = m;
+        lds->marks_too[w - slice] = n;
+      }
       uint32_t of[N];
-      count(w, of);
+      count(m, n, of);
       for (int i = 0; i < N; ++i) at[i] += of[i];
-    }
+    });
   __syncthreads();
 }
 
@@ -189,7 +258,8 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_end(BlocksArgs a) {
   if (__syncthreads_or(stopped(a.status))) return;
   const uint32_t slice = blockIdx.x * SLICE, taken = a.words_of_call[0];
   uint32_t mine[1], given[1];
-  word_sums<1>(a.words, slice, &sums, mine, given, [&](uint32_t w, uint32_t (&of)[1]) { of[0] = __popc(a.marks[w] & ~a.marks_too[w]); });
+  const Words words(a);
+  word_sums<1>(a, words, slice, &sums, mine, given, [](uint32_t m, uint32_t n, uint32_t (&of)[1]) { of[0] = __popc(m & ~n); });
   const uint32_t total = a.n_free + given[0];          // (below 2^32: n_free is at most n_blocks)
   if (taken > total || total - taken > a.n_blocks) {   // (too few; or a list that names blocks in use)
     if (threadIdx.x == 0) *a.status = taken > total ? FIKIT_CACHE_FULL : FIKIT_INVALID_ARG;
@@ -198,7 +268,7 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_end(BlocksArgs a) {
   for (uint32_t i = threadIdx.x; i < SLICE * 32; i += BLOCKS_THREADS) {
     const uint32_t w = slice + i / 32;
     if (w >= a.words) break;
-    const uint32_t marks = a.marks[w] & ~a.marks_too[w], bit = 1u << i % 32;
+    const uint32_t marks = sums.marks[i / 32] & ~sums.marks_too[i / 32], bit = 1u << i % 32;
     if (!(marks & bit)) continue;
     const uint32_t place = a.n_free + sums.before[i / 32][0] + __popc(marks & (bit - 1)), block = w * 32 + i % 32;
     if (place >= taken) {
@@ -349,7 +419,7 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_one(BlocksArgs a) {
 // to the k-th free one before it, and what lies behind it is the new free list.
 
 __global__ __launch_bounds__(BLOCKS_THREADS) void k_compact_begin(BlocksArgs a) {
-  clear_marks(a, blockIdx.x * BLOCKS_THREADS + threadIdx.x, gridDim.x * BLOCKS_THREADS);
+  clear_flags(a, blockIdx.x * BLOCKS_THREADS + threadIdx.x, gridDim.x * BLOCKS_THREADS);
 }
 
 // A wave for each request marks its blocks; the waves behind them the free ones, 64 each.
@@ -366,7 +436,7 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_compact_mark(BlocksArgs a)
     const int32_t* entries = a.table + static_cast<uint64_t>(row) * a.width;
     each_page(entries, pages, [&](uint32_t, int32_t entry) {
       const uint32_t block = static_cast<uint32_t>(entry);
-      if (block < a.n_blocks) mark(a.marks, block);
+      if (block < a.n_blocks) a.flags[block] = 1;
       else *a.status = FIKIT_INVALID_ARG;
     });
     return;
@@ -374,7 +444,7 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_compact_mark(BlocksArgs a)
   const uint32_t i = (row - a.n_requests) * WAVE + lane;
   if (i >= a.n_free) return;
   const uint32_t block = static_cast<uint32_t>(a.free_blocks[i]);
-  if (block < a.n_blocks) mark(a.marks_too, block);
+  if (block < a.n_blocks) a.flags_too[block] = 1;
   else *a.status = FIKIT_INVALID_ARG;
 }
 
@@ -382,23 +452,14 @@ struct Border {
   uint32_t block, used;          // the border, and the used blocks before it
 };
 
-// Where the border lies, in every workgroup: the thread whose words hold the last of the first n_used blocks finds it.
-__device__ __forceinline__ void find_border(const BlocksArgs& a, const uint32_t (&mine)[2], const uint32_t (&total)[2], Border* lds) {
-  const uint32_t per = (a.words + BLOCKS_THREADS - 1) / BLOCKS_THREADS, from = threadIdx.x * per, to = min_u32(from + per, a.words);
-  uint32_t used = mine[0], all = mine[0] + mine[1];
-  if (threadIdx.x == 0 && total[0] == 0) { lds->block = 0; lds->used = 0; }
-  for (uint32_t w = from; w < to && all < total[0]; ++w) {
-    uint32_t of = a.marks[w] | a.marks_too[w];
-    const uint32_t here = __popc(of);
-    if (all + here >= total[0]) {
-      for (uint32_t skip = total[0] - all - 1; skip > 0; --skip) of &= of - 1;
-      const uint32_t bit = __ffs(static_cast<int>(of)) - 1, below = bit == 31 ? ~0u : (2u << bit) - 1;
-      lds->block = w * 32 + bit + 1;
-      lds->used = used + __popc(a.marks[w] & below);
-    }
-    all += here;
-    used += __popc(a.marks[w]);
-  }
+// The border, if the last of the first `total` used and free blocks is one of a word's; used, all: those before the word.
+__device__ __forceinline__ void find_border(uint32_t w, uint32_t marks, uint32_t marks_too, uint32_t used, uint32_t all, uint32_t total, Border* lds) {
+  uint32_t of = marks | marks_too;
+  if (all >= total || all + __popc(of) < total) return;
+  for (uint32_t skip = total - all - 1; skip > 0; --skip) of &= of - 1;
+  const uint32_t bit = __ffs(static_cast<int>(of)) - 1, below = bit == 31 ? ~0u : (2u << bit) - 1;
+  lds->block = w * 32 + bit + 1;
+  lds->used = used + __popc(marks & below);
 }
 
 __global__ __launch_bounds__(BLOCKS_THREADS) void k_compact_lists(BlocksArgs a) {
@@ -407,12 +468,19 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_compact_lists(BlocksArgs a) 
   if (__syncthreads_or(stopped(a.status))) return;
   const uint32_t slice = blockIdx.x * SLICE;
   uint32_t mine[2], total[2], both = 0;
-  word_sums<2>(a.words, slice, &sums, mine, total, [&](uint32_t w, uint32_t (&of)[2]) {
-    of[0] = __popc(a.marks[w]);
-    of[1] = __popc(a.marks_too[w]);
-    both |= a.marks[w] & a.marks_too[w];
+  const Words words(a);
+  word_sums<2>(a, words, slice, &sums, mine, total, [&](uint32_t m, uint32_t n, uint32_t (&of)[2]) {
+    of[0] = __popc(m);
+    of[1] = __popc(n);
+    both |= m & n;
   });
-  find_border(a, mine, total, &border);
+  if (threadIdx.x == 0 && total[0] == 0) border = Border{0, 0};
+  if (mine[0] + mine[1] < total[0])
+    words.each(a, [&](uint32_t w, uint32_t m, uint32_t n) {
+      find_border(w, m, n, mine[0], mine[0] + mine[1], total[0], &border);
+      mine[0] += __popc(m);
+      mine[1] += __popc(n);
+    });
   if (__syncthreads_or(both != 0) || total[1] != a.n_free) {       // a block that is used and free, or free twice
     if (threadIdx.x == 0) *a.status = FIKIT_INVALID_ARG;
     return;
@@ -420,7 +488,7 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_compact_lists(BlocksArgs a) 
   for (uint32_t i = threadIdx.x; i < SLICE * 32; i += BLOCKS_THREADS) {
     const uint32_t w = slice + i / 32;
     if (w >= a.words) break;
-    const uint32_t used = a.marks[w], spare = a.marks_too[w], bit = 1u << i % 32, block = w * 32 + i % 32;
+    const uint32_t used = sums.marks[i / 32], spare = sums.marks_too[i / 32], bit = 1u << i % 32, block = w * 32 + i % 32;
     const uint32_t used_before = sums.before[i / 32][0] + __popc(used & (bit - 1)), spare_before = sums.before[i / 32][1] + __popc(spare & (bit - 1));
     if (i % 32 == 0) a.before[w] = used_before;
     if (block >= border.block) {
@@ -492,10 +560,8 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_compact_one(BlocksArgs a) {
     if (blockIdx.x == 0 && t == 0) *a.status = FIKIT_INVALID_ARG;
     return;
   }
-  a.marks = lds.marks;
-  a.marks_too = lds.marks_too;
-  a.words = BLOCKS_THREADS;
-  find_border(a, mine, total, &border);
+  if (t == 0 && total[0] == 0) border = Border{0, 0};
+  find_border(t, used, spare, mine[0], mine[0] + mine[1], total[0], &border);
   __syncthreads();
   const auto spare_word = [&](uint32_t w) { return lds.marks_too[w]; };
   // where a used block behind the border goes
