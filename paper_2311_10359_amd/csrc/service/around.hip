@@ -116,15 +116,18 @@ struct ScoresCut {
   uint32_t parts, per_part, waves;
   uint64_t sums_bytes, bytes;
 };
-constexpr uint32_t SCORES_FEW = 1024;             // rows below which 16 waves take a row, or a part of it; 4 beyond
-constexpr uint32_t SCORES_CHIP = 256;             // workgroups of 16 waves
+// A row is one workgroup's where that takes it in one turn, of 4 waves or of 16 (one row of 32,000 bfloat16 logits 9.3 us; 10.9 in parts that a second
+// launch joins), and from 128 rows on, of 16 waves up to 1023 rows (256 rows of 50,001 float32 16.0 us; 4 waves 21) and of 4 beyond (1100 rows of
+// 131,072 bfloat16 59.8; 16 waves 72.5).  Else rows are cut into parts of 4 waves, for two workgroups on a compute unit: one compute unit takes 2 us to read
+// what 16 waves want first (one row of 131,072 logits 15.9 us; in parts of 16 waves 17.1, 64 such rows 19.5 and 20.5).
+constexpr uint32_t SCORES_CHIP = 256, SCORES_MANY = 1024;
 
 ScoresCut scores_cut(uint32_t n_rows, uint32_t vocabulary, int32_t value_type, uint32_t n_top) {
   ScoresCut c{};
-  const uint32_t groups = vocabulary / (value_type == FIKIT_F32 ? LogitsF32::VEC : LogitsBf16::VEC);
-  c.waves = n_rows < SCORES_FEW ? 16 : 4;
-  const uint32_t turn = SCORES_BATCH * WAVE * c.waves, most = (groups + turn - 1) / turn;
-  const uint32_t want = n_rows == 0 || n_rows >= SCORES_CHIP ? 1 : SCORES_CHIP / n_rows;
+  const uint32_t groups = vocabulary / (value_type == FIKIT_F32 ? LogitsF32::VEC : LogitsBf16::VEC), turn = SCORES_BATCH * WAVE;
+  const bool few = n_rows < SCORES_CHIP / 2;
+  c.waves = groups <= 4 * turn || n_rows >= SCORES_MANY || (few && groups > 16 * turn) ? 4 : 16;
+  const uint32_t most = (groups + c.waves * turn - 1) / (c.waves * turn), want = n_rows > 0 && few && c.waves == 4 ? 2 * SCORES_CHIP / n_rows : 1;
   c.parts = want < most ? want : most;
   if (c.parts < 1) c.parts = 1;
   const uint32_t each = (groups + c.parts - 1) / c.parts;

@@ -83,24 +83,27 @@ constexpr uint32_t LOWEST_KEY = 0x00800000u;             // of the lowest finite
 __device__ __forceinline__ float value_of_key(uint32_t key) { return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key); }
 
 // A key that k of the wave's keys reach (N to a lane; 0: none) and no more, or the largest one that k or more reach, if some are equal.  More than k
-// keys are given, of which the upper BITS differ; the k-th largest is `least` or more.  (Bit by bit from the first one in which `least` and the
-// largest key differ.)
+// keys are given, of which the upper BITS differ; the k-th largest is `least` or more.  (Two bits at a time from the first one in which `least` and
+// the largest key differ: a step is one trip from the comparisons to the counts and back, however many comparisons it makes.)
 template <int BITS, int N>
 __device__ __forceinline__ uint32_t reached_by(const uint32_t (&keys)[N], uint32_t k, uint32_t least) {
   uint32_t most = keys[0];
 #pragma unroll
   for (int i = 1; i < N; ++i) most = max_u32(most, keys[i]);
   most = max_over_wave(most);
-  const int from = 31 - __builtin_clz((most ^ least) | 1);
+  const int from = (31 - __builtin_clz((most ^ least) | 1)) | 1;             // bits 2 i + 1 and 2 i
   uint32_t found = most >> from >> 1 << from << 1;
 #pragma unroll 1
-  for (int b = from; b >= 32 - BITS; --b) {
-    const uint32_t next = found | 1u << b;
-    uint32_t n = 0;
+  for (int b = from - 1; b >= (32 - BITS) / 2 * 2; b -= 2) {
+    uint32_t n[3] = {};
 #pragma unroll
-    for (int i = 0; i < N; ++i) n += popc64(ballot(keys[i] >= next));
-    if (n >= k) found = next;
-    if (n == k) break;
+    for (uint32_t j = 0; j < 3; ++j)
+#pragma unroll
+      for (int i = 0; i < N; ++i) n[j] += popc64(ballot(keys[i] >= (found | (j + 1) << b)));
+    const uint32_t passed = n[2] >= k ? 3 : n[1] >= k ? 2 : n[0] >= k ? 1 : 0;
+    const uint32_t reached = n[2] >= k ? n[2] : n[1] >= k ? n[1] : n[0];
+    found |= passed << b;
+    if (reached == k) break;
   }
   return found;
 }
@@ -278,7 +281,8 @@ struct Seen {
   __device__ __forceinline__ void begin(float most) {
     const uint32_t keys[1] = {most > -INFINITY ? key_of(most) : 0};
     if (popc64(ballot(keys[0] != 0)) <= k) return;
-    const uint32_t reached = reached_by<L::KEY_BITS, 1>(keys, k, 0);
+    const uint32_t least = ~max_over_wave(keys[0] ? ~keys[0] : 0);
+    const uint32_t reached = reached_by<L::KEY_BITS, 1>(keys, k, least);
     if (reached > LOWEST_KEY) border = value_of_key(reached - (reached == 0x80000000u ? 2 : 1));         // (there is no key of -0)
   }
 
@@ -429,12 +433,18 @@ __global__ __launch_bounds__(W * WAVE) void k_scores(ScoresArgs a) {
     seen.add(x, all, least, a.c);
     if (seen.border == -INFINITY) seen.begin(all);
     if (!ballot(all > seen.border)) continue;
+    // (Groups before these are all that the list holds: one that is only as large as the k-th is none of the k.)
+    uint32_t hits = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < SCORES_BATCH; ++i) hits |= most[i] > seen.border ? 1u << i : 0;
 #pragma unroll 1
-    for (uint32_t i = 0; i < SCORES_BATCH; ++i) {
+    while (ballot(hits)) {                       // a lane's first one, and mostly its only one
+      const uint32_t i = __ffs(static_cast<int>(hits)) - 1;
       float of = most[0];
 #pragma unroll
       for (uint32_t j = 1; j < SCORES_BATCH; ++j) of = i == j ? most[j] : of;
-      seen.append(of > seen.border, of, 1 + mine + i * WAVE, lds);         // (a later group that is only as large as the k-th is none of the k)
+      seen.append(hits && of >= seen.border, of, 1 + mine + i * WAVE, lds);
+      hits &= hits - 1;
       if (seen.n > WAVE) seen.shorten(lds);
     }
   }
