@@ -116,7 +116,8 @@ struct ScoresCut {
   uint32_t parts, per_part, waves;
   uint64_t sums_bytes, bytes;
 };
-// A row is one workgroup's where that takes it in one turn, of 4 waves or of 16 (one row of 32,000 bfloat16 logits 9.3 us; 10.9 in parts that a second
+// A row is one wave's where that takes it in a turn, or in four and there are many (20,000 rows of 1000 bfloat16 logits 40 us, 4 waves 67; 8000 rows of
+// 8192 37 and 42).  It is one workgroup's where that takes it in one turn, of 4 waves or of 16 (one row of 32,000 bfloat16 logits 9.3 us; 10.9 in parts that a second
 // launch joins), and from 128 rows on, of 16 waves up to 1023 rows (256 rows of 50,001 float32 16.0 us; 4 waves 21) and of 4 beyond (1100 rows of
 // 131,072 bfloat16 59.8; 16 waves 72.5).  Else rows are cut into parts of 4 waves, for two workgroups on a compute unit: one compute unit takes 2 us to read
 // what 16 waves want first (one row of 131,072 logits 15.9 us; in parts of 16 waves 17.1, 64 such rows 19.5 and 20.5).
@@ -126,7 +127,8 @@ ScoresCut scores_cut(uint32_t n_rows, uint32_t vocabulary, int32_t value_type, u
   ScoresCut c{};
   const uint32_t groups = vocabulary / (value_type == FIKIT_F32 ? LogitsF32::VEC : LogitsBf16::VEC), turn = SCORES_BATCH * WAVE;
   const bool few = n_rows < SCORES_CHIP / 2;
-  c.waves = groups <= 4 * turn || n_rows >= SCORES_MANY || (few && groups > 16 * turn) ? 4 : 16;
+  const bool one_wave = groups <= turn || (n_rows >= 2 * SCORES_MANY && groups <= 4 * turn);
+  c.waves = one_wave ? 1 : groups <= 4 * turn || n_rows >= SCORES_MANY || (few && groups > 16 * turn) ? 4 : 16;
   const uint32_t most = (groups + c.waves * turn - 1) / (c.waves * turn), want = n_rows > 0 && few && c.waves == 4 ? 2 * SCORES_CHIP / n_rows : 1;
   c.parts = want < most ? want : most;
   if (c.parts < 1) c.parts = 1;
@@ -147,7 +149,10 @@ struct ScoresCall {
   template <typename L>
   int run() {
     const dim3 grid(a.rows * a.parts), block(waves * WAVE), join(JOIN_WAVES * WAVE);
-    if (int rc = waves == 16 ? enqueue(k_scores<L, 16>, grid, block, st, a) : enqueue(k_scores<L, 4>, grid, block, st, a)) return rc;
+    if (int rc = waves == 16  ? enqueue(k_scores<L, 16>, grid, block, st, a)
+                 : waves == 4 ? enqueue(k_scores<L, 4>, grid, block, st, a)
+                              : enqueue(k_scores<L, 1>, grid, block, st, a))
+      return rc;
     return a.parts == 1 ? FIKIT_OK : enqueue(k_scores_join<L>, dim3((a.rows + JOIN_WAVES - 1) / JOIN_WAVES), join, st, a);
   }
 };
