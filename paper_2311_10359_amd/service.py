@@ -1,6 +1,6 @@
 """A language model service's two tasks on one GPU, measured and given to the gap fill.
 
-  python -m paper_2311_10359_amd.service [--layers 4] [--requests 32] [--steps 20] ...
+  python -m paper_2311_10359_amd.service [--layers 4] [--requests 32] [--steps 20] [--rotary 128] [--beams 4] ...
 
 The attention stack of a decoder (random weights; per layer a product to queries, keys and values, attention, a product back)
 serves requests: their prompts first, then one token each per step.  Two tasks result that share the GPU in such a service:
@@ -11,6 +11,9 @@ serves requests: their prompts first, then one token each per step.  Two tasks r
 Every call's start and end are measured with events, as in the measurement phase, and written as launch records (a call
 stands for its launches; its identity is its name and the sizes it was called with).  `fikit_profile_gapfill` then tells how
 much of the prompts' work fits into the decode steps' idle times.
+
+With `--rotary` heads are normed and rotated by position in front of the cache.  With `--beams` a request is continued by several beams:
+every step scores their alternatives, and the best ones fork the requests, whose whole blocks they share.
 """
 from __future__ import annotations
 
@@ -18,7 +21,7 @@ import argparse
 import math
 import random
 import time
-from typing import List, NamedTuple
+from typing import List, NamedTuple, Optional
 
 import numpy as np
 import torch
@@ -34,6 +37,7 @@ class Sizes(NamedTuple):
     block: int = 64
     blocks: int = 4096         # of the cache, per layer
     vocabulary: int = 8192
+    rotary: int = 0            # dimensions of a head that are rotated; 0: heads are neither normed nor rotated
 
     @property
     def hidden(self) -> int:
@@ -90,6 +94,9 @@ class Service:
         self.taken = 0                                  # blocks, from the front of `free`
         self.longest = 0
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
+        if sizes.rotary:
+            self.frequencies = (10000.0 ** (-torch.arange(0, sizes.rotary, 2, device=device, dtype=torch.float64) / sizes.rotary)).float()
+            self.norms = [[(1 + 0.1 * torch.randn(sizes.dim, generator=gen, device=device)).to(torch.bfloat16) for _ in range(2)] for _ in range(sizes.layers)]
 
     def _plan(self, record, added: List[int]) -> binding.CachePlan:
         n, sizes = sum(added), self.sizes
@@ -97,10 +104,13 @@ class Service:
                       torch.tensor(added, dtype=torch.int32).to(self.device, non_blocking=True), n, sizes.block, self.table,
                       self.free[self.taken:], self.status, want_slots=False)
 
-    def _layer(self, record, x, layer, attend, plan):
+    def _layer(self, record, x, layer, attend, plan, positions):
         sizes, n = self.sizes, x.shape[0]
         qkv = record("to queries, keys, values", (n, 1, 1), torch.mm, x, self.w_qkv[layer]).view(n, -1, sizes.dim)
         q, k, v = qkv.split((sizes.q_heads, sizes.kv_heads, sizes.kv_heads), 1)
+        if sizes.rotary:
+            record("rotate", (n, 1, 1), binding.fikit_rotate_heads, q, k, positions, self.frequencies, self.status, q_weight=self.norms[layer][0],
+                   k_weight=self.norms[layer][1], out=binding.RotatedHeads(q, k))
         record("append", (n, 1, 1), binding.fikit_cache_append, *self.caches[layer], k, v, plan.pieces, self.status)
         out = attend(q, k, v, layer)
         return x + record("back", (n, 1, 1), torch.mm, out.view(n, -1), self.w_out[layer])
@@ -112,10 +122,13 @@ class Service:
             raise ValueError("prompts of requests that have no tokens in the cache")
         plan = self._plan(record, lengths)
         scale = 1 / math.sqrt(self.sizes.dim)
+        positions = None
+        if self.sizes.rotary:
+            positions = torch.from_numpy(np.concatenate([np.arange(n, dtype=np.int32) for n in lengths])).to(self.device, non_blocking=True)
         for layer in range(self.sizes.layers):
             x = self._layer(record, x, layer, lambda q, k, v, _: record(
                 "prompt attention", (q.shape[0], len(lengths), 1), binding.fikit_prompt_attention, q, k, v, plan.token_offsets, scale,
-                self.status, want_lse=False).out, plan)
+                self.status, want_lse=False).out, plan, positions)
         self._settle(plan, max(lengths))
         return x
 
@@ -127,24 +140,82 @@ class Service:
         for layer in range(self.sizes.layers):
             x = self._layer(record, x, layer, lambda q, k, v, at: record(
                 "cache attention", (n, 1, 1), binding.fikit_cache_attention, q, *self.caches[at], self.table, plan.lengths, scale,
-                self.status, max_length=self.longest + 1, want_lse=False).out, plan)
+                self.status, max_length=self.longest + 1, want_lse=False).out, plan, self.lengths)
         logits = record("to tokens", (n, 1, 1), torch.mm, x, self.w_tokens)
         self._settle(plan, 1)
         return logits
 
-    def _settle(self, plan, most_added) -> None:
-        """What the host does at the end of a step, when it waits for the outputs anyway."""
+    def tokens(self, tokens: torch.Tensor) -> torch.Tensor:
+        """What goes in for tokens: [n, hidden]."""
+        return self.w_tokens.t()[tokens.long()] * math.sqrt(self.sizes.hidden)
+
+    def score(self, record, logits: torch.Tensor, n_top: int, tokens: Optional[torch.Tensor] = None) -> binding.TokenScores:
+        return record("score", (logits.shape[0], 1, 1), binding.fikit_token_scores, logits, tokens, self.status, n_top=n_top)
+
+    def fork(self, record, parents: torch.Tensor) -> None:
+        """parents: int32 [n].  Request i is from now on the continuation of what was request parents[i], or an empty one for -1; requests that
+        are nobody's parent end."""
+        sizes = self.sizes
+        fork = record("fork", (parents.numel(), 1, 1), binding.fikit_cache_fork, self.table, self.lengths, parents, sizes.block, sizes.blocks,
+                      self.free[self.taken:], self.status)
+        record("copy", (parents.numel(), 1, 1), binding.fikit_cache_copy, self.caches, fork.copies, self.status)
+        self._check()
+        self.table, self.lengths = fork.block_table, fork.lengths
+        self.free, self.taken = fork.free_blocks[:int(fork.counts[2])], 0
+
+    def compact(self, record) -> int:
+        """Moves the blocks in use together; returns the number of blocks behind the last of them."""
+        sizes = self.sizes
+        compaction = record("compact", (self.lengths.numel(), 1, 1), binding.fikit_cache_compact, self.table, self.lengths, sizes.block, sizes.blocks,
+                            self.free[self.taken:], self.status)
+        record("copy", (self.lengths.numel(), 1, 1), binding.fikit_cache_copy, self.caches, compaction.copies, self.status)
+        self._check()
+        self.table, self.free, self.taken = compaction.block_table, compaction.free_blocks, 0
+        return sizes.blocks - int(compaction.counts[1])
+
+    def _check(self) -> None:
         try:
             binding.fikit_check_status(self.status)
         except binding.FikitError:
             self.status.zero_()           # nothing of the step counts, and it can be tried again
             raise
+
+    def _settle(self, plan, most_added) -> None:
+        """What the host does at the end of a step, when it waits for the outputs anyway."""
+        self._check()
         self.lengths = plan.lengths
         self.taken += int(plan.counts[0])
         self.longest += most_added
 
 
-def measure(sizes: Sizes = Sizes(), requests: int = 32, longest_prompt: int = 256, steps: int = 20, host_ms: float = 0.5, seed: int = 0):
+class Beams:
+    """Beam search: every request is continued by the `width` most probable of its beams' alternatives."""
+
+    def __init__(self, service: Service, record, logits: torch.Tensor, width: int):
+        """logits: [requests, vocabulary] behind the prompts."""
+        self.service, self.width = service, width
+        top = service.score(record, logits, width)
+        n = logits.shape[0]
+        service.fork(record, torch.arange(n, dtype=torch.int32, device=logits.device).repeat_interleave(width))
+        self.tokens, self.logprob = top.top_tokens.reshape(-1), top.top_logprob.reshape(-1)
+
+    def step(self, record) -> torch.Tensor:
+        """One more token for each beam; returns the parents, by the beams before."""
+        width = self.width
+        logits = self.service.step(record, self.service.tokens(self.tokens))
+        top = self.service.score(record, logits, width)
+        # a request's width x width continuations, of which width are kept
+        all_of = (self.logprob[:, None] + top.top_logprob).reshape(-1, width * width)
+        self.logprob, best = (t.reshape(-1) for t in torch.topk(all_of, width, 1))
+        request = torch.arange(all_of.shape[0], device=best.device).repeat_interleave(width)
+        self.tokens = top.top_tokens.reshape(-1)[request * width * width + best]
+        parents = (request * width + best // width).to(torch.int32)
+        self.service.fork(record, parents)
+        return parents
+
+
+def measure(sizes: Sizes = Sizes(), requests: int = 32, longest_prompt: int = 256, steps: int = 20, host_ms: float = 0.5, seed: int = 0,
+            beams: int = 1):
     """Records of the two tasks (decode steps, prompts) and the services' last outputs."""
     rng = random.Random(seed)
     lengths = [rng.randint(1, longest_prompt) for _ in range(requests)]
@@ -159,9 +230,16 @@ def measure(sizes: Sizes = Sizes(), requests: int = 32, longest_prompt: int = 25
         got["prompts"] = service.prompts(record, tokens(sum(lengths)), lengths)
         if task != "prompts":
             record = Recorder()
+            if beams > 1:
+                last = torch.from_numpy(np.cumsum(lengths) - 1).to("cuda:0")
+                search = Beams(service, record, torch.mm(got["prompts"][last], service.w_tokens), beams)
             for i in range(steps):
                 record.run = i
-                got["step"] = service.step(record, tokens(requests))
+                if beams > 1:
+                    search.step(record)
+                    got["step"] = search.logprob
+                else:
+                    got["step"] = service.step(record, tokens(requests))
                 time.sleep(host_ms * 1e-3)
         records[task] = (record.records(), record.names)
     return records["decode"], records["prompts"], got, service
@@ -174,8 +252,10 @@ def main(argv=None) -> None:
     p.add_argument("--longest-prompt", type=int, default=256)
     p.add_argument("--steps", type=int, default=20)
     p.add_argument("--host-ms", type=float, default=0.5, help="the host's time between two steps")
+    p.add_argument("--rotary", type=int, default=0, help="dimensions of a head that are rotated by position; 0: no norm and no rotation")
+    p.add_argument("--beams", type=int, default=1, help="beams of a request")
     a = p.parse_args(argv)
-    (decode, names), (prompts, _), _, _ = measure(Sizes(layers=a.layers), a.requests, a.longest_prompt, a.steps, a.host_ms)
+    (decode, names), (prompts, _), _, _ = measure(Sizes(layers=a.layers, rotary=a.rotary), a.requests, a.longest_prompt, a.steps, a.host_ms, beams=a.beams)
     decode["run"] = 0                                   # one trace: the idle times between steps are what is filled
     rec = np.concatenate([decode, prompts])
     off = np.array([0, decode.size, rec.size], dtype=np.uint64)
@@ -185,7 +265,7 @@ def main(argv=None) -> None:
         binding.to_device_records(rec, dev), binding.to_device_u64(off, dev), binding.to_device_u32(hp, dev), binding.to_device_u32(lp, dev),
         binding.to_device_u64(traces.gap_offsets(off, hp), dev), margin_ns=500, min_gap_ns=0, predictor=binding.FIKIT_PREDICT_MEAN)
     rows = binding.rows_to_numpy(profile.rows)
-    print(f"{decode.size} calls in {a.steps} decode steps of {a.requests} requests, {prompts.size} calls for {a.requests} prompts, {rows.size} kernels")
+    print(f"{decode.size} calls in {a.steps} decode steps of {a.requests * a.beams} requests, {prompts.size} calls for {a.requests} prompts, {rows.size} kernels")
     for task, title in ((0, "decode"), (1, "prompts")):
         mine = rows[rows["task"] == task]
         print(f"  {title}: {mine['exec']['sum'].sum() / 1e6:.2f} ms busy, {mine['gap']['sum'].sum() / 1e6:.2f} ms idle")

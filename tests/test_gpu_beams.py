@@ -1,0 +1,144 @@
+"""Beams on the example service: rotation, append, attention, scores, forks, copies and a compaction together, as a search uses them."""
+import math
+
+import pytest
+import torch
+
+import around_model
+import serve_model as model
+from paper_2311_10359_amd import binding, service
+
+pytestmark = pytest.mark.gpu
+SIZES = service.Sizes(layers=2, q_heads=8, kv_heads=2, dim=64, block=16, blocks=120, vocabulary=517, rotary=32)
+
+
+class Watch:
+    """Runs the calls and keeps what the checks need: the first layer's keys and values, rotations, scores."""
+
+    def __init__(self, sizes):
+        self.sizes, self.appended, self.rotated, self.scored, self.attended, self.calls = sizes, [], [], [], [], []
+
+    def __call__(self, name, _, f, *args, **more):
+        before = [args[0].clone(), args[1].clone()] if name == "rotate" else None
+        got = f(*args, **more)
+        nth = sum(c == name for c in self.calls)
+        self.calls.append(name)
+        if nth % self.sizes.layers == 0:
+            if name == "append":
+                self.appended.append((args[4].cpu(), args[5].cpu()))
+            if name == "rotate":
+                self.rotated.append((before, [t.clone() for t in (args[0], args[1])], args[2].clone(), more["q_weight"], more["k_weight"]))
+            if name == "cache attention":
+                self.attended.append((args[0].cpu(), got.out.cpu()))
+        if name == "score":
+            self.scored.append((args[0].clone(), got))
+        return got
+
+
+def test_beams_hold_what_their_parents_put_into_the_cache():
+    lengths, width, steps = [5, 40, 17], 4, 21                       # (over the border of a block and of two)
+    s = service.Service(SIZES, 3, 80, seed=3)
+    watch = Watch(SIZES)
+    gen = torch.Generator(device="cuda:0").manual_seed(4)
+    x = torch.randn((sum(lengths), SIZES.hidden), generator=gen, device="cuda:0").to(torch.bfloat16)
+    out = s.prompts(watch, x, lengths)
+    last = torch.tensor(lengths).cumsum(0) - 1
+    beams = service.Beams(s, watch, torch.mm(out[last.to("cuda:0")], s.w_tokens), width)
+    lineage = [[r] for r in range(3) for _ in range(width)]            # per beam: its request, then its row in the append of each step
+    totals = beams.logprob.cpu().double()
+    for _ in range(steps):
+        parents = beams.step(watch).tolist()
+        lineage = [lineage[p] + [p] for p in parents]
+    assert set(watch.calls) == {"plan", "rotate", "append", "to queries, keys, values", "back", "prompt attention", "cache attention", "to tokens", "score", "fork",
+                                "copy"}
+    assert s.lengths.tolist() == [n + steps for n in lengths for _ in range(width)]
+    # every block is free or in use, none both; whole blocks of the prompts are shared
+    table = s.table.cpu()
+    used = [set(table[i, :-(-int(n) // 16)].tolist()) for i, n in enumerate(s.lengths.tolist())]
+    free = s.free[s.taken:].tolist()
+    assert sorted(set().union(*used) | set(free)) == list(range(SIZES.blocks)) and not set().union(*used) & set(free) and len(set(free)) == len(free)
+    for r, n in enumerate(lengths):
+        for b in range(1, width):
+            assert table[r * width + b, :n // 16].tolist() == table[r * width, :n // 16].tolist()
+    # a beam's keys and values in the cache: the prompt's, then those of the beams that it descends from
+    codes = [c.view(torch.uint8).cpu() for c in s.caches[0]]
+    at = [0] + (last + 1).tolist()
+    held = {}
+    for i, rows in enumerate(lineage):
+        n = int(s.lengths[i])
+        for side in (0, 1):
+            given = torch.cat([watch.appended[0][side][at[rows[0]]:at[rows[0] + 1]]] +
+                              [watch.appended[1 + t][side][row:row + 1] for t, row in enumerate(rows[1:])]).double()
+            kept = model.cache_values(codes[side], codes[2 + side], table[i], n, SIZES.block)
+            # a code is within 2^-4 of a value (half a step twice, where a scale has grown), or half a smallest step of the block's largest scale
+            assert bool(((given - kept).abs() <= given.abs() / 8 + given.abs().max() * 2.0 ** -8).all())
+            held[i, side] = kept
+    # the last step's attention saw the parents' caches, which the beams hold, all but one token
+    q, got = watch.attended[-1]
+    for i, rows in enumerate(lineage):
+        want = model.Rows(q[rows[-1]:rows[-1] + 1], held[i, 0], held[i, 1], 1 / math.sqrt(SIZES.dim), [int(s.lengths[i])], torch.bfloat16)
+        assert model.near(got[rows[-1]:rows[-1] + 1].double(), want.out, want.bound)
+    # rotations, at the positions of the tokens
+    for before, after, positions, *weights in (watch.rotated[0], watch.rotated[1], watch.rotated[-1]):
+        for x0, x1, w in zip(before, after, weights):
+            want, bound = around_model.rotate(x0, w, 1e-6, positions, s.frequencies, False)
+            assert around_model.near(x1, want, bound)
+    assert watch.rotated[0][2].tolist() == [i for n in lengths for i in range(n)]
+    assert watch.rotated[-1][2].tolist() == [n + steps - 1 for n in lengths for _ in range(width)]
+    # scores, and the sums of the beams that were kept: descending, and a parent's sum and an alternative's each
+    for logits, got in watch.scored:
+        scores = around_model.Scores(logits, None, 1.0, width)
+        del scores.want["entropy"], scores.want["lse"]
+        assert scores.differs(got) == []
+    sums = beams.logprob.reshape(3, width)
+    assert bool((sums[:, 1:] <= sums[:, :-1]).all()) and bool((sums[:, 0].cpu() < totals.reshape(3, width)[:, 0]).all())
+
+
+def test_a_compaction_moves_blocks_and_changes_no_attention():
+    s = service.Service(SIZES, 3, 80, seed=5)
+    gen = torch.Generator(device="cuda:0").manual_seed(6)
+
+    def run(name, _, f, *args, **more):
+        return f(*args, **more)
+
+    def tokens(n):
+        return torch.randn((n, SIZES.hidden), generator=gen, device="cuda:0").to(torch.bfloat16)
+    s.prompts(run, tokens(62), [5, 40, 17])
+    s.fork(run, torch.tensor([1, 2, 1, 1, -1], dtype=torch.int32, device="cuda:0"))
+    assert s.lengths.tolist() == [40, 17, 40, 40, 0]
+    for _ in range(3):
+        s.step(run, tokens(5))
+    q = torch.randn((5, 8, 64), generator=gen, device="cuda:0").to(torch.bfloat16)
+
+    def attend():
+        return [binding.fikit_cache_attention(q, *cache, s.table, s.lengths, 0.125, s.status) for cache in s.caches]
+    before, behind, used = attend(), s.compact(run), s.table.cpu()
+    in_use = {b for row, n in zip(used.tolist(), s.lengths.tolist()) for b in row[:-(-n // 16)]}
+    assert in_use == set(range(len(in_use))) and behind == SIZES.blocks - len(in_use) and s.free.tolist() == list(range(len(in_use), SIZES.blocks))
+    for a, b in zip(before, attend()):
+        assert torch.equal(a.out, b.out) and torch.equal(a.lse, b.lse)
+    s.step(run, tokens(5))
+    assert int(s.status) == 0 and s.lengths.tolist() == [44, 21, 44, 44, 4]
+
+
+def test_too_few_blocks_for_a_fork_leave_the_service_as_it_was():
+    s = service.Service(SIZES._replace(blocks=8), 2, 80, seed=7)
+
+    def run(name, _, f, *args, **more):
+        return f(*args, **more)
+    x = torch.zeros((62, SIZES.hidden), dtype=torch.bfloat16, device="cuda:0")
+    s.prompts(run, x, [45, 17])                                         # 3 + 2 blocks of 8
+    table = s.table.clone()
+    many = torch.zeros(9, dtype=torch.int32, device="cuda:0")
+    with pytest.raises(binding.FikitError) as e:
+        s.fork(run, many)
+    assert e.value.status == binding.FIKIT_CACHE_FULL and int(s.status) == 0
+    assert torch.equal(s.table, table) and s.lengths.tolist() == [45, 17] and s.taken == 5
+    s.fork(run, many[:6])                                               # (5 blocks, with the two that request 1 gives back)
+    assert s.lengths.tolist() == [45] * 6 and s.free.numel() == 0
+
+
+def test_the_command_measures_beams():
+    (decode, names), (prompts, _), got, s = service.measure(SIZES, requests=3, longest_prompt=40, steps=3, host_ms=0.1, beams=2)
+    assert {"rotate", "score", "fork", "copy"} <= set(names) and int(s.status) == 0
+    assert bool(torch.isfinite(got["step"]).all()) and got["step"].shape == (6,) and (decode["end_ns"] >= decode["start_ns"]).all()

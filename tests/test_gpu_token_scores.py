@@ -132,7 +132,8 @@ def test_one_token_holds_all():
 
 
 @pytest.mark.parametrize("rows, v, dtype", [(70000, 13, torch.float32), (3000, 1000, torch.bfloat16), (600, 8192, torch.float16), (130, 50000, torch.bfloat16), (3, 1 << 20, torch.float16),
-                                            (1, 2_000_003, torch.float32), (2, 300_001, torch.bfloat16), (511, 20001, torch.bfloat16), (513, 20001, torch.bfloat16)])
+                                            (1, 2_000_003, torch.float32), (2, 300_001, torch.bfloat16), (511, 20001, torch.bfloat16), (513, 20001, torch.bfloat16), (1500, 20001, torch.bfloat16),
+                                            (2100, 8001, torch.bfloat16), (2100, 4001, torch.float32)])
 def test_rows(rows, v, dtype):
     x = torch.randn((rows, v), generator=torch.Generator(device=DEV).manual_seed(rows), device=DEV, dtype=torch.float32).mul_(2).to(dtype)
     check(x, tokens_for(8, rows, v), 20 if v > 100 else 3)

@@ -65,3 +65,23 @@ def test_a_step_that_fails_leaves_the_service_as_it_was():
     assert s.lengths.tolist() == [4, 5] and s.taken == 3 and s.longest == 5 and int(s.status) == 0
     s.step(Fake(), tokens(2))
     assert s.lengths.tolist() == [5, 6]
+
+
+def test_a_fork_that_fails_leaves_the_service_as_it_was():
+    s = service.Service(SIZES, 2, 64, device="cpu")
+    s.prompts(Fake(), tokens(9), [4, 5])
+    table, free = s.table, s.free
+
+    def record(name, sizes, f, *args, **more):
+        if name == "fork":
+            args[-1].fill_(status)
+            return binding.CacheFork(torch.ones((3, 4), dtype=torch.int32), torch.tensor([4, 4, 5], dtype=torch.int32), None, torch.arange(8, dtype=torch.int32),
+                                     torch.tensor([1, 0, 5], dtype=torch.int32))
+        assert name == "copy" and args[0] is s.caches
+    status = binding.FIKIT_CACHE_FULL
+    with pytest.raises(binding.FikitError):
+        s.fork(record, torch.tensor([0, 0, 1], dtype=torch.int32))
+    assert s.table is table and s.free is free and s.taken == 3 and s.lengths.tolist() == [4, 5] and int(s.status) == 0
+    status = binding.FIKIT_OK
+    s.fork(record, torch.tensor([0, 0, 1], dtype=torch.int32))
+    assert s.lengths.tolist() == [4, 4, 5] and s.taken == 0 and s.free.tolist() == [0, 1, 2, 3, 4]
