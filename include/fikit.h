@@ -588,8 +588,8 @@ int fikit_prompt_attention(const fikit_vectors* h_q, const fikit_vectors* h_k, c
  *   fikit_token_scores      what rows of logits say: log probabilities of given tokens, entropy, alternatives
  *
  * Nobody keeps count of a block's holders: it is held as long as a row of the table names it within the request's length, and several
- * rows may (their requests have the same tokens there).  New tokens go into blocks that one request holds alone: fikit_cache_fork leaves every
- * last block that is not full to one request.
+ * rows may (their requests have the same tokens there).  New tokens go into blocks that one request holds alone, so a last block that is not
+ * full has to be one request's; where it was, fikit_cache_fork leaves it so.
  */
 
 typedef enum fikit_pairs {
@@ -613,8 +613,9 @@ typedef enum fikit_pairs {
  *   d_frequencies     [rotary_dim / 2] radians for a position (any table); NULL if rotary_dim is 0.
  *   rotary_dim        a multiple of 16 up to head_dim.
  *   pairs             a fikit_pairs.
- *   h_q_out, h_k_out  outputs of the same sizes, strides of at least head_dim where there are several.  An output may be its own input (the
- *                     same address and strides); else outputs overlap neither each other nor an input.
+ *   h_q_out, h_k_out  outputs of the same sizes, whose vectors lie apart: tokens of heads or heads of tokens, one behind the other or with
+ *                     gaps (else INVALID_ARG).  An output may be its own input (the same address and strides); else outputs overlap neither
+ *                     each other nor an input.
  *
  * The range of the type counts: a norm of values whose squares pass the largest float is right.
  */

@@ -29,9 +29,16 @@ struct RotateCall {
   int with_dim(uint32_t head_dim) { return head_dim == 64 ? run<T, 64>() : head_dim == 128 ? run<T, 128>() : run<T, 256>(); }
 };
 
-// Outputs of `heads` heads whose vectors do not lie over each other.
+// Do the vectors lie apart?  Those of the smaller stride beside each other, and the larger stride beyond all of them.
 bool apart(const fikit_vectors* v, uint32_t heads, uint32_t n_tokens, uint32_t head_dim) {
-  return (heads <= 1 || v->head_stride >= head_dim) && (n_tokens <= 1 || v->token_stride >= head_dim);
+  struct { uint64_t stride, n; } inner{v->head_stride, heads}, outer{v->token_stride, n_tokens};
+  if (inner.n <= 1 || (outer.n > 1 && outer.stride < inner.stride)) {
+    const auto other = inner;
+    inner = outer;
+    outer = other;
+  }
+  if (inner.n > 1 && inner.stride < head_dim) return false;
+  return outer.n <= 1 || (outer.stride >= head_dim && (outer.stride - head_dim) / (inner.n > 1 ? inner.stride : 1) >= (inner.n > 1 ? inner.n - 1 : 0));
 }
 
 bool rotates_in_place_or_elsewhere(const fikit_vectors* in, const fikit_vectors* out, uint32_t heads, uint32_t n_tokens) {

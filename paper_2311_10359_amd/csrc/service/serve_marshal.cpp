@@ -487,8 +487,8 @@ PyObject* py_cache_compact(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
 struct Owned {
   PyObject* o;
   explicit Owned(PyObject* given) : o(given) { if (!o) throw python_error(); }
-  Owned(const Owned&) = delete;
-  ~Owned() { Py_DECREF(o); }
+  Owned(Owned&& other) noexcept : o(other.o) { other.o = nullptr; }
+  ~Owned() { Py_XDECREF(o); }
 };
 
 // caches (a sequence of sequences k_cache, v_cache, k_exp, v_exp), copies, status, stream
@@ -500,8 +500,10 @@ PyObject* py_cache_copy(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   TORCH_CHECK_VALUE(copies.dim() == 2 && copies.size(1) == 2 && status.numel() == 1, "copies: [n, 2]; status: [1]");
   const Owned all(PySequence_Tuple(a[0]));
   std::vector<fikit_cache> caches;
+  std::vector<Owned> held;                     // (other threads may change the sequences while the call enqueues)
   for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(all.o); ++i) {
-    const Owned one(PySequence_Tuple(PyTuple_GET_ITEM(all.o, i)));
+    held.emplace_back(PySequence_Tuple(PyTuple_GET_ITEM(all.o, i)));
+    const Owned& one = held.back();
     TORCH_CHECK_VALUE(PyTuple_GET_SIZE(one.o) == 4, "caches: of k_cache, v_cache, k_exp, v_exp each");
     PyObject* const parts[] = {PyTuple_GET_ITEM(one.o, 0), PyTuple_GET_ITEM(one.o, 1), PyTuple_GET_ITEM(one.o, 2), PyTuple_GET_ITEM(one.o, 3)};
     caches.push_back(cache_of(parts, device));

@@ -23,7 +23,8 @@ def rotate(**change):
 @pytest.mark.parametrize("change, want", [
     (dict(q=vectors(NULL)), INVALID), (dict(q=None), INVALID), (dict(k=vectors(FAKE + 8)), INVALID), (dict(k=vectors(token=4)), INVALID),
     (dict(k_out=vectors(0x40000, head=68)), INVALID), (dict(k_out=None), INVALID), (dict(q_out=vectors(0x30000, head=32)), INVALID),
-    (dict(q_out=vectors(0x30000, token=0)), INVALID), (dict(q_out=vectors(0x30000, head=0)), INVALID),
+    (dict(q_out=vectors(0x30000, token=0)), INVALID), (dict(q_out=vectors(0x30000, token=128)), INVALID), (dict(q_out=vectors(0x30000, token=64, head=128)), INVALID),
+    (dict(q_out=vectors(0x30000, token=248)), INVALID), (dict(k_out=vectors(0x40000, token=120)), INVALID), (dict(q_out=vectors(0x30000, token=64, head=312)), INVALID), (dict(q_out=vectors(0x30000, head=0)), INVALID),
     (dict(q_out=vectors(FAKE, token=1024)), INVALID), (dict(q_out=vectors(FAKE, head=128)), INVALID),       # in place, of other strides
     (dict(q_out=vectors(0x20000)), INVALID), (dict(k_out=vectors(FAKE)), INVALID), (dict(k_out=vectors(0x30000)), INVALID),
     (dict(q_weight=FAKE + 8), INVALID), (dict(k_weight=ODD), INVALID), (dict(epsilon=0.0), INVALID), (dict(epsilon=-1.0), INVALID),
