@@ -5,15 +5,14 @@
 
 namespace fikit {
 
-// A row x of V logits and a scale s.  In units of log 2, with c = s log2(e), R a number near the largest c x and d = c x - R:
+// A row x of V logits and a scale s.  In units of log 2, with c = s log2(e), m the largest logit and d = c (x - m):
 //
-//   S = sum 2^d,  T = sum 2^d d      log(sum exp(s x)) = ln 2 (R + log2 S)      entropy = ln 2 (log2 S - T / S)
+//   S = sum 2^d,  T = sum 2^d d      log(sum exp(s x)) = s m + ln 2 log2 S      entropy = ln 2 (log2 S - T / S)
 //   log probability of a token = ln 2 (d - log2 S)
 //
-// in one pass: every lane keeps R, S and T of what it has seen.  R is a whole number, so sums move to another R by a power of two,
-// exactly, and d has one rounding.  (R = c max x would have a rounding of its own, 2^-24 of up to 150, in every d.)  From 2^22 on, where a float
-// holds no halves, whole or not makes no difference and the rounding of c x would: there d is a difference of rounded products, 0 for equal
-// logits whatever their size.  So that the type's lowest value, a mask in many programs, stays finite, R is held as R / 4.
+// in one pass: every lane keeps m, S and T of what it has seen, and moves the sums to another m where a larger logit comes.  d of the largest is 0 whatever
+// its size, so that one token that holds all has entropy and log probability 0, and the type's lowest value, a mask in many programs, is a number as others.
+// (c x - c m in one instruction would leave the rounding of c m in d; the pass is no faster with it, 97 us for 2999 rows of 100,003.)
 //
 // The k alternatives lie in k groups of neighbouring logits (16 bytes, as one load brings them): those with the largest maxima, among equal ones
 // the first, since of any other group k groups before it in this order hold a value that comes before all of its own.  So the pass looks
@@ -33,15 +32,14 @@ struct ScoresArgs {
   int32_t* top_tokens;
   float* top_logprob;
   int32_t* status;
-  float4* sums;             // workspace: [rows][parts] R / 4, S and T
+  float4* sums;             // workspace: [rows][parts] m, S, T and the border
   float2* lists;            // [rows][parts][n_top] maxima and groups, minus infinity where there is none
   uint32_t rows, vocabulary, n_top, parts, per_part;      // per_part: groups
   float scale, c;           // c = scale log2(e)
 };
 
 constexpr int SCORES_BATCH = 4, SCORES_MOST = 32, SCORES_ROOM = 128, JOIN_WAVES = 4, JOIN_ROOM = 512;
-constexpr float NO_SUM = -3.4028234663852886e38f;       // R / 4 where nothing has been seen
-constexpr float WHOLE = 0x1p20f;                        // R / 4 below which R is whole
+constexpr float LOWEST = -3.4028234663852886e38f;       // m where nothing has been seen
 
 struct LogitsBf16 {
   typedef uint16_t raw;
@@ -152,33 +150,23 @@ __device__ __forceinline__ void lds_in_order() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// R / 4, S and T of some logits.
+// m, S and T of some logits.
 struct Sums {
-  float r = NO_SUM, s = 0, t = 0;
+  float m = LOWEST, s = 0, t = 0;
 
-  // The same relative to another R that is no smaller; far below it nothing is left.
-  __device__ __forceinline__ void move_to(float next) {
-    const float move = 4.f * (r - next), f = exp2_fast(move);
+  // The same relative to another m that is no smaller; far below it nothing is left.
+  __device__ __forceinline__ void move_to(float next, float c) {
+    const float move = (m - next) * c, f = exp2_fast(move);
     t = f == 0.f ? 0.f : (t + move * s) * f;
     s *= f;
-    r = next;
+    m = next;
   }
-  __device__ __forceinline__ void add(Sums other) {
-    const float next = fmaxf(r, other.r);
-    move_to(next);
-    other.move_to(next);
+  __device__ __forceinline__ void add(Sums other, float c) {
+    const float next = fmaxf(m, other.m);
+    move_to(next, c);
+    other.move_to(next, c);
     s += other.s;
     t += other.t;
-  }
-  // d of a logit
-  __device__ __forceinline__ float exponent(float x, float c) const {
-    if (fabsf(r) < WHOLE) return __builtin_fmaf(x, c, -4.f * r);
-    return difference(x, c);
-  }
-  __device__ __forceinline__ float difference(float x, float c) const {
-#pragma clang fp contract(off)
-    const float y = x * (0.25f * c);
-    return 4.f * (y - r);
   }
 };
 
@@ -204,21 +192,19 @@ struct Seen {
 
   template <int N>
   __device__ __forceinline__ void add(const float (&x)[N], float most, float least, float c) {
-    const float quarter = most * (0.25f * c);
-    sums.move_to(fmaxf(sums.r, fabsf(quarter) < WHOLE ? 0.25f * __builtin_rintf(4.f * quarter) : quarter));
-    const float whole = 4.f * sums.r;
+    sums.move_to(fmaxf(sums.m, most), c);
     float s = 0, t = 0;
-    if (ballot(!(fabsf(sums.r) < WHOLE) || __builtin_fmaf(least, c, -whole) == -INFINITY)) {
+    if (ballot((least - sums.m) * c == -INFINITY)) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const float d = sums.difference(x[i], c), e = exp2_fast(d);
+        const float d = (x[i] - sums.m) * c, e = exp2_fast(d);
         s += e;
         t = __builtin_fmaf(e, d == -INFINITY ? 0.f : d, t);       // (nothing times minus infinity)
       }
     } else {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const float d = __builtin_fmaf(x[i], c, -whole), e = exp2_fast(d);
+        const float d = (x[i] - sums.m) * c, e = exp2_fast(d);
         s += e;
         t = __builtin_fmaf(e, d, t);
       }
@@ -292,8 +278,8 @@ struct Seen {
   }
 
   // The lanes' sums become one, in all lanes.
-  __device__ __forceinline__ void sum_over_lanes() {
-    sums.move_to(value_of_key(max_over_wave(key_of(sums.r))));
+  __device__ __forceinline__ void sum_over_lanes(float c) {
+    sums.move_to(value_of_key(max_over_wave(key_of(sums.m))), c);
     sums.s = sum_over_wave(sums.s);
     sums.t = sum_over_wave(sums.t);
   }
@@ -337,11 +323,11 @@ __device__ __forceinline__ void finish_row(const ScoresArgs& a, const Row<L>& ro
   const uint32_t lane = lane_id(), k = a.n_top;
   const Sums& sums = seen.sums;
   const bool nothing = sums.s == 0.f, odd = sums.s != sums.s;
-  const float log_s = __builtin_amdgcn_logf(sums.s), lse = __builtin_fmaf(4.f * LN2, sums.r, LN2 * log_s);
+  const float log_s = __builtin_amdgcn_logf(sums.s), lse = __builtin_fmaf(a.scale, sums.m, LN2 * log_s);
   auto logprob = [&](float v) {
     if (nothing || v == -INFINITY) return -INFINITY;
-    const float d = sums.exponent(v, a.c);
-    return d > -4.f * WHOLE ? fminf(LN2 * (d - log_s), 0.f) : v * a.scale - lse;
+    const float d = (v - sums.m) * a.c;
+    return d > -0x1p22f ? fminf(LN2 * (d - log_s), 0.f) : v * a.scale - lse;
   };
   if (lane == 0 && all) {
     if (given.token >= 0 && static_cast<uint32_t>(given.token) >= a.vocabulary) *a.status = FIKIT_INVALID_ARG;
@@ -463,18 +449,18 @@ __global__ __launch_bounds__(W * WAVE) void k_scores(ScoresArgs a) {
     seen.append(i == 0 && of >= seen.border && of > -INFINITY, of, lane < 8 ? 0 : row.whole + 1, lds);
   }
   if (seen.n > a.n_top) seen.shorten(lds);
-  seen.sum_over_lanes();
-  if (lane == 0) sums[wave] = make_float4(seen.sums.r, seen.sums.s, seen.sums.t, seen.border);
+  seen.sum_over_lanes(a.c);
+  if (lane == 0) sums[wave] = make_float4(seen.sums.m, seen.sums.s, seen.sums.t, seen.border);
   if (lane < a.n_top) firsts[wave * a.n_top + lane] = lane < seen.n ? make_float2(lds->most[lane], __uint_as_float(lds->group[lane])) : make_float2(-INFINITY, 0.f);
   __syncthreads();
   if (wave > 0) return;
   // the first wave joins the sums and the lists
   Seen<L> joined(a.n_top);
-  const float4 of_wave = lane < W ? sums[lane] : make_float4(NO_SUM, 0.f, 0.f, -INFINITY);
+  const float4 of_wave = lane < W ? sums[lane] : make_float4(LOWEST, 0.f, 0.f, -INFINITY);
   joined.sums = Sums{of_wave.x, of_wave.y, of_wave.z};
-  joined.sum_over_lanes();
+  joined.sum_over_lanes(a.c);
   joined.begin_at(of_wave.w);
-  if (a.parts > 1 && lane == 0) a.sums[blockIdx.x] = make_float4(joined.sums.r, joined.sums.s, joined.sums.t, joined.border);
+  if (a.parts > 1 && lane == 0) a.sums[blockIdx.x] = make_float4(joined.sums.m, joined.sums.s, joined.sums.t, joined.border);
   finish_row<L>(a, row, r, given, joined, firsts, W * a.n_top, a.parts == 1, lds);
 }
 
@@ -498,13 +484,13 @@ __global__ __launch_bounds__(JOIN_WAVES * WAVE) void k_scores_join(ScoresArgs a)
   float border = -INFINITY;
   for (uint32_t p = lane; p < a.parts; p += WAVE) {
     const float4 theirs = a.sums[first + p];
-    seen.sums.add(Sums{theirs.x, theirs.y, theirs.z});
+    seen.sums.add(Sums{theirs.x, theirs.y, theirs.z}, a.c);
     border = fmaxf(border, theirs.w);
   }
   if (stop) return;
   const Row<L> row(a, r);
   given.x = given_logit(a, row, given.token);
-  seen.sum_over_lanes();
+  seen.sum_over_lanes(a.c);
   seen.begin_at(border);
   ScoresLds* lds = &lists[wave];
 #pragma unroll

@@ -78,10 +78,11 @@ def compact(table, lengths, block, n_blocks, free):
 class Scores:
     """What fikit_token_scores says about logits [rows, V], in 64 bits, and how far it may be off.
 
-    A term exp(z_j) has the relative error e_j = 2^-22 (1 + |z_j| + |z_j - max z|): the constant scale * log2(e) is rounded twice (2^-23 |z_j|), the
-    difference to the reference once, the exponential is within 2^-23.  Sums: a lane adds up V / 64 terms at most, then 20 steps join lanes, waves and
-    parts, n = (V / 64 + 20) 2^-24 in all.  So the sum's logarithm is off by sum p e + n and its own rounding 2^-22 (1 + |lse|), a log
-    probability by e of its token besides, and the entropy sum p (-log p) by 2 sum p e (1 + |log p|) + 2 n (1 + sum p |z - max z|) + 2^-21 (1 + H)."""
+    A term exp(z_j - max z) has the relative error e_j = 2^-22 (1 + |z_j| + |z_j - max z|) at most: the difference of logits and its product with scale * log2(e),
+    itself rounded twice, are off by 4 * 2^-24 |z_j - max z|, as are the moves of sums from one largest logit to another, which add up to that difference at
+    most; the exponentials of term and moves are within 2^-23 each, of which n below has its share.  Sums: a lane adds up V / 64 terms at most, then 20
+    steps join lanes, waves and parts, n = (V / 64 + 20) 2^-24 in all.  So the sum's logarithm is off by sum p e + n and its own rounding 2^-22 (1 + |lse|),
+    a log probability by e of its token besides, and the entropy sum p (-log p) by 2 sum p e (1 + |log p|) + 2 n (1 + sum p |z - max z|) + 2^-21 (1 + H)."""
 
     def __init__(self, logits, tokens, scale, top):
         x = logits.double().cpu()

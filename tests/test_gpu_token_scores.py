@@ -126,9 +126,19 @@ def test_one_token_holds_all():
     x = torch.zeros(3, 5001, device=DEV)
     x[0, 17], x[1, 5000], x[2, 0] = 200.0, 1e5, 30.0
     got = check(x, torch.tensor([17, 5000, 0], dtype=torch.int32, device=DEV), 2)
-    # The reference is the nearest whole number, so |d| <= 1/2 of the one that counts, S = 2^d (1 + 2^-23) and log2 S = d + 1.45 * 2^-23 + 2^-24 (its own
-    # rounding): entropy and log probability, ln 2 times what that differs from T / S = d (1 + 2^-24) and from d, are within 2^-22 of zero.
-    assert 0 <= float(got.entropy[0]) <= 2.0 ** -22 and -2.0 ** -22 <= float(got.logprob[0]) <= 0 and bool((got.logprob <= 0).all())
+    assert bool((got.entropy[:2] == 0).all()) and bool((got.logprob[:2] == 0).all()) and bool((got.logprob <= 0).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_one_token_is_left(dtype):
+    """Its log probability is 0, and so is the entropy, to the bit, whatever the logit."""
+    for v in (1, 5, 3000, 70001):
+        x = torch.full((40, v), -math.inf)
+        at = torch.arange(40) * 1237 % v
+        x[torch.arange(40), at] = normal(v, 40) * torch.logspace(-3, 3, 40)
+        for scale in (1.0, 0.7, 3.0):
+            got = check(x.to(dtype).to(DEV), at.to(torch.int32).to(DEV), 3, scale)
+            assert not bool(got.entropy.any()) and not bool(got.logprob.any()) and not bool(got.top_logprob[:, 0].any())
 
 
 @pytest.mark.parametrize("rows, v, dtype", [(70000, 13, torch.float32), (3000, 1000, torch.bfloat16), (600, 8192, torch.float16), (130, 50000, torch.bfloat16), (3, 1 << 20, torch.float16),
