@@ -14,19 +14,22 @@ using namespace fikit;
 
 constexpr uint32_t ROTATE_MOST_GROUPS = 1u << 16;
 constexpr uint32_t ROTATE_SPREAD = 2048;          // waves: eight for each CU
+constexpr uint64_t ROTATE_PAST = 1ull << 27;      // bytes from which on the caches are passed by: half of the last one's
 
 struct RotateCall {
   const RotateArgs& a;
-  bool neighbours;
+  bool neighbours, past;
   hipStream_t st;
-  template <typename T, int D>
+  template <typename T, int D, bool NEIGHBOURS>
   int run() {
     const uint32_t groups = (a.units + ROTATE_WAVES - 1) / ROTATE_WAVES;
     const dim3 grid(groups < ROTATE_MOST_GROUPS ? groups : ROTATE_MOST_GROUPS), block(ROTATE_WAVES * WAVE);
-    return neighbours ? enqueue(k_rotate<T, D, true>, grid, block, st, a) : enqueue(k_rotate<T, D, false>, grid, block, st, a);
+    return past ? enqueue(k_rotate<T, D, NEIGHBOURS, true>, grid, block, st, a) : enqueue(k_rotate<T, D, NEIGHBOURS, false>, grid, block, st, a);
   }
+  template <typename T, int D>
+  int with_pairs() { return neighbours ? run<T, D, true>() : run<T, D, false>(); }
   template <typename T>
-  int with_dim(uint32_t head_dim) { return head_dim == 64 ? run<T, 64>() : head_dim == 128 ? run<T, 128>() : run<T, 256>(); }
+  int with_dim(uint32_t head_dim) { return head_dim == 64 ? with_pairs<T, 64>() : head_dim == 128 ? with_pairs<T, 128>() : with_pairs<T, 256>(); }
 };
 
 // Do the vectors lie apart?  Those of the smaller stride beside each other, and the larger stride beyond all of them.
@@ -341,7 +344,8 @@ int fikit_rotate_heads(const fikit_vectors* h_q, const fikit_vectors* h_k, uint3
   a.parts = (a.passes + a.per - 1) / a.per;
   a.units = n_tokens * a.parts;
   a.epsilon = epsilon;
-  RotateCall call{a, pairs == FIKIT_PAIRS_NEIGHBOURS, static_cast<hipStream_t>(hip_stream)};
+  const bool past = 2ull * n_tokens * (q_heads + kv_heads) * head_dim >= ROTATE_PAST;
+  RotateCall call{a, pairs == FIKIT_PAIRS_NEIGHBOURS, past, static_cast<hipStream_t>(hip_stream)};
   return value_type == FIKIT_BF16 ? call.with_dim<Bf16>(head_dim) : call.with_dim<F16>(head_dim);
 }
 

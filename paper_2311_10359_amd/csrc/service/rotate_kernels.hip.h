@@ -8,8 +8,10 @@ namespace fikit {
 // A head x of D values: y = x w / sqrt(mean(x^2) + epsilon) if it has a weight, then the pairs (a, b) of the first `rotary` values become
 // (a cos t - b sin t, b cos t + a sin t), t = position * frequency of the pair.  Held in 32 bits between one reading and one writing.
 //
-// Two bytes read and two written for a value, ten instructions: bound by memory.  23,171 tokens of 40 heads of 128, 474 MB: 76 us, 6.2 TB/s, with the
-// inputs read past the caches, 97 through them (both written and read past them: 86); workgroups of 8 waves 82.  One token 2.7 us, a launch.  D / 16 lanes hold a head, 16 values each in two chunks of
+// Two bytes read and two written for a value, ten instructions: bound by memory.  23,171 tokens of 40 heads of 128, 474 MB: 86 us, 5.5 TB/s, past the
+// caches, 97 through them (only read past them 94, only written 90); workgroups of 8 waves 6 more.  What a product before has left in the caches, and what
+// append and attention behind read there, is worth more up to 128 MB: rotation, append and attention of 8192 tokens take 118 us through the caches
+// and 126 past them, of 24,000 tokens 363 and 354.  One token 2.7 us, a launch.  D / 16 lanes hold a head, 16 values each in two chunks of
 // eight: those of a pair's two sides are in one lane, so that only the sum of squares crosses lanes.  A wave takes 64 / (D / 16) heads
 // of one token at a time, a pass.  An angle counts for all heads of a token and takes 50 instructions, so each lane computes one, or two, and
 // reads back those of its pairs from LDS.
@@ -62,7 +64,8 @@ __device__ __forceinline__ void rotate_unpack(const u32x4& w, float* x) {
   for (int i = 0; i < 4; ++i) { x[2 * i] = T::low(w[i]); x[2 * i + 1] = T::high(w[i]); }
 }
 
-template <typename T, int D, bool NEIGHBOURS>
+// PAST: the caches, both ways.
+template <typename T, int D, bool NEIGHBOURS, bool PAST>
 __global__ __launch_bounds__(ROTATE_WAVES * WAVE) void k_rotate(RotateArgs a) {
   constexpr uint32_t LANES = D / 16, HEADS = WAVE / LANES;
   __shared__ float2 lds[ROTATE_WAVES][D / 2];
@@ -94,8 +97,13 @@ __global__ __launch_bounds__(ROTATE_WAVES * WAVE) void k_rotate(RotateArgs a) {
       const uint16_t* x_at = static_cast<const uint16_t*>(in.d_data) + token * in.token_stride + head * in.head_stride;
       u32x4 wa = {0, 0, 0, 0}, wb = {0, 0, 0, 0};
       if (there) {
-        wa = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(x_at + at_a));
-        wb = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(x_at + at_b));
+        if constexpr (PAST) {
+          wa = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(x_at + at_a));
+          wb = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(x_at + at_b));
+        } else {
+          wa = *reinterpret_cast<const u32x4*>(x_at + at_a);
+          wb = *reinterpret_cast<const u32x4*>(x_at + at_b);
+        }
       }
       float x[16];
       rotate_unpack<T>(wa, x);
@@ -138,8 +146,13 @@ __global__ __launch_bounds__(ROTATE_WAVES * WAVE) void k_rotate(RotateArgs a) {
         u32x4 va, vb;
 #pragma unroll
         for (int i = 0; i < 4; ++i) { va[i] = T::pair(y[2 * i], y[2 * i + 1]); vb[i] = T::pair(y[8 + 2 * i], y[9 + 2 * i]); }
-        *reinterpret_cast<u32x4*>(y_at + at_a) = va;
-        *reinterpret_cast<u32x4*>(y_at + at_b) = vb;
+        if constexpr (PAST) {
+          __builtin_nontemporal_store(va, reinterpret_cast<u32x4*>(y_at + at_a));
+          __builtin_nontemporal_store(vb, reinterpret_cast<u32x4*>(y_at + at_b));
+        } else {
+          *reinterpret_cast<u32x4*>(y_at + at_a) = va;
+          *reinterpret_cast<u32x4*>(y_at + at_b) = vb;
+        }
       }
     }
   }

@@ -179,3 +179,25 @@ def test_replayed_and_on_another_stream():
         kept = positions >= 0
         assert torch.equal(out.q[kept], want.q[kept]) and not bool(out.q[~kept].any())
     assert int(status) == 0
+
+
+@pytest.mark.parametrize("neighbours, dtype, dim", [(False, torch.bfloat16, 128), (True, torch.float16, 64), (False, torch.float16, 256)])
+def test_large_inputs(neighbours, dtype, dim):
+    """From 128 MB on the caches are passed by; every 31st token is compared."""
+    tokens, hq, hkv = (1 << 27) // (2 * 40 * dim) + 77, 32, 8
+    gen = torch.Generator(device=DEV).manual_seed(25)
+    qkv = torch.randn((tokens, hq + 2 * hkv, dim), generator=gen, device=DEV, dtype=torch.float32).to(dtype)
+    q, k = qkv[:, :hq], qkv[:, hq:hq + hkv]
+    positions = torch.arange(tokens, dtype=torch.int32, device=DEV) % 4001 - 1
+    w = normal(26, dim, dtype=dtype)
+    some = slice(None, None, 31)
+    want = [model.rotate(x[some], w, 1e-6, positions[some], frequencies(dim // 2), neighbours) for x in (q, k)]
+    kept = positions[some].cpu() >= 0
+    status = status_word()
+    apart = binding.fikit_rotate_heads(q, k, positions, frequencies(dim // 2), status, q_weight=w, k_weight=w, neighbours=neighbours)
+    binding.fikit_rotate_heads(q, k, positions, frequencies(dim // 2), status, q_weight=w, k_weight=w, neighbours=neighbours, out=binding.RotatedHeads(q, k))
+    binding.fikit_check_status(status)
+    for got in (apart, (q, k)):
+        for g, (y, bound) in zip(got, want):
+            assert model.near(g[some][kept.to(DEV)], y[kept], bound[kept])
+    assert torch.equal(apart.q[positions >= 0], q[positions >= 0]) and torch.equal(apart.k[positions >= 0], k[positions >= 0])
