@@ -148,7 +148,7 @@ ScoresCut scores_cut(uint32_t n_rows, uint32_t vocabulary, int32_t value_type, u
   if (c.parts == 1) return c;
   const uint64_t lists = static_cast<uint64_t>(n_rows) * c.parts;
   c.sums_bytes = (lists * sizeof(float4) + 255) / 256 * 256;
-  c.bytes = c.sums_bytes + (lists * n_top * sizeof(float2) + 255) / 256 * 256;
+  c.bytes = c.sums_bytes + (n_top > 0 ? lists * SCORES_MOST * sizeof(float2) : 0);
   return c;
 }
 

@@ -33,7 +33,7 @@ struct ScoresArgs {
   float* top_logprob;
   int32_t* status;
   float4* sums;             // workspace: [rows][parts] m, S, T and the border
-  float2* lists;            // [rows][parts][n_top] maxima and groups, minus infinity where there is none
+  float2* lists;            // [rows][parts][SCORES_MOST] maxima and groups, minus infinity where there is none
   uint32_t rows, vocabulary, n_top, parts, per_part;      // per_part: groups
   float scale, c;           // c = scale log2(e)
 };
@@ -226,16 +226,29 @@ struct Seen {
     lds_in_order();
   }
 
-  // Takes from a list in LDS the first k that reach the border.  (In one loop, as elsewhere here: code that a wave runs once costs it more to fetch
-  // than to run.)
-  __device__ __forceinline__ void take(const float2* from, uint32_t count, ScoresLds* lds) {
-#pragma unroll 1
-    for (uint32_t at = 0;; at += WAVE) {
-      if (n > (at < count ? WAVE : k)) shorten(lds);
-      if (at >= count) break;
-      const float2 of = at + lane_id() < count ? from[at + lane_id()] : make_float2(-INFINITY, 0.f);
-      append(of.x >= border && of.x > -INFINITY, of.x, __float_as_uint(of.y), lds);
+  // Takes from a list of up to JOIN_ROOM in LDS what can be of the first k, and no more than `room`.  (In loops, as elsewhere here: code that a wave
+  // runs once costs it more to fetch than to run.)
+  __device__ __forceinline__ void take(const float2* from, uint32_t count, bool look, uint32_t room, ScoresLds* lds) {
+    constexpr uint32_t N = JOIN_ROOM / WAVE;
+    const uint32_t lane = lane_id();
+    float of[N], all = -INFINITY;
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i) {
+      of[i] = i * WAVE + lane < count ? from[i * WAVE + lane].x : -INFINITY;
+      all = fmaxf(all, of[i]);
     }
+    if (look) begin(all);
+    uint32_t hits = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i) hits |= of[i] >= border && of[i] > -INFINITY ? 1u << i : 0;
+#pragma unroll 1
+    while (ballot(hits)) {
+      const float2 one = hits ? from[(__ffs(static_cast<int>(hits)) - 1) * WAVE + lane] : make_float2(-INFINITY, 0.f);
+      append(hits && one.x >= border, one.x, __float_as_uint(one.y), lds);
+      hits &= hits - 1;
+      if (n > WAVE) shorten(lds);
+    }
+    if (n > room) shorten(lds);
   }
 
   // The first k stay, of more.  (n is up to SCORES_ROOM)
@@ -263,13 +276,13 @@ struct Seen {
     border = value_of_key(max_u32(reached, LOWEST_KEY));
   }
 
-  // The first batch: the k-th largest of the lanes' maxima is a border for it, and no list of 64 groups in front of it has to be shortened.
+  // The k-th largest of the lanes' maxima is a border for what they have, of which not much more than k is left then.
   __device__ __forceinline__ void begin(float most) {
     const uint32_t keys[1] = {most > -INFINITY ? key_of(most) : 0};
     if (popc64(ballot(keys[0] != 0)) <= k) return;
     const uint32_t least = ~max_over_wave(keys[0] ? ~keys[0] : 0);
     const uint32_t reached = reached_by<L::KEY_BITS, 1>(keys, k, least);
-    if (reached > LOWEST_KEY) border = value_of_key(reached - (reached == 0x80000000u ? 2 : 1));         // (there is no key of -0)
+    if (reached > LOWEST_KEY) border = fmaxf(border, value_of_key(reached - (reached == 0x80000000u ? 2 : 1)));         // (there is no key of -0)
   }
 
   // Lists of others: k groups of each reach its border.
@@ -338,7 +351,7 @@ __device__ __forceinline__ void finish_row(const ScoresArgs& a, const Row<L>& ro
   if (k == 0) return;
 #pragma unroll 1
   for (bool logits = false;; logits = true) {
-    seen.take(from, count, lds);
+    seen.take(from, count, !logits, logits ? WAVE : SCORES_MOST, lds);
     if (logits || !all) break;
     // the groups' logits, of which those that reach the groups' border can be of the k
     constexpr int N = SCORES_MOST * L::VEC / WAVE;
@@ -358,25 +371,24 @@ __device__ __forceinline__ void finish_row(const ScoresArgs& a, const Row<L>& ro
     lds_in_order();
   }
   const uint32_t n = seen.n;
+  const float mine = lane < n ? lds->most[lane] : -INFINITY;
+  const uint32_t which = lane < n ? lds->group[lane] : 0;
   if (!all) {
-    if (lane < k)
-      a.lists[static_cast<uint64_t>(blockIdx.x) * k + lane] = lane < n ? make_float2(lds->most[lane], __uint_as_float(lds->group[lane])) : make_float2(-INFINITY, 0.f);
+    if (lane < SCORES_MOST) a.lists[static_cast<uint64_t>(blockIdx.x) * SCORES_MOST + lane] = make_float2(mine, __uint_as_float(which));
     return;
+  }
+  uint32_t rank = 0;                           // of up to 64
+  for (uint32_t i = 0; i < n; ++i) {
+    const float other = __uint_as_float(read_lane_u32(__float_as_uint(mine), i));
+    rank += other > mine || (other == mine && read_lane_u32(which, i) < which);
   }
   const uint64_t out = static_cast<uint64_t>(r) * k;
   if (lane < k && (lane >= n || odd)) {
     a.top_tokens[out + lane] = -1;
     a.top_logprob[out + lane] = odd ? NAN : -INFINITY;
   }
-  if (lane >= n || odd) return;
-  const float mine = lds->most[lane];
-  const uint32_t token = lds->group[lane];
-  uint32_t rank = 0;
-  for (uint32_t i = 0; i < n; ++i) {
-    const float other = lds->most[i];
-    rank += other > mine || (other == mine && lds->group[i] < token);
-  }
-  a.top_tokens[out + rank] = static_cast<int32_t>(token);
+  if (lane >= n || rank >= k || odd) return;
+  a.top_tokens[out + rank] = static_cast<int32_t>(which);
   a.top_logprob[out + rank] = logprob(mine);
 }
 
@@ -448,10 +460,10 @@ __global__ __launch_bounds__(W * WAVE) void k_scores(ScoresArgs a) {
     const float of = value_of_key(most);
     seen.append(i == 0 && of >= seen.border && of > -INFINITY, of, lane < 8 ? 0 : row.whole + 1, lds);
   }
-  if (seen.n > a.n_top) seen.shorten(lds);
+  if (seen.n > SCORES_MOST) seen.shorten(lds);
   seen.sum_over_lanes(a.c);
   if (lane == 0) sums[wave] = make_float4(seen.sums.m, seen.sums.s, seen.sums.t, seen.border);
-  if (lane < a.n_top) firsts[wave * a.n_top + lane] = lane < seen.n ? make_float2(lds->most[lane], __uint_as_float(lds->group[lane])) : make_float2(-INFINITY, 0.f);
+  if (lane < SCORES_MOST) firsts[wave * SCORES_MOST + lane] = lane < seen.n ? make_float2(lds->most[lane], __uint_as_float(lds->group[lane])) : make_float2(-INFINITY, 0.f);
   __syncthreads();
   if (wave > 0) return;
   // the first wave joins the sums and the lists
@@ -461,7 +473,7 @@ __global__ __launch_bounds__(W * WAVE) void k_scores(ScoresArgs a) {
   joined.sum_over_lanes(a.c);
   joined.begin_at(of_wave.w);
   if (a.parts > 1 && lane == 0) a.sums[blockIdx.x] = make_float4(joined.sums.m, joined.sums.s, joined.sums.t, joined.border);
-  finish_row<L>(a, row, r, given, joined, firsts, W * a.n_top, a.parts == 1, lds);
+  finish_row<L>(a, row, r, given, joined, firsts, W * SCORES_MOST, a.parts == 1, lds);
 }
 
 // Joins a row's parts: a wave each.
@@ -473,9 +485,9 @@ __global__ __launch_bounds__(JOIN_WAVES * WAVE) void k_scores_join(ScoresArgs a)
   if (r >= a.rows) return;
   const bool stop = stopped(a.status);
   const uint64_t first = static_cast<uint64_t>(r) * a.parts;
-  const uint32_t n = a.parts * a.n_top;
-  const float2* entries = a.lists + first * a.n_top;
-  constexpr uint32_t AHEAD = 4;                // loads that wait for nothing
+  const uint32_t n = a.n_top ? a.parts * SCORES_MOST : 0;
+  const float2* entries = a.lists + first * SCORES_MOST;
+  constexpr uint32_t AHEAD = JOIN_ROOM / WAVE;  // loads that wait for nothing
   float2 of[AHEAD];
 #pragma unroll
   for (uint32_t i = 0; i < AHEAD; ++i) of[i] = i * WAVE + lane < n ? entries[i * WAVE + lane] : make_float2(-INFINITY, 0.f);
@@ -495,10 +507,10 @@ __global__ __launch_bounds__(JOIN_WAVES * WAVE) void k_scores_join(ScoresArgs a)
   ScoresLds* lds = &lists[wave];
 #pragma unroll
   for (uint32_t i = 0; i < AHEAD; ++i) firsts[wave][i * WAVE + lane] = of[i];
-  uint32_t at = 0, count = min_u32(n, AHEAD * WAVE);
+  uint32_t at = 0, count = min_u32(n, JOIN_ROOM);
   lds_in_order();
-  while (at + count < n) {                     // (more lists than there is room for: those so far become one)
-    seen.take(firsts[wave], count, lds);
+  while (at + count < n) {                     // more lists than there is room for: those so far become one, which stays
+    seen.take(firsts[wave], count, true, SCORES_MOST, lds);
     at += count;
     count = min_u32(n - at, JOIN_ROOM);
     for (uint32_t e = lane; e < count; e += WAVE) firsts[wave][e] = entries[at + e];

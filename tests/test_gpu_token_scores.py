@@ -48,7 +48,7 @@ def test_vocabularies(v, dtype):
 
 @pytest.mark.parametrize("dtype", TYPES)
 def test_equal_values(dtype):
-    for v in (5, 33, 100, 700, 5000, 33333):
+    for v in (5, 33, 100, 700, 5000, 33333, 300_011):
         for seed, few in enumerate(([0.0], [0.0, -0.0], [1.0, 2.0], [-1.0, -2.0, -0.0, 0.0], [-float("inf"), 3.0])):
             pick = torch.randint(0, len(few), (6, v), generator=torch.Generator().manual_seed(seed + v))
             x = torch.tensor(few)[pick].to(dtype).to(DEV)
@@ -59,7 +59,7 @@ def test_equal_values(dtype):
 @pytest.mark.parametrize("dtype", TYPES)
 def test_orders(dtype):
     """Ascending, descending, periodic and lone large values at every kind of place."""
-    for v in (600, 20000, 40007):
+    for v in (600, 20000, 40007, 500_003):
         up = torch.linspace(-20, 20, v)
         x = torch.stack([up, up.flip(0), torch.arange(v) % 512 / 16.0, torch.arange(v) % 8 / 1.0, torch.arange(v) % 4096 * 1.0 / 256, torch.where(torch.arange(v) < 40, 9.0, -9.0),
                          torch.where(torch.arange(v) >= v - 40, 9.0, -9.0)])
