@@ -146,8 +146,8 @@ class Service:
         return logits
 
     def tokens(self, tokens: torch.Tensor) -> torch.Tensor:
-        """What goes in for tokens: [n, hidden]."""
-        return self.w_tokens.t()[tokens.long()] * math.sqrt(self.sizes.hidden)
+        """What goes in for tokens, [n, hidden]: of a size that leaves the next token open."""
+        return self.w_tokens.t()[tokens.long()] * 4
 
     def score(self, record, logits: torch.Tensor, n_top: int, tokens: Optional[torch.Tensor] = None) -> binding.TokenScores:
         return record("score", (logits.shape[0], 1, 1), binding.fikit_token_scores, logits, tokens, self.status, n_top=n_top)

@@ -85,13 +85,14 @@ def test_beams_hold_what_their_parents_put_into_the_cache():
             assert around_model.near(x1, want, bound)
     assert watch.rotated[0][2].tolist() == [i for n in lengths for i in range(n)]
     assert watch.rotated[-1][2].tolist() == [n + steps - 1 for n in lengths for _ in range(width)]
-    # scores, and the sums of the beams that were kept: descending, and a parent's sum and an alternative's each
+    # scores, and the sums of the beams that were kept: descending, and none grows (a probability of 1 - 2^-25 and more has a logarithm of 0 in 32 bits,
+    # so the best one may also stay as it was)
     for logits, got in watch.scored:
         scores = around_model.Scores(logits, None, 1.0, width)
         del scores.want["entropy"], scores.want["lse"]
         assert scores.differs(got) == []
     sums = beams.logprob.reshape(3, width)
-    assert bool((sums[:, 1:] <= sums[:, :-1]).all()) and bool((sums[:, 0].cpu() < totals.reshape(3, width)[:, 0]).all())
+    assert bool((sums[:, 1:] <= sums[:, :-1]).all()) and bool((sums[:, 0].cpu() <= totals.reshape(3, width)[:, 0]).all())
 
 
 def test_a_compaction_moves_blocks_and_changes_no_attention():
