@@ -107,10 +107,10 @@ __device__ __forceinline__ uint32_t reached_by(const uint32_t (&keys)[N], uint32
 }
 
 // Which of the keys are the first k: the larger ones, and of those equal to the k-th largest the ones of the lowest `order`, which is different for
-// each.  Their places in turn.  Returns a key that all of them reach.
+// each.  Their places in turn.  Returns a key that all of them reach; of those equal to it none of an order of `limit` or more is one of the k.
 template <int BITS, int N>
 __device__ __forceinline__ uint32_t first_of(const uint32_t (&keys)[N], const uint32_t (&order)[N], uint32_t k, uint32_t least, bool (&keep)[N],
-                                             uint32_t (&place)[N]) {
+                                             uint32_t (&place)[N], uint32_t* limit) {
   const uint32_t border = reached_by<BITS, N>(keys, k, least);
   uint32_t reached = 0;
 #pragma unroll
@@ -118,14 +118,29 @@ __device__ __forceinline__ uint32_t first_of(const uint32_t (&keys)[N], const ui
     keep[i] = keys[i] >= border;
     reached += popc64(ballot(keep[i]));
   }
-  if (reached > k) {                           // some are equal: one after the other, of the highest order first, goes
+  *limit = ~0u;
+  if (reached > k) {                           // some are equal to the k-th
     const uint32_t largest_equal = border | (BITS < 32 ? (1u << (32 - BITS) % 32) - 1 : 0);
+    if (reached > k + 16) {                    // many: the order of those that stay, from the largest ~order on
+      uint32_t equal[N], larger = 0;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        equal[i] = keep[i] && keys[i] <= largest_equal ? ~order[i] : 0;
+        larger += popc64(ballot(keys[i] > largest_equal));
+      }
+      const uint32_t last = reached_by<32, N>(equal, k - larger, 0);
+#pragma unroll
+      for (int i = 0; i < N; ++i) keep[i] = keep[i] && (keys[i] > largest_equal || ~order[i] >= last);
+      reached = k;
+      *limit = ~last;
+    }
 #pragma unroll 1
-    for (; reached > k; --reached) {
+    for (; reached > k; --reached) {           // few: one after the other, of the highest order first, goes
       uint32_t last = 0;
 #pragma unroll
       for (int i = 0; i < N; ++i) last = max_u32(last, keep[i] && keys[i] <= largest_equal ? order[i] + 1 : 0);
       last = max_over_wave(last);
+      *limit = last - 1;
 #pragma unroll
       for (int i = 0; i < N; ++i) keep[i] = keep[i] && (keys[i] > largest_equal || order[i] + 1 != last);
     }
@@ -187,6 +202,7 @@ struct Seen {
   Sums sums;                               // of each lane
   uint32_t n = 0, k;                       // groups in the list; how many are wanted
   float border;                            // only groups that reach it are; none reaches NaN
+  uint32_t limit = ~0u;                    // ... and if they are only as large, come before this
 
   __device__ __forceinline__ explicit Seen(uint32_t n_top) : k(n_top), border(n_top ? -INFINITY : NAN) {}
 
@@ -212,6 +228,8 @@ struct Seen {
     sums.s += s;
     sums.t += t;
   }
+
+  __device__ __forceinline__ bool may_be(float most, uint32_t group) const { return most > border || (most == border && group < limit); }
 
   // Groups, one to a lane, of which some join the list.  (It has room for 64 more.)
   __device__ __forceinline__ void append(bool hit, float most, uint32_t group, ScoresLds* lds) {
@@ -244,7 +262,7 @@ struct Seen {
 #pragma unroll 1
     while (ballot(hits)) {
       const float2 one = hits ? from[(__ffs(static_cast<int>(hits)) - 1) * WAVE + lane] : make_float2(-INFINITY, 0.f);
-      append(hits && one.x >= border, one.x, __float_as_uint(one.y), lds);
+      append(hits && may_be(one.x, __float_as_uint(one.y)), one.x, __float_as_uint(one.y), lds);
       hits &= hits - 1;
       if (n > WAVE) shorten(lds);
     }
@@ -264,7 +282,7 @@ struct Seen {
       groups[i] = lds->group[lane + i * WAVE];
     }
     lds_in_order();
-    const uint32_t reached = first_of<L::KEY_BITS, N>(keys, groups, k, key_of(border), keep, place);
+    const uint32_t reached = first_of<L::KEY_BITS, N>(keys, groups, k, key_of(border), keep, place, &limit);
 #pragma unroll
     for (int i = 0; i < N; ++i)
       if (keep[i]) {
@@ -273,7 +291,9 @@ struct Seen {
       }
     lds_in_order();
     n = k;
-    border = value_of_key(max_u32(reached, LOWEST_KEY));
+    // (of negative values the bits that do not differ are ones)
+    constexpr uint32_t LOW = L::KEY_BITS < 32 ? (1u << (32 - L::KEY_BITS) % 32) - 1 : 0;
+    border = value_of_key(reached >> 31 ? reached : max_u32(reached | LOW, LOWEST_KEY));
   }
 
   // The k-th largest of the lanes' maxima is a border for what they have, of which not much more than k is left then.
@@ -282,7 +302,12 @@ struct Seen {
     if (popc64(ballot(keys[0] != 0)) <= k) return;
     const uint32_t least = ~max_over_wave(keys[0] ? ~keys[0] : 0);
     const uint32_t reached = reached_by<L::KEY_BITS, 1>(keys, k, least);
-    if (reached > LOWEST_KEY) border = fmaxf(border, value_of_key(reached - (reached == 0x80000000u ? 2 : 1)));         // (there is no key of -0)
+    if (reached <= LOWEST_KEY) return;
+    const float below = value_of_key(reached - (reached == 0x80000000u ? 2 : 1));         // (there is no key of -0)
+    if (below > border) {
+      border = below;
+      limit = ~0u;
+    }
   }
 
   // Lists of others: k groups of each reach its border.
@@ -368,6 +393,7 @@ __device__ __forceinline__ void finish_row(const ScoresArgs& a, const Row<L>& ro
 #pragma unroll
     for (int i = 0; i < N; ++i) from[lane + i * WAVE] = make_float2(x[i], __uint_as_float(at[i]));
     seen.n = 0;
+    seen.limit = ~0u;                          // (of groups)
     lds_in_order();
   }
   const uint32_t n = seen.n;
@@ -441,7 +467,7 @@ __global__ __launch_bounds__(W * WAVE) void k_scores(ScoresArgs a) {
       float of = most[0];
 #pragma unroll
       for (uint32_t j = 1; j < SCORES_BATCH; ++j) of = i == j ? most[j] : of;
-      seen.append(hits && of >= seen.border, of, 1 + mine + i * WAVE, lds);
+      seen.append(hits && seen.may_be(of, 1 + mine + i * WAVE), of, 1 + mine + i * WAVE, lds);
       hits &= hits - 1;
       if (seen.n > WAVE) seen.shorten(lds);
     }
@@ -458,7 +484,8 @@ __global__ __launch_bounds__(W * WAVE) void k_scores(ScoresArgs a) {
     most = max_u32(most, dpp_move<0x4E>(most));
     most = max_u32(most, dpp_move<0x141>(most));
     const float of = value_of_key(most);
-    seen.append(i == 0 && of >= seen.border && of > -INFINITY, of, lane < 8 ? 0 : row.whole + 1, lds);
+    const uint32_t group = lane < 8 ? 0 : row.whole + 1;
+    seen.append(i == 0 && seen.may_be(of, group) && of > -INFINITY, of, group, lds);
   }
   if (seen.n > SCORES_MOST) seen.shorten(lds);
   seen.sum_over_lanes(a.c);

@@ -87,13 +87,15 @@ def test_masks(left, dtype):
 
 @pytest.mark.parametrize("dtype", TYPES)
 def test_lowest_values_as_masks(dtype):
-    """The type's lowest value in masked places, in place of minus infinity."""
-    lowest = torch.finfo(dtype).min
-    for v in (40, 9000):
-        x = normal(5, 6, v).to(dtype)
-        x[0], x[1, 3:], x[2, ::2], x[3, :-1] = lowest, lowest, lowest, lowest
-        for scale in (2.0 ** -10, 0.7, 1.0):
-            check(x.to(DEV), tokens_for(4, 6, v), 12, scale)
+    """The type's lowest value in masked places, or another large one, in place of minus infinity; alternatives among equal ones too."""
+    for lowest in (torch.finfo(dtype).min, -30000.0):
+        for v in (40, 9000, 300_011):
+            x = normal(5, 6, v).to(dtype)
+            x[0], x[1, 3:], x[2, ::2], x[3, :-1] = lowest, lowest, lowest, lowest
+            x[4, torch.arange(v) % 1999 != 7] = lowest
+            for scale in (2.0 ** -10, 0.7, 1.0):
+                check(x.to(DEV), tokens_for(4, 6, v), 12, scale)
+            check(x.to(DEV), tokens_for(4, 6, v), 32)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
