@@ -127,18 +127,19 @@ struct ScoresCut {
   uint64_t sums_bytes, bytes;
 };
 // A row is one wave's where that takes it in a turn, or in four and there are many (20,000 rows of 1000 bfloat16 logits 40 us, 4 waves 67; 8000 rows of
-// 8192 37 and 42).  It is one workgroup's where that takes it in one turn, of 4 waves or of 16 (one row of 32,000 bfloat16 logits 9.3 us; 10.9 in parts that a second
-// launch joins), and from 128 rows on, of 16 waves up to 1023 rows (256 rows of 50,001 float32 16.0 us; 4 waves 21) and of 4 beyond (1100 rows of
-// 131,072 bfloat16 59.8; 16 waves 72.5).  Else rows are cut into parts of 4 waves, for two workgroups on a compute unit: one compute unit takes 2 us to read
-// what 16 waves want first (one row of 131,072 logits 15.9 us; in parts of 16 waves 17.1, 64 such rows 19.5 and 20.5).
-constexpr uint32_t SCORES_CHIP = 256, SCORES_MANY = 1024;
+// 8192 37 and 42).  It is one workgroup's where that takes it in one turn, of 4 waves or of 16 (one row of 32,000 bfloat16 logits 9.3 us; 10.9 in parts that
+// a second launch joins), and from 128 rows on, of as many waves as the chip holds for so many rows: 16 up to 511 (256 rows of 50,001 float32 15 us, 4 waves
+// 21; 300 rows of 131,072 bfloat16 32, 8 waves 34), 8 up to 1023 (700 such rows 43, 16 waves 48, 4 waves 46), 4 beyond (1100 rows 60, 8 waves 65, 16 waves 72).
+// Else rows are cut into parts of 4 waves, for two workgroups on a compute unit: one compute unit takes 2 us to read what 16 waves want first (one row of
+// 131,072 logits 15.9 us, in parts of 16 waves 17.1, when that was measured; 64 such rows 19.5 and 20.5).
+constexpr uint32_t SCORES_CHIP = 256, SCORES_MORE = 512, SCORES_MANY = 1024;
 
 ScoresCut scores_cut(uint32_t n_rows, uint32_t vocabulary, int32_t value_type, uint32_t n_top) {
   ScoresCut c{};
   const uint32_t groups = vocabulary / (value_type == FIKIT_F32 ? LogitsF32::VEC : LogitsBf16::VEC), turn = SCORES_BATCH * WAVE;
   const bool few = n_rows < SCORES_CHIP / 2;
   const bool one_wave = groups <= turn || (n_rows >= 2 * SCORES_MANY && groups <= 4 * turn);
-  c.waves = one_wave ? 1 : groups <= 4 * turn || n_rows >= SCORES_MANY || (few && groups > 16 * turn) ? 4 : 16;
+  c.waves = one_wave ? 1 : groups <= 4 * turn || n_rows >= SCORES_MANY || (few && groups > 16 * turn) ? 4 : n_rows >= SCORES_MORE ? 8 : 16;
   const uint32_t most = (groups + c.waves * turn - 1) / (c.waves * turn), want = n_rows > 0 && few && c.waves == 4 ? 2 * SCORES_CHIP / n_rows : 1;
   c.parts = want < most ? want : most;
   if (c.parts < 1) c.parts = 1;
@@ -160,6 +161,7 @@ struct ScoresCall {
   int run() {
     const dim3 grid(a.rows * a.parts), block(waves * WAVE), join(JOIN_WAVES * WAVE);
     if (int rc = waves == 16  ? enqueue(k_scores<L, 16>, grid, block, st, a)
+                 : waves == 8 ? enqueue(k_scores<L, 8>, grid, block, st, a)
                  : waves == 4 ? enqueue(k_scores<L, 4>, grid, block, st, a)
                               : enqueue(k_scores<L, 1>, grid, block, st, a))
       return rc;

@@ -143,7 +143,7 @@ def test_one_token_is_left(dtype):
             assert not bool(got.entropy.any()) and not bool(got.logprob.any()) and not bool(got.top_logprob[:, 0].any())
 
 
-@pytest.mark.parametrize("rows, v, dtype", [(70000, 13, torch.float32), (3000, 1000, torch.bfloat16), (600, 8192, torch.float16), (130, 50000, torch.bfloat16), (3, 1 << 20, torch.float16),
+@pytest.mark.parametrize("rows, v, dtype", [(70000, 13, torch.float32), (3000, 1000, torch.bfloat16), (600, 8192, torch.float16), (600, 9001, torch.float16), (1023, 30011, torch.float32), (130, 50000, torch.bfloat16), (3, 1 << 20, torch.float16),
                                             (1, 2_000_003, torch.float32), (2, 300_001, torch.bfloat16), (511, 20001, torch.bfloat16), (513, 20001, torch.bfloat16), (1500, 20001, torch.bfloat16),
                                             (2100, 8001, torch.bfloat16), (2100, 4001, torch.float32)])
 def test_rows(rows, v, dtype):
