@@ -54,8 +54,8 @@ __device__ __forceinline__ void clear_flags(const BlocksArgs& a, uint32_t from, 
     reinterpret_cast<u32x4*>(a.flags)[i] = reinterpret_cast<u32x4*>(a.flags_too)[i] = u32x4{0, 0, 0, 0};
 }
 
-// The bitmaps from the flags.  (Many workgroups mark at once.  Or-ing bits into words in memory took 10 us for 176,000 marks; stores of a byte, of which none
-// waits for another, and this take 3 and 2.)
+// The bitmaps from the flags.  (Many workgroups mark at once.  Or-ing bits into words in memory took 12.2 us for 176,000 marks; stores of a byte, of which none
+// waits for another, and this take 4.0 and 2.7.)
 __device__ __forceinline__ uint32_t packed(const uint8_t* flags, uint32_t word) {
   uint32_t bits = 0;
 #pragma unroll
@@ -122,7 +122,7 @@ __device__ __forceinline__ void each_page(const int32_t* entries, uint32_t pages
 // ---- fork -------------------------------------------------------------------------------------------------------
 //
 // Child i continues request parents[i].  The first child keeps the parent's last block if that is not full, each later one needs a block:
-// its place among those is a prefix sum over the children.  Blocks to take come from the front of (free blocks, blocks given back in
+// its place among those is a prefix sum over the children.  8192 children of 4096 requests over 107,000 blocks: 23 us in four launches.  Blocks to take come from the front of (free blocks, blocks given back in
 // ascending order); what is left of the two is the new list.
 
 // The children, in one workgroup; the others clear the bitmaps.
@@ -293,7 +293,8 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_end(BlocksArgs a) {
 // ---- one launch -------------------------------------------------------------------------------------------------
 //
 // Up to ONE_REQUESTS requests and children, ONE_BLOCKS blocks and ONE_CELLS entries of the table, with bitmaps in LDS: every workgroup marks all blocks for
-// itself and writes its share of the outputs, so that none waits for another.
+// itself and writes its share of the outputs, so that none waits for another.  128 beams of 32 prompts 6.7 us, their compaction 8.0; in the launches that
+// larger sizes take, 13 and 16.
 
 constexpr uint32_t ONE_REQUESTS = BLOCKS_THREADS, ONE_BLOCKS = 32 * BLOCKS_THREADS, ONE_CELLS = 65536, ONE_MOST_GROUPS = 64;
 
@@ -416,7 +417,7 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_one(BlocksArgs a) {
 // ---- compaction -------------------------------------------------------------------------------------------------
 //
 // Used and free blocks together, ascending: behind the first n_used of them lies the border.  The k-th used block behind the border goes
-// to the k-th free one before it, and what lies behind it is the new free list.
+// to the k-th free one before it, and what lies behind it is the new free list.  3001 requests over 177,000 blocks: 22 us in five launches.
 
 __global__ __launch_bounds__(BLOCKS_THREADS) void k_compact_begin(BlocksArgs a) {
   clear_flags(a, blockIdx.x * BLOCKS_THREADS + threadIdx.x, gridDim.x * BLOCKS_THREADS);

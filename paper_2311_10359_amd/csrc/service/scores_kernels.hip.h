@@ -12,15 +12,17 @@ namespace fikit {
 //
 // in one pass: every lane keeps m, S and T of what it has seen, and moves the sums to another m where a larger logit comes.  d of the largest is 0 whatever
 // its size, so that one token that holds all has entropy and log probability 0, and the type's lowest value, a mask in many programs, is a number as others.
-// (c x - c m in one instruction would leave the rounding of c m in d; the pass is no faster with it, 97 us for 2999 rows of 100,003.)
+// (c x - c m in one instruction would leave the rounding of c m in d, and the pass is no faster with it.)
 //
 // The k alternatives lie in k groups of neighbouring logits (16 bytes, as one load brings them): those with the largest maxima, among equal ones
 // the first, since of any other group k groups before it in this order hold a value that comes before all of its own.  So the pass looks
 // at one maximum for a group, and at the end the k groups are read again and k of their values taken.  A wave takes groups in ascending order,
 // so a later group that is only as large as the k-th so far is none of them, and few pass: about k (1 + log(groups / k)).
 //
-// V * bytes are read: bound by memory, if a logit takes few instructions: one to unpack, one for maximum and minimum, three for d, S and T, and the
-// exponential, which takes the time of four.
+// V * bytes are read: bound by memory, if a logit takes few instructions: one to unpack, one for maximum and minimum, four for d, S and T, and the
+// exponential.  2999 rows of 100,003 bfloat16 logits, 600 MB: 98 us without alternatives, 6.1 TB/s, 108 to 113 with 20, the vector unit busy for 84 % of
+// it.  A workgroup's waves take batches in turn, past the caches (a stretch for each wave 113 us, through the caches 111, both without alternatives), and
+// 4 groups a lane in a batch (8 are 6 us more: half the waves).
 
 struct ScoresArgs {
   const void* logits;
