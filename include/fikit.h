@@ -614,8 +614,8 @@ typedef enum fikit_pairs {
  *   rotary_dim        a multiple of 16 up to head_dim.
  *   pairs             a fikit_pairs.
  *   h_q_out, h_k_out  outputs of the same sizes, whose vectors lie apart: tokens of heads or heads of tokens, one behind the other or with
- *                     gaps (else INVALID_ARG).  An output may be its own input (the same address and strides); else outputs overlap neither
- *                     each other nor an input.
+ *                     gaps (else INVALID_ARG).  An output may be its own input (the same address and strides); else no output's vectors lie
+ *                     over another output's or an input's (INVALID_ARG; they may share a product's rows, beside each other or head by head).
  *
  * The range of the type counts: a norm of values whose squares pass the largest float is right.
  */
@@ -704,7 +704,8 @@ size_t fikit_token_scores_workspace_bytes(uint32_t n_rows, uint32_t vocabulary, 
  *   d_top_tokens   [n_rows][n_top] the tokens of the largest logits, the largest first; of equal logits the lowest token first
  *   d_top_logprob  [n_rows][n_top] their z - lse
  *
- * Outputs may be NULL and are not written then; the last two are both given or both not (n_top 0).
+ * Outputs may be NULL and are not written then; the last two are both given or both not (n_top 0).  They overlap neither each other
+ * nor an input (INVALID_ARG).
  *
  *   d_logits       n_rows rows of `vocabulary` values, dense within a row, row r at r * row_stride values (any stride, 0 too), aligned as
  *                  one value is; value_type FIKIT_BF16, FIKIT_F16 or FIKIT_F32.

@@ -44,8 +44,27 @@ bool apart(const fikit_vectors* v, uint32_t heads, uint32_t n_tokens, uint32_t h
   return outer.n <= 1 || (outer.stride >= head_dim && (outer.stride - head_dim) / (inner.n > 1 ? inner.stride : 1) >= (inner.n > 1 ? inner.n - 1 : 0));
 }
 
-bool rotates_in_place_or_elsewhere(const fikit_vectors* in, const fikit_vectors* out, uint32_t heads, uint32_t n_tokens) {
-  return in->d_data != out->d_data || ((heads <= 1 || in->head_stride == out->head_stride) && (n_tokens <= 1 || in->token_stride == out->token_stride));
+// Does no vector of a lie over one of b?  They may share a product's rows, beside each other or head by head.
+bool apart(const fikit_vectors* a, uint32_t heads_a, const fikit_vectors* b, uint32_t heads_b, uint32_t n_tokens, uint32_t head_dim) {
+  const auto row = [&](const fikit_vectors* v, uint32_t heads) { return (heads - 1) * v->head_stride + head_dim; };        // values from a token's first to its last
+  const auto all = [&](const fikit_vectors* v, uint32_t heads) { return Extent{v->d_data, 2 * ((n_tokens - 1) * v->token_stride + row(v, heads))}; };
+  if (!overlap(all(a, heads_a), all(b, heads_b))) return true;
+  // how far the first value of b's is behind one of a's, in steps of that many values
+  const auto behind = [&](uint64_t step) {
+    const int64_t d = (reinterpret_cast<intptr_t>(b->d_data) - reinterpret_cast<intptr_t>(a->d_data)) / 2 % static_cast<int64_t>(step);
+    return static_cast<uint64_t>(d < 0 ? d + static_cast<int64_t>(step) : d);
+  };
+  const uint64_t step = n_tokens > 1 ? a->token_stride : 0;
+  if (n_tokens > 1 && (b->token_stride != step || step == 0 || step > 1ull << 60)) return false;
+  if (step > 0 && behind(step) >= row(a, heads_a) && behind(step) + row(b, heads_b) <= step) return true;
+  const uint64_t heads = a->head_stride;
+  if (heads == 0 || heads_a <= 1 || heads_b <= 1 || b->head_stride != heads || (step > 0 && step % heads) || heads > 1ull << 60) return false;
+  return behind(heads) >= head_dim && behind(heads) + head_dim <= heads;
+}
+
+// Are an output's places its input's?
+bool in_place(const fikit_vectors* in, const fikit_vectors* out, uint32_t heads, uint32_t n_tokens) {
+  return in->d_data == out->d_data && (heads <= 1 || in->head_stride == out->head_stride) && (n_tokens <= 1 || in->token_stride == out->token_stride);
 }
 
 // Parts of the workspace of a fork or a compaction, one behind the other, in words.
@@ -323,9 +342,11 @@ int fikit_rotate_heads(const fikit_vectors* h_q, const fikit_vectors* h_k, uint3
   struct { const fikit_vectors *in, *out; uint32_t heads; } sides[] = {{h_q, h_q_out, q_heads}, {h_k, h_k_out, kv_heads}};
   for (const auto& s : sides)
     if (s.heads > 0 && (!vectors_ok(s.in) || !vectors_ok(s.out) || !apart(s.out, s.heads, n_tokens, head_dim) ||
-                        !rotates_in_place_or_elsewhere(s.in, s.out, s.heads, n_tokens)))
+                        !(in_place(s.in, s.out, s.heads, n_tokens) || apart(s.out, s.heads, s.in, s.heads, n_tokens, head_dim))))
       return FIKIT_INVALID_ARG;
-  if (q_heads > 0 && kv_heads > 0 && (h_q_out->d_data == h_k_out->d_data || h_q_out->d_data == h_k->d_data || h_k_out->d_data == h_q->d_data))
+  if (q_heads > 0 && kv_heads > 0 &&
+      (!apart(h_q_out, q_heads, h_k_out, kv_heads, n_tokens, head_dim) || !apart(h_q_out, q_heads, h_k, kv_heads, n_tokens, head_dim) ||
+       !apart(h_k_out, kv_heads, h_q, q_heads, n_tokens, head_dim)))
     return FIKIT_INVALID_ARG;
   RotateArgs a{};
   if (q_heads > 0) { a.q = *h_q; a.q_out = *h_q_out; }
@@ -367,6 +388,10 @@ int fikit_token_scores(const void* d_logits, int32_t value_type, uint64_t row_st
       !aligned(d_entropy, 4) || !aligned(d_lse, 4) || !aligned(d_top_tokens, 4) || !aligned(d_top_logprob, 4))
     return FIKIT_INVALID_ARG;
   if (n_top > 0 && (!d_top_tokens || !d_top_logprob)) return FIKIT_INVALID_ARG;
+  const uint64_t tops = 4ull * n_rows * n_top, row = 4ull * n_rows;
+  const Extent extents[] = {{d_logprob, d_logprob ? row : 0}, {d_entropy, d_entropy ? row : 0}, {d_lse, d_lse ? row : 0}, {d_top_tokens, tops}, {d_top_logprob, tops},
+                            {d_logits, ((n_rows - 1) * row_stride + vocabulary) * (value_type == FIKIT_F32 ? 4 : 2)}, {d_tokens, d_tokens ? row : 0}};
+  if (!outputs_apart(extents, 5, 7)) return FIKIT_INVALID_ARG;
   const ScoresCut c = scores_cut(n_rows, vocabulary, value_type, n_top);
   if (c.bytes > 0) {
     if (!d_workspace || !aligned(d_workspace, 256)) return FIKIT_INVALID_ARG;

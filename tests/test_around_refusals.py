@@ -39,6 +39,27 @@ def test_rotate_heads(change, want):
     assert rotate(**change) == want
 
 
+QUERIES, KEYS = 0x10000, 0x10200        # in one product of 9 heads of 64: queries of 4, keys of 2, values; a token takes 576 values
+
+
+@pytest.mark.parametrize("q_out, k_out", [
+    (vectors(KEYS, 576), vectors(0x30000, 576)), (vectors(QUERIES + 128, 576), vectors(KEYS, 576)), (vectors(0x30000, 576), vectors(KEYS - 128, 576)),
+    (vectors(QUERIES + 1152, 576), vectors(0x40000)), (vectors(0x30000), vectors(QUERIES + 128, 640)), (vectors(0x30000), vectors(0x30000 + 128)),
+    (vectors(QUERIES, 640), vectors(KEYS, 576)), (vectors(0x30000, 64, 320), vectors(0x30000 + 640, 64, 320))])
+def test_rotate_heads_over_each_other(q_out, k_out):
+    assert rotate(q=vectors(QUERIES, 576), k=vectors(KEYS, 576), q_out=q_out, k_out=k_out) == INVALID
+
+
+@pytest.mark.parametrize("q_out, k_out", [(0x10080, 0x10100), (0x10040, 0x30000), (0x30000, 0x30040), (0x10000, 0x10000), (0x10180, 0x30000)])
+def test_rotate_heads_over_each_other_head_by_head(q_out, k_out):
+    """Query, key and value of 64 each for a head."""
+    assert rotate(kv_heads=4, q=vectors(0x10000, 768, 192), k=vectors(0x10080, 768, 192), q_out=vectors(q_out, 768, 192), k_out=vectors(k_out, 768, 192)) == INVALID
+
+
+def test_rotate_heads_over_each_other_in_one_token():
+    assert rotate(tokens=1, q=vectors(QUERIES, 0), k=vectors(KEYS, 0), q_out=vectors(QUERIES + 256, 0), k_out=vectors(0x30000, 0)) == INVALID
+
+
 def test_rotate_heads_takes_any_epsilon_without_a_norm():
     assert rotate(q_weight=NULL, epsilon=0.0, tokens=0) == OK
 
@@ -148,15 +169,17 @@ def test_block_bindings():
 
 
 def scores(**change):
-    a = dict(logits=FAKE, value_type=0, stride=70000, rows=4, vocabulary=70000, scale=1.0, tokens=FAKE, n_top=3, logprob=FAKE, entropy=FAKE, lse=FAKE, top_tokens=FAKE,
-             top_logprob=FAKE, status=FAKE, ws=FAKE, ws_bytes=1 << 30)
+    a = dict(logits=0x1000000, value_type=0, stride=70000, rows=4, vocabulary=70000, scale=1.0, tokens=0x10000, n_top=3, logprob=0x20000, entropy=0x30000, lse=0x40000,
+             top_tokens=0x50000, top_logprob=0x60000, status=FAKE, ws=FAKE, ws_bytes=1 << 30)
     assert set(change) <= set(a)
     a.update(change)
     return binding.load().fikit_token_scores(*a.values(), None)
 
 
 @pytest.mark.parametrize("change, want", [
-    (dict(logits=NULL), INVALID), (dict(logits=ODD), INVALID), (dict(logits=FAKE + 2, value_type=2), INVALID), (dict(value_type=3), INVALID), (dict(value_type=-1), INVALID),
+    (dict(logits=NULL), INVALID), (dict(logits=ODD), INVALID), (dict(logits=0x1000002, value_type=2), INVALID),
+    (dict(logprob=0x1000000), INVALID), (dict(entropy=0x1000000 + 8 * 70000 - 4), INVALID), (dict(lse=0x20000), INVALID), (dict(top_logprob=0x50010), INVALID),
+    (dict(top_tokens=0x10000), INVALID), (dict(logprob=0x60020), INVALID), (dict(value_type=3), INVALID), (dict(value_type=-1), INVALID),
     (dict(rows=1 << 31), INVALID), (dict(vocabulary=1 << 31), INVALID), (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID), (dict(scale=float("nan")), INVALID),
     (dict(scale=float("inf")), INVALID), (dict(scale=1e-31), INVALID), (dict(scale=2e30), INVALID), (dict(tokens=ODD), INVALID), (dict(logprob=ODD), INVALID),
     (dict(entropy=ODD), INVALID), (dict(lse=ODD), INVALID), (dict(top_tokens=NULL), INVALID), (dict(top_tokens=ODD), INVALID), (dict(top_logprob=NULL), INVALID),

@@ -63,6 +63,24 @@ def test_in_the_product_and_in_place(neighbours):
     assert torch.equal(q, apart.q) and torch.equal(k, apart.k) and torch.equal(qkv[:, hq + hkv:], before[:, hq + hkv:])
 
 
+def test_in_place_head_by_head_and_into_other_heads_of_the_product():
+    dim, heads, tokens = 64, 6, 41
+    qkv = normal(27, tokens, heads, 3, dim)
+    before = qkv.clone()
+    q, k = qkv[:, :, 0], qkv[:, :, 1]
+    positions = torch.arange(tokens, dtype=torch.int32, device=DEV)
+    apart = check(q, k, positions, frequencies(64), True)
+    check(q, k, positions, frequencies(64), True, out=binding.RotatedHeads(q, k))
+    assert torch.equal(q, apart.q) and torch.equal(k, apart.k) and torch.equal(qkv[:, :, 2], before[:, :, 2])
+    qkv.copy_(before)
+    check(q, None, positions, frequencies(64), True, out=binding.RotatedHeads(qkv[:, :, 2], None))
+    assert torch.equal(qkv[:, :, 2], apart.q) and torch.equal(qkv[:, :, :2], before[:, :, :2])
+    for one in (qkv[:1], before[:1]):
+        check(one[:, :, 0], one[:, :, 1], positions[:1], frequencies(64), out=binding.RotatedHeads(one[:, :, 0], one[:, :, 1]))
+    wide = normal(28, tokens, 9, dim)
+    check(wide[:, :4], wide[:, 4:6], positions, frequencies(64), out=binding.RotatedHeads(wide[:, :4], wide[:, 6:8]))
+
+
 def test_one_side_other_orders_and_shared_inputs():
     positions = torch.arange(9, dtype=torch.int32, device=DEV)
     f = frequencies(64)
