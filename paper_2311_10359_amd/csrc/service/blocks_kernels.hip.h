@@ -104,11 +104,11 @@ struct Words {
   }
 };
 
-// f(page, entry) for the first `pages` entries of a row, by a wave, several loads on their way.
+// f(page, entry) for the first `pages` entries of a row, by a wave, several loads on their way; from page `first` on.
 template <typename F>
-__device__ __forceinline__ void each_page(const int32_t* entries, uint32_t pages, F f) {
+__device__ __forceinline__ void each_page(const int32_t* entries, uint32_t pages, F f, uint32_t first = 0) {
   constexpr int AHEAD = 4;
-  for (uint32_t from = lane_id(); from < pages; from += AHEAD * WAVE) {
+  for (uint32_t from = first + lane_id(); from < pages; from += AHEAD * WAVE) {
     int32_t held[AHEAD];
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i)
@@ -342,67 +342,77 @@ __device__ __forceinline__ uint32_t marked_block(const uint32_t* before, uint32_
 __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_one(BlocksArgs a) {
   __shared__ OneLds lds;
   __shared__ uint32_t before[BLOCKS_THREADS], first[ONE_REQUESTS], ranks[ONE_REQUESTS];
-  const uint32_t t = threadIdx.x, within = (1u << a.shift) - 1;
+  __shared__ int32_t lengths[ONE_REQUESTS], parents[ONE_REQUESTS], fresh[ONE_REQUESTS];
+  const uint32_t t = threadIdx.x, lane = lane_id(), waves = BLOCKS_THREADS / WAVE, mine = blockIdx.x * waves + uniform(t / WAVE);
   const bool stop = stopped(a.status);
   const int32_t length = t < a.n_requests ? a.lengths[t] : 0, parent = t < a.n_children ? a.parents[t] : -1;
+  const bool fits = length_ok(a, length) && parent >= -1 && (parent < 0 || static_cast<uint32_t>(parent) < a.n_requests);
   lds.marks[t] = lds.marks_too[t] = 0;
   first[t] = NO_CHILD;
-  const bool whole = length_ok(a, length) && parent >= -1 && (parent < 0 || static_cast<uint32_t>(parent) < a.n_requests);
-  lds.pages[t] = whole ? pages_of(a, static_cast<uint32_t>(length)) : 0;
-  if (__syncthreads_or(stop)) return;
-  if (parent >= 0 && whole) atomicMin(&first[parent], t);
-  if (__syncthreads_or(!whole)) {
-    if (blockIdx.x == 0 && t == 0) *a.status = FIKIT_INVALID_ARG;
+  lengths[t] = length;
+  parents[t] = parent;
+  lds.pages[t] = fits ? pages_of(a, static_cast<uint32_t>(length)) : 0;
+  if (__syncthreads_or(stop || !fits)) {
+    if (!__syncthreads_or(stop) && blockIdx.x == 0 && t == 0) *a.status = FIKIT_INVALID_ARG;
     return;
   }
-  const int32_t child_length = parent >= 0 ? a.lengths[parent] : 0;
+  if (parent >= 0) atomicMin(&first[parent], t);
+  // what the wave's first row begins with is on its way from here on
+  const int32_t my_parent = mine < a.n_children ? parents[mine] : -1;
+  const uint32_t my_pages = my_parent >= 0 ? lds.pages[my_parent] : 0;
+  const int32_t early = lane < my_pages ? a.table[static_cast<uint64_t>(my_parent) * a.width + lane] : 0;
+  __syncthreads();
   bool bad = false;
   if (a.width > 0)
     each_entry(a, lds.pages, [&](uint32_t row, uint32_t block) {
       if (block < a.n_blocks) atomicOr(&(first[row] == NO_CHILD ? lds.marks : lds.marks_too)[block / 32], 1u << block % 32);
       else bad = true;
     });
-  const bool need = parent >= 0 && (static_cast<uint32_t>(child_length) & within) && first[parent] != t;
-  uint32_t taken, given;
-  const uint32_t rank = block_excl_scan_1024(need, lds.scan, taken);
-  ranks[t] = need ? rank : ~0u;
+  const int32_t child_length = parent >= 0 ? lengths[parent] : 0;
+  const bool need = (static_cast<uint32_t>(child_length) & ((1u << a.shift) - 1)) && first[parent] != t;
   if (__syncthreads_or(bad)) {
     if (blockIdx.x == 0 && t == 0) *a.status = FIKIT_INVALID_ARG;
     return;
   }
-  const uint32_t word = lds.marks[t] & ~lds.marks_too[t];
-  before[t] = block_excl_scan_1024(__popc(word), lds.scan, given);
-  const uint32_t total = a.n_free + given;
+  // two sums in one: children that need a block, and blocks given back, up to 32,768
+  uint32_t both;
+  const uint32_t upto = block_excl_scan_1024(__popc(lds.marks[t] & ~lds.marks_too[t]) | (need ? 1u << 16 : 0), lds.scan, both);
+  const uint32_t rank = upto >> 16, taken = both >> 16, given = both & 0xffffu, total = a.n_free + given;
+  ranks[t] = need ? rank : ~0u;
+  before[t] = upto & 0xffffu;
   if (taken > total || total - taken > a.n_blocks) {
     if (blockIdx.x == 0 && t == 0) *a.status = taken > total ? FIKIT_CACHE_FULL : FIKIT_INVALID_ARG;
     return;
   }
+  fresh[t] = need && rank < a.n_free ? a.free_blocks[rank] : 0;
+  const uint32_t from = blockIdx.x * BLOCKS_THREADS + t, stride = gridDim.x * BLOCKS_THREADS;
+  const int32_t left = taken + from < a.n_free ? a.free_blocks[taken + from] : 0;
   __syncthreads();
   const auto given_word = [&](uint32_t w) { return lds.marks[w] & ~lds.marks_too[w]; };
   // rows, a wave each
-  const uint32_t lane = lane_id(), waves = BLOCKS_THREADS / WAVE;
-  for (uint32_t c = blockIdx.x * waves + uniform(t / WAVE); c < a.n_children; c += gridDim.x * waves) {
-    const int32_t p = a.parents[c];
-    const uint32_t pages = p >= 0 ? lds.pages[p] : 0, mine = ranks[c];
-    const int32_t* entries = a.table + static_cast<uint64_t>(p >= 0 ? p : 0) * a.width;
+  for (uint32_t c = mine; c < a.n_children; c += gridDim.x * waves) {
+    const int32_t p = parents[c];
+    const uint32_t pages = p >= 0 ? lds.pages[p] : 0, place = ranks[c];
     int32_t* out = a.new_table + static_cast<uint64_t>(c) * a.width;
-    each_page(entries, pages, [&](uint32_t page, int32_t block) {
-      if (page + 1 == pages && mine != ~0u) {
-        const uint32_t fresh = mine < a.n_free ? static_cast<uint32_t>(a.free_blocks[mine]) : marked_block(before, mine - a.n_free, given_word);
-        if (fresh >= a.n_blocks) *a.status = FIKIT_INVALID_ARG;
-        a.copies[mine] = make_int2(block, static_cast<int32_t>(fresh));
-        block = static_cast<int32_t>(fresh);
+    const auto put = [&](uint32_t page, int32_t block) {
+      if (page + 1 == pages && place != ~0u) {
+        const uint32_t one = place < a.n_free ? static_cast<uint32_t>(fresh[c]) : marked_block(before, place - a.n_free, given_word);
+        if (one >= a.n_blocks) *a.status = FIKIT_INVALID_ARG;
+        a.copies[place] = make_int2(block, static_cast<int32_t>(one));
+        block = static_cast<int32_t>(one);
       }
       out[page] = block;
-    });
+    };
+    if (c == mine && lane < pages) put(lane, early);
+    each_page(a.table + static_cast<uint64_t>(p >= 0 ? p : 0) * a.width, pages, put, c == mine ? WAVE : 0);
     for (uint32_t page = pages + lane; page < a.width; page += WAVE) out[page] = -1;
   }
-  const uint32_t from = blockIdx.x * BLOCKS_THREADS + t, stride = gridDim.x * BLOCKS_THREADS;
   for (uint32_t block = from; block < a.n_blocks; block += stride) {
     const uint32_t marks = given_word(block / 32), bit = 1u << block % 32, place = a.n_free + before[block / 32] + __popc(marks & (bit - 1));
     if ((marks & bit) && place >= taken) a.new_free[place - taken] = static_cast<int32_t>(block);
   }
-  for (uint32_t i = taken + from; i < a.n_free; i += stride) a.new_free[i - taken] = a.free_blocks[i];
+  if (taken + from < a.n_free) a.new_free[from] = left;
+  for (uint32_t i = taken + from + stride; i < a.n_free; i += stride) a.new_free[i - taken] = a.free_blocks[i];
   for (uint32_t i = total - taken + from; i < a.n_blocks; i += stride) a.new_free[i] = -1;
   for (uint32_t i = taken + from; i < a.n_children; i += stride) a.copies[i] = make_int2(-1, -1);
   if (blockIdx.x > 0) return;
@@ -528,6 +538,7 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_compact_rows(BlocksArgs a)
 __global__ __launch_bounds__(BLOCKS_THREADS) void k_compact_one(BlocksArgs a) {
   __shared__ OneLds lds;
   __shared__ uint32_t used_before[BLOCKS_THREADS], spare_before[BLOCKS_THREADS];
+  __shared__ uint16_t holes[ONE_BLOCKS / 2];
   __shared__ Border border;
   const uint32_t t = threadIdx.x;
   const bool stop = stopped(a.status);
@@ -540,43 +551,51 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_compact_one(BlocksArgs a) {
     if (block < a.n_blocks) atomicOr(&marks[block / 32], 1u << block % 32);
     else bad = true;
   };
-  if (a.width > 0) each_entry(a, lds.pages, [&](uint32_t, uint32_t block) { put(lds.marks, block); });
+  // what the wave's first row begins with, and the first free blocks, are on their way from here on
+  const uint32_t lane = lane_id(), waves = BLOCKS_THREADS / WAVE, mine = blockIdx.x * waves + uniform(t / WAVE);
+  const int32_t early = mine < a.n_requests && lane < lds.pages[mine] ? a.table[static_cast<uint64_t>(mine) * a.width + lane] : 0;
   constexpr int AHEAD = 4;
-  for (uint32_t i = t; i < a.n_free; i += AHEAD * BLOCKS_THREADS) {
-    int32_t held[AHEAD];
+  int32_t held[AHEAD];
 #pragma unroll
-    for (int j = 0; j < AHEAD; ++j)
-      if (i + j * BLOCKS_THREADS < a.n_free) held[j] = a.free_blocks[i + j * BLOCKS_THREADS];
+  for (int j = 0; j < AHEAD; ++j)
+    if (t + j * BLOCKS_THREADS < a.n_free) held[j] = a.free_blocks[t + j * BLOCKS_THREADS];
+  if (a.width > 0) each_entry(a, lds.pages, [&](uint32_t, uint32_t block) { put(lds.marks, block); });
 #pragma unroll
-    for (int j = 0; j < AHEAD; ++j)
-      if (i + j * BLOCKS_THREADS < a.n_free) put(lds.marks_too, static_cast<uint32_t>(held[j]));
-  }
+  for (int j = 0; j < AHEAD; ++j)
+    if (t + j * BLOCKS_THREADS < a.n_free) put(lds.marks_too, static_cast<uint32_t>(held[j]));
+  for (uint32_t i = t + AHEAD * BLOCKS_THREADS; i < a.n_free; i += BLOCKS_THREADS) put(lds.marks_too, static_cast<uint32_t>(a.free_blocks[i]));
   __syncthreads();
   const uint32_t used = lds.marks[t], spare = lds.marks_too[t];
   bad |= (used & spare) != 0;
-  uint32_t mine[2], total[2];
-  mine[0] = used_before[t] = block_excl_scan_1024(__popc(used), lds.scan, total[0]);
-  mine[1] = spare_before[t] = block_excl_scan_1024(__popc(spare), lds.scan, total[1]);
+  uint32_t both;                               // two sums in one, of up to 32,768 each
+  const uint32_t upto = block_excl_scan_1024(__popc(used) << 16 | __popc(spare), lds.scan, both);
+  const uint32_t sums[2] = {upto >> 16, upto & 0xffffu}, total[2] = {both >> 16, both & 0xffffu};
+  used_before[t] = sums[0];
+  spare_before[t] = sums[1];
+  if (t == 0 && total[0] == 0) border = Border{0, 0};
+  find_border(t, used, spare, sums[0], sums[0] + sums[1], total[0], &border);
   if (__syncthreads_or(bad) || total[1] != a.n_free) {             // also: a block that is used and free, or free twice
     if (blockIdx.x == 0 && t == 0) *a.status = FIKIT_INVALID_ARG;
     return;
   }
-  if (t == 0 && total[0] == 0) border = Border{0, 0};
-  find_border(t, used, spare, mine[0], mine[0] + mine[1], total[0], &border);
+  // the free blocks before the border, to which used ones go
+  for (uint32_t block = t; block < border.block; block += BLOCKS_THREADS) {
+    const uint32_t w = block / 32, bit = 1u << block % 32, marks = lds.marks_too[w];
+    if (marks & bit) holes[spare_before[w] + __popc(marks & (bit - 1))] = static_cast<uint16_t>(block);
+  }
   __syncthreads();
-  const auto spare_word = [&](uint32_t w) { return lds.marks_too[w]; };
-  // where a used block behind the border goes
   const auto goes = [&](uint32_t block) {
-    const uint32_t w = block / 32, k = used_before[w] + __popc(lds.marks[w] & ((1u << block % 32) - 1)) - border.used;
-    return static_cast<int32_t>(marked_block(spare_before, k, spare_word));
+    const uint32_t w = block / 32;
+    return static_cast<int32_t>(holes[used_before[w] + __popc(lds.marks[w] & ((1u << block % 32) - 1)) - border.used]);
   };
-  const uint32_t lane = lane_id(), waves = BLOCKS_THREADS / WAVE;
-  for (uint32_t r = blockIdx.x * waves + uniform(t / WAVE); r < a.n_requests; r += gridDim.x * waves) {
+  for (uint32_t r = mine; r < a.n_requests; r += gridDim.x * waves) {
     const uint32_t pages = lds.pages[r];
     int32_t* out = a.new_table + static_cast<uint64_t>(r) * a.width;
-    each_page(a.table + static_cast<uint64_t>(r) * a.width, pages, [&](uint32_t page, int32_t entry) {
+    const auto write = [&](uint32_t page, int32_t entry) {
       out[page] = static_cast<uint32_t>(entry) >= border.block ? goes(static_cast<uint32_t>(entry)) : entry;
-    });
+    };
+    if (r == mine && lane < pages) write(lane, early);
+    each_page(a.table + static_cast<uint64_t>(r) * a.width, pages, write, r == mine ? WAVE : 0);
     for (uint32_t page = pages + lane; page < a.width; page += WAVE) out[page] = -1;
   }
   const uint32_t moved = total[0] - border.used, from = blockIdx.x * BLOCKS_THREADS + t, stride = gridDim.x * BLOCKS_THREADS;
