@@ -629,8 +629,8 @@ typedef struct fikit_block_copy {
   int32_t from, to;
 } fikit_block_copy;
 
-/* Bytes of device workspace fikit_cache_fork needs for these sizes (0: sizes it does not take). */
-size_t fikit_cache_fork_workspace_bytes(uint32_t n_requests, uint32_t n_children, uint32_t n_blocks);
+/* Bytes of device workspace fikit_cache_fork needs for these sizes (0: none, d_workspace may be NULL; also for sizes it does not take). */
+size_t fikit_cache_fork_workspace_bytes(uint32_t n_requests, uint32_t n_children, uint32_t table_width, uint32_t n_blocks);
 
 /*
  * The requests of the next step from those of the last: child i continues request d_parents[i], with all its tokens; several children may
@@ -657,8 +657,8 @@ int fikit_cache_fork(const int32_t* d_block_table, uint32_t table_width, const i
                      uint32_t n_free, int32_t* d_new_table, int32_t* d_new_lengths, fikit_block_copy* d_copies, int32_t* d_new_free,
                      int32_t* d_counts, int32_t* d_status, void* d_workspace, size_t workspace_bytes, void* hip_stream);
 
-/* Bytes of device workspace fikit_cache_compact needs for these sizes (0: sizes it does not take). */
-size_t fikit_cache_compact_workspace_bytes(uint32_t n_requests, uint32_t n_blocks);
+/* Bytes of device workspace fikit_cache_compact needs for these sizes (0: none, d_workspace may be NULL; also for sizes it does not take). */
+size_t fikit_cache_compact_workspace_bytes(uint32_t n_requests, uint32_t table_width, uint32_t n_blocks);
 
 /*
  * Compaction: of the blocks in use and the free ones together, the lowest ones are in use afterwards, so that the rest can be given

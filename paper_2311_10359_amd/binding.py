@@ -148,11 +148,11 @@ def load() -> ctypes.CDLL:
         lib.fikit_rotate_heads.restype = ctypes.c_int
         lib.fikit_rotate_heads.argtypes = [p_vec, p_vec, u32, u32, u32, i32, vp, vp, f32, vp, vp, u32, i32, u32, p_vec, p_vec, vp, vp]
         lib.fikit_cache_fork_workspace_bytes.restype = sz
-        lib.fikit_cache_fork_workspace_bytes.argtypes = [u32, u32, u32]
+        lib.fikit_cache_fork_workspace_bytes.argtypes = [u32, u32, u32, u32]
         lib.fikit_cache_fork.restype = ctypes.c_int
         lib.fikit_cache_fork.argtypes = [vp, u32, vp, u32, vp, u32, u32, u32, vp, u32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         lib.fikit_cache_compact_workspace_bytes.restype = sz
-        lib.fikit_cache_compact_workspace_bytes.argtypes = [u32, u32]
+        lib.fikit_cache_compact_workspace_bytes.argtypes = [u32, u32, u32]
         lib.fikit_cache_compact.restype = ctypes.c_int
         lib.fikit_cache_compact.argtypes = [vp, u32, vp, u32, u32, u32, vp, u32, vp, vp, vp, vp, vp, vp, sz, vp]
         lib.fikit_cache_copy.restype = ctypes.c_int
@@ -764,8 +764,8 @@ class CacheFork(NamedTuple):
     counts: torch.Tensor            # int32 [3]: blocks taken, given back, free
 
 
-def fikit_cache_fork_workspace_bytes(n_requests: int, n_children: int, n_blocks: int) -> int:
-    return int(load().fikit_cache_fork_workspace_bytes(n_requests, n_children, n_blocks))
+def fikit_cache_fork_workspace_bytes(n_requests: int, n_children: int, table_width: int, n_blocks: int) -> int:
+    return int(load().fikit_cache_fork_workspace_bytes(n_requests, n_children, table_width, n_blocks))
 
 
 def fikit_cache_fork(block_table: torch.Tensor, lengths: torch.Tensor, parents: torch.Tensor, block_tokens: int, n_blocks: int,
@@ -790,8 +790,8 @@ class CacheCompaction(NamedTuple):
     counts: torch.Tensor            # int32 [2]: copies, blocks in use
 
 
-def fikit_cache_compact_workspace_bytes(n_requests: int, n_blocks: int) -> int:
-    return int(load().fikit_cache_compact_workspace_bytes(n_requests, n_blocks))
+def fikit_cache_compact_workspace_bytes(n_requests: int, table_width: int, n_blocks: int) -> int:
+    return int(load().fikit_cache_compact_workspace_bytes(n_requests, table_width, n_blocks))
 
 
 def fikit_cache_compact(block_table: torch.Tensor, lengths: torch.Tensor, block_tokens: int, n_blocks: int, free_blocks: torch.Tensor,

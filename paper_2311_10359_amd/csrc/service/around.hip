@@ -101,6 +101,13 @@ struct CompactParts : Parts {
   }
 };
 
+// Workgroups of the kernels that do all in one launch, or 0 for sizes that they do not take.
+uint32_t one_launch(uint32_t n_requests, uint32_t n_children, uint32_t rows, uint32_t table_width, uint32_t n_blocks) {
+  if (n_requests > ONE_REQUESTS || n_children > ONE_REQUESTS || n_blocks > ONE_BLOCKS || static_cast<uint64_t>(n_requests) * table_width > ONE_CELLS) return 0;
+  const uint32_t groups = (rows + BLOCKS_THREADS / WAVE - 1) / (BLOCKS_THREADS / WAVE);
+  return groups < 1 ? 1 : groups < ONE_MOST_GROUPS ? groups : ONE_MOST_GROUPS;
+}
+
 bool blocks_fit(uint32_t n_requests, uint32_t n_children, uint32_t n_blocks) {
   return n_requests <= BLOCKS_MOST_REQUESTS && n_children <= BLOCKS_MOST_REQUESTS && n_blocks <= BLOCKS_MOST_BLOCKS;
 }
@@ -190,13 +197,6 @@ struct ScoresCall {
 
 bool logits_ok(int32_t value_type) { return type_ok(value_type) || value_type == FIKIT_F32; }
 
-// Workgroups of the kernels that do all in one launch, or 0 for sizes that they do not take.
-uint32_t one_launch(uint32_t n_requests, uint32_t n_children, uint32_t rows, uint32_t table_width, uint32_t n_blocks) {
-  if (n_requests > ONE_REQUESTS || n_children > ONE_REQUESTS || n_blocks > ONE_BLOCKS || static_cast<uint64_t>(n_requests) * table_width > ONE_CELLS) return 0;
-  const uint32_t groups = (rows + BLOCKS_THREADS / WAVE - 1) / (BLOCKS_THREADS / WAVE);
-  return groups < 1 ? 1 : groups < ONE_MOST_GROUPS ? groups : ONE_MOST_GROUPS;
-}
-
 dim3 clear_groups(uint32_t words) { return dim3((2 * words + BLOCKS_THREADS - 1) / BLOCKS_THREADS); }        // 16 flags of both kinds to a thread
 int pack(const BlocksArgs& a, hipStream_t st) { return enqueue(k_blocks_pack, clear_groups(a.words), dim3(BLOCKS_THREADS), st, a); }
 constexpr uint32_t COPY_GROUPS = 16384;
@@ -205,8 +205,9 @@ constexpr uint32_t COPY_GROUPS = 16384;
 
 extern "C" {
 
-size_t fikit_cache_fork_workspace_bytes(uint32_t n_requests, uint32_t n_children, uint32_t n_blocks) {
-  return blocks_fit(n_requests, n_children, n_blocks) ? static_cast<size_t>(ForkParts(n_requests, n_children, n_blocks).bytes) : 0;
+size_t fikit_cache_fork_workspace_bytes(uint32_t n_requests, uint32_t n_children, uint32_t table_width, uint32_t n_blocks) {
+  if (!blocks_fit(n_requests, n_children, n_blocks) || one_launch(n_requests, n_children, n_children, table_width, n_blocks)) return 0;
+  return static_cast<size_t>(ForkParts(n_requests, n_children, n_blocks).bytes);
 }
 
 int fikit_cache_fork(const int32_t* d_block_table, uint32_t table_width, const int32_t* d_lengths, uint32_t n_requests,
@@ -215,24 +216,29 @@ int fikit_cache_fork(const int32_t* d_block_table, uint32_t table_width, const i
                      int32_t* d_counts, int32_t* d_status, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
   if (int rc = blocks_status(d_block_table, table_width, d_lengths, n_requests, n_children, block_tokens, n_blocks, d_free, n_free, d_status)) return rc;
   if (n_children > 0 && (!d_parents || !d_new_lengths || !d_copies || (table_width > 0 && !d_new_table))) return FIKIT_INVALID_ARG;
-  if (!d_new_free || !d_counts || !d_workspace || !aligned(d_parents, 4) || !aligned(d_new_table, 4) || !aligned(d_new_lengths, 4) ||
-      !aligned(d_copies, 8) || !aligned(d_new_free, 4) || !aligned(d_counts, 4) || !aligned(d_workspace, 256))
+  if (!d_new_free || !d_counts || !aligned(d_parents, 4) || !aligned(d_new_table, 4) || !aligned(d_new_lengths, 4) || !aligned(d_copies, 8) ||
+      !aligned(d_new_free, 4) || !aligned(d_counts, 4))
     return FIKIT_INVALID_ARG;
   const uint64_t row = 4ull * table_width;
   const Extent extents[] = {{d_new_table, row * n_children}, {d_new_lengths, 4ull * n_children}, {d_copies, sizeof(fikit_block_copy) * n_children},
                             {d_new_free, 4ull * n_blocks}, {d_counts, 12}, {d_block_table, row * n_requests}, {d_lengths, 4ull * n_requests},
                             {d_parents, 4ull * n_children}, {d_free, 4ull * n_free}};
   if (!outputs_apart(extents, 5, 9)) return FIKIT_INVALID_ARG;
-  const ForkParts parts(n_requests, n_children, n_blocks);
-  if (workspace_bytes < parts.bytes) return FIKIT_WORKSPACE_TOO_SMALL;
   BlocksArgs a = blocks_args(d_block_table, table_width, d_lengths, n_requests, block_tokens, n_blocks, d_free, n_free, d_status);
-  const auto part = [&](uint64_t at) { return reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(d_workspace) + at); };
   a.parents = d_parents;
   a.new_table = d_new_table;
   a.new_lengths = d_new_lengths;
   a.copies = reinterpret_cast<int2*>(d_copies);
   a.new_free = d_new_free;
   a.counts = d_counts;
+  a.n_children = n_children;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (const uint32_t groups = one_launch(n_requests, n_children, n_children, table_width, n_blocks))
+    return enqueue(k_fork_one, dim3(groups), dim3(BLOCKS_THREADS), st, a);
+  const ForkParts parts(n_requests, n_children, n_blocks);
+  if (!d_workspace || !aligned(d_workspace, 256)) return FIKIT_INVALID_ARG;
+  if (workspace_bytes < parts.bytes) return FIKIT_WORKSPACE_TOO_SMALL;
+  const auto part = [&](uint64_t at) { return reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(d_workspace) + at); };
   a.words_of_call = part(0);
   a.flags = reinterpret_cast<uint8_t*>(part(parts.flags));
   a.flags_too = reinterpret_cast<uint8_t*>(part(parts.flags_too));
@@ -241,10 +247,6 @@ int fikit_cache_fork(const int32_t* d_block_table, uint32_t table_width, const i
   a.first = part(parts.first);
   a.rank = reinterpret_cast<int32_t*>(part(parts.rank));
   a.wants = part(parts.wants);
-  a.n_children = n_children;
-  hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  if (const uint32_t groups = one_launch(n_requests, n_children, n_children, table_width, n_blocks))
-    return enqueue(k_fork_one, dim3(groups), dim3(BLOCKS_THREADS), st, a);
   if (int rc = enqueue(k_fork_begin, dim3(1 + clear_groups(a.words).x), dim3(BLOCKS_THREADS), st, a)) return rc;
   if (const uint32_t rows = n_requests + n_children)
     if (int rc = enqueue(k_fork_rows, dim3((rows + ROW_WAVES - 1) / ROW_WAVES), dim3(ROW_WAVES * WAVE), st, a)) return rc;
@@ -252,8 +254,9 @@ int fikit_cache_fork(const int32_t* d_block_table, uint32_t table_width, const i
   return enqueue(k_fork_end, dim3((a.words + SLICE - 1) / SLICE), dim3(BLOCKS_THREADS), st, a);
 }
 
-size_t fikit_cache_compact_workspace_bytes(uint32_t n_requests, uint32_t n_blocks) {
-  return blocks_fit(n_requests, 0, n_blocks) ? static_cast<size_t>(CompactParts(n_blocks).bytes) : 0;
+size_t fikit_cache_compact_workspace_bytes(uint32_t n_requests, uint32_t table_width, uint32_t n_blocks) {
+  if (!blocks_fit(n_requests, 0, n_blocks) || one_launch(n_requests, 0, n_requests, table_width, n_blocks)) return 0;
+  return static_cast<size_t>(CompactParts(n_blocks).bytes);
 }
 
 int fikit_cache_compact(const int32_t* d_block_table, uint32_t table_width, const int32_t* d_lengths, uint32_t n_requests,
@@ -263,31 +266,30 @@ int fikit_cache_compact(const int32_t* d_block_table, uint32_t table_width, cons
   if (int rc = blocks_status(d_block_table, table_width, d_lengths, n_requests, 0, block_tokens, n_blocks, d_free, n_free, d_status)) return rc;
   const uint32_t room = n_free < n_blocks / 2 ? n_free : n_blocks / 2;
   if ((n_requests > 0 && table_width > 0 && !d_new_table) || (room > 0 && !d_copies) || (n_free > 0 && !d_new_free)) return FIKIT_INVALID_ARG;
-  if (!d_counts || !d_workspace || !aligned(d_new_table, 4) || !aligned(d_copies, 8) || !aligned(d_new_free, 4) || !aligned(d_counts, 4) ||
-      !aligned(d_workspace, 256))
-    return FIKIT_INVALID_ARG;
+  if (!d_counts || !aligned(d_new_table, 4) || !aligned(d_copies, 8) || !aligned(d_new_free, 4) || !aligned(d_counts, 4)) return FIKIT_INVALID_ARG;
   const uint64_t table = 4ull * table_width * n_requests;
   const Extent extents[] = {{d_new_table, table}, {d_copies, sizeof(fikit_block_copy) * room}, {d_new_free, 4ull * n_free}, {d_counts, 8},
                             {d_block_table, table}, {d_lengths, 4ull * n_requests}, {d_free, 4ull * n_free}};
   if (!outputs_apart(extents, 4, 7)) return FIKIT_INVALID_ARG;
-  const CompactParts parts(n_blocks);
-  if (workspace_bytes < parts.bytes) return FIKIT_WORKSPACE_TOO_SMALL;
   BlocksArgs a = blocks_args(d_block_table, table_width, d_lengths, n_requests, block_tokens, n_blocks, d_free, n_free, d_status);
-  const auto part = [&](uint64_t at) { return reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(d_workspace) + at); };
   a.new_table = d_new_table;
   a.copies = reinterpret_cast<int2*>(d_copies);
   a.new_free = d_new_free;
   a.counts = d_counts;
+  a.room = room;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (const uint32_t groups = one_launch(n_requests, 0, n_requests, table_width, n_blocks))
+    return enqueue(k_compact_one, dim3(groups), dim3(BLOCKS_THREADS), st, a);
+  const CompactParts parts(n_blocks);
+  if (!d_workspace || !aligned(d_workspace, 256)) return FIKIT_INVALID_ARG;
+  if (workspace_bytes < parts.bytes) return FIKIT_WORKSPACE_TOO_SMALL;
+  const auto part = [&](uint64_t at) { return reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(d_workspace) + at); };
   a.words_of_call = part(0);
   a.flags = reinterpret_cast<uint8_t*>(part(parts.flags));
   a.flags_too = reinterpret_cast<uint8_t*>(part(parts.flags_too));
   a.marks = part(parts.marks);
   a.marks_too = part(parts.marks_too);
   a.before = part(parts.before);
-  a.room = room;
-  hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  if (const uint32_t groups = one_launch(n_requests, 0, n_requests, table_width, n_blocks))
-    return enqueue(k_compact_one, dim3(groups), dim3(BLOCKS_THREADS), st, a);
   const dim3 rows(ROW_WAVES * WAVE);
   const uint32_t waves = n_requests + (n_free + WAVE - 1) / WAVE;
   if (int rc = enqueue(k_compact_begin, clear_groups(a.words), dim3(BLOCKS_THREADS), st, a)) return rc;

@@ -420,7 +420,7 @@ PyObject* py_cache_fork(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
       new_free = ints.take({n_blocks});
       counts = ints.take({3});
     }
-    const at::Tensor ws = workspace_of(workspace, cache_fork_workspace_bytes(n, children, n_blocks), device);
+    const at::Tensor ws = workspace_of(workspace, cache_fork_workspace_bytes(n, children, width, n_blocks), device);
     rc = cache_fork(dense<int32_t>(table, at::kInt, device, "block_table"), width, dense<int32_t>(lengths, at::kInt, device, "lengths"), n,
                     dense<int32_t>(parents, at::kInt, device, "parents"), children, block_tokens, n_blocks,
                     dense<int32_t>(free, at::kInt, device, "free_blocks"), count(free.numel(), "free_blocks"),
@@ -467,7 +467,7 @@ PyObject* py_cache_compact(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
       new_free = ints.take({n_free});
       counts = ints.take({2});
     }
-    const at::Tensor ws = workspace_of(workspace, cache_compact_workspace_bytes(n, n_blocks), device);
+    const at::Tensor ws = workspace_of(workspace, cache_compact_workspace_bytes(n, width, n_blocks), device);
     rc = cache_compact(dense<int32_t>(table, at::kInt, device, "block_table"), width, dense<int32_t>(lengths, at::kInt, device, "lengths"), n, block_tokens,
                        n_blocks, dense<int32_t>(free, at::kInt, device, "free_blocks"), n_free, dense<int32_t>(new_table, at::kInt, device, "out"),
                        dense<fikit_block_copy>(copies, at::kInt, device, "out"), dense<int32_t>(new_free, at::kInt, device, "out"),

@@ -103,9 +103,10 @@ SHARED = [
     (dict(table=NULL), INVALID), (dict(table=0x1000002), INVALID), (dict(lengths=NULL), INVALID), (dict(lengths=ODD), INVALID), (dict(free=NULL), INVALID),
     (dict(free=ODD), INVALID), (dict(n_free=101), INVALID), (dict(n_blocks=0), INVALID), (dict(new_table=NULL), INVALID), (dict(new_table=ODD), INVALID),
     (dict(copies=NULL), INVALID), (dict(copies=0x7000004), INVALID), (dict(new_free=NULL), INVALID), (dict(new_free=ODD), INVALID), (dict(counts=NULL), INVALID),
-    (dict(counts=ODD), INVALID), (dict(status=NULL), INVALID), (dict(status=ODD), INVALID), (dict(ws=NULL), INVALID), (dict(ws=0xb000010), INVALID),
+    (dict(counts=ODD), INVALID), (dict(status=NULL), INVALID), (dict(status=ODD), INVALID), (dict(n=2000, ws=NULL), INVALID), (dict(n_blocks=40000, ws=0xb000010), INVALID),
     (dict(width=1 << 31), INVALID), (dict(new_table=0x1000000), INVALID), (dict(new_free=0x4000000), INVALID), (dict(new_free=0x4000000 + 32), INVALID),
-    (dict(counts=0x2000000), INVALID), (dict(copies=0x5000000), INVALID), (dict(ws_bytes=256), SMALL), (dict(block=8), UNSUPPORTED), (dict(block=0), UNSUPPORTED),
+    (dict(counts=0x2000000), INVALID), (dict(copies=0x5000000), INVALID), (dict(n=2000, ws_bytes=256), SMALL), (dict(n_blocks=40000, ws_bytes=256), SMALL),
+    (dict(block=8), UNSUPPORTED), (dict(block=0), UNSUPPORTED),
     (dict(block=48), UNSUPPORTED), (dict(block=512), UNSUPPORTED), (dict(n=16385), UNSUPPORTED), (dict(n_blocks=(1 << 20) + 1), UNSUPPORTED)]
 
 
@@ -122,7 +123,8 @@ def test_compact(change, want):
 
 def test_block_workspaces():
     for f, sizes in ((binding.fikit_cache_fork_workspace_bytes, (7, 9)), (binding.fikit_cache_compact_workspace_bytes, (7,))):
-        assert 0 < f(*sizes, 1) <= f(*sizes, 1 << 20) and f(*sizes, (1 << 20) + 1) == 0 and f(*(16385 for _ in sizes), 5) == 0
+        assert f(*sizes, 100, 1000) == 0 and 0 < f(*sizes, 100, 40000) <= f(*sizes, 100, 1 << 20) and 0 < f(*sizes, 10000, 1000)
+        assert f(*sizes, 100, (1 << 20) + 1) == 0 and f(*(16385 for _ in sizes), 100, 5) == 0 and f(*(2000 for _ in sizes), 1, 5) > 0
 
 
 def cache(**change):

@@ -267,8 +267,8 @@ def test_replayed_and_on_another_stream():
     torch.cuda.current_stream().wait_stream(side)
     assert all(torch.equal(a, b) for a, b in zip((*first, *second), (*again, *other)))
     forked, compacted = binding.CacheFork(*(torch.empty_like(x) for x in first)), binding.CacheCompaction(*(torch.empty_like(x) for x in second))
-    ws = [torch.empty(max(256, n), dtype=torch.uint8, device=DEV) for n in (binding.fikit_cache_fork_workspace_bytes(30, 50, n_blocks),
-                                                                           binding.fikit_cache_compact_workspace_bytes(30, n_blocks))]
+    ws = [torch.empty(max(256, n), dtype=torch.uint8, device=DEV) for n in (binding.fikit_cache_fork_workspace_bytes(30, 50, len(table[0]), n_blocks),
+                                                                           binding.fikit_cache_compact_workspace_bytes(30, len(table[0]), n_blocks))]
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         binding.fikit_cache_fork(t, l, p, 16, n_blocks, f, status, out=forked, workspace_buf=ws[0])
