@@ -293,7 +293,7 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_end(BlocksArgs a) {
 // ---- one launch -------------------------------------------------------------------------------------------------
 //
 // Up to ONE_REQUESTS requests and children, ONE_BLOCKS blocks and ONE_CELLS entries of the table, with bitmaps in LDS: every workgroup marks all blocks for
-// itself and writes its share of the outputs, so that none waits for another.  128 beams of 32 prompts 6.7 us, their compaction 8.0; in the launches that
+// itself and writes its share of the outputs, so that none waits for another.  128 beams of 32 prompts 6.0 us, their compaction 6.0; in the launches that
 // larger sizes take, 13 and 16.
 
 constexpr uint32_t ONE_REQUESTS = BLOCKS_THREADS, ONE_BLOCKS = 32 * BLOCKS_THREADS, ONE_CELLS = 65536, ONE_MOST_GROUPS = 64;
