@@ -67,6 +67,8 @@ bool in_place(const fikit_vectors* in, const fikit_vectors* out, uint32_t heads,
   return in->d_data == out->d_data && (heads <= 1 || in->head_stride == out->head_stride) && (n_tokens <= 1 || in->token_stride == out->token_stride);
 }
 
+uint64_t slices_of(uint32_t n_blocks) { return ((n_blocks + 31ull) / 32 + SLICE - 1) / SLICE; }
+
 // Parts of the workspace of a fork or a compaction, one behind the other, in words.
 struct Parts {
   uint64_t bytes = 0;
@@ -77,27 +79,29 @@ struct Parts {
   }
 };
 struct ForkParts : Parts {
-  uint64_t words, flags, flags_too, marks, marks_too, first, rank, wants;
+  uint64_t words, flags, flags_too, marks, sums, first, rank, wants;
   ForkParts(uint32_t n_requests, uint32_t n_children, uint32_t n_blocks) : words((n_blocks + 31) / 32) {
     take(1);
     flags = take(8 * words);
     flags_too = take(8 * words);
-    marks = take(words);
-    marks_too = take(words);
+    marks = take(SLICE * slices_of(n_blocks));
+    sums = take(slices_of(n_blocks));
     first = take(n_requests);
     rank = take(n_children);
     wants = take(n_children);
   }
 };
 struct CompactParts : Parts {
-  uint64_t words, flags, flags_too, marks, marks_too, before;
+  uint64_t words, flags, flags_too, marks, marks_too, sums, sums_too, before;
   explicit CompactParts(uint32_t n_blocks) : words((n_blocks + 31) / 32) {
     take(2);
     flags = take(8 * words);
     flags_too = take(8 * words);
-    marks = take(words);
-    marks_too = take(words);
-    before = take(words);
+    marks = take(SLICE * slices_of(n_blocks));
+    marks_too = take(SLICE * slices_of(n_blocks));
+    sums = take(slices_of(n_blocks));
+    sums_too = take(slices_of(n_blocks));
+    before = take(SLICE * slices_of(n_blocks));
   }
 };
 
@@ -198,7 +202,6 @@ struct ScoresCall {
 bool logits_ok(int32_t value_type) { return type_ok(value_type) || value_type == FIKIT_F32; }
 
 dim3 clear_groups(uint32_t words) { return dim3((2 * words + BLOCKS_THREADS - 1) / BLOCKS_THREADS); }        // 16 flags of both kinds to a thread
-int pack(const BlocksArgs& a, hipStream_t st) { return enqueue(k_blocks_pack, clear_groups(a.words), dim3(BLOCKS_THREADS), st, a); }
 constexpr uint32_t COPY_GROUPS = 16384;
 
 }  // namespace
@@ -243,15 +246,16 @@ int fikit_cache_fork(const int32_t* d_block_table, uint32_t table_width, const i
   a.flags = reinterpret_cast<uint8_t*>(part(parts.flags));
   a.flags_too = reinterpret_cast<uint8_t*>(part(parts.flags_too));
   a.marks = part(parts.marks);
-  a.marks_too = part(parts.marks_too);
+  a.sums = part(parts.sums);
   a.first = part(parts.first);
   a.rank = reinterpret_cast<int32_t*>(part(parts.rank));
   a.wants = part(parts.wants);
   if (int rc = enqueue(k_fork_begin, dim3(1 + clear_groups(a.words).x), dim3(BLOCKS_THREADS), st, a)) return rc;
   if (const uint32_t rows = n_requests + n_children)
     if (int rc = enqueue(k_fork_rows, dim3((rows + ROW_WAVES - 1) / ROW_WAVES), dim3(ROW_WAVES * WAVE), st, a)) return rc;
-  if (int rc = pack(a, st)) return rc;
-  return enqueue(k_fork_end, dim3((a.words + SLICE - 1) / SLICE), dim3(BLOCKS_THREADS), st, a);
+  const uint32_t slices = static_cast<uint32_t>(slices_of(n_blocks));
+  if (int rc = enqueue(k_blocks_pack<true>, dim3(slices), dim3(SLICE), st, a)) return rc;
+  return enqueue(k_fork_end, dim3(slices * SLICE_WAVES / ROW_WAVES), dim3(ROW_WAVES * WAVE), st, a);
 }
 
 size_t fikit_cache_compact_workspace_bytes(uint32_t n_requests, uint32_t table_width, uint32_t n_blocks) {
@@ -289,14 +293,17 @@ int fikit_cache_compact(const int32_t* d_block_table, uint32_t table_width, cons
   a.flags_too = reinterpret_cast<uint8_t*>(part(parts.flags_too));
   a.marks = part(parts.marks);
   a.marks_too = part(parts.marks_too);
+  a.sums = part(parts.sums);
+  a.sums_too = part(parts.sums_too);
   a.before = part(parts.before);
   const dim3 rows(ROW_WAVES * WAVE);
+  const uint32_t slices = static_cast<uint32_t>(slices_of(n_blocks));
   const uint32_t waves = n_requests + (n_free + WAVE - 1) / WAVE;
   if (int rc = enqueue(k_compact_begin, clear_groups(a.words), dim3(BLOCKS_THREADS), st, a)) return rc;
   if (waves > 0)
     if (int rc = enqueue(k_compact_mark, dim3((waves + ROW_WAVES - 1) / ROW_WAVES), rows, st, a)) return rc;
-  if (int rc = pack(a, st)) return rc;
-  if (int rc = enqueue(k_compact_lists, dim3((a.words + SLICE - 1) / SLICE), dim3(BLOCKS_THREADS), st, a)) return rc;
+  if (int rc = enqueue(k_blocks_pack<false>, dim3(slices), dim3(SLICE), st, a)) return rc;
+  if (int rc = enqueue(k_compact_lists, dim3(slices * SLICE_WAVES / ROW_WAVES), rows, st, a)) return rc;
   return n_requests > 0 ? enqueue(k_compact_rows, dim3((n_requests + ROW_WAVES - 1) / ROW_WAVES), rows, st, a) : FIKIT_OK;
 }
 

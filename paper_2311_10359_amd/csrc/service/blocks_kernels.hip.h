@@ -23,10 +23,12 @@ struct BlocksArgs {
   int32_t* new_free;
   int32_t* counts;
   int32_t* status;
-  uint32_t* marks;          // bitmaps; fork: blocks of requests that nobody continues; compaction: used blocks
-  uint32_t* marks_too;      // fork: blocks of the others; compaction: free ones
-  uint8_t* flags;           // the same with a byte for each block, in whole words of the bitmaps
-  uint8_t* flags_too;
+  uint8_t* flags;           // a byte for each block, in whole words of the bitmaps; fork: blocks of requests that nobody continues; compaction: used blocks
+  uint8_t* flags_too;       // fork: blocks of the others; compaction: free ones
+  uint32_t* marks;          // bitmaps, in whole slices; fork: blocks given back; compaction: used blocks
+  uint32_t* marks_too;      // compaction: free blocks
+  uint32_t* sums;           // [slices]: how many of them are marked in a slice
+  uint32_t* sums_too;
   uint32_t* first;          // fork, [n_requests]: a request's first child, or NO_CHILD
   int32_t* rank;            // fork, [n_children]: a child's place among those that need a block for a copy, or -1
   uint32_t* wants;          // fork, [n_children]: the child of a place
@@ -38,7 +40,8 @@ struct BlocksArgs {
 
 constexpr int BLOCKS_THREADS = 1024, ROW_WAVES = 4;
 constexpr uint32_t BLOCKS_MOST_REQUESTS = 16384, BLOCKS_MOST_BLOCKS = 1u << 20;
-constexpr uint32_t SLICE = 256;                // words of the bitmaps whose blocks a workgroup lists
+constexpr uint32_t SLICE = 256;                // words of the bitmaps that are counted together
+constexpr uint32_t SLICE_WAVES = 16;           // waves that list a slice's blocks
 constexpr uint32_t NO_CHILD = 0xffffffffu;
 
 __device__ __forceinline__ uint32_t pages_of(const BlocksArgs& a, uint32_t length) { return (length + (1u << a.shift) - 1) >> a.shift; }
@@ -67,42 +70,78 @@ __device__ __forceinline__ uint32_t packed(const uint8_t* flags, uint32_t word) 
   }
   return bits;
 }
-__global__ __launch_bounds__(BLOCKS_THREADS) void k_blocks_pack(BlocksArgs a) {
-  const uint32_t i = blockIdx.x * BLOCKS_THREADS + threadIdx.x;
-  if (i < a.words) a.marks[i] = packed(a.flags, i);
-  else if (i < 2 * a.words) a.marks_too[i - a.words] = packed(a.flags_too, i - a.words);
+// A slice in a workgroup, with how many are marked in it, so that who lists them reads a number for each slice and the words of its own.  (Lists for which each
+// workgroup added up all words took 7.7 us for a fork and 9.3 for a compaction, these take 4.1 and 5.2.)
+template <bool FORK>
+__global__ __launch_bounds__(SLICE) void k_blocks_pack(BlocksArgs a) {
+  __shared__ uint32_t waves[SLICE / WAVE];
+  const uint32_t w = blockIdx.x * SLICE + threadIdx.x;
+  uint32_t marks = 0, marks_too = 0;
+  if (w < a.words) {
+    marks = packed(a.flags, w);
+    marks_too = packed(a.flags_too, w);
+  }
+  if constexpr (FORK) {
+    marks &= ~marks_too;
+    marks_too = 0;
+  } else {
+    if ((marks & marks_too) && !stopped(a.status)) *a.status = FIKIT_INVALID_ARG;        // used and free
+    a.marks_too[w] = marks_too;
+  }
+  a.marks[w] = marks;
+  const uint32_t sum = sum_over_wave(__popc(marks) << 16 | __popc(marks_too));       // (up to 8192 each)
+  if (lane_id() == 0) waves[threadIdx.x / WAVE] = sum;
+  __syncthreads();
+  if (threadIdx.x > 0) return;
+  uint32_t all = 0;
+  for (uint32_t i = 0; i < SLICE / WAVE; ++i) all += waves[i];
+  a.sums[blockIdx.x] = all >> 16;
+  if constexpr (!FORK) a.sums_too[blockIdx.x] = all & 0xffffu;
 }
 
-// The words of the bitmaps that a thread of a workgroup looks at, neighbours, in its registers.
-constexpr int WORDS_MOST = BLOCKS_MOST_BLOCKS / 32 / BLOCKS_THREADS;
-struct Words {
-  uint32_t from, count, marks[WORDS_MOST], marks_too[WORDS_MOST];
+// The counts of all slices in a wave, two neighbours to a lane.
+struct SliceSums {
+  static_assert(BLOCKS_MOST_BLOCKS / 32 / SLICE <= 2 * WAVE, "two slices to a lane");
+  uint32_t first, both, total, before;                // of the lane's slices, of all, of those before the lane's
 
-  __device__ __forceinline__ explicit Words(const BlocksArgs& a) {
-    const uint32_t per = (a.words + BLOCKS_THREADS - 1) / BLOCKS_THREADS;
-    from = min_u32(threadIdx.x * per, a.words);
-    count = min_u32(per, a.words - from);
-#pragma unroll
-    for (uint32_t i = 0; i < WORDS_MOST; i += 8)
-      if (i < per)                         // (the same in the workgroup: eight loads of each on their way)
-#pragma unroll
-        for (uint32_t j = i; j < i + 8; ++j) {
-          marks[j] = j < count ? a.marks[from + j] : 0;
-          marks_too[j] = j < count ? a.marks_too[from + j] : 0;
-        }
+  __device__ __forceinline__ SliceSums(const BlocksArgs& a, const uint32_t* sums) {
+    const uint32_t at = 2 * lane_id(), slices = (a.words + SLICE - 1) / SLICE;
+    first = at < slices ? sums[at] : 0;
+    both = first + (at + 1 < slices ? sums[at + 1] : 0);
   }
-  // f(word, its marks, its other marks)
-  template <typename F>
-  __device__ __forceinline__ void each(const BlocksArgs& a, F f) const {
-    const uint32_t per = (a.words + BLOCKS_THREADS - 1) / BLOCKS_THREADS;
-#pragma unroll
-    for (uint32_t i = 0; i < WORDS_MOST; i += 8)
-      if (i < per)
-#pragma unroll
-        for (uint32_t j = i; j < i + 8; ++j)
-          if (j < count) f(from + j, marks[j], marks_too[j]);
+  __device__ __forceinline__ void add_up() {
+    const uint32_t upto = wave_incl_scan_u32(both);
+    before = upto - both;
+    total = read_lane_u32(upto, WAVE - 1);
+  }
+  __device__ __forceinline__ uint32_t before_slice(uint32_t slice) const {
+    return read_lane_u32(slice & 1 ? before + first : before, slice / 2);
   }
 };
+
+// A slice's words in a wave, four neighbours to a lane.
+struct SliceWords {
+  u32x4 marks;
+  uint32_t before;                                    // marked ones before the lane's
+
+  __device__ __forceinline__ SliceWords(const uint32_t* words, uint32_t slice) : marks(reinterpret_cast<const u32x4*>(words)[slice * WAVE + lane_id()]) {}
+  __device__ __forceinline__ void add_up(uint32_t before_slice) {
+    const uint32_t mine = __popc(marks[0]) + __popc(marks[1]) + __popc(marks[2]) + __popc(marks[3]);
+    before = before_slice + wave_incl_scan_u32(mine) - mine;
+  }
+};
+
+// The words that each wave lists, two at a time: a lane's word of both, and the marked ones before the lane's block.
+constexpr uint32_t WAVE_WORDS = SLICE / SLICE_WAVES;
+__device__ __forceinline__ uint32_t word_of(const SliceWords& s, uint32_t first, uint32_t pair, uint32_t& before) {
+  const uint32_t e = 2 * pair % 4, from = first / 4 + pair / 2, lane = lane_id();
+  uint32_t until = s.before;
+  if (e == 2) until += __popc(s.marks[0]) + __popc(s.marks[1]);
+  const uint32_t low = read_lane_u32(s.marks[e], from), high = read_lane_u32(s.marks[e + 1], from), at = read_lane_u32(until, from);
+  const uint32_t word = lane < 32 ? low : high;
+  before = at + (lane < 32 ? 0 : __popc(low)) + __popc(word & ((1u << lane % 32) - 1));
+  return word;
+}
 
 // f(page, entry) for the first `pages` entries of a row, by a wave, several loads on their way; from page `first` on.
 template <typename F>
@@ -122,8 +161,8 @@ __device__ __forceinline__ void each_page(const int32_t* entries, uint32_t pages
 // ---- fork -------------------------------------------------------------------------------------------------------
 //
 // Child i continues request parents[i].  The first child keeps the parent's last block if that is not full, each later one needs a block:
-// its place among those is a prefix sum over the children.  8192 children of 4096 requests over 107,000 blocks: 23 us in four launches.  Blocks to take come from the front of (free blocks, blocks given back in
-// ascending order); what is left of the two is the new list.
+// its place among those is a prefix sum over the children.  8192 children of 4096 requests over 107,000 blocks: 19 us in four launches.  Blocks to take come from the front of (free blocks, blocks given back in
+// ascending order); what is left of the two is the new list.  The kernels of both calls load what they may before they look at the status.
 
 // The children, in one workgroup; the others clear the bitmaps.
 __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_begin(BlocksArgs a) {
@@ -132,9 +171,10 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_begin(BlocksArgs a) {
     clear_flags(a, (blockIdx.x - 1) * BLOCKS_THREADS + threadIdx.x, (gridDim.x - 1) * BLOCKS_THREADS);
     return;
   }
-  if (stopped(a.status)) return;               // (nobody else writes it in this launch)
+  const bool stop = stopped(a.status);         // (nobody else writes it in this launch)
   constexpr uint32_t PER = BLOCKS_MOST_REQUESTS / BLOCKS_THREADS, WAVES = BLOCKS_THREADS / WAVE;      // PER: requests and children of a thread, whose
   bool bad = false;                                                                                  // loads are on their way at once
+  const uint32_t wave = uniform(threadIdx.x / WAVE);
   int32_t lengths[PER], parents[PER];
 #pragma unroll
   for (uint32_t i = 0; i < PER; ++i) {
@@ -142,6 +182,7 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_begin(BlocksArgs a) {
     lengths[i] = at < a.n_requests ? a.lengths[at] : 0;
     parents[i] = at < a.n_children ? a.parents[at] : -1;
   }
+  if (stop) return;
 #pragma unroll
   for (uint32_t i = 0; i < PER; ++i) {
     const uint32_t at = i * BLOCKS_THREADS + threadIdx.x;
@@ -160,7 +201,6 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_begin(BlocksArgs a) {
   __syncthreads();
   for (uint32_t r = threadIdx.x; r < a.n_requests; r += BLOCKS_THREADS) a.first[r] = first[r];
   // how many of each 64 children need a block, then the sums of the 64s before: a child's place
-  const uint32_t wave = uniform(threadIdx.x / WAVE);
   uint64_t needs[PER];
 #pragma unroll
   for (uint32_t i = 0; i < PER; ++i) {
@@ -178,7 +218,6 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_begin(BlocksArgs a) {
     const uint32_t c = i * BLOCKS_THREADS + threadIdx.x, place = sums[i * WAVES + wave] + popc_below(needs[i]);
     if (c < a.n_children) {
       const bool need = needs[i] >> lane_id() & 1;
-      a.new_lengths[c] = lengths[i];
       a.rank[c] = need ? static_cast<int32_t>(place) : -1;
       if (need) a.wants[place] = c;
     }
@@ -188,11 +227,12 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_begin(BlocksArgs a) {
 
 // A wave for each request, which marks its blocks, and for each child, which writes its row.
 __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_fork_rows(BlocksArgs a) {
-  if (stopped(a.status)) return;
+  const bool stop = stopped(a.status);
   const uint32_t lane = lane_id(), row = blockIdx.x * ROW_WAVES + uniform(threadIdx.x / WAVE);
   if (row < a.n_requests) {
-    const uint32_t pages = pages_of(a, static_cast<uint32_t>(a.lengths[row]));
-    uint8_t* flags = a.first[row] == NO_CHILD ? a.flags : a.flags_too;
+    const uint32_t pages = pages_of(a, static_cast<uint32_t>(a.lengths[row])), first = a.first[row];
+    if (stop) return;
+    uint8_t* flags = first == NO_CHILD ? a.flags : a.flags_too;
     const int32_t* entries = a.table + static_cast<uint64_t>(row) * a.width;
     each_page(entries, pages, [&](uint32_t, int32_t entry) {
       const uint32_t block = static_cast<uint32_t>(entry);
@@ -204,7 +244,10 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_fork_rows(BlocksArgs a) {
   const uint32_t c = row - a.n_requests;
   if (c >= a.n_children) return;
   const int32_t p = a.parents[c], rank = a.rank[c];
-  const uint32_t pages = p >= 0 ? pages_of(a, static_cast<uint32_t>(a.lengths[p])) : 0;
+  if (stop) return;
+  const int32_t length = p >= 0 ? a.lengths[p] : 0;
+  if (lane == 0) a.new_lengths[c] = length;
+  const uint32_t pages = pages_of(a, static_cast<uint32_t>(length));
   const int32_t* entries = a.table + static_cast<uint64_t>(p >= 0 ? p : 0) * a.width;
   int32_t* out = a.new_table + static_cast<uint64_t>(c) * a.width;
   each_page(entries, pages, [&](uint32_t page, int32_t block) {
@@ -221,71 +264,42 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_fork_rows(BlocksArgs a) {
   for (uint32_t page = pages + lane; page < a.width; page += WAVE) out[page] = -1;
 }
 
-// The sums of N counts over the words of the bitmaps, in every workgroup: those of the words before a thread's and before each word of the workgroup's
-// slice, in LDS with the words themselves, and of all words.  count(marks, other marks, out) gives the counts of a word.
-template <int N>
-struct WordSums {
-  uint32_t before[SLICE][N], marks[SLICE], marks_too[SLICE];
-  uint32_t scan[BLOCKS_THREADS / WAVE];
-};
-template <int N, typename F>
-__device__ __forceinline__ void word_sums(const BlocksArgs& a, const Words& words, uint32_t slice, WordSums<N>* lds, uint32_t (&mine)[N], uint32_t (&total)[N],
-                                          F count) {
-  uint32_t sums[N] = {}, at[N];
-  words.each(a, [&](uint32_t, uint32_t m, uint32_t n) {
-    uint32_t of[N];
-    count(m, n, of);
-    for (int i = 0; i < N; ++i) sums[i] += of[i];
-  });
-  for (int i = 0; i < N; ++i) at[i] = mine[i] = block_excl_scan_1024(sums[i], lds->scan, total[i]);
-  if (words.from < slice + SLICE && words.from + words.count > slice)
-    words.each(a, [&](uint32_t w, uint32_t m, uint32_t n) {
-      if (w >= slice && w < slice + SLICE) {
-        for (int i = 0; i < N; ++i) lds->before[w - slice][i] = at[i];
-        lds->marks[w - slice] = m;
-        lds->marks_too[w - slice] = n;
-      }
-      uint32_t of[N];
-      count(m, n, of);
-      for (int i = 0; i < N; ++i) at[i] += of[i];
-    });
-  __syncthreads();
-}
-
-// The lists.
-__global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_end(BlocksArgs a) {
-  __shared__ WordSums<1> sums;
-  if (__syncthreads_or(stopped(a.status))) return;
-  const uint32_t slice = blockIdx.x * SLICE, taken = a.words_of_call[0];
-  uint32_t mine[1], given[1];
-  const Words words(a);
-  word_sums<1>(a, words, slice, &sums, mine, given, [](uint32_t m, uint32_t n, uint32_t (&of)[1]) { of[0] = __popc(m & ~n); });
-  const uint32_t total = a.n_free + given[0];          // (below 2^32: n_free is at most n_blocks)
-  if (taken > total || total - taken > a.n_blocks) {   // (too few; or a list that names blocks in use)
-    if (threadIdx.x == 0) *a.status = taken > total ? FIKIT_CACHE_FULL : FIKIT_INVALID_ARG;
+// The lists, in waves that do not wait for one another.
+__global__ __launch_bounds__(ROW_WAVES * WAVE) void k_fork_end(BlocksArgs a) {
+  const bool stop = stopped(a.status);
+  const uint32_t row = blockIdx.x * ROW_WAVES + uniform(threadIdx.x / WAVE), slice = row / SLICE_WAVES, word = row % SLICE_WAVES * WAVE_WORDS;
+  const uint32_t lane = lane_id(), taken = a.words_of_call[0];
+  SliceSums sums(a, a.sums);
+  SliceWords words(a.marks, slice);
+  if (stop) return;
+  sums.add_up();
+  words.add_up(sums.before_slice(slice));
+  const uint32_t given = sums.total, total = a.n_free + given;          // (below 2^32: n_free is at most n_blocks)
+  if (taken > total || total - taken > a.n_blocks) {                    // (too few; or a list that names blocks in use)
+    if (lane == 0) *a.status = taken > total ? FIKIT_CACHE_FULL : FIKIT_INVALID_ARG;
     return;
   }
-  for (uint32_t i = threadIdx.x; i < SLICE * 32; i += BLOCKS_THREADS) {
-    const uint32_t w = slice + i / 32;
-    if (w >= a.words) break;
-    const uint32_t marks = sums.marks[i / 32] & ~sums.marks_too[i / 32], bit = 1u << i % 32;
-    if (!(marks & bit)) continue;
-    const uint32_t place = a.n_free + sums.before[i / 32][0] + __popc(marks & (bit - 1)), block = w * 32 + i % 32;
-    if (place >= taken) {
+#pragma unroll
+  for (uint32_t pair = 0; pair < WAVE_WORDS / 2; ++pair) {
+    uint32_t place;
+    const bool is_given = word_of(words, word, pair, place) >> lane % 32 & 1;
+    const uint32_t block = (slice * SLICE + word + 2 * pair) * 32 + lane;
+    place += a.n_free;
+    if (is_given && place >= taken) {
       a.new_free[place - taken] = static_cast<int32_t>(block);
-    } else {
+    } else if (is_given) {
       const uint32_t c = a.wants[place];
       a.copies[place].y = static_cast<int32_t>(block);
       a.new_table[static_cast<uint64_t>(c) * a.width + pages_of(a, static_cast<uint32_t>(a.new_lengths[c])) - 1] = static_cast<int32_t>(block);
     }
   }
-  const uint32_t from = blockIdx.x * BLOCKS_THREADS + threadIdx.x, stride = gridDim.x * BLOCKS_THREADS;
+  const uint32_t from = blockIdx.x * ROW_WAVES * WAVE + threadIdx.x, stride = gridDim.x * ROW_WAVES * WAVE;
   for (uint32_t i = taken + from; i < a.n_free; i += stride) a.new_free[i - taken] = a.free_blocks[i];
   for (uint32_t i = total - taken + from; i < a.n_blocks; i += stride) a.new_free[i] = -1;
   for (uint32_t i = taken + from; i < a.n_children; i += stride) a.copies[i] = make_int2(-1, -1);
   if (from == 0) {
     a.counts[0] = static_cast<int32_t>(taken);
-    a.counts[1] = static_cast<int32_t>(given[0]);
+    a.counts[1] = static_cast<int32_t>(given);
     a.counts[2] = static_cast<int32_t>(total - taken);
   }
 }
@@ -427,7 +441,7 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_one(BlocksArgs a) {
 // ---- compaction -------------------------------------------------------------------------------------------------
 //
 // Used and free blocks together, ascending: behind the first n_used of them lies the border.  The k-th used block behind the border goes
-// to the k-th free one before it, and what lies behind it is the new free list.  3001 requests over 177,000 blocks: 22 us in five launches.
+// to the k-th free one before it, and what lies behind it is the new free list.  3001 requests over 177,000 blocks: 19 us in five launches.
 
 __global__ __launch_bounds__(BLOCKS_THREADS) void k_compact_begin(BlocksArgs a) {
   clear_flags(a, blockIdx.x * BLOCKS_THREADS + threadIdx.x, gridDim.x * BLOCKS_THREADS);
@@ -435,10 +449,11 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_compact_begin(BlocksArgs a) 
 
 // A wave for each request marks its blocks; the waves behind them the free ones, 64 each.
 __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_compact_mark(BlocksArgs a) {
-  if (stopped(a.status)) return;
+  const bool stop = stopped(a.status);
   const uint32_t lane = lane_id(), row = blockIdx.x * ROW_WAVES + uniform(threadIdx.x / WAVE);
   if (row < a.n_requests) {
     const int32_t length = a.lengths[row];
+    if (stop) return;
     if (!length_ok(a, length)) {
       *a.status = FIKIT_INVALID_ARG;
       return;
@@ -455,6 +470,7 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_compact_mark(BlocksArgs a)
   const uint32_t i = (row - a.n_requests) * WAVE + lane;
   if (i >= a.n_free) return;
   const uint32_t block = static_cast<uint32_t>(a.free_blocks[i]);
+  if (stop) return;
   if (block < a.n_blocks) a.flags_too[block] = 1;
   else *a.status = FIKIT_INVALID_ARG;
 }
@@ -473,47 +489,68 @@ __device__ __forceinline__ void find_border(uint32_t w, uint32_t marks, uint32_t
   lds->used = used + __popc(marks & below);
 }
 
-__global__ __launch_bounds__(BLOCKS_THREADS) void k_compact_lists(BlocksArgs a) {
-  __shared__ WordSums<2> sums;
-  __shared__ Border border;
-  if (__syncthreads_or(stopped(a.status))) return;
-  const uint32_t slice = blockIdx.x * SLICE;
-  uint32_t mine[2], total[2], both = 0;
-  const Words words(a);
-  word_sums<2>(a, words, slice, &sums, mine, total, [&](uint32_t m, uint32_t n, uint32_t (&of)[2]) {
-    of[0] = __popc(m);
-    of[1] = __popc(n);
-    both |= m & n;
-  });
-  if (threadIdx.x == 0 && total[0] == 0) border = Border{0, 0};
-  if (mine[0] + mine[1] < total[0])
-    words.each(a, [&](uint32_t w, uint32_t m, uint32_t n) {
-      find_border(w, m, n, mine[0], mine[0] + mine[1], total[0], &border);
-      mine[0] += __popc(m);
-      mine[1] += __popc(n);
-    });
-  if (__syncthreads_or(both != 0) || total[1] != a.n_free) {       // a block that is used and free, or free twice
-    if (threadIdx.x == 0) *a.status = FIKIT_INVALID_ARG;
+// The border, in a wave: in the slice, the lane's four words and the word in which used and free blocks come to `total`.
+__device__ __forceinline__ Border border_of(const BlocksArgs& a, const SliceSums& used, const SliceSums& spare, uint32_t total) {
+  if (total == 0) return Border{0, 0};
+  const uint32_t lane = lane_id(), upto = used.before + spare.before;
+  const uint32_t at = static_cast<uint32_t>(__builtin_ctzll(ballot(upto < total && upto + used.both + spare.both >= total)));
+  const uint32_t slice = 2 * at + (read_lane_u32(upto + used.first + spare.first, at) < total ? 1 : 0);
+  SliceWords marks(a.marks, slice), marks_too(a.marks_too, slice);
+  marks.add_up(used.before_slice(slice));
+  marks_too.add_up(spare.before_slice(slice));
+  const u32x4 of = marks.marks | marks_too.marks;
+  const uint32_t all = marks.before + marks_too.before;
+  const uint32_t in = static_cast<uint32_t>(__builtin_ctzll(ballot(all < total && all + __popc(of[0]) + __popc(of[1]) + __popc(of[2]) + __popc(of[3]) >= total)));
+  uint32_t left = total - read_lane_u32(all, in), before = read_lane_u32(marks.before, in);
+  Border border{0, 0};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t word = read_lane_u32(of[e], in), mine = read_lane_u32(marks.marks[e], in), here = __popc(word);
+    if (left > 0 && left <= here) {
+      const uint32_t bit = static_cast<uint32_t>(__builtin_ctzll(ballot(lane < 32 && (word >> lane % 32 & 1) && __popc(word & ((1u << lane % 32) - 1)) == left - 1)));
+      border.block = (slice * SLICE + 4 * in + e) * 32 + bit + 1;
+      border.used = before + __popc(mine & (bit == 31 ? ~0u : (2u << bit) - 1));
+    }
+    left = left > here ? left - here : 0;
+    before += __popc(mine);
+  }
+  return border;
+}
+
+__global__ __launch_bounds__(ROW_WAVES * WAVE) void k_compact_lists(BlocksArgs a) {
+  const bool stop = stopped(a.status);
+  const uint32_t row = blockIdx.x * ROW_WAVES + uniform(threadIdx.x / WAVE), slice = row / SLICE_WAVES, word = row % SLICE_WAVES * WAVE_WORDS;
+  const uint32_t lane = lane_id();
+  SliceSums used(a, a.sums), spare(a, a.sums_too);
+  SliceWords marks(a.marks, slice), marks_too(a.marks_too, slice);
+  if (stop) return;
+  used.add_up();
+  spare.add_up();
+  if (spare.total != a.n_free) {                     // free twice
+    if (lane == 0) *a.status = FIKIT_INVALID_ARG;
     return;
   }
-  for (uint32_t i = threadIdx.x; i < SLICE * 32; i += BLOCKS_THREADS) {
-    const uint32_t w = slice + i / 32;
-    if (w >= a.words) break;
-    const uint32_t used = sums.marks[i / 32], spare = sums.marks_too[i / 32], bit = 1u << i % 32, block = w * 32 + i % 32;
-    const uint32_t used_before = sums.before[i / 32][0] + __popc(used & (bit - 1)), spare_before = sums.before[i / 32][1] + __popc(spare & (bit - 1));
-    if (i % 32 == 0) a.before[w] = used_before;
+  const Border border = border_of(a, used, spare, used.total);
+  marks.add_up(used.before_slice(slice));
+  marks_too.add_up(spare.before_slice(slice));
+#pragma unroll
+  for (uint32_t pair = 0; pair < WAVE_WORDS / 2; ++pair) {
+    uint32_t used_before, spare_before;
+    const uint32_t w = slice * SLICE + word + 2 * pair, block = w * 32 + lane;
+    const bool is_used = word_of(marks, word, pair, used_before) >> lane % 32 & 1, is_spare = word_of(marks_too, word, pair, spare_before) >> lane % 32 & 1;
+    if (lane % 32 == 0) a.before[w + lane / 32] = used_before;
     if (block >= border.block) {
-      if (used & bit) a.copies[used_before - border.used].x = static_cast<int32_t>(block);
-      if ((used | spare) & bit) a.new_free[used_before + spare_before - total[0]] = static_cast<int32_t>(block);
-    } else if (spare & bit) {
+      if (is_used) a.copies[used_before - border.used].x = static_cast<int32_t>(block);
+      if (is_used || is_spare) a.new_free[used_before + spare_before - used.total] = static_cast<int32_t>(block);
+    } else if (is_spare) {
       a.copies[spare_before].y = static_cast<int32_t>(block);
     }
   }
-  const uint32_t moved = total[0] - border.used, from = blockIdx.x * BLOCKS_THREADS + threadIdx.x, stride = gridDim.x * BLOCKS_THREADS;
+  const uint32_t moved = used.total - border.used, from = blockIdx.x * ROW_WAVES * WAVE + threadIdx.x, stride = gridDim.x * ROW_WAVES * WAVE;
   for (uint32_t i = moved + from; i < a.room; i += stride) a.copies[i] = make_int2(-1, -1);
   if (from == 0) {
     a.counts[0] = static_cast<int32_t>(moved);
-    a.counts[1] = static_cast<int32_t>(total[0]);
+    a.counts[1] = static_cast<int32_t>(used.total);
     a.words_of_call[0] = border.block;
     a.words_of_call[1] = border.used;
   }
@@ -521,10 +558,11 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_compact_lists(BlocksArgs a) 
 
 // A wave for each request writes its row.
 __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_compact_rows(BlocksArgs a) {
-  if (stopped(a.status)) return;
+  const bool stop = stopped(a.status);
   const uint32_t lane = lane_id(), row = blockIdx.x * ROW_WAVES + uniform(threadIdx.x / WAVE);
   if (row >= a.n_requests) return;
   const uint32_t border = a.words_of_call[0], used = a.words_of_call[1], pages = pages_of(a, static_cast<uint32_t>(a.lengths[row]));
+  if (stop) return;
   const int32_t* entries = a.table + static_cast<uint64_t>(row) * a.width;
   int32_t* out = a.new_table + static_cast<uint64_t>(row) * a.width;
   each_page(entries, pages, [&](uint32_t page, int32_t entry) {
