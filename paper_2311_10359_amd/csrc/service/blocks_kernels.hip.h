@@ -667,7 +667,7 @@ struct CopyArgs {
 };
 
 __global__ __launch_bounds__(COPY_THREADS) void k_cache_copy(CopyArgs a) {
-  if (stopped(a.status)) return;
+  const bool stop = stopped(a.status);
   const uint32_t rest = blockIdx.x % a.per_copy, side = rest / a.chunks, chunk = rest % a.chunks, lane = lane_id();
   const auto& cache = a.caches[side / 2];
   uint8_t* codes = side % 2 ? cache.v : cache.k;
@@ -676,6 +676,7 @@ __global__ __launch_bounds__(COPY_THREADS) void k_cache_copy(CopyArgs a) {
   for (uint64_t first = blockIdx.x / a.per_copy; first < a.n_copies; first += static_cast<uint64_t>(WAVE) * a.step) {
     const uint64_t mine = first + static_cast<uint64_t>(lane) * a.step;
     const int2 copy = mine < a.n_copies ? a.copies[mine] : make_int2(-1, -1);
+    if (stop) return;
     const bool used = (copy.x & copy.y) != -1;
     const bool bad = used && (static_cast<uint32_t>(copy.x) >= a.n_blocks || static_cast<uint32_t>(copy.y) >= a.n_blocks);
     if (bad) *a.status = FIKIT_INVALID_ARG;

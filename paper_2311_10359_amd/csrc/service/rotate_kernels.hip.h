@@ -69,7 +69,7 @@ template <typename T, int D, bool NEIGHBOURS, bool PAST>
 __global__ __launch_bounds__(ROTATE_WAVES * WAVE) void k_rotate(RotateArgs a) {
   constexpr uint32_t LANES = D / 16, HEADS = WAVE / LANES;
   __shared__ float2 lds[ROTATE_WAVES][D / 2];
-  if (stopped(a.status)) return;
+  const bool stop = stopped(a.status);         // (the first position is on its way meanwhile)
   const uint32_t lane = lane_id(), wave = uniform(threadIdx.x / WAVE), j = lane % LANES;
   const bool turned = 8 * j < a.half;
   // where the lane's chunks begin in a head
@@ -78,6 +78,7 @@ __global__ __launch_bounds__(ROTATE_WAVES * WAVE) void k_rotate(RotateArgs a) {
   for (uint64_t at = static_cast<uint64_t>(blockIdx.x) * ROTATE_WAVES + wave; at < a.units; at += static_cast<uint64_t>(gridDim.x) * ROTATE_WAVES) {
     const uint32_t unit = static_cast<uint32_t>(at), token = unit / a.parts, part = unit % a.parts;
     const int32_t position = static_cast<int32_t>(uniform(static_cast<uint32_t>(a.positions[token])));
+    if (stop) return;
     if (position < 0) continue;
     for (uint32_t p = lane; p < a.half; p += WAVE)
       angles[p] = cos_sin_of_turns(static_cast<double>(position) * static_cast<double>(a.frequencies[p]) * 0.15915494309189533577);

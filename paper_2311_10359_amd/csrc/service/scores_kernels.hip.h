@@ -427,7 +427,6 @@ __global__ __launch_bounds__(W * WAVE) void k_scores(ScoresArgs a) {
   __shared__ float2 firsts[JOIN_ROOM];
   __shared__ float4 sums[W];
   static_assert(W * SCORES_MOST <= JOIN_ROOM && SCORES_MOST * L::VEC <= JOIN_ROOM, "room for the waves' lists, and for their groups' logits");
-  if (__syncthreads_or(stopped(a.status))) return;
   const uint32_t lane = lane_id(), wave = uniform(threadIdx.x / WAVE), r = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
   const Row<L> row(a, r);
   ScoresLds* lds = &lists[wave];
@@ -474,6 +473,7 @@ __global__ __launch_bounds__(W * WAVE) void k_scores(ScoresArgs a) {
       if (seen.n > WAVE) seen.shorten(lds);
     }
   }
+  const bool stop = stopped(a.status);         // (nothing is written before; asked for at the start it costs 0.5 us, and registers if not waited for)
   if (wave == 0) given.x = given_logit(a, row, given.token);
   if (wave == W - 1 && (part == 0 || part == a.parts - 1)) {
     // what is less than a group, a logit to a lane: the head in the first eight lanes, the rest in the next
@@ -493,8 +493,7 @@ __global__ __launch_bounds__(W * WAVE) void k_scores(ScoresArgs a) {
   seen.sum_over_lanes(a.c);
   if (lane == 0) sums[wave] = make_float4(seen.sums.m, seen.sums.s, seen.sums.t, seen.border);
   if (lane < SCORES_MOST) firsts[wave * SCORES_MOST + lane] = lane < seen.n ? make_float2(lds->most[lane], __uint_as_float(lds->group[lane])) : make_float2(-INFINITY, 0.f);
-  __syncthreads();
-  if (wave > 0) return;
+  if (__syncthreads_or(stop) || wave > 0) return;
   // the first wave joins the sums and the lists
   Seen<L> joined(a.n_top);
   const float4 of_wave = lane < W ? sums[lane] : make_float4(LOWEST, 0.f, 0.f, -INFINITY);
