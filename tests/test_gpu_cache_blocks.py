@@ -291,3 +291,76 @@ def test_replayed_and_on_another_stream():
                 for now, w in zip(c, b):
                     w[y] = w[x]
                     assert torch.equal(now, w)
+
+
+def test_borders_of_slices():
+    """More blocks than one launch takes; where the border falls at ends of lanes' words, of words and of counted slices."""
+    rng = np.random.default_rng(12)
+    for n_blocks in (40960, 40961):
+        order = [int(b) for b in rng.permutation(n_blocks)]
+        for n_used in (1, 31, 32, 33, 127, 128, 129, 8191, 8192, 8193, 16384, 24577):
+            for used in (order[:n_used], list(range(n_blocks))[-n_used:], list(range(n_used))):
+                taken = set(used)
+                rest = [b for b in order if b not in taken]
+                check_compact([used], [16 * n_used], 16, n_blocks, rest, n_used)
+                check_compact([used], [16 * n_used], 16, n_blocks, rest[:n_blocks // 3], n_used)
+                check_fork([used], [16 * n_used], [-1], 16, n_blocks, rest, n_used)
+
+
+@pytest.mark.parametrize("n_blocks", [5, 8192, 40000, 1 << 20])
+def test_no_requests(n_blocks):
+    rng = np.random.default_rng(13)
+    free = [int(b) for b in rng.permutation(n_blocks)]
+    for some in (free, free[:n_blocks // 2], []):
+        check_fork([], [], [], 16, n_blocks, some, 3)
+        status = status_word()
+        got = binding.fikit_cache_fork(int32([], 0, 3), int32([]), int32([-1, -1, -1]), 16, n_blocks, int32(some), status)
+        binding.fikit_check_status(status)
+        assert bool((got.block_table == -1).all()) and bool((got.lengths == 0).all()) and bool((got.copies == -1).all())
+        assert got.free_blocks.tolist() == some + [-1] * (n_blocks - len(some)) and got.counts.tolist() == [0, 0, len(some)]
+        check_compact([], [], 16, n_blocks, some, 3)
+
+
+def several_launches(a, children, n_blocks=40000):
+    """A fork and a compaction into outputs with a border, from a workspace that holds anything: (statuses, outputs, are the borders as they were?)."""
+    t, f = int32(a["table"], 2, 2), int32(a["free"])
+    lengths = torch.tensor(a["lengths"], dtype=torch.int64).to(torch.int32).to(DEV)
+    sizes = [(2 * children, (children, 2)), (children, (children,)), (2 * children, (children, 2)), (n_blocks, (n_blocks,)), (3, (3,)),
+             (4, (2, 2)), (2 * len(f), (len(f), 2)), (len(f), (len(f),)), (2, (2,))]
+    guard = torch.full((2 * n_blocks,), 77, dtype=torch.int32, device=DEV)
+    inside = torch.zeros(2 * n_blocks, dtype=torch.bool, device=DEV)
+    out, at = [], 64
+    for size, shape in sizes:
+        out.append(guard[at:at + size].view(shape))
+        inside[at:at + size] = True
+        at += size + 64 - size % 64
+    bytes_of = [binding.fikit_cache_fork_workspace_bytes(2, children, 2, n_blocks), binding.fikit_cache_compact_workspace_bytes(2, 2, n_blocks)]
+    assert all(bytes_of)
+    found = [status_word(a.get("status", 0)) for _ in bytes_of]
+    work = [torch.full((n + 64,), 255, dtype=torch.uint8, device=DEV) for n in bytes_of]
+    binding.fikit_cache_fork(t, lengths, int32(a["parents"]), 16, n_blocks, f, found[0], out=binding.CacheFork(*out[:5]), workspace_buf=work[0][:bytes_of[0]])
+    binding.fikit_cache_compact(t, lengths, 16, n_blocks, f, found[1], out=binding.CacheCompaction(*out[5:]), workspace_buf=work[1][:bytes_of[1]])
+    kept = bool((guard[~inside] == 77).all()) and all(bool((w[n:] == 255).all()) for w, n in zip(work, bytes_of))
+    return [int(s) for s in found], out, kept
+
+
+@pytest.mark.parametrize("change", [
+    dict(parents=[0, 2]), dict(parents=[-2]), dict(parents=[1 << 30]), dict(lengths=[17, -1]), dict(lengths=[17, 33]), dict(lengths=[17, 1 << 31]),
+    dict(table=[[3, 40000], [1, 2]]), dict(table=[[3, -1], [1, 2]]), dict(table=[[3, 1 << 30], [1, 2]]), dict(free=[40000, 5]), dict(free=[-1, 5]),
+    dict(free=[6, 5, 6]), dict(free=[1, 5])])
+def test_refusals_in_several_launches(change):
+    a = dict(table=[[3, 4], [1, 2]], lengths=[17, 32], parents=[0, 0, 0], free=[39999, 5])
+    a.update(change)
+    statuses, _, kept = several_launches(a, len(a["parents"]))
+    assert kept
+    if change.get("free") not in ([6, 5, 6], [1, 5]):       # (which a fork does not look at)
+        assert statuses[0] == binding.FIKIT_INVALID_ARG
+    assert statuses[1] == (0 if "parents" in change else binding.FIKIT_INVALID_ARG)
+
+
+def test_too_few_and_nothing_behind_an_error_in_several_launches():
+    a = dict(table=[[3, 4], [1, 2]], lengths=[17, 31], parents=[0, 0, 0, 1, 1], free=[39999])
+    statuses, _, kept = several_launches(a, 5)
+    assert kept and statuses == [binding.FIKIT_CACHE_FULL, 0]
+    statuses, out, kept = several_launches(dict(a, status=binding.FIKIT_CACHE_FULL), 5)
+    assert kept and statuses == [binding.FIKIT_CACHE_FULL] * 2 and all(bool((t == 77).all()) for t in out)
