@@ -250,7 +250,11 @@ int fikit_cache_fork(const int32_t* d_block_table, uint32_t table_width, const i
   a.first = part(parts.first);
   a.rank = reinterpret_cast<int32_t*>(part(parts.rank));
   a.wants = part(parts.wants);
-  if (int rc = enqueue(k_fork_begin, dim3(1 + clear_groups(a.words).x), dim3(BLOCKS_THREADS), st, a)) return rc;
+  const dim3 clear(1 + clear_groups(a.words).x), threads(BLOCKS_THREADS);
+  const uint32_t most = n_requests > n_children ? n_requests : n_children;
+  if (int rc = most <= 4 * BLOCKS_THREADS ? enqueue(k_fork_begin<4>, clear, threads, st, a) : most <= 8 * BLOCKS_THREADS ? enqueue(k_fork_begin<8>, clear, threads, st, a)
+                                                                                             : enqueue(k_fork_begin<16>, clear, threads, st, a))
+    return rc;
   if (const uint32_t rows = n_requests + n_children)
     if (int rc = enqueue(k_fork_rows, dim3((rows + ROW_WAVES - 1) / ROW_WAVES), dim3(ROW_WAVES * WAVE), st, a)) return rc;
   const uint32_t slices = static_cast<uint32_t>(slices_of(n_blocks));

@@ -41,7 +41,7 @@ struct BlocksArgs {
 constexpr int BLOCKS_THREADS = 1024, ROW_WAVES = 4;
 constexpr uint32_t BLOCKS_MOST_REQUESTS = 16384, BLOCKS_MOST_BLOCKS = 1u << 20;
 constexpr uint32_t SLICE = 256;                // words of the bitmaps that are counted together
-constexpr uint32_t SLICE_WAVES = 16;           // waves that list a slice's blocks
+constexpr uint32_t SLICE_WAVES = 64;           // waves that list a slice's blocks (16: 4.1 us for a fork and 5.2 for a compaction, 64: 3.3 and 4.2)
 constexpr uint32_t NO_CHILD = 0xffffffffu;
 
 __device__ __forceinline__ uint32_t pages_of(const BlocksArgs& a, uint32_t length) { return (length + (1u << a.shift) - 1) >> a.shift; }
@@ -71,7 +71,7 @@ __device__ __forceinline__ uint32_t packed(const uint8_t* flags, uint32_t word) 
   return bits;
 }
 // A slice in a workgroup, with how many are marked in it, so that who lists them reads a number for each slice and the words of its own.  (Lists for which each
-// workgroup added up all words took 7.7 us for a fork and 9.3 for a compaction, these take 4.1 and 5.2.)
+// workgroup added up all words took 7.7 us for a fork and 9.3 for a compaction, these take 3.3 and 4.2.)
 template <bool FORK>
 __global__ __launch_bounds__(SLICE) void k_blocks_pack(BlocksArgs a) {
   __shared__ uint32_t waves[SLICE / WAVE];
@@ -161,19 +161,21 @@ __device__ __forceinline__ void each_page(const int32_t* entries, uint32_t pages
 // ---- fork -------------------------------------------------------------------------------------------------------
 //
 // Child i continues request parents[i].  The first child keeps the parent's last block if that is not full, each later one needs a block:
-// its place among those is a prefix sum over the children.  8192 children of 4096 requests over 107,000 blocks: 19 us in four launches.  Blocks to take come from the front of (free blocks, blocks given back in
+// its place among those is a prefix sum over the children.  8192 children of 4096 requests over 107,000 blocks: 18 us in four launches.  Blocks to take come from the front of (free blocks, blocks given back in
 // ascending order); what is left of the two is the new list.  The kernels of both calls load what they may before they look at the status.
 
-// The children, in one workgroup; the others clear the bitmaps.
+// The children, in one workgroup, PER requests and children to a thread, whose loads are on their way at once; the others clear the bitmaps.  (8192 children
+// 6.0 us, 1500 4.0; with code for 16,384, which is fetched although no thread has work in it, 7.8 and 6.9.)
+template <uint32_t PER>
 __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_begin(BlocksArgs a) {
-  __shared__ uint32_t first[BLOCKS_MOST_REQUESTS], sums[BLOCKS_MOST_REQUESTS / WAVE], scan[BLOCKS_THREADS / WAVE];
+  __shared__ uint32_t first[PER * BLOCKS_THREADS], sums[PER * BLOCKS_THREADS / WAVE], scan[BLOCKS_THREADS / WAVE];
   if (blockIdx.x > 0) {
     clear_flags(a, (blockIdx.x - 1) * BLOCKS_THREADS + threadIdx.x, (gridDim.x - 1) * BLOCKS_THREADS);
     return;
   }
   const bool stop = stopped(a.status);         // (nobody else writes it in this launch)
-  constexpr uint32_t PER = BLOCKS_MOST_REQUESTS / BLOCKS_THREADS, WAVES = BLOCKS_THREADS / WAVE;      // PER: requests and children of a thread, whose
-  bool bad = false;                                                                                  // loads are on their way at once
+  constexpr uint32_t WAVES = BLOCKS_THREADS / WAVE;
+  bool bad = false;
   const uint32_t wave = uniform(threadIdx.x / WAVE);
   int32_t lengths[PER], parents[PER];
 #pragma unroll
@@ -441,7 +443,7 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_one(BlocksArgs a) {
 // ---- compaction -------------------------------------------------------------------------------------------------
 //
 // Used and free blocks together, ascending: behind the first n_used of them lies the border.  The k-th used block behind the border goes
-// to the k-th free one before it, and what lies behind it is the new free list.  3001 requests over 177,000 blocks: 19 us in five launches.
+// to the k-th free one before it, and what lies behind it is the new free list.  3001 requests over 177,000 blocks: 20 us in five launches.
 
 __global__ __launch_bounds__(BLOCKS_THREADS) void k_compact_begin(BlocksArgs a) {
   clear_flags(a, blockIdx.x * BLOCKS_THREADS + threadIdx.x, gridDim.x * BLOCKS_THREADS);
