@@ -364,3 +364,12 @@ def test_too_few_and_nothing_behind_an_error_in_several_launches():
     assert kept and statuses == [binding.FIKIT_CACHE_FULL, 0]
     statuses, out, kept = several_launches(dict(a, status=binding.FIKIT_CACHE_FULL), 5)
     assert kept and statuses == [binding.FIKIT_CACHE_FULL] * 2 and all(bool((t == 77).all()) for t in out)
+
+
+@pytest.mark.parametrize("requests, children", [(4096, 4096), (4096, 4097), (4097, 5), (5, 8192), (8192, 8193), (8193, 300), (16384, 1), (1, 16384)])
+def test_how_many_requests_and_children_a_thread_has(requests, children):
+    rng = np.random.default_rng(requests + children)
+    table, lengths, n_blocks, free = some_cache(rng, requests, 70, 16, groups=3, spare=requests // 2 + children // 3)
+    width = len(table[0])
+    for parents in (rng.integers(-1, requests, children), np.minimum(rng.geometric(0.01, children) - 1, requests - 1), np.full(children, requests - 1)):
+        check_fork(table, lengths, [int(p) for p in parents], 16, n_blocks, free, width)
