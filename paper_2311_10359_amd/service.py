@@ -116,8 +116,8 @@ class Service:
         return x + record("back", (n, 1, 1), torch.mm, out.view(n, -1), self.w_out[layer])
 
     def prompts(self, record, x: torch.Tensor, lengths: List[int]) -> torch.Tensor:
-        """x: [sum of lengths, hidden], the prompts one behind the other; returns the last layer's output.  They come first: prompt
-        attention sees the new tokens only, so prompts behind tokens in the cache are refused."""
+        """x: [sum of lengths, hidden], the prompts one behind the other; returns the last layer's output.  They come first, or where every
+        request has ended: prompt attention sees the new tokens only, so prompts behind tokens in the cache are refused."""
         if self.longest > 0:
             raise ValueError("prompts of requests that have no tokens in the cache")
         plan = self._plan(record, lengths)
@@ -162,6 +162,7 @@ class Service:
         self._check()
         self.table, self.lengths = fork.block_table, fork.lengths
         self.free, self.taken = fork.free_blocks[:int(fork.counts[2])], 0
+        self.longest = max(fork.lengths.tolist(), default=0)          # (the longest one may have ended)
 
     def compact(self, record) -> int:
         """Moves the blocks in use together; returns the number of blocks behind the last of them."""
