@@ -639,7 +639,8 @@ size_t fikit_cache_fork_workspace_bytes(uint32_t n_requests, uint32_t n_children
  *   d_block_table    [n_requests][table_width], d_lengths [n_requests]: as fikit_cache_plan leaves them; what lies behind a request's
  *                    blocks is not looked at.  n_requests, n_children up to 16,384.
  *   n_blocks         of the cache, up to 2^20.
- *   d_free           [n_free] blocks that nobody holds, n_free <= n_blocks.
+ *   d_free           [n_free] blocks that nobody holds, n_free <= n_blocks.  Each is looked at, also those that are not taken: of d_new_free
+ *                    the next call is given the first d_counts[2], as the -1 behind them are no blocks.
  *   d_new_table      [n_children][table_width] receives the children's rows, -1 behind their blocks.  Full blocks are shared.  If a request's
  *                    last block is not full, it stays with its first child (the lowest), and each later one gets a block of its own.
  *   d_new_lengths    [n_children].

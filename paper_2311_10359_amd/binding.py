@@ -760,7 +760,7 @@ class CacheFork(NamedTuple):
     block_table: torch.Tensor       # int32 [children, width]
     lengths: torch.Tensor           # int32 [children]
     copies: torch.Tensor            # int32 [children, 2]: from, to; -1 behind the last one
-    free_blocks: torch.Tensor       # int32 [n_blocks]; -1 behind the last one
+    free_blocks: torch.Tensor       # int32 [n_blocks]; -1 behind the last one, of which the next call is given none: free_blocks[:counts[2]]
     counts: torch.Tensor            # int32 [3]: blocks taken, given back, free
 
 

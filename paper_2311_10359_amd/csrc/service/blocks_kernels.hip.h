@@ -296,7 +296,13 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_fork_end(BlocksArgs a) {
     }
   }
   const uint32_t from = blockIdx.x * ROW_WAVES * WAVE + threadIdx.x, stride = gridDim.x * ROW_WAVES * WAVE;
-  for (uint32_t i = taken + from; i < a.n_free; i += stride) a.new_free[i - taken] = a.free_blocks[i];
+  bool bad = false;                              // (those that are taken: k_fork_rows)
+  for (uint32_t i = taken + from; i < a.n_free; i += stride) {
+    const int32_t block = a.free_blocks[i];
+    bad |= static_cast<uint32_t>(block) >= a.n_blocks;
+    a.new_free[i - taken] = block;
+  }
+  if (bad) *a.status = FIKIT_INVALID_ARG;
   for (uint32_t i = total - taken + from; i < a.n_blocks; i += stride) a.new_free[i] = -1;
   for (uint32_t i = taken + from; i < a.n_children; i += stride) a.copies[i] = make_int2(-1, -1);
   if (from == 0) {
@@ -427,8 +433,16 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_one(BlocksArgs a) {
     const uint32_t marks = given_word(block / 32), bit = 1u << block % 32, place = a.n_free + before[block / 32] + __popc(marks & (bit - 1));
     if ((marks & bit) && place >= taken) a.new_free[place - taken] = static_cast<int32_t>(block);
   }
-  if (taken + from < a.n_free) a.new_free[from] = left;
-  for (uint32_t i = taken + from + stride; i < a.n_free; i += stride) a.new_free[i - taken] = a.free_blocks[i];
+  if (taken + from < a.n_free) {
+    a.new_free[from] = left;
+    bad |= static_cast<uint32_t>(left) >= a.n_blocks;
+  }
+  for (uint32_t i = taken + from + stride; i < a.n_free; i += stride) {
+    const int32_t block = a.free_blocks[i];
+    bad |= static_cast<uint32_t>(block) >= a.n_blocks;
+    a.new_free[i - taken] = block;
+  }
+  if (bad) *a.status = FIKIT_INVALID_ARG;
   for (uint32_t i = total - taken + from; i < a.n_blocks; i += stride) a.new_free[i] = -1;
   for (uint32_t i = taken + from; i < a.n_children; i += stride) a.copies[i] = make_int2(-1, -1);
   if (blockIdx.x > 0) return;
