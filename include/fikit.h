@@ -639,8 +639,9 @@ size_t fikit_cache_fork_workspace_bytes(uint32_t n_requests, uint32_t n_children
  *   d_block_table    [n_requests][table_width], d_lengths [n_requests]: as fikit_cache_plan leaves them; what lies behind a request's
  *                    blocks is not looked at.  n_requests, n_children up to 16,384.
  *   n_blocks         of the cache, up to 2^20.
- *   d_free           [n_free] blocks that nobody holds, n_free <= n_blocks.  Each is looked at, also those that are not taken: of d_new_free
- *                    the next call is given the first d_counts[2], as the -1 behind them are no blocks.
+ *   d_free           [n_free] blocks that nobody holds, n_free <= n_blocks.  Each is looked at, also those that are not taken: one that is in use
+ *                    or there twice is INVALID_ARG through d_status.  Of d_new_free the next call is given the first d_counts[2], as the -1
+ *                    behind them are no blocks.
  *   d_new_table      [n_children][table_width] receives the children's rows, -1 behind their blocks.  Full blocks are shared.  If a request's
  *                    last block is not full, it stays with its first child (the lowest), and each later one gets a block of its own.
  *   d_new_lengths    [n_children].
@@ -651,7 +652,7 @@ size_t fikit_cache_fork_workspace_bytes(uint32_t n_requests, uint32_t n_children
  *                    Outputs overlap neither each other nor an input (INVALID_ARG).
  *   d_workspace      256-byte aligned, at least fikit_cache_fork_workspace_bytes(...) bytes.
  *
- * Through d_status: INVALID_ARG (a parent, a length or a block that cannot be), CACHE_FULL if too few blocks are free.
+ * Through d_status: INVALID_ARG (a parent, a length or a block that cannot be), else CACHE_FULL if too few blocks are free.
  */
 int fikit_cache_fork(const int32_t* d_block_table, uint32_t table_width, const int32_t* d_lengths, uint32_t n_requests,
                      const int32_t* d_parents, uint32_t n_children, uint32_t block_tokens, uint32_t n_blocks, const int32_t* d_free,

@@ -79,13 +79,15 @@ struct Parts {
   }
 };
 struct ForkParts : Parts {
-  uint64_t words, flags, flags_too, marks, sums, first, rank, wants;
+  uint64_t words, flags, flags_too, flags_free, marks, sums, sums_too, first, rank, wants;
   ForkParts(uint32_t n_requests, uint32_t n_children, uint32_t n_blocks) : words((n_blocks + 31) / 32) {
     take(1);
     flags = take(8 * words);
     flags_too = take(8 * words);
+    flags_free = take(8 * words);
     marks = take(SLICE * slices_of(n_blocks));
     sums = take(slices_of(n_blocks));
+    sums_too = take(slices_of(n_blocks));
     first = take(n_requests);
     rank = take(n_children);
     wants = take(n_children);
@@ -237,7 +239,7 @@ int fikit_cache_fork(const int32_t* d_block_table, uint32_t table_width, const i
   a.n_children = n_children;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (const uint32_t groups = one_launch(n_requests, n_children, n_children, table_width, n_blocks))
-    return enqueue(k_fork_one, dim3(groups), dim3(BLOCKS_THREADS), st, a);
+    return enqueue(k_fork_one, dim3(groups + 1), dim3(BLOCKS_THREADS), st, a);
   const ForkParts parts(n_requests, n_children, n_blocks);
   if (!d_workspace || !aligned(d_workspace, 256)) return FIKIT_INVALID_ARG;
   if (workspace_bytes < parts.bytes) return FIKIT_WORKSPACE_TOO_SMALL;
@@ -245,8 +247,10 @@ int fikit_cache_fork(const int32_t* d_block_table, uint32_t table_width, const i
   a.words_of_call = part(0);
   a.flags = reinterpret_cast<uint8_t*>(part(parts.flags));
   a.flags_too = reinterpret_cast<uint8_t*>(part(parts.flags_too));
+  a.flags_free = reinterpret_cast<uint8_t*>(part(parts.flags_free));
   a.marks = part(parts.marks);
   a.sums = part(parts.sums);
+  a.sums_too = part(parts.sums_too);
   a.first = part(parts.first);
   a.rank = reinterpret_cast<int32_t*>(part(parts.rank));
   a.wants = part(parts.wants);
@@ -255,7 +259,7 @@ int fikit_cache_fork(const int32_t* d_block_table, uint32_t table_width, const i
   if (int rc = most <= 4 * BLOCKS_THREADS ? enqueue(k_fork_begin<4>, clear, threads, st, a) : most <= 8 * BLOCKS_THREADS ? enqueue(k_fork_begin<8>, clear, threads, st, a)
                                                                                              : enqueue(k_fork_begin<16>, clear, threads, st, a))
     return rc;
-  if (const uint32_t rows = n_requests + n_children)
+  if (const uint32_t rows = n_requests + n_children + (n_free + WAVE - 1) / WAVE)
     if (int rc = enqueue(k_fork_rows, dim3((rows + ROW_WAVES - 1) / ROW_WAVES), dim3(ROW_WAVES * WAVE), st, a)) return rc;
   const uint32_t slices = static_cast<uint32_t>(slices_of(n_blocks));
   if (int rc = enqueue(k_blocks_pack<true>, dim3(slices), dim3(SLICE), st, a)) return rc;

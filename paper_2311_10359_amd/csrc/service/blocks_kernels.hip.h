@@ -25,10 +25,11 @@ struct BlocksArgs {
   int32_t* status;
   uint8_t* flags;           // a byte for each block, in whole words of the bitmaps; fork: blocks of requests that nobody continues; compaction: used blocks
   uint8_t* flags_too;       // fork: blocks of the others; compaction: free ones
+  uint8_t* flags_free;      // fork: free ones
   uint32_t* marks;          // bitmaps, in whole slices; fork: blocks given back; compaction: used blocks
   uint32_t* marks_too;      // compaction: free blocks
   uint32_t* sums;           // [slices]: how many of them are marked in a slice
-  uint32_t* sums_too;
+  uint32_t* sums_too;       // how many are free
   uint32_t* first;          // fork, [n_requests]: a request's first child, or NO_CHILD
   int32_t* rank;            // fork, [n_children]: a child's place among those that need a block for a copy, or -1
   uint32_t* wants;          // fork, [n_children]: the child of a place
@@ -52,9 +53,22 @@ __device__ __forceinline__ bool length_ok(const BlocksArgs& a, int32_t length) {
 }
 
 // Whole sets of flags as words of 16 bytes.
+template <bool FORK>
 __device__ __forceinline__ void clear_flags(const BlocksArgs& a, uint32_t from, uint32_t stride) {
-  for (uint32_t i = from; i < 2 * a.words; i += stride)
+  for (uint32_t i = from; i < 2 * a.words; i += stride) {
     reinterpret_cast<u32x4*>(a.flags)[i] = reinterpret_cast<u32x4*>(a.flags_too)[i] = u32x4{0, 0, 0, 0};
+    if constexpr (FORK) reinterpret_cast<u32x4*>(a.flags_free)[i] = u32x4{0, 0, 0, 0};
+  }
+}
+
+// 64 entries of the free list in a wave, from the first-th on.  (The status is looked at behind the load.)
+__device__ __forceinline__ void mark_free(const BlocksArgs& a, uint32_t first, bool stop, uint8_t* flags) {
+  const uint32_t i = first + lane_id();
+  if (i >= a.n_free) return;
+  const uint32_t block = static_cast<uint32_t>(a.free_blocks[i]);
+  if (stop) return;
+  if (block < a.n_blocks) flags[block] = 1;
+  else *a.status = FIKIT_INVALID_ARG;
 }
 
 // The bitmaps from the flags.  (Many workgroups mark at once.  Or-ing bits into words in memory took 12.2 us for 176,000 marks; stores of a byte, of which none
@@ -76,27 +90,24 @@ template <bool FORK>
 __global__ __launch_bounds__(SLICE) void k_blocks_pack(BlocksArgs a) {
   __shared__ uint32_t waves[SLICE / WAVE];
   const uint32_t w = blockIdx.x * SLICE + threadIdx.x;
-  uint32_t marks = 0, marks_too = 0;
+  uint32_t marks = 0, marks_too = 0, spare = 0;
   if (w < a.words) {
     marks = packed(a.flags, w);
     marks_too = packed(a.flags_too, w);
+    spare = FORK ? packed(a.flags_free, w) : marks_too;
   }
-  if constexpr (FORK) {
-    marks &= ~marks_too;
-    marks_too = 0;
-  } else {
-    if ((marks & marks_too) && !stopped(a.status)) *a.status = FIKIT_INVALID_ARG;        // used and free
-    a.marks_too[w] = marks_too;
-  }
+  if (((FORK ? marks | marks_too : marks) & spare) && !stopped(a.status)) *a.status = FIKIT_INVALID_ARG;        // used and free
+  if constexpr (FORK) marks &= ~marks_too;
+  else a.marks_too[w] = marks_too;
   a.marks[w] = marks;
-  const uint32_t sum = sum_over_wave(__popc(marks) << 16 | __popc(marks_too));       // (up to 8192 each)
+  const uint32_t sum = sum_over_wave(__popc(marks) << 16 | __popc(spare));       // (up to 8192 each)
   if (lane_id() == 0) waves[threadIdx.x / WAVE] = sum;
   __syncthreads();
   if (threadIdx.x > 0) return;
   uint32_t all = 0;
   for (uint32_t i = 0; i < SLICE / WAVE; ++i) all += waves[i];
   a.sums[blockIdx.x] = all >> 16;
-  if constexpr (!FORK) a.sums_too[blockIdx.x] = all & 0xffffu;
+  a.sums_too[blockIdx.x] = all & 0xffffu;
 }
 
 // The counts of all slices in a wave, two neighbours to a lane.
@@ -170,7 +181,7 @@ template <uint32_t PER>
 __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_begin(BlocksArgs a) {
   __shared__ uint32_t first[PER * BLOCKS_THREADS], sums[PER * BLOCKS_THREADS / WAVE], scan[BLOCKS_THREADS / WAVE];
   if (blockIdx.x > 0) {
-    clear_flags(a, (blockIdx.x - 1) * BLOCKS_THREADS + threadIdx.x, (gridDim.x - 1) * BLOCKS_THREADS);
+    clear_flags<true>(a, (blockIdx.x - 1) * BLOCKS_THREADS + threadIdx.x, (gridDim.x - 1) * BLOCKS_THREADS);
     return;
   }
   const bool stop = stopped(a.status);         // (nobody else writes it in this launch)
@@ -227,7 +238,8 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_begin(BlocksArgs a) {
   if (threadIdx.x == 0) a.words_of_call[0] = taken;
 }
 
-// A wave for each request, which marks its blocks, and for each child, which writes its row.
+// A wave for each request, which marks its blocks, for each child, which writes its row, and for 64 free blocks, which marks them: one that is in use, or
+// there twice, would be handed out while somebody holds it.
 __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_fork_rows(BlocksArgs a) {
   const bool stop = stopped(a.status);
   const uint32_t lane = lane_id(), row = blockIdx.x * ROW_WAVES + uniform(threadIdx.x / WAVE);
@@ -244,7 +256,7 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_fork_rows(BlocksArgs a) {
     return;
   }
   const uint32_t c = row - a.n_requests;
-  if (c >= a.n_children) return;
+  if (c >= a.n_children) return mark_free(a, (c - a.n_children) * WAVE, stop, a.flags_free);
   const int32_t p = a.parents[c], rank = a.rank[c];
   if (stop) return;
   const int32_t length = p >= 0 ? a.lengths[p] : 0;
@@ -257,7 +269,6 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_fork_rows(BlocksArgs a) {
       a.copies[rank].x = block;
       if (static_cast<uint32_t>(rank) < a.n_free) {
         block = a.free_blocks[rank];
-        if (static_cast<uint32_t>(block) >= a.n_blocks) *a.status = FIKIT_INVALID_ARG;
         a.copies[rank].y = block;
       }                                          // (else what is given back says which: k_fork_end)
     }
@@ -271,14 +282,15 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_fork_end(BlocksArgs a) {
   const bool stop = stopped(a.status);
   const uint32_t row = blockIdx.x * ROW_WAVES + uniform(threadIdx.x / WAVE), slice = row / SLICE_WAVES, word = row % SLICE_WAVES * WAVE_WORDS;
   const uint32_t lane = lane_id(), taken = a.words_of_call[0];
-  SliceSums sums(a, a.sums);
+  SliceSums sums(a, a.sums), spare(a, a.sums_too);
   SliceWords words(a.marks, slice);
   if (stop) return;
   sums.add_up();
+  spare.add_up();
   words.add_up(sums.before_slice(slice));
-  const uint32_t given = sums.total, total = a.n_free + given;          // (below 2^32: n_free is at most n_blocks)
-  if (taken > total || total - taken > a.n_blocks) {                    // (too few; or a list that names blocks in use)
-    if (lane == 0) *a.status = taken > total ? FIKIT_CACHE_FULL : FIKIT_INVALID_ARG;
+  const uint32_t given = sums.total, total = a.n_free + given;          // (as free blocks are not in use, nor there twice, at most n_blocks)
+  if (spare.total != a.n_free || taken > total) {                       // free twice; too few
+    if (lane == 0) *a.status = spare.total != a.n_free ? FIKIT_INVALID_ARG : FIKIT_CACHE_FULL;
     return;
   }
 #pragma unroll
@@ -296,13 +308,7 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_fork_end(BlocksArgs a) {
     }
   }
   const uint32_t from = blockIdx.x * ROW_WAVES * WAVE + threadIdx.x, stride = gridDim.x * ROW_WAVES * WAVE;
-  bool bad = false;                              // (those that are taken: k_fork_rows)
-  for (uint32_t i = taken + from; i < a.n_free; i += stride) {
-    const int32_t block = a.free_blocks[i];
-    bad |= static_cast<uint32_t>(block) >= a.n_blocks;
-    a.new_free[i - taken] = block;
-  }
-  if (bad) *a.status = FIKIT_INVALID_ARG;
+  for (uint32_t i = taken + from; i < a.n_free; i += stride) a.new_free[i - taken] = a.free_blocks[i];
   for (uint32_t i = total - taken + from; i < a.n_blocks; i += stride) a.new_free[i] = -1;
   for (uint32_t i = taken + from; i < a.n_children; i += stride) a.copies[i] = make_int2(-1, -1);
   if (from == 0) {
@@ -315,7 +321,8 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_fork_end(BlocksArgs a) {
 // ---- one launch -------------------------------------------------------------------------------------------------
 //
 // Up to ONE_REQUESTS requests and children, ONE_BLOCKS blocks and ONE_CELLS entries of the table, with bitmaps in LDS: every workgroup marks all blocks for
-// itself and writes its share of the outputs, so that none waits for another.  128 beams of 32 prompts 6.0 us, their compaction 6.0; in the launches that
+// itself and writes its share of the outputs, so that none waits for another.  A fork has one more, which marks the free blocks too and alone says what is
+// wrong, so that the others neither read all of that list nor find different errors.  128 beams of 32 prompts 6.0 us, their compaction 6.0; in the launches that
 // larger sizes take, 13 and 16.
 
 constexpr uint32_t ONE_REQUESTS = BLOCKS_THREADS, ONE_BLOCKS = 32 * BLOCKS_THREADS, ONE_CELLS = 65536, ONE_MOST_GROUPS = 64;
@@ -363,26 +370,31 @@ __device__ __forceinline__ uint32_t marked_block(const uint32_t* before, uint32_
 
 __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_one(BlocksArgs a) {
   __shared__ OneLds lds;
-  __shared__ uint32_t before[BLOCKS_THREADS], first[ONE_REQUESTS], ranks[ONE_REQUESTS];
+  __shared__ uint32_t before[BLOCKS_THREADS], spare[BLOCKS_THREADS], first[ONE_REQUESTS], ranks[ONE_REQUESTS];
   __shared__ int32_t lengths[ONE_REQUESTS], parents[ONE_REQUESTS], fresh[ONE_REQUESTS];
-  const uint32_t t = threadIdx.x, lane = lane_id(), waves = BLOCKS_THREADS / WAVE, mine = blockIdx.x * waves + uniform(t / WAVE);
-  const bool stop = stopped(a.status);
+  const uint32_t t = threadIdx.x, lane = lane_id(), waves = BLOCKS_THREADS / WAVE, groups = gridDim.x - 1, mine = blockIdx.x * waves + uniform(t / WAVE);
+  const bool checks = blockIdx.x == groups, stop = stopped(a.status);
   const int32_t length = t < a.n_requests ? a.lengths[t] : 0, parent = t < a.n_children ? a.parents[t] : -1;
   const bool fits = length_ok(a, length) && parent >= -1 && (parent < 0 || static_cast<uint32_t>(parent) < a.n_requests);
-  lds.marks[t] = lds.marks_too[t] = 0;
+  lds.marks[t] = lds.marks_too[t] = spare[t] = 0;
   first[t] = NO_CHILD;
   lengths[t] = length;
   parents[t] = parent;
   lds.pages[t] = fits ? pages_of(a, static_cast<uint32_t>(length)) : 0;
   if (__syncthreads_or(stop || !fits)) {
-    if (!__syncthreads_or(stop) && blockIdx.x == 0 && t == 0) *a.status = FIKIT_INVALID_ARG;
+    if (!__syncthreads_or(stop) && checks && t == 0) *a.status = FIKIT_INVALID_ARG;
     return;
   }
   if (parent >= 0) atomicMin(&first[parent], t);
   // what the wave's first row begins with is on its way from here on
-  const int32_t my_parent = mine < a.n_children ? parents[mine] : -1;
+  const int32_t my_parent = !checks && mine < a.n_children ? parents[mine] : -1;
   const uint32_t my_pages = my_parent >= 0 ? lds.pages[my_parent] : 0;
   const int32_t early = lane < my_pages ? a.table[static_cast<uint64_t>(my_parent) * a.width + lane] : 0;
+  constexpr int AHEAD = 4;
+  int32_t held[AHEAD];                                           // (so are the first free blocks)
+#pragma unroll
+  for (int j = 0; j < AHEAD; ++j)
+    if (checks && t + j * BLOCKS_THREADS < a.n_free) held[j] = a.free_blocks[t + j * BLOCKS_THREADS];
   __syncthreads();
   bool bad = false;
   if (a.width > 0)
@@ -392,8 +404,21 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_one(BlocksArgs a) {
     });
   const int32_t child_length = parent >= 0 ? lengths[parent] : 0;
   const bool need = (static_cast<uint32_t>(child_length) & ((1u << a.shift) - 1)) && first[parent] != t;
-  if (__syncthreads_or(bad)) {
-    if (blockIdx.x == 0 && t == 0) *a.status = FIKIT_INVALID_ARG;
+  if (checks) {
+    const auto put = [&](uint32_t block) {
+      const uint32_t bit = 1u << block % 32;
+      if (block >= a.n_blocks) bad = true;
+      else bad |= (atomicOr(&spare[block / 32], bit) & bit) != 0;               // there twice
+    };
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j)
+      if (t + j * BLOCKS_THREADS < a.n_free) put(static_cast<uint32_t>(held[j]));
+    for (uint32_t i = t + AHEAD * BLOCKS_THREADS; i < a.n_free; i += BLOCKS_THREADS) put(static_cast<uint32_t>(a.free_blocks[i]));
+  }
+  bad = __syncthreads_or(bad);
+  if (checks) bad = __syncthreads_or(bad || (spare[t] & (lds.marks[t] | lds.marks_too[t])));
+  if (bad) {
+    if (checks && t == 0) *a.status = FIKIT_INVALID_ARG;
     return;
   }
   // two sums in one: children that need a block, and blocks given back, up to 32,768
@@ -402,24 +427,21 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_one(BlocksArgs a) {
   const uint32_t rank = upto >> 16, taken = both >> 16, given = both & 0xffffu, total = a.n_free + given;
   ranks[t] = need ? rank : ~0u;
   before[t] = upto & 0xffffu;
-  if (taken > total || total - taken > a.n_blocks) {
-    if (blockIdx.x == 0 && t == 0) *a.status = taken > total ? FIKIT_CACHE_FULL : FIKIT_INVALID_ARG;
-    return;
-  }
+  if (checks && taken > total && t == 0) *a.status = FIKIT_CACHE_FULL;
+  if (checks || taken > total || total - taken > a.n_blocks) return;           // (more than n_blocks: of a list that the one which checks refuses)
   fresh[t] = need && rank < a.n_free ? a.free_blocks[rank] : 0;
-  const uint32_t from = blockIdx.x * BLOCKS_THREADS + t, stride = gridDim.x * BLOCKS_THREADS;
+  const uint32_t from = blockIdx.x * BLOCKS_THREADS + t, stride = groups * BLOCKS_THREADS;
   const int32_t left = taken + from < a.n_free ? a.free_blocks[taken + from] : 0;
   __syncthreads();
   const auto given_word = [&](uint32_t w) { return lds.marks[w] & ~lds.marks_too[w]; };
   // rows, a wave each
-  for (uint32_t c = mine; c < a.n_children; c += gridDim.x * waves) {
+  for (uint32_t c = mine; c < a.n_children; c += groups * waves) {
     const int32_t p = parents[c];
     const uint32_t pages = p >= 0 ? lds.pages[p] : 0, place = ranks[c];
     int32_t* out = a.new_table + static_cast<uint64_t>(c) * a.width;
     const auto put = [&](uint32_t page, int32_t block) {
       if (page + 1 == pages && place != ~0u) {
         const uint32_t one = place < a.n_free ? static_cast<uint32_t>(fresh[c]) : marked_block(before, place - a.n_free, given_word);
-        if (one >= a.n_blocks) *a.status = FIKIT_INVALID_ARG;
         a.copies[place] = make_int2(block, static_cast<int32_t>(one));
         block = static_cast<int32_t>(one);
       }
@@ -433,16 +455,8 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_one(BlocksArgs a) {
     const uint32_t marks = given_word(block / 32), bit = 1u << block % 32, place = a.n_free + before[block / 32] + __popc(marks & (bit - 1));
     if ((marks & bit) && place >= taken) a.new_free[place - taken] = static_cast<int32_t>(block);
   }
-  if (taken + from < a.n_free) {
-    a.new_free[from] = left;
-    bad |= static_cast<uint32_t>(left) >= a.n_blocks;
-  }
-  for (uint32_t i = taken + from + stride; i < a.n_free; i += stride) {
-    const int32_t block = a.free_blocks[i];
-    bad |= static_cast<uint32_t>(block) >= a.n_blocks;
-    a.new_free[i - taken] = block;
-  }
-  if (bad) *a.status = FIKIT_INVALID_ARG;
+  if (taken + from < a.n_free) a.new_free[from] = left;
+  for (uint32_t i = taken + from + stride; i < a.n_free; i += stride) a.new_free[i - taken] = a.free_blocks[i];
   for (uint32_t i = total - taken + from; i < a.n_blocks; i += stride) a.new_free[i] = -1;
   for (uint32_t i = taken + from; i < a.n_children; i += stride) a.copies[i] = make_int2(-1, -1);
   if (blockIdx.x > 0) return;
@@ -460,13 +474,13 @@ __global__ __launch_bounds__(BLOCKS_THREADS) void k_fork_one(BlocksArgs a) {
 // to the k-th free one before it, and what lies behind it is the new free list.  3001 requests over 177,000 blocks: 20 us in five launches.
 
 __global__ __launch_bounds__(BLOCKS_THREADS) void k_compact_begin(BlocksArgs a) {
-  clear_flags(a, blockIdx.x * BLOCKS_THREADS + threadIdx.x, gridDim.x * BLOCKS_THREADS);
+  clear_flags<false>(a, blockIdx.x * BLOCKS_THREADS + threadIdx.x, gridDim.x * BLOCKS_THREADS);
 }
 
 // A wave for each request marks its blocks; the waves behind them the free ones, 64 each.
 __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_compact_mark(BlocksArgs a) {
   const bool stop = stopped(a.status);
-  const uint32_t lane = lane_id(), row = blockIdx.x * ROW_WAVES + uniform(threadIdx.x / WAVE);
+  const uint32_t row = blockIdx.x * ROW_WAVES + uniform(threadIdx.x / WAVE);
   if (row < a.n_requests) {
     const int32_t length = a.lengths[row];
     if (stop) return;
@@ -483,12 +497,7 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_compact_mark(BlocksArgs a)
     });
     return;
   }
-  const uint32_t i = (row - a.n_requests) * WAVE + lane;
-  if (i >= a.n_free) return;
-  const uint32_t block = static_cast<uint32_t>(a.free_blocks[i]);
-  if (stop) return;
-  if (block < a.n_blocks) a.flags_too[block] = 1;
-  else *a.status = FIKIT_INVALID_ARG;
+  mark_free(a, (row - a.n_requests) * WAVE, stop, a.flags_too);
 }
 
 struct Border {
