@@ -108,8 +108,8 @@ struct CompactParts : Parts {
 };
 
 // Workgroups of the kernels that do all in one launch, or 0 for sizes that they do not take.
-uint32_t one_launch(uint32_t n_requests, uint32_t n_children, uint32_t rows, uint32_t table_width, uint32_t n_blocks) {
-  if (n_requests > ONE_REQUESTS || n_children > ONE_REQUESTS || n_blocks > ONE_BLOCKS || static_cast<uint64_t>(n_requests) * table_width > ONE_CELLS) return 0;
+uint32_t one_launch(uint32_t n_requests, uint32_t rows, uint32_t table_width, uint32_t n_blocks, uint32_t most_cells) {
+  if (n_requests > ONE_REQUESTS || rows > ONE_REQUESTS || n_blocks > ONE_BLOCKS || static_cast<uint64_t>(n_requests) * table_width > most_cells) return 0;
   const uint32_t groups = (rows + BLOCKS_THREADS / WAVE - 1) / (BLOCKS_THREADS / WAVE);
   return groups < 1 ? 1 : groups < ONE_MOST_GROUPS ? groups : ONE_MOST_GROUPS;
 }
@@ -211,7 +211,7 @@ constexpr uint32_t COPY_GROUPS = 16384;
 extern "C" {
 
 size_t fikit_cache_fork_workspace_bytes(uint32_t n_requests, uint32_t n_children, uint32_t table_width, uint32_t n_blocks) {
-  if (!blocks_fit(n_requests, n_children, n_blocks) || one_launch(n_requests, n_children, n_children, table_width, n_blocks)) return 0;
+  if (!blocks_fit(n_requests, n_children, n_blocks) || one_launch(n_requests, n_children, table_width, n_blocks, FORK_CELLS)) return 0;
   return static_cast<size_t>(ForkParts(n_requests, n_children, n_blocks).bytes);
 }
 
@@ -238,7 +238,7 @@ int fikit_cache_fork(const int32_t* d_block_table, uint32_t table_width, const i
   a.counts = d_counts;
   a.n_children = n_children;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  if (const uint32_t groups = one_launch(n_requests, n_children, n_children, table_width, n_blocks))
+  if (const uint32_t groups = one_launch(n_requests, n_children, table_width, n_blocks, FORK_CELLS))
     return enqueue(k_fork_one, dim3(groups + 1), dim3(BLOCKS_THREADS), st, a);
   const ForkParts parts(n_requests, n_children, n_blocks);
   if (!d_workspace || !aligned(d_workspace, 256)) return FIKIT_INVALID_ARG;
@@ -267,7 +267,7 @@ int fikit_cache_fork(const int32_t* d_block_table, uint32_t table_width, const i
 }
 
 size_t fikit_cache_compact_workspace_bytes(uint32_t n_requests, uint32_t table_width, uint32_t n_blocks) {
-  if (!blocks_fit(n_requests, 0, n_blocks) || one_launch(n_requests, 0, n_requests, table_width, n_blocks)) return 0;
+  if (!blocks_fit(n_requests, 0, n_blocks) || one_launch(n_requests, n_requests, table_width, n_blocks, COMPACT_CELLS)) return 0;
   return static_cast<size_t>(CompactParts(n_blocks).bytes);
 }
 
@@ -290,7 +290,7 @@ int fikit_cache_compact(const int32_t* d_block_table, uint32_t table_width, cons
   a.counts = d_counts;
   a.room = room;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  if (const uint32_t groups = one_launch(n_requests, 0, n_requests, table_width, n_blocks))
+  if (const uint32_t groups = one_launch(n_requests, n_requests, table_width, n_blocks, COMPACT_CELLS))
     return enqueue(k_compact_one, dim3(groups), dim3(BLOCKS_THREADS), st, a);
   const CompactParts parts(n_blocks);
   if (!d_workspace || !aligned(d_workspace, 256)) return FIKIT_INVALID_ARG;

@@ -320,12 +320,24 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_fork_end(BlocksArgs a) {
 
 // ---- one launch -------------------------------------------------------------------------------------------------
 //
-// Up to ONE_REQUESTS requests and children, ONE_BLOCKS blocks and ONE_CELLS entries of the table, with bitmaps in LDS: every workgroup marks all blocks for
-// itself and writes its share of the outputs, so that none waits for another.  A fork has one more, which marks the free blocks too and alone says what is
-// wrong, so that the others neither read all of that list nor find different errors.  128 beams of 32 prompts 6.0 us, their compaction 6.0; in the launches that
-// larger sizes take, 13 and 16.
+// Up to ONE_REQUESTS requests and children, ONE_BLOCKS blocks and FORK_CELLS or COMPACT_CELLS entries of the table, with bitmaps in LDS: every workgroup marks all
+// blocks for itself and writes its share of the outputs, so that none waits for another.  A fork has one more, which marks the free blocks too and alone says
+// what is wrong, so that the others neither read all of that list nor find different errors.  128 beams of 32 prompts 6.0 us, their compaction 6.0; in the launches
+// that larger sizes take, 13 and 16.
+//
+// The marks that every workgroup makes bound it, and with them the entries that are read.  Calls of 128 requests whose rows are full, of scattered blocks and of
+// neighbouring ones, whose bits lie in one word; compactions of 16 requests, in several launches, come to 17 to 25 us for scattered blocks:
+//
+//                        fork                                compaction
+//   entries              scattered   neighbours   several    scattered   neighbours   several
+//   8192                   6.9          13          12          8.9          15        17
+//   16,384                 9.0          21          12         11            23        14-17
+//   32,768                12.6          34          12         14            35        14-18
+//   65,536                20            52          12         20            53        16-19
+//
+// The new table's entries cost the same either way: 1024 children of one request, 16.8 million of them, 25 us and 28.
 
-constexpr uint32_t ONE_REQUESTS = BLOCKS_THREADS, ONE_BLOCKS = 32 * BLOCKS_THREADS, ONE_CELLS = 65536, ONE_MOST_GROUPS = 64;
+constexpr uint32_t ONE_REQUESTS = BLOCKS_THREADS, ONE_BLOCKS = 32 * BLOCKS_THREADS, ONE_MOST_GROUPS = 64, FORK_CELLS = 16384, COMPACT_CELLS = 32768;
 
 struct OneLds {
   uint32_t marks[BLOCKS_THREADS], marks_too[BLOCKS_THREADS], pages[ONE_REQUESTS], scan[BLOCKS_THREADS / WAVE];
