@@ -146,8 +146,8 @@ class Service:
         return logits
 
     def tokens(self, tokens: torch.Tensor) -> torch.Tensor:
-        """What goes in for tokens, [n, hidden]: of a size that leaves the next token open."""
-        return self.w_tokens.t()[tokens.long()] * 4
+        """What goes in for tokens, [n, hidden]: of a size that leaves the next token open.  A negative token is none, and zeros go in."""
+        return torch.where(tokens[:, None] < 0, 0, self.w_tokens.t()[tokens.clamp(min=0).long()] * 4)
 
     def score(self, record, logits: torch.Tensor, n_top: int, tokens: Optional[torch.Tensor] = None) -> binding.TokenScores:
         return record("score", (logits.shape[0], 1, 1), binding.fikit_token_scores, logits, tokens, self.status, n_top=n_top)
@@ -190,29 +190,43 @@ class Service:
 
 
 class Beams:
-    """Beam search: every request is continued by the `width` most probable of its beams' alternatives."""
+    """Beam search: every request is continued by the `width` most probable of its beams' alternatives.  Where less are left, the other beams are
+    empty requests: of token -1, minus infinity for a log probability and no parent."""
+
+    MOST = 32                  # alternatives that a score lists
 
     def __init__(self, service: Service, record, logits: torch.Tensor, width: int):
         """logits: [requests, vocabulary] behind the prompts."""
+        if not 1 <= width <= min(self.MOST, logits.shape[1]):
+            raise ValueError(f"width: from 1 to {self.MOST} and no more than tokens")
         self.service, self.width = service, width
-        top = service.score(record, logits, width)
+        top = self._alternatives(record, logits)
         n = logits.shape[0]
-        service.fork(record, torch.arange(n, dtype=torch.int32, device=logits.device).repeat_interleave(width))
-        self.tokens, self.logprob = top.top_tokens.reshape(-1), top.top_logprob.reshape(-1)
+        self._continue(record, top.top_logprob.reshape(-1), top.top_tokens.reshape(-1), torch.arange(n, device=logits.device).repeat_interleave(width))
+
+    def _alternatives(self, record, logits: torch.Tensor) -> binding.TokenScores:
+        top = self.service.score(record, logits, self.width)
+        if bool(top.top_logprob.isnan().any()):            # (they would be sorted in front of those that are)
+            raise FloatingPointError("logits that are not numbers, or infinite")
+        return top
+
+    def _continue(self, record, logprob, tokens, parents) -> torch.Tensor:
+        none = logprob == -math.inf
+        parents = torch.where(none, -1, parents).to(torch.int32)
+        self.service.fork(record, parents)
+        self.tokens, self.logprob = torch.where(none, -1, tokens), logprob
+        return parents
 
     def step(self, record) -> torch.Tensor:
         """One more token for each beam; returns the parents, by the beams before."""
         width = self.width
         logits = self.service.step(record, self.service.tokens(self.tokens))
-        top = self.service.score(record, logits, width)
+        top = self._alternatives(record, logits)
         # a request's width x width continuations, of which width are kept
         all_of = (self.logprob[:, None] + top.top_logprob).reshape(-1, width * width)
-        self.logprob, best = (t.reshape(-1) for t in torch.topk(all_of, width, 1))
+        logprob, best = (t.reshape(-1) for t in torch.topk(all_of, width, 1))
         request = torch.arange(all_of.shape[0], device=best.device).repeat_interleave(width)
-        self.tokens = top.top_tokens.reshape(-1)[request * width * width + best]
-        parents = (request * width + best // width).to(torch.int32)
-        self.service.fork(record, parents)
-        return parents
+        return self._continue(record, logprob, top.top_tokens.reshape(-1)[request * width * width + best], request * width + best // width)
 
 
 def measure(sizes: Sizes = Sizes(), requests: int = 32, longest_prompt: int = 256, steps: int = 20, host_ms: float = 0.5, seed: int = 0,
@@ -254,8 +268,10 @@ def main(argv=None) -> None:
     p.add_argument("--steps", type=int, default=20)
     p.add_argument("--host-ms", type=float, default=0.5, help="the host's time between two steps")
     p.add_argument("--rotary", type=int, default=0, help="dimensions of a head that are rotated by position; 0: no norm and no rotation")
-    p.add_argument("--beams", type=int, default=1, help="beams of a request")
+    p.add_argument("--beams", type=int, default=1, help=f"beams of a request, up to {Beams.MOST}")
     a = p.parse_args(argv)
+    if not 1 <= a.beams <= Beams.MOST:
+        p.error(f"--beams: from 1 to {Beams.MOST}")
     (decode, names), (prompts, _), _, _ = measure(Sizes(layers=a.layers, rotary=a.rotary), a.requests, a.longest_prompt, a.steps, a.host_ms, beams=a.beams)
     decode["run"] = 0                                   # one trace: the idle times between steps are what is filled
     rec = np.concatenate([decode, prompts])

@@ -70,3 +70,62 @@ def test_a_fork_to_nothing_leaves_no_tokens():
     assert s.lengths.tolist() == [2, 3, 4]
     s.fork(calls, parents())
     assert s.longest == 0 and s.lengths.numel() == 0
+
+
+def search(width, first, lengths=(4, 5)):
+    s, calls = begun(lengths)
+    calls.tops.append(first)
+    return service.Beams(s, calls, torch.zeros((len(lengths), SIZES.vocabulary)), width), s, calls
+
+
+@pytest.mark.parametrize("width", [0, -1, 17, 33])
+def test_more_beams_than_alternatives_are_refused(width):
+    """At most as many as tokens, and as a score lists."""
+    s, calls = begun()
+    with pytest.raises(ValueError):
+        service.Beams(s, calls, torch.zeros((2, SIZES.vocabulary)), width)
+    wide = service.Service(SIZES._replace(vocabulary=100), 2, 64, device="cpu")
+    with pytest.raises(ValueError):
+        service.Beams(wide, calls, torch.zeros((2, 100)), 33)
+    assert calls.parents == [] and s.lengths.tolist() == [40, 5]
+
+
+def test_the_command_refuses_more_beams_than_alternatives(capsys):
+    for beams in ("0", "33"):
+        with pytest.raises(SystemExit):
+            service.main(["--beams", beams])
+        assert "--beams" in capsys.readouterr().err
+
+
+def test_alternatives_that_are_none_have_no_request():
+    """A row with less than `width` tokens left: its other beams are empty requests, which nothing continues."""
+    none = -math.inf
+    beams, s, calls = search(2, ([[7, 3], [9, -1]], [[-0.5, -1.0], [0.0, none]]))
+    assert calls.parents == [[0, 0, 1, -1]] and s.lengths.tolist() == [4, 4, 5, 0]
+    # the empty request's own alternatives do not count, whatever they are; request 1 has one beam of two alternatives
+    calls.tops.append(([[1, 2], [3, 4], [5, 6], [8, 7]], [[-0.1, -9.0], [-9.0, -9.0], [-0.2, -0.3], [-0.1, -0.1]]))
+    assert beams.step(calls).tolist() == [0, 0, 2, 2] == calls.parents[-1]
+    assert beams.tokens.tolist() == [1, 2, 5, 6] and torch.allclose(beams.logprob, torch.tensor([-0.6, -9.5, -0.2, -0.3]))
+    # nothing is left of request 0 but one
+    calls.tops.append(([[-1, -1], [2, -1], [5, 6], [8, 7]], [[none, none], [-0.1, none], [-0.2, -0.3], [-0.01, -0.02]]))
+    assert beams.step(calls).tolist() == [1, -1, 3, 3] == calls.parents[-1]
+    assert beams.tokens.tolist() == [2, -1, 8, 7] and float(beams.logprob[1]) == none and int(s.lengths[1]) == 0
+
+
+def test_no_token_puts_in_zeros():
+    s, _ = begun()
+    x = s.tokens(torch.tensor([3, -1, 15], dtype=torch.int32))
+    assert not bool(x[1].any()) and torch.equal(x[0], s.w_tokens[:, 3] * 4) and torch.equal(x[2], s.w_tokens[:, 15] * 4)
+
+
+def test_scores_that_are_not_numbers_are_an_error():
+    """They would be sorted in front of those that are, and nothing else tells of them."""
+    nan = math.nan
+    with pytest.raises(FloatingPointError):
+        search(2, ([[7, 3], [-1, -1]], [[-0.5, -1.0], [nan, nan]]))
+    beams, s, calls = search(2, ([[7, 3], [9, 2]], [[-0.5, -1.0], [0.0, -1.0]]))
+    before, table = (beams.tokens.tolist(), beams.logprob.tolist()), s.table
+    calls.tops.append(([[1, 2], [-1, -1], [5, 6], [8, 7]], [[-0.1, -9.0], [nan, nan], [-0.2, -0.3], [-0.1, -0.1]]))
+    with pytest.raises(FloatingPointError):
+        beams.step(calls)
+    assert (beams.tokens.tolist(), beams.logprob.tolist()) == before and s.table is table and len(calls.parents) == 1
