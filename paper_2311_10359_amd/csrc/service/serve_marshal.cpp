@@ -9,6 +9,7 @@
 
 #include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/AutogradState.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/python_numbers.h>
@@ -64,9 +65,11 @@ int32_t value_type(const at::Tensor& t, const char* what) {
   return t.scalar_type() == at::kBFloat16 ? FIKIT_BF16 : FIKIT_F16;
 }
 
-// (For inference only: an output that silently had no gradient would be wrong.)
+// (For inference only: an output that silently had no gradient, or no tangent in forward mode, would be wrong.)
 void without_gradient(const at::Tensor& t, const char* what) {
   TORCH_CHECK_VALUE(!(t.requires_grad() && at::GradMode::is_enabled()), what, ": requires a gradient, and there is no backward pass; detach it or use no_grad()");
+  TORCH_CHECK_VALUE(!(t._fw_grad(0).defined() && c10::AutogradState::get_tls_state().get_fw_grad_mode()), what,
+                    ": has a tangent, and there is no forward mode; unpack it");
 }
 
 // [tokens, heads, head_dim] with the last dimension dense.
