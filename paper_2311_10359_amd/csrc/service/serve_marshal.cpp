@@ -220,7 +220,9 @@ void given_out(const at::Tensor& q, PyObject* given, at::Tensor* out, at::Tensor
   *out = tensor(PyTuple_GET_ITEM(given, 0), "out");
   *lse = given_or_none(PyTuple_GET_ITEM(given, 1), "lse");
   TORCH_CHECK_VALUE(out->sizes() == q.sizes(), "out: the shape of q");
+  without_gradient(*out, "out");
   TORCH_CHECK_VALUE(!lse->defined() || (lse->dim() == 2 && lse->size(0) == q.size(0) && lse->size(1) == q.size(1)), "lse: [rows, q heads]");
+  if (lse->defined()) without_gradient(*lse, "lse");
 }
 
 // New ones, if none are.
@@ -547,6 +549,8 @@ PyObject* py_token_scores(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     top_logprob = given_or_none(PyTuple_GET_ITEM(a[5], 4), "top_logprob");
     for (const at::Tensor* t : {&logprob, &entropy, &lse}) TORCH_CHECK_VALUE(!t->defined() || t->numel() == rows, "out: [rows]");
     const int64_t tops = static_cast<int64_t>(rows) * n_top;
+    for (const at::Tensor* t : {&logprob, &entropy, &lse, &top_logprob})
+      if (t->defined()) without_gradient(*t, "out");
     for (const at::Tensor* t : {&top_tokens, &top_logprob}) TORCH_CHECK_VALUE(t->defined() ? t->numel() == tops : n_top == 0, "out: [rows, n_top]");
   }
   const at::Tensor workspace = given_or_none(a[6], "workspace_buf");

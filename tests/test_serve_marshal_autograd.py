@@ -1,10 +1,13 @@
-"""What the marshalling of a service's calls owes to torch's bookkeeping of gradients, without a GPU: tangents of forward mode."""
+"""What the marshalling of a service's calls owes to torch's bookkeeping of gradients, without a GPU: tangents, outputs, versions."""
 import pytest
 import torch
 import torch.autograd.forward_ad as forward_ad
 
 from paper_2311_10359_amd import binding
-from test_serve_marshal import append, decode, i32, marshal, nothing, prompt, vectors  # noqa: F401
+from test_serve_marshal import address, append, cache, decode, i32, marshal, nothing, prompt, vectors  # noqa: F401
+
+AROUND = ("fikit_rotate_heads", "fikit_cache_fork_workspace_bytes", "fikit_cache_fork", "fikit_cache_compact_workspace_bytes", "fikit_cache_compact",
+          "fikit_cache_copy", "fikit_token_scores_workspace_bytes", "fikit_token_scores")
 
 
 def scores(logits):
@@ -43,3 +46,50 @@ def test_gradients_that_are_off_do_not_hide_a_tangent(marshal):  # noqa: F811
             decode(native, q=x)
         with torch.inference_mode():                   # (and not in this)
             decode(native, q=x)
+
+
+@pytest.fixture
+def replaced(marshal):  # noqa: F811
+    """The module, with a C function in the place of all that enqueue."""
+    def replace(f):
+        native = marshal(f)
+        native.bind_around(*(address(getattr(binding.load(), name) if "bytes" in name else f) for name in AROUND))
+        return native
+    return replace
+
+
+def outputs(floating):
+    """Calls into given outputs: (name, function of the module and outputs, those outputs)."""
+    x, table, codes = vectors(), i32(3, 2), cache()
+    flat = [torch.zeros(3), torch.zeros(3), torch.zeros(3), i32(3, 2), torch.zeros(3, 2)]
+    tensors = [
+        ("decode", lambda n, o: n.cache_attention(*codes, x, table, i32(3), 0.1, i32(1), None, True, tuple(o), None, 0), [vectors(), torch.zeros(3, 2)]),
+        ("prompt", lambda n, o: n.prompt_attention(x, x, x, i32(2), 0.1, i32(1), True, tuple(o), 0), [vectors(), torch.zeros(3, 2)]),
+        ("rotate", lambda n, o: n.rotate_heads(x, x, i32(3), None, i32(1), None, None, 1e-6, False, tuple(o), 0), [vectors(), vectors()]),
+        ("scores", lambda n, o: n.token_scores(torch.zeros(3, 10), i32(3), i32(1), 1.0, 2, tuple(o), None, 0), flat)]
+    if floating:
+        return tensors
+    return tensors + [
+        ("plan", lambda n, o: n.cache_plan(i32(3), i32(3), 5, 16, o[0], i32(6), i32(1), True, tuple(o[1:]), None, 0),
+         [i32(3, 4), i32(3), i32(4), torch.zeros(5, dtype=torch.int64), i32(binding.fikit_cache_pieces(5, 3, 16), 4), i32(2)]),
+        ("append", lambda n, o: n.cache_append(*o, x, x, i32(2, 4), i32(1), 0), list(cache())),
+        ("fork", lambda n, o: n.cache_fork(table, i32(3), i32(5), 16, 9, i32(4), i32(1), tuple(o), None, 0), [i32(5, 2), i32(5), i32(5, 2), i32(9), i32(3)]),
+        ("compact", lambda n, o: n.cache_compact(table, i32(3), 16, 9, i32(4), i32(1), tuple(o), None, 0), [i32(3, 2), i32(4, 2), i32(4), i32(2)]),
+        ("copy", lambda n, o: n.cache_copy([o[:4], o[4:]], i32(2, 2), i32(1), 0), [*cache(), *cache()])]
+
+
+def test_outputs_that_require_gradients_are_refused(replaced):
+    """They would be written without a trace of where their values come from."""
+    native = replaced(nothing)
+    for name, call, out in outputs(floating=True):
+        for i, t in enumerate(out):
+            if t.is_floating_point():
+                changed = list(out)
+                changed[i] = t.clone().requires_grad_()
+                with pytest.raises(ValueError, match="no_grad"):
+                    call(native, changed)
+                with torch.no_grad():
+                    call(native, changed)
+                with forward_ad.dual_level(), pytest.raises(ValueError, match="tangent"):
+                    changed[i] = forward_ad.make_dual(t.clone(), torch.ones_like(t))
+                    call(native, changed)
