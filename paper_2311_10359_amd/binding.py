@@ -591,7 +591,8 @@ def fikit_profile_merge(rows_a: torch.Tensor, task_row_offsets_a: torch.Tensor, 
 # ---- tasks of a language model service -----------------------------------------------------------
 # These calls enqueue their kernels and return; errors that depend on data are left in `status`, an int32 [1] device tensor
 # that starts as zero and that fikit_check_status looks at.  Tensors that a call allocates belong to the stream it runs on.
-# For inference only: inputs that require gradients are a ValueError unless gradients are off.
+# For inference only: inputs and given outputs that require gradients, or have a tangent in forward mode, are a ValueError unless
+# gradients are off.  Tensors that a call writes in place count up their version, as after any operation in place.
 
 
 def _outputs(kind, got, what: str):

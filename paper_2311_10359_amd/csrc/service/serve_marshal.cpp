@@ -14,6 +14,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/python_numbers.h>
 
+#include <initializer_list>
 #include <vector>
 
 #include "fikit.h"
@@ -130,6 +131,14 @@ PyObject* wrapped(const at::Tensor& t) {
   return THPVariable_Wrap(t);
 }
 
+// What a call has written in place: autograd, if it has saved one of these tensors, has to know.  (An inference tensor has no version; the status word and
+// the workspace are the calls' own.)
+void written(int rc, std::initializer_list<const at::Tensor*> tensors) {
+  if (rc != FIKIT_OK && rc != FIKIT_HIP_ERROR) return;         // refused
+  for (const at::Tensor* t : tensors)
+    if (t->defined() && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
+
 void need_arguments(Py_ssize_t n, Py_ssize_t want) { TORCH_CHECK_VALUE(n == want, "takes ", want, " arguments"); }
 
 // cached, added, n_tokens, block_tokens, block_table, free_blocks, status, want_slots, out, workspace_buf, stream
@@ -182,6 +191,8 @@ PyObject* py_cache_plan(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                     dense<int32_t>(status, at::kInt, device, "status"), ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? ws.numel() : 0,
                     stream);
   }
+  written(rc, {&table});
+  if (!allocate) written(rc, {&lengths, &offsets, &slots, &pieces, &counts});
   if (rc != FIKIT_OK) return PyLong_FromLong(rc);
   if (!allocate) {
     Py_INCREF(a[8]);
@@ -209,6 +220,7 @@ PyObject* py_cache_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     rc = cache_append(&cache, &kv, &vv, count(k.size(0), "tokens"), type, dense<fikit_piece>(pieces, at::kInt, device, "pieces"),
                       static_cast<uint64_t>(pieces.size(0)), dense<int32_t>(status, at::kInt, device, "status"), stream);
   }
+  for (int i = 0; i < 4; ++i) written(rc, {&THPVariable_Unpack(a[i])});
   return PyLong_FromLong(rc);
   END_HANDLE_TH_ERRORS
 }
@@ -233,6 +245,7 @@ void new_out(const at::Tensor& q, bool want_lse, at::Tensor* out, at::Tensor* ls
 }
 
 PyObject* attention_result(int rc, PyObject* given, const at::Tensor& out, const at::Tensor& lse) {
+  if (given != Py_None) written(rc, {&out, &lse});
   if (rc != FIKIT_OK) return PyLong_FromLong(rc);
   if (given != Py_None) {
     Py_INCREF(given);
@@ -365,6 +378,7 @@ PyObject* py_rotate_heads(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                       frequencies.defined() ? count(2 * frequencies.numel(), "frequencies") : 0, neighbours ? FIKIT_PAIRS_NEIGHBOURS : FIKIT_PAIRS_HALVES,
                       count(any.size(0), "tokens"), &out[0], &out[1], dense<int32_t>(status, at::kInt, device, "status"), stream);
   }
+  if (a[9] != Py_None) written(rc, {&q_out, &k_out});
   if (rc != FIKIT_OK) return PyLong_FromLong(rc);
   if (a[9] != Py_None) {
     Py_INCREF(a[9]);
@@ -434,6 +448,7 @@ PyObject* py_cache_fork(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                     dense<int32_t>(counts, at::kInt, device, "out"), dense<int32_t>(status, at::kInt, device, "status"),
                     ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? ws.numel() : 0, stream);
   }
+  if (!allocate) written(rc, {&new_table, &new_lengths, &copies, &new_free, &counts});
   if (rc != FIKIT_OK) return PyLong_FromLong(rc);
   if (!allocate) {
     Py_INCREF(a[7]);
@@ -479,6 +494,7 @@ PyObject* py_cache_compact(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                        dense<int32_t>(counts, at::kInt, device, "out"), dense<int32_t>(status, at::kInt, device, "status"),
                        ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? ws.numel() : 0, stream);
   }
+  if (!allocate) written(rc, {&new_table, &copies, &new_free, &counts});
   if (rc != FIKIT_OK) return PyLong_FromLong(rc);
   if (!allocate) {
     Py_INCREF(a[6]);
@@ -520,6 +536,8 @@ PyObject* py_cache_copy(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     rc = cache_copy(caches.data(), count(static_cast<int64_t>(caches.size()), "caches"), dense<fikit_block_copy>(copies, at::kInt, device, "copies"),
                     count(copies.size(0), "copies"), dense<int32_t>(status, at::kInt, device, "status"), stream);
   }
+  for (const Owned& one : held)
+    for (int i = 0; i < 4; ++i) written(rc, {&THPVariable_Unpack(PyTuple_GET_ITEM(one.o, i))});
   return PyLong_FromLong(rc);
   END_HANDLE_TH_ERRORS
 }
@@ -574,6 +592,7 @@ PyObject* py_token_scores(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                       top_tokens.defined() ? dense<int32_t>(top_tokens, at::kInt, device, "out") : nullptr, floats(top_logprob),
                       dense<int32_t>(status, at::kInt, device, "status"), ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? ws.numel() : 0, stream);
   }
+  if (!allocate) written(rc, {&logprob, &entropy, &lse, &top_tokens, &top_logprob});
   if (rc != FIKIT_OK) return PyLong_FromLong(rc);
   if (!allocate) {
     Py_INCREF(a[5]);

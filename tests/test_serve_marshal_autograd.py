@@ -1,4 +1,6 @@
 """What the marshalling of a service's calls owes to torch's bookkeeping of gradients, without a GPU: tangents, outputs, versions."""
+import ctypes
+
 import pytest
 import torch
 import torch.autograd.forward_ad as forward_ad
@@ -93,3 +95,60 @@ def test_outputs_that_require_gradients_are_refused(replaced):
                 with forward_ad.dual_level(), pytest.raises(ValueError, match="tangent"):
                     changed[i] = forward_ad.make_dual(t.clone(), torch.ones_like(t))
                     call(native, changed)
+
+
+def test_what_is_written_in_place_has_another_version(replaced):
+    """... each tensor that a call writes, none that it reads; of its own outputs a call needs none."""
+    native = replaced(nothing)
+    for name, call, out in outputs(floating=False):
+        before = [t._version for t in out]
+        call(native, out)
+        assert all(t._version > v for t, v in zip(out, before)), name
+    x, logits = vectors(), torch.zeros(3, 10)
+    native.rotate_heads(x, x, i32(3), None, i32(1), None, None, 1e-6, False, None, 0)
+    prompt(native, q=x)
+    native.token_scores(logits, None, i32(1), 1.0, 0, None, None, 0)
+    assert x._version == 0 and logits._version == 0
+    native.rotate_heads(x, None, i32(3), None, i32(1), None, None, 1e-6, False, (x, None), 0)
+    assert x._version == 1
+
+
+def test_outputs_of_a_call_go_into_the_next(replaced):
+    """They are parts of one piece of memory."""
+    native, logits = replaced(nothing), torch.zeros(3, 10)
+    for mode in (torch.enable_grad, torch.inference_mode):
+        with mode():
+            out = native.token_scores(logits, i32(3), i32(1), 1.0, 2, None, None, 0)
+            native.token_scores(logits, i32(3), i32(1), 1.0, 2, out, None, 0)
+        assert all(t.is_inference() or t._version == 1 for t in out) and all(t.is_inference() == (mode is torch.inference_mode) for t in out)
+        native.token_scores(logits, i32(3), i32(1), 1.0, 2, out, None, 0)
+
+
+def test_what_a_refused_call_has_not_written_keeps_its_version(replaced):
+    @ctypes.CFUNCTYPE(ctypes.c_int)
+    def refused():
+        return binding.FIKIT_INVALID_ARG
+    native = replaced(refused)
+    for name, call, out in outputs(floating=False):
+        assert call(native, out) == binding.FIKIT_INVALID_ARG and all(t._version == 0 for t in out), name
+
+
+def test_a_backward_pass_notices(replaced):
+    """Heads that a product has saved are rotated in place: its backward pass would use other values."""
+    native = replaced(nothing)
+    q, w = vectors().float(), torch.ones(64, requires_grad=True)
+    heads = q.to(torch.bfloat16)
+    y = (heads * w).sum()
+    native.rotate_heads(heads[:, :1], None, i32(3), None, i32(1), None, None, 1e-6, False, (heads[:, :1], None), 0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+
+
+def test_inference_tensors_have_no_version(replaced):
+    native = replaced(nothing)
+    with torch.inference_mode():
+        made = outputs(floating=False)
+        for _, call, out in made:
+            call(native, out)
+    for _, call, out in made:
+        call(native, out)
