@@ -172,8 +172,10 @@ __device__ __forceinline__ void each_page(const int32_t* entries, uint32_t pages
 // ---- fork -------------------------------------------------------------------------------------------------------
 //
 // Child i continues request parents[i].  The first child keeps the parent's last block if that is not full, each later one needs a block:
-// its place among those is a prefix sum over the children.  8192 children of 4096 requests over 107,000 blocks: 18 us in four launches.  Blocks to take come from the front of (free blocks, blocks given back in
+// its place among those is a prefix sum over the children.  Blocks to take come from the front of (free blocks, blocks given back in
 // ascending order); what is left of the two is the new list.  The kernels of both calls load what they may before they look at the status.
+//
+// 8192 children of 4096 requests over 107,000 blocks: 17 to 19 us in four launches, of which marks of the free blocks, to refuse those in use, take 0.4.
 
 // The children, in one workgroup, PER requests and children to a thread, whose loads are on their way at once; the others clear the bitmaps.  (8192 children
 // 6.0 us, 1500 4.0; with code for 16,384, which is fetched although no thread has work in it, 7.8 and 6.9.)
@@ -322,7 +324,7 @@ __global__ __launch_bounds__(ROW_WAVES * WAVE) void k_fork_end(BlocksArgs a) {
 //
 // Up to ONE_REQUESTS requests and children, ONE_BLOCKS blocks and FORK_CELLS or COMPACT_CELLS entries of the table, with bitmaps in LDS: every workgroup marks all
 // blocks for itself and writes its share of the outputs, so that none waits for another.  A fork has one more, which marks the free blocks too and alone says
-// what is wrong, so that the others neither read all of that list nor find different errors.  128 beams of 32 prompts 6.0 us, their compaction 6.0; in the launches
+// what is wrong, so that the others neither read all of that list nor find different errors.  128 beams of 32 prompts 6.1 us, their compaction 5.9; in the launches
 // that larger sizes take, 13 and 16.
 //
 // The marks that every workgroup makes bound it, and with them the entries that are read.  Calls of 128 requests whose rows are full, of scattered blocks and of

@@ -21,7 +21,7 @@ namespace fikit {
 //
 // V * bytes are read: bound by memory, if a logit takes few instructions: one to unpack, one for maximum and minimum, four for d, S and T, and the
 // exponential.  2999 rows of 100,003 bfloat16 logits, 600 MB: 98 us without alternatives, 6.1 TB/s, 108 to 113 with 20, the vector unit busy for 84 % of
-// it.  A workgroup's waves take batches in turn, past the caches (a stretch for each wave 113 us, through the caches 111, both without alternatives), and
+// it.  A workgroup's waves take batches in turn, past the caches (without alternatives 100 us when that was tried, a stretch for each wave 113, through the caches 111), and
 // 4 groups a lane in a batch (8 are 6 us more: half the waves).
 
 struct ScoresArgs {
